@@ -60,12 +60,14 @@ enum cast_status {
     CAST_ERR_NM     = -4,   /* unsupported N:M, or index-form metadata asked for N:M != 2:4 */
     CAST_ERR_HYPER  = -5,   /* hyper-parameter out of range (see cast_adams_step)           */
     CAST_ERR_CUDA   = -6,   /* a CUDA runtime call failed; see cast_last_cuda_error()       */
-    CAST_ERR_PLAN   = -7,   /* invalid plan / context handle, or it is too small            */
+    CAST_ERR_PLAN   = -7,   /* invalid plan / context handle, or it (or a workspace) is too small */
     CAST_ERR_ALIAS  = -8,   /* two buffers of one matrix overlap                            */
     CAST_ERR_MEMORY = -9,   /* a pointer is not of the required kind (device / host)        */
     CAST_ERR_STAGING = -10  /* an earlier step of this plan gave up waiting for one of its bulk
                                copies (see CAST_F_BULK_STAGING): a tile of the state was left as it
-                               was; the plan refuses further steps                            */
+                               was; the plan refuses further steps.  Also: an earlier tensor-core product
+                               (cast_linear_ce, cast_orthogonalize) gave up a wait; its results are
+                               incomplete, and both calls refuse from then on                 */
 };
 
 enum cast_flags {
@@ -440,6 +442,84 @@ CAST_API int cast_host_step_static(float* w, float* m, float* v, const cast_bf16
                    int64_t step, int64_t total_steps,
                    uint32_t flags, unsigned long long* flip_count,
                    cast_stream_t stream);
+
+/*
+ * The ends of a language model around its pruned matrices, and an optimizer for the hidden matrices that are not
+ * pruned.  (The paper has no counterpart to these entry points; they complete a training step.)
+ *
+ * Shared conventions: arrays are contiguous and row-major; an id or label outside [0, vocab) means "none".  A call that
+ * needs a workspace takes one of at least the size its *_workspace function names (device memory, 16-byte aligned,
+ * contents need not be kept; CAST_ERR_PLAN if it is too small); calls that run at the same time need separate ones.
+ * Results do not depend on the order in which CTAs run: repeated calls give the same bits.
+ */
+
+/*
+ * cast_embed -- out[t] = scale * table[ids[t]], a zero row for no id.  Asynchronous on `stream`.
+ *
+ *   table   device, bf16 [vocab][dim].      ids   device, int32 [tokens].      out   device, bf16 [tokens][dim].
+ * dim % 8 == 0 with 16-byte aligned buffers takes the vector path, anything else a slower scalar one.  Values are
+ * bf16(scale * entry), round to nearest even.  scale finite.
+ */
+CAST_API int cast_embed(const cast_bf16* table, const int32_t* ids, cast_bf16* out, int64_t tokens, int64_t vocab, int64_t dim,
+               float scale, cast_stream_t stream);
+
+/*
+ * cast_embed_grad -- grad_table[v] = scale * sum over {t: ids[t] = v} of grad_out[t]: the gradient of cast_embed with respect
+ * to the table.  The tokens are sorted by id first; a row's tokens are summed in fp32 in their order and rounded once.
+ *
+ *   grad_out     device, bf16 [tokens][dim].   ids   device, int32 [tokens].
+ *   grad_table   device, bf16 [vocab][dim], out.  accumulate == 0: every row is written, zeros where no token is.
+ *                accumulate != 0: the sums are added to what is there (in fp32, one rounding) and rows without a token
+ *                are not touched, e.g. onto the head's gradient where embedding and head share one matrix.
+ */
+CAST_API int cast_embed_grad_workspace(int64_t tokens, int64_t dim, uint64_t* bytes);
+CAST_API int cast_embed_grad(const cast_bf16* grad_out, const int32_t* ids, cast_bf16* grad_table, int64_t tokens, int64_t vocab,
+                    int64_t dim, float scale, int accumulate, void* workspace, uint64_t workspace_bytes, cast_stream_t stream);
+
+/*
+ * cast_linear_ce -- softmax cross entropy of a linear head and its gradients, without the logits in memory.  With
+ * l = hidden weight^T and p the softmax of each row of l:
+ *
+ *     loss[i]     = logsumexp(l[i]) - l[i][labels[i]]                     (0 for a token without a label)
+ *     grad_hidden = dl weight,   grad_weight = dl^T hidden,   dl[i] = grad_scale (p[i] - onehot(labels[i]))   (0 likewise)
+ *
+ *   hidden        device, bf16 [tokens][dim].        weight   device, bf16 [vocab][dim].
+ *   labels        device, int32 [tokens].            loss     device, fp32 [tokens], out.
+ *   grad_hidden   device, bf16 [tokens][dim], out, or NULL.    grad_weight   device, bf16 [vocab][dim], out, or NULL.
+ *                 Without either, only the loss is computed (scoring).
+ *   grad_scale    finite; carries the reduction (1/tokens for a mean) and any loss scaling.
+ *   piece_tokens  tokens whose exponentials (bf16 [piece][vocab]) are held at a time; 0 = as many as fit 1 GiB.  With more
+ *                 than one piece, grad_weight is accumulated in fp32 in the workspace.
+ *   dim % 8 == 0; hidden, weight, grad_hidden, grad_weight and workspace 16-byte aligned.
+ * The products take bf16 operands and accumulate in fp32; the loss and all statistics are fp32.  The workspace size depends
+ * on the device.  The first call of a process allocates one word of page-locked host memory: make it outside any
+ * stream capture.
+ */
+CAST_API int cast_linear_ce_workspace(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece_tokens, int want_hidden_grad,
+                             int want_weight_grad, uint64_t* bytes);
+CAST_API int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, const int32_t* labels, float* loss,
+                   cast_bf16* grad_hidden, cast_bf16* grad_weight, int64_t tokens, int64_t vocab, int64_t dim,
+                   float grad_scale, int64_t piece_tokens, void* workspace, uint64_t workspace_bytes, cast_stream_t stream);
+
+/*
+ * cast_orthogonalize -- Newton-Schulz orthogonalisation of `n` updates of the same shape:
+ *
+ *     X = U / (|U|_F + eps);   steps times   X <- a X + (b A + c A A) X,  A = X X^T;   out = scale * X
+ *
+ * (X <- a X + X (b A + c A A) with A = X^T X where rows > cols: the same result from smaller products.)
+ *
+ *   updates       host array of n device pointers: fp32 [rows][cols], or bf16 where updates_bf16 != 0.  Not changed.
+ *   out           host array of n device pointers: bf16 [rows][cols].  No result may overlap an update or another result.
+ *   coeffs        host, [steps][3]: a, b, c of every step, or NULL for (3.4445, -4.7750, 2.0315) in all of them.  They must
+ *                 keep the singular values of X below about 8 (those do: below 1.3).
+ *   steps in [1, 100]; eps >= 0; scale finite.  A zero update gives a zero result.
+ * rows*cols < 2^31.  The matrices are worked on together, as many at a time as make 64 M entries.
+ * Products take fp16 operands (X scaled by 2^12) and accumulate in fp32; X itself is held in 22 bits.
+ */
+CAST_API int cast_orthogonalize_workspace(int n, int64_t rows, int64_t cols, uint64_t* bytes);
+CAST_API int cast_orthogonalize(const void* const* updates, int updates_bf16, cast_bf16* const* out, int n, int64_t rows, int64_t cols,
+                       const float* coeffs, int steps, float eps, float scale, void* workspace, uint64_t workspace_bytes,
+                       cast_stream_t stream);
 
 /*
  * Measurement aids.  Neither computes anything of the method (the paper has no counterpart); a benchmark puts their

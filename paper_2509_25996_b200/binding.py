@@ -44,6 +44,8 @@ EXPORTS = (
     "cast_plan_create", "cast_plan_create_ex", "cast_plan_step", "cast_plan_step_stats", "cast_plan_destroy", "cast_plan_report_staging_failure",
     "cast_host_ctx_create", "cast_host_step", "cast_host_ctx_sync", "cast_host_ctx_destroy",
     "cast_host_step_static", "cast_kd_loss", "cast_prune_fold", "cast_plan_prune_fold", "cast_mask_stats", "cast_plan_mask_stats",
+    "cast_embed", "cast_embed_grad", "cast_embed_grad_workspace", "cast_linear_ce", "cast_linear_ce_workspace",
+    "cast_orthogonalize", "cast_orthogonalize_workspace",
     "cast_probe_launch", "cast_probe_stream", "cast_bulk_timeout_count",
     "cast_strerror", "cast_last_cuda_error", "cast_kernel_launch_count",
 )
@@ -149,6 +151,25 @@ def load_library() -> ctypes.CDLL:
     lib.cast_probe_launch.argtypes = [ctypes.c_int64, ctypes.c_void_p]
     lib.cast_probe_stream.restype = ctypes.c_int
     lib.cast_probe_stream.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_int64, ctypes.c_void_p]
+    size_out = ctypes.POINTER(ctypes.c_uint64)
+    lib.cast_embed.restype = ctypes.c_int
+    lib.cast_embed.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int64] * 3 + [ctypes.c_float, ctypes.c_void_p]
+    lib.cast_embed_grad_workspace.restype = ctypes.c_int
+    lib.cast_embed_grad_workspace.argtypes = [ctypes.c_int64, ctypes.c_int64, size_out]
+    lib.cast_embed_grad.restype = ctypes.c_int
+    lib.cast_embed_grad.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int64] * 3 + [ctypes.c_float, ctypes.c_int, ctypes.c_void_p,
+                                                                                   ctypes.c_uint64, ctypes.c_void_p]
+    lib.cast_linear_ce_workspace.restype = ctypes.c_int
+    lib.cast_linear_ce_workspace.argtypes = [ctypes.c_int64] * 4 + [ctypes.c_int, ctypes.c_int, size_out]
+    lib.cast_linear_ce.restype = ctypes.c_int
+    lib.cast_linear_ce.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_int64] * 3 + [ctypes.c_float, ctypes.c_int64, ctypes.c_void_p,
+                                                                                  ctypes.c_uint64, ctypes.c_void_p]
+    lib.cast_orthogonalize_workspace.restype = ctypes.c_int
+    lib.cast_orthogonalize_workspace.argtypes = [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, size_out]
+    lib.cast_orthogonalize.restype = ctypes.c_int
+    lib.cast_orthogonalize.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int, ctypes.POINTER(ctypes.c_void_p), ctypes.c_int,
+                                       ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_float,
+                                       ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
     lib.cast_host_ctx_sync.restype = ctypes.c_int
     lib.cast_host_ctx_sync.argtypes = [ctypes.c_void_p]
     lib.cast_host_ctx_destroy.restype = ctypes.c_int
@@ -348,6 +369,53 @@ def cast_plan_mask_stats(plan, meta_refs, flags, stats, stream=None) -> int:
     if meta_refs is not None:
         arr = (ctypes.c_void_p * len(meta_refs))(*[_ptr(r) for r in meta_refs])
     return load_library().cast_plan_mask_stats(plan, arr, int(flags), _ptr(stats), _stream(stream))
+
+
+def cast_embed(table, ids, out, tokens, vocab, dim, scale=1.0, stream=None) -> int:
+    return load_library().cast_embed(_ptr(table), _ptr(ids), _ptr(out), int(tokens), int(vocab), int(dim), scale, _stream(stream))
+
+
+def cast_embed_grad_workspace(tokens, dim):
+    """Returns (status, bytes)."""
+    out = ctypes.c_uint64(0)
+    rc = load_library().cast_embed_grad_workspace(int(tokens), int(dim), ctypes.byref(out))
+    return rc, out.value
+
+
+def cast_embed_grad(grad_out, ids, grad_table, tokens, vocab, dim, scale, accumulate, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().cast_embed_grad(_ptr(grad_out), _ptr(ids), _ptr(grad_table), int(tokens), int(vocab), int(dim), scale,
+                                          1 if accumulate else 0, _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def cast_linear_ce_workspace(tokens, vocab, dim, piece_tokens=0, want_hidden_grad=True, want_weight_grad=True):
+    """Returns (status, bytes)."""
+    out = ctypes.c_uint64(0)
+    rc = load_library().cast_linear_ce_workspace(int(tokens), int(vocab), int(dim), int(piece_tokens), 1 if want_hidden_grad else 0,
+                                                 1 if want_weight_grad else 0, ctypes.byref(out))
+    return rc, out.value
+
+
+def cast_linear_ce(hidden, weight, labels, loss, grad_hidden, grad_weight, tokens, vocab, dim, grad_scale, piece_tokens, workspace,
+                   workspace_bytes, stream=None) -> int:
+    return load_library().cast_linear_ce(_ptr(hidden), _ptr(weight), _ptr(labels), _ptr(loss), _ptr(grad_hidden), _ptr(grad_weight),
+                                         int(tokens), int(vocab), int(dim), grad_scale, int(piece_tokens), _ptr(workspace),
+                                         int(workspace_bytes), _stream(stream))
+
+
+def cast_orthogonalize_workspace(n, rows, cols):
+    """Returns (status, bytes)."""
+    out = ctypes.c_uint64(0)
+    rc = load_library().cast_orthogonalize_workspace(int(n), int(rows), int(cols), ctypes.byref(out))
+    return rc, out.value
+
+
+def cast_orthogonalize(updates, updates_bf16, outs, rows, cols, coeffs, steps, eps, scale, workspace, workspace_bytes, stream=None) -> int:
+    """`updates`, `outs`: sequences of one buffer per matrix; `coeffs`: a flat sequence of 3 * steps numbers, or None."""
+    pu = None if updates is None else (ctypes.c_void_p * len(updates))(*[_ptr(u) for u in updates])
+    po = None if outs is None else (ctypes.c_void_p * len(outs))(*[_ptr(o) for o in outs])
+    pc = None if coeffs is None else (ctypes.c_float * len(coeffs))(*coeffs)
+    return load_library().cast_orthogonalize(pu, 1 if updates_bf16 else 0, po, 0 if updates is None else len(updates), int(rows), int(cols),
+                                             pc, int(steps), eps, scale, _ptr(workspace), int(workspace_bytes), _stream(stream))
 
 
 def cast_bulk_timeout_count():

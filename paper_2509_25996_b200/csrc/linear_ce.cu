@@ -1,0 +1,699 @@
+// Softmax cross entropy of a linear head, l = hidden weight^T, without the logits in memory, and its gradients.
+//
+// With r_i = h_i . w_label(i) (the target logit) and S_i = sum_{j != label} e^(l_ij - r_i):
+//     loss_i = log(1 + S_i),   p_ij = e^(l_ij - r_i) / (1 + S_i),   1 - p_i,label = S_i / (1 + S_i)
+// so nothing cancels for a confident token, and a tile of logits needs no statistics of the rest of its row: the product's
+// epilogue turns the accumulators into E_ij = e^(l_ij - r_i) (0 at the label) and its row sums at once.  Per piece of tokens:
+//     target logits   r_i, one warp per token
+//     E = exp(H W^T - r)            product, epilogue writes E (bf16) and the row sums of its 256 (128) columns
+//     finish          S, loss, a_i = s / (1 + S_i), b_i = s S_i / (1 + S_i), and a H as bf16
+//     dH = a (E W) - b W_label      product over the vocabulary; the label's row is added in fp32 by the epilogue
+//     dW = E^T (a H)                product over the tokens
+//     dW_label -= b H               rows of the piece in label order (the embedding gradient's sums), added in fp32
+// The two backward products read E as it was written: no pass over it to apply the normaliser.
+//
+// E is the only large intermediate, 2 bytes per logit of a piece.  Several pieces accumulate dW in fp32.
+// Range: e^(l - r) beyond e^40 (a target that is that improbable) would leave the range of the later sums.  The epilogue
+// sees it in its row sum, forms that row's part of the tile relative to the tile's own maximum instead and says so by a negative
+// sum; finish then brings the row to one reference.
+//
+// Rounding: the products take bf16 operands, so E and a H are rounded to bf16 (2^-9 relative each); everything that is
+// summed, and all statistics, are fp32.  The label's terms, the largest of a row, are never rounded before the result is.
+#include <cmath>
+
+#include "embed.cuh"
+#include "tile_product.cuh"
+
+namespace cast {
+namespace {
+
+using namespace product;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kMostSum = 2.35e17f;        // e^40
+
+__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// ------------------------------------------------------------------------------------------------ target logits
+
+// refs[t] = h_t . w_label, 0 without a label.  One warp per token; dim % 8 == 0.
+__global__ void __launch_bounds__(256)
+target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restrict__ weight, const int32_t* __restrict__ labels,
+                    float* __restrict__ refs, int64_t tokens, int vocab, int dim)
+{
+    const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (t >= tokens) return;
+    const int lane = (int)threadIdx.x & 31;
+    const int label = labels[t];
+    float sum = 0.0f;
+    if ((unsigned)label < (unsigned)vocab) {
+        const uint4* h = reinterpret_cast<const uint4*>(hidden + t * dim);
+        const uint4* w = reinterpret_cast<const uint4*>(weight + (int64_t)label * dim);
+#pragma unroll 4
+        for (int i = lane; i < dim / 8; i += 32) {
+            const uint4 a = __ldg(h + i), b = __ldg(w + i);
+            sum += lo16(a.x) * lo16(b.x) + hi16(a.x) * hi16(b.x) + lo16(a.y) * lo16(b.y) + hi16(a.y) * hi16(b.y) +
+                   lo16(a.z) * lo16(b.z) + hi16(a.z) * hi16(b.z) + lo16(a.w) * lo16(b.w) + hi16(a.w) * hi16(b.w);
+        }
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    if (lane == 0) refs[t] = sum;
+}
+
+// ------------------------------------------------------------------------------------------------ E and its row sums
+
+struct ExpEpi {
+    static constexpr bool kSym = false;
+    CUtensorMap map_e;
+    const float* refs;           // target logits of the piece
+    const int32_t* labels;
+    float* sums;                 // [n_tiles][tokens]; negative: relative to `tops`
+    float* tops;                 // [n_tiles][tokens], base 2
+    int write_e;
+
+    // One pass over the accumulator row relative to ref2: returns the sum; writes E.
+    template <int BN>
+    __device__ __forceinline__ float pass(const Shape& s, EpiTile& e, float ref2, int label, bool active) const
+    {
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll 1
+        for (int c = 0; c < BN; c += 64) {
+            const int n = e.col0 + c;
+            if (n >= s.n) break;
+            uint32_t slot = 0;
+            if (write_e) slot = slot_acquire(e);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[32];
+                tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
+                const int n1 = n + 32 * h;
+                const bool special = !active || (unsigned)(label - n1) < 32u || n1 + 32 > s.n;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = ex2(fmaf(v[i], kLog2e, -ref2));
+                if (__any_sync(0xFFFFFFFFu, special)) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!active || n1 + i == label || n1 + i >= s.n) v[i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) { s0 += v[i]; s1 += v[i + 1]; }
+                if (write_e) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        slot_write(slot, e.lane, 4 * h + q, pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]),
+                                   pack2(v[8 * q + 4], v[8 * q + 5]), pack2(v[8 * q + 6], v[8 * q + 7]));
+                }
+            }
+            if (write_e) slot_store(e, slot, &map_e, n, e.row0, 0, e.row0 < s.m);
+        }
+        return s0 + s1;
+    }
+
+    template <int BN>
+    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    {
+        const int row = e.row0 + e.lane;
+        int label = -1;
+        float ref2 = 0.0f;
+        if (row < s.m) {
+            label = __ldg(labels + row);
+            if ((unsigned)label >= (unsigned)s.n) label = -1;
+            ref2 = __ldg(refs + row) * kLog2e;
+        }
+        const bool active = label >= 0;
+        float sum = pass<BN>(s, e, ref2, label, active);
+        const bool over = !(sum <= kMostSum);          // also a sum that is not a number
+        if (__any_sync(0xFFFFFFFFu, over)) {
+            float top = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < BN; c += 32) {
+                float v[32];
+                if (e.col0 + c >= s.n) break;
+                tmem_load32(e.acc + (uint32_t)c, v);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (e.col0 + c + i != label && e.col0 + c + i < s.n) top = fmaxf(top, v[i]);
+            }
+            const float top2 = top * kLog2e;
+            if (e.lane == 0) store_wait_all();          // the first pass has been written before the second overwrites it
+            __syncwarp();
+            const float again = pass<BN>(s, e, over ? top2 : ref2, label, active);
+            if (over) {
+                sum = -again;
+                tops[(int64_t)e.tile.tn * s.m + row] = top2;
+            }
+        }
+        if (row < s.m) sums[(int64_t)e.tile.tn * s.m + row] = sum;
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ finish
+
+constexpr int kFinishTokens = 8;      // 8 tokens x 4 bytes: one sector of a row of `sums`
+
+struct FinishArgs {
+    const uint16_t* hidden;
+    const int32_t* labels;
+    const float* refs;
+    const float* sums;
+    const float* tops;
+    float* loss;
+    float* a;                 // s / (1 + S), 0 without a label
+    float* b;                 // s S / (1 + S)
+    uint16_t* e;              // [tokens][e_ld] or nullptr
+    uint16_t* scaled;         // a H, bf16, or nullptr
+    int64_t tokens, e_ld;
+    int vocab, dim, n_tiles, tile_cols;
+    float grad_scale;
+};
+
+__global__ void __launch_bounds__(256)
+finish_kernel(const __grid_constant__ FinishArgs p)
+{
+    __shared__ float part[32][kFinishTokens];
+    __shared__ float sh_a[kFinishTokens], sh_ref[kFinishTokens];
+    __shared__ int sh_over[kFinishTokens];
+    const int k = (int)threadIdx.x & 7, lane = (int)threadIdx.x >> 3;
+    const int64_t t = (int64_t)blockIdx.x * kFinishTokens + k;
+    const bool in = t < p.tokens;
+    const int label = in ? p.labels[t] : -1;
+    const bool active = (unsigned)label < (unsigned)p.vocab;
+    const float ref = in ? p.refs[t] : 0.0f, ref2 = ref * kLog2e;
+
+    // largest reference of the row's tiles (the target logit where none was too large)
+    float top2 = ref2;
+    int over = 0;
+    float sum = 0.0f;
+    if (active)
+        for (int i = lane; i < p.n_tiles; i += 32) {
+            const float v = p.sums[(int64_t)i * p.tokens + t];
+            if (v >= 0.0f) sum += v;
+            else { over = 1; top2 = fmaxf(top2, p.tops[(int64_t)i * p.tokens + t]); }
+        }
+    part[lane][k] = top2;
+    const int any_over = __syncthreads_or(over);
+    if (any_over) {           // rare: bring the tiles of such rows to one reference
+        for (int i = 0; i < 32; ++i) top2 = fmaxf(top2, part[i][k]);
+        __syncthreads();
+        sum = 0.0f;
+        if (active)
+            for (int i = lane; i < p.n_tiles; i += 32) {
+                const float v = p.sums[(int64_t)i * p.tokens + t];
+                sum += v >= 0.0f ? v * ex2(ref2 - top2) : -v * ex2(p.tops[(int64_t)i * p.tokens + t] - top2);
+            }
+    }
+    part[lane][k] = sum;
+    __syncthreads();
+    if (threadIdx.x < kFinishTokens) {
+        float s = 0.0f;
+        for (int i = 0; i < 32; ++i) s += part[i][k];
+        // the epilogue subtracted ref log2(e) rounded to fp32, the same for the whole row: put the rest of that product back
+        const float missed = fmaf(ref, kLog2e, -ref2) * kLn2;
+        float loss = 0.0f, a = 0.0f, b = 0.0f;
+        if (active) {
+            const float own = ex2(ref2 - top2);          // the target's own term, 1 unless the reference moved
+            if (top2 == ref2) {
+                s -= s * missed;
+                loss = log1pf(s);
+            } else {
+                loss = (top2 - ref2) * kLn2 + logf(own + s);
+            }
+            a = (p.grad_scale - p.grad_scale * missed) / (own + s);
+            b = p.grad_scale * (s / (own + s));
+        }
+        if (in) {
+            p.loss[t] = loss;
+            if (p.a) { p.a[t] = a; p.b[t] = b; }
+        }
+        sh_a[k] = a;
+        sh_ref[k] = top2;
+        sh_over[k] = active && top2 != ref2;
+    }
+    __syncthreads();
+    const int64_t t0 = (int64_t)blockIdx.x * kFinishTokens;
+    const int warp = (int)threadIdx.x >> 5, wl = (int)threadIdx.x & 31;      // one warp per token
+    if (t0 + warp >= p.tokens) return;
+    if (p.scaled) {
+        const float a = sh_a[warp];
+        const uint4* h = reinterpret_cast<const uint4*>(p.hidden + (t0 + warp) * p.dim);
+        uint4* o = reinterpret_cast<uint4*>(p.scaled + (t0 + warp) * p.dim);
+#pragma unroll 4
+        for (int i = wl; i < p.dim / 8; i += 32) {
+            const uint4 x = __ldg(h + i);
+            uint4 r = make_uint4(0u, 0u, 0u, 0u);        // a token without a label contributes nothing, whatever it holds
+            if (a != 0.0f)
+                r = make_uint4(pack2(a * lo16(x.x), a * hi16(x.x)), pack2(a * lo16(x.y), a * hi16(x.y)),
+                               pack2(a * lo16(x.z), a * hi16(x.z)), pack2(a * lo16(x.w), a * hi16(x.w)));
+            o[i] = r;
+        }
+    }
+    if (p.e && sh_over[warp]) {
+        uint16_t* row = p.e + (t0 + warp) * p.e_ld;
+        const float r2 = p.refs[t0 + warp] * kLog2e;
+        for (int j = wl; j < p.vocab; j += 32) {
+            const int64_t at = (int64_t)(j / p.tile_cols) * p.tokens + t0 + warp;
+            const float from = p.sums[at] >= 0.0f ? r2 : p.tops[at];
+            row[j] = (uint16_t)(pack2(__uint_as_float((uint32_t)row[j] << 16) * ex2(from - sh_ref[warp]), 0.0f) & 0xFFFFu);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ gradients
+
+__device__ __forceinline__ void store_bf16_row(uint32_t slot, int lane, int half, const float (&v)[32])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        slot_write(slot, lane, 4 * half + q, pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]),
+                   pack2(v[8 * q + 4], v[8 * q + 5]), pack2(v[8 * q + 6], v[8 * q + 7]));
+}
+
+// One fp32 slot holds 32 columns.
+__device__ __forceinline__ void store_f32_row(uint32_t slot, int lane, const float (&v)[32])
+{
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        slot_write(slot, lane, q, __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+}
+
+// dH tile: a (E W) - b W_label as bf16, or with several splits over the vocabulary the plain sums as fp32.
+struct HiddenGradEpi {
+    static constexpr bool kSym = false;
+    CUtensorMap map_out;         // bf16 [tokens][dim], or fp32 [splits][tokens][dim]
+    const float* a;
+    const float* b;
+    const int32_t* labels;
+    const uint16_t* weight;
+    int vocab, partial;
+
+    template <int BN>
+    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    {
+        if (partial) {
+#pragma unroll 1
+            for (int c = 0; c < BN && e.col0 + c < s.n; c += 32) {
+                float v[32];
+                const uint32_t slot = slot_acquire(e);
+                tmem_load32(e.acc + (uint32_t)c, v);
+                store_f32_row(slot, e.lane, v);
+                slot_store(e, slot, &map_out, e.col0 + c, e.row0, e.tile.split, e.row0 < s.m);
+            }
+            return;
+        }
+        const int row = e.row0 + e.lane;
+        float fa = 0.0f, fb = 0.0f;
+        int label = -1;
+        if (row < s.m) {
+            label = __ldg(labels + row);
+            if ((unsigned)label >= (unsigned)vocab) label = -1;
+            fa = __ldg(a + row);
+            fb = __ldg(b + row);
+        }
+        const uint16_t* w = weight + (int64_t)(label < 0 ? 0 : label) * s.n;
+#pragma unroll 1
+        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+            const uint32_t slot = slot_acquire(e);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n1 = e.col0 + c + 32 * h;
+                uint4 x[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)        // dim % 8 == 0: whole vectors
+                    x[q] = (label >= 0 && n1 + 8 * q < s.n) ? __ldg(reinterpret_cast<const uint4*>(w + n1) + q) : make_uint4(0u, 0u, 0u, 0u);
+                float v[32];
+                tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t u[4] = {x[q].x, x[q].y, x[q].z, x[q].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float& lo = v[8 * q + 2 * i];
+                        float& hi = v[8 * q + 2 * i + 1];
+                        lo = label >= 0 ? fa * lo - fb * lo16(u[i]) : 0.0f;
+                        hi = label >= 0 ? fa * hi - fb * hi16(u[i]) : 0.0f;
+                    }
+                }
+                store_bf16_row(slot, e.lane, h, v);
+            }
+            slot_store(e, slot, &map_out, e.col0 + c, e.row0, 0, e.row0 < s.m);
+        }
+    }
+};
+
+// Adds the splits' sums in order and finishes dH.  One thread per 8 columns.
+__global__ void __launch_bounds__(256)
+join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restrict__ a, const float* __restrict__ b,
+                        const int32_t* __restrict__ labels, const uint16_t* __restrict__ weight, uint16_t* __restrict__ out,
+                        int64_t tokens, int dim, int vocab, int splits)
+{
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int per = dim / 8;
+    if (u >= tokens * per) return;
+    const int64_t t = u / per;
+    const int c = (int)(u - t * per) * 8;
+    const int label = labels[t];
+    uint4 r = make_uint4(0u, 0u, 0u, 0u);
+    if ((unsigned)label < (unsigned)vocab) {
+        float v[8] = {};
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float4* p = reinterpret_cast<const float4*>(partial + ((int64_t)s * tokens + t) * dim + c);
+            const float4 x = __ldg(p), y = __ldg(p + 1);
+            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+        }
+        const float fa = a[t], fb = b[t];
+        const uint4 w = __ldg(reinterpret_cast<const uint4*>(weight + (int64_t)label * dim + c));
+        r = make_uint4(pack2(fa * v[0] - fb * lo16(w.x), fa * v[1] - fb * hi16(w.x)), pack2(fa * v[2] - fb * lo16(w.y), fa * v[3] - fb * hi16(w.y)),
+                       pack2(fa * v[4] - fb * lo16(w.z), fa * v[5] - fb * hi16(w.z)), pack2(fa * v[6] - fb * lo16(w.w), fa * v[7] - fb * hi16(w.w)));
+    }
+    *reinterpret_cast<uint4*>(out + t * dim + c) = r;
+}
+
+// dW tile: bf16 result after the last piece, fp32 running sums before it.
+struct WeightGradEpi {
+    static constexpr bool kSym = false;
+    CUtensorMap map_out;         // bf16 [vocab][dim]
+    CUtensorMap map_acc;         // fp32 [vocab][dim]
+    const float* acc;
+    int add, last;
+
+    __device__ __forceinline__ void add_running(const Shape& s, int row, int n1, float (&v)[32]) const
+    {
+        if (row >= s.m) return;
+        const float* p = acc + (int64_t)row * s.n + n1;
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (n1 + 4 * q < s.n) {
+                const float4 x = __ldcs(reinterpret_cast<const float4*>(p) + q);
+                v[4 * q] += x.x; v[4 * q + 1] += x.y; v[4 * q + 2] += x.z; v[4 * q + 3] += x.w;
+            }
+    }
+
+    template <int BN>
+    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    {
+        const int row = e.row0 + e.lane;
+        if (last) {
+#pragma unroll 1
+            for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+                const uint32_t slot = slot_acquire(e);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float v[32];
+                    tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
+                    if (add) add_running(s, row, e.col0 + c + 32 * h, v);
+                    store_bf16_row(slot, e.lane, h, v);
+                }
+                slot_store(e, slot, &map_out, e.col0 + c, e.row0, 0, e.row0 < s.m);
+            }
+        } else {
+#pragma unroll 1
+            for (int c = 0; c < BN && e.col0 + c < s.n; c += 32) {
+                const uint32_t slot = slot_acquire(e);
+                float v[32];
+                tmem_load32(e.acc + (uint32_t)c, v);
+                if (add) add_running(s, row, e.col0 + c, v);
+                store_f32_row(slot, e.lane, v);
+                slot_store(e, slot, &map_acc, e.col0 + c, e.row0, 0, e.row0 < s.m);
+            }
+        }
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ host
+
+constexpr uint64_t kDefaultPieceBytes = 1ull << 30;       // of E
+
+int64_t e_row_elems(int64_t vocab) { return (vocab + 63) / 64 * 64; }
+
+int64_t piece_of(int64_t tokens, int64_t vocab, int64_t piece_tokens)
+{
+    if (piece_tokens > 0) return piece_tokens < tokens ? piece_tokens : tokens;
+    int64_t fit = (int64_t)(kDefaultPieceBytes / (2ull * (uint64_t)e_row_elems(vocab)));
+    if (fit < 256) fit = 256;
+    if (fit >= tokens) return tokens;
+    // equal pieces, whole tiles of tokens
+    const int64_t n = (tokens + fit - 1) / fit;
+    const int64_t each = (tokens + n - 1) / n;
+    return (each + 255) / 256 * 256;
+}
+
+bool paired(int64_t tokens) { return tokens > 128; }
+int64_t tile_cols(int64_t tokens) { return paired(tokens) ? 256 : 128; }
+
+// Splits of the vocabulary for dH: few tokens give few tiles, and each has the whole vocabulary to sum.  The time of
+// `splits` is taken as rounds of tiles x (blocks + 8 for filling and draining the pipeline).
+int hidden_splits(int64_t tokens, int64_t vocab, int64_t dim, int sms)
+{
+    const bool two = paired(tokens);
+    const int64_t units = two ? sms / 2 : sms, bm = two ? 256 : 128, bn = two ? 256 : 128;
+    const int64_t tiles = ((tokens + bm - 1) / bm) * ((dim + bn - 1) / bn), blocks = (vocab + kBK - 1) / kBK;
+    int best = 1;
+    int64_t best_cost = INT64_MAX;
+    for (int s = 1; s <= 64 && s <= blocks; ++s) {
+        const int64_t rounds = (tiles * s + units - 1) / units;
+        const int64_t cost = rounds * ((blocks + s - 1) / s + 8) + (s > 1 ? 8 + s / 2 : 0);
+        if (cost < best_cost) { best_cost = cost; best = s; }
+    }
+    return best;
+}
+
+struct Layout {
+    int64_t piece, pieces, e_ld, n_tiles;
+    int splits;
+    uint64_t e, scaled, refs, a, b, sums, tops, partial, acc, scatter, total;
+};
+
+int layout_of(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece_tokens, bool want_h, bool want_w, int sms, Layout* l)
+{
+    l->piece = piece_of(tokens, vocab, piece_tokens);
+    l->pieces = (tokens + l->piece - 1) / l->piece;
+    l->e_ld = e_row_elems(vocab);
+    l->n_tiles = (vocab + tile_cols(l->piece) - 1) / tile_cols(l->piece);
+    // the last piece may be short enough for the narrower tiles
+    const int64_t tail = tokens - (l->pieces - 1) * l->piece;
+    const int64_t tail_tiles = (vocab + tile_cols(tail) - 1) / tile_cols(tail);
+    int s1 = 1, s2 = 1;
+    if (want_h) { s1 = hidden_splits(l->piece, vocab, dim, sms); s2 = hidden_splits(tail, vocab, dim, sms); }
+    l->splits = s1;
+    const bool grads = want_h || want_w;
+    uint64_t at = 0;
+    auto take = [&at](uint64_t bytes) { const uint64_t o = at; at += align256(bytes); return o; };
+    const uint64_t P = (uint64_t)l->piece, D = (uint64_t)dim;
+    l->e = take(grads ? 2ull * P * (uint64_t)l->e_ld : 0);
+    l->scaled = take(want_w ? 2ull * P * D : 0);
+    l->refs = take(4ull * (uint64_t)tokens);
+    l->a = take(grads ? 4ull * (uint64_t)tokens : 0);
+    l->b = take(grads ? 4ull * (uint64_t)tokens : 0);
+    const uint64_t stat = 4ull * (P * (uint64_t)l->n_tiles > (uint64_t)tail * (uint64_t)tail_tiles ? P * (uint64_t)l->n_tiles : (uint64_t)tail * (uint64_t)tail_tiles);
+    l->sums = take(stat);
+    l->tops = take(stat);
+    const uint64_t p1 = s1 > 1 ? 4ull * (uint64_t)s1 * P * D : 0, p2 = s2 > 1 ? 4ull * (uint64_t)s2 * (uint64_t)tail * D : 0;
+    l->partial = take(p1 > p2 ? p1 : p2);
+    l->acc = take(want_w && l->pieces > 1 ? 4ull * (uint64_t)vocab * D : 0);
+    l->scatter = take(want_w ? scatter_scratch_bytes(tokens, dim) : 0);
+    l->total = at;
+    return CAST_OK;
+}
+
+int check_ce_shape(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece_tokens)
+{
+    if (tokens < 1 || vocab < 1 || dim < 8 || dim % 8 != 0 || piece_tokens < 0) return CAST_ERR_SHAPE;
+    if (tokens > 0x3FFFFFFF || vocab > 0x7FFFFF00 || dim > (1 << 20)) return CAST_ERR_SHAPE;
+    return CAST_OK;
+}
+
+struct Call {
+    const uint16_t* hidden;
+    const uint16_t* weight;
+    const int32_t* labels;
+    uint16_t* grad_hidden;
+    uint16_t* grad_weight;
+    int64_t tokens, vocab, dim;
+    uint8_t* ws;
+    const Layout* l;
+    cudaStream_t stream;
+    int sms;
+};
+
+// The three products of one piece of tokens [t0, t0 + n).
+template <int CG, int BN>
+int exp_product(const Call& c, int64_t t0, int64_t n)
+{
+    const Layout& l = *c.l;
+    CUtensorMap ma, mb;
+    Shape s;
+    ExpEpi epi;
+    int rc;
+    const bool grads = c.grad_hidden || c.grad_weight;
+    if ((rc = make_shape<CG, BN, false, false, false>(&s, true, n, c.vocab, c.dim, 1, 1, 16 / CG)) != CAST_OK) return rc;
+    if ((rc = operand_map<false>(&ma, c.hidden + t0 * c.dim, n, c.dim, 1, c.dim, 0, 128)) != CAST_OK) return rc;
+    if ((rc = operand_map<false>(&mb, c.weight, c.vocab, c.dim, 1, c.dim, 0, BN / CG)) != CAST_OK) return rc;
+    epi.refs = reinterpret_cast<const float*>(c.ws + l.refs) + t0;
+    epi.labels = c.labels + t0;
+    epi.sums = reinterpret_cast<float*>(c.ws + l.sums);
+    epi.tops = reinterpret_cast<float*>(c.ws + l.tops);
+    epi.write_e = grads;
+    epi.map_e = ma;
+    if (grads && (rc = make_map(&epi.map_e, c.ws + l.e, 2, c.vocab, n, 1, l.e_ld, 0, 64, 32, true)) != CAST_OK) return rc;
+    return launch<CG, BN, false, false>(ma, mb, s, epi, c.stream);
+}
+
+template <int CG, int BN>
+int hidden_product(const Call& c, int64_t t0, int64_t n)
+{
+    const Layout& l = *c.l;
+    CUtensorMap ma, mb;
+    Shape s;
+    HiddenGradEpi epi;
+    int rc;
+    const int splits = hidden_splits(n, c.vocab, c.dim, c.sms);
+    if ((rc = make_shape<CG, BN, false, true, false>(&s, true, n, c.dim, c.vocab, 1, splits, 16 / CG)) != CAST_OK) return rc;
+    if ((rc = operand_map<false>(&ma, c.ws + l.e, n, c.vocab, 1, l.e_ld, 0, 128)) != CAST_OK) return rc;
+    if ((rc = operand_map<true>(&mb, c.weight, c.dim, c.vocab, 1, c.dim, 0, BN / CG)) != CAST_OK) return rc;
+    epi.a = reinterpret_cast<const float*>(c.ws + l.a) + t0;
+    epi.b = reinterpret_cast<const float*>(c.ws + l.b) + t0;
+    epi.labels = c.labels + t0;
+    epi.weight = c.weight;
+    epi.vocab = (int)c.vocab;
+    epi.partial = s.splits > 1;
+    float* partial = reinterpret_cast<float*>(c.ws + l.partial);
+    if (epi.partial) rc = make_map(&epi.map_out, partial, 4, c.dim, n, s.splits, c.dim, (uint64_t)n * c.dim, 32, 32, true);
+    else rc = make_map(&epi.map_out, c.grad_hidden + t0 * c.dim, 2, c.dim, n, 1, c.dim, 0, 64, 32, true);
+    if (rc != CAST_OK) return rc;
+    if ((rc = launch<CG, BN, false, true>(ma, mb, s, epi, c.stream)) != CAST_OK) return rc;
+    if (epi.partial) {
+        const int64_t units = n * (c.dim / 8);
+        join_hidden_grad_kernel<<<(unsigned)((units + 255) / 256), 256, 0, c.stream>>>(partial, epi.a, epi.b, epi.labels, c.weight,
+                                                                                     c.grad_hidden + t0 * c.dim, n, (int)c.dim, (int)c.vocab, s.splits);
+        CAST_CUDA_TRY(cudaGetLastError());
+        count_launch();
+    }
+    return CAST_OK;
+}
+
+int weight_product(const Call& c, int64_t n, bool first, bool last)
+{
+    constexpr int CG = 2, BN = 256;
+    const Layout& l = *c.l;
+    CUtensorMap ma, mb;
+    Shape s;
+    WeightGradEpi epi;
+    int rc;
+    if ((rc = make_shape<CG, BN, true, true, false>(&s, true, c.vocab, c.dim, n, 1, 1, 8)) != CAST_OK) return rc;
+    if ((rc = operand_map<true>(&ma, c.ws + l.e, c.vocab, n, 1, l.e_ld, 0, 128)) != CAST_OK) return rc;
+    if ((rc = operand_map<true>(&mb, c.ws + l.scaled, c.dim, n, 1, c.dim, 0, BN / CG)) != CAST_OK) return rc;
+    epi.acc = reinterpret_cast<const float*>(c.ws + l.acc);
+    epi.add = !first;
+    epi.last = last;
+    if ((rc = make_map(&epi.map_out, c.grad_weight, 2, c.dim, c.vocab, 1, c.dim, 0, 64, 32, true)) != CAST_OK) return rc;
+    epi.map_acc = epi.map_out;
+    if (l.pieces > 1 && (rc = make_map(&epi.map_acc, c.ws + l.acc, 4, c.dim, c.vocab, 1, c.dim, 0, 32, 32, true)) != CAST_OK) return rc;
+    return launch<CG, BN, true, true>(ma, mb, s, epi, c.stream);
+}
+
+}  // namespace
+}  // namespace cast
+
+using namespace cast;
+
+extern "C" int cast_linear_ce_workspace(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece_tokens, int want_hidden_grad,
+                                        int want_weight_grad, uint64_t* bytes)
+{
+    if (!bytes) return CAST_ERR_NULL;
+    int rc, sms;
+    if ((rc = check_ce_shape(tokens, vocab, dim, piece_tokens)) != CAST_OK) return rc;
+    if ((rc = product::sm_count(&sms)) != CAST_OK) return rc;
+    Layout l;
+    if ((rc = layout_of(tokens, vocab, dim, piece_tokens, want_hidden_grad != 0, want_weight_grad != 0, sms, &l)) != CAST_OK) return rc;
+    *bytes = l.total;
+    return CAST_OK;
+}
+
+extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, const int32_t* labels, float* loss, cast_bf16* grad_hidden,
+                              cast_bf16* grad_weight, int64_t tokens, int64_t vocab, int64_t dim, float grad_scale, int64_t piece_tokens,
+                              void* workspace, uint64_t workspace_bytes, cast_stream_t stream)
+{
+    if (!hidden || !weight || !labels || !loss || !workspace) return CAST_ERR_NULL;
+    int rc;
+    if ((rc = check_ce_shape(tokens, vocab, dim, piece_tokens)) != CAST_OK) return rc;
+    if (!std::isfinite(grad_scale)) return CAST_ERR_HYPER;
+    if (((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)grad_hidden | (uintptr_t)grad_weight | (uintptr_t)workspace) & 15u) return CAST_ERR_ALIGN;
+    if (((uintptr_t)labels | (uintptr_t)loss) & 3u) return CAST_ERR_ALIGN;
+    const uint64_t th = 2ull * (uint64_t)tokens * (uint64_t)dim, vw = 2ull * (uint64_t)vocab * (uint64_t)dim, t4 = 4ull * (uint64_t)tokens;
+    int sms;
+    if ((rc = product::sm_count(&sms)) != CAST_OK) return rc;
+    Layout l;
+    if ((rc = layout_of(tokens, vocab, dim, piece_tokens, grad_hidden != nullptr, grad_weight != nullptr, sms, &l)) != CAST_OK) return rc;
+    if (workspace_bytes < l.total) return CAST_ERR_PLAN;
+    const void* in[3] = {hidden, weight, labels};
+    const uint64_t in_bytes[3] = {th, vw, t4};
+    const void* out[4] = {loss, grad_hidden, grad_weight, workspace};
+    const uint64_t out_bytes[4] = {t4, th, vw, l.total};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 3; ++j)
+            if (ranges_overlap(out[i], out_bytes[i], in[j], in_bytes[j])) return CAST_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (ranges_overlap(out[i], out_bytes[i], out[j], out_bytes[j])) return CAST_ERR_ALIAS;
+    }
+    const void* ptrs[7] = {hidden, weight, labels, loss, grad_hidden, grad_weight, workspace};
+    if ((rc = check_device_memory(ptrs, 7)) != CAST_OK) return rc;
+
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    cudaStream_t st = (cudaStream_t)stream;
+    const Call c = {hidden, weight, labels, grad_hidden, grad_weight, tokens, vocab, dim, ws, &l, st, sms};
+    float* refs = reinterpret_cast<float*>(ws + l.refs);
+    float* a = reinterpret_cast<float*>(ws + l.a);
+    float* b = reinterpret_cast<float*>(ws + l.b);
+    target_logit_kernel<<<(unsigned)((tokens + 7) / 8), 256, 0, st>>>(hidden, weight, labels, refs, tokens, (int)vocab, (int)dim);
+    CAST_CUDA_TRY(cudaGetLastError());
+    count_launch();
+    for (int64_t i = 0; i < l.pieces; ++i) {
+        const int64_t t0 = i * l.piece, n = tokens - t0 < l.piece ? tokens - t0 : l.piece;
+        rc = paired(n) ? exp_product<2, 256>(c, t0, n) : exp_product<1, 128>(c, t0, n);
+        if (rc != CAST_OK) return rc;
+        FinishArgs f;
+        f.hidden = hidden + t0 * dim;
+        f.labels = labels + t0;
+        f.refs = refs + t0;
+        f.sums = reinterpret_cast<const float*>(ws + l.sums);
+        f.tops = reinterpret_cast<const float*>(ws + l.tops);
+        f.loss = loss + t0;
+        const bool grads = grad_hidden || grad_weight;
+        f.a = grads ? a + t0 : nullptr;
+        f.b = grads ? b + t0 : nullptr;
+        f.e = grads ? reinterpret_cast<uint16_t*>(ws + l.e) : nullptr;
+        f.scaled = grad_weight ? reinterpret_cast<uint16_t*>(ws + l.scaled) : nullptr;
+        f.tokens = n;
+        f.e_ld = l.e_ld;
+        f.vocab = (int)vocab;
+        f.dim = (int)dim;
+        f.tile_cols = (int)tile_cols(n);
+        f.n_tiles = (int)((vocab + f.tile_cols - 1) / f.tile_cols);
+        f.grad_scale = grad_scale;
+        finish_kernel<<<(unsigned)((n + kFinishTokens - 1) / kFinishTokens), 256, 0, st>>>(f);
+        CAST_CUDA_TRY(cudaGetLastError());
+        count_launch();
+        if (grad_hidden) {
+            rc = paired(n) ? hidden_product<2, 256>(c, t0, n) : hidden_product<1, 128>(c, t0, n);
+            if (rc != CAST_OK) return rc;
+        }
+        if (grad_weight && (rc = weight_product(c, n, i == 0, i + 1 == l.pieces)) != CAST_OK) return rc;
+    }
+    if (grad_weight) {
+        const int32_t *sorted, *order;
+        if ((rc = sort_tokens(labels, tokens, vocab, dim, ws + l.scatter, &sorted, &order, st)) != CAST_OK) return rc;
+        // b holds s S / (1 + S): the label's term of dW is -b H
+        if ((rc = scatter_rows(hidden, b, -1.0f, sorted, order, grad_weight, tokens, vocab, dim, true, ws + l.scatter, st)) != CAST_OK) return rc;
+    }
+    return CAST_OK;
+}

@@ -1,0 +1,533 @@
+// Newton-Schulz orthogonalisation of updates (as the Muon optimiser applies it to hidden matrices):
+//     X = U / (|U|_F + eps),   steps times  X <- a X + (b A + c A A) X,  A = X X^T,   out = scale X
+// and X <- a X + X (b A + c A A) with A = X^T X where there are more rows than columns, so that A is the smaller square.
+//
+// Each step is three products on the tensor cores over all matrices of the call at once:
+//     A = X X^T               symmetric: only tiles on and below the diagonal, each stored twice (once transposed)
+//     P = b A + c A A         symmetric likewise; b A is added by the epilogue
+//     X' = a X + P X          a X is added by the epilogue
+// Operands are never transposed in memory: X is read K-major in one product and MN-major in the other.
+//
+// Numbers: the operands are fp16, not bf16.  Every value is bounded (|X| singular values stay near 1), so the range is
+// enough and the 3 more bits of significand are worth 8 times less rounding noise.  X is held as hi + lo, two fp16 words scaled
+// by 2^12 (22 bits): the products read hi, a X reads both.  That matters because a = 3.4 per step amplifies small singular
+// directions 500-fold over five steps: noise from rounding X itself would be amplified with them, while noise that enters
+// through the products is confined to directions that are large already.  A and P (b A + c A A, without a I) are plain fp16.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include <cuda_fp16.h>
+
+#include "embed.cuh"
+#include "tile_product.cuh"
+
+namespace cast {
+namespace {
+
+using namespace product;
+
+constexpr float kX = 4096.0f;               // X is stored times this
+constexpr int kGroup = 64;                  // matrices per launch at most
+constexpr int64_t kGroupElems = 64 << 20;   // ... and elements, which bounds the workspace
+constexpr int kNormBlocks = 128;
+
+struct PtrTable { const void* p[kGroup]; };
+struct OutTable { uint16_t* p[kGroup]; };
+
+__device__ __forceinline__ float f16_lo(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xFFFFu))); }
+__device__ __forceinline__ float f16_hi(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+// round to nearest, and to the largest finite value beyond the range (coefficients under which X grows without bound)
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(fminf(fmaxf(lo, -65504.0f), 65504.0f), fminf(fmaxf(hi, -65504.0f), 65504.0f));
+    uint32_t r;
+    memcpy(&r, &h, 4);
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_b16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------------ norm and first X
+
+template <bool BF16, int VEC>
+__device__ __forceinline__ void load_update(const void* u, int64_t unit, float (&v)[VEC])
+{
+    if constexpr (VEC == 1) {
+        if constexpr (BF16) v[0] = __uint_as_float((uint32_t)__ldg(static_cast<const uint16_t*>(u) + unit) << 16);
+        else v[0] = __ldg(static_cast<const float*>(u) + unit);
+    } else if constexpr (BF16) {
+        const uint4 x = __ldg(static_cast<const uint4*>(u) + unit);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    } else {
+        const float4 x = __ldg(static_cast<const float4*>(u) + 2 * unit), y = __ldg(static_cast<const float4*>(u) + 2 * unit + 1);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    }
+}
+
+__device__ __forceinline__ double block_sum(double x)
+{
+    __shared__ double part[8];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = 0.0;
+    for (int i = 0; i < 8; ++i) x += part[i];
+    return x;
+}
+
+// Squares in fp64: gradients are small enough for their squares to leave the range of fp32.
+template <bool BF16, int VEC>
+__global__ void __launch_bounds__(256)
+square_sum_kernel(const __grid_constant__ PtrTable updates, double* __restrict__ partial, int64_t units)
+{
+    const void* u = updates.p[blockIdx.y];
+    double sum = 0.0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
+        float v[VEC];
+        load_update<BF16, VEC>(u, i, v);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum += (double)v[j] * (double)v[j];
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) partial[(int64_t)blockIdx.y * kNormBlocks + blockIdx.x] = sum;
+}
+
+template <bool BF16, int VEC>
+__global__ void __launch_bounds__(256)
+first_x_kernel(const __grid_constant__ PtrTable updates, const double* __restrict__ partial, int parts, uint16_t* __restrict__ hi,
+               uint16_t* __restrict__ lo, int64_t units, uint32_t units_per_row, int64_t ld, int64_t stride, double eps)
+{
+    const double sum = block_sum((int)threadIdx.x < parts ? partial[(int64_t)blockIdx.y * kNormBlocks + threadIdx.x] : 0.0);
+    const double norm = sqrt(sum) + eps;
+    const double f = norm > 0.0 ? (double)kX / norm : 0.0;      // not in fp32: 1 / norm of a tiny update leaves its range
+    const void* u = updates.p[blockIdx.y];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
+        float v[VEC];
+        load_update<BF16, VEC>(u, i, v);
+        const int64_t row = i / units_per_row;
+        const int64_t at = (int64_t)blockIdx.y * stride + row * ld + (i - row * units_per_row) * VEC;
+        float x[VEC], rest[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            x[j] = (float)((double)v[j] * f);
+            rest[j] = x[j] - __half2float(__float2half_rn(x[j]));
+        }
+        if constexpr (VEC == 8) {
+            *reinterpret_cast<uint4*>(hi + at) = make_uint4(pack_f16(x[0], x[1]), pack_f16(x[2], x[3]), pack_f16(x[4], x[5]), pack_f16(x[6], x[7]));
+            *reinterpret_cast<uint4*>(lo + at) = make_uint4(pack_f16(rest[0], rest[1]), pack_f16(rest[2], rest[3]), pack_f16(rest[4], rest[5]), pack_f16(rest[6], rest[7]));
+        } else {
+            hi[at] = (uint16_t)pack_f16(x[0], 0.0f);
+            lo[at] = (uint16_t)pack_f16(rest[0], 0.0f);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ epilogues
+
+// 64 columns of fp16 values in fp32 -> this lane's row of a slot
+__device__ __forceinline__ void f16_half_row(uint32_t slot, int lane, int half, const float (&v)[32])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        slot_write(slot, lane, 4 * half + q, pack_f16(v[8 * q], v[8 * q + 1]), pack_f16(v[8 * q + 2], v[8 * q + 3]),
+                   pack_f16(v[8 * q + 4], v[8 * q + 5]), pack_f16(v[8 * q + 6], v[8 * q + 7]));
+}
+
+// Symmetric result: scale x acc (+ add x aux), stored at (row, col) and, off the diagonal, at (col, row).
+struct SymEpi {
+    static constexpr bool kSym = true;
+    CUtensorMap map_out;         // boxes of 32 rows x 64 columns, swizzled
+    CUtensorMap map_mirror;      // the same array, boxes of 64 rows x 32 columns, not swizzled
+    const uint16_t* aux;         // fp16, laid out as the result; nullptr: none
+    int64_t ld, stride;
+    float scale, add;
+
+    template <int BN>
+    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    {
+        const int row = e.row0 + e.lane;
+        const bool mirror = e.tile.tm != e.tile.tn;
+#pragma unroll 1
+        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+            const int n = e.col0 + c;
+            uint4 x[8];
+            if (aux && row < s.m) {
+                // rows are padded to whole 128-byte lines: reading past the last column stays inside the row
+                const uint4* p = reinterpret_cast<const uint4*>(aux + (int64_t)e.tile.batch * stride + (int64_t)row * ld + n);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x[q] = __ldg(p + q);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x[q] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            const uint32_t slot = slot_acquire(e);
+            uint32_t packed[32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[32];
+                tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint4 w = x[4 * h + q];
+                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float lo = scale * v[8 * q + 2 * i], hi = scale * v[8 * q + 2 * i + 1];
+                        packed[16 * h + 4 * q + i] = aux ? pack_f16(fmaf(add, f16_lo(u[i]), lo), fmaf(add, f16_hi(u[i]), hi)) : pack_f16(lo, hi);
+                    }
+                    slot_write(slot, e.lane, 4 * h + q, packed[16 * h + 4 * q], packed[16 * h + 4 * q + 1], packed[16 * h + 4 * q + 2], packed[16 * h + 4 * q + 3]);
+                }
+            }
+            slot_store(e, slot, &map_out, n, e.row0, e.tile.batch, e.row0 < s.m);
+            if (mirror) {
+                // rows of 32 elements (64 bytes): column j of the chunk becomes row j, this lane its element
+                const uint32_t t = slot_acquire(e);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const uint32_t at = t + (uint32_t)(2 * j) * 64u + (uint32_t)e.lane * 2u;
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((unsigned short)(packed[j] & 0xFFFFu)) : "memory");
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 64u), "h"((unsigned short)(packed[j] >> 16)) : "memory");
+                }
+                slot_store(e, t, &map_mirror, e.row0, n, e.tile.batch, e.row0 < s.m);
+            }
+        }
+    }
+};
+
+// X' = a X + acc: two fp16 words per entry, or after the last step bf16(scale X').
+struct StepEpi {
+    static constexpr bool kSym = false;
+    CUtensorMap map_hi, map_lo;      // outputs
+    const uint16_t* hi;
+    const uint16_t* lo;
+    int64_t ld, stride;
+    OutTable out;
+    float a, scale;
+    int last, vec;
+
+    template <int BN>
+    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    {
+        const int row = e.row0 + e.lane;
+        const int64_t at = (int64_t)e.tile.batch * stride + (int64_t)row * ld;
+#pragma unroll 1
+        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+            const int n = e.col0 + c;
+            const uint32_t slot_hi = slot_acquire(e);
+            uint32_t slot_lo = 0;
+            if (!last) {
+                if (e.lane == 0) store_wait_read<0>();
+                __syncwarp();
+                slot_lo = e.slots + (uint32_t)(e.slot * kSlotBytes);
+                e.slot = (e.slot + 1) % kSlotsPerWarp;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint4 x[4], y[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { x[q] = make_uint4(0u, 0u, 0u, 0u); y[q] = x[q]; }
+                if (row < s.m) {
+                    const uint4* p = reinterpret_cast<const uint4*>(hi + at + n) + 4 * h;
+                    const uint4* r = reinterpret_cast<const uint4*>(lo + at + n) + 4 * h;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) { x[q] = __ldg(p + q); y[q] = __ldg(r + q); }
+                }
+                float v[32];
+                tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t u[4] = {x[q].x, x[q].y, x[q].z, x[q].w}, w[4] = {y[q].x, y[q].y, y[q].z, y[q].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float& l = v[8 * q + 2 * i];
+                        float& g = v[8 * q + 2 * i + 1];
+                        l = fmaf(a, f16_lo(u[i]) + f16_lo(w[i]), l);
+                        g = fmaf(a, f16_hi(u[i]) + f16_hi(w[i]), g);
+                    }
+                }
+                if (last) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        slot_write(slot_hi, e.lane, 4 * h + q, pack_b16(scale * v[8 * q], scale * v[8 * q + 1]),
+                                   pack_b16(scale * v[8 * q + 2], scale * v[8 * q + 3]), pack_b16(scale * v[8 * q + 4], scale * v[8 * q + 5]),
+                                   pack_b16(scale * v[8 * q + 6], scale * v[8 * q + 7]));
+                } else {
+                    f16_half_row(slot_hi, e.lane, h, v);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
+                    f16_half_row(slot_lo, e.lane, h, v);
+                }
+            }
+            if (last) {
+                // rows of the caller's matrix may have any length: whole rows of the slot by ordinary stores
+                __syncwarp();
+                uint16_t* o = out.p[e.tile.batch];
+#pragma unroll 1
+                for (int r0 = 0; r0 < 32; r0 += 4) {
+                    const int r = r0 + (e.lane >> 3), q = e.lane & 7;
+                    uint4 w;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                                 : "r"(slot_hi + (uint32_t)r * 128u + (uint32_t)((q ^ (r & 7)) << 4)));
+                    if (e.row0 + r >= s.m) continue;
+                    uint16_t* to = o + (int64_t)(e.row0 + r) * s.n + n + 8 * q;
+                    if (vec) {
+                        if (n + 8 * q < s.n) *reinterpret_cast<uint4*>(to) = w;
+                    } else {
+                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (n + 8 * q + i < s.n) to[i] = (uint16_t)(i & 1 ? u[i / 2] >> 16 : u[i / 2] & 0xFFFFu);
+                    }
+                }
+                __syncwarp();
+                if (e.lane == 0) store_commit();
+            } else {
+                slot_store(e, slot_hi, &map_hi, n, e.row0, e.tile.batch, e.row0 < s.m);
+                slot_store(e, slot_lo, &map_lo, n, e.row0, e.tile.batch, e.row0 < s.m);
+            }
+        }
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ host
+
+struct Layout {
+    int64_t group, ld, sq, sq_ld;
+    uint64_t norms, hi[2], lo[2], a, p, total;
+};
+
+Layout layout_of(int64_t n, int64_t rows, int64_t cols)
+{
+    Layout l;
+    int64_t fit = kGroupElems / (rows * cols);
+    fit = fit < 1 ? 1 : fit > kGroup ? kGroup : fit;
+    l.group = n < fit ? n : fit;
+    l.ld = (cols + 63) / 64 * 64;
+    l.sq = rows < cols ? rows : cols;
+    l.sq_ld = (l.sq + 63) / 64 * 64;
+    uint64_t at = 0;
+    auto take = [&at](uint64_t bytes) { const uint64_t o = at; at += align256(bytes); return o; };
+    const uint64_t x = 2ull * (uint64_t)(l.group * rows * l.ld), q = 2ull * (uint64_t)(l.group * l.sq * l.sq_ld);
+    l.norms = take(8ull * kNormBlocks * kGroup);
+    for (int i = 0; i < 2; ++i) { l.hi[i] = take(x); l.lo[i] = take(x); }
+    l.a = take(q);
+    l.p = take(q);
+    l.total = at;
+    return l;
+}
+
+// Pairs of CTAs with 256 x 256 tiles, or single CTAs with 128 x 128 ones: rounds over the SMs x cycles per tile.  A 64-deep
+// block takes 512 cycles of a pair's tensor cores and about 350 of a single CTA's (256, held up by its shared memory);
+// filling and draining a tile's pipeline about 3000.
+bool use_pairs(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int sms)
+{
+    const int64_t kb = (k + kBK - 1) / kBK;
+    auto tiles = [&](int64_t t) {
+        const int64_t a = (m + t - 1) / t, b = (n + t - 1) / t;
+        return (sym ? a * (a + 1) / 2 : a * b) * batch;
+    };
+    const int64_t pairs = sms / 2;
+    const int64_t two = (tiles(256) + pairs - 1) / pairs * (kb * 512 + 3000), one = (tiles(128) + sms - 1) / sms * (kb * 350 + 3000);
+    return two <= one;
+}
+
+template <int CG, int BN, bool MN>
+int sym_product(const uint16_t* x, int64_t mn, int64_t k, int64_t batch, int64_t x_ld, int64_t x_stride, uint16_t* out, const Layout& l,
+                const uint16_t* aux, float scale, float add, cudaStream_t stream)
+{
+    CUtensorMap m;
+    Shape s;
+    SymEpi epi;
+    int rc;
+    const int64_t stride = l.sq * l.sq_ld;
+    if ((rc = make_shape<CG, BN, MN, MN, true>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
+    if ((rc = operand_map<MN>(&m, x, mn, k, batch, x_ld, x_stride, 128)) != CAST_OK) return rc;
+    static_assert(BN / CG == 128, "one map serves both operands");
+    if ((rc = make_map(&epi.map_out, out, 2, mn, mn, batch, l.sq_ld, stride, 64, 32, true)) != CAST_OK) return rc;
+    if ((rc = make_map(&epi.map_mirror, out, 2, mn, mn, batch, l.sq_ld, stride, 32, 64, false)) != CAST_OK) return rc;
+    epi.aux = aux;
+    epi.ld = l.sq_ld;
+    epi.stride = stride;
+    epi.scale = scale;
+    epi.add = add;
+    return launch<CG, BN, MN, MN>(m, m, s, epi, stream);
+}
+
+// X' = a X + P X (wide) or a X + X P (tall)
+template <int CG, int BN, bool WIDE>
+int step_product(const uint16_t* p, const uint16_t* hi, int64_t rows, int64_t cols, int64_t batch, const Layout& l, uint16_t* hi_out,
+                 uint16_t* lo_out, StepEpi& epi, cudaStream_t stream)
+{
+    CUtensorMap ma, mb;
+    Shape s;
+    int rc;
+    const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
+    if ((rc = make_shape<CG, BN, false, WIDE, false>(&s, false, rows, cols, l.sq, batch, 1, 16 / CG)) != CAST_OK) return rc;
+    if (WIDE) {
+        if ((rc = operand_map<false>(&ma, p, rows, rows, batch, l.sq_ld, ps, 128)) != CAST_OK) return rc;
+        if ((rc = operand_map<true>(&mb, hi, cols, rows, batch, l.ld, xs, BN / CG)) != CAST_OK) return rc;
+    } else {
+        if ((rc = operand_map<false>(&ma, hi, rows, cols, batch, l.ld, xs, 128)) != CAST_OK) return rc;
+        if ((rc = operand_map<false>(&mb, p, cols, cols, batch, l.sq_ld, ps, BN / CG)) != CAST_OK) return rc;
+    }
+    if ((rc = make_map(&epi.map_hi, hi_out, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
+    if ((rc = make_map(&epi.map_lo, lo_out, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
+    epi.ld = l.ld;
+    epi.stride = xs;
+    return launch<CG, BN, false, WIDE>(ma, mb, s, epi, stream);
+}
+
+template <bool BF16, int VEC>
+int launch_first(const PtrTable& t, int64_t batch, int64_t rows, int64_t cols, uint8_t* ws, const Layout& l, float eps, cudaStream_t stream)
+{
+    const int64_t units = rows * cols / VEC;
+    int64_t parts = (units + 256 * 8 - 1) / (256 * 8);
+    if (parts > kNormBlocks) parts = kNormBlocks;
+    double* norms = reinterpret_cast<double*>(ws + l.norms);
+    square_sum_kernel<BF16, VEC><<<dim3((unsigned)parts, (unsigned)batch), 256, 0, stream>>>(t, norms, units);
+    CAST_CUDA_TRY(cudaGetLastError());
+    count_launch();
+    int64_t blocks = (units + 256 * 4 - 1) / (256 * 4);
+    if (blocks > 2048) blocks = 2048;
+    first_x_kernel<BF16, VEC><<<dim3((unsigned)blocks, (unsigned)batch), 256, 0, stream>>>(
+        t, norms, (int)parts, reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.lo[0]), units,
+        (uint32_t)(cols / VEC), l.ld, rows * l.ld, (double)eps);
+    CAST_CUDA_TRY(cudaGetLastError());
+    count_launch();
+    return CAST_OK;
+}
+
+int check_ortho_shape(int64_t n, int64_t rows, int64_t cols)
+{
+    if (n < 1 || rows < 1 || cols < 1 || n > 0x7FFFFFFF) return CAST_ERR_SHAPE;
+    if (rows > 0x7FFFFFFF / cols) return CAST_ERR_SHAPE;      // rows*cols < 2^31, as for every matrix of the library
+    return CAST_OK;
+}
+
+// No result shares memory with an update or another result: the ranges in address order, against the furthest end so far.
+int check_apart(const void* const* updates, uint64_t in_bytes, cast_bf16* const* out, uint64_t out_bytes, int n)
+{
+    struct Range { uintptr_t lo, hi; bool result; };
+    Range few[64];
+    Range* r = 2 * (int64_t)n <= 64 ? few : new (std::nothrow) Range[2 * (size_t)n];
+    if (!r) return CAST_ERR_MEMORY;
+    for (int i = 0; i < n; ++i) {
+        const uintptr_t u = (uintptr_t)updates[i], o = (uintptr_t)out[i];
+        r[2 * i] = {u, u + in_bytes, false};
+        r[2 * i + 1] = {o, o + out_bytes, true};
+    }
+    std::sort(r, r + 2 * (size_t)n, [](const Range& a, const Range& b) { return a.lo < b.lo; });
+    uintptr_t any = 0, result = 0;
+    int rc = CAST_OK;
+    for (size_t i = 0; i < 2 * (size_t)n; ++i) {
+        if (r[i].lo < (r[i].result ? any : result)) rc = CAST_ERR_ALIAS;
+        any = std::max(any, r[i].hi);
+        if (r[i].result) result = std::max(result, r[i].hi);
+    }
+    if (r != few) delete[] r;
+    return rc;
+}
+
+}  // namespace
+}  // namespace cast
+
+using namespace cast;
+
+extern "C" int cast_orthogonalize_workspace(int n, int64_t rows, int64_t cols, uint64_t* bytes)
+{
+    if (!bytes) return CAST_ERR_NULL;
+    int rc;
+    if ((rc = check_ortho_shape(n, rows, cols)) != CAST_OK) return rc;
+    *bytes = layout_of(n, rows, cols).total;
+    return CAST_OK;
+}
+
+extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, cast_bf16* const* out, int n, int64_t rows, int64_t cols,
+                                  const float* coeffs, int steps, float eps, float scale, void* workspace, uint64_t workspace_bytes,
+                                  cast_stream_t stream)
+{
+    static const float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
+    if (!updates || !out || !workspace) return CAST_ERR_NULL;
+    int rc, sms;
+    if ((rc = check_ortho_shape(n, rows, cols)) != CAST_OK) return rc;
+    if (steps < 1 || steps > 100 || !(eps >= 0.0f) || !std::isfinite(eps) || !std::isfinite(scale)) return CAST_ERR_HYPER;
+    for (int i = 0; coeffs && i < 3 * steps; ++i)
+        if (!std::isfinite(coeffs[i])) return CAST_ERR_HYPER;
+    if ((uintptr_t)workspace & 15u) return CAST_ERR_ALIGN;
+    const Layout l = layout_of(n, rows, cols);
+    if (workspace_bytes < l.total) return CAST_ERR_PLAN;
+    const uintptr_t mask = updates_bf16 ? 1u : 3u;
+    const uint64_t in_bytes = (updates_bf16 ? 2ull : 4ull) * (uint64_t)(rows * cols), out_bytes = 2ull * (uint64_t)(rows * cols);
+    for (int i = 0; i < n; ++i) {
+        if (!updates[i] || !out[i]) return CAST_ERR_NULL;
+        if (((uintptr_t)updates[i] & mask) || ((uintptr_t)out[i] & 1u)) return CAST_ERR_ALIGN;
+        if (ranges_overlap(workspace, l.total, updates[i], in_bytes) || ranges_overlap(workspace, l.total, out[i], out_bytes)) return CAST_ERR_ALIAS;
+    }
+    if ((rc = check_apart(updates, in_bytes, out, out_bytes, n)) != CAST_OK) return rc;
+    if ((rc = check_device_memory(updates, n)) != CAST_OK) return rc;
+    if ((rc = check_device_memory(reinterpret_cast<const void* const*>(out), n)) != CAST_OK) return rc;
+    if ((rc = check_device_memory(&workspace, 1)) != CAST_OK) return rc;
+    if ((rc = product::sm_count(&sms)) != CAST_OK) return rc;
+
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool wide = rows <= cols;
+    const int64_t big = wide ? cols : rows;
+    uint16_t* hi[2] = {reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.hi[1])};
+    uint16_t* lo[2] = {reinterpret_cast<uint16_t*>(ws + l.lo[0]), reinterpret_cast<uint16_t*>(ws + l.lo[1])};
+    uint16_t* a = reinterpret_cast<uint16_t*>(ws + l.a);
+    uint16_t* p = reinterpret_cast<uint16_t*>(ws + l.p);
+    for (int first = 0; first < n; first += (int)l.group) {
+        const int64_t batch = n - first < l.group ? n - first : l.group;
+        PtrTable in;
+        StepEpi epi;
+        bool in_vec = cols % 8 == 0, out_vec = cols % 8 == 0;
+        for (int64_t i = 0; i < batch; ++i) {
+            in.p[i] = updates[first + i];
+            epi.out.p[i] = out[first + i];
+            in_vec = in_vec && !((uintptr_t)in.p[i] & 15u);
+            out_vec = out_vec && !((uintptr_t)epi.out.p[i] & 15u);
+        }
+        for (int64_t i = batch; i < kGroup; ++i) { in.p[i] = nullptr; epi.out.p[i] = nullptr; }
+        if (updates_bf16) rc = in_vec ? launch_first<true, 8>(in, batch, rows, cols, ws, l, eps, st) : launch_first<true, 1>(in, batch, rows, cols, ws, l, eps, st);
+        else rc = in_vec ? launch_first<false, 8>(in, batch, rows, cols, ws, l, eps, st) : launch_first<false, 1>(in, batch, rows, cols, ws, l, eps, st);
+        if (rc != CAST_OK) return rc;
+        const bool gram2 = use_pairs(l.sq, l.sq, big, batch, true, sms), sq2 = use_pairs(l.sq, l.sq, l.sq, batch, true, sms);
+        const bool step2 = use_pairs(rows, cols, l.sq, batch, false, sms);
+        const float down = 1.0f / (kX * kX);
+        for (int k = 0; k < steps; ++k) {
+            const float* q = coeffs ? coeffs + 3 * k : kQuintic;
+            const int cur = k & 1;
+            const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
+            if (wide) rc = gram2 ? sym_product<2, 256, false>(hi[cur], rows, cols, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st)
+                                 : sym_product<1, 128, false>(hi[cur], rows, cols, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st);
+            else rc = gram2 ? sym_product<2, 256, true>(hi[cur], cols, rows, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st)
+                            : sym_product<1, 128, true>(hi[cur], cols, rows, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st);
+            if (rc != CAST_OK) return rc;
+            rc = sq2 ? sym_product<2, 256, false>(a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, a, q[2], q[1], st)
+                     : sym_product<1, 128, false>(a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, a, q[2], q[1], st);
+            if (rc != CAST_OK) return rc;
+            epi.hi = hi[cur];
+            epi.lo = lo[cur];
+            epi.a = q[0];
+            epi.scale = scale / kX;
+            epi.last = k + 1 == steps;
+            epi.vec = out_vec;
+            if (wide) rc = step2 ? step_product<2, 256, true>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
+                                 : step_product<1, 128, true>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
+            else rc = step2 ? step_product<2, 256, false>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
+                            : step_product<1, 128, false>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
+            if (rc != CAST_OK) return rc;
+        }
+    }
+    return CAST_OK;
+}

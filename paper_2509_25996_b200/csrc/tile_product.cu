@@ -1,0 +1,74 @@
+// Host side of the tensor-core products: tensor maps, the failure word, the number of SMs.
+#include <mutex>
+
+#include <cudaTypedefs.h>
+
+#include "tile_product.cuh"
+
+namespace cast {
+namespace product {
+
+namespace {
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_entry()
+{
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    }();
+    return fn;
+}
+
+}  // namespace
+
+int make_map(CUtensorMap* map, const void* base, int elem_bytes, uint64_t inner, uint64_t rows, uint64_t batch, uint64_t ld,
+             uint64_t batch_stride, uint32_t box_inner, uint32_t box_rows, bool swizzle)
+{
+    const auto encode = encode_entry();
+    if (!encode) return cuda_failed(cudaErrorNotSupported);
+    // the two outer strides only matter where there is more than one row or matrix, but must be valid all the same
+    const cuuint64_t dims[3] = {inner, rows, batch};
+    const cuuint64_t strides[2] = {ld * (uint64_t)elem_bytes, (batch > 1 ? batch_stride : ld) * (uint64_t)elem_bytes};
+    const cuuint32_t box[3] = {box_inner, box_rows, 1};
+    const cuuint32_t steps[3] = {1, 1, 1};
+    const CUtensorMapDataType type = elem_bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    const CUresult r = encode(map, type, 3, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CAST_OK : cuda_failed(cudaErrorInvalidValue);
+}
+
+int fail_word(unsigned long long** word)
+{
+    static std::mutex lock;
+    static unsigned long long* w = nullptr;
+    std::lock_guard<std::mutex> hold(lock);
+    if (!w) {
+        void* p = nullptr;
+        CAST_CUDA_TRY(cudaHostAlloc(&p, sizeof(unsigned long long), cudaHostAllocPortable | cudaHostAllocMapped));
+        w = static_cast<unsigned long long*>(p);
+        *w = 0ull;
+    }
+    *word = w;
+    return *static_cast<volatile unsigned long long*>(w) == 0ull ? CAST_OK : CAST_ERR_STAGING;
+}
+
+int sm_count(int* n)
+{
+    static int known[64] = {};
+    int dev;
+    CAST_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 64 && known[dev] > 0) { *n = known[dev]; return CAST_OK; }
+    CAST_CUDA_TRY(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
+    if (dev < 64) known[dev] = *n;
+    return CAST_OK;
+}
+
+}  // namespace product
+}  // namespace cast

@@ -1,0 +1,489 @@
+// Matrix products of 16-bit operands on the fifth-generation tensor cores, shared by the loss and the orthogonalisation:
+// D[m, n] = sum_k A[m, k] B[n, k], accumulated in fp32, each accumulator tile handed to an epilogue.
+//
+// One persistent kernel.  A CTA (CG = 1) or a pair of CTAs on neighbouring SMs (CG = 2) owns a tile of 128 CG x BN; tiles are
+// dealt out round robin.  Per CTA:
+//   warp 0    one lane moves operand blocks of 64 k (128 bytes, the swizzle width) with TMA into a ring of stages
+//   warp 1    one lane of the pair's first CTA issues tcgen05.mma over each stage and commits it back to the ring
+//   warp 2    allocates and frees tensor memory: two accumulators, so the next tile's products run under an epilogue
+//   warps 4-7 epilogue: 32 accumulator rows each (a lane is a row), through shared memory to TMA stores where the result
+//             is a matrix
+// In a pair every CTA stages its own 128 rows of A and its own half of B; the tensor cores read both halves of B, which
+// halves the shared-memory traffic per product.  No load is multicast.
+//
+// An operand is "K-major" (k contiguous in memory) or "MN-major" (its m or n index contiguous).  Both are staged with the
+// 128-byte swizzle.  K-major: rows of 64 k, groups of 8 rows 1024 bytes apart.  MN-major: rows of 64 m (or n), one row per k,
+// groups of 8 k 1024 bytes apart, and the next 64 m follow after the 64 k of the block (8192 bytes).
+//
+// Every wait is bounded (kWaitCycles); a role that gives up raises the CTA's stop flag, which ends the other roles, and
+// counts the failure in a word of host memory that the next call of the library reads.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "cast_internal.h"
+
+namespace cast {
+namespace product {
+
+constexpr int kBK = 64;                          // k per stage: 64 x 2 bytes = one 128-byte swizzle row
+constexpr int kThreads = 256;
+constexpr int kEpiWarps = 4;
+constexpr int kStageBytesA = 128 * kBK * 2;      // 128 rows of A per CTA
+constexpr int kSlotBytes = 4096;                 // epilogue staging: 32 rows of 128 bytes
+constexpr int kSlotsPerWarp = 2;
+constexpr int kStagingBytes = kEpiWarps * kSlotsPerWarp * kSlotBytes;
+constexpr long long kWaitCycles = 4000000000ll;  // ~2 s; the longest wait of a healthy run is a tile (tens of microseconds)
+
+// Shape of one launch.  k_blocks = ceil(k / 64) blocks are cut into `splits` runs of at most split_blocks, each of which
+// is a tile of its own (its epilogue sees Tile::split).
+struct Shape {
+    int m, n;                      // result rows and columns
+    int k_blocks, splits, split_blocks;
+    int m_tiles, n_tiles, batch;
+    int group;                     // tile rows that are walked together, so that their operands stay in L2
+    int total;                     // tiles of all batches and splits
+    uint32_t idesc;                // instruction descriptor
+    unsigned long long* fail_word; // host memory
+};
+
+struct Tile { int batch, split, tm, tn, kb0, kb1; };
+
+template <bool SYM>
+__device__ __forceinline__ Tile tile_of(const Shape& s, int t)
+{
+    Tile r;
+    if constexpr (SYM) {           // lower triangle, tile rows first to last
+        const int per = s.m_tiles * (s.m_tiles + 1) / 2;
+        r.batch = t / per;
+        const int i = t - r.batch * per;
+        int row = (int)((sqrtf(8.0f * (float)i + 1.0f) - 1.0f) * 0.5f);
+        while (row * (row + 1) / 2 > i) --row;
+        while ((row + 1) * (row + 2) / 2 <= i) ++row;
+        r.tm = row;
+        r.tn = i - row * (row + 1) / 2;
+        r.split = 0;
+    } else {
+        const int per = s.m_tiles * s.n_tiles;
+        const int o = t / per;
+        int i = t - o * per;
+        r.batch = o / s.splits;
+        r.split = o - r.batch * s.splits;
+        const int band = s.group * s.n_tiles;
+        const int g = i / band;
+        i -= g * band;
+        const int rows = min(s.group, s.m_tiles - g * s.group);
+        r.tn = i / rows;
+        r.tm = g * s.group + (i - r.tn * rows);
+    }
+    r.kb0 = r.split * s.split_blocks;
+    r.kb1 = min(s.k_blocks, r.kb0 + s.split_blocks);
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------------ instructions
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)      // bar: shared::cluster address
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{ .reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+
+struct Stop { volatile int* flag; unsigned long long* fail_word; };
+
+// Waits for a phase; false once the CTA has stopped or the limit has passed.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Stop& stop)
+{
+    if (mbar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t i = 1;; ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if ((i & 31u) == 0u) {
+            if (*stop.flag) return false;
+            if (clock64() - t0 > kWaitCycles) break;
+        }
+    }
+    *stop.flag = 1;
+    atomicAdd_system(stop.fail_word, 1ull);
+    return false;
+}
+
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z)
+{
+    if constexpr (CG == 2)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+template <int CG>
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (CG == 2)
+        asm volatile("{ .reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{ .reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrives on `bar` (at the same offset in both CTAs of a pair) once every product issued so far has been done.
+template <int CG>
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    if constexpr (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t cols)
+{
+    if constexpr (CG == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t cols)
+{
+    if constexpr (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
+}
+// 32 consecutive accumulator columns of this lane's row.  The values may be used after tmem_wait().
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32])
+{
+    uint32_t r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// Shared-memory matrix descriptor, 128-byte swizzle (bits 61-63 = 2, version 1 at bit 46): start address, leading and
+// stride byte offsets in units of 16 bytes.
+template <bool MN_MAJOR>
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr)
+{
+    constexpr uint64_t lead = MN_MAJOR ? (kBK * 128) >> 4 : 1;     // next 64 m (n) of an MN-major block; unused in K-major form
+    constexpr uint64_t hi = (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+    return hi | (uint64_t)((addr & 0x3FFFFu) >> 4);
+}
+template <bool MN_MAJOR>
+constexpr uint64_t kDescStep = MN_MAJOR ? (16 * 128) >> 4 : (16 * 2) >> 4;      // 16 k further
+
+// ------------------------------------------------------------------------------------------------ the kernel
+
+template <int CG, int BN>
+struct Config {
+    static constexpr int BM = 128 * CG;
+    static constexpr int b_rows = BN / CG;                         // rows of B staged by one CTA
+    static constexpr int stage_bytes = kStageBytesA + b_rows * kBK * 2;
+    static constexpr int stages = stage_bytes >= 32768 ? 6 : 8;
+    static constexpr int smem_bytes = stages * stage_bytes + kStagingBytes + 1024 /* alignment */ + 256 /* barriers */;
+    static constexpr uint32_t tmem_cols = 2 * BN;
+    static_assert(BN == 256 || BN == 128 || BN == 64, "two accumulators of BN columns: a power of two of at least 32");
+    static_assert(b_rows % 64 == 0, "MN-major blocks are 64 wide");
+    static_assert(smem_bytes <= 232448, "227 KB of shared memory per CTA");
+};
+
+// What an epilogue warp is given for one tile.
+struct EpiTile {
+    Tile tile;
+    int row0;            // first result row of this warp's 32
+    int col0;            // first result column of the tile
+    uint32_t acc;        // tensor-memory address of this warp's rows, column 0
+    uint32_t slots;      // this warp's staging memory (kSlotsPerWarp slots of 4 KB, 1024-byte aligned)
+    int lane;
+    int slot;            // staging slot to use next (kept from tile to tile)
+};
+
+// 16 bytes of this lane's row in a swizzled 32 x 128-byte slot.
+__device__ __forceinline__ void slot_write(uint32_t slot_addr, int lane, int chunk, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(slot_addr + (uint32_t)lane * 128u + (uint32_t)((chunk ^ (lane & 7)) << 4)),
+                 "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// Takes the next staging slot once the store that last used it has read it.
+__device__ __forceinline__ uint32_t slot_acquire(EpiTile& e)
+{
+    if (e.lane == 0) store_wait_read<kSlotsPerWarp - 1>();
+    __syncwarp();
+    const uint32_t a = e.slots + (uint32_t)(e.slot * kSlotBytes);
+    e.slot = (e.slot + 1) % kSlotsPerWarp;
+    return a;
+}
+// Hands a written slot to a TMA store (commits an empty group where nothing is to be stored, so that the groups count slots).
+__device__ __forceinline__ void slot_store(const EpiTile& e, uint32_t slot_addr, const CUtensorMap* map, int x, int y, int z, bool any)
+{
+    fence_async_smem();
+    __syncwarp();
+    if (e.lane == 0) {
+        if (any) tma_store(map, slot_addr, x, y, z);
+        store_commit();
+    }
+}
+
+template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
+__global__ void __launch_bounds__(kThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ Shape shape, const __grid_constant__ Epi epi)
+{
+    using C = Config<CG, BN>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t ring = base;
+    const uint32_t staging = base + C::stages * C::stage_bytes;
+    __shared__ __align__(8) unsigned long long bars[2 * C::stages + 4];
+    __shared__ uint32_t tmem_base_smem;
+    __shared__ int stop_flag;
+    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::stages, accf0 = empty0 + 8 * C::stages, acce0 = accf0 + 16;
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+
+    if (threadIdx.x == 0) {
+        stop_flag = 0;
+        for (int i = 0; i < C::stages; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(accf0 + 8 * i, 1); mbar_init(acce0 + 8 * i, CG * kEpiWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) tmem_alloc<CG>(smem_u32(&tmem_base_smem), C::tmem_cols);
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_smem;
+    const Stop stop = {&stop_flag, shape.fail_word};
+    const int first = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; ok && t < shape.total; t += step) {
+                const Tile tile = tile_of<Epi::kSym>(shape, t);
+                const int m0 = tile.tm * C::BM + (int)rank * 128, n0 = tile.tn * BN + (int)rank * C::b_rows;
+                for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
+                    if (!(ok = mbar_wait(empty0 + 8 * s, phase ^ 1u, stop))) break;
+                    const uint32_t a = ring + s * C::stage_bytes, b = a + kStageBytesA;
+                    uint32_t full = full0 + 8 * s;
+                    if (rank == 0) mbar_expect(full, CG * C::stage_bytes);
+                    if constexpr (CG == 2) full = map_to_rank(full, 0);
+                    if constexpr (A_MN) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) tma_load<CG>(a + i * 8192, &map_a, full, m0 + 64 * i, kb * kBK, tile.batch);
+                    } else {
+                        tma_load<CG>(a, &map_a, full, kb * kBK, m0, tile.batch);
+                    }
+                    if constexpr (B_MN) {
+#pragma unroll
+                        for (int i = 0; i < C::b_rows / 64; ++i) tma_load<CG>(b + i * 8192, &map_b, full, n0 + 64 * i, kb * kBK, tile.batch);
+                    } else {
+                        tma_load<CG>(b, &map_b, full, kb * kBK, n0, tile.batch);
+                    }
+                    if (++s == C::stages) { s = 0; phase ^= 1u; }
+                }
+            }
+            // every stage handed back: nothing of this CTA is in flight when it leaves
+            for (int i = 0; ok && i < C::stages; ++i) {
+                ok = mbar_wait(empty0 + 8 * s, phase ^ 1u, stop);
+                if (++s == C::stages) { s = 0; phase ^= 1u; }
+            }
+            if (!ok) {      // given up: leave copies that are under way the time to land
+                const long long t0 = clock64();
+                while (clock64() - t0 < 10000000ll) __nanosleep(1000);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            int s = 0, n_done = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; ok && t < shape.total; t += step, ++n_done) {
+                const Tile tile = tile_of<Epi::kSym>(shape, t);
+                const int buf = n_done & 1;
+                if (!(ok = mbar_wait(acce0 + 8 * buf, (uint32_t)((n_done >> 1) & 1) ^ 1u, stop))) break;
+                tc_fence_after();
+                const uint32_t d = tmem + (uint32_t)(buf * BN);
+                for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
+                    if (!(ok = mbar_wait(full0 + 8 * s, phase, stop))) break;
+                    tc_fence_after();
+                    const uint64_t a = operand_desc<A_MN>(ring + s * C::stage_bytes);
+                    const uint64_t b = operand_desc<B_MN>(ring + s * C::stage_bytes + kStageBytesA);
+#pragma unroll
+                    for (int i = 0; i < kBK / 16; ++i)
+                        tc_mma<CG>(d, a + i * kDescStep<A_MN>, b + i * kDescStep<B_MN>, shape.idesc, (kb > tile.kb0 || i > 0) ? 1u : 0u);
+                    tc_commit<CG>(empty0 + 8 * s);
+                    if (++s == C::stages) { s = 0; phase ^= 1u; }
+                }
+                if (ok) tc_commit<CG>(accf0 + 8 * buf);
+            }
+        }
+    } else if (warp >= 4) {
+        EpiTile e;
+        e.lane = lane;
+        e.slots = staging + (uint32_t)((warp - 4) * kSlotsPerWarp * kSlotBytes);
+        e.slot = 0;
+        int n_done = 0;
+        for (int t = first; t < shape.total; t += step, ++n_done) {
+            e.tile = tile_of<Epi::kSym>(shape, t);
+            const int buf = n_done & 1;
+            bool ok = mbar_wait(accf0 + 8 * buf, (uint32_t)(n_done >> 1) & 1u, stop);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            tc_fence_after();
+            e.row0 = e.tile.tm * C::BM + (int)rank * 128 + (warp - 4) * 32;
+            e.col0 = e.tile.tn * BN;
+            e.acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)((warp - 4) * 32) << 16);
+            epi.template tile<BN>(shape, e);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_rank(acce0 + 8 * buf, 0));
+        }
+        if (lane == 0) store_wait_all();
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();
+    tc_fence_after();
+    if (warp == 2) tmem_free<CG>(tmem, C::tmem_cols);
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+
+// A [batch][rows][inner] array of 2- or 4-byte elements, moved in boxes of box_rows x box_inner.  `ld` and `batch_stride`
+// in elements; ld x element size and the base must be multiples of 16 bytes.
+int make_map(CUtensorMap* map, const void* base, int elem_bytes, uint64_t inner, uint64_t rows, uint64_t batch, uint64_t ld,
+             uint64_t batch_stride, uint32_t box_inner, uint32_t box_rows, bool swizzle);
+
+// The operand maps: rows of A (128 per CTA) or B (b_rows per CTA).  K-major: inner = k, rows = m; MN-major: inner = m, rows = k.
+template <bool MN_MAJOR>
+int operand_map(CUtensorMap* map, const void* base, uint64_t mn, uint64_t k, uint64_t batch, uint64_t ld, uint64_t batch_stride, uint32_t rows_per_cta)
+{
+    if (MN_MAJOR) return make_map(map, base, 2, mn, k, batch, ld, batch_stride, 64, kBK, true);
+    return make_map(map, base, 2, k, mn, batch, ld, batch_stride, kBK, rows_per_cta, true);
+}
+
+// Page-locked word the kernels report an abandoned wait in; CAST_ERR_STAGING once it is not zero.
+int fail_word(unsigned long long** word);
+int sm_count(int* n);
+
+inline uint32_t instruction_desc(bool bf16, bool a_mn, bool b_mn, int m, int n)
+{
+    // D fp32 (bit 4), A and B type (bits 7, 10: 1 = bf16, 0 = f16), transposes (15, 16), n / 8 (17), m / 16 (24)
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+template <int CG, int BN, bool A_MN, bool B_MN, bool SYM>
+int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t batch, int splits, int group)
+{
+    using C = Config<CG, BN>;
+    const int64_t mt = (m + C::BM - 1) / C::BM, nt = (n + BN - 1) / BN;
+    if (SYM && C::BM != BN) return CAST_ERR_SHAPE;
+    s->m = (int)m;
+    s->n = (int)n;
+    s->k_blocks = (int)((k + kBK - 1) / kBK);
+    s->split_blocks = (s->k_blocks + splits - 1) / splits;
+    s->splits = (s->k_blocks + s->split_blocks - 1) / s->split_blocks;
+    s->m_tiles = (int)mt;
+    s->n_tiles = (int)nt;
+    s->batch = (int)batch;
+    s->group = group;
+    const int64_t per = SYM ? mt * (mt + 1) / 2 : mt * nt * s->splits;
+    if (per * batch > 0x3FFFFFFF) return CAST_ERR_SHAPE;
+    s->total = (int)(per * batch);
+    s->idesc = instruction_desc(bf16, A_MN, B_MN, C::BM, BN);
+    return fail_word(&s->fail_word);
+}
+
+template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
+int launch(const CUtensorMap& a, const CUtensorMap& b, const Shape& s, const Epi& epi, cudaStream_t stream)
+{
+    using C = Config<CG, BN>;
+    auto kernel = product_kernel<CG, BN, A_MN, B_MN, Epi>;
+    int sms, rc;
+    if ((rc = sm_count(&sms)) != CAST_OK) return rc;
+    CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes));
+    const int units = s.total < sms / CG ? s.total : sms / CG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * CG));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = C::smem_bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CAST_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, b, s, epi));
+    count_launch();
+    return CAST_OK;
+}
+
+}  // namespace product
+}  // namespace cast

@@ -1,0 +1,289 @@
+"""cast_linear_ce against a plain 64-bit evaluation on the same bf16 inputs.
+
+Tolerances.  With A_i = max_j sum_k |h_ik w_jk|: a logit is a sum of exact products in fp32, taken 16 at a time, so its error
+is at most (dim/16 + 4) 2^-23 A_i; the exponent's argument adds 2^-22 of the largest |logit|, the row sums (128 terms in
+sequence, then a tree) 160 2^-24, ex2 2^-22:
+    eps_i   = 2 (dim/16 + 4) 2^-23 A_i + 2^-21 max|l_i| + 1.2e-5           (relative error of 1 + S and of S)
+    loss    |cuda - exact| <= eps_i
+    dH      <= 2^-8 |exact| + s sum_{j != label} p_ij |w_jk| (2^-8 + eps_i + vocab 2^-27) + s (1 - p_label) |w_label,k| (eps_i + 2^-22)
+    dW      <= 2^-8 |exact| + s sum_{i: label != j} p_ij |h_ik| (3 2^-8 + eps_i + tokens 2^-27)
+                            + s sum_{i: label = j} (1 - p_ij) |h_ik| (eps_i + tokens 2^-23)
+(operands of the backward products are rounded to bf16, 2^-9 each; results are rounded to bf16, dW of a row with labels twice)."""
+import math
+
+import pytest
+import torch
+
+import paper_2509_25996_b200 as cast
+from paper_2509_25996_b200 import binding as B
+from paper_2509_25996_b200 import ops
+import gpu_util as U
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def draw(tokens, vocab, dim, seed, lift=6.0):
+    """Hidden states partly aligned with the label's row: target probabilities from chance to near one."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    w = (torch.randn((vocab, dim), generator=g, device=DEV) / math.sqrt(dim)).to(torch.bfloat16)
+    y = torch.randint(0, vocab, (tokens,), generator=g, device=DEV).int()
+    h = torch.randn((tokens, dim), generator=g, device=DEV) + torch.rand((tokens, 1), generator=g, device=DEV) * lift * w[y.long()].float()
+    return h.to(torch.bfloat16), w, y
+
+
+def exact(h, w, y, s):
+    h, w = h.double(), w.double()
+    vocab, dim = w.shape
+    tokens = h.shape[0]
+    rows = torch.nonzero((y >= 0) & (y < vocab))[:, 0]
+    label = y[rows].long()
+    hr = h[rows]
+    l = hr @ w.T
+    lse = torch.logsumexp(l, 1)
+    at = torch.arange(len(rows), device=DEV)
+    loss, eps = torch.zeros(tokens, dtype=torch.float64, device=DEV), torch.zeros(tokens, dtype=torch.float64, device=DEV)
+    others = torch.exp(l - l[at, label][:, None])
+    others[at, label] = 0.0
+    loss[rows] = torch.log1p(others.sum(1))             # = lse - l_label, without its cancellation
+    size = (hr.abs() @ w.abs().T).amax(1)
+    e = 2 * (dim / 16 + 4) * 2.0 ** -23 * size + 2.0 ** -21 * l.abs().amax(1) + 1.2e-5
+    eps[rows] = e
+    p = torch.exp(l - lse[:, None])
+    p[at, label] = 0.0                                  # the other columns
+    rest = p.sum(1)                                     # 1 - p_label, without its cancellation
+    s = abs(s), (1.0 if s >= 0 else -1.0)
+    gh, bh = torch.zeros_like(h), torch.zeros_like(h)
+    gh[rows] = s[0] * s[1] * (p @ w - rest[:, None] * w[label])
+    bh[rows] = s[0] * ((p * (2.0 ** -8 + e[:, None] + vocab * 2.0 ** -27)) @ w.abs() + (rest * (e + 2.0 ** -22))[:, None] * w[label].abs())
+    gw = s[0] * s[1] * (p.T @ hr).index_add_(0, label, -rest[:, None] * hr)
+    bw = s[0] * ((p * (3 * 2.0 ** -8 + e[:, None] + tokens * 2.0 ** -27)).T @ hr.abs()).index_add_(
+        0, label, (rest * (e + tokens * 2.0 ** -23))[:, None] * hr.abs())
+    return (loss, eps), (gh, 2.0 ** -8 * gh.abs() + bh + 1e-37), (gw, 2.0 ** -8 * gw.abs() + bw + 1e-37)
+
+
+def run(h, w, y, s, want_h=True, want_w=True, piece=0):
+    (tokens, dim), vocab = h.shape, w.shape[0]
+    gl, gh, gw = (U.Guarded(n, t, DEV) for n, t in ((tokens, torch.float32), (tokens * dim, torch.bfloat16), (vocab * dim, torch.bfloat16)))
+    rc, need = cast.cast_linear_ce_workspace(tokens, vocab, dim, piece, want_h, want_w)
+    cast.check(rc)
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device=DEV)        # NaN patterns: nothing may be read before it is written
+    cast.check(cast.cast_linear_ce(h, w, y, gl.view, gh.view if want_h else None, gw.view if want_w else None, tokens, vocab, dim, s, piece,
+                                   ws, need, torch.cuda.current_stream()))
+    torch.cuda.synchronize()
+    assert gl.intact() and gh.intact() and gw.intact() and bool((ws[need:] == 255).all())
+    assert cast.cast_bulk_timeout_count() == (0, 0)
+    return gl.view, gh.view.reshape(tokens, dim), gw.view.reshape(vocab, dim)
+
+
+def close(got, pair, what):
+    want, bound = pair
+    err = (got.double() - want).abs()
+    assert bool((err <= bound).all()), f"{what}: worst {float((err / bound).nan_to_num(nan=math.inf).max()):.3g} x the bound"
+
+
+def check(h, w, y, s, label="", **kw):
+    loss, gh, gw = run(h, w, y, s, **kw)
+    l, a, b = exact(h, w, y, s)
+    close(loss, l, f"{label} loss")
+    if kw.get("want_h", True):
+        close(gh, a, f"{label} dH")
+    if kw.get("want_w", True):
+        close(gw, b, f"{label} dW")
+    return loss, gh, gw
+
+
+SHAPES = [(1, 1, 8), (1, 2, 8), (1, 1000, 64), (2, 63, 16), (17, 130, 72), (64, 256, 64), (127, 1003, 264), (128, 5000, 768), (129, 257, 256),
+          (200, 32000, 128), (257, 513, 520), (512, 4096, 512), (1000, 50257, 96), (1, 32000, 4096)]
+
+
+@pytest.mark.parametrize("tokens,vocab,dim", SHAPES)
+def test_shapes(tokens, vocab, dim):
+    h, w, y = draw(tokens, vocab, dim, tokens + vocab)
+    check(h, w, y, 1.0 / tokens, f"{tokens}x{vocab}x{dim}")
+
+
+@pytest.mark.parametrize("tokens,piece", [(700, 256), (700, 100), (513, 256), (300, 129), (5, 1), (1024, 512)])
+def test_pieces_of_tokens(tokens, piece):
+    h, w, y = draw(tokens, 1500, 136, tokens)
+    y[3 % tokens] = -1
+    loss, gh, gw = check(h, w, y, 0.5, f"{tokens} in pieces of {piece}", piece=piece)
+    whole = run(h, w, y, 0.5)
+    close(gw, (whole[2].double(), 2 * exact(h, w, y, 0.5)[2][1]), "pieces against whole")
+
+
+@pytest.mark.parametrize("tokens", [40, 300])
+def test_single_results_are_those_of_the_full_call(tokens):
+    h, w, y = draw(tokens, 900, 128, 5)
+    loss, gh, gw = run(h, w, y, -2.0)
+    check(h, w, y, -2.0, "negative scale")
+    only, _, _ = run(h, w, y, -2.0, want_h=False, want_w=False)
+    assert torch.equal(only, loss)
+    l2, h2, _ = run(h, w, y, -2.0, want_w=False)
+    assert torch.equal(l2, loss) and torch.equal(h2, gh)
+    l3, _, w3 = run(h, w, y, -2.0, want_h=False)
+    assert torch.equal(l3, loss) and torch.equal(w3, gw)
+
+
+@pytest.mark.parametrize("tokens", [100, 400])
+def test_tokens_without_a_label(tokens):
+    h, w, y = draw(tokens, 600, 64, 7)
+    y[::3] = -1
+    y[1] = 600
+    y[2] = 2 ** 31 - 1
+    y[tokens - 1] = -2 ** 31
+    loss, gh, gw = check(h, w, y, 1.0, "some without a label")
+    none = (y < 0) | (y >= 600)
+    assert not loss[none].any() and not gh[none].any()
+    # what those tokens hold does not matter
+    h2 = h.clone()
+    h2[none] = float("nan")
+    h2[none.nonzero()[0, 0]] = float("inf")
+    again = run(h2, w, y, 1.0)
+    assert all(torch.equal(a, b) for a, b in zip((loss, gh, gw), again))
+    # none at all
+    loss, gh, gw = run(h, w, torch.full_like(y, -100), 1.0)
+    assert not loss.any() and not gh.any() and not gw.any()
+
+
+def test_equal_labels_and_confident_tokens():
+    """All tokens on one label (one long sum), and targets so likely that 1 - p underflows a subtraction in fp32."""
+    h, w, y = draw(500, 700, 256, 8, lift=60.0)
+    y[:] = 123
+    h[:250] = (torch.randn((250, 256), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV) * 0.2 + 45.0 * w[123].float()).to(torch.bfloat16)
+    loss, _, _ = check(h, w, y, 1.0, "one label")
+    assert float(loss[:250].max()) < 1e-4
+    ref = exact(h, w, y, 1.0)[0][0][:250]
+    assert float(((loss[:250].double() - ref).abs() / ref).max()) < 1e-2        # small losses keep their leading digits
+
+
+@pytest.mark.parametrize("gap", [30.0, 39.0, 45.0, 80.0, 200.0])
+@pytest.mark.parametrize("tokens", [20, 300])
+def test_improbable_targets(gap, tokens):
+    """Other logits far above the target's: beyond e^40 the row is brought to another reference."""
+    vocab, dim = 1300, 64
+    g = torch.Generator(device=DEV).manual_seed(3)
+    w = (torch.randn((vocab, dim), generator=g, device=DEV) / 8).to(torch.bfloat16)
+    y = torch.randint(0, vocab, (tokens,), generator=g, device=DEV).int()
+    h = torch.randn((tokens, dim), generator=g, device=DEV).to(torch.bfloat16)
+    # one column pushes a single other logit up by about `gap` for every second token
+    w[:, 0] = 0.0
+    w[777, 0] = 1.0
+    h[:, 0] = 0.0
+    h[::2, 0] = gap
+    y[y == 777] = 5
+    check(h, w, y, 1.0 / tokens, f"gap {gap}")
+    check(h, w, y, 1.0 / tokens, f"gap {gap} in pieces", piece=max(1, tokens // 3))
+
+
+def test_extreme_values():
+    """Large logits of both signs; a vocabulary whose other rows are all far below the target."""
+    h, w, y = draw(150, 300, 64, 12)
+    check((h.float() * 30).to(torch.bfloat16), w, y, 1.0, "logits of hundreds")
+    w2 = w.clone()
+    w2[:] = -50.0
+    w2[y[0].long()] = 50.0
+    h2 = torch.ones_like(h)
+    loss, gh, gw = run(h2, w2, torch.full_like(y, int(y[0])), 1.0)
+    assert not loss.any() and not gh.any() and not gw.any()
+
+
+def test_gradients_against_differences():
+    """Central differences of the kernel's own loss along directions that keep the inputs exact in bf16.  The third
+    derivative of logsumexp along u is at most range(u)^3; the losses carry eps each."""
+    tokens, vocab, dim = 60, 200, 64
+    g = torch.Generator(device=DEV).manual_seed(4)
+    w = (torch.randint(-8, 9, (vocab, dim), generator=g, device=DEV) / 16).to(torch.bfloat16)
+    h = (torch.randint(-8, 9, (tokens, dim), generator=g, device=DEV) / 16).to(torch.bfloat16)
+    y = torch.randint(0, vocab, (tokens,), generator=g, device=DEV).int()
+    y[5] = -1
+    _, gh, gw = run(h, w, y, 1.0)
+    step = 1.0 / 64
+    dh = (torch.randint(0, 2, (tokens, dim), generator=g, device=DEV) * 2 - 1).to(torch.bfloat16)
+    dw = (torch.randint(0, 2, (vocab, dim), generator=g, device=DEV) * 2 - 1).to(torch.bfloat16)
+    (_, eps), _, _ = exact(h, w, y, 1.0)
+    for name, moved, inner, span in (
+            ("hidden", lambda t: run((h + t * dh), w, y, 1.0, False, False)[0], float((gh.double() * dh.double()).sum()), dh.double() @ w.double().T),
+            ("weight", lambda t: run(h, (w + t * dw), y, 1.0, False, False)[0], float((gw.double() * dw.double()).sum()), h.double() @ dw.double().T)):
+        up, down = moved(step), moved(-step)
+        slope = float((up.double() - down.double()).sum()) / (2 * step)
+        width = (span.amax(1) - span.amin(1))
+        tol = float((2 * eps).sum()) / (2 * step) + step ** 2 / 6 * float((width ** 3).sum()) + 2.0 ** -8 * float(
+            ((gh.double() if name == "hidden" else gw.double()).abs()).sum())
+        assert abs(slope - inner) <= tol, (name, slope, inner, tol)
+        assert tol < 0.5 * abs(float(((gh if name == "hidden" else gw).double().abs()).sum()))        # the bound says something
+
+
+def test_more_exponentials_than_32_bits_address():
+    """One piece whose exponentials are more than 2^31: the last tokens' results against the same tokens on their own."""
+    tokens, vocab, dim = 17000, 128256, 64
+    h, w, y = draw(tokens, vocab, dim, 21)
+    loss, gh, gw = run(h, w, y, 1.0, piece=tokens)
+    tail = slice(tokens - 300, tokens)
+    (l, eps), (a, ba), _ = exact(h[tail], w, y[tail], 1.0)
+    close(loss[tail], (l, eps), "loss")
+    close(gh[tail], (a, ba), "dH")
+    cols = torch.randint(0, vocab, (64,), device=DEV)
+    part, size = torch.zeros((64, dim), dtype=torch.float64, device=DEV), torch.zeros((64, dim), dtype=torch.float64, device=DEV)
+    for t0 in range(0, tokens, 2000):
+        hd = h[t0:t0 + 2000].double()
+        logits = hd @ w.double().T
+        p = torch.exp(logits[:, cols] - torch.logsumexp(logits, 1, keepdim=True))
+        hot = (y[t0:t0 + 2000, None] == cols[None]).double()
+        part += (p - hot).T @ hd
+        size += (p + hot).T @ hd.abs()
+    err = (gw[cols].double() - part).abs()
+    assert bool((err <= 2.0 ** -8 * part.abs() + size * (4 * 2.0 ** -8 + tokens * 2.0 ** -23)).all())
+
+
+def test_repeatable_on_any_stream():
+    h, w, y = draw(700, 3000, 200, 30)
+    one = ops.linear_ce(h, w, y, 0.1)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        two = ops.linear_ce(h, w, y, 0.1)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(one, two))
+    loss, gh, gw = ops.linear_ce(h[:0], w, y[:0])
+    assert loss.numel() == 0 and gh.shape == (0, 200) and not gw.any()
+
+
+def test_graph_capture():
+    h, w, y = draw(100, 900, 64, 31)
+    want = ops.linear_ce(h, w, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ops.linear_ce(h, w, y)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_refusals():
+    h, w, y = draw(10, 50, 64, 32)
+    loss, gh, gw = torch.empty(10, device=DEV), torch.empty_like(h), torch.empty_like(w)
+    need = cast.cast_linear_ce_workspace(10, 50, 64)[1]
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    before = cast.cast_kernel_launch_count()
+
+    def call(**over):
+        a = dict(hidden=h, weight=w, labels=y, loss=loss, grad_hidden=gh, grad_weight=gw, tokens=10, vocab=50, dim=64, grad_scale=1.0, piece_tokens=0,
+                 workspace=ws, workspace_bytes=need)
+        a.update(over)
+        return cast.cast_linear_ce(**a)
+    assert call(workspace_bytes=need - 1) == B.CAST_ERR_PLAN
+    assert call(grad_hidden=h) == B.CAST_ERR_ALIAS
+    assert call(grad_weight=gh) == B.CAST_ERR_ALIAS
+    assert call(loss=ws) == B.CAST_ERR_ALIAS
+    assert call(labels=y.cpu()) == B.CAST_ERR_MEMORY
+    assert cast.cast_kernel_launch_count() == before
+    with pytest.raises(ValueError, match="columns"):
+        ops.linear_ce(h, w[:, :32].contiguous(), y)
+    with pytest.raises(ValueError, match="not contiguous"):
+        ops.linear_ce(h, w[:, :32], y)
+    with pytest.raises(ValueError, match="labels"):
+        ops.linear_ce(h, w, y[:5])
+    with pytest.raises(cast.CastError):
+        ops.linear_ce(h[:, :60].contiguous(), w[:, :60].contiguous(), y)
