@@ -6,15 +6,20 @@
 // Gradient: the tokens are put in the order (id, position) first, so that every table row sums its tokens in one fixed
 // order, in fp32 registers, and is rounded and written once, without atomics: results do not change from run to run.
 //   * sort: runs of 1024 are ranked by counting (a key's place = the keys of its run that come before it, an all-pairs
-//     comparison from shared memory: 1024 comparisons per key, ~1 us, no passes and no histograms), then groups of 16 runs
+//     comparison from shared memory: 1024 comparisons per key, no passes and no histograms), then groups of 16 runs
 //     are merged at once: a key's new place = its place in its own run + its bounds in the 15 others, found by binary
 //     searches that advance together, so that their loads overlap.  16384 tokens take two launches, 262144 three.
-//   * sums: a row with many tokens would be one CTA's work.  Aligned pieces of kPiece sorted tokens that belong to one row
-//     entirely are summed first (fp32 partial rows, one CTA each); a row then adds its head, its partial rows and its
-//     tail.  Work per CTA is bounded by 2 kPiece token rows + tokens / kPiece partial rows.
+//   * sums: a CTA takes kPiece sorted tokens and a block of columns, asks for all of its rows at once and stores the table rows
+//     whose tokens all lie in its piece.  A table row whose tokens go on in the next piece leaves fp32 partial rows (the
+//     part that enters a piece and the part that leaves it), which a second kernel adds in order.  Every token row is read
+//     once, and a CTA's work does not depend on how often an id occurs; only the adding of partial rows of a frequent
+//     id is a chain, of tokens / kPiece rows.
+//   * rows without a token: the sort is latency, not bandwidth, so the whole gradient is filled with zeros by further CTAs of
+//     its kernels meanwhile.
 #include <cmath>
 #include <type_traits>
 
+#include "chained.cuh"
 #include "embed.cuh"
 
 namespace cast {
@@ -22,7 +27,7 @@ namespace {
 
 constexpr int kRun = 1024;          // keys ranked by counting
 constexpr int kWays = 16;           // runs merged at once
-constexpr int kPiece = 64;          // sorted tokens per partial row
+constexpr int kPiece = 16;          // sorted tokens per CTA
 constexpr uint32_t kNoId = 0x7FFFFFFFu;
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -42,8 +47,9 @@ template <> struct Cols<8> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0.0f;
     }
-    __device__ __forceinline__ void add(const uint16_t* p, float c) {
-        const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
+    using Raw = uint4;
+    static __device__ __forceinline__ Raw load(const uint16_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void add(const Raw& x, float c) {
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) { v[2 * i] = fmaf(c, bf16_lo(w[i]), v[2 * i]); v[2 * i + 1] = fmaf(c, bf16_hi(w[i]), v[2 * i + 1]); }
@@ -70,7 +76,9 @@ template <> struct Cols<8> {
 template <> struct Cols<1> {
     float v;
     __device__ __forceinline__ void zero() { v = 0.0f; }
-    __device__ __forceinline__ void add(const uint16_t* p, float c) { v = fmaf(c, bf16_lo(__ldg(p)), v); }
+    using Raw = uint16_t;
+    static __device__ __forceinline__ Raw load(const uint16_t* p) { return __ldg(p); }
+    __device__ __forceinline__ void add(Raw x, float c) { v = fmaf(c, bf16_lo(x), v); }
     __device__ __forceinline__ void add_partial(const float* p) { v += __ldg(p); }
     __device__ __forceinline__ void store_partial(float* p) const { *p = v; }
     __device__ __forceinline__ void store(uint16_t* p, float scale, bool accumulate) const {
@@ -120,21 +128,50 @@ embed_kernel(const uint16_t* __restrict__ table, const int32_t* __restrict__ ids
     }
 }
 
+// ------------------------------------------------------------------------------------------------ zeros on the side
+
+// A part of the gradient that CTAs [first, first + blocks) of a kernel fill with zeros.
+struct Fill {
+    uint16_t* dest;
+    int64_t elems;
+    unsigned first, blocks;
+};
+constexpr int64_t kFillElems = 32768;      // per CTA: 64 KB
+
+__device__ __forceinline__ bool filled(const Fill& f)
+{
+    if (blockIdx.x < f.first) return false;
+    const int64_t from = (int64_t)(blockIdx.x - f.first) * kFillElems, to = min(f.elems, from + kFillElems);
+    if (blockIdx.y != 0) return true;
+    const int64_t odd = min(to - from, (int64_t)((16u - ((uint32_t)(uintptr_t)(f.dest + from) & 15u)) & 15u) / 2);      // up to a 16-byte boundary
+    const int64_t vecs = (to - from - odd) / 8;
+    uint4* v = reinterpret_cast<uint4*>(f.dest + from + odd);
+    for (int64_t i = threadIdx.x; i < vecs; i += blockDim.x) v[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int64_t i = threadIdx.x; i < odd; i += blockDim.x) f.dest[from + i] = 0;
+    for (int64_t i = from + odd + 8 * vecs + threadIdx.x; i < to; i += blockDim.x) f.dest[i] = 0;
+    return true;
+}
+
 // ------------------------------------------------------------------------------------------------ order of the tokens
 
-constexpr int kRankThreads = 128;
+constexpr int kRankKeys = 128;        // keys of a run that one CTA places ...
+constexpr int kRankShare = 4;         // ... with this many threads each
 
-__global__ void __launch_bounds__(kRankThreads)
-rank_runs_kernel(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_ids, int32_t* __restrict__ order, int64_t tokens, uint32_t vocab)
+__global__ void __launch_bounds__(kRankKeys * kRankShare)
+rank_runs_kernel(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_ids, int32_t* __restrict__ order, int64_t tokens, uint32_t vocab,
+                 const __grid_constant__ Fill fill)
 {
     __shared__ uint4 keys4[kRun / 4];
     uint32_t* keys = reinterpret_cast<uint32_t*>(keys4);
-    const int64_t run0 = (int64_t)(blockIdx.x / (kRun / kRankThreads)) * kRun;
+    chain_next();
+    if (filled(fill)) return;
+    chain_wait();
+    const int64_t run0 = (int64_t)(blockIdx.x / (kRun / kRankKeys)) * kRun;
     const int len = (int)min((int64_t)kRun, tokens - run0);
-    const int p = (int)(blockIdx.x % (kRun / kRankThreads)) * kRankThreads + (int)threadIdx.x;
-    if (p - (int)threadIdx.x >= len) return;      // uniform over the CTA
+    const int first = (int)(blockIdx.x % (kRun / kRankKeys)) * kRankKeys;
+    if (first >= len) return;             // uniform over the CTA
     const int n4 = (len + 3) / 4;
-    for (int i = threadIdx.x; i < 4 * n4; i += kRankThreads) {
+    for (int i = threadIdx.x; i < 4 * n4; i += kRankKeys * kRankShare) {
         // past the end: larger than every key, so that it comes before none
         uint32_t k = 0xFFFFFFFFu;
         if (i < len) {
@@ -144,49 +181,59 @@ rank_runs_kernel(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_i
         keys[i] = k;
     }
     __syncthreads();
-    if (p >= len) return;
+    const int p = min(first + (int)threadIdx.x / kRankShare, len - 1), share = (int)threadIdx.x % kRankShare;
     const uint32_t k = keys[p];
     const int own = p >> 2;
     int place = 0;
 #pragma unroll 4
-    for (int v = 0; v < n4; ++v) {
+    for (int v = share; v < n4; v += kRankShare) {
         const uint4 o = keys4[v];
         const uint32_t limit = k + (v < own ? 1u : 0u);      // equal keys before this one count, equal keys after it do not
         place += (o.x < limit) + (o.y < limit) + (o.z < limit) + (o.w < limit);
     }
-    for (int j = 4 * own; j < p; ++j) place += keys[j] == k;
-    sorted_ids[run0 + place] = (int32_t)k;
-    order[run0 + place] = (int32_t)(run0 + p);
+    if (share == 0)
+        for (int j = 4 * own; j < p; ++j) place += keys[j] == k;
+#pragma unroll
+    for (int d = 1; d < kRankShare; d *= 2) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
+    if (share == 0 && first + (int)threadIdx.x / kRankShare < len) {
+        sorted_ids[run0 + place] = (int32_t)k;
+        order[run0 + place] = (int32_t)(run0 + p);
+    }
 }
 
-constexpr int kMergeThreads = 256;
+constexpr int kMergeThreads = 128;
 
-// Merges groups of kWays runs of `run` keys.
+// Merges groups of kWays runs of `run` keys.  The searches of a key advance together and without branches: kWays
+// independent loads per halving.
 __global__ void __launch_bounds__(kMergeThreads)
 merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict__ order_in, int32_t* __restrict__ ids_out,
-                  int32_t* __restrict__ order_out, int64_t tokens, int64_t run)
+                  int32_t* __restrict__ order_out, int32_t tokens, int32_t run, const __grid_constant__ Fill fill)
 {
-    const int64_t i = (int64_t)blockIdx.x * kMergeThreads + threadIdx.x;
+    chain_next();
+    if (filled(fill)) return;
+    chain_wait();
+    const int32_t i = (int32_t)blockIdx.x * kMergeThreads + (int32_t)threadIdx.x;
     if (i >= tokens) return;
-    const int64_t group0 = i / (run * kWays) * (run * kWays);
-    const int own = (int)((i - group0) / run);
+    const int64_t group = (int64_t)run * kWays;
+    const int32_t group0 = (int32_t)(i / group * group);
+    const int own = (i - group0) / run;
     const uint32_t k = (uint32_t)ids_in[i];
-    uint32_t pos[kWays];
+    const int32_t left = tokens - group0;            // keys of the group, and of the groups after it
+    int32_t pos[kWays];
 #pragma unroll
-    for (int j = 0; j < kWays; ++j) pos[j] = 0u;
-    for (uint32_t half = (uint32_t)run; half; half >>= 1) {
+    for (int j = 0; j < kWays; ++j) pos[j] = 0;
+    for (int32_t half = run; half; half >>= 1) {
 #pragma unroll
         for (int j = 0; j < kWays; ++j) {
-            const int64_t start = group0 + j * run;
-            const int64_t len = min(run, tokens - start);      // not positive past the last run
-            const uint32_t at = pos[j] + half;
-            if (j != own && (int64_t)at <= len) {
-                const uint32_t limit = k + (j < own ? 1u : 0u);
-                if ((uint32_t)__ldg(ids_in + start + at - 1) < limit) pos[j] = at;
-            }
+            const int64_t before = (int64_t)j * run;                 // keys of the group ahead of run j
+            const int32_t at = pos[j] + half;
+            const bool there = at <= run && before + at <= left;
+            const uint32_t limit = j == own ? 0u : k + (j < own ? 1u : 0u);
+            const uint32_t other = (uint32_t)__ldg(ids_in + group0 + (there ? (int32_t)before + at - 1 : 0));
+            pos[j] = there && other < limit ? at : pos[j];
         }
     }
-    int64_t to = group0 + (i - group0 - own * run);
+    int64_t to = (int64_t)group0 + (i - group0 - own * run);
 #pragma unroll
     for (int j = 0; j < kWays; ++j) to += pos[j];
     ids_out[to] = (int32_t)k;
@@ -202,122 +249,143 @@ struct ScatterArgs {
     const float* coef;            // per token, or nullptr
     const int32_t* ids;           // sorted
     const int32_t* order;
-    float* partial;               // [tokens / kPiece][dim]
+    float* partial;               // [pieces][2][dim]: what enters a piece, what leaves it
     uint16_t* dest;
-    int64_t tokens, vocab, dim;
+    int64_t dim;
+    int32_t tokens, pieces;
     float scale;
-    int lanes;                    // threads per row (a power of two)
+    int lanes;                    // threads per row: 32 .. 256, a power of two
+    int accumulate;
 };
 
-template <int VEC, bool COEF>
-__device__ __forceinline__ void add_tokens(Cols<VEC>& acc, const ScatterArgs& a, int64_t s, int64_t e, int64_t col)
+// Column of this thread: a.lanes threads per row, the rest of a long row in blockIdx.y.
+template <int VEC>
+__device__ __forceinline__ int32_t column_of(const ScatterArgs& a)
 {
-#pragma unroll 4
-    for (int64_t p = s; p < e; ++p) {
-        const int64_t t = __ldg(a.order + p);
-        acc.add(a.src + t * a.dim + col, COEF ? __ldg(a.coef + t) : 1.0f);
-    }
+    return ((int32_t)blockIdx.y * a.lanes + (int)threadIdx.x % a.lanes) * VEC;
 }
 
-// Partial rows of the aligned pieces that lie inside one table row's tokens.
+// One piece of kPiece sorted tokens per group of a.lanes threads.
 template <int VEC, bool COEF>
-__global__ void __launch_bounds__(kScatterThreads)
+__global__ void __launch_bounds__(kScatterThreads, 3)
 piece_sums_kernel(const __grid_constant__ ScatterArgs a)
 {
-    const int64_t s = (int64_t)blockIdx.x * kPiece;
-    const int32_t id = a.ids[s];
-    if (id != a.ids[s + kPiece - 1] || (uint32_t)id == kNoId) return;
-    for (int64_t col = (int64_t)threadIdx.x * VEC; col < a.dim; col += kScatterThreads * VEC) {
-        Cols<VEC> acc;
-        acc.zero();
-        add_tokens<VEC, COEF>(acc, a, s, s + kPiece, col);
-        acc.store_partial(a.partial + (int64_t)blockIdx.x * a.dim + col);
+    constexpr int kBatch = 8;             // token rows asked for at a time
+    chain_next();
+    chain_wait();
+    const int32_t piece = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
+    if (piece >= a.pieces) return;
+    const int32_t col = column_of<VEC>(a);
+    if (col >= a.dim) return;
+    const int32_t p0 = piece * kPiece, n = min(kPiece, a.tokens - p0);
+    // the ids of the piece, the one before it and the one after it; 0xFFFFFFFF where there is none
+    uint32_t id[kPiece + 2];
+    int32_t t[kPiece];
+#pragma unroll
+    for (int i = 0; i < kPiece + 2; ++i) {
+        const int32_t p = p0 + i - 1;
+        id[i] = p >= 0 && p < a.tokens ? (uint32_t)__ldg(a.ids + p) : 0xFFFFFFFFu;
     }
-}
-
-template <int VEC, bool COEF>
-__device__ __forceinline__ void sum_row(const ScatterArgs& a, int64_t row, int64_t s, int64_t e, int lane, bool accumulate)
-{
-    const int64_t p0 = (s + kPiece - 1) / kPiece, p1 = e / kPiece;      // whole pieces [p0, p1)
-    for (int64_t col = (int64_t)lane * VEC; col < a.dim; col += (int64_t)a.lanes * VEC) {
-        Cols<VEC> acc;
-        acc.zero();
-        if (p0 < p1) {
-            add_tokens<VEC, COEF>(acc, a, s, p0 * kPiece, col);
-#pragma unroll 4
-            for (int64_t p = p0; p < p1; ++p) acc.add_partial(a.partial + p * a.dim + col);
-            add_tokens<VEC, COEF>(acc, a, p1 * kPiece, e, col);
-        } else {
-            add_tokens<VEC, COEF>(acc, a, s, e, col);
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) t[i] = i < n && id[i + 1] != kNoId ? __ldg(a.order + p0 + i) : -1;
+    const uint16_t* src = a.src + col;
+    float* partial = a.partial + (int64_t)piece * 2 * a.dim + col;
+    bool entered = id[0] == id[1];        // the current row's tokens began in an earlier piece
+    Cols<VEC> acc;
+    acc.zero();
+#pragma unroll
+    for (int b = 0; b < kPiece; b += kBatch) {
+        typename Cols<VEC>::Raw x[kBatch];
+        float c[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            c[i] = 1.0f;
+            if (t[b + i] >= 0) {
+                x[i] = Cols<VEC>::load(src + (int64_t)t[b + i] * a.dim);
+                if constexpr (COEF) c[i] = __ldg(a.coef + t[b + i]);
+            }
         }
-        acc.store(a.dest + row * a.dim + col, a.scale, accumulate);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (t[b + i] < 0) continue;
+            acc.add(x[i], c[i]);
+            const uint32_t own = id[b + i + 1];
+            if (id[b + i + 2] != own) {                    // its last token
+                if (entered) acc.store_partial(partial);
+                else acc.store(a.dest + (int64_t)own * a.dim + col, a.scale, a.accumulate);
+                entered = false;
+                acc.zero();
+            } else if (b + i == kPiece - 1) {              // goes on in the next piece
+                acc.store_partial(entered ? partial : partial + a.dim);
+            }
+        }
     }
 }
 
-// first sorted position with an id of at least `id`
-__device__ __forceinline__ int64_t lower_bound(const int32_t* ids, int64_t n, int64_t id)
+// End of the positions after p that hold the id at p.  All lanes of a warp ask for the same p: 32 positions per load.
+__device__ __forceinline__ int32_t end_of(const int32_t* ids, int32_t n, int32_t p, int32_t id)
 {
-    int64_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if ((int64_t)__ldg(ids + mid) < id) lo = mid + 1; else hi = mid;
+    const int lane = (int)threadIdx.x & 31;
+    int32_t lo = p + 1, step = 1;                          // [p, lo) hold it
+    for (;;) {                                             // strides of 1, 32, 1024, ... positions until one ends it
+        const int64_t at = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
+        const int same = __popc(__ballot_sync(0xFFFFFFFFu, at < n && __ldg(ids + at) == id));
+        lo += same * step;
+        if (same < 32) break;
+        step *= 32;
+    }
+    while (step > 1) {                                     // then 32 times finer inside the stride that did
+        step /= 32;
+        const int64_t at = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
+        lo += __popc(__ballot_sync(0xFFFFFFFFu, at < n && __ldg(ids + at) == id)) * step;
     }
     return lo;
 }
 
-constexpr int kRowsPerLaneGroup = 8;
-
-// Every table row, the ones without a token as zeros.  A CTA takes kRowsPerLaneGroup rows per group of a.lanes threads.
-template <int VEC, bool COEF>
+// The table rows that leave a piece they began in: what left it, then what entered the pieces after it.
+template <int VEC>
 __global__ void __launch_bounds__(kScatterThreads)
-scatter_dense_kernel(const __grid_constant__ ScatterArgs a)
+join_pieces_kernel(const __grid_constant__ ScatterArgs a)
 {
-    const int groups = kScatterThreads / a.lanes;
-    const int rows = groups * kRowsPerLaneGroup;
-    __shared__ int64_t bound[kScatterThreads * kRowsPerLaneGroup + 1];
-    const int64_t row0 = (int64_t)blockIdx.x * rows;
-    for (int i = threadIdx.x; i <= rows; i += kScatterThreads) bound[i] = lower_bound(a.ids, a.tokens, min(row0 + i, a.vocab));
-    __syncthreads();
-    const int group = (int)threadIdx.x / a.lanes, lane = (int)threadIdx.x % a.lanes;
-    for (int i = group; i < rows; i += groups)
-        if (row0 + i < a.vocab) sum_row<VEC, COEF>(a, row0 + i, bound[i], bound[i + 1], lane, false);
+    chain_next();
+    chain_wait();
+    const int32_t piece = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
+    const int32_t p0 = piece * kPiece, last = p0 + kPiece - 1;
+    if (piece + 1 >= a.pieces) return;                     // the last piece: nothing leaves it
+    const int32_t id = __ldg(a.ids + last);
+    if ((uint32_t)id == kNoId || __ldg(a.ids + last + 1) != id || (p0 > 0 && __ldg(a.ids + p0 - 1) == id)) return;
+    const int32_t e = end_of(a.ids, a.tokens, last, id);
+    const int32_t col = column_of<VEC>(a);
+    if (col >= a.dim) return;
+    Cols<VEC> acc;
+    acc.zero();
+    const float* p = a.partial + (int64_t)piece * 2 * a.dim + col;
+    acc.add_partial(p + a.dim);
+    const int32_t count = (e - 1) / kPiece - piece;
+#pragma unroll 8
+    for (int32_t i = 0; i < count; ++i) {
+        p += 2 * a.dim;
+        acc.add_partial(p);
+    }
+    acc.store(a.dest + (int64_t)id * a.dim + col, a.scale, a.accumulate);
 }
 
-// Only the rows with a token, added to what is there.  A CTA looks at kRowsPerLaneGroup sorted positions per group of
-// threads; a position that begins a row's tokens does that row.
-template <int VEC, bool COEF>
-__global__ void __launch_bounds__(kScatterThreads)
-scatter_touched_kernel(const __grid_constant__ ScatterArgs a)
+// Part `i` of `n` equal parts of a gradient, whole CTAs of zeros each.
+Fill fill_part(uint16_t* dest, int64_t elems, int i, int n, unsigned first)
 {
-    const int groups = kScatterThreads / a.lanes;
-    const int group = (int)threadIdx.x / a.lanes, lane = (int)threadIdx.x % a.lanes;
-    const int64_t first = (int64_t)blockIdx.x * groups * kRowsPerLaneGroup;
-    for (int i = group; i < groups * kRowsPerLaneGroup; i += groups) {
-        const int64_t p = first + i;
-        if (p >= a.tokens) break;
-        const int32_t id = __ldg(a.ids + p);
-        if ((uint32_t)id == kNoId || (p > 0 && __ldg(a.ids + p - 1) == id)) continue;
-        int64_t e = p + 1;
-        if (e < a.tokens && __ldg(a.ids + e) == id) e = lower_bound(a.ids, a.tokens, (int64_t)id + 1);
-        sum_row<VEC, COEF>(a, id, p, e, lane, true);
-    }
+    const int64_t blocks = (elems + kFillElems - 1) / kFillElems, from = blocks * i / n, to = blocks * (i + 1) / n;
+    const int64_t start = from * kFillElems, stop = to * kFillElems < elems ? to * kFillElems : elems;
+    return {dest + start, stop - start, first, (unsigned)(to - from)};
 }
 
 template <int VEC, bool COEF>
-int launch_scatter(const ScatterArgs& a, bool accumulate, cudaStream_t stream)
+int launch_scatter(const ScatterArgs& a, cudaStream_t stream)
 {
-    if (a.tokens >= kPiece) {
-        const int64_t pieces = a.tokens / kPiece;
-        piece_sums_kernel<VEC, COEF><<<(unsigned)pieces, kScatterThreads, 0, stream>>>(a);
-        CAST_CUDA_TRY(cudaGetLastError());
-        count_launch();
-    }
-    const int64_t per = (int64_t)kScatterThreads / a.lanes * kRowsPerLaneGroup;
-    if (accumulate) scatter_touched_kernel<VEC, COEF><<<(unsigned)((a.tokens + per - 1) / per), kScatterThreads, 0, stream>>>(a);
-    else scatter_dense_kernel<VEC, COEF><<<(unsigned)((a.vocab + per - 1) / per), kScatterThreads, 0, stream>>>(a);
-    CAST_CUDA_TRY(cudaGetLastError());
-    count_launch();
-    return CAST_OK;
+    const int64_t units = (a.dim + VEC - 1) / VEC, groups = kScatterThreads / a.lanes;
+    const dim3 grid((unsigned)((a.pieces + groups - 1) / groups), (unsigned)((units + a.lanes - 1) / a.lanes));
+    const int rc = launch_chained(false, piece_sums_kernel<VEC, COEF>, grid, kScatterThreads, 0, stream, 1, a);
+    if (rc != CAST_OK || a.pieces < 2) return rc;
+    return launch_chained(false, join_pieces_kernel<VEC>, grid, kScatterThreads, 0, stream, 1, a);
 }
 
 int64_t sort_array_bytes(int64_t tokens) { return (int64_t)align256(4ull * (uint64_t)tokens); }
@@ -327,52 +395,64 @@ int64_t sort_array_bytes(int64_t tokens) { return (int64_t)align256(4ull * (uint
 uint64_t scatter_scratch_bytes(int64_t tokens, int64_t dim)
 {
     // two copies of (sorted ids, order), then the partial rows
-    return 4ull * (uint64_t)sort_array_bytes(tokens) + align256(4ull * (uint64_t)(tokens / kPiece) * (uint64_t)dim);
+    return 4ull * (uint64_t)sort_array_bytes(tokens) + align256(8ull * (uint64_t)((tokens + kPiece - 1) / kPiece) * (uint64_t)dim);
 }
 
-int sort_tokens(const int32_t* ids, int64_t tokens, int64_t vocab, int64_t, void* scratch, const int32_t** sorted_ids,
-                const int32_t** order, cudaStream_t stream)
+int sort_tokens(bool first, const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, uint16_t* zeros, SortedTokens* sorted,
+                cudaStream_t stream)
 {
     const int64_t step = sort_array_bytes(tokens);
     uint8_t* b = static_cast<uint8_t*>(scratch);
     int32_t* id_buf[2] = {reinterpret_cast<int32_t*>(b), reinterpret_cast<int32_t*>(b + 2 * step)};
     int32_t* or_buf[2] = {reinterpret_cast<int32_t*>(b + step), reinterpret_cast<int32_t*>(b + 3 * step)};
-    const int64_t runs = (tokens + kRun - 1) / kRun;
-    rank_runs_kernel<<<(unsigned)(runs * (kRun / kRankThreads)), kRankThreads, 0, stream>>>(ids, id_buf[0], or_buf[0], tokens, (uint32_t)vocab);
-    CAST_CUDA_TRY(cudaGetLastError());
-    count_launch();
+    int kernels = 1, done = 0;            // that share the filling: the ranking and the merges
+    for (int64_t run = kRun; run < tokens; run *= kWays) ++kernels;
+    auto part = [&](unsigned own) {
+        const Fill f = zeros ? fill_part(zeros, vocab * dim, done, kernels, own) : Fill{nullptr, 0, own, 0};
+        ++done;
+        return f;
+    };
+    const unsigned rank_blocks = (unsigned)((tokens + kRun - 1) / kRun * (kRun / kRankKeys));
+    Fill f = part(rank_blocks);
+    int rc = launch_chained(first, rank_runs_kernel, dim3(rank_blocks + f.blocks), kRankKeys * kRankShare, 0, stream, 1, ids, id_buf[0], or_buf[0], tokens,
+                            (uint32_t)vocab, f);
+    if (rc != CAST_OK) return rc;
     int cur = 0;
     for (int64_t run = kRun; run < tokens; run *= kWays, cur ^= 1) {
-        merge_runs_kernel<<<(unsigned)((tokens + kMergeThreads - 1) / kMergeThreads), kMergeThreads, 0, stream>>>(
-            id_buf[cur], or_buf[cur], id_buf[cur ^ 1], or_buf[cur ^ 1], tokens, run);
-        CAST_CUDA_TRY(cudaGetLastError());
-        count_launch();
+        const unsigned own = (unsigned)((tokens + kMergeThreads - 1) / kMergeThreads);
+        f = part(own);
+        rc = launch_chained(false, merge_runs_kernel, dim3(own + f.blocks), kMergeThreads, 0, stream, 1, id_buf[cur], or_buf[cur], id_buf[cur ^ 1],
+                            or_buf[cur ^ 1], (int32_t)tokens, (int32_t)run, f);
+        if (rc != CAST_OK) return rc;
     }
-    *sorted_ids = id_buf[cur];
-    *order = or_buf[cur];
+    sorted->ids = id_buf[cur];
+    sorted->order = or_buf[cur];
+    sorted->scratch = b + 4 * step;
+    sorted->tokens = tokens;
     return CAST_OK;
 }
 
-int scatter_rows(const uint16_t* src, const float* coef, float scale, const int32_t* sorted_ids, const int32_t* order, uint16_t* dest,
-                 int64_t tokens, int64_t vocab, int64_t dim, bool accumulate, void* scratch, cudaStream_t stream)
+int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t dim,
+                 bool accumulate, cudaStream_t stream)
 {
     ScatterArgs a;
     a.src = src;
     a.coef = coef;
-    a.ids = sorted_ids;
-    a.order = order;
-    a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + 4 * sort_array_bytes(tokens));
+    a.ids = sorted.ids;
+    a.order = sorted.order;
+    a.partial = static_cast<float*>(sorted.scratch);
     a.dest = dest;
-    a.tokens = tokens;
-    a.vocab = vocab;
+    a.tokens = (int32_t)sorted.tokens;
+    a.pieces = (int32_t)((sorted.tokens + kPiece - 1) / kPiece);
     a.dim = dim;
     a.scale = scale;
+    a.accumulate = accumulate;
     const bool vec = dim % 8 == 0 && !((uintptr_t)src & 15u) && !((uintptr_t)dest & 15u);
     const int64_t units = vec ? dim / 8 : dim;
-    a.lanes = 1;
+    a.lanes = 32;
     while (a.lanes < kScatterThreads && a.lanes < units) a.lanes *= 2;
-    if (vec) return coef ? launch_scatter<8, true>(a, accumulate, stream) : launch_scatter<8, false>(a, accumulate, stream);
-    return coef ? launch_scatter<1, true>(a, accumulate, stream) : launch_scatter<1, false>(a, accumulate, stream);
+    if (vec) return coef ? launch_scatter<8, true>(a, stream) : launch_scatter<8, false>(a, stream);
+    return coef ? launch_scatter<1, true>(a, stream) : launch_scatter<1, false>(a, stream);
 }
 
 }  // namespace cast
@@ -381,10 +461,12 @@ using namespace cast;
 
 namespace {
 
+constexpr int64_t kMostColumns = 1 << 23;      // blocks of 256 accesses of one column each: fewer than 2^16
+
 int check_rows(const void* a, const void* ids, const void* b, int64_t tokens, int64_t vocab, int64_t dim, float scale)
 {
     if (!a || !ids || !b) return CAST_ERR_NULL;
-    if (tokens < 1 || vocab < 1 || dim < 1 || tokens > 0x3FFFFFFF || vocab > 0x7FFFFFFE || dim > 0x7FFFFFFF) return CAST_ERR_SHAPE;
+    if (tokens < 1 || vocab < 1 || dim < 1 || tokens > 0x3FFFFFFF || vocab > 0x7FFFFFFE || dim > kMostColumns) return CAST_ERR_SHAPE;
     if (vocab > ((int64_t)1 << 40) / dim || tokens > ((int64_t)1 << 40) / dim) return CAST_ERR_SHAPE;
     if (!std::isfinite(scale)) return CAST_ERR_HYPER;
     if (((uintptr_t)a & 1u) || ((uintptr_t)b & 1u) || ((uintptr_t)ids & 3u)) return CAST_ERR_ALIGN;
@@ -418,7 +500,7 @@ extern "C" int cast_embed(const cast_bf16* table, const int32_t* ids, cast_bf16*
 extern "C" int cast_embed_grad_workspace(int64_t tokens, int64_t dim, uint64_t* bytes)
 {
     if (!bytes) return CAST_ERR_NULL;
-    if (tokens < 1 || dim < 1 || tokens > 0x3FFFFFFF || tokens > ((int64_t)1 << 40) / dim) return CAST_ERR_SHAPE;
+    if (tokens < 1 || dim < 1 || tokens > 0x3FFFFFFF || dim > kMostColumns || tokens > ((int64_t)1 << 40) / dim) return CAST_ERR_SHAPE;
     *bytes = scatter_scratch_bytes(tokens, dim);
     return CAST_OK;
 }
@@ -439,7 +521,7 @@ extern "C" int cast_embed_grad(const cast_bf16* grad_out, const int32_t* ids, ca
         return CAST_ERR_ALIAS;
     const void* ptrs[4] = {grad_out, ids, grad_table, workspace};
     if ((rc = check_device_memory(ptrs, 4)) != CAST_OK) return rc;
-    const int32_t *sorted, *order;
-    if ((rc = sort_tokens(ids, tokens, vocab, dim, workspace, &sorted, &order, (cudaStream_t)stream)) != CAST_OK) return rc;
-    return scatter_rows(grad_out, nullptr, scale, sorted, order, grad_table, tokens, vocab, dim, accumulate != 0, workspace, (cudaStream_t)stream);
+    SortedTokens sorted;
+    if ((rc = sort_tokens(true, ids, tokens, vocab, dim, workspace, accumulate ? nullptr : grad_table, &sorted, (cudaStream_t)stream)) != CAST_OK) return rc;
+    return scatter_rows(sorted, grad_out, nullptr, scale, grad_table, dim, accumulate != 0, (cudaStream_t)stream);
 }

@@ -8,14 +8,22 @@ namespace cast {
 // Scratch of sort_tokens + scatter_rows over up to `tokens` tokens of width `dim`.
 uint64_t scatter_scratch_bytes(int64_t tokens, int64_t dim);
 
-// Order of the tokens by (id, position); ids outside [0, vocab) come last, as 0x7FFFFFFF.  Both arrays lie in `scratch`.
-int sort_tokens(const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, const int32_t** sorted_ids,
-                const int32_t** order, cudaStream_t stream);
+// The tokens of a call in the order (id, position); ids outside [0, vocab) last, as 0x7FFFFFFF.
+struct SortedTokens {
+    const int32_t* ids;
+    const int32_t* order;
+    void* scratch;          // partial rows
+    int64_t tokens;
+};
 
-// dest[v] = scale * sum_{t: id = v} coef[t] src[t] over the sorted tokens (coef NULL: 1).  accumulate: added to dest, whose
-// rows without a token are left alone; otherwise those rows become zero.
-int scatter_rows(const uint16_t* src, const float* coef, float scale, const int32_t* sorted_ids, const int32_t* order, uint16_t* dest,
-                 int64_t tokens, int64_t vocab, int64_t dim, bool accumulate, void* scratch, cudaStream_t stream);
+// Sorts into `scratch`.  zeros: an array [vocab][dim] that is filled with zeros meanwhile, or NULL.  `first`: the first kernel of the call (see chained.cuh).
+int sort_tokens(bool first, const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, uint16_t* zeros, SortedTokens* sorted,
+                cudaStream_t stream);
+
+// dest[v] = scale * sum_{t: id = v} coef[t] src[t] (coef NULL: 1) for the rows that have a token; accumulate: added to what
+// is there.
+int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t dim, bool accumulate,
+                 cudaStream_t stream);
 
 // Address ranges [a, a + na) and [b, b + nb) share a byte.
 inline bool ranges_overlap(const void* a, uint64_t na, const void* b, uint64_t nb)

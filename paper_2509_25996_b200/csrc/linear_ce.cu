@@ -49,6 +49,7 @@ __global__ void __launch_bounds__(256)
 target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restrict__ weight, const int32_t* __restrict__ labels,
                     float* __restrict__ refs, int64_t tokens, int vocab, int dim)
 {
+    chain_next();
     const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (t >= tokens) return;
     const int lane = (int)threadIdx.x & 31;
@@ -182,6 +183,8 @@ finish_kernel(const __grid_constant__ FinishArgs p)
     __shared__ float part[32][kFinishTokens];
     __shared__ float sh_a[kFinishTokens], sh_ref[kFinishTokens];
     __shared__ int sh_over[kFinishTokens];
+    chain_next();
+    chain_wait();
     const int k = (int)threadIdx.x & 7, lane = (int)threadIdx.x >> 3;
     const int64_t t = (int64_t)blockIdx.x * kFinishTokens + k;
     const bool in = t < p.tokens;
@@ -191,17 +194,22 @@ finish_kernel(const __grid_constant__ FinishArgs p)
 
     // largest reference of the row's tiles (the target logit where none was too large)
     float top2 = ref2;
-    int over = 0;
+    bool over = false;
     float sum = 0.0f;
-    if (active)
+    if (active) {
+#pragma unroll 4
         for (int i = lane; i < p.n_tiles; i += 32) {
             const float v = p.sums[(int64_t)i * p.tokens + t];
-            if (v >= 0.0f) sum += v;
-            else { over = 1; top2 = fmaxf(top2, p.tops[(int64_t)i * p.tokens + t]); }
+            over |= !(v >= 0.0f);
+            sum += v;
         }
-    part[lane][k] = top2;
-    const int any_over = __syncthreads_or(over);
-    if (any_over) {           // rare: bring the tiles of such rows to one reference
+    }
+    if (__syncthreads_or(over)) {           // rare: bring the tiles of such rows to one reference
+        if (over)
+            for (int i = lane; i < p.n_tiles; i += 32)
+                if (!(p.sums[(int64_t)i * p.tokens + t] >= 0.0f)) top2 = fmaxf(top2, p.tops[(int64_t)i * p.tokens + t]);
+        part[lane][k] = top2;
+        __syncthreads();
         for (int i = 0; i < 32; ++i) top2 = fmaxf(top2, part[i][k]);
         __syncthreads();
         sum = 0.0f;
@@ -355,6 +363,8 @@ join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restri
                         const int32_t* __restrict__ labels, const uint16_t* __restrict__ weight, uint16_t* __restrict__ out,
                         int64_t tokens, int dim, int vocab, int splits)
 {
+    chain_next();
+    chain_wait();
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int per = dim / 8;
     if (u >= tokens * per) return;
@@ -364,7 +374,7 @@ join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restri
     uint4 r = make_uint4(0u, 0u, 0u, 0u);
     if ((unsigned)label < (unsigned)vocab) {
         float v[8] = {};
-#pragma unroll 4
+#pragma unroll 8
         for (int s = 0; s < splits; ++s) {
             const float4* p = reinterpret_cast<const float4*>(partial + ((int64_t)s * tokens + t) * dim + c);
             const float4 x = __ldg(p), y = __ldg(p + 1);
@@ -451,7 +461,8 @@ bool paired(int64_t tokens) { return tokens > 128; }
 int64_t tile_cols(int64_t tokens) { return paired(tokens) ? 256 : 128; }
 
 // Splits of the vocabulary for dH: few tokens give few tiles, and each has the whole vocabulary to sum.  The time of
-// `splits` is taken as rounds of tiles x (blocks + 8 for filling and draining the pipeline).
+// `splits` is taken as rounds of tiles x (blocks + 8 for filling and draining the pipeline), in blocks (~0.3 us for a pair),
+// plus writing and reading the partial sums at ~5 TB/s.
 int hidden_splits(int64_t tokens, int64_t vocab, int64_t dim, int sms)
 {
     const bool two = paired(tokens);
@@ -461,7 +472,7 @@ int hidden_splits(int64_t tokens, int64_t vocab, int64_t dim, int sms)
     int64_t best_cost = INT64_MAX;
     for (int s = 1; s <= 64 && s <= blocks; ++s) {
         const int64_t rounds = (tiles * s + units - 1) / units;
-        const int64_t cost = rounds * ((blocks + s - 1) / s + 8) + (s > 1 ? 8 + s / 2 : 0);
+        const int64_t cost = rounds * ((blocks + s - 1) / s + 8) + (s > 1 ? 8 + s * tokens * dim * 8 / (two ? 1500000 : 1000000) : 0);
         if (cost < best_cost) { best_cost = cost; best = s; }
     }
     return best;
@@ -573,10 +584,8 @@ int hidden_product(const Call& c, int64_t t0, int64_t n)
     if ((rc = launch<CG, BN, false, true>(ma, mb, s, epi, c.stream)) != CAST_OK) return rc;
     if (epi.partial) {
         const int64_t units = n * (c.dim / 8);
-        join_hidden_grad_kernel<<<(unsigned)((units + 255) / 256), 256, 0, c.stream>>>(partial, epi.a, epi.b, epi.labels, c.weight,
-                                                                                     c.grad_hidden + t0 * c.dim, n, (int)c.dim, (int)c.vocab, s.splits);
-        CAST_CUDA_TRY(cudaGetLastError());
-        count_launch();
+        return launch_chained(false, join_hidden_grad_kernel, dim3((unsigned)((units + 255) / 256)), 256, 0, c.stream, 1, partial, epi.a, epi.b,
+                              epi.labels, c.weight, c.grad_hidden + t0 * c.dim, n, (int)c.dim, (int)c.vocab, s.splits);
     }
     return CAST_OK;
 }
@@ -654,9 +663,9 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
     float* refs = reinterpret_cast<float*>(ws + l.refs);
     float* a = reinterpret_cast<float*>(ws + l.a);
     float* b = reinterpret_cast<float*>(ws + l.b);
-    target_logit_kernel<<<(unsigned)((tokens + 7) / 8), 256, 0, st>>>(hidden, weight, labels, refs, tokens, (int)vocab, (int)dim);
-    CAST_CUDA_TRY(cudaGetLastError());
-    count_launch();
+    if ((rc = launch_chained(true, target_logit_kernel, dim3((unsigned)((tokens + 7) / 8)), 256, 0, st, 1, hidden, weight, labels, refs, tokens,
+                             (int)vocab, (int)dim)) != CAST_OK)
+        return rc;
     for (int64_t i = 0; i < l.pieces; ++i) {
         const int64_t t0 = i * l.piece, n = tokens - t0 < l.piece ? tokens - t0 : l.piece;
         rc = paired(n) ? exp_product<2, 256>(c, t0, n) : exp_product<1, 128>(c, t0, n);
@@ -680,9 +689,7 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
         f.tile_cols = (int)tile_cols(n);
         f.n_tiles = (int)((vocab + f.tile_cols - 1) / f.tile_cols);
         f.grad_scale = grad_scale;
-        finish_kernel<<<(unsigned)((n + kFinishTokens - 1) / kFinishTokens), 256, 0, st>>>(f);
-        CAST_CUDA_TRY(cudaGetLastError());
-        count_launch();
+        if ((rc = launch_chained(false, finish_kernel, dim3((unsigned)((n + kFinishTokens - 1) / kFinishTokens)), 256, 0, st, 1, f)) != CAST_OK) return rc;
         if (grad_hidden) {
             rc = paired(n) ? hidden_product<2, 256>(c, t0, n) : hidden_product<1, 128>(c, t0, n);
             if (rc != CAST_OK) return rc;
@@ -690,10 +697,10 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
         if (grad_weight && (rc = weight_product(c, n, i == 0, i + 1 == l.pieces)) != CAST_OK) return rc;
     }
     if (grad_weight) {
-        const int32_t *sorted, *order;
-        if ((rc = sort_tokens(labels, tokens, vocab, dim, ws + l.scatter, &sorted, &order, st)) != CAST_OK) return rc;
+        SortedTokens sorted;
+        if ((rc = sort_tokens(false, labels, tokens, vocab, dim, ws + l.scatter, nullptr, &sorted, st)) != CAST_OK) return rc;
         // b holds s S / (1 + S): the label's term of dW is -b H
-        if ((rc = scatter_rows(hidden, b, -1.0f, sorted, order, grad_weight, tokens, vocab, dim, true, ws + l.scatter, st)) != CAST_OK) return rc;
+        if ((rc = scatter_rows(sorted, hidden, b, -1.0f, grad_weight, dim, true, st)) != CAST_OK) return rc;
     }
     return CAST_OK;
 }

@@ -89,6 +89,8 @@ template <bool BF16, int VEC>
 __global__ void __launch_bounds__(256)
 square_sum_kernel(const __grid_constant__ PtrTable updates, double* __restrict__ partial, int64_t units)
 {
+    chain_next();
+    chain_wait();
     const void* u = updates.p[blockIdx.y];
     double sum = 0.0;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
@@ -106,6 +108,8 @@ __global__ void __launch_bounds__(256)
 first_x_kernel(const __grid_constant__ PtrTable updates, const double* __restrict__ partial, int parts, uint16_t* __restrict__ hi,
                uint16_t* __restrict__ lo, int64_t units, uint32_t units_per_row, int64_t ld, int64_t stride, double eps)
 {
+    chain_next();
+    chain_wait();
     const double sum = block_sum((int)threadIdx.x < parts ? partial[(int64_t)blockIdx.y * kNormBlocks + threadIdx.x] : 0.0);
     const double norm = sqrt(sum) + eps;
     const double f = norm > 0.0 ? (double)kX / norm : 0.0;      // not in fp32: 1 / norm of a tiny update leaves its range
@@ -387,23 +391,19 @@ int step_product(const uint16_t* p, const uint16_t* hi, int64_t rows, int64_t co
 }
 
 template <bool BF16, int VEC>
-int launch_first(const PtrTable& t, int64_t batch, int64_t rows, int64_t cols, uint8_t* ws, const Layout& l, float eps, cudaStream_t stream)
+int launch_first(bool first, const PtrTable& t, int64_t batch, int64_t rows, int64_t cols, uint8_t* ws, const Layout& l, float eps, cudaStream_t stream)
 {
     const int64_t units = rows * cols / VEC;
     int64_t parts = (units + 256 * 8 - 1) / (256 * 8);
     if (parts > kNormBlocks) parts = kNormBlocks;
     double* norms = reinterpret_cast<double*>(ws + l.norms);
-    square_sum_kernel<BF16, VEC><<<dim3((unsigned)parts, (unsigned)batch), 256, 0, stream>>>(t, norms, units);
-    CAST_CUDA_TRY(cudaGetLastError());
-    count_launch();
+    int rc = launch_chained(first, square_sum_kernel<BF16, VEC>, dim3((unsigned)parts, (unsigned)batch), 256, 0, stream, 1, t, norms, units);
+    if (rc != CAST_OK) return rc;
     int64_t blocks = (units + 256 * 4 - 1) / (256 * 4);
     if (blocks > 2048) blocks = 2048;
-    first_x_kernel<BF16, VEC><<<dim3((unsigned)blocks, (unsigned)batch), 256, 0, stream>>>(
-        t, norms, (int)parts, reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.lo[0]), units,
-        (uint32_t)(cols / VEC), l.ld, rows * l.ld, (double)eps);
-    CAST_CUDA_TRY(cudaGetLastError());
-    count_launch();
-    return CAST_OK;
+    return launch_chained(false, first_x_kernel<BF16, VEC>, dim3((unsigned)blocks, (unsigned)batch), 256, 0, stream, 1, t, norms, (int)parts,
+                          reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.lo[0]), units, (uint32_t)(cols / VEC), l.ld,
+                          rows * l.ld, (double)eps);
 }
 
 int check_ortho_shape(int64_t n, int64_t rows, int64_t cols)
@@ -498,8 +498,8 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
             out_vec = out_vec && !((uintptr_t)epi.out.p[i] & 15u);
         }
         for (int64_t i = batch; i < kGroup; ++i) { in.p[i] = nullptr; epi.out.p[i] = nullptr; }
-        if (updates_bf16) rc = in_vec ? launch_first<true, 8>(in, batch, rows, cols, ws, l, eps, st) : launch_first<true, 1>(in, batch, rows, cols, ws, l, eps, st);
-        else rc = in_vec ? launch_first<false, 8>(in, batch, rows, cols, ws, l, eps, st) : launch_first<false, 1>(in, batch, rows, cols, ws, l, eps, st);
+        if (updates_bf16) rc = in_vec ? launch_first<true, 8>(first == 0, in, batch, rows, cols, ws, l, eps, st) : launch_first<true, 1>(first == 0, in, batch, rows, cols, ws, l, eps, st);
+        else rc = in_vec ? launch_first<false, 8>(first == 0, in, batch, rows, cols, ws, l, eps, st) : launch_first<false, 1>(first == 0, in, batch, rows, cols, ws, l, eps, st);
         if (rc != CAST_OK) return rc;
         const bool gram2 = use_pairs(l.sq, l.sq, big, batch, true, sms), sq2 = use_pairs(l.sq, l.sq, l.sq, batch, true, sms);
         const bool step2 = use_pairs(rows, cols, l.sq, batch, false, sms);

@@ -23,7 +23,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include "cast_internal.h"
+#include "chained.cuh"
 
 namespace cast {
 namespace product {
@@ -302,6 +302,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
 
+    chain_next();
     if (threadIdx.x == 0) {
         stop_flag = 0;
         for (int i = 0; i < C::stages; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 1); }
@@ -313,6 +314,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __syncthreads();
     if constexpr (CG == 2) cluster_barrier();
     tc_fence_after();
+    chain_wait();
     const uint32_t tmem = tmem_base_smem;
     const Stop stop = {&stop_flag, shape.fail_word};
     const int first = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
@@ -468,21 +470,7 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const Shape& s, const Epi
     if ((rc = sm_count(&sms)) != CAST_OK) return rc;
     CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes));
     const int units = s.total < sms / CG ? s.total : sms / CG;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * CG));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = C::smem_bytes;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    CAST_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, b, s, epi));
-    count_launch();
-    return CAST_OK;
+    return launch_chained(false, kernel, dim3((unsigned)(units * CG)), kThreads, C::smem_bytes, stream, CG, a, b, s, epi);
 }
 
 }  // namespace product
