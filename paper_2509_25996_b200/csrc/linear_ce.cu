@@ -72,8 +72,7 @@ target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restr
 
 // ------------------------------------------------------------------------------------------------ E and its row sums
 
-struct ExpEpi {
-    static constexpr bool kSym = false;
+struct ExpEpi : StoringEpi {
     CUtensorMap map_e;
     const float* refs;           // target logits of the piece
     const int32_t* labels;
@@ -119,8 +118,10 @@ struct ExpEpi {
         return s0 + s1;
     }
 
-    template <int BN>
-    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    __device__ __forceinline__ void prefetch() const { if (write_e) prefetch_map(&map_e); }
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State&) const
     {
         const int row = e.row0 + e.lane;
         int label = -1;
@@ -154,6 +155,7 @@ struct ExpEpi {
             }
         }
         if (row < s.m) sums[(int64_t)e.tile.tn * s.m + row] = sum;
+        return true;
     }
 };
 
@@ -294,8 +296,7 @@ __device__ __forceinline__ void store_f32_row(uint32_t slot, int lane, const flo
 }
 
 // dH tile: a (E W) - b W_label as bf16, or with several splits over the vocabulary the plain sums as fp32.
-struct HiddenGradEpi {
-    static constexpr bool kSym = false;
+struct HiddenGradEpi : StoringEpi {
     CUtensorMap map_out;         // bf16 [tokens][dim], or fp32 [splits][tokens][dim]
     const float* a;
     const float* b;
@@ -303,8 +304,10 @@ struct HiddenGradEpi {
     const uint16_t* weight;
     int vocab, partial;
 
-    template <int BN>
-    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    __device__ __forceinline__ void prefetch() const { prefetch_map(&map_out); }
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State&) const
     {
         if (partial) {
 #pragma unroll 1
@@ -315,7 +318,7 @@ struct HiddenGradEpi {
                 store_f32_row(slot, e.lane, v);
                 slot_store(e, slot, &map_out, e.col0 + c, e.row0, e.tile.split, e.row0 < s.m);
             }
-            return;
+            return true;
         }
         const int row = e.row0 + e.lane;
         float fa = 0.0f, fb = 0.0f;
@@ -354,6 +357,7 @@ struct HiddenGradEpi {
             }
             slot_store(e, slot, &map_out, e.col0 + c, e.row0, 0, e.row0 < s.m);
         }
+        return true;
     }
 };
 
@@ -389,8 +393,7 @@ join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restri
 }
 
 // dW tile: bf16 result after the last piece, fp32 running sums before it.
-struct WeightGradEpi {
-    static constexpr bool kSym = false;
+struct WeightGradEpi : StoringEpi {
     CUtensorMap map_out;         // bf16 [vocab][dim]
     CUtensorMap map_acc;         // fp32 [vocab][dim]
     const float* acc;
@@ -408,8 +411,10 @@ struct WeightGradEpi {
             }
     }
 
-    template <int BN>
-    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    __device__ __forceinline__ void prefetch() const { prefetch_map(last ? &map_out : &map_acc); }
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State&) const
     {
         const int row = e.row0 + e.lane;
         if (last) {
@@ -436,6 +441,7 @@ struct WeightGradEpi {
                 slot_store(e, slot, &map_acc, e.col0 + c, e.row0, 0, e.row0 < s.m);
             }
         }
+        return true;
     }
 };
 
@@ -546,7 +552,7 @@ int exp_product(const Call& c, int64_t t0, int64_t n)
     ExpEpi epi;
     int rc;
     const bool grads = c.grad_hidden || c.grad_weight;
-    if ((rc = make_shape<CG, BN, false, false, false>(&s, true, n, c.vocab, c.dim, 1, 1, 16 / CG)) != CAST_OK) return rc;
+    if ((rc = make_shape<CG, BN, false, false, ExpEpi>(&s, true, n, c.vocab, c.dim, 1, 1, 16 / CG)) != CAST_OK) return rc;
     if ((rc = operand_map<false>(&ma, c.hidden + t0 * c.dim, n, c.dim, 1, c.dim, 0, 128)) != CAST_OK) return rc;
     if ((rc = operand_map<false>(&mb, c.weight, c.vocab, c.dim, 1, c.dim, 0, BN / CG)) != CAST_OK) return rc;
     epi.refs = reinterpret_cast<const float*>(c.ws + l.refs) + t0;
@@ -568,7 +574,7 @@ int hidden_product(const Call& c, int64_t t0, int64_t n)
     HiddenGradEpi epi;
     int rc;
     const int splits = hidden_splits(n, c.vocab, c.dim, c.sms);
-    if ((rc = make_shape<CG, BN, false, true, false>(&s, true, n, c.dim, c.vocab, 1, splits, 16 / CG)) != CAST_OK) return rc;
+    if ((rc = make_shape<CG, BN, false, true, HiddenGradEpi>(&s, true, n, c.dim, c.vocab, 1, splits, 16 / CG)) != CAST_OK) return rc;
     if ((rc = operand_map<false>(&ma, c.ws + l.e, n, c.vocab, 1, l.e_ld, 0, 128)) != CAST_OK) return rc;
     if ((rc = operand_map<true>(&mb, c.weight, c.dim, c.vocab, 1, c.dim, 0, BN / CG)) != CAST_OK) return rc;
     epi.a = reinterpret_cast<const float*>(c.ws + l.a) + t0;
@@ -598,7 +604,7 @@ int weight_product(const Call& c, int64_t n, bool first, bool last)
     Shape s;
     WeightGradEpi epi;
     int rc;
-    if ((rc = make_shape<CG, BN, true, true, false>(&s, true, c.vocab, c.dim, n, 1, 1, 8)) != CAST_OK) return rc;
+    if ((rc = make_shape<CG, BN, true, true, WeightGradEpi>(&s, true, c.vocab, c.dim, n, 1, 1, 8)) != CAST_OK) return rc;
     if ((rc = operand_map<true>(&ma, c.ws + l.e, c.vocab, n, 1, l.e_ld, 0, 128)) != CAST_OK) return rc;
     if ((rc = operand_map<true>(&mb, c.ws + l.scaled, c.dim, n, 1, c.dim, 0, BN / CG)) != CAST_OK) return rc;
     epi.acc = reinterpret_cast<const float*>(c.ws + l.acc);

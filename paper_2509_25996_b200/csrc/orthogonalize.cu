@@ -15,7 +15,6 @@
 // through the products is confined to directions that are large already.  A and P (b A + c A A, without a I) are plain fp16.
 #include <algorithm>
 #include <cmath>
-#include <cstring>
 #include <new>
 
 #include <cuda_fp16.h>
@@ -41,9 +40,8 @@ __device__ __forceinline__ float f16_hi(uint32_t w) { return __half2float(__usho
 // round to nearest, and to the largest finite value beyond the range (coefficients under which X grows without bound)
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
-    const __half2 h = __floats2half2_rn(fminf(fmaxf(lo, -65504.0f), 65504.0f), fminf(fmaxf(hi, -65504.0f), 65504.0f));
     uint32_t r;
-    memcpy(&r, &h, 4);
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 __device__ __forceinline__ uint32_t pack_b16(float lo, float hi)
@@ -137,43 +135,39 @@ first_x_kernel(const __grid_constant__ PtrTable updates, const double* __restric
 
 // ------------------------------------------------------------------------------------------------ epilogues
 
-// 64 columns of fp16 values in fp32 -> this lane's row of a slot
-__device__ __forceinline__ void f16_half_row(uint32_t slot, int lane, int half, const float (&v)[32])
-{
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        slot_write(slot, lane, 4 * half + q, pack_f16(v[8 * q], v[8 * q + 1]), pack_f16(v[8 * q + 2], v[8 * q + 3]),
-                   pack_f16(v[8 * q + 4], v[8 * q + 5]), pack_f16(v[8 * q + 6], v[8 * q + 7]));
-}
-
 // Symmetric result: scale x acc (+ add x aux), stored at (row, col) and, off the diagonal, at (col, row).
 struct SymEpi {
     static constexpr bool kSym = true;
+    static constexpr int kStaging = (kRing + 2) * kSlotBytes;      // the ring, and two slots for the mirrored chunks in turn
+    using State = AuxRing<1>;
     CUtensorMap map_out;         // boxes of 32 rows x 64 columns, swizzled
     CUtensorMap map_mirror;      // the same array, boxes of 64 rows x 32 columns, not swizzled
-    const uint16_t* aux;         // fp16, laid out as the result; nullptr: none
-    int64_t ld, stride;
+    CUtensorMap map_aux;         // fp16, read like map_out
+    int has_aux;
     float scale, add;
 
-    template <int BN>
-    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    __device__ __forceinline__ void prefetch() const
     {
-        const int row = e.row0 + e.lane;
-        const bool mirror = e.tile.tm != e.tile.tn;
+        prefetch_map(&map_out);
+        prefetch_map(&map_mirror);
+        if (has_aux) prefetch_map(&map_aux);
+    }
+    template <int BM, int BN>
+    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
+    {
+        ring.start<true>(s, e);
+        for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, true>(s, e, &map_aux, nullptr, has_aux);
+    }
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
+    {
+        const bool mirror = e.col0 + BN <= e.tile.tm * BM;
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
-            uint4 x[8];
-            if (aux && row < s.m) {
-                // rows are padded to whole 128-byte lines: reading past the last column stays inside the row
-                const uint4* p = reinterpret_cast<const uint4*>(aux + (int64_t)e.tile.batch * stride + (int64_t)row * ld + n);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) x[q] = __ldg(p + q);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) x[q] = make_uint4(0u, 0u, 0u, 0u);
-            }
-            const uint32_t slot = slot_acquire(e);
+            const uint32_t slot = ring.slot(e, ring.step, 0);
+            if (has_aux && !ring.wait(e)) return false;
             uint32_t packed[32];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -181,106 +175,116 @@ struct SymEpi {
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint4 w = x[4 * h + q];
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                    uint32_t* p = packed + 16 * h + 4 * q;
+                    if (has_aux) {
+                        const uint4 w = slot_read(slot, e.lane, 4 * h + q);
+                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float lo = scale * v[8 * q + 2 * i], hi = scale * v[8 * q + 2 * i + 1];
-                        packed[16 * h + 4 * q + i] = aux ? pack_f16(fmaf(add, f16_lo(u[i]), lo), fmaf(add, f16_hi(u[i]), hi)) : pack_f16(lo, hi);
+                        for (int i = 0; i < 4; ++i)
+                            p[i] = pack_f16(fmaf(add, f16_lo(u[i]), scale * v[8 * q + 2 * i]), fmaf(add, f16_hi(u[i]), scale * v[8 * q + 2 * i + 1]));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[i] = pack_f16(scale * v[8 * q + 2 * i], scale * v[8 * q + 2 * i + 1]);
                     }
-                    slot_write(slot, e.lane, 4 * h + q, packed[16 * h + 4 * q], packed[16 * h + 4 * q + 1], packed[16 * h + 4 * q + 2], packed[16 * h + 4 * q + 3]);
+                    slot_write(slot, e.lane, 4 * h + q, p[0], p[1], p[2], p[3]);
                 }
             }
-            slot_store(e, slot, &map_out, n, e.row0, e.tile.batch, e.row0 < s.m);
+            const uint32_t t = e.slots + (uint32_t)((kRing + e.slot) * kSlotBytes);
             if (mirror) {
                 // rows of 32 elements (64 bytes): column j of the chunk becomes row j, this lane its element
-                const uint32_t t = slot_acquire(e);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
                     const uint32_t at = t + (uint32_t)(2 * j) * 64u + (uint32_t)e.lane * 2u;
                     asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((unsigned short)(packed[j] & 0xFFFFu)) : "memory");
                     asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 64u), "h"((unsigned short)(packed[j] >> 16)) : "memory");
                 }
-                slot_store(e, t, &map_mirror, e.row0, n, e.tile.batch, e.row0 < s.m);
+                e.slot ^= 1;
             }
+            fence_async_smem();
+            __syncwarp();
+            if (e.lane == 0) {
+                if (e.row0 < s.m) {
+                    tma_store(&map_out, slot, n, e.row0, e.tile.batch);
+                    if (mirror) tma_store(&map_mirror, t, e.row0, n, e.tile.batch);
+                }
+                store_commit();
+                store_wait_read<1>();      // the chunk before this one has left: its step and its mirror slot are free
+            }
+            __syncwarp();
+            ring.next();
+            ring.load<BM, BN, true>(s, e, &map_aux, nullptr, has_aux);
         }
+        return true;
     }
 };
 
 // X' = a X + acc: two fp16 words per entry, or after the last step bf16(scale X').
 struct StepEpi {
     static constexpr bool kSym = false;
-    CUtensorMap map_hi, map_lo;      // outputs
-    const uint16_t* hi;
-    const uint16_t* lo;
-    int64_t ld, stride;
+    static constexpr int kStaging = kRing * 2 * kSlotBytes;
+    using State = AuxRing<2>;
+    CUtensorMap map_hi, map_lo;            // X'
+    CUtensorMap map_hi_in, map_lo_in;      // X
     OutTable out;
     float a, scale;
     int last, vec;
 
-    template <int BN>
-    __device__ __forceinline__ void tile(const Shape& s, EpiTile& e) const
+    __device__ __forceinline__ void prefetch() const
     {
-        const int row = e.row0 + e.lane;
-        const int64_t at = (int64_t)e.tile.batch * stride + (int64_t)row * ld;
+        prefetch_map(&map_hi_in);
+        prefetch_map(&map_lo_in);
+        if (!last) {
+            prefetch_map(&map_hi);
+            prefetch_map(&map_lo);
+        }
+    }
+    template <int BM, int BN>
+    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
+    {
+        ring.start<false>(s, e);
+        for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, false>(s, e, &map_hi_in, &map_lo_in, 2);
+    }
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
+    {
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
-            const uint32_t slot_hi = slot_acquire(e);
-            uint32_t slot_lo = 0;
-            if (!last) {
-                if (e.lane == 0) store_wait_read<0>();
-                __syncwarp();
-                slot_lo = e.slots + (uint32_t)(e.slot * kSlotBytes);
-                e.slot = (e.slot + 1) % kSlotsPerWarp;
-            }
+            const uint32_t hi = ring.slot(e, ring.step, 0), lo = ring.slot(e, ring.step, 1);
+            if (!ring.wait(e)) return false;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                uint4 x[4], y[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) { x[q] = make_uint4(0u, 0u, 0u, 0u); y[q] = x[q]; }
-                if (row < s.m) {
-                    const uint4* p = reinterpret_cast<const uint4*>(hi + at + n) + 4 * h;
-                    const uint4* r = reinterpret_cast<const uint4*>(lo + at + n) + 4 * h;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) { x[q] = __ldg(p + q); y[q] = __ldg(r + q); }
-                }
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint32_t u[4] = {x[q].x, x[q].y, x[q].z, x[q].w}, w[4] = {y[q].x, y[q].y, y[q].z, y[q].w};
+                    const uint4 x = slot_read(hi, e.lane, 4 * h + q), y = slot_read(lo, e.lane, 4 * h + q);
+                    const uint32_t u[4] = {x.x, x.y, x.z, x.w}, w[4] = {y.x, y.y, y.z, y.w};
+                    uint32_t r[4], d[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float& l = v[8 * q + 2 * i];
-                        float& g = v[8 * q + 2 * i + 1];
-                        l = fmaf(a, f16_lo(u[i]) + f16_lo(w[i]), l);
-                        g = fmaf(a, f16_hi(u[i]) + f16_hi(w[i]), g);
+                        const float g0 = fmaf(a, f16_lo(u[i]) + f16_lo(w[i]), v[8 * q + 2 * i]);
+                        const float g1 = fmaf(a, f16_hi(u[i]) + f16_hi(w[i]), v[8 * q + 2 * i + 1]);
+                        if (last) {
+                            r[i] = pack_b16(scale * g0, scale * g1);
+                        } else {
+                            r[i] = pack_f16(g0, g1);
+                            d[i] = pack_f16(g0 - f16_lo(r[i]), g1 - f16_hi(r[i]));
+                        }
                     }
-                }
-                if (last) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        slot_write(slot_hi, e.lane, 4 * h + q, pack_b16(scale * v[8 * q], scale * v[8 * q + 1]),
-                                   pack_b16(scale * v[8 * q + 2], scale * v[8 * q + 3]), pack_b16(scale * v[8 * q + 4], scale * v[8 * q + 5]),
-                                   pack_b16(scale * v[8 * q + 6], scale * v[8 * q + 7]));
-                } else {
-                    f16_half_row(slot_hi, e.lane, h, v);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-                    f16_half_row(slot_lo, e.lane, h, v);
+                    slot_write(hi, e.lane, 4 * h + q, r[0], r[1], r[2], r[3]);
+                    if (!last) slot_write(lo, e.lane, 4 * h + q, d[0], d[1], d[2], d[3]);
                 }
             }
             if (last) {
                 // rows of the caller's matrix may have any length: whole rows of the slot by ordinary stores
                 __syncwarp();
                 uint16_t* o = out.p[e.tile.batch];
-#pragma unroll 1
+#pragma unroll 4
                 for (int r0 = 0; r0 < 32; r0 += 4) {
                     const int r = r0 + (e.lane >> 3), q = e.lane & 7;
-                    uint4 w;
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                                 : "r"(slot_hi + (uint32_t)r * 128u + (uint32_t)((q ^ (r & 7)) << 4)));
+                    const uint4 w = slot_read(hi, r, q);
                     if (e.row0 + r >= s.m) continue;
                     uint16_t* to = o + (int64_t)(e.row0 + r) * s.n + n + 8 * q;
                     if (vec) {
@@ -293,12 +297,23 @@ struct StepEpi {
                     }
                 }
                 __syncwarp();
-                if (e.lane == 0) store_commit();
             } else {
-                slot_store(e, slot_hi, &map_hi, n, e.row0, e.tile.batch, e.row0 < s.m);
-                slot_store(e, slot_lo, &map_lo, n, e.row0, e.tile.batch, e.row0 < s.m);
+                fence_async_smem();
+                __syncwarp();
+                if (e.lane == 0) {
+                    if (e.row0 < s.m) {
+                        tma_store(&map_hi, hi, n, e.row0, e.tile.batch);
+                        tma_store(&map_lo, lo, n, e.row0, e.tile.batch);
+                    }
+                    store_commit();
+                    store_wait_read<1>();      // the chunk before this one has left its step
+                }
+                __syncwarp();
             }
+            ring.next();
+            ring.load<BM, BN, false>(s, e, &map_hi_in, &map_lo_in, 2);
         }
+        return true;
     }
 };
 
@@ -353,29 +368,30 @@ int sym_product(const uint16_t* x, int64_t mn, int64_t k, int64_t batch, int64_t
     SymEpi epi;
     int rc;
     const int64_t stride = l.sq * l.sq_ld;
-    if ((rc = make_shape<CG, BN, MN, MN, true>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
+    if ((rc = make_shape<CG, BN, MN, MN, SymEpi>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
     if ((rc = operand_map<MN>(&m, x, mn, k, batch, x_ld, x_stride, 128)) != CAST_OK) return rc;
-    static_assert(BN / CG == 128, "one map serves both operands");
+    CUtensorMap mb = m;
+    if (BN / CG != 128 && (rc = operand_map<MN>(&mb, x, mn, k, batch, x_ld, x_stride, BN / CG)) != CAST_OK) return rc;
     if ((rc = make_map(&epi.map_out, out, 2, mn, mn, batch, l.sq_ld, stride, 64, 32, true)) != CAST_OK) return rc;
     if ((rc = make_map(&epi.map_mirror, out, 2, mn, mn, batch, l.sq_ld, stride, 32, 64, false)) != CAST_OK) return rc;
-    epi.aux = aux;
-    epi.ld = l.sq_ld;
-    epi.stride = stride;
+    epi.has_aux = aux != nullptr;
+    epi.map_aux = epi.map_out;
+    if (aux && (rc = make_map(&epi.map_aux, aux, 2, mn, mn, batch, l.sq_ld, stride, 64, 32, true)) != CAST_OK) return rc;
     epi.scale = scale;
     epi.add = add;
-    return launch<CG, BN, MN, MN>(m, m, s, epi, stream);
+    return launch<CG, BN, MN, MN>(m, mb, s, epi, stream);
 }
 
 // X' = a X + P X (wide) or a X + X P (tall)
 template <int CG, int BN, bool WIDE>
-int step_product(const uint16_t* p, const uint16_t* hi, int64_t rows, int64_t cols, int64_t batch, const Layout& l, uint16_t* hi_out,
+int step_product(const uint16_t* p, const uint16_t* hi, const uint16_t* lo, int64_t rows, int64_t cols, int64_t batch, const Layout& l, uint16_t* hi_out,
                  uint16_t* lo_out, StepEpi& epi, cudaStream_t stream)
 {
     CUtensorMap ma, mb;
     Shape s;
     int rc;
     const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
-    if ((rc = make_shape<CG, BN, false, WIDE, false>(&s, false, rows, cols, l.sq, batch, 1, 16 / CG)) != CAST_OK) return rc;
+    if ((rc = make_shape<CG, BN, false, WIDE, StepEpi>(&s, false, rows, cols, l.sq, batch, 1, 16 / CG)) != CAST_OK) return rc;
     if (WIDE) {
         if ((rc = operand_map<false>(&ma, p, rows, rows, batch, l.sq_ld, ps, 128)) != CAST_OK) return rc;
         if ((rc = operand_map<true>(&mb, hi, cols, rows, batch, l.ld, xs, BN / CG)) != CAST_OK) return rc;
@@ -385,8 +401,8 @@ int step_product(const uint16_t* p, const uint16_t* hi, int64_t rows, int64_t co
     }
     if ((rc = make_map(&epi.map_hi, hi_out, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
     if ((rc = make_map(&epi.map_lo, lo_out, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
-    epi.ld = l.ld;
-    epi.stride = xs;
+    if ((rc = make_map(&epi.map_hi_in, hi, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
+    if ((rc = make_map(&epi.map_lo_in, lo, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
     return launch<CG, BN, false, WIDE>(ma, mb, s, epi, stream);
 }
 
@@ -516,16 +532,14 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
             rc = sq2 ? sym_product<2, 256, false>(a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, a, q[2], q[1], st)
                      : sym_product<1, 128, false>(a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, a, q[2], q[1], st);
             if (rc != CAST_OK) return rc;
-            epi.hi = hi[cur];
-            epi.lo = lo[cur];
             epi.a = q[0];
             epi.scale = scale / kX;
             epi.last = k + 1 == steps;
             epi.vec = out_vec;
-            if (wide) rc = step2 ? step_product<2, 256, true>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
-                                 : step_product<1, 128, true>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
-            else rc = step2 ? step_product<2, 256, false>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
-                            : step_product<1, 128, false>(p, hi[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
+            if (wide) rc = step2 ? step_product<2, 256, true>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
+                                 : step_product<1, 128, true>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
+            else rc = step2 ? step_product<2, 256, false>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
+                            : step_product<1, 128, false>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
             if (rc != CAST_OK) return rc;
         }
     }

@@ -7,7 +7,7 @@
 //   warp 1    one lane of the pair's first CTA issues tcgen05.mma over each stage and commits it back to the ring
 //   warp 2    allocates and frees tensor memory: two accumulators, so the next tile's products run under an epilogue
 //   warps 4-7 epilogue: 32 accumulator rows each (a lane is a row), through shared memory to TMA stores where the result
-//             is a matrix
+//             is a matrix; arrays that it combines with the accumulators come by TMA as well (AuxRing)
 // In a pair every CTA stages its own 128 rows of A and its own half of B; the tensor cores read both halves of B, which
 // halves the shared-memory traffic per product.  No load is multicast.
 //
@@ -33,8 +33,7 @@ constexpr int kThreads = 256;
 constexpr int kEpiWarps = 4;
 constexpr int kStageBytesA = 128 * kBK * 2;      // 128 rows of A per CTA
 constexpr int kSlotBytes = 4096;                 // epilogue staging: 32 rows of 128 bytes
-constexpr int kSlotsPerWarp = 2;
-constexpr int kStagingBytes = kEpiWarps * kSlotsPerWarp * kSlotBytes;
+constexpr int kRing = 3;                         // steps of an epilogue's ring (see AuxRing)
 constexpr long long kWaitCycles = 4000000000ll;  // ~2 s; the longest wait of a healthy run is a tile (tens of microseconds)
 
 // Shape of one launch.  k_blocks = ceil(k / 64) blocks are cut into `splits` runs of at most split_blocks, each of which
@@ -43,7 +42,7 @@ struct Shape {
     int m, n;                      // result rows and columns
     int k_blocks, splits, split_blocks;
     int m_tiles, n_tiles, batch;
-    int group;                     // tile rows that are walked together, so that their operands stay in L2
+    int group;                     // tile rows that are walked together, so that their operands stay in L2 (symmetric: see tile_of)
     int total;                     // tiles of all batches and splits
     uint32_t idesc;                // instruction descriptor
     unsigned long long* fail_word; // host memory
@@ -55,15 +54,15 @@ template <bool SYM>
 __device__ __forceinline__ Tile tile_of(const Shape& s, int t)
 {
     Tile r;
-    if constexpr (SYM) {           // lower triangle, tile rows first to last
-        const int per = s.m_tiles * (s.m_tiles + 1) / 2;
+    if constexpr (SYM) {           // tiles that touch the lower triangle, tile rows first to last; `group` tile columns per tile row
+        const int per = s.group * (s.m_tiles * (s.m_tiles + 1) / 2);
         r.batch = t / per;
-        const int i = t - r.batch * per;
-        int row = (int)((sqrtf(8.0f * (float)i + 1.0f) - 1.0f) * 0.5f);
-        while (row * (row + 1) / 2 > i) --row;
-        while ((row + 1) * (row + 2) / 2 <= i) ++row;
+        const int i = t - r.batch * per, j = i / s.group;
+        int row = (int)((sqrtf(8.0f * (float)j + 1.0f) - 1.0f) * 0.5f);
+        while (row * (row + 1) / 2 > j) --row;
+        while ((row + 1) * (row + 2) / 2 <= j) ++row;
         r.tm = row;
-        r.tn = i - row * (row + 1) / 2;
+        r.tn = i - s.group * (row * (row + 1) / 2);
         r.split = 0;
     } else {
         const int per = s.m_tiles * s.n_tiles;
@@ -162,6 +161,7 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, 
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -235,17 +235,19 @@ constexpr uint64_t kDescStep = MN_MAJOR ? (16 * 128) >> 4 : (16 * 2) >> 4;      
 
 // ------------------------------------------------------------------------------------------------ the kernel
 
-template <int CG, int BN>
+// `staging`: shared memory of one epilogue warp.
+template <int CG, int BN, int STAGING>
 struct Config {
     static constexpr int BM = 128 * CG;
     static constexpr int b_rows = BN / CG;                         // rows of B staged by one CTA
     static constexpr int stage_bytes = kStageBytesA + b_rows * kBK * 2;
-    static constexpr int stages = stage_bytes >= 32768 ? 6 : 8;
-    static constexpr int smem_bytes = stages * stage_bytes + kStagingBytes + 1024 /* alignment */ + 256 /* barriers */;
+    static constexpr int room = (232448 - 1024 /* alignment */ - 768 /* barriers */ - kEpiWarps * STAGING) / stage_bytes;
+    static constexpr int stages = room < 8 ? room : 8;
+    static constexpr int smem_bytes = stages * stage_bytes + kEpiWarps * STAGING + 1024;
     static constexpr uint32_t tmem_cols = 2 * BN;
     static_assert(BN == 256 || BN == 128 || BN == 64, "two accumulators of BN columns: a power of two of at least 32");
     static_assert(b_rows % 64 == 0, "MN-major blocks are 64 wide");
-    static_assert(smem_bytes <= 232448, "227 KB of shared memory per CTA");
+    static_assert(stages >= 3, "a ring of stages");
 };
 
 // What an epilogue warp is given for one tile.
@@ -254,9 +256,13 @@ struct EpiTile {
     int row0;            // first result row of this warp's 32
     int col0;            // first result column of the tile
     uint32_t acc;        // tensor-memory address of this warp's rows, column 0
-    uint32_t slots;      // this warp's staging memory (kSlotsPerWarp slots of 4 KB, 1024-byte aligned)
+    uint32_t slots;      // this warp's staging memory (slots of 4 KB, 1024-byte aligned)
+    uint32_t bars;       // this warp's kRing mbarriers
     int lane;
     int slot;            // staging slot to use next (kept from tile to tile)
+    int first_row;       // of this warp in a tile
+    int index, step;     // of the tile among all tiles, and to this CTA's next one
+    const Stop* stop;
 };
 
 // 16 bytes of this lane's row in a swizzled 32 x 128-byte slot.
@@ -265,13 +271,22 @@ __device__ __forceinline__ void slot_write(uint32_t slot_addr, int lane, int chu
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(slot_addr + (uint32_t)lane * 128u + (uint32_t)((chunk ^ (lane & 7)) << 4)),
                  "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// Takes the next staging slot once the store that last used it has read it.
+__device__ __forceinline__ uint4 slot_read(uint32_t slot_addr, int row, int chunk)
+{
+    uint4 w;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                 : "r"(slot_addr + (uint32_t)row * 128u + (uint32_t)((chunk ^ (row & 7)) << 4)) : "memory");
+    return w;
+}
+
+// Two slots in turn, for epilogues that only store: takes the next one once the store that last used it has read it.
+constexpr int kTurns = 2;
 __device__ __forceinline__ uint32_t slot_acquire(EpiTile& e)
 {
-    if (e.lane == 0) store_wait_read<kSlotsPerWarp - 1>();
+    if (e.lane == 0) store_wait_read<kTurns - 1>();
     __syncwarp();
     const uint32_t a = e.slots + (uint32_t)(e.slot * kSlotBytes);
-    e.slot = (e.slot + 1) % kSlotsPerWarp;
+    e.slot = (e.slot + 1) % kTurns;
     return a;
 }
 // Hands a written slot to a TMA store (commits an empty group where nothing is to be stored, so that the groups count slots).
@@ -285,20 +300,83 @@ __device__ __forceinline__ void slot_store(const EpiTile& e, uint32_t slot_addr,
     }
 }
 
+// An epilogue provides: kSym (only tiles of the lower triangle), kStaging (bytes per warp), State (kept from tile to tile),
+// prefetch() (its tensor maps), start() (before the first tile), tile() (false: give up).
+struct StoringEpi {
+    static constexpr bool kSym = false;
+    static constexpr int kStaging = kTurns * kSlotBytes;
+    struct State {};
+    template <int BM, int BN>
+    __device__ __forceinline__ void start(const Shape&, const EpiTile&, State&) const {}
+};
+
+// The ring of an epilogue that combines its tile with arrays of the same layout: chunks of 32 rows x 64 columns come by TMA
+// into the slots of a step, two chunks ahead of their use (over tile borders too), are replaced in place by results and leave by
+// TMA from there.  One commit group per chunk; a step is loaded again once the group of its last chunk has read it.
+template <int N>      // slots per step
+struct AuxRing {
+    int index, c;        // tile and column of the chunk to load next
+    Tile tile;
+    int load_step, step;
+    uint32_t phase;      // parity of the current use of `step`
+
+    template <bool SYM>
+    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e)
+    {
+        index = e.index;
+        c = 0;
+        load_step = step = 0;
+        phase = 0;
+        if (index < s.total) tile = tile_of<SYM>(s, index);
+    }
+    __device__ __forceinline__ uint32_t slot(const EpiTile& e, int st, int k) const { return e.slots + (uint32_t)((st * N + k) * kSlotBytes); }
+
+    // Loads the next chunk's `n` arrays (0: only the cursor moves on).  Its step has to be free.
+    template <int BM, int BN, bool SYM>
+    __device__ __forceinline__ void load(const Shape& s, const EpiTile& e, const CUtensorMap* m0, const CUtensorMap* m1, int n)
+    {
+        if (index >= s.total) return;
+        if (e.lane == 0 && n > 0) {
+            const int x = tile.tn * BN + c, y = tile.tm * BM + e.first_row;
+            const uint32_t bar = e.bars + 8u * (uint32_t)load_step;
+            mbar_expect(bar, (uint32_t)(n * kSlotBytes));
+            tma_load<1>(slot(e, load_step, 0), m0, bar, x, y, tile.batch);
+            if (n > 1) tma_load<1>(slot(e, load_step, 1), m1, bar, x, y, tile.batch);
+        }
+        load_step = load_step + 1 == kRing ? 0 : load_step + 1;
+        c += 64;
+        if (c >= BN || tile.tn * BN + c >= s.n) {
+            c = 0;
+            index += e.step;
+            if (index < s.total) tile = tile_of<SYM>(s, index);
+        }
+    }
+    // Waits for the current chunk's arrays.
+    __device__ __forceinline__ bool wait(const EpiTile& e) const
+    {
+        return __all_sync(0xFFFFFFFFu, mbar_wait(e.bars + 8u * (uint32_t)step, phase, *e.stop));
+    }
+    __device__ __forceinline__ void next()
+    {
+        step = step + 1 == kRing ? 0 : step + 1;
+        if (step == 0) phase ^= 1u;
+    }
+};
+
 template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ Shape shape, const __grid_constant__ Epi epi)
 {
-    using C = Config<CG, BN>;
+    using C = Config<CG, BN, Epi::kStaging>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t ring = base;
     const uint32_t staging = base + C::stages * C::stage_bytes;
-    __shared__ __align__(8) unsigned long long bars[2 * C::stages + 4];
+    __shared__ __align__(8) unsigned long long bars[2 * C::stages + 4 + kEpiWarps * kRing];
     __shared__ uint32_t tmem_base_smem;
     __shared__ int stop_flag;
-    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::stages, accf0 = empty0 + 8 * C::stages, acce0 = accf0 + 16;
+    const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::stages, accf0 = empty0 + 8 * C::stages, acce0 = accf0 + 16, ring0 = acce0 + 16;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
 
@@ -307,7 +385,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         stop_flag = 0;
         for (int i = 0; i < C::stages; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(accf0 + 8 * i, 1); mbar_init(acce0 + 8 * i, CG * kEpiWarps); }
+        for (int i = 0; i < kEpiWarps * kRing; ++i) mbar_init(ring0 + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 32) {      // descriptors are fetched while the predecessor drains
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+        epi.prefetch();
     }
     if (warp == 2) tmem_alloc<CG>(smem_u32(&tmem_base_smem), C::tmem_cols);
     tc_fence_before();
@@ -386,24 +470,33 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     } else if (warp >= 4) {
         EpiTile e;
         e.lane = lane;
-        e.slots = staging + (uint32_t)((warp - 4) * kSlotsPerWarp * kSlotBytes);
+        e.slots = staging + (uint32_t)((warp - 4) * Epi::kStaging);
+        e.bars = ring0 + (uint32_t)((warp - 4) * kRing * 8);
         e.slot = 0;
+        e.first_row = (int)rank * 128 + (warp - 4) * 32;
+        e.index = first;
+        e.step = step;
+        e.stop = &stop;
+        typename Epi::State state;
+        epi.template start<C::BM, BN>(shape, e, state);
         int n_done = 0;
         for (int t = first; t < shape.total; t += step, ++n_done) {
+            e.index = t;
             e.tile = tile_of<Epi::kSym>(shape, t);
             const int buf = n_done & 1;
             bool ok = mbar_wait(accf0 + 8 * buf, (uint32_t)(n_done >> 1) & 1u, stop);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             tc_fence_after();
-            e.row0 = e.tile.tm * C::BM + (int)rank * 128 + (warp - 4) * 32;
+            e.row0 = e.tile.tm * C::BM + e.first_row;
             e.col0 = e.tile.tn * BN;
             e.acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)((warp - 4) * 32) << 16);
-            epi.template tile<BN>(shape, e);
+            ok = epi.template tile<C::BM, BN>(shape, e, state);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(map_to_rank(acce0 + 8 * buf, 0));
+            if (!ok) break;
         }
-        if (lane == 0) store_wait_all();
+        if (lane == 0) store_wait_read<0>();      // the results are on their way; the shared memory may go
     }
     __syncwarp();
     tc_fence_before();
@@ -439,12 +532,13 @@ inline uint32_t instruction_desc(bool bf16, bool a_mn, bool b_mn, int m, int n)
            ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-template <int CG, int BN, bool A_MN, bool B_MN, bool SYM>
+template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
 int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t batch, int splits, int group)
 {
-    using C = Config<CG, BN>;
+    using C = Config<CG, BN, Epi::kStaging>;
+    constexpr bool SYM = Epi::kSym;
     const int64_t mt = (m + C::BM - 1) / C::BM, nt = (n + BN - 1) / BN;
-    if (SYM && C::BM != BN) return CAST_ERR_SHAPE;
+    static_assert(!SYM || C::BM % BN == 0, "the triangle's blocks are whole tiles");
     s->m = (int)m;
     s->n = (int)n;
     s->k_blocks = (int)((k + kBK - 1) / kBK);
@@ -453,8 +547,8 @@ int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t bat
     s->m_tiles = (int)mt;
     s->n_tiles = (int)nt;
     s->batch = (int)batch;
-    s->group = group;
-    const int64_t per = SYM ? mt * (mt + 1) / 2 : mt * nt * s->splits;
+    s->group = SYM ? C::BM / BN : group;
+    const int64_t per = SYM ? mt * (mt + 1) / 2 * s->group : mt * nt * s->splits;
     if (per * batch > 0x3FFFFFFF) return CAST_ERR_SHAPE;
     s->total = (int)(per * batch);
     s->idesc = instruction_desc(bf16, A_MN, B_MN, C::BM, BN);
@@ -464,7 +558,7 @@ int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t bat
 template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
 int launch(const CUtensorMap& a, const CUtensorMap& b, const Shape& s, const Epi& epi, cudaStream_t stream)
 {
-    using C = Config<CG, BN>;
+    using C = Config<CG, BN, Epi::kStaging>;
     auto kernel = product_kernel<CG, BN, A_MN, B_MN, Epi>;
     int sms, rc;
     if ((rc = sm_count(&sms)) != CAST_OK) return rc;
