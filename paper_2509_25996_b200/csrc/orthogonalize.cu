@@ -4,15 +4,17 @@
 //
 // Each step is three products on the tensor cores over all matrices of the call at once:
 //     A = X X^T               symmetric: only tiles on and below the diagonal, each stored twice (once transposed)
-//     P = b A + c A A         symmetric likewise; b A is added by the epilogue
-//     X' = a X + P X          a X is added by the epilogue
+//     P = a I + b A + c A A   symmetric likewise; a I + b A is added by the epilogue
+//     X' = P X
 // Operands are never transposed in memory: X is read K-major in one product and MN-major in the other.
 //
 // Numbers: the operands are fp16, not bf16.  Every value is bounded (|X| singular values stay near 1), so the range is
-// enough and the 3 more bits of significand are worth 8 times less rounding noise.  X is held as hi + lo, two fp16 words scaled
-// by 2^12 (22 bits): the products read hi, a X reads both.  That matters because a = 3.4 per step amplifies small singular
-// directions 500-fold over five steps: noise from rounding X itself would be amplified with them, while noise that enters
-// through the products is confined to directions that are large already.  A and P (b A + c A A, without a I) are plain fp16.
+// enough and the 3 more bits of significand are worth 8 times less rounding noise.  Noise of A and P is harmless: it enters
+// through directions that are large already.  Rounding X itself is not: that noise lies in all directions, and a step
+// multiplies small ones by a = 3.4, five steps by 500, which swamps an update of low rank (measured on 768 x 768 of rank 8 over
+// 2 % noise: 2.8e-2 from the exact result, where rounding the result to bf16 is 1.7e-3).  So while the steps still to come
+// amplify by more than kAmplify, X is held as hi + lo, two fp16 words scaled by 2^12 (22 bits): the products read hi, the
+// epilogue adds a lo.  With five steps X_0, X_1 and X_2 have a lo: 2.4e-3 on that update.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -31,6 +33,7 @@ constexpr float kX = 4096.0f;               // X is stored times this
 constexpr int kGroup = 64;                  // matrices per launch at most
 constexpr int64_t kGroupElems = 64 << 20;   // ... and elements, which bounds the workspace
 constexpr int kNormBlocks = 128;
+constexpr float kAmplify = 12.0f;           // X keeps its lo while later steps multiply small directions by more
 
 struct PtrTable { const void* p[kGroup]; };
 struct OutTable { uint16_t* p[kGroup]; };
@@ -135,28 +138,40 @@ first_x_kernel(const __grid_constant__ PtrTable updates, const double* __restric
 
 // ------------------------------------------------------------------------------------------------ epilogues
 
-// Symmetric result: scale x acc (+ add x aux), stored at (row, col) and, off the diagonal, at (col, row).
+__device__ __forceinline__ void write_f16(uint32_t slot, int lane, int half, const float (&v)[32])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        slot_write(slot, lane, 4 * half + q, pack_f16(v[8 * q], v[8 * q + 1]), pack_f16(v[8 * q + 2], v[8 * q + 3]),
+                   pack_f16(v[8 * q + 4], v[8 * q + 5]), pack_f16(v[8 * q + 6], v[8 * q + 7]));
+}
+
+// A symmetric result, stored at (row, col) and, off the diagonal, at (col, row): scale acc, or with POLY
+// scale acc + add aux + diag I.
+template <bool POLY>
 struct SymEpi {
     static constexpr bool kSym = true;
-    static constexpr int kStaging = (kRing + 2) * kSlotBytes;      // the ring, and two slots for the mirrored chunks in turn
-    using State = AuxRing<1>;
+    // POLY: the ring of aux, replaced in place, and a slot for the mirrored chunk; otherwise a slot for each
+    static constexpr int kStaging = (POLY ? kRing + 1 : 2) * kSlotBytes;
+    using State = AuxRing;
     CUtensorMap map_out;         // boxes of 32 rows x 64 columns, swizzled
     CUtensorMap map_mirror;      // the same array, boxes of 64 rows x 32 columns, not swizzled
     CUtensorMap map_aux;         // fp16, read like map_out
-    int has_aux;
-    float scale, add;
+    float scale, add, diag;
 
     __device__ __forceinline__ void prefetch() const
     {
         prefetch_map(&map_out);
         prefetch_map(&map_mirror);
-        if (has_aux) prefetch_map(&map_aux);
+        if constexpr (POLY) prefetch_map(&map_aux);
     }
     template <int BM, int BN>
     __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
     {
-        ring.start<true>(s, e);
-        for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, true>(s, e, &map_aux, nullptr, has_aux);
+        if constexpr (POLY) {
+            ring.start<BN, true>(s, e);
+            for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, true>(s, e, &map_aux);
+        }
     }
 
     template <int BM, int BN>
@@ -166,39 +181,52 @@ struct SymEpi {
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
-            const uint32_t slot = ring.slot(e, ring.step, 0);
-            if (has_aux && !ring.wait(e)) return false;
-            uint32_t packed[32];
+            slots_free(e);
+            uint32_t slot = e.slots;
+            if constexpr (POLY) {
+                ring.load<BM, BN, true>(s, e, &map_aux);
+                slot = ring.slot(e);
+                if (!ring.wait(e)) return false;
+            }
+            const uint32_t t = e.slots + (uint32_t)((POLY ? kRing : 1) * kSlotBytes);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t* p = packed + 16 * h + 4 * q;
-                    if (has_aux) {
+                for (int i = 0; i < 32; ++i) v[i] *= scale;
+                if constexpr (POLY) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
                         const uint4 w = slot_read(slot, e.lane, 4 * h + q);
                         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            p[i] = pack_f16(fmaf(add, f16_lo(u[i]), scale * v[8 * q + 2 * i]), fmaf(add, f16_hi(u[i]), scale * v[8 * q + 2 * i + 1]));
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) p[i] = pack_f16(scale * v[8 * q + 2 * i], scale * v[8 * q + 2 * i + 1]);
+                        for (int i = 0; i < 4; ++i) {
+                            v[8 * q + 2 * i] = fmaf(add, f16_lo(u[i]), v[8 * q + 2 * i]);
+                            v[8 * q + 2 * i + 1] = fmaf(add, f16_hi(u[i]), v[8 * q + 2 * i + 1]);
+                        }
                     }
-                    slot_write(slot, e.lane, 4 * h + q, p[0], p[1], p[2], p[3]);
-                }
-            }
-            const uint32_t t = e.slots + (uint32_t)((kRing + e.slot) * kSlotBytes);
-            if (mirror) {
-                // rows of 32 elements (64 bytes): column j of the chunk becomes row j, this lane its element
+                    // the chunk's 32 rows meet the diagonal in one half of its columns, or not at all
+                    if (n + 32 * h == e.row0) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const uint32_t at = t + (uint32_t)(2 * j) * 64u + (uint32_t)e.lane * 2u;
-                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((unsigned short)(packed[j] & 0xFFFFu)) : "memory");
-                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 64u), "h"((unsigned short)(packed[j] >> 16)) : "memory");
+                        for (int i = 0; i < 32; ++i)
+                            if (i == e.lane) v[i] += diag;
+                    }
                 }
-                e.slot ^= 1;
+                uint32_t p[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[i] = pack_f16(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) slot_write(slot, e.lane, 4 * h + q, p[4 * q], p[4 * q + 1], p[4 * q + 2], p[4 * q + 3]);
+                if (mirror) {
+                    // rows of 32 elements (64 bytes): column j of the chunk becomes row j, this lane its element
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const uint32_t at = t + (uint32_t)(32 * h + 2 * j) * 64u + (uint32_t)e.lane * 2u;
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((unsigned short)(p[j] & 0xFFFFu)) : "memory");
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + 64u), "h"((unsigned short)(p[j] >> 16)) : "memory");
+                    }
+                }
             }
             fence_async_smem();
             __syncwarp();
@@ -208,41 +236,40 @@ struct SymEpi {
                     if (mirror) tma_store(&map_mirror, t, e.row0, n, e.tile.batch);
                 }
                 store_commit();
-                store_wait_read<1>();      // the chunk before this one has left: its step and its mirror slot are free
             }
-            __syncwarp();
-            ring.next();
-            ring.load<BM, BN, true>(s, e, &map_aux, nullptr, has_aux);
+            if constexpr (POLY) ring.next();
         }
         return true;
     }
 };
 
-// X' = a X + acc: two fp16 words per entry, or after the last step bf16(scale X').
+// X' = acc (+ a lo): as hi + lo, or hi alone.
+template <bool LO_IN>
 struct StepEpi {
     static constexpr bool kSym = false;
-    static constexpr int kStaging = kRing * 2 * kSlotBytes;
-    using State = AuxRing<2>;
-    CUtensorMap map_hi, map_lo;            // X'
-    CUtensorMap map_hi_in, map_lo_in;      // X
-    OutTable out;
-    float a, scale;
-    int last, vec;
+    // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise two slots for hi in turn
+    static constexpr int kStaging = (LO_IN ? kRing + 1 : kTurns) * kSlotBytes;
+    using State = AuxRing;
+    CUtensorMap map_hi, map_lo;      // X'
+    CUtensorMap map_lo_in;           // X
+    float a;
+    int lo_out;                      // only with LO_IN: lo is dropped at some step and does not come back
 
     __device__ __forceinline__ void prefetch() const
     {
-        prefetch_map(&map_hi_in);
-        prefetch_map(&map_lo_in);
-        if (!last) {
-            prefetch_map(&map_hi);
-            prefetch_map(&map_lo);
+        prefetch_map(&map_hi);
+        if constexpr (LO_IN) {
+            prefetch_map(&map_lo_in);
+            if (lo_out) prefetch_map(&map_lo);
         }
     }
     template <int BM, int BN>
     __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
     {
-        ring.start<false>(s, e);
-        for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, false>(s, e, &map_hi_in, &map_lo_in, 2);
+        if constexpr (LO_IN) {
+            ring.start<BN, false>(s, e);
+            for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, false>(s, e, &map_lo_in);
+        }
     }
 
     template <int BM, int BN>
@@ -251,67 +278,127 @@ struct StepEpi {
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
-            const uint32_t hi = ring.slot(e, ring.step, 0), lo = ring.slot(e, ring.step, 1);
-            if (!ring.wait(e)) return false;
+            uint32_t hi, lo = 0;
+            if constexpr (LO_IN) {
+                slots_free(e);
+                ring.load<BM, BN, false>(s, e, &map_lo_in);
+                hi = e.slots + kRing * kSlotBytes;
+                lo = ring.slot(e);
+                if (!ring.wait(e)) return false;
+            } else {
+                hi = slot_acquire(e);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[32];
+                tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
+                if constexpr (LO_IN) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint4 y = slot_read(lo, e.lane, 4 * h + q);
+                        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                        uint32_t r[4], d[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float g0 = fmaf(a, f16_lo(w[i]), v[8 * q + 2 * i]), g1 = fmaf(a, f16_hi(w[i]), v[8 * q + 2 * i + 1]);
+                            r[i] = pack_f16(g0, g1);
+                            d[i] = pack_f16(g0 - f16_lo(r[i]), g1 - f16_hi(r[i]));
+                        }
+                        slot_write(hi, e.lane, 4 * h + q, r[0], r[1], r[2], r[3]);
+                        if (lo_out) slot_write(lo, e.lane, 4 * h + q, d[0], d[1], d[2], d[3]);
+                    }
+                } else {
+                    write_f16(hi, e.lane, h, v);
+                }
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (e.lane == 0) {
+                if (e.row0 < s.m) {
+                    tma_store(&map_hi, hi, n, e.row0, e.tile.batch);
+                    if (LO_IN && lo_out) tma_store(&map_lo, lo, n, e.row0, e.tile.batch);
+                }
+                store_commit();
+            }
+            if constexpr (LO_IN) ring.next();
+        }
+        return true;
+    }
+};
+
+// The result: bf16(scale (acc + a lo)) into the caller's matrices, whose rows may have any length and alignment: through a slot,
+// then whole rows of it by ordinary stores.
+template <bool LO_IN>
+struct ResultEpi {
+    static constexpr bool kSym = false;
+    static constexpr int kStaging = (LO_IN ? kRing : 1) * kSlotBytes;
+    using State = AuxRing;
+    CUtensorMap map_lo_in;
+    OutTable out;
+    float a, scale;
+    int vec;
+
+    __device__ __forceinline__ void prefetch() const { if constexpr (LO_IN) prefetch_map(&map_lo_in); }
+    template <int BM, int BN>
+    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
+    {
+        if constexpr (LO_IN) {
+            ring.start<BN, false>(s, e);
+            for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, false>(s, e, &map_lo_in);
+        }
+    }
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
+    {
+        uint16_t* o = out.p[e.tile.batch];
+#pragma unroll 1
+        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+            const int n = e.col0 + c;
+            __syncwarp();          // the chunk before this one has been read
+            uint32_t slot = e.slots;
+            if constexpr (LO_IN) {
+                ring.load<BM, BN, false>(s, e, &map_lo_in);
+                slot = ring.slot(e);
+                if (!ring.wait(e)) return false;
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint4 x = slot_read(hi, e.lane, 4 * h + q), y = slot_read(lo, e.lane, 4 * h + q);
-                    const uint32_t u[4] = {x.x, x.y, x.z, x.w}, w[4] = {y.x, y.y, y.z, y.w};
-                    uint32_t r[4], d[4];
+                    if constexpr (LO_IN) {
+                        const uint4 y = slot_read(slot, e.lane, 4 * h + q);
+                        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float g0 = fmaf(a, f16_lo(u[i]) + f16_lo(w[i]), v[8 * q + 2 * i]);
-                        const float g1 = fmaf(a, f16_hi(u[i]) + f16_hi(w[i]), v[8 * q + 2 * i + 1]);
-                        if (last) {
-                            r[i] = pack_b16(scale * g0, scale * g1);
-                        } else {
-                            r[i] = pack_f16(g0, g1);
-                            d[i] = pack_f16(g0 - f16_lo(r[i]), g1 - f16_hi(r[i]));
+                        for (int i = 0; i < 4; ++i) {
+                            v[8 * q + 2 * i] = fmaf(a, f16_lo(w[i]), v[8 * q + 2 * i]);
+                            v[8 * q + 2 * i + 1] = fmaf(a, f16_hi(w[i]), v[8 * q + 2 * i + 1]);
                         }
                     }
-                    slot_write(hi, e.lane, 4 * h + q, r[0], r[1], r[2], r[3]);
-                    if (!last) slot_write(lo, e.lane, 4 * h + q, d[0], d[1], d[2], d[3]);
+                    slot_write(slot, e.lane, 4 * h + q, pack_b16(scale * v[8 * q], scale * v[8 * q + 1]),
+                               pack_b16(scale * v[8 * q + 2], scale * v[8 * q + 3]), pack_b16(scale * v[8 * q + 4], scale * v[8 * q + 5]),
+                               pack_b16(scale * v[8 * q + 6], scale * v[8 * q + 7]));
                 }
             }
-            if (last) {
-                // rows of the caller's matrix may have any length: whole rows of the slot by ordinary stores
-                __syncwarp();
-                uint16_t* o = out.p[e.tile.batch];
+            __syncwarp();
 #pragma unroll 4
-                for (int r0 = 0; r0 < 32; r0 += 4) {
-                    const int r = r0 + (e.lane >> 3), q = e.lane & 7;
-                    const uint4 w = slot_read(hi, r, q);
-                    if (e.row0 + r >= s.m) continue;
-                    uint16_t* to = o + (int64_t)(e.row0 + r) * s.n + n + 8 * q;
-                    if (vec) {
-                        if (n + 8 * q < s.n) *reinterpret_cast<uint4*>(to) = w;
-                    } else {
-                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            for (int r0 = 0; r0 < 32; r0 += 4) {
+                const int r = r0 + (e.lane >> 3), q = e.lane & 7;
+                const uint4 w = slot_read(slot, r, q);
+                if (e.row0 + r >= s.m) continue;
+                uint16_t* to = o + (int64_t)(e.row0 + r) * s.n + n + 8 * q;
+                if (vec) {
+                    if (n + 8 * q < s.n) *reinterpret_cast<uint4*>(to) = w;
+                } else {
+                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (n + 8 * q + i < s.n) to[i] = (uint16_t)(i & 1 ? u[i / 2] >> 16 : u[i / 2] & 0xFFFFu);
-                    }
+                    for (int i = 0; i < 8; ++i)
+                        if (n + 8 * q + i < s.n) to[i] = (uint16_t)(i & 1 ? u[i / 2] >> 16 : u[i / 2] & 0xFFFFu);
                 }
-                __syncwarp();
-            } else {
-                fence_async_smem();
-                __syncwarp();
-                if (e.lane == 0) {
-                    if (e.row0 < s.m) {
-                        tma_store(&map_hi, hi, n, e.row0, e.tile.batch);
-                        tma_store(&map_lo, lo, n, e.row0, e.tile.batch);
-                    }
-                    store_commit();
-                    store_wait_read<1>();      // the chunk before this one has left its step
-                }
-                __syncwarp();
             }
-            ring.next();
-            ring.load<BM, BN, false>(s, e, &map_hi_in, &map_lo_in, 2);
+            if constexpr (LO_IN) ring.next();
         }
         return true;
     }
@@ -344,66 +431,119 @@ Layout layout_of(int64_t n, int64_t rows, int64_t cols)
     return l;
 }
 
-// Pairs of CTAs with 256 x 256 tiles, or single CTAs with 128 x 128 ones: rounds over the SMs x cycles per tile.  A 64-deep
-// block takes 512 cycles of a pair's tensor cores and about 350 of a single CTA's (256, held up by its shared memory);
-// filling and draining a tile's pipeline about 3000.
-bool use_pairs(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int sms)
+enum TileForm { kPair256, kSingle128, kSingle64 };      // 256 x 256 on two CTAs, 128 x 128 or 128 x 64 on one
+
+// The form that takes least: rounds over the SMs x cycles per tile.  A 64-deep block of a pair's 256 x 256 takes 512 cycles of its
+// tensor cores; a single CTA is bound by its L2 port, 64 bytes per cycle: 512 cycles for 32 KB (128 x 128), 384 for 24 KB
+// (128 x 64).  Filling and draining a tile's pipeline: about 3000 cycles and 8 per column of its epilogue.
+TileForm tile_form(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int sms)
 {
     const int64_t kb = (k + kBK - 1) / kBK;
-    auto tiles = [&](int64_t t) {
-        const int64_t a = (m + t - 1) / t, b = (n + t - 1) / t;
-        return (sym ? a * (a + 1) / 2 : a * b) * batch;
+    auto cost = [&](int64_t bm, int64_t bn, int64_t units, int64_t block) {
+        const int64_t a = (m + bm - 1) / bm, b = (n + bn - 1) / bn;
+        const int64_t tiles = (sym ? a * (a + 1) / 2 * (bm / bn) : a * b) * batch;
+        return (tiles + units - 1) / units * (kb * block) + 3000 + 16 * bn;
     };
-    const int64_t pairs = sms / 2;
-    const int64_t two = (tiles(256) + pairs - 1) / pairs * (kb * 512 + 3000), one = (tiles(128) + sms - 1) / sms * (kb * 350 + 3000);
-    return two <= one;
+    const int64_t p = cost(256, 256, sms / 2, 512), s = cost(128, 128, sms, 512), t = cost(128, 64, sms, 384);
+    return p <= s && p <= t ? kPair256 : s <= t ? kSingle128 : kSingle64;
 }
 
-template <int CG, int BN, bool MN>
+// One square product over the batch: A = down X X^T (x: [mn] x [k] or, MN, its transpose), or P from A.
+template <int CG, int BN, bool MN, bool POLY>
 int sym_product(const uint16_t* x, int64_t mn, int64_t k, int64_t batch, int64_t x_ld, int64_t x_stride, uint16_t* out, const Layout& l,
-                const uint16_t* aux, float scale, float add, cudaStream_t stream)
+                float scale, float add, float diag, cudaStream_t stream)
 {
-    CUtensorMap m;
+    CUtensorMap ma, mb;
     Shape s;
-    SymEpi epi;
+    SymEpi<POLY> epi;
     int rc;
     const int64_t stride = l.sq * l.sq_ld;
-    if ((rc = make_shape<CG, BN, MN, MN, SymEpi>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
-    if ((rc = operand_map<MN>(&m, x, mn, k, batch, x_ld, x_stride, 128)) != CAST_OK) return rc;
-    CUtensorMap mb = m;
+    if ((rc = make_shape<CG, BN, MN, MN, SymEpi<POLY>>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
+    if ((rc = operand_map<MN>(&ma, x, mn, k, batch, x_ld, x_stride, 128)) != CAST_OK) return rc;
+    mb = ma;
     if (BN / CG != 128 && (rc = operand_map<MN>(&mb, x, mn, k, batch, x_ld, x_stride, BN / CG)) != CAST_OK) return rc;
     if ((rc = make_map(&epi.map_out, out, 2, mn, mn, batch, l.sq_ld, stride, 64, 32, true)) != CAST_OK) return rc;
     if ((rc = make_map(&epi.map_mirror, out, 2, mn, mn, batch, l.sq_ld, stride, 32, 64, false)) != CAST_OK) return rc;
-    epi.has_aux = aux != nullptr;
     epi.map_aux = epi.map_out;
-    if (aux && (rc = make_map(&epi.map_aux, aux, 2, mn, mn, batch, l.sq_ld, stride, 64, 32, true)) != CAST_OK) return rc;
+    if (POLY && (rc = make_map(&epi.map_aux, x, 2, mn, mn, batch, x_ld, x_stride, 64, 32, true)) != CAST_OK) return rc;
     epi.scale = scale;
     epi.add = add;
-    return launch<CG, BN, MN, MN>(m, mb, s, epi, stream);
+    epi.diag = diag;
+    return launch<CG, BN, MN, MN>(ma, mb, s, epi, stream);
 }
 
-// X' = a X + P X (wide) or a X + X P (tall)
-template <int CG, int BN, bool WIDE>
-int step_product(const uint16_t* p, const uint16_t* hi, const uint16_t* lo, int64_t rows, int64_t cols, int64_t batch, const Layout& l, uint16_t* hi_out,
-                 uint16_t* lo_out, StepEpi& epi, cudaStream_t stream)
+template <bool MN, bool POLY>
+int sym_product(TileForm f, const uint16_t* x, int64_t mn, int64_t k, int64_t batch, int64_t x_ld, int64_t x_stride, uint16_t* out, const Layout& l,
+                float scale, float add, float diag, cudaStream_t stream)
+{
+    if (f == kPair256) return sym_product<2, 256, MN, POLY>(x, mn, k, batch, x_ld, x_stride, out, l, scale, add, diag, stream);
+    if (f == kSingle128) return sym_product<1, 128, MN, POLY>(x, mn, k, batch, x_ld, x_stride, out, l, scale, add, diag, stream);
+    return sym_product<1, 64, MN, POLY>(x, mn, k, batch, x_ld, x_stride, out, l, scale, add, diag, stream);
+}
+
+struct StepCall {
+    const uint16_t *p, *hi, *lo;      // lo NULL: X is hi alone
+    uint16_t *hi_out, *lo_out;        // hi_out NULL: the result
+    const OutTable* out;
+    int64_t rows, cols, batch;
+    const Layout* l;
+    float a, scale;
+    bool vec;
+    cudaStream_t stream;
+};
+
+// X' = P X (wide) or X P (tall)
+template <int CG, int BN, bool WIDE, class Epi>
+int step_product(const StepCall& c, Epi& epi)
 {
     CUtensorMap ma, mb;
     Shape s;
     int rc;
-    const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
-    if ((rc = make_shape<CG, BN, false, WIDE, StepEpi>(&s, false, rows, cols, l.sq, batch, 1, 16 / CG)) != CAST_OK) return rc;
+    const Layout& l = *c.l;
+    const int64_t xs = c.rows * l.ld, ps = l.sq * l.sq_ld;
+    if ((rc = make_shape<CG, BN, false, WIDE, Epi>(&s, false, c.rows, c.cols, l.sq, c.batch, 1, 16 / CG)) != CAST_OK) return rc;
     if (WIDE) {
-        if ((rc = operand_map<false>(&ma, p, rows, rows, batch, l.sq_ld, ps, 128)) != CAST_OK) return rc;
-        if ((rc = operand_map<true>(&mb, hi, cols, rows, batch, l.ld, xs, BN / CG)) != CAST_OK) return rc;
+        if ((rc = operand_map<false>(&ma, c.p, c.rows, c.rows, c.batch, l.sq_ld, ps, 128)) != CAST_OK) return rc;
+        if ((rc = operand_map<true>(&mb, c.hi, c.cols, c.rows, c.batch, l.ld, xs, BN / CG)) != CAST_OK) return rc;
     } else {
-        if ((rc = operand_map<false>(&ma, hi, rows, cols, batch, l.ld, xs, 128)) != CAST_OK) return rc;
-        if ((rc = operand_map<false>(&mb, p, cols, cols, batch, l.sq_ld, ps, BN / CG)) != CAST_OK) return rc;
+        if ((rc = operand_map<false>(&ma, c.hi, c.rows, c.cols, c.batch, l.ld, xs, 128)) != CAST_OK) return rc;
+        if ((rc = operand_map<false>(&mb, c.p, c.cols, c.cols, c.batch, l.sq_ld, ps, BN / CG)) != CAST_OK) return rc;
     }
-    if ((rc = make_map(&epi.map_hi, hi_out, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
-    if ((rc = make_map(&epi.map_lo, lo_out, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
-    if ((rc = make_map(&epi.map_hi_in, hi, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
-    if ((rc = make_map(&epi.map_lo_in, lo, 2, cols, rows, batch, l.ld, xs, 64, 32, true)) != CAST_OK) return rc;
-    return launch<CG, BN, false, WIDE>(ma, mb, s, epi, stream);
+    return launch<CG, BN, false, WIDE>(ma, mb, s, epi, c.stream);
+}
+
+template <int CG, int BN, bool WIDE, bool LO_IN>
+int step_product(const StepCall& c)
+{
+    const Layout& l = *c.l;
+    const int64_t xs = c.rows * l.ld;
+    auto map = [&](CUtensorMap* m, const uint16_t* x) { return make_map(m, x, 2, c.cols, c.rows, c.batch, l.ld, xs, 64, 32, true); };
+    int rc;
+    if (!c.hi_out) {
+        ResultEpi<LO_IN> epi;
+        if ((rc = map(&epi.map_lo_in, LO_IN ? c.lo : c.hi)) != CAST_OK) return rc;
+        epi.out = *c.out;
+        epi.a = c.a;
+        epi.scale = c.scale;
+        epi.vec = c.vec;
+        return step_product<CG, BN, WIDE>(c, epi);
+    }
+    StepEpi<LO_IN> epi;
+    if ((rc = map(&epi.map_hi, c.hi_out)) != CAST_OK) return rc;
+    epi.map_lo = epi.map_lo_in = epi.map_hi;
+    if (LO_IN && (rc = map(&epi.map_lo_in, c.lo)) != CAST_OK) return rc;
+    if (c.lo_out && (rc = map(&epi.map_lo, c.lo_out)) != CAST_OK) return rc;
+    epi.a = c.a;
+    epi.lo_out = c.lo_out != nullptr;
+    return step_product<CG, BN, WIDE>(c, epi);
+}
+
+template <bool WIDE>
+int step_product(TileForm f, const StepCall& c)
+{
+    if (f == kPair256) return c.lo ? step_product<2, 256, WIDE, true>(c) : step_product<2, 256, WIDE, false>(c);
+    if (f == kSingle128) return c.lo ? step_product<1, 128, WIDE, true>(c) : step_product<1, 128, WIDE, false>(c);
+    return c.lo ? step_product<1, 64, WIDE, true>(c) : step_product<1, 64, WIDE, false>(c);
 }
 
 template <bool BF16, int VEC>
@@ -505,42 +645,51 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
     for (int first = 0; first < n; first += (int)l.group) {
         const int64_t batch = n - first < l.group ? n - first : l.group;
         PtrTable in;
-        StepEpi epi;
+        OutTable to;
         bool in_vec = cols % 8 == 0, out_vec = cols % 8 == 0;
         for (int64_t i = 0; i < batch; ++i) {
             in.p[i] = updates[first + i];
-            epi.out.p[i] = out[first + i];
+            to.p[i] = out[first + i];
             in_vec = in_vec && !((uintptr_t)in.p[i] & 15u);
-            out_vec = out_vec && !((uintptr_t)epi.out.p[i] & 15u);
+            out_vec = out_vec && !((uintptr_t)to.p[i] & 15u);
         }
-        for (int64_t i = batch; i < kGroup; ++i) { in.p[i] = nullptr; epi.out.p[i] = nullptr; }
+        for (int64_t i = batch; i < kGroup; ++i) { in.p[i] = nullptr; to.p[i] = nullptr; }
         if (updates_bf16) rc = in_vec ? launch_first<true, 8>(first == 0, in, batch, rows, cols, ws, l, eps, st) : launch_first<true, 1>(first == 0, in, batch, rows, cols, ws, l, eps, st);
         else rc = in_vec ? launch_first<false, 8>(first == 0, in, batch, rows, cols, ws, l, eps, st) : launch_first<false, 1>(first == 0, in, batch, rows, cols, ws, l, eps, st);
         if (rc != CAST_OK) return rc;
-        const bool gram2 = use_pairs(l.sq, l.sq, big, batch, true, sms), sq2 = use_pairs(l.sq, l.sq, l.sq, batch, true, sms);
-        const bool step2 = use_pairs(rows, cols, l.sq, batch, false, sms);
+        const TileForm gram = tile_form(l.sq, l.sq, big, batch, true, sms), poly = tile_form(l.sq, l.sq, l.sq, batch, true, sms);
+        const TileForm step = tile_form(rows, cols, l.sq, batch, false, sms);
         const float down = 1.0f / (kX * kX);
+        const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
+        bool has_lo = true;
         for (int k = 0; k < steps; ++k) {
             const float* q = coeffs ? coeffs + 3 * k : kQuintic;
             const int cur = k & 1;
-            const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
-            if (wide) rc = gram2 ? sym_product<2, 256, false>(hi[cur], rows, cols, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st)
-                                 : sym_product<1, 128, false>(hi[cur], rows, cols, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st);
-            else rc = gram2 ? sym_product<2, 256, true>(hi[cur], cols, rows, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st)
-                            : sym_product<1, 128, true>(hi[cur], cols, rows, batch, l.ld, xs, a, l, nullptr, down, 0.0f, st);
+            rc = wide ? sym_product<false, false>(gram, hi[cur], rows, cols, batch, l.ld, xs, a, l, down, 0.0f, 0.0f, st)
+                      : sym_product<true, false>(gram, hi[cur], cols, rows, batch, l.ld, xs, a, l, down, 0.0f, 0.0f, st);
             if (rc != CAST_OK) return rc;
-            rc = sq2 ? sym_product<2, 256, false>(a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, a, q[2], q[1], st)
-                     : sym_product<1, 128, false>(a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, a, q[2], q[1], st);
-            if (rc != CAST_OK) return rc;
-            epi.a = q[0];
-            epi.scale = scale / kX;
-            epi.last = k + 1 == steps;
-            epi.vec = out_vec;
-            if (wide) rc = step2 ? step_product<2, 256, true>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
-                                 : step_product<1, 128, true>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
-            else rc = step2 ? step_product<2, 256, false>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st)
-                            : step_product<1, 128, false>(p, hi[cur], lo[cur], rows, cols, batch, l, hi[cur ^ 1], lo[cur ^ 1], epi, st);
-            if (rc != CAST_OK) return rc;
+            if ((rc = sym_product<false, true>(poly, a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, q[2], q[1], q[0], st)) != CAST_OK) return rc;
+            const bool last = k + 1 == steps;
+            float amplify = 1.0f;      // of a small direction of X', by the steps after this one
+            for (int j = k + 1; j < steps; ++j) amplify *= std::fabs(coeffs ? coeffs[3 * j] : kQuintic[0]);
+            const bool lo_out = has_lo && !last && amplify > kAmplify;
+            StepCall c;
+            c.p = p;
+            c.hi = hi[cur];
+            c.lo = has_lo ? lo[cur] : nullptr;
+            c.hi_out = last ? nullptr : hi[cur ^ 1];
+            c.lo_out = lo_out ? lo[cur ^ 1] : nullptr;
+            c.out = &to;
+            c.rows = rows;
+            c.cols = cols;
+            c.batch = batch;
+            c.l = &l;
+            c.a = q[0];
+            c.scale = scale / kX;
+            c.vec = out_vec;
+            c.stream = st;
+            if ((rc = wide ? step_product<true>(step, c) : step_product<false>(step, c)) != CAST_OK) return rc;
+            has_lo = lo_out;
         }
     }
     return CAST_OK;

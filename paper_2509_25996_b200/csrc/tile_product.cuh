@@ -33,7 +33,7 @@ constexpr int kThreads = 256;
 constexpr int kEpiWarps = 4;
 constexpr int kStageBytesA = 128 * kBK * 2;      // 128 rows of A per CTA
 constexpr int kSlotBytes = 4096;                 // epilogue staging: 32 rows of 128 bytes
-constexpr int kRing = 3;                         // steps of an epilogue's ring (see AuxRing)
+constexpr int kRing = 3;                         // slots of an epilogue's ring (see AuxRing)
 constexpr long long kWaitCycles = 4000000000ll;  // ~2 s; the longest wait of a healthy run is a tile (tens of microseconds)
 
 // Shape of one launch.  k_blocks = ceil(k / 64) blocks are cut into `splits` runs of at most split_blocks, each of which
@@ -96,13 +96,13 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)      // bar: shared::cluster address
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
     asm volatile("{ .reg .pred p;\n\t"
-                 "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
@@ -310,48 +310,53 @@ struct StoringEpi {
     __device__ __forceinline__ void start(const Shape&, const EpiTile&, State&) const {}
 };
 
-// The ring of an epilogue that combines its tile with arrays of the same layout: chunks of 32 rows x 64 columns come by TMA
-// into the slots of a step, two chunks ahead of their use (over tile borders too), are replaced in place by results and leave by
-// TMA from there.  One commit group per chunk; a step is loaded again once the group of its last chunk has read it.
-template <int N>      // slots per step
+// The ring of an epilogue that combines its tile with an array of the same layout: chunks of 32 rows x 64 columns come by TMA
+// into kRing slots, two chunks ahead of their use (over tile borders too), and may be replaced in place by results that leave
+// by TMA from there.  A slot is loaded again once the stores of the chunk that used it have read it.
 struct AuxRing {
     int index, c;        // tile and column of the chunk to load next
     Tile tile;
     int load_step, step;
     uint32_t phase;      // parity of the current use of `step`
 
-    template <bool SYM>
+    template <int BN, bool SYM>
     __device__ __forceinline__ void start(const Shape& s, const EpiTile& e)
     {
         index = e.index;
         c = 0;
         load_step = step = 0;
         phase = 0;
-        if (index < s.total) tile = tile_of<SYM>(s, index);
+        find<BN, SYM>(s, e);
     }
-    __device__ __forceinline__ uint32_t slot(const EpiTile& e, int st, int k) const { return e.slots + (uint32_t)((st * N + k) * kSlotBytes); }
+    // The tile at `index`, or the first one after it that has columns (a triangle's last blocks may have none).
+    template <int BN, bool SYM>
+    __device__ __forceinline__ void find(const Shape& s, const EpiTile& e)
+    {
+        for (; index < s.total; index += e.step) {
+            tile = tile_of<SYM>(s, index);
+            if (tile.tn * BN < s.n) break;
+        }
+    }
+    __device__ __forceinline__ uint32_t slot(const EpiTile& e) const { return e.slots + (uint32_t)(step * kSlotBytes); }
 
-    // Loads the next chunk's `n` arrays (0: only the cursor moves on).  Its step has to be free.
     template <int BM, int BN, bool SYM>
-    __device__ __forceinline__ void load(const Shape& s, const EpiTile& e, const CUtensorMap* m0, const CUtensorMap* m1, int n)
+    __device__ __forceinline__ void load(const Shape& s, const EpiTile& e, const CUtensorMap* map)
     {
         if (index >= s.total) return;
-        if (e.lane == 0 && n > 0) {
-            const int x = tile.tn * BN + c, y = tile.tm * BM + e.first_row;
+        if (e.lane == 0) {
             const uint32_t bar = e.bars + 8u * (uint32_t)load_step;
-            mbar_expect(bar, (uint32_t)(n * kSlotBytes));
-            tma_load<1>(slot(e, load_step, 0), m0, bar, x, y, tile.batch);
-            if (n > 1) tma_load<1>(slot(e, load_step, 1), m1, bar, x, y, tile.batch);
+            mbar_expect(bar, kSlotBytes);
+            tma_load<1>(e.slots + (uint32_t)(load_step * kSlotBytes), map, bar, tile.tn * BN + c, tile.tm * BM + e.first_row, tile.batch);
         }
         load_step = load_step + 1 == kRing ? 0 : load_step + 1;
         c += 64;
         if (c >= BN || tile.tn * BN + c >= s.n) {
             c = 0;
             index += e.step;
-            if (index < s.total) tile = tile_of<SYM>(s, index);
+            find<BN, SYM>(s, e);
         }
     }
-    // Waits for the current chunk's arrays.
+    // Waits for the current chunk.
     __device__ __forceinline__ bool wait(const EpiTile& e) const
     {
         return __all_sync(0xFFFFFFFFu, mbar_wait(e.bars + 8u * (uint32_t)step, phase, *e.stop));
@@ -362,6 +367,12 @@ struct AuxRing {
         if (step == 0) phase ^= 1u;
     }
 };
+// All stores of this warp have read their slots.
+__device__ __forceinline__ void slots_free(const EpiTile& e)
+{
+    if (e.lane == 0) store_wait_read<0>();
+    __syncwarp();
+}
 
 template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
