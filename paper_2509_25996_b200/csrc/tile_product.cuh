@@ -3,8 +3,8 @@
 //
 // One persistent kernel.  A CTA (CG = 1) or a pair of CTAs on neighbouring SMs (CG = 2) owns a tile of 128 CG x BN; tiles are
 // dealt out round robin.  Per CTA:
-//   warp 0    one lane moves operand blocks of 64 k (128 bytes, the swizzle width) with TMA into a ring of stages
-//   warp 1    one lane of the pair's first CTA issues tcgen05.mma over each stage and commits it back to the ring
+//   warp 0    moves operand blocks of 64 k (128 bytes, the swizzle width) with TMA into a ring of stages
+//   warp 1    of the pair's first CTA issues tcgen05.mma over each stage and commits it back to the ring
 //   warp 2    allocates and frees tensor memory: two accumulators, so the next tile's products run under an epilogue
 //   warps 4-7 epilogue: 32 accumulator rows each (a lane is a row), through shared memory to TMA stores where the result
 //             is a matrix; arrays that it combines with the accumulators come by TMA as well (AuxRing)
@@ -105,6 +105,14 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
                  "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
+}
+
+// One lane of a converged warp, always the same one.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{ .reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
 }
 
 struct Stop { volatile int* flag; unsigned long long* fail_word; };
@@ -388,7 +396,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __shared__ uint32_t tmem_base_smem;
     __shared__ int stop_flag;
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::stages, accf0 = empty0 + 8 * C::stages, acce0 = accf0 + 16, ring0 = acce0 + 16;
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = (int)threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
 
     chain_next();
@@ -409,25 +417,28 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __syncthreads();
     if constexpr (CG == 2) cluster_barrier();
     tc_fence_after();
-    chain_wait();
     const uint32_t tmem = tmem_base_smem;
     const Stop stop = {&stop_flag, shape.fail_word};
     const int first = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
 
+    // The two issuing roles run as whole warps on uniform values, with one lane elected for the instructions themselves: in a
+    // single lane's branch the compiler has to move every descriptor word from vector to uniform registers, and issuing the
+    // four products of a stage took ~590 cycles instead of ~130, more than the 512 that they take to compute.
     if (warp == 0) {
-        if (lane == 0) {
-            int s = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (int t = first; ok && t < shape.total; t += step) {
-                const Tile tile = tile_of<Epi::kSym>(shape, t);
-                const int m0 = tile.tm * C::BM + (int)rank * 128, n0 = tile.tn * BN + (int)rank * C::b_rows;
-                for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
-                    if (!(ok = mbar_wait(empty0 + 8 * s, phase ^ 1u, stop))) break;
-                    const uint32_t a = ring + s * C::stage_bytes, b = a + kStageBytesA;
-                    uint32_t full = full0 + 8 * s;
-                    if (rank == 0) mbar_expect(full, CG * C::stage_bytes);
-                    if constexpr (CG == 2) full = map_to_rank(full, 0);
+        int s = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        Tile tile = tile_of<Epi::kSym>(shape, first);
+        const uint32_t full_base = CG == 2 ? map_to_rank(full0, 0) : full0;
+        chain_wait();
+        for (int t = first; ok && t < shape.total;) {
+            const int m0 = tile.tm * C::BM + (int)rank * 128, n0 = tile.tn * BN + (int)rank * C::b_rows;
+            for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
+                if (!(ok = mbar_wait(empty0 + 8 * s, phase ^ 1u, stop))) break;
+                __syncwarp();
+                if (elect_one()) {
+                    const uint32_t a = ring + s * C::stage_bytes, b = a + kStageBytesA, full = full_base + 8 * s;
+                    if (rank == 0) mbar_expect(full0 + 8 * s, CG * C::stage_bytes);
                     if constexpr (A_MN) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) tma_load<CG>(a + i * 8192, &map_a, full, m0 + 64 * i, kb * kBK, tile.batch);
@@ -440,24 +451,28 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     } else {
                         tma_load<CG>(b, &map_b, full, kb * kBK, n0, tile.batch);
                     }
-                    if (++s == C::stages) { s = 0; phase ^= 1u; }
                 }
-            }
-            // every stage handed back: nothing of this CTA is in flight when it leaves
-            for (int i = 0; ok && i < C::stages; ++i) {
-                ok = mbar_wait(empty0 + 8 * s, phase ^ 1u, stop);
+                __syncwarp();
                 if (++s == C::stages) { s = 0; phase ^= 1u; }
             }
-            if (!ok) {      // given up: leave copies that are under way the time to land
-                const long long t0 = clock64();
-                while (clock64() - t0 < 10000000ll) __nanosleep(1000);
-            }
+            t += step;
+            if (t < shape.total) tile = tile_of<Epi::kSym>(shape, t);
+        }
+        // every stage handed back: nothing of this CTA is in flight when it leaves
+        for (int i = 0; ok && i < C::stages; ++i) {
+            ok = mbar_wait(empty0 + 8 * s, phase ^ 1u, stop);
+            if (++s == C::stages) { s = 0; phase ^= 1u; }
+        }
+        if (!ok) {      // given up: leave copies that are under way the time to land
+            const long long t0 = clock64();
+            while (clock64() - t0 < 10000000ll) __nanosleep(1000);
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             int s = 0, n_done = 0;
             uint32_t phase = 0;
             bool ok = true;
+            const uint64_t a0 = operand_desc<A_MN>(ring), b0 = operand_desc<B_MN>(ring + kStageBytesA);
             for (int t = first; ok && t < shape.total; t += step, ++n_done) {
                 const Tile tile = tile_of<Epi::kSym>(shape, t);
                 const int buf = n_done & 1;
@@ -466,16 +481,19 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
                 for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
                     if (!(ok = mbar_wait(full0 + 8 * s, phase, stop))) break;
+                    __syncwarp();
                     tc_fence_after();
-                    const uint64_t a = operand_desc<A_MN>(ring + s * C::stage_bytes);
-                    const uint64_t b = operand_desc<B_MN>(ring + s * C::stage_bytes + kStageBytesA);
+                    if (elect_one()) {
+                        const uint64_t a = a0 + (uint64_t)(s * (C::stage_bytes >> 4)), b = b0 + (uint64_t)(s * (C::stage_bytes >> 4));
 #pragma unroll
-                    for (int i = 0; i < kBK / 16; ++i)
-                        tc_mma<CG>(d, a + i * kDescStep<A_MN>, b + i * kDescStep<B_MN>, shape.idesc, (kb > tile.kb0 || i > 0) ? 1u : 0u);
-                    tc_commit<CG>(empty0 + 8 * s);
+                        for (int i = 0; i < kBK / 16; ++i)
+                            tc_mma<CG>(d, a + i * kDescStep<A_MN>, b + i * kDescStep<B_MN>, shape.idesc, (kb > tile.kb0 || i > 0) ? 1u : 0u);
+                        tc_commit<CG>(empty0 + 8 * s);
+                        if (kb + 1 == tile.kb1) tc_commit<CG>(accf0 + 8 * buf);
+                    }
+                    __syncwarp();
                     if (++s == C::stages) { s = 0; phase ^= 1u; }
                 }
-                if (ok) tc_commit<CG>(accf0 + 8 * buf);
             }
         }
     } else if (warp >= 4) {
@@ -489,6 +507,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         e.step = step;
         e.stop = &stop;
         typename Epi::State state;
+        chain_wait();
         epi.template start<C::BM, BN>(shape, e, state);
         int n_done = 0;
         for (int t = first; t < shape.total; t += step, ++n_done) {
