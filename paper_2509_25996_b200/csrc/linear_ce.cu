@@ -73,6 +73,7 @@ target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restr
 // ------------------------------------------------------------------------------------------------ E and its row sums
 
 struct ExpEpi : StoringEpi {
+    static constexpr bool kInputsOnly = true;
     CUtensorMap map_e;
     const float* refs;           // target logits of the piece
     const int32_t* labels;
@@ -91,7 +92,7 @@ struct ExpEpi : StoringEpi {
             if (n >= s.n) break;
             uint32_t slot = 0;
             if (write_e) slot = slot_acquire(e);
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < 2; ++h) {
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
@@ -333,7 +334,7 @@ struct HiddenGradEpi : StoringEpi {
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const uint32_t slot = slot_acquire(e);
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < 2; ++h) {
                 const int n1 = e.col0 + c + 32 * h;
                 uint4 x[4];
@@ -421,7 +422,7 @@ struct WeightGradEpi : StoringEpi {
 #pragma unroll 1
             for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
                 const uint32_t slot = slot_acquire(e);
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     float v[32];
                     tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);

@@ -151,6 +151,7 @@ __device__ __forceinline__ void write_f16(uint32_t slot, int lane, int half, con
 template <bool POLY>
 struct SymEpi {
     static constexpr bool kSym = true;
+    static constexpr bool kInputsOnly = false;
     // POLY: the ring of aux, replaced in place, and a slot for the mirrored chunk; otherwise a slot for each
     static constexpr int kStaging = (POLY ? kRing + 1 : 2) * kSlotBytes;
     using State = AuxRing;
@@ -189,8 +190,8 @@ struct SymEpi {
                 if (!ring.wait(e)) return false;
             }
             const uint32_t t = e.slots + (uint32_t)((POLY ? kRing : 1) * kSlotBytes);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {      // a loop: half the code to fetch in a kernel that runs a few microseconds
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
 #pragma unroll
@@ -247,6 +248,7 @@ struct SymEpi {
 template <bool LO_IN>
 struct StepEpi {
     static constexpr bool kSym = false;
+    static constexpr bool kInputsOnly = false;
     // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise two slots for hi in turn
     static constexpr int kStaging = (LO_IN ? kRing + 1 : kTurns) * kSlotBytes;
     using State = AuxRing;
@@ -288,8 +290,8 @@ struct StepEpi {
             } else {
                 hi = slot_acquire(e);
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {      // a loop: half the code to fetch in a kernel that runs a few microseconds
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
                 if constexpr (LO_IN) {
@@ -331,6 +333,7 @@ struct StepEpi {
 template <bool LO_IN>
 struct ResultEpi {
     static constexpr bool kSym = false;
+    static constexpr bool kInputsOnly = false;
     static constexpr int kStaging = (LO_IN ? kRing : 1) * kSlotBytes;
     using State = AuxRing;
     CUtensorMap map_lo_in;
@@ -362,8 +365,8 @@ struct ResultEpi {
                 slot = ring.slot(e);
                 if (!ring.wait(e)) return false;
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {      // a loop: half the code to fetch in a kernel that runs a few microseconds
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
 #pragma unroll
@@ -448,47 +451,94 @@ TileForm tile_form(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int
     return p <= s && p <= t ? kPair256 : s <= t ? kSingle128 : kSingle64;
 }
 
-// One square product over the batch: A = down X X^T (x: [mn] x [k] or, MN, its transpose), or P from A.
-template <int CG, int BN, bool MN, bool POLY>
-int sym_product(const uint16_t* x, int64_t mn, int64_t k, int64_t batch, int64_t x_ld, int64_t x_stride, uint16_t* out, const Layout& l,
-                float scale, float add, float diag, cudaStream_t stream)
+// The tensor maps of a call, made once: its arrays stay where they are from step to step.  X and its two words exist twice, in
+// turn.
+struct Maps {
+    CUtensorMap x_k[2], x_k_narrow[2];            // X (hi) as a K-major operand (k = columns) of 128 or 64 rows per CTA
+    CUtensorMap x_mn[2];                          // ... as an MN-major one (k = rows); its boxes are 64 wide either way
+    CUtensorMap x_hi[2], x_lo[2];                 // X in chunks of 32 rows x 64 columns
+    CUtensorMap a_op, a_op_narrow, p_op, p_op_narrow;      // the squares as K-major operands
+    CUtensorMap a_chunk, a_mirror, p_chunk, p_mirror;      // ... as chunks, and as the mirrored ones (64 rows x 32 columns)
+};
+
+int make_maps(Maps* m, uint16_t* const* hi, uint16_t* const* lo, const uint16_t* a, const uint16_t* p, int64_t rows, int64_t cols, int64_t batch, const Layout& l)
 {
-    CUtensorMap ma, mb;
-    Shape s;
-    SymEpi<POLY> epi;
-    int rc;
-    const int64_t stride = l.sq * l.sq_ld;
-    if ((rc = make_shape<CG, BN, MN, MN, SymEpi<POLY>>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
-    if ((rc = operand_map<MN>(&ma, x, mn, k, batch, x_ld, x_stride, 128)) != CAST_OK) return rc;
-    mb = ma;
-    if (BN / CG != 128 && (rc = operand_map<MN>(&mb, x, mn, k, batch, x_ld, x_stride, BN / CG)) != CAST_OK) return rc;
-    if ((rc = make_map(&epi.map_out, out, 2, mn, mn, batch, l.sq_ld, stride, 64, 32, true)) != CAST_OK) return rc;
-    if ((rc = make_map(&epi.map_mirror, out, 2, mn, mn, batch, l.sq_ld, stride, 32, 64, false)) != CAST_OK) return rc;
-    epi.map_aux = epi.map_out;
-    if (POLY && (rc = make_map(&epi.map_aux, x, 2, mn, mn, batch, x_ld, x_stride, 64, 32, true)) != CAST_OK) return rc;
-    epi.scale = scale;
-    epi.add = add;
-    epi.diag = diag;
-    return launch<CG, BN, MN, MN>(ma, mb, s, epi, stream);
+    const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
+    int rc = CAST_OK;
+    auto also = [&rc](int r) { if (rc == CAST_OK) rc = r; };
+    for (int i = 0; i < 2; ++i) {
+        also(operand_map<false>(&m->x_k[i], hi[i], rows, cols, batch, l.ld, xs, 128));
+        also(operand_map<false>(&m->x_k_narrow[i], hi[i], rows, cols, batch, l.ld, xs, 64));
+        also(operand_map<true>(&m->x_mn[i], hi[i], cols, rows, batch, l.ld, xs, 128));
+        also(make_map(&m->x_hi[i], hi[i], 2, cols, rows, batch, l.ld, xs, 64, 32, true));
+        also(make_map(&m->x_lo[i], lo[i], 2, cols, rows, batch, l.ld, xs, 64, 32, true));
+    }
+    auto square = [&](const uint16_t* x, CUtensorMap* op, CUtensorMap* narrow, CUtensorMap* chunk, CUtensorMap* mirror) {
+        also(operand_map<false>(op, x, l.sq, l.sq, batch, l.sq_ld, ps, 128));
+        also(operand_map<false>(narrow, x, l.sq, l.sq, batch, l.sq_ld, ps, 64));
+        also(make_map(chunk, x, 2, l.sq, l.sq, batch, l.sq_ld, ps, 64, 32, true));
+        also(make_map(mirror, x, 2, l.sq, l.sq, batch, l.sq_ld, ps, 32, 64, false));
+    };
+    square(a, &m->a_op, &m->a_op_narrow, &m->a_chunk, &m->a_mirror);
+    square(p, &m->p_op, &m->p_op_narrow, &m->p_chunk, &m->p_mirror);
+    return rc;
 }
 
-template <bool MN, bool POLY>
-int sym_product(TileForm f, const uint16_t* x, int64_t mn, int64_t k, int64_t batch, int64_t x_ld, int64_t x_stride, uint16_t* out, const Layout& l,
-                float scale, float add, float diag, cudaStream_t stream)
+// A = down X X^T over the batch (`cur`: which X), the tall form from X^T; then P = c A A + b A + a I.
+template <int CG, int BN, bool MN>
+int gram_product(const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, cudaStream_t stream)
 {
-    if (f == kPair256) return sym_product<2, 256, MN, POLY>(x, mn, k, batch, x_ld, x_stride, out, l, scale, add, diag, stream);
-    if (f == kSingle128) return sym_product<1, 128, MN, POLY>(x, mn, k, batch, x_ld, x_stride, out, l, scale, add, diag, stream);
-    return sym_product<1, 64, MN, POLY>(x, mn, k, batch, x_ld, x_stride, out, l, scale, add, diag, stream);
+    Shape s;
+    SymEpi<false> epi;
+    int rc;
+    if ((rc = make_shape<CG, BN, MN, MN, SymEpi<false>>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
+    epi.map_out = epi.map_aux = m.a_chunk;
+    epi.map_mirror = m.a_mirror;
+    epi.scale = down;
+    epi.add = epi.diag = 0.0f;
+    const bool narrow = BN / CG == 64;
+    return launch<CG, BN, MN, MN>(MN ? m.x_mn[cur] : m.x_k[cur], MN ? m.x_mn[cur] : narrow ? m.x_k_narrow[cur] : m.x_k[cur],
+                                  s, epi, stream);
+}
+
+template <int CG, int BN>
+int poly_product(const Maps& m, int64_t mn, int64_t batch, const float* q, cudaStream_t stream)
+{
+    Shape s;
+    SymEpi<true> epi;
+    int rc;
+    if ((rc = make_shape<CG, BN, false, false, SymEpi<true>>(&s, false, mn, mn, mn, batch, 1, 1)) != CAST_OK) return rc;
+    epi.map_out = m.p_chunk;
+    epi.map_mirror = m.p_mirror;
+    epi.map_aux = m.a_chunk;
+    epi.diag = q[0];
+    epi.add = q[1];
+    epi.scale = q[2];
+    return launch<CG, BN, false, false>(m.a_op, BN / CG == 64 ? m.a_op_narrow : m.a_op, s, epi, stream);
+}
+
+template <bool MN>
+int gram_product(TileForm f, const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, cudaStream_t stream)
+{
+    if (f == kPair256) return gram_product<2, 256, MN>(m, cur, mn, k, batch, down, stream);
+    if (f == kSingle128) return gram_product<1, 128, MN>(m, cur, mn, k, batch, down, stream);
+    return gram_product<1, 64, MN>(m, cur, mn, k, batch, down, stream);
+}
+
+int poly_product(TileForm f, const Maps& m, int64_t mn, int64_t batch, const float* q, cudaStream_t stream)
+{
+    if (f == kPair256) return poly_product<2, 256>(m, mn, batch, q, stream);
+    if (f == kSingle128) return poly_product<1, 128>(m, mn, batch, q, stream);
+    return poly_product<1, 64>(m, mn, batch, q, stream);
 }
 
 struct StepCall {
-    const uint16_t *p, *hi, *lo;      // lo NULL: X is hi alone
-    uint16_t *hi_out, *lo_out;        // hi_out NULL: the result
+    const Maps* maps;
     const OutTable* out;
-    int64_t rows, cols, batch;
-    const Layout* l;
+    int64_t rows, cols, batch, sq;
     float a, scale;
-    bool vec;
+    int cur;                          // which X
+    bool lo_in, lo_out, last, vec;
     cudaStream_t stream;
 };
 
@@ -496,32 +546,22 @@ struct StepCall {
 template <int CG, int BN, bool WIDE, class Epi>
 int step_product(const StepCall& c, Epi& epi)
 {
-    CUtensorMap ma, mb;
     Shape s;
     int rc;
-    const Layout& l = *c.l;
-    const int64_t xs = c.rows * l.ld, ps = l.sq * l.sq_ld;
-    if ((rc = make_shape<CG, BN, false, WIDE, Epi>(&s, false, c.rows, c.cols, l.sq, c.batch, 1, 16 / CG)) != CAST_OK) return rc;
-    if (WIDE) {
-        if ((rc = operand_map<false>(&ma, c.p, c.rows, c.rows, c.batch, l.sq_ld, ps, 128)) != CAST_OK) return rc;
-        if ((rc = operand_map<true>(&mb, c.hi, c.cols, c.rows, c.batch, l.ld, xs, BN / CG)) != CAST_OK) return rc;
-    } else {
-        if ((rc = operand_map<false>(&ma, c.hi, c.rows, c.cols, c.batch, l.ld, xs, 128)) != CAST_OK) return rc;
-        if ((rc = operand_map<false>(&mb, c.p, c.cols, c.cols, c.batch, l.sq_ld, ps, BN / CG)) != CAST_OK) return rc;
-    }
-    return launch<CG, BN, false, WIDE>(ma, mb, s, epi, c.stream);
+    const Maps& m = *c.maps;
+    const bool narrow = BN / CG == 64;
+    if ((rc = make_shape<CG, BN, false, WIDE, Epi>(&s, false, c.rows, c.cols, c.sq, c.batch, 1, 16 / CG)) != CAST_OK) return rc;
+    if (WIDE) return launch<CG, BN, false, WIDE>(m.p_op, m.x_mn[c.cur], s, epi, c.stream);
+    return launch<CG, BN, false, WIDE>(m.x_k[c.cur], narrow ? m.p_op_narrow : m.p_op, s, epi, c.stream);
 }
 
 template <int CG, int BN, bool WIDE, bool LO_IN>
 int step_product(const StepCall& c)
 {
-    const Layout& l = *c.l;
-    const int64_t xs = c.rows * l.ld;
-    auto map = [&](CUtensorMap* m, const uint16_t* x) { return make_map(m, x, 2, c.cols, c.rows, c.batch, l.ld, xs, 64, 32, true); };
-    int rc;
-    if (!c.hi_out) {
+    const Maps& m = *c.maps;
+    if (c.last) {
         ResultEpi<LO_IN> epi;
-        if ((rc = map(&epi.map_lo_in, LO_IN ? c.lo : c.hi)) != CAST_OK) return rc;
+        epi.map_lo_in = m.x_lo[c.cur];
         epi.out = *c.out;
         epi.a = c.a;
         epi.scale = c.scale;
@@ -529,21 +569,20 @@ int step_product(const StepCall& c)
         return step_product<CG, BN, WIDE>(c, epi);
     }
     StepEpi<LO_IN> epi;
-    if ((rc = map(&epi.map_hi, c.hi_out)) != CAST_OK) return rc;
-    epi.map_lo = epi.map_lo_in = epi.map_hi;
-    if (LO_IN && (rc = map(&epi.map_lo_in, c.lo)) != CAST_OK) return rc;
-    if (c.lo_out && (rc = map(&epi.map_lo, c.lo_out)) != CAST_OK) return rc;
+    epi.map_hi = m.x_hi[c.cur ^ 1];
+    epi.map_lo = m.x_lo[c.cur ^ 1];
+    epi.map_lo_in = m.x_lo[c.cur];
     epi.a = c.a;
-    epi.lo_out = c.lo_out != nullptr;
+    epi.lo_out = c.lo_out;
     return step_product<CG, BN, WIDE>(c, epi);
 }
 
 template <bool WIDE>
 int step_product(TileForm f, const StepCall& c)
 {
-    if (f == kPair256) return c.lo ? step_product<2, 256, WIDE, true>(c) : step_product<2, 256, WIDE, false>(c);
-    if (f == kSingle128) return c.lo ? step_product<1, 128, WIDE, true>(c) : step_product<1, 128, WIDE, false>(c);
-    return c.lo ? step_product<1, 64, WIDE, true>(c) : step_product<1, 64, WIDE, false>(c);
+    if (f == kPair256) return c.lo_in ? step_product<2, 256, WIDE, true>(c) : step_product<2, 256, WIDE, false>(c);
+    if (f == kSingle128) return c.lo_in ? step_product<1, 128, WIDE, true>(c) : step_product<1, 128, WIDE, false>(c);
+    return c.lo_in ? step_product<1, 64, WIDE, true>(c) : step_product<1, 64, WIDE, false>(c);
 }
 
 template <bool BF16, int VEC>
@@ -659,35 +698,21 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
         if (rc != CAST_OK) return rc;
         const TileForm gram = tile_form(l.sq, l.sq, big, batch, true, sms), poly = tile_form(l.sq, l.sq, l.sq, batch, true, sms);
         const TileForm step = tile_form(rows, cols, l.sq, batch, false, sms);
-        const float down = 1.0f / (kX * kX);
-        const int64_t xs = rows * l.ld, ps = l.sq * l.sq_ld;
+        Maps maps;
+        if ((rc = make_maps(&maps, hi, lo, a, p, rows, cols, batch, l)) != CAST_OK) return rc;
         bool has_lo = true;
         for (int k = 0; k < steps; ++k) {
             const float* q = coeffs ? coeffs + 3 * k : kQuintic;
             const int cur = k & 1;
-            rc = wide ? sym_product<false, false>(gram, hi[cur], rows, cols, batch, l.ld, xs, a, l, down, 0.0f, 0.0f, st)
-                      : sym_product<true, false>(gram, hi[cur], cols, rows, batch, l.ld, xs, a, l, down, 0.0f, 0.0f, st);
+            rc = wide ? gram_product<false>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), st)
+                      : gram_product<true>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), st);
             if (rc != CAST_OK) return rc;
-            if ((rc = sym_product<false, true>(poly, a, l.sq, l.sq, batch, l.sq_ld, ps, p, l, q[2], q[1], q[0], st)) != CAST_OK) return rc;
+            if ((rc = poly_product(poly, maps, l.sq, batch, q, st)) != CAST_OK) return rc;
             const bool last = k + 1 == steps;
             float amplify = 1.0f;      // of a small direction of X', by the steps after this one
             for (int j = k + 1; j < steps; ++j) amplify *= std::fabs(coeffs ? coeffs[3 * j] : kQuintic[0]);
             const bool lo_out = has_lo && !last && amplify > kAmplify;
-            StepCall c;
-            c.p = p;
-            c.hi = hi[cur];
-            c.lo = has_lo ? lo[cur] : nullptr;
-            c.hi_out = last ? nullptr : hi[cur ^ 1];
-            c.lo_out = lo_out ? lo[cur ^ 1] : nullptr;
-            c.out = &to;
-            c.rows = rows;
-            c.cols = cols;
-            c.batch = batch;
-            c.l = &l;
-            c.a = q[0];
-            c.scale = scale / kX;
-            c.vec = out_vec;
-            c.stream = st;
+            const StepCall c = {&maps, &to, rows, cols, batch, l.sq, q[0], scale / kX, cur, has_lo, lo_out, last, out_vec, st};
             if ((rc = wide ? step_product<true>(step, c) : step_product<false>(step, c)) != CAST_OK) return rc;
             has_lo = lo_out;
         }

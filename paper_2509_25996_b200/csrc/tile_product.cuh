@@ -23,20 +23,23 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "chained.cuh"
 
 namespace cast {
 namespace product {
 
-constexpr int kBK = 64;                          // k per stage: 64 x 2 bytes = one 128-byte swizzle row
+constexpr int kBK = 64;                          // k per block: 64 x 2 bytes = one 128-byte swizzle row
 constexpr int kThreads = 256;
 constexpr int kEpiWarps = 4;
-constexpr int kStageBytesA = 128 * kBK * 2;      // 128 rows of A per CTA
+constexpr int kStageBytesA = 128 * kBK * 2;      // one block of 128 rows of A
 constexpr int kSlotBytes = 4096;                 // epilogue staging: 32 rows of 128 bytes
 constexpr int kRing = 3;                         // slots of an epilogue's ring (see AuxRing)
+constexpr int64_t kRotateBytes = 8 << 20;
 constexpr long long kWaitCycles = 4000000000ll;  // ~2 s; the longest wait of a healthy run is a tile (tens of microseconds)
 
-// Shape of one launch.  k_blocks = ceil(k / 64) blocks are cut into `splits` runs of at most split_blocks, each of which
+// Shape of one launch.  k_blocks = ceil(k / (64 blocks per stage)) stages are cut into `splits` runs of at most split_blocks, each of which
 // is a tile of its own (its epilogue sees Tile::split).
 struct Shape {
     int m, n;                      // result rows and columns
@@ -44,6 +47,7 @@ struct Shape {
     int m_tiles, n_tiles, batch;
     int group;                     // tile rows that are walked together, so that their operands stay in L2 (symmetric: see tile_of)
     int total;                     // tiles of all batches and splits
+    int rotate;                    // tiles begin their k loop this many blocks apart
     uint32_t idesc;                // instruction descriptor
     unsigned long long* fail_word; // host memory
 };
@@ -134,6 +138,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const S
     return false;
 }
 
+// The same for a converged warp, with one answer for all of its lanes (which the compiler then knows to be uniform).
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const Stop& stop)
+{
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, stop));
+}
+
 __device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank)
 {
     uint32_t r;
@@ -176,15 +186,18 @@ __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.a
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// Descriptors by halves: the upper ones are constants, only the addresses in the lower ones change.
 template <int CG>
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate)
 {
     if constexpr (CG == 2)
-        asm volatile("{ .reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        asm volatile("{ .reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p; }"
+                     ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
     else
-        asm volatile("{ .reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        asm volatile("{ .reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p; }"
+                     ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
 // Arrives on `bar` (at the same offset in both CTAs of a pair) once every product issued so far has been done.
 template <int CG>
@@ -231,24 +244,27 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32])
 
 // Shared-memory matrix descriptor, 128-byte swizzle (bits 61-63 = 2, version 1 at bit 46): start address, leading and
 // stride byte offsets in units of 16 bytes.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 template <bool MN_MAJOR>
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr)
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr)
 {
-    constexpr uint64_t lead = MN_MAJOR ? (kBK * 128) >> 4 : 1;     // next 64 m (n) of an MN-major block; unused in K-major form
-    constexpr uint64_t hi = (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-    return hi | (uint64_t)((addr & 0x3FFFFu) >> 4);
+    constexpr uint32_t lead = MN_MAJOR ? (kBK * 128) >> 4 : 1;     // next 64 m (n) of an MN-major block; unused in K-major form
+    return (lead << 16) | ((addr & 0x3FFFFu) >> 4);
 }
 template <bool MN_MAJOR>
-constexpr uint64_t kDescStep = MN_MAJOR ? (16 * 128) >> 4 : (16 * 2) >> 4;      // 16 k further
+constexpr uint32_t kDescStep = MN_MAJOR ? (16 * 128) >> 4 : (16 * 2) >> 4;      // 16 k further
 
 // ------------------------------------------------------------------------------------------------ the kernel
 
-// `staging`: shared memory of one epilogue warp.
+// `staging`: shared memory of one epilogue warp.  A stage is one 64-deep block (issued in ~250 cycles, computed in 512 by a pair
+// and 256 by a single CTA with 128 columns), and two of them where they are computed in 128.
 template <int CG, int BN, int STAGING>
 struct Config {
     static constexpr int BM = 128 * CG;
+    static constexpr int blocks = CG == 1 && BN == 64 ? 2 : 1;
     static constexpr int b_rows = BN / CG;                         // rows of B staged by one CTA
-    static constexpr int stage_bytes = kStageBytesA + b_rows * kBK * 2;
+    static constexpr int b_bytes = b_rows * kBK * 2;               // of one block
+    static constexpr int stage_bytes = blocks * (kStageBytesA + b_bytes);
     static constexpr int room = (232448 - 1024 /* alignment */ - 768 /* barriers */ - kEpiWarps * STAGING) / stage_bytes;
     static constexpr int stages = room < 8 ? room : 8;
     static constexpr int smem_bytes = stages * stage_bytes + kEpiWarps * STAGING + 1024;
@@ -308,10 +324,12 @@ __device__ __forceinline__ void slot_store(const EpiTile& e, uint32_t slot_addr,
     }
 }
 
-// An epilogue provides: kSym (only tiles of the lower triangle), kStaging (bytes per warp), State (kept from tile to tile),
+// An epilogue provides: kSym (only tiles of the lower triangle), kInputsOnly (both operands are the caller's, whole before the
+// call's first kernel began), kStaging (bytes per warp), State (kept from tile to tile),
 // prefetch() (its tensor maps), start() (before the first tile), tile() (false: give up).
 struct StoringEpi {
     static constexpr bool kSym = false;
+    static constexpr bool kInputsOnly = false;
     static constexpr int kStaging = kTurns * kSlotBytes;
     struct State {};
     template <int BM, int BN>
@@ -397,7 +415,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __shared__ int stop_flag;
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::stages, accf0 = empty0 + 8 * C::stages, acce0 = accf0 + 16, ring0 = acce0 + 16;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = (int)threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    const uint32_t rank = CG == 2 ? __shfl_sync(0xFFFFFFFFu, cluster_rank(), 0) : 0u;
 
     chain_next();
     if (threadIdx.x == 0) {
@@ -417,7 +435,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __syncthreads();
     if constexpr (CG == 2) cluster_barrier();
     tc_fence_after();
-    const uint32_t tmem = tmem_base_smem;
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_base_smem, 0);
     const Stop stop = {&stop_flag, shape.fail_word};
     const int first = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
 
@@ -430,26 +448,31 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         bool ok = true;
         Tile tile = tile_of<Epi::kSym>(shape, first);
         const uint32_t full_base = CG == 2 ? map_to_rank(full0, 0) : full0;
-        chain_wait();
+        if constexpr (!Epi::kInputsOnly) chain_wait();
         for (int t = first; ok && t < shape.total;) {
             const int m0 = tile.tm * C::BM + (int)rank * 128, n0 = tile.tn * BN + (int)rank * C::b_rows;
-            for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
-                if (!(ok = mbar_wait(empty0 + 8 * s, phase ^ 1u, stop))) break;
-                __syncwarp();
+            int kb = tile.kb0 + (int)((unsigned)(t * shape.rotate) % (unsigned)(tile.kb1 - tile.kb0));
+            for (int i = tile.kb0; i < tile.kb1; ++i, kb = kb + 1 == tile.kb1 ? tile.kb0 : kb + 1) {
+                if (!(ok = mbar_wait_warp(empty0 + 8 * s, phase ^ 1u, stop))) break;
                 if (elect_one()) {
-                    const uint32_t a = ring + s * C::stage_bytes, b = a + kStageBytesA, full = full_base + 8 * s;
+                    const uint32_t a = ring + s * C::stage_bytes, b = a + C::blocks * kStageBytesA, full = full_base + 8 * s;
                     if (rank == 0) mbar_expect(full0 + 8 * s, CG * C::stage_bytes);
-                    if constexpr (A_MN) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) tma_load<CG>(a + i * 8192, &map_a, full, m0 + 64 * i, kb * kBK, tile.batch);
-                    } else {
-                        tma_load<CG>(a, &map_a, full, kb * kBK, m0, tile.batch);
-                    }
-                    if constexpr (B_MN) {
+                    for (int j = 0; j < C::blocks; ++j) {
+                        const int k = (kb * C::blocks + j) * kBK;      // past the end of k: zeros
+                        const uint32_t aj = a + j * kStageBytesA, bj = b + j * C::b_bytes;
+                        if constexpr (A_MN) {
 #pragma unroll
-                        for (int i = 0; i < C::b_rows / 64; ++i) tma_load<CG>(b + i * 8192, &map_b, full, n0 + 64 * i, kb * kBK, tile.batch);
-                    } else {
-                        tma_load<CG>(b, &map_b, full, kb * kBK, n0, tile.batch);
+                            for (int i = 0; i < 2; ++i) tma_load<CG>(aj + i * 8192, &map_a, full, m0 + 64 * i, k, tile.batch);
+                        } else {
+                            tma_load<CG>(aj, &map_a, full, k, m0, tile.batch);
+                        }
+                        if constexpr (B_MN) {
+#pragma unroll
+                            for (int i = 0; i < C::b_rows / 64; ++i) tma_load<CG>(bj + i * 8192, &map_b, full, n0 + 64 * i, k, tile.batch);
+                        } else {
+                            tma_load<CG>(bj, &map_b, full, k, n0, tile.batch);
+                        }
                     }
                 }
                 __syncwarp();
@@ -472,27 +495,33 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int s = 0, n_done = 0;
             uint32_t phase = 0;
             bool ok = true;
-            const uint64_t a0 = operand_desc<A_MN>(ring), b0 = operand_desc<B_MN>(ring + kStageBytesA);
+            const uint32_t a0 = desc_lo<A_MN>(ring), b0 = desc_lo<B_MN>(ring + C::blocks * kStageBytesA);
+            uint32_t at = 0;          // of the stage, in units of 16 bytes
             for (int t = first; ok && t < shape.total; t += step, ++n_done) {
                 const Tile tile = tile_of<Epi::kSym>(shape, t);
                 const int buf = n_done & 1;
-                if (!(ok = mbar_wait(acce0 + 8 * buf, (uint32_t)((n_done >> 1) & 1) ^ 1u, stop))) break;
+                if (!(ok = mbar_wait_warp(acce0 + 8 * buf, (uint32_t)((n_done >> 1) & 1) ^ 1u, stop))) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
+                uint32_t accumulate = 0;
                 for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
-                    if (!(ok = mbar_wait(full0 + 8 * s, phase, stop))) break;
-                    __syncwarp();
+                    if (!(ok = mbar_wait_warp(full0 + 8 * s, phase, stop))) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint64_t a = a0 + (uint64_t)(s * (C::stage_bytes >> 4)), b = b0 + (uint64_t)(s * (C::stage_bytes >> 4));
+                        const uint32_t a = a0 + at, b = b0 + at;
 #pragma unroll
-                        for (int i = 0; i < kBK / 16; ++i)
-                            tc_mma<CG>(d, a + i * kDescStep<A_MN>, b + i * kDescStep<B_MN>, shape.idesc, (kb > tile.kb0 || i > 0) ? 1u : 0u);
+                        for (int i = 0; i < C::blocks * (kBK / 16); ++i) {
+                            const int j = i / (kBK / 16), k = i % (kBK / 16);
+                            tc_mma<CG>(d, a + j * (kStageBytesA >> 4) + k * kDescStep<A_MN>, kDescHi, b + j * (C::b_bytes >> 4) + k * kDescStep<B_MN>,
+                                       kDescHi, shape.idesc, i ? 1u : accumulate);
+                        }
                         tc_commit<CG>(empty0 + 8 * s);
                         if (kb + 1 == tile.kb1) tc_commit<CG>(accf0 + 8 * buf);
                     }
                     __syncwarp();
-                    if (++s == C::stages) { s = 0; phase ^= 1u; }
+                    accumulate = 1;
+                    at += C::stage_bytes >> 4;
+                    if (++s == C::stages) { s = 0; at = 0; phase ^= 1u; }
                 }
             }
         }
@@ -571,9 +600,13 @@ int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t bat
     static_assert(!SYM || C::BM % BN == 0, "the triangle's blocks are whole tiles");
     s->m = (int)m;
     s->n = (int)n;
-    s->k_blocks = (int)((k + kBK - 1) / kBK);
+    s->k_blocks = (int)((k + C::blocks * kBK - 1) / (C::blocks * kBK));
+    if (splits > s->k_blocks) splits = s->k_blocks;
     s->split_blocks = (s->k_blocks + splits - 1) / splits;
     s->splits = (s->k_blocks + s->split_blocks - 1) / s->split_blocks;
+    // Operands of a few MB: tiles that walk k in step ask the same L2 lines of every SM at once.  Larger ones need them to, so that
+    // a line is still there for the next tile.
+    s->rotate = 2 * (m + n) * k <= kRotateBytes ? 5 : 0;
     s->m_tiles = (int)mt;
     s->n_tiles = (int)nt;
     s->batch = (int)batch;
@@ -592,7 +625,14 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const Shape& s, const Epi
     auto kernel = product_kernel<CG, BN, A_MN, B_MN, Epi>;
     int sms, rc;
     if ((rc = sm_count(&sms)) != CAST_OK) return rc;
-    CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes));
+    // once per kernel and device (setting it again, by another thread, does no harm)
+    static std::atomic<uint64_t> allowed{0};
+    int dev;
+    CAST_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1u)) {
+        CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem_bytes));
+        if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     const int units = s.total < sms / CG ? s.total : sms / CG;
     return launch_chained(false, kernel, dim3((unsigned)(units * CG)), kThreads, C::smem_bytes, stream, CG, a, b, s, epi);
 }
