@@ -14,8 +14,9 @@
 //     part that enters a piece and the part that leaves it), which a second kernel adds in order.  Every token row is read
 //     once, and a CTA's work does not depend on how often an id occurs; only the adding of partial rows of a frequent
 //     id is a chain, of tokens / kPiece rows.
-//   * rows without a token: the sort is latency, not bandwidth, so the whole gradient is filled with zeros by further CTAs of
-//     its kernels meanwhile.
+//   * up to kFew tokens are not sorted: the first token of an id looks for the others among the ids.
+//   * rows without a token become zeros in further CTAs of the kernel that sums: each looks up which of its kZeroRows rows
+//     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.
 #include <cmath>
 #include <type_traits>
 
@@ -25,10 +26,8 @@
 namespace cast {
 namespace {
 
-constexpr int kRun = 1024;          // keys ranked by counting
 constexpr int kWays = 16;           // runs merged at once
 constexpr int kPiece = 16;          // sorted tokens per CTA
-constexpr uint32_t kNoId = 0x7FFFFFFFu;
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -58,15 +57,19 @@ template <> struct Cols<8> {
         const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
         v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
     }
+    __device__ __forceinline__ void add(const Cols& o) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += o.v[i];
+    }
     __device__ __forceinline__ void store_partial(float* p) const {
         reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
         reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
-    __device__ __forceinline__ void store(uint16_t* p, float scale, bool accumulate) const {
+    static __device__ __forceinline__ Raw load_own(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }      // memory this kernel writes
+    // scale times the sums, added to `old` or not, rounded once
+    __device__ __forceinline__ void store(uint16_t* p, float scale, bool add, const Raw& old) const {
         uint4* q = reinterpret_cast<uint4*>(p);
-        uint4 old = make_uint4(0u, 0u, 0u, 0u);
-        if (accumulate) old = *q;
-        const uint32_t o[4] = {old.x, old.y, old.z, old.w};
+        const uint32_t o[4] = {add ? old.x : 0u, add ? old.y : 0u, add ? old.z : 0u, add ? old.w : 0u};
         uint32_t r[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[i] = pack_bf16(fmaf(scale, v[2 * i], bf16_lo(o[i])), fmaf(scale, v[2 * i + 1], bf16_hi(o[i])));
@@ -80,9 +83,11 @@ template <> struct Cols<1> {
     static __device__ __forceinline__ Raw load(const uint16_t* p) { return __ldg(p); }
     __device__ __forceinline__ void add(Raw x, float c) { v = fmaf(c, bf16_lo(x), v); }
     __device__ __forceinline__ void add_partial(const float* p) { v += __ldg(p); }
+    __device__ __forceinline__ void add(const Cols& o) { v += o.v; }
     __device__ __forceinline__ void store_partial(float* p) const { *p = v; }
-    __device__ __forceinline__ void store(uint16_t* p, float scale, bool accumulate) const {
-        *p = (uint16_t)(pack_bf16(fmaf(scale, v, accumulate ? bf16_lo(*p) : 0.0f), 0.0f) & 0xFFFFu);
+    static __device__ __forceinline__ Raw load_own(const uint16_t* p) { return *p; }
+    __device__ __forceinline__ void store(uint16_t* p, float scale, bool add, Raw old) const {
+        *p = (uint16_t)(pack_bf16(fmaf(scale, v, add ? bf16_lo(old) : 0.0f), 0.0f) & 0xFFFFu);
     }
 };
 
@@ -128,97 +133,44 @@ embed_kernel(const uint16_t* __restrict__ table, const int32_t* __restrict__ ids
     }
 }
 
-// ------------------------------------------------------------------------------------------------ zeros on the side
-
-// A part of the gradient that CTAs [first, first + blocks) of a kernel fill with zeros.
-struct Fill {
-    uint16_t* dest;
-    int64_t elems;
-    unsigned first, blocks;
-};
-constexpr int64_t kFillElems = 32768;      // per CTA: 64 KB
-
-__device__ __forceinline__ bool filled(const Fill& f)
-{
-    if (blockIdx.x < f.first) return false;
-    const int64_t from = (int64_t)(blockIdx.x - f.first) * kFillElems, to = min(f.elems, from + kFillElems);
-    if (blockIdx.y != 0) return true;
-    const int64_t odd = min(to - from, (int64_t)((16u - ((uint32_t)(uintptr_t)(f.dest + from) & 15u)) & 15u) / 2);      // up to a 16-byte boundary
-    const int64_t vecs = (to - from - odd) / 8;
-    uint4* v = reinterpret_cast<uint4*>(f.dest + from + odd);
-    for (int64_t i = threadIdx.x; i < vecs; i += blockDim.x) v[i] = make_uint4(0u, 0u, 0u, 0u);
-    for (int64_t i = threadIdx.x; i < odd; i += blockDim.x) f.dest[from + i] = 0;
-    for (int64_t i = from + odd + 8 * vecs + threadIdx.x; i < to; i += blockDim.x) f.dest[i] = 0;
-    return true;
-}
-
 // ------------------------------------------------------------------------------------------------ order of the tokens
 
-constexpr int kRankKeys = 128;        // keys of a run that one CTA places ...
-constexpr int kRankShare = 4;         // ... with this many threads each
-
-__global__ void __launch_bounds__(kRankKeys * kRankShare)
-rank_runs_kernel(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_ids, int32_t* __restrict__ order, int64_t tokens, uint32_t vocab,
-                 const __grid_constant__ Fill fill)
+__global__ void __launch_bounds__(kRankThreads)
+rank_runs_kernel(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_ids, int32_t* __restrict__ order, int64_t tokens, uint32_t vocab)
 {
-    __shared__ uint4 keys4[kRun / 4];
-    uint32_t* keys = reinterpret_cast<uint32_t*>(keys4);
     chain_next();
-    if (filled(fill)) return;
     chain_wait();
-    const int64_t run0 = (int64_t)(blockIdx.x / (kRun / kRankKeys)) * kRun;
-    const int len = (int)min((int64_t)kRun, tokens - run0);
-    const int first = (int)(blockIdx.x % (kRun / kRankKeys)) * kRankKeys;
-    if (first >= len) return;             // uniform over the CTA
-    const int n4 = (len + 3) / 4;
-    for (int i = threadIdx.x; i < 4 * n4; i += kRankKeys * kRankShare) {
-        // past the end: larger than every key, so that it comes before none
-        uint32_t k = 0xFFFFFFFFu;
-        if (i < len) {
-            k = (uint32_t)ids[run0 + i];
-            if (k >= vocab) k = kNoId;
-        }
-        keys[i] = k;
-    }
-    __syncthreads();
-    const int p = min(first + (int)threadIdx.x / kRankShare, len - 1), share = (int)threadIdx.x % kRankShare;
-    const uint32_t k = keys[p];
-    const int own = p >> 2;
-    int place = 0;
-#pragma unroll 4
-    for (int v = share; v < n4; v += kRankShare) {
-        const uint4 o = keys4[v];
-        const uint32_t limit = k + (v < own ? 1u : 0u);      // equal keys before this one count, equal keys after it do not
-        place += (o.x < limit) + (o.y < limit) + (o.z < limit) + (o.w < limit);
-    }
-    if (share == 0)
-        for (int j = 4 * own; j < p; ++j) place += keys[j] == k;
-#pragma unroll
-    for (int d = 1; d < kRankShare; d *= 2) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
-    if (share == 0 && first + (int)threadIdx.x / kRankShare < len) {
-        sorted_ids[run0 + place] = (int32_t)k;
-        order[run0 + place] = (int32_t)(run0 + p);
-    }
+    rank_keys(ids, sorted_ids, order, tokens, vocab, blockIdx.x);
 }
 
-constexpr int kMergeThreads = 128;
+constexpr int kMergeThreads = 256;
 
-// Merges groups of kWays runs of `run` keys.  The searches of a key advance together and without branches: kWays
-// independent loads per halving.
+// Merges groups of kWays runs of `run` keys.  The searches of a key advance together and without branches: kWays independent
+// loads per halving, from shared memory where a group fits (runs of kRun keys: 64 KB), from L2 where it does not.
+template <bool SHARED>
 __global__ void __launch_bounds__(kMergeThreads)
 merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict__ order_in, int32_t* __restrict__ ids_out,
-                  int32_t* __restrict__ order_out, int32_t tokens, int32_t run, const __grid_constant__ Fill fill)
+                  int32_t* __restrict__ order_out, int32_t tokens, int32_t run)
 {
+    extern __shared__ int32_t group_ids[];
     chain_next();
-    if (filled(fill)) return;
     chain_wait();
     const int32_t i = (int32_t)blockIdx.x * kMergeThreads + (int32_t)threadIdx.x;
-    if (i >= tokens) return;
     const int64_t group = (int64_t)run * kWays;
-    const int32_t group0 = (int32_t)(i / group * group);
-    const int own = (i - group0) / run;
-    const uint32_t k = (uint32_t)ids_in[i];
+    const int32_t group0 = (int32_t)((int64_t)blockIdx.x * kMergeThreads / group * group);      // of the CTA: its keys are of one run
     const int32_t left = tokens - group0;            // keys of the group, and of the groups after it
+    const int32_t* keys = ids_in + group0;
+    if constexpr (SHARED) {
+        const int32_t n4 = (min(left, kRun * kWays) + 3) / 4;      // the arrays are padded to whole vectors
+#pragma unroll 8
+        for (int32_t v = threadIdx.x; v < n4; v += kMergeThreads)
+            reinterpret_cast<int4*>(group_ids)[v] = __ldg(reinterpret_cast<const int4*>(keys) + v);
+        __syncthreads();
+        keys = group_ids;
+    }
+    if (i >= tokens) return;
+    const int own = (i - group0) / run;
+    const uint32_t k = (uint32_t)keys[i - group0];
     int32_t pos[kWays];
 #pragma unroll
     for (int j = 0; j < kWays; ++j) pos[j] = 0;
@@ -229,7 +181,7 @@ merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict_
             const int32_t at = pos[j] + half;
             const bool there = at <= run && before + at <= left;
             const uint32_t limit = j == own ? 0u : k + (j < own ? 1u : 0u);
-            const uint32_t other = (uint32_t)__ldg(ids_in + group0 + (there ? (int32_t)before + at - 1 : 0));
+            const uint32_t other = (uint32_t)keys[there ? (int32_t)before + at - 1 : 0];
             pos[j] = there && other < limit ? at : pos[j];
         }
     }
@@ -251,8 +203,9 @@ struct ScatterArgs {
     const int32_t* order;
     float* partial;               // [pieces][2][dim]: what enters a piece, what leaves it
     uint16_t* dest;
-    int64_t dim;
+    int64_t dim, vocab;
     int32_t tokens, pieces;
+    unsigned own;                 // CTAs that sum; the ones after them write zeros
     float scale;
     int lanes;                    // threads per row: 32 .. 256, a power of two
     int accumulate;
@@ -265,14 +218,81 @@ __device__ __forceinline__ int32_t column_of(const ScatterArgs& a)
     return ((int32_t)blockIdx.y * a.lanes + (int)threadIdx.x % a.lanes) * VEC;
 }
 
-// One piece of kPiece sorted tokens per group of a.lanes threads.
-template <int VEC, bool COEF>
-__global__ void __launch_bounds__(kScatterThreads, 3)
+// First sorted position with an id of at least `id`, found by the 32 lanes of a warp together (32 ways per step).
+__device__ __forceinline__ int32_t warp_lower_bound(const int32_t* ids, int32_t n, int64_t id)
+{
+    const int lane = (int)threadIdx.x & 31;
+    int32_t lo = 0, hi = n;                       // the answer is in [lo, hi]
+    while (lo < hi) {
+        const int32_t step = (hi - lo + 31) / 32;
+        const int64_t at = (int64_t)lo + (int64_t)(lane + 1) * step - 1;          // last position of this lane's part
+        const bool less = at < hi && (int64_t)__ldg(ids + at) < id;
+        const int parts = __popc(__ballot_sync(0xFFFFFFFFu, less));
+        lo += parts * step;
+        hi = min(hi, lo + step - 1);
+    }
+    return lo;
+}
+
+constexpr int kZeroRows = 32;
+
+// Writes the rows without a token among rows [row0, row0 + kZeroRows); `held`: bit i for row0 + i.
+template <int VEC>
+__device__ __forceinline__ void zero_rows(const ScatterArgs& a, int64_t row0, uint32_t held)
+{
+    using Raw = typename Cols<VEC>::Raw;
+    const uint32_t per = (uint32_t)(a.dim / VEC);
+    if (per >= (unsigned)kScatterThreads) {
+        for (int r = 0; r < kZeroRows && row0 + r < a.vocab; ++r) {
+            if (held >> r & 1u) continue;
+            Raw* to = reinterpret_cast<Raw*>(a.dest + (row0 + r) * a.dim);
+            for (uint32_t i = threadIdx.x; i < per; i += kScatterThreads) to[i] = Raw{};
+        }
+    } else {
+        Raw* to = reinterpret_cast<Raw*>(a.dest + row0 * a.dim);
+        const uint32_t rows = (uint32_t)min((int64_t)kZeroRows, a.vocab - row0);
+        for (uint32_t i = threadIdx.x; i < rows * per; i += kScatterThreads)
+            if (!(held >> (i / per) & 1u)) to[i] = Raw{};
+    }
+}
+
+// A CTA past the ones that sum: finds out which rows of its block the sorted ids hold, and writes the others.
+template <int VEC>
+__device__ __forceinline__ void zero_block(const ScatterArgs& a)
+{
+    __shared__ int32_t range[2];
+    __shared__ uint32_t held;
+    const int64_t row0 = (int64_t)(blockIdx.x - a.own) * kZeroRows;
+    const int warp = (int)threadIdx.x >> 5;
+    if (threadIdx.x == 0) held = 0;
+    if (warp < 2) {
+        const int32_t b = warp_lower_bound(a.ids, a.tokens, row0 + (warp ? kZeroRows : 0));
+        if ((threadIdx.x & 31) == 0) range[warp] = b;
+    }
+    __syncthreads();
+    for (int32_t p = range[0] + (int)threadIdx.x; p < range[1]; p += kScatterThreads) {
+        const int64_t id = __ldg(a.ids + p);
+        if (id < a.vocab) atomicOr(&held, 1u << (int)(id - row0));       // a block that ends past the vocabulary also sees the ids that are none
+    }
+    __syncthreads();
+    zero_rows<VEC>(a, row0, held);
+}
+
+// One piece of kPiece sorted tokens per group of a.lanes threads.  ACC: table rows are added to; what is there is asked for
+// together with the token rows, which would otherwise be one dependent load after the other.
+template <int VEC, bool COEF, bool ACC>
+__global__ void __launch_bounds__(kScatterThreads, ACC ? 2 : 3)
 piece_sums_kernel(const __grid_constant__ ScatterArgs a)
 {
     constexpr int kBatch = 8;             // token rows asked for at a time
     chain_next();
     chain_wait();
+    if constexpr (!ACC) {
+        if (blockIdx.x >= a.own) {
+            if (blockIdx.y == 0) zero_block<VEC>(a);
+            return;
+        }
+    }
     const int32_t piece = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
     if (piece >= a.pieces) return;
     const int32_t col = column_of<VEC>(a);
@@ -295,7 +315,7 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
     acc.zero();
 #pragma unroll
     for (int b = 0; b < kPiece; b += kBatch) {
-        typename Cols<VEC>::Raw x[kBatch];
+        typename Cols<VEC>::Raw x[kBatch], old[ACC ? kBatch : 1];
         float c[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
@@ -303,6 +323,8 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
             if (t[b + i] >= 0) {
                 x[i] = Cols<VEC>::load(src + (int64_t)t[b + i] * a.dim);
                 if constexpr (COEF) c[i] = __ldg(a.coef + t[b + i]);
+                if constexpr (ACC)
+                    if (id[b + i + 2] != id[b + i + 1]) old[i] = Cols<VEC>::load_own(a.dest + (int64_t)id[b + i + 1] * a.dim + col);
             }
         }
 #pragma unroll
@@ -312,7 +334,7 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
             const uint32_t own = id[b + i + 1];
             if (id[b + i + 2] != own) {                    // its last token
                 if (entered) acc.store_partial(partial);
-                else acc.store(a.dest + (int64_t)own * a.dim + col, a.scale, a.accumulate);
+                else acc.store(a.dest + (int64_t)own * a.dim + col, a.scale, ACC, old[ACC ? i : 0]);
                 entered = false;
                 acc.zero();
             } else if (b + i == kPiece - 1) {              // goes on in the next piece
@@ -342,50 +364,106 @@ __device__ __forceinline__ int32_t end_of(const int32_t* ids, int32_t n, int32_t
     return lo;
 }
 
-// The table rows that leave a piece they began in: what left it, then what entered the pieces after it.
+// The table rows that leave a piece they began in: what left it, then what entered the pieces after it.  One piece per CTA (most
+// find nothing to do); a frequent id's partial rows are cut into kJoinParts runs that are added side by side.
+constexpr int kJoinThreads = 512;
+constexpr int kJoinLanes = 128;
+constexpr int kJoinParts = kJoinThreads / kJoinLanes;
+
 template <int VEC>
-__global__ void __launch_bounds__(kScatterThreads)
+__global__ void __launch_bounds__(kJoinThreads)
 join_pieces_kernel(const __grid_constant__ ScatterArgs a)
 {
+    __shared__ Cols<VEC> part[kJoinParts - 1][kJoinLanes];
     chain_next();
     chain_wait();
-    const int32_t piece = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
+    const int32_t piece = (int32_t)blockIdx.x;             // never the last one: nothing leaves it
     const int32_t p0 = piece * kPiece, last = p0 + kPiece - 1;
-    if (piece + 1 >= a.pieces) return;                     // the last piece: nothing leaves it
-    const int32_t id = __ldg(a.ids + last);
-    if ((uint32_t)id == kNoId || __ldg(a.ids + last + 1) != id || (p0 > 0 && __ldg(a.ids + p0 - 1) == id)) return;
+    const int32_t id = __ldg(a.ids + last), after = __ldg(a.ids + last + 1), before = p0 > 0 ? __ldg(a.ids + p0 - 1) : -1;
+    if ((uint32_t)id == kNoId || after != id || before == id) return;
     const int32_t e = end_of(a.ids, a.tokens, last, id);
-    const int32_t col = column_of<VEC>(a);
-    if (col >= a.dim) return;
-    Cols<VEC> acc;
-    acc.zero();
-    const float* p = a.partial + (int64_t)piece * 2 * a.dim + col;
-    acc.add_partial(p + a.dim);
-    const int32_t count = (e - 1) / kPiece - piece;
+    const int lane = (int)threadIdx.x % kJoinLanes, own = (int)threadIdx.x / kJoinLanes;
+    const int32_t count = (e - 1) / kPiece - piece;        // pieces that it enters
+    const int32_t each = (count + kJoinParts - 1) / kJoinParts, from = own * each, to = min(count, from + each);
+    for (int64_t col0 = (int64_t)blockIdx.y * kJoinLanes * VEC; col0 < a.dim; col0 += (int64_t)gridDim.y * kJoinLanes * VEC) {
+        const int64_t col = col0 + (int64_t)lane * VEC;
+        const bool in = col < a.dim;
+        Cols<VEC> acc;
+        acc.zero();
+        if (in) {
+            const float* p = a.partial + (int64_t)piece * 2 * a.dim + col;
+            if (own == 0) acc.add_partial(p + a.dim);
+            p += (int64_t)(from + 1) * 2 * a.dim;
 #pragma unroll 8
-    for (int32_t i = 0; i < count; ++i) {
-        p += 2 * a.dim;
-        acc.add_partial(p);
+            for (int32_t i = from; i < to; ++i, p += 2 * a.dim) acc.add_partial(p);
+        }
+        __syncthreads();          // the sums of the columns before these have been taken
+        if (own > 0) part[own - 1][lane] = acc;
+        __syncthreads();
+        if (own == 0 && in) {
+#pragma unroll
+            for (int i = 0; i < kJoinParts - 1; ++i) acc.add(part[i][lane]);
+            uint16_t* dest = a.dest + (int64_t)id * a.dim + col;
+            typename Cols<VEC>::Raw old = {};
+            if (a.accumulate) old = Cols<VEC>::load_own(dest);
+            acc.store(dest, a.scale, a.accumulate, old);
+        }
     }
-    acc.store(a.dest + (int64_t)id * a.dim + col, a.scale, a.accumulate);
 }
 
-// Part `i` of `n` equal parts of a gradient, whole CTAs of zeros each.
-Fill fill_part(uint16_t* dest, int64_t elems, int i, int n, unsigned first)
+// Few tokens need no order: the group of threads that holds an id's first token looks through all ids for the others.
+constexpr int kFew = 256;
+
+template <int VEC, bool COEF>
+__global__ void __launch_bounds__(kScatterThreads)
+few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      // a.ids: as the caller gave them
 {
-    const int64_t blocks = (elems + kFillElems - 1) / kFillElems, from = blocks * i / n, to = blocks * (i + 1) / n;
-    const int64_t start = from * kFillElems, stop = to * kFillElems < elems ? to * kFillElems : elems;
-    return {dest + start, stop - start, first, (unsigned)(to - from)};
+    __shared__ uint32_t ids[kFew];
+    __shared__ uint32_t held;
+    chain_next();
+    if (threadIdx.x == 0) held = 0;
+    if ((int)threadIdx.x < a.tokens) ids[threadIdx.x] = (uint32_t)__ldg(a.ids + threadIdx.x);
+    __syncthreads();
+    if (blockIdx.x >= a.own) {           // a block of rows: zeros where no token is (only in a call of its own)
+        if (blockIdx.y != 0) return;
+        const int64_t row0 = (int64_t)(blockIdx.x - a.own) * kZeroRows;
+        if ((int)threadIdx.x < a.tokens) {
+            const int64_t id = (int64_t)ids[threadIdx.x] - row0;
+            if (ids[threadIdx.x] < vocab && id >= 0 && id < kZeroRows) atomicOr(&held, 1u << (int)id);
+        }
+        __syncthreads();
+        zero_rows<VEC>(a, row0, held);
+        return;
+    }
+    const int32_t t = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
+    const int32_t col = column_of<VEC>(a);
+    const uint32_t id = t < a.tokens ? ids[t] : 0xFFFFFFFFu;
+    bool first = id < vocab && col < a.dim;
+    for (int32_t i = 0; i < t; ++i) first &= ids[i] != id;
+    chain_wait();
+    if (!first) return;
+    uint16_t* to = a.dest + (int64_t)id * a.dim + col;
+    typename Cols<VEC>::Raw old = {};
+    if (a.accumulate) old = Cols<VEC>::load_own(to);
+    Cols<VEC> acc;
+    acc.zero();
+    for (int32_t i = t; i < a.tokens; ++i)
+        if (ids[i] == id) acc.add(Cols<VEC>::load(a.src + (int64_t)i * a.dim + col), COEF ? __ldg(a.coef + i) : 1.0f);
+    acc.store(to, a.scale, a.accumulate, old);
 }
 
 template <int VEC, bool COEF>
-int launch_scatter(const ScatterArgs& a, cudaStream_t stream)
+int launch_scatter(ScatterArgs a, const SortedTokens& sorted, cudaStream_t stream)
 {
-    const int64_t units = (a.dim + VEC - 1) / VEC, groups = kScatterThreads / a.lanes;
-    const dim3 grid((unsigned)((a.pieces + groups - 1) / groups), (unsigned)((units + a.lanes - 1) / a.lanes));
-    const int rc = launch_chained(false, piece_sums_kernel<VEC, COEF>, grid, kScatterThreads, 0, stream, 1, a);
+    const int64_t units = (a.dim + VEC - 1) / VEC, groups = kScatterThreads / a.lanes, items = sorted.few ? a.tokens : a.pieces;
+    a.own = (unsigned)((items + groups - 1) / groups);
+    const unsigned zeros = a.accumulate ? 0u : (unsigned)((a.vocab + kZeroRows - 1) / kZeroRows);
+    const dim3 grid(a.own + zeros, (unsigned)((units + a.lanes - 1) / a.lanes));
+    if (sorted.few) return launch_chained(sorted.first, few_tokens_kernel<VEC, COEF>, grid, kScatterThreads, 0, stream, 1, a, (uint32_t)a.vocab);
+    const int rc = a.accumulate ? launch_chained(false, piece_sums_kernel<VEC, COEF, true>, grid, kScatterThreads, 0, stream, 1, a)
+                                : launch_chained(false, piece_sums_kernel<VEC, COEF, false>, grid, kScatterThreads, 0, stream, 1, a);
     if (rc != CAST_OK || a.pieces < 2) return rc;
-    return launch_chained(false, join_pieces_kernel<VEC>, grid, kScatterThreads, 0, stream, 1, a);
+    return launch_chained(false, join_pieces_kernel<VEC>, dim3((unsigned)(a.pieces - 1), units > kJoinLanes ? 2u : 1u), kJoinThreads, 0, stream, 1, a);
 }
 
 int64_t sort_array_bytes(int64_t tokens) { return (int64_t)align256(4ull * (uint64_t)tokens); }
@@ -398,41 +476,53 @@ uint64_t scatter_scratch_bytes(int64_t tokens, int64_t dim)
     return 4ull * (uint64_t)sort_array_bytes(tokens) + align256(8ull * (uint64_t)((tokens + kPiece - 1) / kPiece) * (uint64_t)dim);
 }
 
-int sort_tokens(bool first, const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, uint16_t* zeros, SortedTokens* sorted,
-                cudaStream_t stream)
+void sort_arrays(void* scratch, int64_t tokens, int i, int32_t** ids, int32_t** order)
 {
     const int64_t step = sort_array_bytes(tokens);
     uint8_t* b = static_cast<uint8_t*>(scratch);
-    int32_t* id_buf[2] = {reinterpret_cast<int32_t*>(b), reinterpret_cast<int32_t*>(b + 2 * step)};
-    int32_t* or_buf[2] = {reinterpret_cast<int32_t*>(b + step), reinterpret_cast<int32_t*>(b + 3 * step)};
-    int kernels = 1, done = 0;            // that share the filling: the ranking and the merges
-    for (int64_t run = kRun; run < tokens; run *= kWays) ++kernels;
-    auto part = [&](unsigned own) {
-        const Fill f = zeros ? fill_part(zeros, vocab * dim, done, kernels, own) : Fill{nullptr, 0, own, 0};
-        ++done;
-        return f;
-    };
-    const unsigned rank_blocks = (unsigned)((tokens + kRun - 1) / kRun * (kRun / kRankKeys));
-    Fill f = part(rank_blocks);
-    int rc = launch_chained(first, rank_runs_kernel, dim3(rank_blocks + f.blocks), kRankKeys * kRankShare, 0, stream, 1, ids, id_buf[0], or_buf[0], tokens,
-                            (uint32_t)vocab, f);
-    if (rc != CAST_OK) return rc;
+    *ids = reinterpret_cast<int32_t*>(b + 2 * i * step);
+    *order = reinterpret_cast<int32_t*>(b + (2 * i + 1) * step);
+}
+
+int rank_blocks(int64_t tokens) { return tokens <= kFew ? 0 : (int)((tokens + kRun - 1) / kRun * (kRun / kRankKeys)); }
+
+int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, void* scratch, SortedTokens* sorted, cudaStream_t stream)
+{
+    *sorted = {};
+    sorted->tokens = tokens;
+    if (tokens <= kFew) {
+        sorted->few = true;
+        sorted->ids = ids;
+        sorted->first = !ranked;
+        return CAST_OK;
+    }
+    int32_t *id_buf[2], *or_buf[2];
+    for (int i = 0; i < 2; ++i) sort_arrays(scratch, tokens, i, &id_buf[i], &or_buf[i]);
+    int rc;
+    if (!ranked && (rc = launch_chained(true, rank_runs_kernel, dim3((unsigned)rank_blocks(tokens)), kRankThreads, 0, stream, 1, ids, id_buf[0],
+                                        or_buf[0], tokens, (uint32_t)vocab)) != CAST_OK)
+        return rc;
     int cur = 0;
     for (int64_t run = kRun; run < tokens; run *= kWays, cur ^= 1) {
-        const unsigned own = (unsigned)((tokens + kMergeThreads - 1) / kMergeThreads);
-        f = part(own);
-        rc = launch_chained(false, merge_runs_kernel, dim3(own + f.blocks), kMergeThreads, 0, stream, 1, id_buf[cur], or_buf[cur], id_buf[cur ^ 1],
-                            or_buf[cur ^ 1], (int32_t)tokens, (int32_t)run, f);
+        const dim3 grid((unsigned)((tokens + kMergeThreads - 1) / kMergeThreads));
+        if (run == kRun) {
+            constexpr size_t smem = sizeof(int32_t) * kRun * kWays;
+            CAST_CUDA_TRY(cudaFuncSetAttribute(merge_runs_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+            rc = launch_chained(false, merge_runs_kernel<true>, grid, kMergeThreads, smem, stream, 1, id_buf[cur], or_buf[cur], id_buf[cur ^ 1],
+                                or_buf[cur ^ 1], (int32_t)tokens, (int32_t)run);
+        } else {
+            rc = launch_chained(false, merge_runs_kernel<false>, grid, kMergeThreads, 0, stream, 1, id_buf[cur], or_buf[cur], id_buf[cur ^ 1],
+                                or_buf[cur ^ 1], (int32_t)tokens, (int32_t)run);
+        }
         if (rc != CAST_OK) return rc;
     }
     sorted->ids = id_buf[cur];
     sorted->order = or_buf[cur];
-    sorted->scratch = b + 4 * step;
-    sorted->tokens = tokens;
+    sorted->scratch = static_cast<uint8_t*>(scratch) + 4 * sort_array_bytes(tokens);
     return CAST_OK;
 }
 
-int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t dim,
+int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t vocab, int64_t dim,
                  bool accumulate, cudaStream_t stream)
 {
     ScatterArgs a;
@@ -445,14 +535,16 @@ int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* c
     a.tokens = (int32_t)sorted.tokens;
     a.pieces = (int32_t)((sorted.tokens + kPiece - 1) / kPiece);
     a.dim = dim;
+    a.vocab = vocab;
+    a.own = 0;
     a.scale = scale;
     a.accumulate = accumulate;
     const bool vec = dim % 8 == 0 && !((uintptr_t)src & 15u) && !((uintptr_t)dest & 15u);
     const int64_t units = vec ? dim / 8 : dim;
     a.lanes = 32;
     while (a.lanes < kScatterThreads && a.lanes < units) a.lanes *= 2;
-    if (vec) return coef ? launch_scatter<8, true>(a, stream) : launch_scatter<8, false>(a, stream);
-    return coef ? launch_scatter<1, true>(a, stream) : launch_scatter<1, false>(a, stream);
+    if (vec) return coef ? launch_scatter<8, true>(a, sorted, stream) : launch_scatter<8, false>(a, sorted, stream);
+    return coef ? launch_scatter<1, true>(a, sorted, stream) : launch_scatter<1, false>(a, sorted, stream);
 }
 
 }  // namespace cast
@@ -522,6 +614,6 @@ extern "C" int cast_embed_grad(const cast_bf16* grad_out, const int32_t* ids, ca
     const void* ptrs[4] = {grad_out, ids, grad_table, workspace};
     if ((rc = check_device_memory(ptrs, 4)) != CAST_OK) return rc;
     SortedTokens sorted;
-    if ((rc = sort_tokens(true, ids, tokens, vocab, dim, workspace, accumulate ? nullptr : grad_table, &sorted, (cudaStream_t)stream)) != CAST_OK) return rc;
-    return scatter_rows(sorted, grad_out, nullptr, scale, grad_table, dim, accumulate != 0, (cudaStream_t)stream);
+    if ((rc = sort_tokens(false, ids, tokens, vocab, workspace, &sorted, (cudaStream_t)stream)) != CAST_OK) return rc;
+    return scatter_rows(sorted, grad_out, nullptr, scale, grad_table, vocab, dim, accumulate != 0, (cudaStream_t)stream);
 }

@@ -14,22 +14,75 @@ struct SortedTokens {
     const int32_t* order;
     void* scratch;          // partial rows
     int64_t tokens;
+    bool few;               // so few that they are left as they came
+    bool first;             // few, and no kernel of the call has been launched yet
 };
 
-// Sorts into `scratch`.  zeros: an array [vocab][dim] that is filled with zeros meanwhile, or NULL.  `first`: the first kernel of the call (see chained.cuh).
-int sort_tokens(bool first, const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, uint16_t* zeros, SortedTokens* sorted,
-                cudaStream_t stream);
+// Sorts into `scratch`: runs of kRun keys (rank_keys, launched here, or with `ranked` already done by rank_blocks() CTAs of the
+// call's first kernel into sort_arrays(0)), then merges of the runs.
+int rank_blocks(int64_t tokens);
+void sort_arrays(void* scratch, int64_t tokens, int i, int32_t** ids, int32_t** order);
+int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, void* scratch, SortedTokens* sorted, cudaStream_t stream);
 
-// dest[v] = scale * sum_{t: id = v} coef[t] src[t] (coef NULL: 1) for the rows that have a token; accumulate: added to what
-// is there.
-int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t dim, bool accumulate,
-                 cudaStream_t stream);
+// dest[v] = scale * sum_{t: id = v} coef[t] src[t] (coef NULL: 1).  accumulate: added to dest, whose rows without a token are left
+// alone; otherwise those become zero.
+int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t vocab, int64_t dim,
+                 bool accumulate, cudaStream_t stream);
 
 // Address ranges [a, a + na) and [b, b + nb) share a byte.
 inline bool ranges_overlap(const void* a, uint64_t na, const void* b, uint64_t nb)
 {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return a && b && x < y + nb && y < x + na;
+}
+
+// ------------------------------------------------------------------------------------------------ runs of keys
+
+constexpr uint32_t kNoId = 0x7FFFFFFFu;
+constexpr int kRun = 1024;            // keys ranked by counting
+constexpr int kRankKeys = 128;        // keys of a run that one CTA places ...
+constexpr int kRankShare = 4;         // ... with this many threads each
+constexpr int kRankThreads = kRankKeys * kRankShare;
+
+// One CTA's part of ranking runs of kRun keys: a key's place is the number of keys of its run that come before it.
+__device__ __forceinline__ void rank_keys(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_ids, int32_t* __restrict__ order, int64_t tokens,
+                                          uint32_t vocab, unsigned block)
+{
+    __shared__ uint4 keys4[kRun / 4];
+    uint32_t* keys = reinterpret_cast<uint32_t*>(keys4);
+    const int64_t run0 = (int64_t)(block / (kRun / kRankKeys)) * kRun;
+    const int len = (int)min((int64_t)kRun, tokens - run0);
+    const int first = (int)(block % (kRun / kRankKeys)) * kRankKeys;
+    if (first >= len) return;             // uniform over the CTA
+    const int n4 = (len + 3) / 4;
+    for (int i = threadIdx.x; i < 4 * n4; i += kRankThreads) {
+        // past the end: larger than every key, so that it comes before none
+        uint32_t k = 0xFFFFFFFFu;
+        if (i < len) {
+            k = (uint32_t)ids[run0 + i];
+            if (k >= vocab) k = kNoId;
+        }
+        keys[i] = k;
+    }
+    __syncthreads();
+    const int p = min(first + (int)threadIdx.x / kRankShare, len - 1), share = (int)threadIdx.x % kRankShare;
+    const uint32_t k = keys[p];
+    const int own = p >> 2;
+    int place = 0;
+#pragma unroll 4
+    for (int v = share; v < n4; v += kRankShare) {
+        const uint4 o = keys4[v];
+        const uint32_t limit = k + (v < own ? 1u : 0u);      // equal keys before this one count, equal keys after it do not
+        place += (o.x < limit) + (o.y < limit) + (o.z < limit) + (o.w < limit);
+    }
+    if (share == 0)
+        for (int j = 4 * own; j < p; ++j) place += keys[j] == k;
+#pragma unroll
+    for (int d = 1; d < kRankShare; d *= 2) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
+    if (share == 0 && first + (int)threadIdx.x / kRankShare < len) {
+        sorted_ids[run0 + place] = (int32_t)k;
+        order[run0 + place] = (int32_t)(run0 + p);
+    }
 }
 
 inline uint64_t align256(uint64_t n) { return (n + 255u) & ~255ull; }

@@ -44,13 +44,19 @@ __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0
 
 // ------------------------------------------------------------------------------------------------ target logits
 
-// refs[t] = h_t . w_label, 0 without a label.  One warp per token; dim % 8 == 0.
-__global__ void __launch_bounds__(256)
+// refs[t] = h_t . w_label, 0 without a label.  One warp per token; dim % 8 == 0.  The CTAs after the tokens' own begin the order of
+// the labels, which dW's label terms need.
+__global__ void __launch_bounds__(kRankThreads)
 target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restrict__ weight, const int32_t* __restrict__ labels,
-                    float* __restrict__ refs, int64_t tokens, int vocab, int dim)
+                    float* __restrict__ refs, int64_t tokens, int vocab, int dim, unsigned own, int32_t* __restrict__ sorted_ids,
+                    int32_t* __restrict__ order)
 {
     chain_next();
-    const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (blockIdx.x >= own) {
+        rank_keys(labels, sorted_ids, order, tokens, (uint32_t)vocab, blockIdx.x - own);
+        return;
+    }
+    const int64_t t = (int64_t)blockIdx.x * (kRankThreads / 32) + (threadIdx.x >> 5);
     if (t >= tokens) return;
     const int lane = (int)threadIdx.x & 31;
     const int label = labels[t];
@@ -180,6 +186,8 @@ struct FinishArgs {
     float grad_scale;
 };
 
+constexpr int kAhead = 4;             // vectors of the token's hidden row that a lane loads before it needs them
+
 __global__ void __launch_bounds__(256)
 finish_kernel(const __grid_constant__ FinishArgs p)
 {
@@ -187,6 +195,15 @@ finish_kernel(const __grid_constant__ FinishArgs p)
     __shared__ float sh_a[kFinishTokens], sh_ref[kFinishTokens];
     __shared__ int sh_over[kFinishTokens];
     chain_next();
+    const int warp = (int)threadIdx.x >> 5, wl = (int)threadIdx.x & 31;      // later: one warp per token
+    const int64_t t0 = (int64_t)blockIdx.x * kFinishTokens;
+    const uint4* h = reinterpret_cast<const uint4*>(p.hidden + (t0 + warp) * p.dim);
+    uint4 ahead[kAhead];
+    if (p.scaled && t0 + warp < p.tokens) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (wl + 32 * i < p.dim / 8) ahead[i] = __ldg(h + wl + 32 * i);
+    }
     chain_wait();
     const int k = (int)threadIdx.x & 7, lane = (int)threadIdx.x >> 3;
     const int64_t t = (int64_t)blockIdx.x * kFinishTokens + k;
@@ -250,22 +267,20 @@ finish_kernel(const __grid_constant__ FinishArgs p)
         sh_over[k] = active && top2 != ref2;
     }
     __syncthreads();
-    const int64_t t0 = (int64_t)blockIdx.x * kFinishTokens;
-    const int warp = (int)threadIdx.x >> 5, wl = (int)threadIdx.x & 31;      // one warp per token
     if (t0 + warp >= p.tokens) return;
     if (p.scaled) {
         const float a = sh_a[warp];
-        const uint4* h = reinterpret_cast<const uint4*>(p.hidden + (t0 + warp) * p.dim);
         uint4* o = reinterpret_cast<uint4*>(p.scaled + (t0 + warp) * p.dim);
+        auto scaled = [a](const uint4& x) {
+            if (a == 0.0f) return make_uint4(0u, 0u, 0u, 0u);        // a token without a label contributes nothing, whatever it holds
+            return make_uint4(pack2(a * lo16(x.x), a * hi16(x.x)), pack2(a * lo16(x.y), a * hi16(x.y)),
+                              pack2(a * lo16(x.z), a * hi16(x.z)), pack2(a * lo16(x.w), a * hi16(x.w)));
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (wl + 32 * i < p.dim / 8) o[wl + 32 * i] = scaled(ahead[i]);
 #pragma unroll 4
-        for (int i = wl; i < p.dim / 8; i += 32) {
-            const uint4 x = __ldg(h + i);
-            uint4 r = make_uint4(0u, 0u, 0u, 0u);        // a token without a label contributes nothing, whatever it holds
-            if (a != 0.0f)
-                r = make_uint4(pack2(a * lo16(x.x), a * hi16(x.x)), pack2(a * lo16(x.y), a * hi16(x.y)),
-                               pack2(a * lo16(x.z), a * hi16(x.z)), pack2(a * lo16(x.w), a * hi16(x.w)));
-            o[i] = r;
-        }
+        for (int i = wl + 32 * kAhead; i < p.dim / 8; i += 32) o[i] = scaled(__ldg(h + i));
     }
     if (p.e && sh_over[warp]) {
         uint16_t* row = p.e + (t0 + warp) * p.e_ld;
@@ -369,24 +384,26 @@ join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restri
                         int64_t tokens, int dim, int vocab, int splits)
 {
     chain_next();
-    chain_wait();
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int per = dim / 8;
     if (u >= tokens * per) return;
     const int64_t t = u / per;
     const int c = (int)(u - t * per) * 8;
-    const int label = labels[t];
-    uint4 r = make_uint4(0u, 0u, 0u, 0u);
-    if ((unsigned)label < (unsigned)vocab) {
+    const int label = __ldg(labels + t);
+    const bool active = (unsigned)label < (unsigned)vocab;
+    uint4 w = make_uint4(0u, 0u, 0u, 0u), r = w;
+    if (active) w = __ldg(reinterpret_cast<const uint4*>(weight + (int64_t)label * dim + c));
+    chain_wait();
+    if (active) {
         float v[8] = {};
+        const float4* p = reinterpret_cast<const float4*>(partial + t * dim + c);
+        const int64_t step = tokens * dim / 4;
+        const float fa = a[t], fb = b[t];
 #pragma unroll 8
-        for (int s = 0; s < splits; ++s) {
-            const float4* p = reinterpret_cast<const float4*>(partial + ((int64_t)s * tokens + t) * dim + c);
+        for (int s = 0; s < splits; ++s, p += step) {
             const float4 x = __ldg(p), y = __ldg(p + 1);
             v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
         }
-        const float fa = a[t], fb = b[t];
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(weight + (int64_t)label * dim + c));
         r = make_uint4(pack2(fa * v[0] - fb * lo16(w.x), fa * v[1] - fb * hi16(w.x)), pack2(fa * v[2] - fb * lo16(w.y), fa * v[3] - fb * hi16(w.y)),
                        pack2(fa * v[4] - fb * lo16(w.z), fa * v[5] - fb * hi16(w.z)), pack2(fa * v[6] - fb * lo16(w.w), fa * v[7] - fb * hi16(w.w)));
     }
@@ -670,8 +687,11 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
     float* refs = reinterpret_cast<float*>(ws + l.refs);
     float* a = reinterpret_cast<float*>(ws + l.a);
     float* b = reinterpret_cast<float*>(ws + l.b);
-    if ((rc = launch_chained(true, target_logit_kernel, dim3((unsigned)((tokens + 7) / 8)), 256, 0, st, 1, hidden, weight, labels, refs, tokens,
-                             (int)vocab, (int)dim)) != CAST_OK)
+    const unsigned own = (unsigned)((tokens + kRankThreads / 32 - 1) / (kRankThreads / 32));
+    int32_t *sorted_ids, *order;
+    sort_arrays(ws + l.scatter, tokens, 0, &sorted_ids, &order);
+    if ((rc = launch_chained(true, target_logit_kernel, dim3(own + (grad_weight ? (unsigned)rank_blocks(tokens) : 0u)), kRankThreads, 0, st, 1, hidden,
+                             weight, labels, refs, tokens, (int)vocab, (int)dim, own, sorted_ids, order)) != CAST_OK)
         return rc;
     for (int64_t i = 0; i < l.pieces; ++i) {
         const int64_t t0 = i * l.piece, n = tokens - t0 < l.piece ? tokens - t0 : l.piece;
@@ -705,9 +725,9 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
     }
     if (grad_weight) {
         SortedTokens sorted;
-        if ((rc = sort_tokens(false, labels, tokens, vocab, dim, ws + l.scatter, nullptr, &sorted, st)) != CAST_OK) return rc;
+        if ((rc = sort_tokens(true, labels, tokens, vocab, ws + l.scatter, &sorted, st)) != CAST_OK) return rc;
         // b holds s S / (1 + S): the label's term of dW is -b H
-        if ((rc = scatter_rows(sorted, hidden, b, -1.0f, grad_weight, dim, true, st)) != CAST_OK) return rc;
+        if ((rc = scatter_rows(sorted, hidden, b, -1.0f, grad_weight, vocab, dim, true, st)) != CAST_OK) return rc;
     }
     return CAST_OK;
 }
