@@ -33,10 +33,23 @@ def _tokens(ids: torch.Tensor, name: str, device) -> int:
     return ids.numel()
 
 
-def _workspace(status_and_bytes, device) -> torch.Tensor:
+def _workspace(status_and_bytes, like: torch.Tensor) -> torch.Tensor:
     rc, n = status_and_bytes
     B.check(rc)
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return like.new_empty(n, dtype=torch.uint8)
+
+
+# the current stream as the integer the library takes; the object that torch.cuda.current_stream() makes costs 3 us
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _on(device: torch.device, call) -> None:
+    """call(stream) with `device` current, and its current stream."""
+    if device.index == torch.cuda.current_device():
+        B.check(call(_raw_stream(device.index)))
+    else:
+        with torch.cuda.device(device):
+            B.check(call(_raw_stream(device.index)))
 
 
 def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -46,14 +59,13 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optio
     vocab, dim = table.shape
     shape = (*ids.shape, dim)
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=table.device)
+        out = table.new_empty(shape)
     else:
         _need(out, "out", torch.bfloat16, len(shape), table.device)
         if tuple(out.shape) != shape:
             raise ValueError(f"out: shape {tuple(out.shape)} instead of {shape}")
     if tokens:
-        with torch.cuda.device(table.device):
-            B.check(B.cast_embed(table, ids, out, tokens, vocab, dim, scale, torch.cuda.current_stream()))
+        _on(table.device, lambda stream: B.cast_embed(table.data_ptr(), ids.data_ptr(), out.data_ptr(), tokens, vocab, dim, scale, stream))
     return out
 
 
@@ -68,17 +80,16 @@ def embed_grad(grad_out: torch.Tensor, ids: torch.Tensor, vocab: int, scale: flo
     if grad_table is None:
         if accumulate:
             raise ValueError("accumulate needs a grad_table")
-        grad_table = torch.empty((vocab, dim), dtype=torch.bfloat16, device=dev)
+        grad_table = grad_out.new_empty((vocab, dim))
     else:
         _need(grad_table, "grad_table", torch.bfloat16, 2, dev)
         if tuple(grad_table.shape) != (vocab, dim):
             raise ValueError(f"grad_table: shape {tuple(grad_table.shape)} instead of {(vocab, dim)}")
     if tokens == 0:
         return grad_table if accumulate else grad_table.zero_()
-    with torch.cuda.device(dev):
-        ws = _workspace(B.cast_embed_grad_workspace(tokens, dim), dev)
-        B.check(B.cast_embed_grad(grad_out, ids, grad_table, tokens, vocab, dim, scale, accumulate, ws, ws.numel(),
-                                  torch.cuda.current_stream()))
+    ws = _workspace(B.cast_embed_grad_workspace(tokens, dim), grad_out)
+    _on(dev, lambda stream: B.cast_embed_grad(grad_out.data_ptr(), ids.data_ptr(), grad_table.data_ptr(), tokens, vocab, dim, scale, accumulate,
+                                              ws.data_ptr(), ws.numel(), stream))
     return grad_table
 
 
@@ -96,15 +107,17 @@ def linear_ce(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, 
         raise ValueError(f"weight: {weight.shape[1]} columns for hidden states of {dim}")
     if _tokens(labels, "labels", dev) != tokens or labels.dim() != 1:
         raise ValueError(f"labels: shape {tuple(labels.shape)} instead of {(tokens,)}")
-    loss = torch.empty(tokens, dtype=torch.float32, device=dev)
+    loss = hidden.new_empty(tokens, dtype=torch.float32)
     gh = torch.empty_like(hidden) if hidden_grad else None
     gw = torch.empty_like(weight) if weight_grad else None
     if tokens == 0:
         return loss, gh, gw.zero_() if gw is not None else None
-    with torch.cuda.device(dev):
-        ws = _workspace(B.cast_linear_ce_workspace(tokens, vocab, dim, piece_tokens, hidden_grad, weight_grad), dev)
-        B.check(B.cast_linear_ce(hidden, weight, labels, loss, gh, gw, tokens, vocab, dim, grad_scale, piece_tokens, ws, ws.numel(),
-                                 torch.cuda.current_stream()))
+    def call(stream):
+        rc, need = B.cast_linear_ce_workspace(tokens, vocab, dim, piece_tokens, hidden_grad, weight_grad)      # depends on the device
+        ws = _workspace((rc, need), hidden)
+        return B.cast_linear_ce(hidden.data_ptr(), weight.data_ptr(), labels.data_ptr(), loss.data_ptr(), None if gh is None else gh.data_ptr(),
+                                None if gw is None else gw.data_ptr(), tokens, vocab, dim, grad_scale, piece_tokens, ws.data_ptr(), need, stream)
+    _on(dev, call)
     return loss, gh, gw
 
 
@@ -123,7 +136,7 @@ def orthogonalize(updates: Sequence[torch.Tensor], steps: int = 5, coeffs: Optio
         if u.shape != first.shape:
             raise ValueError(f"updates[{i}]: shape {tuple(u.shape)} instead of {(rows, cols)}")
     if outs is None:
-        outs = [torch.empty((rows, cols), dtype=torch.bfloat16, device=first.device) for _ in updates]
+        outs = [first.new_empty((rows, cols), dtype=torch.bfloat16) for _ in updates]
     else:
         if len(outs) != len(updates):
             raise ValueError(f"{len(outs)} outs for {len(updates)} updates")
@@ -137,8 +150,7 @@ def orthogonalize(updates: Sequence[torch.Tensor], steps: int = 5, coeffs: Optio
             coeffs = coeffs * steps
         if len(coeffs) != 3 * steps:
             raise ValueError(f"{len(coeffs)} coefficients for {steps} steps")
-    with torch.cuda.device(first.device):
-        ws = _workspace(B.cast_orthogonalize_workspace(len(updates), rows, cols), first.device)
-        B.check(B.cast_orthogonalize(updates, first.dtype == torch.bfloat16, outs, rows, cols, coeffs, steps, eps, scale, ws, ws.numel(),
-                                     torch.cuda.current_stream()))
+    ws = _workspace(B.cast_orthogonalize_workspace(len(updates), rows, cols), first)
+    _on(first.device, lambda stream: B.cast_orthogonalize([u.data_ptr() for u in updates], first.dtype == torch.bfloat16, [o.data_ptr() for o in outs],
+                                                          rows, cols, coeffs, steps, eps, scale, ws.data_ptr(), ws.numel(), stream))
     return list(outs)
