@@ -67,7 +67,8 @@ enum cast_status {
                                copies (see CAST_F_BULK_STAGING): a tile of the state was left as it
                                was; the plan refuses further steps.  Also: an earlier tensor-core product
                                (cast_linear_ce, cast_orthogonalize) gave up a wait; its results are
-                               incomplete, and both calls refuse from then on                 */
+                               incomplete, and both calls refuse until cast_product_failures
+                               has cleared it                                                 */
 };
 
 enum cast_flags {
@@ -520,6 +521,15 @@ CAST_API int cast_orthogonalize_workspace(int n, int64_t rows, int64_t cols, uin
 CAST_API int cast_orthogonalize(const void* const* updates, int updates_bf16, cast_bf16* const* out, int n, int64_t rows, int64_t cols,
                        const float* coeffs, int steps, float eps, float scale, void* workspace, uint64_t workspace_bytes,
                        cast_stream_t stream);
+
+/*
+ * cast_product_failures -- the tensor-core products of cast_linear_ce and cast_orthogonalize wait for their copies with a limit
+ * (about 2 s; a wait takes microseconds).  One that gives up leaves its results incomplete and is counted in a word of the
+ * process; both calls then answer CAST_ERR_STAGING.  *count_out (may be NULL) receives the count as it was; then action 0
+ * leaves it, 1 adds one (fault injection on the host, for tests of a caller's error handling), 2 clears it.  Does not
+ * synchronise: what is still running may yet be counted.
+ */
+CAST_API int cast_product_failures(unsigned long long* count_out, int action);
 
 /*
  * Measurement aids.  Neither computes anything of the method (the paper has no counterpart); a benchmark puts their

@@ -11,7 +11,7 @@ from .binding import (  # noqa: F401
     cast_host_ctx_create, cast_host_step, cast_host_ctx_sync, cast_host_ctx_destroy,
     cast_host_step_static, cast_kd_loss, cast_prune_fold, cast_plan_prune_fold, cast_mask_stats, cast_plan_mask_stats,
     cast_embed, cast_embed_grad, cast_embed_grad_workspace, cast_linear_ce, cast_linear_ce_workspace,
-    cast_orthogonalize, cast_orthogonalize_workspace,
+    cast_orthogonalize, cast_orthogonalize_workspace, cast_product_failures,
     cast_probe_launch, cast_probe_stream, cast_bulk_timeout_count,
     cast_strerror, cast_last_cuda_error, cast_kernel_launch_count,
 )

@@ -45,7 +45,7 @@ EXPORTS = (
     "cast_host_ctx_create", "cast_host_step", "cast_host_ctx_sync", "cast_host_ctx_destroy",
     "cast_host_step_static", "cast_kd_loss", "cast_prune_fold", "cast_plan_prune_fold", "cast_mask_stats", "cast_plan_mask_stats",
     "cast_embed", "cast_embed_grad", "cast_embed_grad_workspace", "cast_linear_ce", "cast_linear_ce_workspace",
-    "cast_orthogonalize", "cast_orthogonalize_workspace",
+    "cast_orthogonalize", "cast_orthogonalize_workspace", "cast_product_failures",
     "cast_probe_launch", "cast_probe_stream", "cast_bulk_timeout_count",
     "cast_strerror", "cast_last_cuda_error", "cast_kernel_launch_count",
 )
@@ -170,6 +170,8 @@ def load_library() -> ctypes.CDLL:
     lib.cast_orthogonalize.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int, ctypes.POINTER(ctypes.c_void_p), ctypes.c_int,
                                        ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_float,
                                        ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
+    lib.cast_product_failures.restype = ctypes.c_int
+    lib.cast_product_failures.argtypes = [ctypes.POINTER(ctypes.c_ulonglong), ctypes.c_int]
     lib.cast_host_ctx_sync.restype = ctypes.c_int
     lib.cast_host_ctx_sync.argtypes = [ctypes.c_void_p]
     lib.cast_host_ctx_destroy.restype = ctypes.c_int
@@ -416,6 +418,13 @@ def cast_orthogonalize(updates, updates_bf16, outs, rows, cols, coeffs, steps, e
     pc = None if coeffs is None else (ctypes.c_float * len(coeffs))(*coeffs)
     return load_library().cast_orthogonalize(pu, 1 if updates_bf16 else 0, po, 0 if updates is None else len(updates), int(rows), int(cols),
                                              pc, int(steps), eps, scale, _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def cast_product_failures(action: int = 0):
+    """Returns (status, count before the action); action 0 reads, 1 adds one (for tests), 2 clears."""
+    out = ctypes.c_ulonglong(0)
+    rc = load_library().cast_product_failures(ctypes.byref(out), int(action))
+    return rc, int(out.value)
 
 
 def cast_bulk_timeout_count():

@@ -44,7 +44,10 @@ int make_map(CUtensorMap* map, const void* base, int elem_bytes, uint64_t inner,
     return r == CUDA_SUCCESS ? CAST_OK : cuda_failed(cudaErrorInvalidValue);
 }
 
-int fail_word(unsigned long long** word)
+namespace {
+
+// Allocated at the first use and kept until the process ends: kernels may still be reading its address.
+int the_word(unsigned long long** word)
 {
     static std::mutex lock;
     static unsigned long long* w = nullptr;
@@ -56,7 +59,16 @@ int fail_word(unsigned long long** word)
         *w = 0ull;
     }
     *word = w;
-    return *static_cast<volatile unsigned long long*>(w) == 0ull ? CAST_OK : CAST_ERR_STAGING;
+    return CAST_OK;
+}
+
+}  // namespace
+
+int fail_word(unsigned long long** word)
+{
+    const int rc = the_word(word);
+    if (rc != CAST_OK) return rc;
+    return *static_cast<volatile unsigned long long*>(*word) == 0ull ? CAST_OK : CAST_ERR_STAGING;
 }
 
 int sm_count(int* n)
@@ -72,3 +84,16 @@ int sm_count(int* n)
 
 }  // namespace product
 }  // namespace cast
+
+extern "C" int cast_product_failures(unsigned long long* count_out, int action)
+{
+    if (action < 0 || action > 2) return CAST_ERR_HYPER;
+    unsigned long long* w;
+    const int rc = cast::product::the_word(&w);
+    if (rc != CAST_OK) return rc;
+    volatile unsigned long long* v = w;
+    if (count_out) *count_out = *v;
+    if (action == 1) *v = *v + 1;
+    else if (action == 2) *v = 0;
+    return CAST_OK;
+}

@@ -73,7 +73,7 @@ def run(h, w, y, s, want_h=True, want_w=True, piece=0):
                                    ws, need, torch.cuda.current_stream()))
     torch.cuda.synchronize()
     assert gl.intact() and gh.intact() and gw.intact() and bool((ws[need:] == 255).all())
-    assert cast.cast_bulk_timeout_count() == (0, 0)
+    assert cast.cast_product_failures() == (0, 0)
     return gl.view, gh.view.reshape(tokens, dim), gw.view.reshape(vocab, dim)
 
 
@@ -287,3 +287,19 @@ def test_refusals():
         ops.linear_ce(h, w, y[:5])
     with pytest.raises(cast.CastError):
         ops.linear_ce(h[:, :60].contiguous(), w[:, :60].contiguous(), y)
+
+
+def test_a_counted_failure_stops_further_calls():
+    """What a product that gives up a wait does to the calls after it, with the count set on the host."""
+    h, w, y = draw(10, 50, 64, 33)
+    want = ops.linear_ce(h, w, y)
+    assert cast.cast_product_failures(1) == (0, 0)
+    try:
+        with pytest.raises(cast.CastError) as e:
+            ops.linear_ce(h, w, y)
+        assert e.value.status == B.CAST_ERR_STAGING
+        with pytest.raises(cast.CastError):
+            ops.orthogonalize([torch.ones((8, 8), device=DEV)])
+    finally:
+        assert cast.cast_product_failures(2) == (0, 1)
+    assert all(torch.equal(a, b) for a, b in zip(want, ops.linear_ce(h, w, y)))

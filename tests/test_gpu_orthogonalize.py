@@ -67,7 +67,7 @@ def test_shapes(rows, cols, dtype):
                                        torch.cuda.current_stream()))
     torch.cuda.synchronize()
     assert all(g.intact() for g in guards) and bool((ws[need:] == 255).all())
-    assert cast.cast_bulk_timeout_count() == (0, 0)
+    assert cast.cast_product_failures() == (0, 0)
     assert all(torch.equal(a, b) for a, b in zip(u, before))
     for x, g in zip(u, guards):
         assert distance(g.view.reshape(rows, cols), exact(x, QUINTIC, 5, scale=1.5)) <= tolerance(5, rows * cols)

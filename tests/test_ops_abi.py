@@ -100,6 +100,11 @@ def test_orthogonalize(over, status):
     assert cast.cast_orthogonalize(**a) == status
 
 
+def test_product_failures():
+    assert cast.cast_product_failures(3)[0] == B.CAST_ERR_HYPER
+    assert cast.cast_product_failures(-1)[0] == B.CAST_ERR_HYPER
+
+
 def test_torch_level_calls_refuse_host_tensors():
     x = torch.zeros((4, 8), dtype=torch.bfloat16)
     ids = torch.zeros(4, dtype=torch.int32)
