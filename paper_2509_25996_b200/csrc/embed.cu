@@ -17,6 +17,7 @@
 //   * up to kFew tokens are not sorted: the first token of an id looks for the others among the ids.
 //   * rows without a token become zeros in further CTAs of the kernel that sums: each looks up which of its kZeroRows rows
 //     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -394,8 +395,16 @@ join_pieces_kernel(const __grid_constant__ ScatterArgs a)
             const float* p = a.partial + (int64_t)piece * 2 * a.dim + col;
             if (own == 0) acc.add_partial(p + a.dim);
             p += (int64_t)(from + 1) * 2 * a.dim;
-#pragma unroll 8
-            for (int32_t i = from; i < to; ++i, p += 2 * a.dim) acc.add_partial(p);
+            for (int32_t i = from; i < to; i += 8, p += 16 * a.dim) {      // eight rows at a time, the last ones too
+                Cols<VEC> row[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    row[j].zero();
+                    if (i + j < to) row[j].add_partial(p + (int64_t)j * 2 * a.dim);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc.add(row[j]);
+            }
         }
         __syncthreads();          // the sums of the columns before these have been taken
         if (own > 0) part[own - 1][lane] = acc;
@@ -411,44 +420,68 @@ join_pieces_kernel(const __grid_constant__ ScatterArgs a)
     }
 }
 
-// Few tokens need no order: the group of threads that holds an id's first token looks through all ids for the others.
+// Few tokens need no order: the threads that hold an id's first token list the others by warp votes over all ids.
 constexpr int kFew = 256;
 
 template <int VEC, bool COEF>
 __global__ void __launch_bounds__(kScatterThreads)
 few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      // a.ids: as the caller gave them
 {
+    constexpr int kWarps = kScatterThreads / 32;
     __shared__ uint32_t ids[kFew];
+    __shared__ uint8_t same[kWarps][kFew];
     __shared__ uint32_t held;
     chain_next();
     if (threadIdx.x == 0) held = 0;
-    if ((int)threadIdx.x < a.tokens) ids[threadIdx.x] = (uint32_t)__ldg(a.ids + threadIdx.x);
+    ids[threadIdx.x] = (int)threadIdx.x < a.tokens ? (uint32_t)__ldg(a.ids + threadIdx.x) : 0xFFFFFFFFu;
     __syncthreads();
     if (blockIdx.x >= a.own) {           // a block of rows: zeros where no token is (only in a call of its own)
         if (blockIdx.y != 0) return;
         const int64_t row0 = (int64_t)(blockIdx.x - a.own) * kZeroRows;
-        if ((int)threadIdx.x < a.tokens) {
-            const int64_t id = (int64_t)ids[threadIdx.x] - row0;
-            if (ids[threadIdx.x] < vocab && id >= 0 && id < kZeroRows) atomicOr(&held, 1u << (int)id);
-        }
+        const int64_t id = (int64_t)ids[threadIdx.x] - row0;
+        if (ids[threadIdx.x] < vocab && id >= 0 && id < kZeroRows) atomicOr(&held, 1u << (int)id);
         __syncthreads();
         zero_rows<VEC>(a, row0, held);
         return;
     }
-    const int32_t t = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
-    const int32_t col = column_of<VEC>(a);
+    const int32_t t = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;      // one token per warp
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const uint32_t id = t < a.tokens ? ids[t] : 0xFFFFFFFFu;
-    bool first = id < vocab && col < a.dim;
-    for (int32_t i = 0; i < t; ++i) first &= ids[i] != id;
+    if (id >= vocab) return;
+    int count = 0;
+#pragma unroll
+    for (int k = 0; k < kFew / 32; ++k) {
+        const bool mine = ids[32 * k + lane] == id;
+        const uint32_t m = __ballot_sync(0xFFFFFFFFu, mine);
+        if (mine) same[warp][count + __popc(m & ((1u << lane) - 1u))] = (uint8_t)(32 * k + lane);
+        count += __popc(m);
+    }
+    __syncwarp();
+    const bool first = same[warp][0] == t;
+    const int32_t col = column_of<VEC>(a);
+    if (!first || col >= a.dim) return;
     chain_wait();
-    if (!first) return;
     uint16_t* to = a.dest + (int64_t)id * a.dim + col;
     typename Cols<VEC>::Raw old = {};
     if (a.accumulate) old = Cols<VEC>::load_own(to);
     Cols<VEC> acc;
     acc.zero();
-    for (int32_t i = t; i < a.tokens; ++i)
-        if (ids[i] == id) acc.add(Cols<VEC>::load(a.src + (int64_t)i * a.dim + col), COEF ? __ldg(a.coef + i) : 1.0f);
+    for (int32_t i0 = 0; i0 < count; i0 += 4) {
+        typename Cols<VEC>::Raw x[4];
+        float c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = 1.0f;
+            if (i0 + i < count) {
+                const int32_t token = same[warp][i0 + i];
+                x[i] = Cols<VEC>::load(a.src + (int64_t)token * a.dim + col);
+                if constexpr (COEF) c[i] = __ldg(a.coef + token);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i0 + i < count) acc.add(x[i], c[i]);
+    }
     acc.store(to, a.scale, a.accumulate, old);
 }
 
@@ -463,7 +496,7 @@ int launch_scatter(ScatterArgs a, const SortedTokens& sorted, cudaStream_t strea
     const int rc = a.accumulate ? launch_chained(false, piece_sums_kernel<VEC, COEF, true>, grid, kScatterThreads, 0, stream, 1, a)
                                 : launch_chained(false, piece_sums_kernel<VEC, COEF, false>, grid, kScatterThreads, 0, stream, 1, a);
     if (rc != CAST_OK || a.pieces < 2) return rc;
-    return launch_chained(false, join_pieces_kernel<VEC>, dim3((unsigned)(a.pieces - 1), units > kJoinLanes ? 2u : 1u), kJoinThreads, 0, stream, 1, a);
+    return launch_chained(false, join_pieces_kernel<VEC>, dim3((unsigned)(a.pieces - 1), (unsigned)std::min<int64_t>((units + kJoinLanes - 1) / kJoinLanes, 4)), kJoinThreads, 0, stream, 1, a);
 }
 
 int64_t sort_array_bytes(int64_t tokens) { return (int64_t)align256(4ull * (uint64_t)tokens); }

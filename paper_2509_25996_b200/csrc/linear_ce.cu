@@ -31,6 +31,9 @@ using namespace product;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMostSum = 2.35e17f;        // e^40
+// The tensor cores truncate where they add a k-step to an accumulator, which shrinks a logit by 1.0e-9 of itself per k on the mean
+// (measured at k = 768, 5120 and 16384: 6.8e-7, 5.0e-6, 1.6e-5); the factor on the accumulators takes the mean out again.
+constexpr double kShrinkPerK = 1.0e-9;
 
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
@@ -64,11 +67,20 @@ target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restr
     if ((unsigned)label < (unsigned)vocab) {
         const uint4* h = reinterpret_cast<const uint4*>(hidden + t * dim);
         const uint4* w = reinterpret_cast<const uint4*>(weight + (int64_t)label * dim);
-#pragma unroll 4
-        for (int i = lane; i < dim / 8; i += 32) {
-            const uint4 a = __ldg(h + i), b = __ldg(w + i);
-            sum += lo16(a.x) * lo16(b.x) + hi16(a.x) * hi16(b.x) + lo16(a.y) * lo16(b.y) + hi16(a.y) * hi16(b.y) +
-                   lo16(a.z) * lo16(b.z) + hi16(a.z) * hi16(b.z) + lo16(a.w) * lo16(b.w) + hi16(a.w) * hi16(b.w);
+        // four vectors of each row at a time, the last ones too: a loop's remainder would wait for one load after the other
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        for (int i0 = lane; i0 < dim / 8; i0 += 128) {
+            uint4 a[4], b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool in = i0 + 32 * j < dim / 8;
+                a[j] = in ? __ldg(h + i0 + 32 * j) : zero;
+                b[j] = in ? __ldg(w + i0 + 32 * j) : zero;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                sum += lo16(a[j].x) * lo16(b[j].x) + hi16(a[j].x) * hi16(b[j].x) + lo16(a[j].y) * lo16(b[j].y) + hi16(a[j].y) * hi16(b[j].y) +
+                       lo16(a[j].z) * lo16(b[j].z) + hi16(a[j].z) * hi16(b[j].z) + lo16(a[j].w) * lo16(b[j].w) + hi16(a[j].w) * hi16(b[j].w);
         }
     }
 #pragma unroll
@@ -85,6 +97,7 @@ struct ExpEpi : StoringEpi {
     const int32_t* labels;
     float* sums;                 // [n_tiles][tokens]; negative: relative to `tops`
     float* tops;                 // [n_tiles][tokens], base 2
+    float to_base2;              // log2(e), and the factor above
     int write_e;
 
     // One pass over the accumulator row relative to ref2: returns the sum; writes E.
@@ -105,7 +118,7 @@ struct ExpEpi : StoringEpi {
                 const int n1 = n + 32 * h;
                 const bool special = !active || (unsigned)(label - n1) < 32u || n1 + 32 > s.n;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = ex2(fmaf(v[i], kLog2e, -ref2));
+                for (int i = 0; i < 32; ++i) v[i] = ex2(fmaf(v[i], to_base2, -ref2));
                 if (__any_sync(0xFFFFFFFFu, special)) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
@@ -152,7 +165,7 @@ struct ExpEpi : StoringEpi {
                 for (int i = 0; i < 32; ++i)
                     if (e.col0 + c + i != label && e.col0 + c + i < s.n) top = fmaxf(top, v[i]);
             }
-            const float top2 = top * kLog2e;
+            const float top2 = top * to_base2;
             if (e.lane == 0) store_wait_all();          // the first pass has been written before the second overwrites it
             __syncwarp();
             const float again = pass<BN>(s, e, over ? top2 : ref2, label, active);
@@ -217,11 +230,15 @@ finish_kernel(const __grid_constant__ FinishArgs p)
     bool over = false;
     float sum = 0.0f;
     if (active) {
-#pragma unroll 4
-        for (int i = lane; i < p.n_tiles; i += 32) {
-            const float v = p.sums[(int64_t)i * p.tokens + t];
-            over |= !(v >= 0.0f);
-            sum += v;
+        for (int i0 = lane; i0 < p.n_tiles; i0 += 256) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < p.n_tiles ? p.sums[(int64_t)(i0 + 32 * j) * p.tokens + t] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                over |= !(v[j] >= 0.0f);
+                sum += v[j];
+            }
         }
     }
     if (__syncthreads_or(over)) {           // rare: bring the tiles of such rows to one reference
@@ -279,8 +296,14 @@ finish_kernel(const __grid_constant__ FinishArgs p)
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
             if (wl + 32 * i < p.dim / 8) o[wl + 32 * i] = scaled(ahead[i]);
-#pragma unroll 4
-        for (int i = wl + 32 * kAhead; i < p.dim / 8; i += 32) o[i] = scaled(__ldg(h + i));
+        for (int i0 = wl + 32 * kAhead; i0 < p.dim / 8; i0 += 32 * kAhead) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (i0 + 32 * i < p.dim / 8) ahead[i] = __ldg(h + i0 + 32 * i);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (i0 + 32 * i < p.dim / 8) o[i0 + 32 * i] = scaled(ahead[i]);
+        }
     }
     if (p.e && sh_over[warp]) {
         uint16_t* row = p.e + (t0 + warp) * p.e_ld;
@@ -378,13 +401,15 @@ struct HiddenGradEpi : StoringEpi {
 };
 
 // Adds the splits' sums in order and finishes dH.  One thread per 8 columns.
-__global__ void __launch_bounds__(256)
+constexpr int kJoinThreads = 64;
+
+__global__ void __launch_bounds__(kJoinThreads)
 join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restrict__ a, const float* __restrict__ b,
                         const int32_t* __restrict__ labels, const uint16_t* __restrict__ weight, uint16_t* __restrict__ out,
                         int64_t tokens, int dim, int vocab, int splits)
 {
     chain_next();
-    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t u = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
     const int per = dim / 8;
     if (u >= tokens * per) return;
     const int64_t t = u / per;
@@ -399,10 +424,19 @@ join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restri
         const float4* p = reinterpret_cast<const float4*>(partial + t * dim + c);
         const int64_t step = tokens * dim / 4;
         const float fa = a[t], fb = b[t];
-#pragma unroll 8
-        for (int s = 0; s < splits; ++s, p += step) {
-            const float4 x = __ldg(p), y = __ldg(p + 1);
-            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+        for (int s0 = 0; s0 < splits; s0 += 8, p += 8 * step) {
+            float4 x[8], y[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const bool in = s0 + s < splits;
+                x[s] = in ? __ldg(p + s * step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                y[s] = in ? __ldg(p + s * step + 1) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                v[0] += x[s].x; v[1] += x[s].y; v[2] += x[s].z; v[3] += x[s].w;
+                v[4] += y[s].x; v[5] += y[s].y; v[6] += y[s].z; v[7] += y[s].w;
+            }
         }
         r = make_uint4(pack2(fa * v[0] - fb * lo16(w.x), fa * v[1] - fb * hi16(w.x)), pack2(fa * v[2] - fb * lo16(w.y), fa * v[3] - fb * hi16(w.y)),
                        pack2(fa * v[4] - fb * lo16(w.z), fa * v[5] - fb * hi16(w.z)), pack2(fa * v[6] - fb * lo16(w.w), fa * v[7] - fb * hi16(w.w)));
@@ -577,6 +611,7 @@ int exp_product(const Call& c, int64_t t0, int64_t n)
     epi.labels = c.labels + t0;
     epi.sums = reinterpret_cast<float*>(c.ws + l.sums);
     epi.tops = reinterpret_cast<float*>(c.ws + l.tops);
+    epi.to_base2 = (float)(1.4426950408889634 * (1.0 + kShrinkPerK * (double)c.dim));
     epi.write_e = grads;
     epi.map_e = ma;
     if (grads && (rc = make_map(&epi.map_e, c.ws + l.e, 2, c.vocab, n, 1, l.e_ld, 0, 64, 32, true)) != CAST_OK) return rc;
@@ -608,7 +643,7 @@ int hidden_product(const Call& c, int64_t t0, int64_t n)
     if ((rc = launch<CG, BN, false, true>(ma, mb, s, epi, c.stream)) != CAST_OK) return rc;
     if (epi.partial) {
         const int64_t units = n * (c.dim / 8);
-        return launch_chained(false, join_hidden_grad_kernel, dim3((unsigned)((units + 255) / 256)), 256, 0, c.stream, 1, partial, epi.a, epi.b,
+        return launch_chained(false, join_hidden_grad_kernel, dim3((unsigned)((units + kJoinThreads - 1) / kJoinThreads)), kJoinThreads, 0, c.stream, 1, partial, epi.a, epi.b,
                               epi.labels, c.weight, c.grad_hidden + t0 * c.dim, n, (int)c.dim, (int)c.vocab, s.splits);
     }
     return CAST_OK;
