@@ -13,11 +13,11 @@
 //     whose tokens all lie in its piece.  A table row whose tokens go on in the next piece leaves fp32 partial rows (the
 //     part that enters a piece and the part that leaves it), which a second kernel adds in order.  Every token row is read
 //     once, and a CTA's work does not depend on how often an id occurs; only the adding of partial rows of a frequent
-//     id is a chain, of tokens / kPiece rows.
+//     id is a chain, of tokens / kPiece rows.  (Letting a piece finish the row that it leaves, where that ends in the next
+//     piece, saves most of the partial rows but makes its loads a longer chain: 80 + 15 instead of 66 + 20 us.)
 //   * up to kFew tokens are not sorted: the first token of an id looks for the others among the ids.
 //   * rows without a token become zeros in further CTAs of the kernel that sums: each looks up which of its kZeroRows rows
 //     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.
-#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -144,7 +144,7 @@ rank_runs_kernel(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_i
     rank_keys(ids, sorted_ids, order, tokens, vocab, blockIdx.x);
 }
 
-constexpr int kMergeThreads = 256;
+constexpr int kMergeThreads = 128;
 
 // Merges groups of kWays runs of `run` keys.  The searches of a key advance together and without branches: kWays independent
 // loads per halving, from shared memory where a group fits (runs of kRun keys: 64 KB), from L2 where it does not.
@@ -179,6 +179,7 @@ merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict_
 #pragma unroll
         for (int j = 0; j < kWays; ++j) {
             const int64_t before = (int64_t)j * run;                 // keys of the group ahead of run j
+            if (before >= left) break;                               // no such run (the same for the whole CTA)
             const int32_t at = pos[j] + half;
             const bool there = at <= run && before + at <= left;
             const uint32_t limit = j == own ? 0u : k + (j < own ? 1u : 0u);
@@ -345,78 +346,98 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
     }
 }
 
-// End of the positions after p that hold the id at p.  All lanes of a warp ask for the same p: 32 positions per load.
-__device__ __forceinline__ int32_t end_of(const int32_t* ids, int32_t n, int32_t p, int32_t id)
+// Partial rows 1 + from .. to of a piece that a row leaves (`p`: of the piece), eight at a time, the last ones too.
+template <int VEC>
+__device__ __forceinline__ void add_partials(Cols<VEC>& acc, const float* p, int64_t stride, int32_t from, int32_t to)
 {
-    const int lane = (int)threadIdx.x & 31;
-    int32_t lo = p + 1, step = 1;                          // [p, lo) hold it
-    for (;;) {                                             // strides of 1, 32, 1024, ... positions until one ends it
-        const int64_t at = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
-        const int same = __popc(__ballot_sync(0xFFFFFFFFu, at < n && __ldg(ids + at) == id));
-        lo += same * step;
-        if (same < 32) break;
-        step *= 32;
+    for (int32_t i = from; i < to; i += 8) {
+        Cols<VEC> row[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            row[j].zero();
+            if (i + j < to) row[j].add_partial(p + (int64_t)(i + j + 1) * stride);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc.add(row[j]);
     }
-    while (step > 1) {                                     // then 32 times finer inside the stride that did
-        step /= 32;
-        const int64_t at = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
-        lo += __popc(__ballot_sync(0xFFFFFFFFu, at < n && __ldg(ids + at) == id)) * step;
-    }
-    return lo;
 }
 
-// The table rows that leave a piece they began in: what left it, then what entered the pieces after it.  One piece per CTA (most
-// find nothing to do); a frequent id's partial rows are cut into kJoinParts runs that are added side by side.
-constexpr int kJoinThreads = 512;
-constexpr int kJoinLanes = 128;
-constexpr int kJoinParts = kJoinThreads / kJoinLanes;
+// The table rows that leave a piece they began in: what left it, then what entered the pieces after it.  One warp per piece and block
+// of 32 VEC columns; most find nothing to do, and most that do add a few rows.  A frequent id's partial rows are cut into a
+// run per warp of the CTA.
+constexpr int kJoinWarps = kScatterThreads / 32;
 
 template <int VEC>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kScatterThreads)
 join_pieces_kernel(const __grid_constant__ ScatterArgs a)
 {
-    __shared__ Cols<VEC> part[kJoinParts - 1][kJoinLanes];
+    __shared__ int32_t found_id[kJoinWarps], found_count[kJoinWarps];
+    __shared__ Cols<VEC> part[kJoinWarps][32];
     chain_next();
     chain_wait();
-    const int32_t piece = (int32_t)blockIdx.x;             // never the last one: nothing leaves it
-    const int32_t p0 = piece * kPiece, last = p0 + kPiece - 1;
-    const int32_t id = __ldg(a.ids + last), after = __ldg(a.ids + last + 1), before = p0 > 0 ? __ldg(a.ids + p0 - 1) : -1;
-    if ((uint32_t)id == kNoId || after != id || before == id) return;
-    const int32_t e = end_of(a.ids, a.tokens, last, id);
-    const int lane = (int)threadIdx.x % kJoinLanes, own = (int)threadIdx.x / kJoinLanes;
-    const int32_t count = (e - 1) / kPiece - piece;        // pieces that it enters
-    const int32_t each = (count + kJoinParts - 1) / kJoinParts, from = own * each, to = min(count, from + each);
-    for (int64_t col0 = (int64_t)blockIdx.y * kJoinLanes * VEC; col0 < a.dim; col0 += (int64_t)gridDim.y * kJoinLanes * VEC) {
-        const int64_t col = col0 + (int64_t)lane * VEC;
-        const bool in = col < a.dim;
+    const int lane = (int)threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
+    const int32_t first = (int32_t)blockIdx.x * kJoinWarps, piece = first + warp;
+    const int64_t col = ((int64_t)blockIdx.y * 32 + lane) * VEC, stride = 2 * a.dim;
+    const bool in = col < a.dim;
+    int32_t id = -1, count = 0;
+    if (piece + 1 < a.pieces) {                            // nothing leaves the last piece
+        const int32_t p0 = piece * kPiece, next = p0 + kPiece;
+        id = __ldg(a.ids + next - 1);
+        const int32_t after = __ldg(a.ids + next), before = p0 > 0 ? __ldg(a.ids + p0 - 1) : -1;
+        // how many of the 128 pieces after this one begin with the id, asked for in the same breath
+        int same[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t at = (int64_t)next + (int64_t)(32 * j + lane) * kPiece;
+            same[j] = at < a.tokens ? __ldg(a.ids + at) : -1;
+        }
+        if ((uint32_t)id == kNoId || after != id || before == id) id = -1;
+        else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) count += __popc(__ballot_sync(0xFFFFFFFFu, same[j] == id));
+            for (int32_t base = 128; count == base; base += 32) {
+                const int64_t at = (int64_t)next + (int64_t)(base + lane) * kPiece;
+                count += __popc(__ballot_sync(0xFFFFFFFFu, at < a.tokens && __ldg(a.ids + at) == id));
+            }
+        }
+    }
+    const bool together = id >= 0 && count > 8;
+    if (lane == 0) {
+        found_id[warp] = together ? id : -1;
+        found_count[warp] = count;
+    }
+    if (id >= 0 && !together && in) {
+        const float* p = a.partial + (int64_t)piece * stride + col;
+        uint16_t* dest = a.dest + (int64_t)id * a.dim + col;
+        typename Cols<VEC>::Raw old = {};
+        if (a.accumulate) old = Cols<VEC>::load_own(dest);
+        Cols<VEC> acc;
+        acc.zero();
+        acc.add_partial(p + a.dim);
+        add_partials<VEC>(acc, p, stride, 0, count);
+        acc.store(dest, a.scale, a.accumulate, old);
+    }
+    __syncthreads();
+    for (int f = 0; f < kJoinWarps; ++f) {
+        if (found_id[f] < 0) continue;
+        const int32_t n = found_count[f], each = (n + kJoinWarps - 1) / kJoinWarps, from = warp * each;
+        const float* p = a.partial + (int64_t)(first + f) * stride + col;
         Cols<VEC> acc;
         acc.zero();
         if (in) {
-            const float* p = a.partial + (int64_t)piece * 2 * a.dim + col;
-            if (own == 0) acc.add_partial(p + a.dim);
-            p += (int64_t)(from + 1) * 2 * a.dim;
-            for (int32_t i = from; i < to; i += 8, p += 16 * a.dim) {      // eight rows at a time, the last ones too
-                Cols<VEC> row[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    row[j].zero();
-                    if (i + j < to) row[j].add_partial(p + (int64_t)j * 2 * a.dim);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc.add(row[j]);
-            }
+            if (warp == 0) acc.add_partial(p + a.dim);
+            add_partials<VEC>(acc, p, stride, from, min(n, from + each));
         }
-        __syncthreads();          // the sums of the columns before these have been taken
-        if (own > 0) part[own - 1][lane] = acc;
+        part[warp][lane] = acc;
         __syncthreads();
-        if (own == 0 && in) {
-#pragma unroll
-            for (int i = 0; i < kJoinParts - 1; ++i) acc.add(part[i][lane]);
-            uint16_t* dest = a.dest + (int64_t)id * a.dim + col;
+        if (warp == 0 && in) {
+            for (int i = 1; i < kJoinWarps; ++i) acc.add(part[i][lane]);
+            uint16_t* dest = a.dest + (int64_t)found_id[f] * a.dim + col;
             typename Cols<VEC>::Raw old = {};
             if (a.accumulate) old = Cols<VEC>::load_own(dest);
             acc.store(dest, a.scale, a.accumulate, old);
         }
+        __syncthreads();
     }
 }
 
@@ -496,7 +517,8 @@ int launch_scatter(ScatterArgs a, const SortedTokens& sorted, cudaStream_t strea
     const int rc = a.accumulate ? launch_chained(false, piece_sums_kernel<VEC, COEF, true>, grid, kScatterThreads, 0, stream, 1, a)
                                 : launch_chained(false, piece_sums_kernel<VEC, COEF, false>, grid, kScatterThreads, 0, stream, 1, a);
     if (rc != CAST_OK || a.pieces < 2) return rc;
-    return launch_chained(false, join_pieces_kernel<VEC>, dim3((unsigned)(a.pieces - 1), (unsigned)std::min<int64_t>((units + kJoinLanes - 1) / kJoinLanes, 4)), kJoinThreads, 0, stream, 1, a);
+    return launch_chained(false, join_pieces_kernel<VEC>, dim3((unsigned)((a.pieces - 1 + kJoinWarps - 1) / kJoinWarps), (unsigned)((units + 31) / 32)),
+                          kScatterThreads, 0, stream, 1, a);
 }
 
 int64_t sort_array_bytes(int64_t tokens) { return (int64_t)align256(4ull * (uint64_t)tokens); }
@@ -586,7 +608,7 @@ using namespace cast;
 
 namespace {
 
-constexpr int64_t kMostColumns = 1 << 23;      // blocks of 256 accesses of one column each: fewer than 2^16
+constexpr int64_t kMostColumns = 1 << 20;      // blocks of 32 accesses of one column each: fewer than 2^16
 
 int check_rows(const void* a, const void* ids, const void* b, int64_t tokens, int64_t vocab, int64_t dim, float scale)
 {

@@ -520,7 +520,8 @@ int64_t tile_cols(int64_t tokens) { return paired(tokens) ? 256 : 128; }
 
 // Splits of the vocabulary for dH: few tokens give few tiles, and each has the whole vocabulary to sum.  The time of
 // `splits` is taken as rounds of tiles x (blocks + 8 for filling and draining the pipeline), in blocks (~0.3 us for a pair),
-// plus writing and reading the partial sums at ~5 TB/s.
+// plus writing and reading the partial sums at ~5 TB/s.  A split has to save a twentieth: SMs that idle in a last round leave
+// their power to the others (4096 tokens x 32000 x 4096, which would take two splits: 2.54-2.58 ms with them, 2.55-2.56 without).
 int hidden_splits(int64_t tokens, int64_t vocab, int64_t dim, int sms)
 {
     const bool two = paired(tokens);
@@ -531,7 +532,7 @@ int hidden_splits(int64_t tokens, int64_t vocab, int64_t dim, int sms)
     for (int s = 1; s <= 64 && s <= blocks; ++s) {
         const int64_t rounds = (tiles * s + units - 1) / units;
         const int64_t cost = rounds * ((blocks + s - 1) / s + 8) + (s > 1 ? 8 + s * tokens * dim * 8 / (two ? 1500000 : 1000000) : 0);
-        if (cost < best_cost) { best_cost = cost; best = s; }
+        if (cost + cost / 20 < best_cost) { best_cost = cost; best = s; }
     }
     return best;
 }
@@ -728,6 +729,8 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
     if ((rc = launch_chained(true, target_logit_kernel, dim3(own + (grad_weight ? (unsigned)rank_blocks(tokens) : 0u)), kRankThreads, 0, st, 1, hidden,
                              weight, labels, refs, tokens, (int)vocab, (int)dim, own, sorted_ids, order)) != CAST_OK)
         return rc;
+    SortedTokens sorted;      // the merges now, while the ids are in L2, not after the products have swept it
+    if (grad_weight && (rc = sort_tokens(true, labels, tokens, vocab, ws + l.scatter, &sorted, st)) != CAST_OK) return rc;
     for (int64_t i = 0; i < l.pieces; ++i) {
         const int64_t t0 = i * l.piece, n = tokens - t0 < l.piece ? tokens - t0 : l.piece;
         rc = paired(n) ? exp_product<2, 256>(c, t0, n) : exp_product<1, 128>(c, t0, n);
@@ -759,8 +762,6 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
         if (grad_weight && (rc = weight_product(c, n, i == 0, i + 1 == l.pieces)) != CAST_OK) return rc;
     }
     if (grad_weight) {
-        SortedTokens sorted;
-        if ((rc = sort_tokens(true, labels, tokens, vocab, ws + l.scatter, &sorted, st)) != CAST_OK) return rc;
         // b holds s S / (1 + S): the label's term of dW is -b H
         if ((rc = scatter_rows(sorted, hidden, b, -1.0f, grad_weight, vocab, dim, true, st)) != CAST_OK) return rc;
     }
