@@ -14,7 +14,8 @@
 // multiplies small ones by a = 3.4, five steps by 500, which swamps an update of low rank (measured on 768 x 768 of rank 8 over
 // 2 % noise: 2.8e-2 from the exact result, where rounding the result to bf16 is 1.7e-3).  So while the steps still to come
 // amplify by more than kAmplify, X is held as hi + lo, two fp16 words scaled by 2^12 (22 bits): the products read hi, the
-// epilogue adds a lo.  With five steps X_0, X_1 and X_2 have a lo: 2.4e-3 on that update.
+// epilogue adds a lo.  With five steps X_0 (of an fp32 update; a bf16 one is exact in hi), X_1 and X_2 have a lo: 2.4e-3 on that
+// update.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -32,7 +33,7 @@ using namespace product;
 constexpr float kX = 4096.0f;               // X is stored times this
 constexpr int kGroup = 64;                  // matrices per launch at most
 constexpr int64_t kGroupElems = 64 << 20;   // ... and elements, which bounds the workspace
-constexpr int kNormBlocks = 128;
+constexpr int kNormBlocks = 1024;           // per matrix at most
 constexpr float kAmplify = 12.0f;           // X keeps its lo while later steps multiply small directions by more
 
 struct PtrTable { const void* p[kGroup]; };
@@ -85,6 +86,14 @@ __device__ __forceinline__ double block_sum(double x)
     return x;
 }
 
+// Sum of squares of a matrix from its CTAs' parts, by every CTA that needs it, in the same order.
+__device__ __forceinline__ double total_of(const double* part, int parts)
+{
+    double sum = 0.0;
+    for (int i = (int)threadIdx.x; i < parts; i += 256) sum += part[i];
+    return block_sum(sum);
+}
+
 // Squares in fp64: gradients are small enough for their squares to leave the range of fp32.
 template <bool BF16, int VEC>
 __global__ void __launch_bounds__(256)
@@ -104,16 +113,23 @@ square_sum_kernel(const __grid_constant__ PtrTable updates, double* __restrict__
     if (threadIdx.x == 0) partial[(int64_t)blockIdx.y * kNormBlocks + blockIdx.x] = sum;
 }
 
+// X_0, stored times kX.  A bf16 update keeps its significands: it is scaled by a power of two, hi is exact, there is no lo, and
+// the rest of the scale, gain[matrix] in [1, 2), is applied by the first step's epilogues.
 template <bool BF16, int VEC>
 __global__ void __launch_bounds__(256)
 first_x_kernel(const __grid_constant__ PtrTable updates, const double* __restrict__ partial, int parts, uint16_t* __restrict__ hi,
-               uint16_t* __restrict__ lo, int64_t units, uint32_t units_per_row, int64_t ld, int64_t stride, double eps)
+               uint16_t* __restrict__ lo, float* __restrict__ gain, int64_t units, uint32_t units_per_row, int64_t ld, int64_t stride, double eps)
 {
     chain_next();
     chain_wait();
-    const double sum = block_sum((int)threadIdx.x < parts ? partial[(int64_t)blockIdx.y * kNormBlocks + threadIdx.x] : 0.0);
-    const double norm = sqrt(sum) + eps;
-    const double f = norm > 0.0 ? (double)kX / norm : 0.0;      // not in fp32: 1 / norm of a tiny update leaves its range
+    const double norm = sqrt(total_of(partial + (int64_t)blockIdx.y * kNormBlocks, parts)) + eps;
+    double f = norm > 0.0 ? (double)kX / norm : 0.0;      // not in fp32: 1 / norm of a tiny update leaves its range
+    if constexpr (BF16) {
+        int e = 0;
+        const double g = f > 0.0 ? 2.0 * frexp(f, &e) : 1.0;
+        f = f > 0.0 ? ldexp(1.0, e - 1) : 0.0;
+        if (blockIdx.x == 0 && threadIdx.x == 0) gain[blockIdx.y] = (float)g;
+    }
     const void* u = updates.p[blockIdx.y];
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
         float v[VEC];
@@ -128,23 +144,16 @@ first_x_kernel(const __grid_constant__ PtrTable updates, const double* __restric
         }
         if constexpr (VEC == 8) {
             *reinterpret_cast<uint4*>(hi + at) = make_uint4(pack_f16(x[0], x[1]), pack_f16(x[2], x[3]), pack_f16(x[4], x[5]), pack_f16(x[6], x[7]));
-            *reinterpret_cast<uint4*>(lo + at) = make_uint4(pack_f16(rest[0], rest[1]), pack_f16(rest[2], rest[3]), pack_f16(rest[4], rest[5]), pack_f16(rest[6], rest[7]));
+            if constexpr (!BF16)
+                *reinterpret_cast<uint4*>(lo + at) = make_uint4(pack_f16(rest[0], rest[1]), pack_f16(rest[2], rest[3]), pack_f16(rest[4], rest[5]), pack_f16(rest[6], rest[7]));
         } else {
             hi[at] = (uint16_t)pack_f16(x[0], 0.0f);
-            lo[at] = (uint16_t)pack_f16(rest[0], 0.0f);
+            if constexpr (!BF16) lo[at] = (uint16_t)pack_f16(rest[0], 0.0f);
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------------ epilogues
-
-__device__ __forceinline__ void write_f16(uint32_t slot, int lane, int half, const float (&v)[32])
-{
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        slot_write(slot, lane, 4 * half + q, pack_f16(v[8 * q], v[8 * q + 1]), pack_f16(v[8 * q + 2], v[8 * q + 3]),
-                   pack_f16(v[8 * q + 4], v[8 * q + 5]), pack_f16(v[8 * q + 6], v[8 * q + 7]));
-}
 
 // A symmetric result, stored at (row, col) and, off the diagonal, at (col, row): scale acc, or with POLY
 // scale acc + add aux + diag I.
@@ -158,6 +167,7 @@ struct SymEpi {
     CUtensorMap map_out;         // boxes of 32 rows x 64 columns, swizzled
     CUtensorMap map_mirror;      // the same array, boxes of 64 rows x 32 columns, not swizzled
     CUtensorMap map_aux;         // fp16, read like map_out
+    const float* gain;           // per matrix, its square multiplies the result; nullptr: 1
     float scale, add, diag;
 
     __device__ __forceinline__ void prefetch() const
@@ -179,6 +189,7 @@ struct SymEpi {
     __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
     {
         const bool mirror = e.col0 + BN <= e.tile.tm * BM;
+        const float g = gain ? __ldg(gain + e.tile.batch) : 1.0f, scale_all = scale * g * g;
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
@@ -195,7 +206,7 @@ struct SymEpi {
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] *= scale;
+                for (int i = 0; i < 32; ++i) v[i] *= scale_all;
                 if constexpr (POLY) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -244,26 +255,24 @@ struct SymEpi {
     }
 };
 
-// X' = acc (+ a lo): as hi + lo, or hi alone.
-template <bool LO_IN>
+// X' = gain acc (+ a lo): as hi + lo, or hi alone.
+template <bool LO_IN, bool LO_OUT>
 struct StepEpi {
     static constexpr bool kSym = false;
     static constexpr bool kInputsOnly = false;
-    // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise two slots for hi in turn
+    // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise a slot for each, or two for hi in turn
     static constexpr int kStaging = (LO_IN ? kRing + 1 : kTurns) * kSlotBytes;
     using State = AuxRing;
     CUtensorMap map_hi, map_lo;      // X'
     CUtensorMap map_lo_in;           // X
+    const float* gain;               // per matrix; nullptr: 1 (only without LO_IN)
     float a;
-    int lo_out;                      // only with LO_IN: lo is dropped at some step and does not come back
 
     __device__ __forceinline__ void prefetch() const
     {
         prefetch_map(&map_hi);
-        if constexpr (LO_IN) {
-            prefetch_map(&map_lo_in);
-            if (lo_out) prefetch_map(&map_lo);
-        }
+        if constexpr (LO_IN) prefetch_map(&map_lo_in);
+        if constexpr (LO_OUT) prefetch_map(&map_lo);
     }
     template <int BM, int BN>
     __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
@@ -277,6 +286,8 @@ struct StepEpi {
     template <int BM, int BN>
     __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
     {
+        float g = 1.0f;
+        if constexpr (!LO_IN) g = gain ? __ldg(gain + e.tile.batch) : 1.0f;
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
@@ -287,6 +298,10 @@ struct StepEpi {
                 hi = e.slots + kRing * kSlotBytes;
                 lo = ring.slot(e);
                 if (!ring.wait(e)) return false;
+            } else if constexpr (LO_OUT) {
+                slots_free(e);
+                hi = e.slots;
+                lo = e.slots + kSlotBytes;
             } else {
                 hi = slot_acquire(e);
             }
@@ -294,23 +309,28 @@ struct StepEpi {
             for (int h = 0; h < 2; ++h) {      // a loop: half the code to fetch in a kernel that runs a few microseconds
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
-                if constexpr (LO_IN) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t w[4] = {0u, 0u, 0u, 0u}, r[4], d[4];
+                    if constexpr (LO_IN) {
                         const uint4 y = slot_read(lo, e.lane, 4 * h + q);
-                        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-                        uint32_t r[4], d[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float g0 = fmaf(a, f16_lo(w[i]), v[8 * q + 2 * i]), g1 = fmaf(a, f16_hi(w[i]), v[8 * q + 2 * i + 1]);
-                            r[i] = pack_f16(g0, g1);
-                            d[i] = pack_f16(g0 - f16_lo(r[i]), g1 - f16_hi(r[i]));
-                        }
-                        slot_write(hi, e.lane, 4 * h + q, r[0], r[1], r[2], r[3]);
-                        if (lo_out) slot_write(lo, e.lane, 4 * h + q, d[0], d[1], d[2], d[3]);
+                        w[0] = y.x; w[1] = y.y; w[2] = y.z; w[3] = y.w;
                     }
-                } else {
-                    write_f16(hi, e.lane, h, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float g0 = v[8 * q + 2 * i], g1 = v[8 * q + 2 * i + 1];
+                        if constexpr (LO_IN) {
+                            g0 = fmaf(a, f16_lo(w[i]), g0);
+                            g1 = fmaf(a, f16_hi(w[i]), g1);
+                        } else {
+                            g0 *= g;
+                            g1 *= g;
+                        }
+                        r[i] = pack_f16(g0, g1);
+                        if constexpr (LO_OUT) d[i] = pack_f16(g0 - f16_lo(r[i]), g1 - f16_hi(r[i]));
+                    }
+                    slot_write(hi, e.lane, 4 * h + q, r[0], r[1], r[2], r[3]);
+                    if constexpr (LO_OUT) slot_write(lo, e.lane, 4 * h + q, d[0], d[1], d[2], d[3]);
                 }
             }
             fence_async_smem();
@@ -318,7 +338,7 @@ struct StepEpi {
             if (e.lane == 0) {
                 if (e.row0 < s.m) {
                     tma_store(&map_hi, hi, n, e.row0, e.tile.batch);
-                    if (LO_IN && lo_out) tma_store(&map_lo, lo, n, e.row0, e.tile.batch);
+                    if constexpr (LO_OUT) tma_store(&map_lo, lo, n, e.row0, e.tile.batch);
                 }
                 store_commit();
             }
@@ -338,6 +358,7 @@ struct ResultEpi {
     using State = AuxRing;
     CUtensorMap map_lo_in;
     OutTable out;
+    const float* gain;               // as in StepEpi
     float a, scale;
     int vec;
 
@@ -355,6 +376,8 @@ struct ResultEpi {
     __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
     {
         uint16_t* o = out.p[e.tile.batch];
+        float by = scale;
+        if constexpr (!LO_IN) by *= gain ? __ldg(gain + e.tile.batch) : 1.0f;
 #pragma unroll 1
         for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
@@ -380,9 +403,9 @@ struct ResultEpi {
                             v[8 * q + 2 * i + 1] = fmaf(a, f16_hi(w[i]), v[8 * q + 2 * i + 1]);
                         }
                     }
-                    slot_write(slot, e.lane, 4 * h + q, pack_b16(scale * v[8 * q], scale * v[8 * q + 1]),
-                               pack_b16(scale * v[8 * q + 2], scale * v[8 * q + 3]), pack_b16(scale * v[8 * q + 4], scale * v[8 * q + 5]),
-                               pack_b16(scale * v[8 * q + 6], scale * v[8 * q + 7]));
+                    slot_write(slot, e.lane, 4 * h + q, pack_b16(by * v[8 * q], by * v[8 * q + 1]),
+                               pack_b16(by * v[8 * q + 2], by * v[8 * q + 3]), pack_b16(by * v[8 * q + 4], by * v[8 * q + 5]),
+                               pack_b16(by * v[8 * q + 6], by * v[8 * q + 7]));
                 }
             }
             __syncwarp();
@@ -411,7 +434,7 @@ struct ResultEpi {
 
 struct Layout {
     int64_t group, ld, sq, sq_ld;
-    uint64_t norms, hi[2], lo[2], a, p, total;
+    uint64_t norms, gains, hi[2], lo[2], a, p, total;
 };
 
 Layout layout_of(int64_t n, int64_t rows, int64_t cols)
@@ -426,7 +449,8 @@ Layout layout_of(int64_t n, int64_t rows, int64_t cols)
     uint64_t at = 0;
     auto take = [&at](uint64_t bytes) { const uint64_t o = at; at += align256(bytes); return o; };
     const uint64_t x = 2ull * (uint64_t)(l.group * rows * l.ld), q = 2ull * (uint64_t)(l.group * l.sq * l.sq_ld);
-    l.norms = take(8ull * kNormBlocks * kGroup);
+    l.norms = take(8ull * kNormBlocks * (uint64_t)l.group);
+    l.gains = take(4ull * (uint64_t)l.group);
     for (int i = 0; i < 2; ++i) { l.hi[i] = take(x); l.lo[i] = take(x); }
     l.a = take(q);
     l.p = take(q);
@@ -486,7 +510,7 @@ int make_maps(Maps* m, uint16_t* const* hi, uint16_t* const* lo, const uint16_t*
 
 // A = down X X^T over the batch (`cur`: which X), the tall form from X^T; then P = c A A + b A + a I.
 template <int CG, int BN, bool MN>
-int gram_product(const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, cudaStream_t stream)
+int gram_product(const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, const float* gain, cudaStream_t stream)
 {
     Shape s;
     SymEpi<false> epi;
@@ -494,6 +518,7 @@ int gram_product(const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, f
     if ((rc = make_shape<CG, BN, MN, MN, SymEpi<false>>(&s, false, mn, mn, k, batch, 1, 1)) != CAST_OK) return rc;
     epi.map_out = epi.map_aux = m.a_chunk;
     epi.map_mirror = m.a_mirror;
+    epi.gain = gain;
     epi.scale = down;
     epi.add = epi.diag = 0.0f;
     const bool narrow = BN / CG == 64;
@@ -511,6 +536,7 @@ int poly_product(const Maps& m, int64_t mn, int64_t batch, const float* q, cudaS
     epi.map_out = m.p_chunk;
     epi.map_mirror = m.p_mirror;
     epi.map_aux = m.a_chunk;
+    epi.gain = nullptr;
     epi.diag = q[0];
     epi.add = q[1];
     epi.scale = q[2];
@@ -518,11 +544,11 @@ int poly_product(const Maps& m, int64_t mn, int64_t batch, const float* q, cudaS
 }
 
 template <bool MN>
-int gram_product(TileForm f, const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, cudaStream_t stream)
+int gram_product(TileForm f, const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, const float* gain, cudaStream_t stream)
 {
-    if (f == kPair256) return gram_product<2, 256, MN>(m, cur, mn, k, batch, down, stream);
-    if (f == kSingle128) return gram_product<1, 128, MN>(m, cur, mn, k, batch, down, stream);
-    return gram_product<1, 64, MN>(m, cur, mn, k, batch, down, stream);
+    if (f == kPair256) return gram_product<2, 256, MN>(m, cur, mn, k, batch, down, gain, stream);
+    if (f == kSingle128) return gram_product<1, 128, MN>(m, cur, mn, k, batch, down, gain, stream);
+    return gram_product<1, 64, MN>(m, cur, mn, k, batch, down, gain, stream);
 }
 
 int poly_product(TileForm f, const Maps& m, int64_t mn, int64_t batch, const float* q, cudaStream_t stream)
@@ -535,6 +561,7 @@ int poly_product(TileForm f, const Maps& m, int64_t mn, int64_t batch, const flo
 struct StepCall {
     const Maps* maps;
     const OutTable* out;
+    const float* gain;
     int64_t rows, cols, batch, sq;
     float a, scale;
     int cur;                          // which X
@@ -555,34 +582,46 @@ int step_product(const StepCall& c, Epi& epi)
     return launch<CG, BN, false, WIDE>(m.x_k[c.cur], narrow ? m.p_op_narrow : m.p_op, s, epi, c.stream);
 }
 
-template <int CG, int BN, bool WIDE, bool LO_IN>
-int step_product(const StepCall& c)
+template <int CG, int BN, bool WIDE, bool LO_IN, bool LO_OUT>
+int next_product(const StepCall& c)
 {
     const Maps& m = *c.maps;
-    if (c.last) {
-        ResultEpi<LO_IN> epi;
-        epi.map_lo_in = m.x_lo[c.cur];
-        epi.out = *c.out;
-        epi.a = c.a;
-        epi.scale = c.scale;
-        epi.vec = c.vec;
-        return step_product<CG, BN, WIDE>(c, epi);
-    }
-    StepEpi<LO_IN> epi;
+    StepEpi<LO_IN, LO_OUT> epi;
     epi.map_hi = m.x_hi[c.cur ^ 1];
     epi.map_lo = m.x_lo[c.cur ^ 1];
     epi.map_lo_in = m.x_lo[c.cur];
+    epi.gain = c.gain;
     epi.a = c.a;
-    epi.lo_out = c.lo_out;
     return step_product<CG, BN, WIDE>(c, epi);
+}
+
+template <int CG, int BN, bool WIDE, bool LO_IN>
+int result_product(const StepCall& c)
+{
+    ResultEpi<LO_IN> epi;
+    epi.map_lo_in = c.maps->x_lo[c.cur];
+    epi.out = *c.out;
+    epi.gain = c.gain;
+    epi.a = c.a;
+    epi.scale = c.scale;
+    epi.vec = c.vec;
+    return step_product<CG, BN, WIDE>(c, epi);
+}
+
+template <int CG, int BN, bool WIDE>
+int any_product(const StepCall& c)
+{
+    if (c.last) return c.lo_in ? result_product<CG, BN, WIDE, true>(c) : result_product<CG, BN, WIDE, false>(c);
+    if (c.lo_in) return c.lo_out ? next_product<CG, BN, WIDE, true, true>(c) : next_product<CG, BN, WIDE, true, false>(c);
+    return c.lo_out ? next_product<CG, BN, WIDE, false, true>(c) : next_product<CG, BN, WIDE, false, false>(c);
 }
 
 template <bool WIDE>
 int step_product(TileForm f, const StepCall& c)
 {
-    if (f == kPair256) return c.lo_in ? step_product<2, 256, WIDE, true>(c) : step_product<2, 256, WIDE, false>(c);
-    if (f == kSingle128) return c.lo_in ? step_product<1, 128, WIDE, true>(c) : step_product<1, 128, WIDE, false>(c);
-    return c.lo_in ? step_product<1, 64, WIDE, true>(c) : step_product<1, 64, WIDE, false>(c);
+    if (f == kPair256) return any_product<2, 256, WIDE>(c);
+    if (f == kSingle128) return any_product<1, 128, WIDE>(c);
+    return any_product<1, 64, WIDE>(c);
 }
 
 template <bool BF16, int VEC>
@@ -597,7 +636,7 @@ int launch_first(bool first, const PtrTable& t, int64_t batch, int64_t rows, int
     int64_t blocks = (units + 256 * 4 - 1) / (256 * 4);
     if (blocks > 2048) blocks = 2048;
     return launch_chained(false, first_x_kernel<BF16, VEC>, dim3((unsigned)blocks, (unsigned)batch), 256, 0, stream, 1, t, norms, (int)parts,
-                          reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.lo[0]), units, (uint32_t)(cols / VEC), l.ld,
+                          reinterpret_cast<uint16_t*>(ws + l.hi[0]), reinterpret_cast<uint16_t*>(ws + l.lo[0]), reinterpret_cast<float*>(ws + l.gains), units, (uint32_t)(cols / VEC), l.ld,
                           rows * l.ld, (double)eps);
 }
 
@@ -700,19 +739,20 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
         const TileForm step = tile_form(rows, cols, l.sq, batch, false, sms);
         Maps maps;
         if ((rc = make_maps(&maps, hi, lo, a, p, rows, cols, batch, l)) != CAST_OK) return rc;
-        bool has_lo = true;
+        bool has_lo = !updates_bf16;
         for (int k = 0; k < steps; ++k) {
             const float* q = coeffs ? coeffs + 3 * k : kQuintic;
             const int cur = k & 1;
-            rc = wide ? gram_product<false>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), st)
-                      : gram_product<true>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), st);
+            const float* gain = updates_bf16 && k == 0 ? reinterpret_cast<const float*>(ws + l.gains) : nullptr;
+            rc = wide ? gram_product<false>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, st)
+                      : gram_product<true>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, st);
             if (rc != CAST_OK) return rc;
             if ((rc = poly_product(poly, maps, l.sq, batch, q, st)) != CAST_OK) return rc;
             const bool last = k + 1 == steps;
             float amplify = 1.0f;      // of a small direction of X', by the steps after this one
             for (int j = k + 1; j < steps; ++j) amplify *= std::fabs(coeffs ? coeffs[3 * j] : kQuintic[0]);
-            const bool lo_out = has_lo && !last && amplify > kAmplify;
-            const StepCall c = {&maps, &to, rows, cols, batch, l.sq, q[0], scale / kX, cur, has_lo, lo_out, last, out_vec, st};
+            const bool lo_out = !last && amplify > kAmplify;
+            const StepCall c = {&maps, &to, gain, rows, cols, batch, l.sq, q[0], scale / kX, cur, has_lo, lo_out, last, out_vec, st};
             if ((rc = wide ? step_product<true>(step, c) : step_product<false>(step, c)) != CAST_OK) return rc;
             has_lo = lo_out;
         }
