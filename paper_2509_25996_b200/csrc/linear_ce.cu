@@ -5,7 +5,7 @@
 // so nothing cancels for a confident token, and a tile of logits needs no statistics of the rest of its row: the product's
 // epilogue turns the accumulators into E_ij = e^(l_ij - r_i) (0 at the label) and its row sums at once.  Per piece of tokens:
 //     target logits   r_i, one warp per token
-//     E = exp(H W^T - r)            product, epilogue writes E (bf16) and the row sums of its 256 (128) columns
+//     E = exp(H W^T - r)            product, epilogue writes E (bf16) and the row sums of half a tile each
 //     finish          S, loss, a_i = s / (1 + S_i), b_i = s S_i / (1 + S_i), and a H as bf16
 //     dH = a (E W) - b W_label      product over the vocabulary; the label's row is added in fp32 by the epilogue
 //     dW = E^T (a H)                product over the tokens
@@ -31,6 +31,7 @@ using namespace product;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMostSum = 2.35e17f;        // e^40
+constexpr int kHalves = 2;                  // a tile's columns are summed by two warps
 // The tensor cores truncate where they add a k-step to an accumulator, which shrinks a logit by 1.0e-9 of itself per k on the mean
 // (measured at k = 768, 5120 and 16384: 6.8e-7, 5.0e-6, 1.6e-5); the factor on the accumulators takes the mean out again.
 constexpr double kShrinkPerK = 1.0e-9;
@@ -95,8 +96,8 @@ struct ExpEpi : StoringEpi {
     CUtensorMap map_e;
     const float* refs;           // target logits of the piece
     const int32_t* labels;
-    float* sums;                 // [n_tiles][tokens]; negative: relative to `tops`
-    float* tops;                 // [n_tiles][tokens], base 2
+    float* sums;                 // [2 per tile: its halves][tokens]; negative: relative to `tops`
+    float* tops;                 // likewise, base 2
     float to_base2;              // log2(e), and the factor above
     int write_e;
 
@@ -106,7 +107,7 @@ struct ExpEpi : StoringEpi {
     {
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll 1
-        for (int c = 0; c < BN; c += 64) {
+        for (int c = e.c0; c < e.c1; c += 64) {
             const int n = e.col0 + c;
             if (n >= s.n) break;
             uint32_t slot = 0;
@@ -151,13 +152,14 @@ struct ExpEpi : StoringEpi {
             if ((unsigned)label >= (unsigned)s.n) label = -1;
             ref2 = __ldg(refs + row) * kLog2e;
         }
+        const int64_t at = (int64_t)(e.tile.tn * kHalves + (e.c0 ? 1 : 0)) * s.m;
         const bool active = label >= 0;
         float sum = pass<BN>(s, e, ref2, label, active);
         const bool over = !(sum <= kMostSum);          // also a sum that is not a number
         if (__any_sync(0xFFFFFFFFu, over)) {
             float top = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < BN; c += 32) {
+            for (int c = e.c0; c < e.c1; c += 32) {
                 float v[32];
                 if (e.col0 + c >= s.n) break;
                 tmem_load32(e.acc + (uint32_t)c, v);
@@ -171,10 +173,10 @@ struct ExpEpi : StoringEpi {
             const float again = pass<BN>(s, e, over ? top2 : ref2, label, active);
             if (over) {
                 sum = -again;
-                tops[(int64_t)e.tile.tn * s.m + row] = top2;
+                tops[at + row] = top2;
             }
         }
-        if (row < s.m) sums[(int64_t)e.tile.tn * s.m + row] = sum;
+        if (row < s.m) sums[at + row] = sum;
         return true;
     }
 };
@@ -350,7 +352,7 @@ struct HiddenGradEpi : StoringEpi {
     {
         if (partial) {
 #pragma unroll 1
-            for (int c = 0; c < BN && e.col0 + c < s.n; c += 32) {
+            for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 32) {
                 float v[32];
                 const uint32_t slot = slot_acquire(e);
                 tmem_load32(e.acc + (uint32_t)c, v);
@@ -370,7 +372,7 @@ struct HiddenGradEpi : StoringEpi {
         }
         const uint16_t* w = weight + (int64_t)(label < 0 ? 0 : label) * s.n;
 #pragma unroll 1
-        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+        for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
             const uint32_t slot = slot_acquire(e);
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
@@ -471,7 +473,7 @@ struct WeightGradEpi : StoringEpi {
         const int row = e.row0 + e.lane;
         if (last) {
 #pragma unroll 1
-            for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+            for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
                 const uint32_t slot = slot_acquire(e);
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
@@ -484,7 +486,7 @@ struct WeightGradEpi : StoringEpi {
             }
         } else {
 #pragma unroll 1
-            for (int c = 0; c < BN && e.col0 + c < s.n; c += 32) {
+            for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 32) {
                 const uint32_t slot = slot_acquire(e);
                 float v[32];
                 tmem_load32(e.acc + (uint32_t)c, v);
@@ -516,7 +518,14 @@ int64_t piece_of(int64_t tokens, int64_t vocab, int64_t piece_tokens)
 }
 
 bool paired(int64_t tokens) { return tokens > 128; }
-int64_t tile_cols(int64_t tokens) { return paired(tokens) ? 256 : 128; }
+int64_t tile_cols(int64_t tokens) { return (paired(tokens) ? 256 : 128) / kHalves; }      // of one row sum
+
+// Rows of `sums`: the halves of all tiles, the last one's empty half too.
+int64_t sum_rows(int64_t vocab, int64_t tokens)
+{
+    const int64_t tile = tile_cols(tokens) * kHalves;
+    return (vocab + tile - 1) / tile * kHalves;
+}
 
 // Splits of the vocabulary for dH: few tokens give few tiles, and each has the whole vocabulary to sum.  The time of
 // `splits` is taken as rounds of tiles x (blocks + 8 for filling and draining the pipeline), in blocks (~0.3 us for a pair),
@@ -548,10 +557,10 @@ int layout_of(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece_tokens, 
     l->piece = piece_of(tokens, vocab, piece_tokens);
     l->pieces = (tokens + l->piece - 1) / l->piece;
     l->e_ld = e_row_elems(vocab);
-    l->n_tiles = (vocab + tile_cols(l->piece) - 1) / tile_cols(l->piece);
+    l->n_tiles = sum_rows(vocab, l->piece);
     // the last piece may be short enough for the narrower tiles
     const int64_t tail = tokens - (l->pieces - 1) * l->piece;
-    const int64_t tail_tiles = (vocab + tile_cols(tail) - 1) / tile_cols(tail);
+    const int64_t tail_tiles = sum_rows(vocab, tail);
     int s1 = 1, s2 = 1;
     if (want_h) { s1 = hidden_splits(l->piece, vocab, dim, sms); s2 = hidden_splits(tail, vocab, dim, sms); }
     l->splits = s1;
@@ -752,7 +761,7 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
         f.vocab = (int)vocab;
         f.dim = (int)dim;
         f.tile_cols = (int)tile_cols(n);
-        f.n_tiles = (int)((vocab + f.tile_cols - 1) / f.tile_cols);
+        f.n_tiles = (int)sum_rows(vocab, n);
         f.grad_scale = grad_scale;
         if ((rc = launch_chained(false, finish_kernel, dim3((unsigned)((n + kFinishTokens - 1) / kFinishTokens)), 256, 0, st, 1, f)) != CAST_OK) return rc;
         if (grad_hidden) {

@@ -161,6 +161,7 @@ template <bool POLY>
 struct SymEpi {
     static constexpr bool kSym = true;
     static constexpr bool kInputsOnly = false;
+    static constexpr int kWarps = POLY ? 4 : 8;
     // POLY: the ring of aux, replaced in place, and a slot for the mirrored chunk; otherwise a slot for each
     static constexpr int kStaging = (POLY ? kRing + 1 : 2) * kSlotBytes;
     using State = AuxRing;
@@ -191,7 +192,7 @@ struct SymEpi {
         const bool mirror = e.col0 + BN <= e.tile.tm * BM;
         const float g = gain ? __ldg(gain + e.tile.batch) : 1.0f, scale_all = scale * g * g;
 #pragma unroll 1
-        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+        for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
             slots_free(e);
             uint32_t slot = e.slots;
@@ -260,8 +261,9 @@ template <bool LO_IN, bool LO_OUT>
 struct StepEpi {
     static constexpr bool kSym = false;
     static constexpr bool kInputsOnly = false;
-    // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise a slot for each, or two for hi in turn
-    static constexpr int kStaging = (LO_IN ? kRing + 1 : kTurns) * kSlotBytes;
+    static constexpr int kWarps = LO_IN ? 4 : 8;
+    // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise a slot for each
+    static constexpr int kStaging = (LO_IN ? kRing + 1 : LO_OUT ? 2 : 1) * kSlotBytes;
     using State = AuxRing;
     CUtensorMap map_hi, map_lo;      // X'
     CUtensorMap map_lo_in;           // X
@@ -289,7 +291,7 @@ struct StepEpi {
         float g = 1.0f;
         if constexpr (!LO_IN) g = gain ? __ldg(gain + e.tile.batch) : 1.0f;
 #pragma unroll 1
-        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+        for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
             uint32_t hi, lo = 0;
             if constexpr (LO_IN) {
@@ -354,6 +356,7 @@ template <bool LO_IN>
 struct ResultEpi {
     static constexpr bool kSym = false;
     static constexpr bool kInputsOnly = false;
+    static constexpr int kWarps = LO_IN ? 4 : 8;
     static constexpr int kStaging = (LO_IN ? kRing : 1) * kSlotBytes;
     using State = AuxRing;
     CUtensorMap map_lo_in;
@@ -379,7 +382,7 @@ struct ResultEpi {
         float by = scale;
         if constexpr (!LO_IN) by *= gain ? __ldg(gain + e.tile.batch) : 1.0f;
 #pragma unroll 1
-        for (int c = 0; c < BN && e.col0 + c < s.n; c += 64) {
+        for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
             __syncwarp();          // the chunk before this one has been read
             uint32_t slot = e.slots;

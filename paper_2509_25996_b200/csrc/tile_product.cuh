@@ -6,8 +6,9 @@
 //   warp 0    moves operand blocks of 64 k (128 bytes, the swizzle width) with TMA into a ring of stages
 //   warp 1    of the pair's first CTA issues tcgen05.mma over each stage and commits it back to the ring
 //   warp 2    allocates and frees tensor memory: two accumulators, so the next tile's products run under an epilogue
-//   warps 4-7 epilogue: 32 accumulator rows each (a lane is a row), through shared memory to TMA stores where the result
-//             is a matrix; arrays that it combines with the accumulators come by TMA as well (AuxRing)
+//   warps 4-  epilogue: 32 accumulator rows each (a lane is a row), all columns with four of these warps, half of them with
+//             eight; through shared memory to TMA stores where the result is a matrix; arrays that it combines with the
+//             accumulators come by TMA as well (AuxRing)
 // In a pair every CTA stages its own 128 rows of A and its own half of B; the tensor cores read both halves of B, which
 // halves the shared-memory traffic per product.  No load is multicast.
 //
@@ -31,8 +32,6 @@ namespace cast {
 namespace product {
 
 constexpr int kBK = 64;                          // k per block: 64 x 2 bytes = one 128-byte swizzle row
-constexpr int kThreads = 256;
-constexpr int kEpiWarps = 4;
 constexpr int kStageBytesA = 128 * kBK * 2;      // one block of 128 rows of A
 constexpr int kSlotBytes = 4096;                 // epilogue staging: 32 rows of 128 bytes
 constexpr int kRing = 3;                         // slots of an epilogue's ring (see AuxRing)
@@ -256,18 +255,21 @@ constexpr uint32_t kDescStep = MN_MAJOR ? (16 * 128) >> 4 : (16 * 2) >> 4;      
 
 // ------------------------------------------------------------------------------------------------ the kernel
 
-// `staging`: shared memory of one epilogue warp.  A stage is one 64-deep block (issued in ~250 cycles, computed in 512 by a pair
+// Of Epi: kWarps epilogue warps (four where a tile is only one chunk wide), each with kStaging bytes of shared memory.  A stage is one 64-deep block (issued in ~250 cycles, computed in 512 by a pair
 // and 256 by a single CTA with 128 columns), and two of them where they are computed in 128.
-template <int CG, int BN, int STAGING>
+template <int CG, int BN, class Epi>
 struct Config {
     static constexpr int BM = 128 * CG;
+    static constexpr int warps = BN >= 128 ? Epi::kWarps : 4;
+    static constexpr int threads = 128 + 32 * warps;
+    static constexpr int cols = BN / (warps / 4);                  // of one epilogue warp
     static constexpr int blocks = CG == 1 && BN == 64 ? 2 : 1;
     static constexpr int b_rows = BN / CG;                         // rows of B staged by one CTA
     static constexpr int b_bytes = b_rows * kBK * 2;               // of one block
     static constexpr int stage_bytes = blocks * (kStageBytesA + b_bytes);
-    static constexpr int room = (232448 - 1024 /* alignment */ - 768 /* barriers */ - kEpiWarps * STAGING) / stage_bytes;
+    static constexpr int room = (232448 - 1024 /* alignment */ - 768 /* barriers */ - warps * Epi::kStaging) / stage_bytes;
     static constexpr int stages = room < 8 ? room : 8;
-    static constexpr int smem_bytes = stages * stage_bytes + kEpiWarps * STAGING + 1024;
+    static constexpr int smem_bytes = stages * stage_bytes + warps * Epi::kStaging + 1024;
     static constexpr uint32_t tmem_cols = 2 * BN;
     static_assert(BN == 256 || BN == 128 || BN == 64, "two accumulators of BN columns: a power of two of at least 32");
     static_assert(b_rows % 64 == 0, "MN-major blocks are 64 wide");
@@ -279,11 +281,11 @@ struct EpiTile {
     Tile tile;
     int row0;            // first result row of this warp's 32
     int col0;            // first result column of the tile
+    int c0, c1;          // this warp's columns of the tile
     uint32_t acc;        // tensor-memory address of this warp's rows, column 0
     uint32_t slots;      // this warp's staging memory (slots of 4 KB, 1024-byte aligned)
     uint32_t bars;       // this warp's kRing mbarriers
     int lane;
-    int slot;            // staging slot to use next (kept from tile to tile)
     int first_row;       // of this warp in a tile
     int index, step;     // of the tile among all tiles, and to this CTA's next one
     const Stop* stop;
@@ -303,15 +305,13 @@ __device__ __forceinline__ uint4 slot_read(uint32_t slot_addr, int row, int chun
     return w;
 }
 
-// Two slots in turn, for epilogues that only store: takes the next one once the store that last used it has read it.
-constexpr int kTurns = 2;
-__device__ __forceinline__ uint32_t slot_acquire(EpiTile& e)
+// The slot of an epilogue that only stores, once the store that last used it has read it.  (One is enough: two such warps share a
+// scheduler, and the other one computes meanwhile.)
+__device__ __forceinline__ uint32_t slot_acquire(const EpiTile& e)
 {
-    if (e.lane == 0) store_wait_read<kTurns - 1>();
+    if (e.lane == 0) store_wait_read<0>();
     __syncwarp();
-    const uint32_t a = e.slots + (uint32_t)(e.slot * kSlotBytes);
-    e.slot = (e.slot + 1) % kTurns;
-    return a;
+    return e.slots;
 }
 // Hands a written slot to a TMA store (commits an empty group where nothing is to be stored, so that the groups count slots).
 __device__ __forceinline__ void slot_store(const EpiTile& e, uint32_t slot_addr, const CUtensorMap* map, int x, int y, int z, bool any)
@@ -325,12 +325,13 @@ __device__ __forceinline__ void slot_store(const EpiTile& e, uint32_t slot_addr,
 }
 
 // An epilogue provides: kSym (only tiles of the lower triangle), kInputsOnly (both operands are the caller's, whole before the
-// call's first kernel began), kStaging (bytes per warp), State (kept from tile to tile),
+// call's first kernel began), kWarps, kStaging (bytes per warp), State (kept from tile to tile),
 // prefetch() (its tensor maps), start() (before the first tile), tile() (false: give up).
 struct StoringEpi {
     static constexpr bool kSym = false;
     static constexpr bool kInputsOnly = false;
-    static constexpr int kStaging = kTurns * kSlotBytes;
+    static constexpr int kWarps = 8;
+    static constexpr int kStaging = kSlotBytes;
     struct State {};
     template <int BM, int BN>
     __device__ __forceinline__ void start(const Shape&, const EpiTile&, State&) const {}
@@ -349,18 +350,18 @@ struct AuxRing {
     __device__ __forceinline__ void start(const Shape& s, const EpiTile& e)
     {
         index = e.index;
-        c = 0;
+        c = e.c0;
         load_step = step = 0;
         phase = 0;
         find<BN, SYM>(s, e);
     }
-    // The tile at `index`, or the first one after it that has columns (a triangle's last blocks may have none).
+    // The tile at `index`, or the first one after it in which this warp has columns.
     template <int BN, bool SYM>
     __device__ __forceinline__ void find(const Shape& s, const EpiTile& e)
     {
         for (; index < s.total; index += e.step) {
             tile = tile_of<SYM>(s, index);
-            if (tile.tn * BN < s.n) break;
+            if (tile.tn * BN + c < s.n) break;
         }
     }
     __device__ __forceinline__ uint32_t slot(const EpiTile& e) const { return e.slots + (uint32_t)(step * kSlotBytes); }
@@ -376,8 +377,8 @@ struct AuxRing {
         }
         load_step = load_step + 1 == kRing ? 0 : load_step + 1;
         c += 64;
-        if (c >= BN || tile.tn * BN + c >= s.n) {
-            c = 0;
+        if (c >= e.c1 || tile.tn * BN + c >= s.n) {
+            c = e.c0;
             index += e.step;
             find<BN, SYM>(s, e);
         }
@@ -401,16 +402,16 @@ __device__ __forceinline__ void slots_free(const EpiTile& e)
 }
 
 template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__((Config<CG, BN, Epi>::threads), 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ Shape shape, const __grid_constant__ Epi epi)
 {
-    using C = Config<CG, BN, Epi::kStaging>;
+    using C = Config<CG, BN, Epi>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t ring = base;
     const uint32_t staging = base + C::stages * C::stage_bytes;
-    __shared__ __align__(8) unsigned long long bars[2 * C::stages + 4 + kEpiWarps * kRing];
+    __shared__ __align__(8) unsigned long long bars[2 * C::stages + 4 + C::warps * kRing];
     __shared__ uint32_t tmem_base_smem;
     __shared__ int stop_flag;
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::stages, accf0 = empty0 + 8 * C::stages, acce0 = accf0 + 16, ring0 = acce0 + 16;
@@ -421,8 +422,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (threadIdx.x == 0) {
         stop_flag = 0;
         for (int i = 0; i < C::stages; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(accf0 + 8 * i, 1); mbar_init(acce0 + 8 * i, CG * kEpiWarps); }
-        for (int i = 0; i < kEpiWarps * kRing; ++i) mbar_init(ring0 + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(accf0 + 8 * i, 1); mbar_init(acce0 + 8 * i, CG * C::warps); }
+        for (int i = 0; i < C::warps * kRing; ++i) mbar_init(ring0 + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x == 32) {      // descriptors are fetched while the predecessor drains
@@ -530,8 +531,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         e.lane = lane;
         e.slots = staging + (uint32_t)((warp - 4) * Epi::kStaging);
         e.bars = ring0 + (uint32_t)((warp - 4) * kRing * 8);
-        e.slot = 0;
-        e.first_row = (int)rank * 128 + (warp - 4) * 32;
+        e.first_row = (int)rank * 128 + (warp & 3) * 32;      // a warp reads the quarter of tensor memory that its index gives
+        e.c0 = (warp - 4) / 4 * C::cols;
+        e.c1 = e.c0 + C::cols;
         e.index = first;
         e.step = step;
         e.stop = &stop;
@@ -548,7 +550,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             tc_fence_after();
             e.row0 = e.tile.tm * C::BM + e.first_row;
             e.col0 = e.tile.tn * BN;
-            e.acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)((warp - 4) * 32) << 16);
+            e.acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)((warp & 3) * 32) << 16);
             ok = epi.template tile<C::BM, BN>(shape, e, state);
             tc_fence_before();
             __syncwarp();
@@ -594,7 +596,7 @@ inline uint32_t instruction_desc(bool bf16, bool a_mn, bool b_mn, int m, int n)
 template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
 int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t batch, int splits, int group)
 {
-    using C = Config<CG, BN, Epi::kStaging>;
+    using C = Config<CG, BN, Epi>;
     constexpr bool SYM = Epi::kSym;
     const int64_t mt = (m + C::BM - 1) / C::BM, nt = (n + BN - 1) / BN;
     static_assert(!SYM || C::BM % BN == 0, "the triangle's blocks are whole tiles");
@@ -621,7 +623,7 @@ int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t bat
 template <int CG, int BN, bool A_MN, bool B_MN, class Epi>
 int launch(const CUtensorMap& a, const CUtensorMap& b, const Shape& s, const Epi& epi, cudaStream_t stream)
 {
-    using C = Config<CG, BN, Epi::kStaging>;
+    using C = Config<CG, BN, Epi>;
     auto kernel = product_kernel<CG, BN, A_MN, B_MN, Epi>;
     int sms, rc;
     if ((rc = sm_count(&sms)) != CAST_OK) return rc;
@@ -634,7 +636,7 @@ int launch(const CUtensorMap& a, const CUtensorMap& b, const Shape& s, const Epi
         if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     const int units = s.total < sms / CG ? s.total : sms / CG;
-    return launch_chained(false, kernel, dim3((unsigned)(units * CG)), kThreads, C::smem_bytes, stream, CG, a, b, s, epi);
+    return launch_chained(false, kernel, dim3((unsigned)(units * CG)), C::threads, C::smem_bytes, stream, CG, a, b, s, epi);
 }
 
 }  // namespace product
