@@ -16,7 +16,7 @@
 // 128-byte swizzle.  K-major: rows of 64 k, groups of 8 rows 1024 bytes apart.  MN-major: rows of 64 m (or n), one row per k,
 // groups of 8 k 1024 bytes apart, and the next 64 m follow after the 64 k of the block (8192 bytes).
 //
-// Every wait is bounded (kWaitCycles); a role that gives up raises the CTA's stop flag, which ends the other roles, and
+// Every wait is bounded (kWaitCycles, kStageCycles); a role that gives up raises the CTA's stop flag, which ends the other roles, and
 // counts the failure in a word of host memory that the next call of the library reads.
 #pragma once
 
@@ -36,7 +36,8 @@ constexpr int kStageBytesA = 128 * kBK * 2;      // one block of 128 rows of A
 constexpr int kSlotBytes = 4096;                 // epilogue staging: 32 rows of 128 bytes
 constexpr int kRing = 3;                         // slots of an epilogue's ring (see AuxRing)
 constexpr int64_t kRotateBytes = 8 << 20;
-constexpr long long kWaitCycles = 4000000000ll;  // ~2 s; the longest wait of a healthy run is a tile (tens of microseconds)
+constexpr long long kWaitCycles = 4000000000ll;  // ~2 s; a copy or a stage's products take microseconds
+constexpr long long kStageCycles = 4096;         // allowed on top per stage of a tile, to who waits for the whole of it (a stage takes ~512)
 
 // Shape of one launch.  k_blocks = ceil(k / (64 blocks per stage)) stages are cut into `splits` runs of at most split_blocks, each of which
 // is a tile of its own (its epilogue sees Tile::split).
@@ -120,8 +121,8 @@ __device__ __forceinline__ bool elect_one()
 
 struct Stop { volatile int* flag; unsigned long long* fail_word; };
 
-// Waits for a phase; false once the CTA has stopped or the limit has passed.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Stop& stop)
+// Waits for a phase; false once the CTA has stopped or the limit (and `more` cycles) has passed.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Stop& stop, long long more = 0)
 {
     if (mbar_try(bar, parity)) return true;
     const long long t0 = clock64();
@@ -129,7 +130,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const S
         if (mbar_try(bar, parity)) return true;
         if ((i & 31u) == 0u) {
             if (*stop.flag) return false;
-            if (clock64() - t0 > kWaitCycles) break;
+            if (clock64() - t0 > kWaitCycles + more) break;
         }
     }
     *stop.flag = 1;
@@ -498,6 +499,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bool ok = true;
             const uint32_t a0 = desc_lo<A_MN>(ring), b0 = desc_lo<B_MN>(ring + C::blocks * kStageBytesA);
             uint32_t at = 0;          // of the stage, in units of 16 bytes
+            if constexpr (!Epi::kInputsOnly) chain_wait();      // the limits below are not for waiting for a predecessor
             for (int t = first; ok && t < shape.total; t += step, ++n_done) {
                 const Tile tile = tile_of<Epi::kSym>(shape, t);
                 const int buf = n_done & 1;
@@ -545,7 +547,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             e.index = t;
             e.tile = tile_of<Epi::kSym>(shape, t);
             const int buf = n_done & 1;
-            bool ok = mbar_wait(accf0 + 8 * buf, (uint32_t)(n_done >> 1) & 1u, stop);
+            bool ok = mbar_wait(accf0 + 8 * buf, (uint32_t)(n_done >> 1) & 1u, stop, (e.tile.kb1 - e.tile.kb0) * kStageCycles);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             tc_fence_after();
             e.row0 = e.tile.tm * C::BM + e.first_row;
