@@ -6,6 +6,7 @@
 //     A = X X^T               symmetric: only tiles on and below the diagonal, each stored twice (once transposed)
 //     P = a I + b A + c A A   symmetric likewise; a I + b A is added by the epilogue
 //     X' = P X
+// A long and narrow X gives A few tiles with a long sum each: its k is then cut into splits whose fp32 sums a small kernel adds.
 // Operands are never transposed in memory: X is read K-major in one product and MN-major in the other.
 //
 // Numbers: the operands are fp16, not bf16.  Every value is bounded (|X| singular values stay near 1), so the range is
@@ -256,6 +257,77 @@ struct SymEpi {
     }
 };
 
+// One split's sums of A as they are, fp32 [matrix][split][row][column]; blocks above the diagonal are left out.
+struct PartEpi {
+    static constexpr bool kSym = true;
+    static constexpr bool kInputsOnly = false;
+    static constexpr int kWarps = 8;
+    static constexpr int kStaging = kSlotBytes;
+    struct State {};
+    CUtensorMap map_out;
+
+    __device__ __forceinline__ void prefetch() const { prefetch_map(&map_out); }
+    template <int BM, int BN>
+    __device__ __forceinline__ void start(const Shape&, const EpiTile&, State&) const {}
+
+    template <int BM, int BN>
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State&) const
+    {
+#pragma unroll 1
+        for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 32) {
+            float v[32];
+            const uint32_t slot = slot_acquire(e);
+            tmem_load32(e.acc + (uint32_t)c, v);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                slot_write(slot, e.lane, q, __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+            slot_store(e, slot, &map_out, e.col0 + c, e.row0, e.tile.batch * s.splits + e.tile.split, e.row0 < s.m);
+        }
+        return true;
+    }
+};
+
+// A = scale gain^2 (sum of the splits, in order): a CTA takes one 32 x 32 block on or below the diagonal and stores it twice.
+__global__ void __launch_bounds__(256)
+add_parts_kernel(const float* __restrict__ parts, uint16_t* __restrict__ out, const float* __restrict__ gain, int splits, int n, int64_t part_ld, int64_t ld,
+                 float scale)
+{
+    __shared__ uint16_t block[32][33];
+    chain_next();
+    chain_wait();
+    int row = (int)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
+    while (row * (row + 1) / 2 > (int)blockIdx.x) --row;
+    while ((row + 1) * (row + 2) / 2 <= (int)blockIdx.x) ++row;
+    const int r0 = 32 * row, c0 = 32 * ((int)blockIdx.x - row * (row + 1) / 2);
+    const int r = (int)threadIdx.x >> 3, c = ((int)threadIdx.x & 7) * 4;        // four columns of a row
+    const float g = gain ? __ldg(gain + blockIdx.y) : 1.0f, by = scale * g * g;
+    const int64_t size = (int64_t)n * part_ld;
+    if (r0 + r < n) {
+        // rows are padded to whole vectors; what lies past the last column is not stored
+        const float* p = parts + (int64_t)blockIdx.y * splits * size + (int64_t)(r0 + r) * part_ld + c0 + c;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int s0 = 0; s0 < splits; s0 += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) x[s] = s0 + s < splits ? __ldg(reinterpret_cast<const float4*>(p + (s0 + s) * size)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int s = 0; s < 8; ++s) { sum.x += x[s].x; sum.y += x[s].y; sum.z += x[s].z; sum.w += x[s].w; }
+        }
+        const uint32_t lo = pack_f16(by * sum.x, by * sum.y), hi = pack_f16(by * sum.z, by * sum.w);
+        block[r][c] = (uint16_t)(lo & 0xFFFFu);
+        block[r][c + 1] = (uint16_t)(lo >> 16);
+        block[r][c + 2] = (uint16_t)(hi & 0xFFFFu);
+        block[r][c + 3] = (uint16_t)(hi >> 16);
+    }
+    __syncthreads();
+    uint16_t* o = out + (int64_t)blockIdx.y * n * ld;
+    for (int i = threadIdx.x; i < 1024; i += 256) {
+        const int y = i >> 5, x = i & 31;
+        if (r0 + y < n && c0 + x < n) o[(int64_t)(r0 + y) * ld + c0 + x] = block[y][x];
+        if (r0 != c0 && r0 + x < n && c0 + y < n) o[(int64_t)(c0 + y) * ld + r0 + x] = block[x][y];
+    }
+}
+
 // X' = gain acc (+ a lo): as hi + lo, or hi alone.
 template <bool LO_IN, bool LO_OUT>
 struct StepEpi {
@@ -435,9 +507,43 @@ struct ResultEpi {
 
 // ------------------------------------------------------------------------------------------------ host
 
+enum TileForm { kPair256, kSingle128, kSingle64 };      // 256 x 256 on two CTAs, 128 x 128 or 128 x 64 on one
+
+constexpr int kSms = 148;                                // the choice goes by a B200's, so that the workspace's size does not depend on the device
+constexpr int kMostSplits = 16;
+constexpr int64_t kPartBytes = 64 << 20;                 // of fp32 sums at most
+
+struct Form { TileForm tile; int splits; };
+
+// The form that takes least: rounds over the SMs x cycles per tile.  A 64-deep block of a pair's 256 x 256 takes 512 cycles of its
+// tensor cores; a single CTA is bound by its L2 port, 64 bytes per cycle: 512 cycles for 32 KB (128 x 128), 384 for 24 KB
+// (128 x 64).  Filling and draining a tile's pipeline: about 3000 cycles and 16 per column of its epilogue.  Splits of k (symmetric
+// products only) cost another kernel, about 8000 cycles, and their sums written and read at ~2.5 KB per cycle.  (Measured from
+// 256 x 256 to 4096 x 4096, alone and in batches: no other tile is more than 3 % faster than the one chosen.)
+Form choose_form(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int most_splits = kMostSplits)
+{
+    const int64_t kb = (k + kBK - 1) / kBK;
+    Form best = {kPair256, 1};
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= most_splits && s <= kb; ++s) {
+        if (s > 1 && 4 * s * batch * m * ((n + 63) / 64 * 64) > kPartBytes) break;
+        auto consider = [&](TileForm f, int64_t bm, int64_t bn, int64_t units, int64_t block) {
+            const int64_t a = (m + bm - 1) / bm, b = (n + bn - 1) / bn;
+            const int64_t tiles = (sym ? a * (a + 1) / 2 * (bm / bn) : a * b) * batch * s;
+            int64_t cost = (tiles + units - 1) / units * ((kb + s - 1) / s * block) + 3000 + 16 * bn;
+            if (s > 1) cost += 8000 + 8 * s * batch * m * n / 2500;
+            if (cost < least) { least = cost; best = {f, s}; }
+        };
+        consider(kPair256, 256, 256, kSms / 2, 512);
+        consider(kSingle128, 128, 128, kSms, 512);
+        consider(kSingle64, 128, 64, kSms, 384);
+    }
+    return best;
+}
+
 struct Layout {
     int64_t group, ld, sq, sq_ld;
-    uint64_t norms, gains, hi[2], lo[2], a, p, total;
+    uint64_t norms, gains, hi[2], lo[2], a, p, parts, total;
 };
 
 Layout layout_of(int64_t n, int64_t rows, int64_t cols)
@@ -457,25 +563,15 @@ Layout layout_of(int64_t n, int64_t rows, int64_t cols)
     for (int i = 0; i < 2; ++i) { l.hi[i] = take(x); l.lo[i] = take(x); }
     l.a = take(q);
     l.p = take(q);
+    auto parts_of = [&](int64_t batch) {
+        const Form f = choose_form(l.sq, l.sq, rows < cols ? cols : rows, batch, true);
+        return f.splits > 1 ? 4ull * (uint64_t)(f.splits * batch * l.sq * l.sq_ld) : 0ull;
+    };
+    const int64_t tail = n % l.group;            // the last group, where it is not full, may take more splits
+    const uint64_t parts = std::max(parts_of(l.group), tail ? parts_of(tail) : 0ull);
+    l.parts = take(parts);
     l.total = at;
     return l;
-}
-
-enum TileForm { kPair256, kSingle128, kSingle64 };      // 256 x 256 on two CTAs, 128 x 128 or 128 x 64 on one
-
-// The form that takes least: rounds over the SMs x cycles per tile.  A 64-deep block of a pair's 256 x 256 takes 512 cycles of its
-// tensor cores; a single CTA is bound by its L2 port, 64 bytes per cycle: 512 cycles for 32 KB (128 x 128), 384 for 24 KB
-// (128 x 64).  Filling and draining a tile's pipeline: about 3000 cycles and 8 per column of its epilogue.
-TileForm tile_form(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int sms)
-{
-    const int64_t kb = (k + kBK - 1) / kBK;
-    auto cost = [&](int64_t bm, int64_t bn, int64_t units, int64_t block) {
-        const int64_t a = (m + bm - 1) / bm, b = (n + bn - 1) / bn;
-        const int64_t tiles = (sym ? a * (a + 1) / 2 * (bm / bn) : a * b) * batch;
-        return (tiles + units - 1) / units * (kb * block) + 3000 + 16 * bn;
-    };
-    const int64_t p = cost(256, 256, sms / 2, 512), s = cost(128, 128, sms, 512), t = cost(128, 64, sms, 384);
-    return p <= s && p <= t ? kPair256 : s <= t ? kSingle128 : kSingle64;
 }
 
 // The tensor maps of a call, made once: its arrays stay where they are from step to step.  X and its two words exist twice, in
@@ -546,9 +642,33 @@ int poly_product(const Maps& m, int64_t mn, int64_t batch, const float* q, cudaS
     return launch<CG, BN, false, false>(m.a_op, BN / CG == 64 ? m.a_op_narrow : m.a_op, s, epi, stream);
 }
 
-template <bool MN>
-int gram_product(TileForm f, const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, const float* gain, cudaStream_t stream)
+// A in splits of k: their sums, then the kernel that adds them.
+template <int CG, int BN, bool MN>
+int gram_parts(int splits, const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, const float* gain, float* parts, uint16_t* a, int64_t ld,
+               cudaStream_t stream)
 {
+    Shape s;
+    PartEpi epi;
+    int rc;
+    if ((rc = make_shape<CG, BN, MN, MN, PartEpi>(&s, false, mn, mn, k, batch, splits, 1)) != CAST_OK) return rc;
+    if ((rc = make_map(&epi.map_out, parts, 4, mn, mn, batch * s.splits, ld, mn * ld, 32, 32, true)) != CAST_OK) return rc;
+    const bool narrow = BN / CG == 64;
+    if ((rc = launch<CG, BN, MN, MN>(MN ? m.x_mn[cur] : m.x_k[cur], MN ? m.x_mn[cur] : narrow ? m.x_k_narrow[cur] : m.x_k[cur], s, epi, stream)) != CAST_OK) return rc;
+    const int64_t blocks = (mn + 31) / 32;
+    return launch_chained(false, add_parts_kernel, dim3((unsigned)(blocks * (blocks + 1) / 2), (unsigned)batch), 256, 0, stream, 1, parts, a, gain, s.splits,
+                          (int)mn, ld, ld, down);
+}
+
+template <bool MN>
+int gram_product(const Form& form, const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, float down, const float* gain, float* parts, uint16_t* a,
+                 int64_t ld, cudaStream_t stream)
+{
+    const TileForm f = form.tile;
+    if (form.splits > 1) {
+        if (f == kPair256) return gram_parts<2, 256, MN>(form.splits, m, cur, mn, k, batch, down, gain, parts, a, ld, stream);
+        if (f == kSingle128) return gram_parts<1, 128, MN>(form.splits, m, cur, mn, k, batch, down, gain, parts, a, ld, stream);
+        return gram_parts<1, 64, MN>(form.splits, m, cur, mn, k, batch, down, gain, parts, a, ld, stream);
+    }
     if (f == kPair256) return gram_product<2, 256, MN>(m, cur, mn, k, batch, down, gain, stream);
     if (f == kSingle128) return gram_product<1, 128, MN>(m, cur, mn, k, batch, down, gain, stream);
     return gram_product<1, 64, MN>(m, cur, mn, k, batch, down, gain, stream);
@@ -694,7 +814,7 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
 {
     static const float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
     if (!updates || !out || !workspace) return CAST_ERR_NULL;
-    int rc, sms;
+    int rc;
     if ((rc = check_ortho_shape(n, rows, cols)) != CAST_OK) return rc;
     if (steps < 1 || steps > 100 || !(eps >= 0.0f) || !std::isfinite(eps) || !std::isfinite(scale)) return CAST_ERR_HYPER;
     for (int i = 0; coeffs && i < 3 * steps; ++i)
@@ -713,7 +833,6 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
     if ((rc = check_device_memory(updates, n)) != CAST_OK) return rc;
     if ((rc = check_device_memory(reinterpret_cast<const void* const*>(out), n)) != CAST_OK) return rc;
     if ((rc = check_device_memory(&workspace, 1)) != CAST_OK) return rc;
-    if ((rc = product::sm_count(&sms)) != CAST_OK) return rc;
 
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     cudaStream_t st = (cudaStream_t)stream;
@@ -738,8 +857,9 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
         if (updates_bf16) rc = in_vec ? launch_first<true, 8>(first == 0, in, batch, rows, cols, ws, l, eps, st) : launch_first<true, 1>(first == 0, in, batch, rows, cols, ws, l, eps, st);
         else rc = in_vec ? launch_first<false, 8>(first == 0, in, batch, rows, cols, ws, l, eps, st) : launch_first<false, 1>(first == 0, in, batch, rows, cols, ws, l, eps, st);
         if (rc != CAST_OK) return rc;
-        const TileForm gram = tile_form(l.sq, l.sq, big, batch, true, sms), poly = tile_form(l.sq, l.sq, l.sq, batch, true, sms);
-        const TileForm step = tile_form(rows, cols, l.sq, batch, false, sms);
+        const Form gram = choose_form(l.sq, l.sq, big, batch, true);
+        const TileForm poly = choose_form(l.sq, l.sq, l.sq, batch, true, 1).tile, step = choose_form(rows, cols, l.sq, batch, false, 1).tile;
+        float* parts = reinterpret_cast<float*>(ws + l.parts);
         Maps maps;
         if ((rc = make_maps(&maps, hi, lo, a, p, rows, cols, batch, l)) != CAST_OK) return rc;
         bool has_lo = !updates_bf16;
@@ -747,8 +867,8 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
             const float* q = coeffs ? coeffs + 3 * k : kQuintic;
             const int cur = k & 1;
             const float* gain = updates_bf16 && k == 0 ? reinterpret_cast<const float*>(ws + l.gains) : nullptr;
-            rc = wide ? gram_product<false>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, st)
-                      : gram_product<true>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, st);
+            rc = wide ? gram_product<false>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, parts, a, l.sq_ld, st)
+                      : gram_product<true>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, parts, a, l.sq_ld, st);
             if (rc != CAST_OK) return rc;
             if ((rc = poly_product(poly, maps, l.sq, batch, q, st)) != CAST_OK) return rc;
             const bool last = k + 1 == steps;

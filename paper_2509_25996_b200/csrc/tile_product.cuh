@@ -59,15 +59,15 @@ __device__ __forceinline__ Tile tile_of(const Shape& s, int t)
 {
     Tile r;
     if constexpr (SYM) {           // tiles that touch the lower triangle, tile rows first to last; `group` tile columns per tile row
-        const int per = s.group * (s.m_tiles * (s.m_tiles + 1) / 2);
-        r.batch = t / per;
-        const int i = t - r.batch * per, j = i / s.group;
+        const int per = s.group * (s.m_tiles * (s.m_tiles + 1) / 2), o = t / per;
+        r.batch = o / s.splits;
+        r.split = o - r.batch * s.splits;
+        const int i = t - o * per, j = i / s.group;
         int row = (int)((sqrtf(8.0f * (float)j + 1.0f) - 1.0f) * 0.5f);
         while (row * (row + 1) / 2 > j) --row;
         while ((row + 1) * (row + 2) / 2 <= j) ++row;
         r.tm = row;
         r.tn = i - s.group * (row * (row + 1) / 2);
-        r.split = 0;
     } else {
         const int per = s.m_tiles * s.n_tiles;
         const int o = t / per;
@@ -615,7 +615,7 @@ int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t bat
     s->n_tiles = (int)nt;
     s->batch = (int)batch;
     s->group = SYM ? C::BM / BN : group;
-    const int64_t per = SYM ? mt * (mt + 1) / 2 * s->group : mt * nt * s->splits;
+    const int64_t per = (SYM ? mt * (mt + 1) / 2 * s->group : mt * nt) * s->splits;
     if (per * batch > 0x3FFFFFFF) return CAST_ERR_SHAPE;
     s->total = (int)(per * batch);
     s->idesc = instruction_desc(bf16, A_MN, B_MN, C::BM, BN);

@@ -73,6 +73,24 @@ def test_shapes(rows, cols, dtype):
         assert distance(g.view.reshape(rows, cols), exact(x, QUINTIC, 5, scale=1.5)) <= tolerance(5, rows * cols)
 
 
+@pytest.mark.parametrize("n,rows,cols", [(1, 64, 5000), (1, 5000, 72), (3, 130, 8192), (1, 100, 6001), (2, 9000, 33), (1, 513, 7000), (66, 70, 4100)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_and_narrow(n, rows, cols, dtype):
+    """Few tiles with a long sum each: A is summed in splits.  (66: a full group and one of two, which takes other splits.)"""
+    u = draw(n, rows, cols, rows, dtype)
+    guards = [U.Guarded(rows * cols, torch.bfloat16, DEV) for _ in u]
+    rc, need = cast.cast_orthogonalize_workspace(n, rows, cols)
+    cast.check(rc)
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device=DEV)
+    cast.check(cast.cast_orthogonalize(u, dtype == torch.bfloat16, [g.view for g in guards], rows, cols, None, 5, 1e-7, 1.0, ws, need,
+                                       torch.cuda.current_stream()))
+    torch.cuda.synchronize()
+    assert all(g.intact() for g in guards) and bool((ws[need:] == 255).all())
+    for i in {0, n // 2, n - 1}:
+        assert distance(guards[i].view.reshape(rows, cols), exact(u[i], QUINTIC, 5)) <= tolerance(5)
+    assert torch.equal(guards[n - 1].view.reshape(rows, cols), ops.orthogonalize(u)[n - 1])
+
+
 @pytest.mark.parametrize("rows,cols,rank", [(512, 512, 8), (400, 1200, 4), (1200, 400, 16), (1024, 1024, 1)])
 def test_low_rank_updates(rows, cols, rank):
     """Spectra as momenta have them: few strong directions over weak ones, which the iteration amplifies."""
