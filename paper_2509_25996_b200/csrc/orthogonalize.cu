@@ -220,12 +220,10 @@ struct SymEpi {
                             v[8 * q + 2 * i + 1] = fmaf(add, f16_hi(u[i]), v[8 * q + 2 * i + 1]);
                         }
                     }
-                    // the chunk's 32 rows meet the diagonal in one half of its columns, or not at all
-                    if (n + 32 * h == e.row0) {
+                    // (no branch around this: the few warps that meet the diagonal would fetch its code for ~1500 cycles)
+                    const int d = e.row0 + e.lane - (n + 32 * h);      // where this row's diagonal entry lies in these columns
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i == e.lane) v[i] += diag;
-                    }
+                    for (int i = 0; i < 32; ++i) v[i] += i == d ? diag : 0.0f;
                 }
                 uint32_t p[16];
 #pragma unroll

@@ -450,13 +450,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         bool ok = true;
         Tile tile = tile_of<Epi::kSym>(shape, first);
         const uint32_t full_base = CG == 2 ? map_to_rank(full0, 0) : full0;
-        if constexpr (!Epi::kInputsOnly) chain_wait();
+        // The loop runs once without effect before the wait for the predecessor, so that its code is there when that ends.
+        bool live = Epi::kInputsOnly;
         for (int t = first; ok && t < shape.total;) {
             const int m0 = tile.tm * C::BM + (int)rank * 128, n0 = tile.tn * BN + (int)rank * C::b_rows;
             int kb = tile.kb0 + (int)((unsigned)(t * shape.rotate) % (unsigned)(tile.kb1 - tile.kb0));
-            for (int i = tile.kb0; i < tile.kb1; ++i, kb = kb + 1 == tile.kb1 ? tile.kb0 : kb + 1) {
+            for (int i = live ? tile.kb0 : tile.kb1 - 1; i < tile.kb1; ++i, kb = kb + 1 == tile.kb1 ? tile.kb0 : kb + 1) {
                 if (!(ok = mbar_wait_warp(empty0 + 8 * s, phase ^ 1u, stop))) break;
-                if (elect_one()) {
+                if (live && elect_one()) {
                     const uint32_t a = ring + s * C::stage_bytes, b = a + C::blocks * kStageBytesA, full = full_base + 8 * s;
                     if (rank == 0) mbar_expect(full0 + 8 * s, CG * C::stage_bytes);
 #pragma unroll
@@ -478,7 +479,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     }
                 }
                 __syncwarp();
-                if (++s == C::stages) { s = 0; phase ^= 1u; }
+                if (live && ++s == C::stages) { s = 0; phase ^= 1u; }
+            }
+            if (!live) {
+                live = true;
+                chain_wait();
+                continue;
             }
             t += step;
             if (t < shape.total) tile = tile_of<Epi::kSym>(shape, t);
