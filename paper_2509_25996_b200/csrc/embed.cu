@@ -11,10 +11,9 @@
 //     searches that advance together, so that their loads overlap.  16384 tokens take two launches, 262144 three.
 //   * sums: a CTA takes kPiece sorted tokens and a block of columns, asks for all of its rows at once and stores the table rows
 //     whose tokens all lie in its piece.  A table row whose tokens go on in the next piece leaves fp32 partial rows (the
-//     part that enters a piece and the part that leaves it), which a second kernel adds in order.  Every token row is read
-//     once, and a CTA's work does not depend on how often an id occurs; only the adding of partial rows of a frequent
-//     id is a chain, of tokens / kPiece rows.  (Letting a piece finish the row that it leaves, where that ends in the next
-//     piece, saves most of the partial rows but makes its loads a longer chain: 80 + 15 instead of 66 + 20 us.)
+//     part that enters a piece and the part that leaves it), which the warp that stores the last of them adds, in order.  Every
+//     token row is read once, and a CTA's work does not depend on how often an id occurs.  (Letting a piece finish the row
+//     that it leaves, where that ends in the next piece, saves partial rows but makes its loads a longer chain.)
 //   * up to kFew tokens are not sorted: the first token of an id looks for the others among the ids.
 //   * rows without a token become zeros in further CTAs of the kernel that sums: each looks up which of its kZeroRows rows
 //     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.
@@ -54,8 +53,9 @@ template <> struct Cols<8> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { v[2 * i] = fmaf(c, bf16_lo(w[i]), v[2 * i]); v[2 * i + 1] = fmaf(c, bf16_hi(w[i]), v[2 * i + 1]); }
     }
+    // a partial row that another SM may have written in this kernel: from L2
     __device__ __forceinline__ void add_partial(const float* p) {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+        const float4 a = __ldcg(reinterpret_cast<const float4*>(p)), b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
         v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
     }
     __device__ __forceinline__ void add(const Cols& o) {
@@ -83,7 +83,7 @@ template <> struct Cols<1> {
     using Raw = uint16_t;
     static __device__ __forceinline__ Raw load(const uint16_t* p) { return __ldg(p); }
     __device__ __forceinline__ void add(Raw x, float c) { v = fmaf(c, bf16_lo(x), v); }
-    __device__ __forceinline__ void add_partial(const float* p) { v += __ldg(p); }
+    __device__ __forceinline__ void add_partial(const float* p) { v += __ldcg(p); }
     __device__ __forceinline__ void add(const Cols& o) { v += o.v; }
     __device__ __forceinline__ void store_partial(float* p) const { *p = v; }
     static __device__ __forceinline__ Raw load_own(const uint16_t* p) { return *p; }
@@ -137,11 +137,11 @@ embed_kernel(const uint16_t* __restrict__ table, const int32_t* __restrict__ ids
 // ------------------------------------------------------------------------------------------------ order of the tokens
 
 __global__ void __launch_bounds__(kRankThreads)
-rank_runs_kernel(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_ids, int32_t* __restrict__ order, int64_t tokens, uint32_t vocab)
+rank_runs_kernel(const int32_t* __restrict__ ids, const SortStart start, int64_t tokens, uint32_t vocab)
 {
     chain_next();
     chain_wait();
-    rank_keys(ids, sorted_ids, order, tokens, vocab, blockIdx.x);
+    rank_keys(ids, start, tokens, vocab, blockIdx.x, gridDim.x);
 }
 
 constexpr int kMergeThreads = 128;
@@ -204,6 +204,7 @@ struct ScatterArgs {
     const int32_t* ids;           // sorted
     const int32_t* order;
     float* partial;               // [pieces][2][dim]: what enters a piece, what leaves it
+    uint32_t* arrivals;           // [2 pieces + groups][warp columns], zero
     uint16_t* dest;
     int64_t dim, vocab;
     int32_t tokens, pieces;
@@ -280,6 +281,99 @@ __device__ __forceinline__ void zero_block(const ScatterArgs& a)
     zero_rows<VEC>(a, row0, held);
 }
 
+// ------------------------------------------------------------------------------------------------ rows of several pieces
+
+// A table row whose tokens lie in several pieces has a partial row in each: what left the first, what entered the others.  Each warp
+// that has stored one counts itself in, and the last one adds them all, in the order of the pieces; nobody waits.  Pieces are
+// counted in groups of kGroup (aligned, so that the order of the additions depends on the sorted ids alone); a row of several
+// groups, a frequent token's, is joined from the groups' sums in the same way.
+constexpr int kGroup = 16;
+
+// The id that crosses the start of a piece (the token before it and its first one have it), -1 where none does.
+__device__ __forceinline__ int32_t crossing(const ScatterArgs& a, int64_t piece)
+{
+    const int64_t p = piece * kPiece;
+    if (p <= 0 || p >= a.tokens) return -1;
+    const int32_t before = __ldg(a.ids + p - 1), first = __ldg(a.ids + p);
+    return before == first ? first : -1;
+}
+
+// The warp has stored its part; whether all `parts` of this counter have been.
+__device__ __forceinline__ bool arrive_last(uint32_t* counter, int32_t parts)
+{
+    __threadfence();
+    __syncwarp();
+    uint32_t before = 0;
+    if ((threadIdx.x & 31) == 0) before = atomicAdd(counter, 1u);
+    before = __shfl_sync(0xFFFFFFFFu, before, 0);
+    if (before + 1 != (uint32_t)parts) return false;
+    __threadfence();
+    return true;
+}
+
+// Rows p, p + stride, ... of `count`, four at a time, the last ones too.
+template <int VEC>
+__device__ __forceinline__ void add_partials(Cols<VEC>& acc, const float* p, int64_t stride, int32_t count)
+{
+    for (int32_t i = 0; i < count; i += 4) {
+        Cols<VEC> row[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            row[j].zero();
+            if (i + j < count) row[j].add_partial(p + (int64_t)(i + j) * stride);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc.add(row[j]);
+    }
+}
+
+// `crossed`: of the row with this id, bit j for the start of piece kGroup group + j, j <= kGroup.  A whole warp; `in`: this lane has columns.
+template <int VEC>
+__device__ __forceinline__ void join_row(const ScatterArgs& a, int32_t id, uint32_t crossed, int32_t group, int32_t col, int32_t warp_col, int32_t warp_cols, bool in)
+{
+    const int lane = (int)threadIdx.x & 31;
+    const int32_t piece0 = group * kGroup, low = __ffs((int)crossed) - 1;
+    const bool begins = low > 0, goes_on = crossed >> kGroup & 1u;              // the row's first token is in this group; its last one is not
+    const int32_t entered = __popc(crossed & ((1u << kGroup) - 1u));            // pieces of the group that it enters
+    const int64_t row0 = begins ? 2 * (int64_t)(piece0 + low - 1) + 1 : 2 * (int64_t)piece0;      // its first partial row in the group
+    if (!arrive_last(a.arrivals + row0 * warp_cols + warp_col, entered + (begins ? 1 : 0))) return;
+    Cols<VEC> acc;
+    acc.zero();
+    if (in) {
+        if (begins) acc.add_partial(a.partial + row0 * a.dim + col);
+        add_partials<VEC>(acc, a.partial + 2 * (int64_t)(piece0 + low) * a.dim + col, 2 * a.dim, entered);
+    }
+    if (!begins || goes_on) {
+        if (in) acc.store_partial(a.partial + row0 * a.dim + col);             // the group's sum, where its first row was
+        int32_t head = group, tail = group;                                     // the groups with the row's first and last token
+        for (bool more = !begins; more;) {
+            const int32_t g = head - 1 - lane;                                  // does it enter this group, too?
+            const uint32_t no = ~__ballot_sync(0xFFFFFFFFu, crossing(a, (int64_t)g * kGroup) == id);
+            head -= no ? __ffs((int)no) : 32;
+            more = !no;
+        }
+        for (bool more = goes_on; more;) {
+            const int32_t g = tail + 2 + lane;
+            const uint32_t no = ~__ballot_sync(0xFFFFFFFFu, crossing(a, (int64_t)g * kGroup) == id);
+            tail += no ? __ffs((int)no) : 32;
+            more = !no;
+        }
+        // only one row goes on from a group to the next
+        if (!arrive_last(a.arrivals + (2 * (int64_t)a.pieces + head) * warp_cols + warp_col, tail - head + 1)) return;
+        const uint32_t starts = __ballot_sync(0xFFFFFFFFu, lane <= kGroup && crossing(a, (int64_t)head * kGroup + lane) == id);
+        acc.zero();
+        if (in) {
+            acc.add_partial(a.partial + (2 * (int64_t)(head * kGroup + __ffs((int)starts) - 2) + 1) * a.dim + col);
+            add_partials<VEC>(acc, a.partial + 2 * (int64_t)(head + 1) * kGroup * a.dim + col, 2 * kGroup * a.dim, tail - head);
+        }
+    }
+    if (!in) return;
+    uint16_t* dest = a.dest + (int64_t)id * a.dim + col;
+    typename Cols<VEC>::Raw old = {};
+    if (a.accumulate) old = Cols<VEC>::load_own(dest);
+    acc.store(dest, a.scale, a.accumulate, old);
+}
+
 // One piece of kPiece sorted tokens per group of a.lanes threads.  ACC: table rows are added to; what is there is asked for
 // together with the token rows, which would otherwise be one dependent load after the other.
 template <int VEC, bool COEF, bool ACC>
@@ -298,7 +392,7 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
     const int32_t piece = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
     if (piece >= a.pieces) return;
     const int32_t col = column_of<VEC>(a);
-    if (col >= a.dim) return;
+    const bool in = col < a.dim;
     const int32_t p0 = piece * kPiece, n = min(kPiece, a.tokens - p0);
     // the ids of the piece, the one before it and the one after it; 0xFFFFFFFF where there is none
     uint32_t id[kPiece + 2];
@@ -309,7 +403,9 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
         id[i] = p >= 0 && p < a.tokens ? (uint32_t)__ldg(a.ids + p) : 0xFFFFFFFFu;
     }
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) t[i] = i < n && id[i + 1] != kNoId ? __ldg(a.order + p0 + i) : -1;
+    for (int i = 0; i < kPiece; ++i) t[i] = in && i < n && id[i + 1] != kNoId ? __ldg(a.order + p0 + i) : -1;
+    const int lane = (int)threadIdx.x & 31;
+    const int32_t group = piece / kGroup, crosses = lane <= kGroup ? crossing(a, (int64_t)group * kGroup + lane) : -1;
     const uint16_t* src = a.src + col;
     float* partial = a.partial + (int64_t)piece * 2 * a.dim + col;
     bool entered = id[0] == id[1];        // the current row's tokens began in an earlier piece
@@ -344,101 +440,11 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
             }
         }
     }
-}
-
-// Partial rows 1 + from .. to of a piece that a row leaves (`p`: of the piece), eight at a time, the last ones too.
-template <int VEC>
-__device__ __forceinline__ void add_partials(Cols<VEC>& acc, const float* p, int64_t stride, int32_t from, int32_t to)
-{
-    for (int32_t i = from; i < to; i += 8) {
-        Cols<VEC> row[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            row[j].zero();
-            if (i + j < to) row[j].add_partial(p + (int64_t)(i + j + 1) * stride);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc.add(row[j]);
-    }
-}
-
-// The table rows that leave a piece they began in: what left it, then what entered the pieces after it.  One warp per piece and block
-// of 32 VEC columns; most find nothing to do, and most that do add a few rows.  A frequent id's partial rows are cut into a
-// run per warp of the CTA.
-constexpr int kJoinWarps = kScatterThreads / 32;
-
-template <int VEC>
-__global__ void __launch_bounds__(kScatterThreads)
-join_pieces_kernel(const __grid_constant__ ScatterArgs a)
-{
-    __shared__ int32_t found_id[kJoinWarps], found_count[kJoinWarps];
-    __shared__ Cols<VEC> part[kJoinWarps][32];
-    chain_next();
-    chain_wait();
-    const int lane = (int)threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
-    const int32_t first = (int32_t)blockIdx.x * kJoinWarps, piece = first + warp;
-    const int64_t col = ((int64_t)blockIdx.y * 32 + lane) * VEC, stride = 2 * a.dim;
-    const bool in = col < a.dim;
-    int32_t id = -1, count = 0;
-    if (piece + 1 < a.pieces) {                            // nothing leaves the last piece
-        const int32_t p0 = piece * kPiece, next = p0 + kPiece;
-        id = __ldg(a.ids + next - 1);
-        const int32_t after = __ldg(a.ids + next), before = p0 > 0 ? __ldg(a.ids + p0 - 1) : -1;
-        // how many of the 128 pieces after this one begin with the id, asked for in the same breath
-        int same[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t at = (int64_t)next + (int64_t)(32 * j + lane) * kPiece;
-            same[j] = at < a.tokens ? __ldg(a.ids + at) : -1;
-        }
-        if ((uint32_t)id == kNoId || after != id || before == id) id = -1;
-        else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) count += __popc(__ballot_sync(0xFFFFFFFFu, same[j] == id));
-            for (int32_t base = 128; count == base; base += 32) {
-                const int64_t at = (int64_t)next + (int64_t)(base + lane) * kPiece;
-                count += __popc(__ballot_sync(0xFFFFFFFFu, at < a.tokens && __ldg(a.ids + at) == id));
-            }
-        }
-    }
-    const bool together = id >= 0 && count > 8;
-    if (lane == 0) {
-        found_id[warp] = together ? id : -1;
-        found_count[warp] = count;
-    }
-    if (id >= 0 && !together && in) {
-        const float* p = a.partial + (int64_t)piece * stride + col;
-        uint16_t* dest = a.dest + (int64_t)id * a.dim + col;
-        typename Cols<VEC>::Raw old = {};
-        if (a.accumulate) old = Cols<VEC>::load_own(dest);
-        Cols<VEC> acc;
-        acc.zero();
-        acc.add_partial(p + a.dim);
-        add_partials<VEC>(acc, p, stride, 0, count);
-        acc.store(dest, a.scale, a.accumulate, old);
-    }
-    __syncthreads();
-    for (int f = 0; f < kJoinWarps; ++f) {
-        if (found_id[f] < 0) continue;
-        const int32_t n = found_count[f], each = (n + kJoinWarps - 1) / kJoinWarps, from = warp * each;
-        const float* p = a.partial + (int64_t)(first + f) * stride + col;
-        Cols<VEC> acc;
-        acc.zero();
-        if (in) {
-            if (warp == 0) acc.add_partial(p + a.dim);
-            add_partials<VEC>(acc, p, stride, from, min(n, from + each));
-        }
-        part[warp][lane] = acc;
-        __syncthreads();
-        if (warp == 0 && in) {
-            for (int i = 1; i < kJoinWarps; ++i) acc.add(part[i][lane]);
-            uint16_t* dest = a.dest + (int64_t)found_id[f] * a.dim + col;
-            typename Cols<VEC>::Raw old = {};
-            if (a.accumulate) old = Cols<VEC>::load_own(dest);
-            acc.store(dest, a.scale, a.accumulate, old);
-        }
-        __syncthreads();
-    }
+    const bool enters = id[0] == id[1] && id[1] != kNoId, leaves = id[kPiece] == id[kPiece + 1] && id[kPiece] < kNoId;
+    const int32_t warp_col = (int32_t)blockIdx.y * (a.lanes / 32) + (int)threadIdx.x % a.lanes / 32, warp_cols = (int32_t)gridDim.y * (a.lanes / 32);
+    if (enters) join_row<VEC>(a, (int32_t)id[1], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[1]), group, col, warp_col, warp_cols, in);
+    if (leaves && !(enters && id[kPiece] == id[1]))
+        join_row<VEC>(a, (int32_t)id[kPiece], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[kPiece]), group, col, warp_col, warp_cols, in);
 }
 
 // Few tokens need no order: the threads that hold an id's first token list the others by warp votes over all ids.
@@ -514,34 +520,40 @@ int launch_scatter(ScatterArgs a, const SortedTokens& sorted, cudaStream_t strea
     const unsigned zeros = a.accumulate ? 0u : (unsigned)((a.vocab + kZeroRows - 1) / kZeroRows);
     const dim3 grid(a.own + zeros, (unsigned)((units + a.lanes - 1) / a.lanes));
     if (sorted.few) return launch_chained(sorted.first, few_tokens_kernel<VEC, COEF>, grid, kScatterThreads, 0, stream, 1, a, (uint32_t)a.vocab);
-    const int rc = a.accumulate ? launch_chained(false, piece_sums_kernel<VEC, COEF, true>, grid, kScatterThreads, 0, stream, 1, a)
-                                : launch_chained(false, piece_sums_kernel<VEC, COEF, false>, grid, kScatterThreads, 0, stream, 1, a);
-    if (rc != CAST_OK || a.pieces < 2) return rc;
-    return launch_chained(false, join_pieces_kernel<VEC>, dim3((unsigned)((a.pieces - 1 + kJoinWarps - 1) / kJoinWarps), (unsigned)((units + 31) / 32)),
-                          kScatterThreads, 0, stream, 1, a);
+    return a.accumulate ? launch_chained(false, piece_sums_kernel<VEC, COEF, true>, grid, kScatterThreads, 0, stream, 1, a)
+                        : launch_chained(false, piece_sums_kernel<VEC, COEF, false>, grid, kScatterThreads, 0, stream, 1, a);
 }
 
 int64_t sort_array_bytes(int64_t tokens) { return (int64_t)align256(4ull * (uint64_t)tokens); }
+
+int64_t pieces_of(int64_t tokens) { return (tokens + kPiece - 1) / kPiece; }
+
+// Counters of join_row: two per piece and one per group, for each warp of columns (at most: one column per lane).
+int64_t arrival_count(int64_t tokens, int64_t dim)
+{
+    const int64_t pieces = pieces_of(tokens);
+    return (2 * pieces + (pieces + kGroup - 1) / kGroup) * ((dim + kScatterThreads - 1) / kScatterThreads * (kScatterThreads / 32));
+}
 
 }  // namespace
 
 uint64_t scatter_scratch_bytes(int64_t tokens, int64_t dim)
 {
-    // two copies of (sorted ids, order), then the partial rows
-    return 4ull * (uint64_t)sort_array_bytes(tokens) + align256(8ull * (uint64_t)((tokens + kPiece - 1) / kPiece) * (uint64_t)dim);
+    // two copies of (sorted ids, order), the counters, the partial rows
+    return 4ull * (uint64_t)sort_array_bytes(tokens) + align256(4ull * (uint64_t)arrival_count(tokens, dim)) +
+           align256(8ull * (uint64_t)pieces_of(tokens) * (uint64_t)dim);
 }
 
-void sort_arrays(void* scratch, int64_t tokens, int i, int32_t** ids, int32_t** order)
+SortStart sort_start(void* scratch, int64_t tokens, int64_t dim)
 {
     const int64_t step = sort_array_bytes(tokens);
     uint8_t* b = static_cast<uint8_t*>(scratch);
-    *ids = reinterpret_cast<int32_t*>(b + 2 * i * step);
-    *order = reinterpret_cast<int32_t*>(b + (2 * i + 1) * step);
+    return {reinterpret_cast<int32_t*>(b), reinterpret_cast<int32_t*>(b + step), reinterpret_cast<uint32_t*>(b + 4 * step), arrival_count(tokens, dim)};
 }
 
 int rank_blocks(int64_t tokens) { return tokens <= kFew ? 0 : (int)((tokens + kRun - 1) / kRun * (kRun / kRankKeys)); }
 
-int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, void* scratch, SortedTokens* sorted, cudaStream_t stream)
+int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, SortedTokens* sorted, cudaStream_t stream)
 {
     *sorted = {};
     sorted->tokens = tokens;
@@ -551,11 +563,12 @@ int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, 
         sorted->first = !ranked;
         return CAST_OK;
     }
-    int32_t *id_buf[2], *or_buf[2];
-    for (int i = 0; i < 2; ++i) sort_arrays(scratch, tokens, i, &id_buf[i], &or_buf[i]);
+    const SortStart start = sort_start(scratch, tokens, dim);
+    const int64_t step = sort_array_bytes(tokens) / 4;
+    int32_t *const id_buf[2] = {start.ids, start.ids + 2 * step}, *const or_buf[2] = {start.order, start.order + 2 * step};
     int rc;
-    if (!ranked && (rc = launch_chained(true, rank_runs_kernel, dim3((unsigned)rank_blocks(tokens)), kRankThreads, 0, stream, 1, ids, id_buf[0],
-                                        or_buf[0], tokens, (uint32_t)vocab)) != CAST_OK)
+    if (!ranked && (rc = launch_chained(true, rank_runs_kernel, dim3((unsigned)rank_blocks(tokens)), kRankThreads, 0, stream, 1, ids, start, tokens,
+                                        (uint32_t)vocab)) != CAST_OK)
         return rc;
     int cur = 0;
     for (int64_t run = kRun; run < tokens; run *= kWays, cur ^= 1) {
@@ -573,7 +586,8 @@ int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, 
     }
     sorted->ids = id_buf[cur];
     sorted->order = or_buf[cur];
-    sorted->scratch = static_cast<uint8_t*>(scratch) + 4 * sort_array_bytes(tokens);
+    sorted->arrivals = start.arrivals;
+    sorted->partial = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(start.arrivals) + align256(4ull * (uint64_t)start.arrival_count));
     return CAST_OK;
 }
 
@@ -585,10 +599,11 @@ int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* c
     a.coef = coef;
     a.ids = sorted.ids;
     a.order = sorted.order;
-    a.partial = static_cast<float*>(sorted.scratch);
+    a.partial = sorted.partial;
+    a.arrivals = sorted.arrivals;
     a.dest = dest;
     a.tokens = (int32_t)sorted.tokens;
-    a.pieces = (int32_t)((sorted.tokens + kPiece - 1) / kPiece);
+    a.pieces = (int32_t)pieces_of(sorted.tokens);
     a.dim = dim;
     a.vocab = vocab;
     a.own = 0;
@@ -669,6 +684,6 @@ extern "C" int cast_embed_grad(const cast_bf16* grad_out, const int32_t* ids, ca
     const void* ptrs[4] = {grad_out, ids, grad_table, workspace};
     if ((rc = check_device_memory(ptrs, 4)) != CAST_OK) return rc;
     SortedTokens sorted;
-    if ((rc = sort_tokens(false, ids, tokens, vocab, workspace, &sorted, (cudaStream_t)stream)) != CAST_OK) return rc;
+    if ((rc = sort_tokens(false, ids, tokens, vocab, dim, workspace, &sorted, (cudaStream_t)stream)) != CAST_OK) return rc;
     return scatter_rows(sorted, grad_out, nullptr, scale, grad_table, vocab, dim, accumulate != 0, (cudaStream_t)stream);
 }

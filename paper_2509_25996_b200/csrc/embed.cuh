@@ -12,17 +12,26 @@ uint64_t scatter_scratch_bytes(int64_t tokens, int64_t dim);
 struct SortedTokens {
     const int32_t* ids;
     const int32_t* order;
-    void* scratch;          // partial rows
+    uint32_t* arrivals;     // counters of partial rows
+    float* partial;
     int64_t tokens;
     bool few;               // so few that they are left as they came
     bool first;             // few, and no kernel of the call has been launched yet
 };
 
+// What the first kernel of a sort writes: ranked runs, and zeros to the counters.
+struct SortStart {
+    int32_t* ids;
+    int32_t* order;
+    uint32_t* arrivals;
+    int64_t arrival_count;
+};
+SortStart sort_start(void* scratch, int64_t tokens, int64_t dim);
+
 // Sorts into `scratch`: runs of kRun keys (rank_keys, launched here, or with `ranked` already done by rank_blocks() CTAs of the
-// call's first kernel into sort_arrays(0)), then merges of the runs.
+// call's first kernel), then merges of the runs.
 int rank_blocks(int64_t tokens);
-void sort_arrays(void* scratch, int64_t tokens, int i, int32_t** ids, int32_t** order);
-int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, void* scratch, SortedTokens* sorted, cudaStream_t stream);
+int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, SortedTokens* sorted, cudaStream_t stream);
 
 // dest[v] = scale * sum_{t: id = v} coef[t] src[t] (coef NULL: 1).  accumulate: added to dest, whose rows without a token are left
 // alone; otherwise those become zero.
@@ -44,10 +53,11 @@ constexpr int kRankKeys = 128;        // keys of a run that one CTA places ...
 constexpr int kRankShare = 4;         // ... with this many threads each
 constexpr int kRankThreads = kRankKeys * kRankShare;
 
-// One CTA's part of ranking runs of kRun keys: a key's place is the number of keys of its run that come before it.
-__device__ __forceinline__ void rank_keys(const int32_t* __restrict__ ids, int32_t* __restrict__ sorted_ids, int32_t* __restrict__ order, int64_t tokens,
-                                          uint32_t vocab, unsigned block)
+// One of `blocks` CTAs' part of ranking runs of kRun keys: a key's place is the number of keys of its run that come before it.
+__device__ __forceinline__ void rank_keys(const int32_t* __restrict__ ids, const SortStart& start, int64_t tokens, uint32_t vocab, unsigned block,
+                                          unsigned blocks)
 {
+    for (int64_t i = (int64_t)block * kRankThreads + threadIdx.x; i < start.arrival_count; i += (int64_t)blocks * kRankThreads) start.arrivals[i] = 0u;
     __shared__ uint4 keys4[kRun / 4];
     uint32_t* keys = reinterpret_cast<uint32_t*>(keys4);
     const int64_t run0 = (int64_t)(block / (kRun / kRankKeys)) * kRun;
@@ -80,8 +90,8 @@ __device__ __forceinline__ void rank_keys(const int32_t* __restrict__ ids, int32
 #pragma unroll
     for (int d = 1; d < kRankShare; d *= 2) place += __shfl_xor_sync(0xFFFFFFFFu, place, d);
     if (share == 0 && first + (int)threadIdx.x / kRankShare < len) {
-        sorted_ids[run0 + place] = (int32_t)k;
-        order[run0 + place] = (int32_t)(run0 + p);
+        start.ids[run0 + place] = (int32_t)k;
+        start.order[run0 + place] = (int32_t)(run0 + p);
     }
 }
 

@@ -52,12 +52,11 @@ __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0
 // the labels, which dW's label terms need.
 __global__ void __launch_bounds__(kRankThreads)
 target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restrict__ weight, const int32_t* __restrict__ labels,
-                    float* __restrict__ refs, int64_t tokens, int vocab, int dim, unsigned own, int32_t* __restrict__ sorted_ids,
-                    int32_t* __restrict__ order)
+                    float* __restrict__ refs, int64_t tokens, int vocab, int dim, unsigned own, const SortStart start)
 {
     chain_next();
     if (blockIdx.x >= own) {
-        rank_keys(labels, sorted_ids, order, tokens, (uint32_t)vocab, blockIdx.x - own);
+        rank_keys(labels, start, tokens, (uint32_t)vocab, blockIdx.x - own, gridDim.x - own);
         return;
     }
     const int64_t t = (int64_t)blockIdx.x * (kRankThreads / 32) + (threadIdx.x >> 5);
@@ -733,13 +732,12 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
     float* a = reinterpret_cast<float*>(ws + l.a);
     float* b = reinterpret_cast<float*>(ws + l.b);
     const unsigned own = (unsigned)((tokens + kRankThreads / 32 - 1) / (kRankThreads / 32));
-    int32_t *sorted_ids, *order;
-    sort_arrays(ws + l.scatter, tokens, 0, &sorted_ids, &order);
+    const SortStart start = sort_start(ws + l.scatter, tokens, dim);
     if ((rc = launch_chained(true, target_logit_kernel, dim3(own + (grad_weight ? (unsigned)rank_blocks(tokens) : 0u)), kRankThreads, 0, st, 1, hidden,
-                             weight, labels, refs, tokens, (int)vocab, (int)dim, own, sorted_ids, order)) != CAST_OK)
+                             weight, labels, refs, tokens, (int)vocab, (int)dim, own, start)) != CAST_OK)
         return rc;
     SortedTokens sorted;      // the merges now, while the ids are in L2, not after the products have swept it
-    if (grad_weight && (rc = sort_tokens(true, labels, tokens, vocab, ws + l.scatter, &sorted, st)) != CAST_OK) return rc;
+    if (grad_weight && (rc = sort_tokens(true, labels, tokens, vocab, dim, ws + l.scatter, &sorted, st)) != CAST_OK) return rc;
     for (int64_t i = 0; i < l.pieces; ++i) {
         const int64_t t0 = i * l.piece, n = tokens - t0 < l.piece ? tokens - t0 : l.piece;
         rc = paired(n) ? exp_product<2, 256>(c, t0, n) : exp_product<1, 128>(c, t0, n);
