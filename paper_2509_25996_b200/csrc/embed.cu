@@ -208,17 +208,17 @@ struct ScatterArgs {
     uint16_t* dest;
     int64_t dim, vocab;
     int32_t tokens, pieces;
-    unsigned own;                 // CTAs that sum; the ones after them write zeros
+    unsigned own, columns;        // CTAs that sum: own / columns for the tokens x columns; the ones after them write zeros
     float scale;
     int lanes;                    // threads per row: 32 .. 256, a power of two
     int accumulate;
 };
 
-// Column of this thread: a.lanes threads per row, the rest of a long row in blockIdx.y.
+// Column of this thread: a.lanes threads per row, the rest of a long row in the CTAs beside it.
 template <int VEC>
 __device__ __forceinline__ int32_t column_of(const ScatterArgs& a)
 {
-    return ((int32_t)blockIdx.y * a.lanes + (int)threadIdx.x % a.lanes) * VEC;
+    return ((int32_t)(blockIdx.x % a.columns) * a.lanes + (int)threadIdx.x % a.lanes) * VEC;
 }
 
 // First sorted position with an id of at least `id`, found by the 32 lanes of a warp together (32 ways per step).
@@ -385,11 +385,11 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
     chain_wait();
     if constexpr (!ACC) {
         if (blockIdx.x >= a.own) {
-            if (blockIdx.y == 0) zero_block<VEC>(a);
+            zero_block<VEC>(a);
             return;
         }
     }
-    const int32_t piece = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
+    const int32_t piece = (int32_t)(blockIdx.x / a.columns) * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;
     if (piece >= a.pieces) return;
     const int32_t col = column_of<VEC>(a);
     const bool in = col < a.dim;
@@ -441,7 +441,7 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
         }
     }
     const bool enters = id[0] == id[1] && id[1] != kNoId, leaves = id[kPiece] == id[kPiece + 1] && id[kPiece] < kNoId;
-    const int32_t warp_col = (int32_t)blockIdx.y * (a.lanes / 32) + (int)threadIdx.x % a.lanes / 32, warp_cols = (int32_t)gridDim.y * (a.lanes / 32);
+    const int32_t warp_col = col / (32 * VEC), warp_cols = (int32_t)a.columns * (a.lanes / 32);
     if (enters) join_row<VEC>(a, (int32_t)id[1], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[1]), group, col, warp_col, warp_cols, in);
     if (leaves && !(enters && id[kPiece] == id[1]))
         join_row<VEC>(a, (int32_t)id[kPiece], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[kPiece]), group, col, warp_col, warp_cols, in);
@@ -463,7 +463,6 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
     ids[threadIdx.x] = (int)threadIdx.x < a.tokens ? (uint32_t)__ldg(a.ids + threadIdx.x) : 0xFFFFFFFFu;
     __syncthreads();
     if (blockIdx.x >= a.own) {           // a block of rows: zeros where no token is (only in a call of its own)
-        if (blockIdx.y != 0) return;
         const int64_t row0 = (int64_t)(blockIdx.x - a.own) * kZeroRows;
         const int64_t id = (int64_t)ids[threadIdx.x] - row0;
         if (ids[threadIdx.x] < vocab && id >= 0 && id < kZeroRows) atomicOr(&held, 1u << (int)id);
@@ -471,7 +470,7 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
         zero_rows<VEC>(a, row0, held);
         return;
     }
-    const int32_t t = (int32_t)blockIdx.x * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;      // one token per warp
+    const int32_t t = (int32_t)(blockIdx.x / a.columns) * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;      // one token per warp
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const uint32_t id = t < a.tokens ? ids[t] : 0xFFFFFFFFu;
     if (id >= vocab) return;
@@ -516,9 +515,10 @@ template <int VEC, bool COEF>
 int launch_scatter(ScatterArgs a, const SortedTokens& sorted, cudaStream_t stream)
 {
     const int64_t units = (a.dim + VEC - 1) / VEC, groups = kScatterThreads / a.lanes, items = sorted.few ? a.tokens : a.pieces;
-    a.own = (unsigned)((items + groups - 1) / groups);
+    a.columns = (unsigned)((units + a.lanes - 1) / a.lanes);
+    a.own = (unsigned)((items + groups - 1) / groups) * a.columns;
     const unsigned zeros = a.accumulate ? 0u : (unsigned)((a.vocab + kZeroRows - 1) / kZeroRows);
-    const dim3 grid(a.own + zeros, (unsigned)((units + a.lanes - 1) / a.lanes));
+    const dim3 grid(a.own + zeros);
     if (sorted.few) return launch_chained(sorted.first, few_tokens_kernel<VEC, COEF>, grid, kScatterThreads, 0, stream, 1, a, (uint32_t)a.vocab);
     return a.accumulate ? launch_chained(false, piece_sums_kernel<VEC, COEF, true>, grid, kScatterThreads, 0, stream, 1, a)
                         : launch_chained(false, piece_sums_kernel<VEC, COEF, false>, grid, kScatterThreads, 0, stream, 1, a);
@@ -606,7 +606,7 @@ int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* c
     a.pieces = (int32_t)pieces_of(sorted.tokens);
     a.dim = dim;
     a.vocab = vocab;
-    a.own = 0;
+    a.own = a.columns = 0;
     a.scale = scale;
     a.accumulate = accumulate;
     const bool vec = dim % 8 == 0 && !((uintptr_t)src & 15u) && !((uintptr_t)dest & 15u);
