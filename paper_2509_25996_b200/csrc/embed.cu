@@ -74,7 +74,7 @@ template <> struct Cols<8> {
         uint32_t r[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[i] = pack_bf16(fmaf(scale, v[2 * i], bf16_lo(o[i])), fmaf(scale, v[2 * i + 1], bf16_hi(o[i])));
-        *q = make_uint4(r[0], r[1], r[2], r[3]);
+        __stcs(q, make_uint4(r[0], r[1], r[2], r[3]));
     }
 };
 template <> struct Cols<1> {
@@ -249,13 +249,13 @@ __device__ __forceinline__ void zero_rows(const ScatterArgs& a, int64_t row0, ui
         for (int r = 0; r < kZeroRows && row0 + r < a.vocab; ++r) {
             if (held >> r & 1u) continue;
             Raw* to = reinterpret_cast<Raw*>(a.dest + (row0 + r) * a.dim);
-            for (uint32_t i = threadIdx.x; i < per; i += kScatterThreads) to[i] = Raw{};
+            for (uint32_t i = threadIdx.x; i < per; i += kScatterThreads) __stcs(to + i, Raw{});
         }
     } else {
         Raw* to = reinterpret_cast<Raw*>(a.dest + row0 * a.dim);
         const uint32_t rows = (uint32_t)min((int64_t)kZeroRows, a.vocab - row0);
         for (uint32_t i = threadIdx.x; i < rows * per; i += kScatterThreads)
-            if (!(held >> (i / per) & 1u)) to[i] = Raw{};
+            if (!(held >> (i / per) & 1u)) __stcs(to + i, Raw{});
     }
 }
 
