@@ -78,7 +78,8 @@ def reference(grad, ids, vocab, scale, base=None):
 
 CASES = [(1, 1, 8, "any"), (1, 7, 61, "any"), (63, 40, 64, "one"), (64, 40, 64, "one"), (65, 40, 64, "one"), (127, 3, 72, "hot"), (1000, 400, 768, "any"),
          (1024, 50, 8, "any"), (1025, 50, 16, "hot"), (2048, 5000, 24, "sorted"), (5000, 90, 61, "hot"), (16384, 3000, 32, "hot"), (16385, 30, 40, "any"),
-         (20000, 10, 8, "one"), (40000, 100000, 8, "hot"), (270000, 500, 8, "hot")]
+         (20000, 10, 8, "one"), (40000, 100000, 8, "hot"), (270000, 500, 8, "hot"),
+         (3000, 5, 4096, "hot"), (5000, 3, 300, "one"), (9000, 6, 777, "hot")]
 
 
 @pytest.mark.parametrize("tokens,vocab,dim,kind", CASES)
