@@ -440,6 +440,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_base_smem, 0);
     const Stop stop = {&stop_flag, shape.fail_word};
     const int first = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
+    // Both operands of a symmetric product are the same array: a square tile on the diagonal stages its rows once, for A and B.
+    constexpr bool kSquare = Epi::kSym && A_MN == B_MN && C::BM == BN;
 
     // The two issuing roles run as whole warps on uniform values, with one lane elected for the instructions themselves: in a
     // single lane's branch the compiler has to move every descriptor word from vector to uniform registers, and issuing the
@@ -453,13 +455,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // The loop runs once without effect before the wait for the predecessor, so that its code is there when that ends.
         bool live = Epi::kInputsOnly;
         for (int t = first; ok && t < shape.total;) {
+            const bool once = kSquare && tile.tm == tile.tn;
             const int m0 = tile.tm * C::BM + (int)rank * 128, n0 = tile.tn * BN + (int)rank * C::b_rows;
             int kb = tile.kb0 + (int)((unsigned)(t * shape.rotate) % (unsigned)(tile.kb1 - tile.kb0));
             for (int i = live ? tile.kb0 : tile.kb1 - 1; i < tile.kb1; ++i, kb = kb + 1 == tile.kb1 ? tile.kb0 : kb + 1) {
                 if (!(ok = mbar_wait_warp(empty0 + 8 * s, phase ^ 1u, stop))) break;
                 if (live && elect_one()) {
                     const uint32_t a = ring + s * C::stage_bytes, b = a + C::blocks * kStageBytesA, full = full_base + 8 * s;
-                    if (rank == 0) mbar_expect(full0 + 8 * s, CG * C::stage_bytes);
+                    if (rank == 0) mbar_expect(full0 + 8 * s, CG * (once ? C::blocks * kStageBytesA : C::stage_bytes));
 #pragma unroll
                     for (int j = 0; j < C::blocks; ++j) {
                         const int k = (kb * C::blocks + j) * kBK;      // past the end of k: zeros
@@ -470,6 +473,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         } else {
                             tma_load<CG>(aj, &map_a, full, k, m0, tile.batch);
                         }
+                        if (once) continue;
                         if constexpr (B_MN) {
 #pragma unroll
                             for (int i = 0; i < C::b_rows / 64; ++i) tma_load<CG>(bj + i * 8192, &map_b, full, n0 + 64 * i, k, tile.batch);
@@ -512,12 +516,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (!(ok = mbar_wait_warp(acce0 + 8 * buf, (uint32_t)((n_done >> 1) & 1) ^ 1u, stop))) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
+                const uint32_t b_at = kSquare && tile.tm == tile.tn ? a0 : b0;
                 uint32_t accumulate = 0;
                 for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
                     if (!(ok = mbar_wait_warp(full0 + 8 * s, phase, stop))) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint32_t a = a0 + at, b = b0 + at;
+                        const uint32_t a = a0 + at, b = b_at + at;
 #pragma unroll
                         for (int i = 0; i < C::blocks * (kBK / 16); ++i) {
                             const int j = i / (kBK / 16), k = i % (kBK / 16);
