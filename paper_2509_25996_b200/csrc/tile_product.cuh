@@ -35,7 +35,6 @@ constexpr int kBK = 64;                          // k per block: 64 x 2 bytes = 
 constexpr int kStageBytesA = 128 * kBK * 2;      // one block of 128 rows of A
 constexpr int kSlotBytes = 4096;                 // epilogue staging: 32 rows of 128 bytes
 constexpr int kRing = 3;                         // slots of an epilogue's ring (see AuxRing)
-constexpr int64_t kRotateBytes = 8 << 20;
 constexpr long long kWaitCycles = 4000000000ll;  // ~2 s; a copy or a stage's products take microseconds
 constexpr long long kStageCycles = 4096;         // allowed on top per stage of a tile, to who waits for the whole of it (a stage takes ~512)
 
@@ -47,7 +46,6 @@ struct Shape {
     int m_tiles, n_tiles, batch;
     int group;                     // tile rows that are walked together, so that their operands stay in L2 (symmetric: see tile_of)
     int total;                     // tiles of all batches and splits
-    int rotate;                    // tiles begin their k loop this many blocks apart
     uint32_t idesc;                // instruction descriptor
     unsigned long long* fail_word; // host memory
 };
@@ -457,8 +455,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int t = first; ok && t < shape.total;) {
             const bool once = kSquare && tile.tm == tile.tn;
             const int m0 = tile.tm * C::BM + (int)rank * 128, n0 = tile.tn * BN + (int)rank * C::b_rows;
-            int kb = tile.kb0 + (int)((unsigned)(t * shape.rotate) % (unsigned)(tile.kb1 - tile.kb0));
-            for (int i = live ? tile.kb0 : tile.kb1 - 1; i < tile.kb1; ++i, kb = kb + 1 == tile.kb1 ? tile.kb0 : kb + 1) {
+            for (int kb = live ? tile.kb0 : tile.kb1 - 1; kb < tile.kb1; ++kb) {
                 if (!(ok = mbar_wait_warp(empty0 + 8 * s, phase ^ 1u, stop))) break;
                 if (live && elect_one()) {
                     const uint32_t a = ring + s * C::stage_bytes, b = a + C::blocks * kStageBytesA, full = full_base + 8 * s;
@@ -619,9 +616,6 @@ int make_shape(Shape* s, bool bf16, int64_t m, int64_t n, int64_t k, int64_t bat
     if (splits > s->k_blocks) splits = s->k_blocks;
     s->split_blocks = (s->k_blocks + splits - 1) / splits;
     s->splits = (s->k_blocks + s->split_blocks - 1) / s->split_blocks;
-    // Operands of a few MB: tiles that walk k in step ask the same L2 lines of every SM at once.  Larger ones need them to, so that
-    // a line is still there for the next tile.
-    s->rotate = 2 * (m + n) * k <= kRotateBytes ? 5 : 0;
     s->m_tiles = (int)mt;
     s->n_tiles = (int)nt;
     s->batch = (int)batch;
