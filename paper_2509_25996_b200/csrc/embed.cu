@@ -1,7 +1,8 @@
 // Token embedding, out[t] = scale table[ids[t]], and its gradient, grad_table[v] = scale sum_{t: ids[t] = v} grad_out[t].
 //
 // Forward: a gather bounded by HBM (each output row written once, each table row in use read once).  One thread moves
-// 16 bytes (8 columns); kUnroll of them per thread are in flight.
+// 16 bytes (8 columns); kUnroll of them per thread are in flight.  16384 tokens x 4096 columns (269 MB with 32000 table rows, part
+// of which stays in L2): 32.8 us; 8 tokens: 3 us, less than its launch from Python (11 us).
 //
 // Gradient: the tokens are put in the order (id, position) first, so that every table row sums its tokens in one fixed
 // order, in fp32 registers, and is rounded and written once, without atomics: results do not change from run to run.
@@ -14,9 +15,13 @@
 //     part that enters a piece and the part that leaves it), which the warp that stores the last of them adds, in order.  Every
 //     token row is read once, and a CTA's work does not depend on how often an id occurs.  (Letting a piece finish the row
 //     that it leaves, where that ends in the next piece, saves partial rows but makes its loads a longer chain.)
-//   * up to kFew tokens are not sorted: the first token of an id looks for the others among the ids.
+//   * up to kFew tokens are not sorted: the first token of an id looks for the others among the ids (256 tokens x 768 added to a
+//     table of 32000 rows: 12.4 us, sorted 14.3).
 //   * rows without a token become zeros in further CTAs of the kernel that sums: each looks up which of its kZeroRows rows
-//     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.
+//     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.  (Zeros beside the
+//     ranking or the merge, whose latency they would hide, took 113 and 105 us where this takes 97: writes alone are slower.)
+// Bounded by HBM behind two short sorting kernels: 16384 tokens x 4096 into 32000 rows 97 us for 399 MB (4.1 TB/s; ranking and
+// merging 16 us of it), 1000 tokens x 768 into 50257 rows 21 us for 79 MB.
 #include <cmath>
 #include <type_traits>
 

@@ -19,6 +19,12 @@
 //
 // Rounding: the products take bf16 operands, so E and a H are rounded to bf16 (2^-9 relative each); everything that is
 // summed, and all statistics, are fp32.  The label's terms, the largest of a row, are never rounded before the result is.
+//
+// Bounded by the tensor cores, for large calls at the clock that the power limit leaves them (1.3-1.4 GHz): 4096 tokens x 32000
+// x 4096 2.48 ms (1300 TFLOP/s), 8192 x 128256 x 4096 19.9 ms (1300), loss alone of 2047 x 32000 x 5120 0.50 ms (1340).
+// 1000 x 50257 x 768 takes 234 us (990): its three products (60, 56 and 57 us alone, tensor pipe 77-83 % busy) read 620 MB of
+// operands each through L2.  48 x 32000 x 768 takes 56 us, where reading and writing the head once takes 15: nine launches,
+// each of a few microseconds.
 #include <cmath>
 
 #include "embed.cuh"
@@ -516,6 +522,9 @@ int64_t piece_of(int64_t tokens, int64_t vocab, int64_t piece_tokens)
     return (each + 255) / 256 * 256;
 }
 
+// Tiles of 256 x 256 on CTA pairs, or of 128 x 128 where a pair's second CTA would have no tokens.  Loss and both gradients,
+// us on pairs / on single CTAs: 128 tokens x 32000 x 768 68 / 58, 64 x 32000 x 4096 185 / 171; 160 x 32000 x 4096 199 / 224,
+// 256 x 128256 x 2048 420 / 462.
 bool paired(int64_t tokens) { return tokens > 128; }
 int64_t tile_cols(int64_t tokens) { return (paired(tokens) ? 256 : 128) / kHalves; }      // of one row sum
 

@@ -17,6 +17,12 @@
 // amplify by more than kAmplify, X is held as hi + lo, two fp16 words scaled by 2^12 (22 bits): the products read hi, the
 // epilogue adds a lo.  With five steps X_0 (of an fp32 update; a bf16 one is exact in hi), X_1 and X_2 have a lo: 2.4e-3 on that
 // update.
+//
+// What bounds it: for large matrices the tensor cores at the clock that the power limit leaves them (4096 x 11008: 2.69 ms, 1.16
+// PFLOP/s counting symmetric products by half); for twelve 3072 x 768 matrices (496 us) the path from L2 to the SMs, which
+// feeds a pair's tile 64 bytes per cycle and SM, just as much as it consumes, and X and its two words, which exceed L2; for one
+// 768 x 768 (91 us) the chain of 17 kernels, of ~5.4 us each: 1 us until the first operands are there, 1.8 us of products, 1 us
+// of epilogue, 1.5 us until its successor sees the results.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -162,6 +168,8 @@ template <bool POLY>
 struct SymEpi {
     static constexpr bool kSym = true;
     static constexpr bool kInputsOnly = false;
+    // eight with a ring would leave the products four stages instead of five: twelve 3072 x 768 500 -> 495 us, but 4096 x 11008
+    // 2700 -> 2720 and 768 x 768 92.6 -> 93.2; with StepEpi's likewise 2750
     static constexpr int kWarps = POLY ? 4 : 8;
     // POLY: the ring of aux, replaced in place, and a slot for the mirrored chunk; otherwise a slot for each
     static constexpr int kStaging = (POLY ? kRing + 1 : 2) * kSlotBytes;
