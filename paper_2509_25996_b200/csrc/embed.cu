@@ -149,10 +149,12 @@ rank_runs_kernel(const int32_t* __restrict__ ids, const SortStart start, int64_t
     rank_keys(ids, start, tokens, vocab, blockIdx.x, gridDim.x);
 }
 
-constexpr int kMergeThreads = 128;
+constexpr int kMergeKeys = 128;                   // per CTA ...
+constexpr int kMergeShare = 4;                    // ... searched for by this many threads each
+constexpr int kMergeThreads = kMergeKeys * kMergeShare;
 
-// Merges groups of kWays runs of `run` keys.  The searches of a key advance together and without branches: kWays independent
-// loads per halving, from shared memory where a group fits (runs of kRun keys: 64 KB), from L2 where it does not.
+// Merges groups of kWays runs of `run` keys.  A thread's searches advance together and without branches: independent loads in
+// each halving, from shared memory where a group fits (runs of kRun keys: 64 KB), from L2 where it does not.
 template <bool SHARED>
 __global__ void __launch_bounds__(kMergeThreads)
 merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict__ order_in, int32_t* __restrict__ ids_out,
@@ -161,9 +163,11 @@ merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict_
     extern __shared__ int32_t group_ids[];
     chain_next();
     chain_wait();
-    const int32_t i = (int32_t)blockIdx.x * kMergeThreads + (int32_t)threadIdx.x;
+    const int share = (int)threadIdx.x % kMergeShare;
+    const int64_t place = (int64_t)blockIdx.x * kMergeKeys + (int)threadIdx.x / kMergeShare;
+    const int32_t i = (int32_t)min(place, (int64_t)tokens - 1), from = __ldg(order_in + i);
     const int64_t group = (int64_t)run * kWays;
-    const int32_t group0 = (int32_t)((int64_t)blockIdx.x * kMergeThreads / group * group);      // of the CTA: its keys are of one run
+    const int32_t group0 = (int32_t)((int64_t)blockIdx.x * kMergeKeys / group * group);      // of the CTA: its keys are of one run
     const int32_t left = tokens - group0;            // keys of the group, and of the groups after it
     const int32_t* keys = ids_in + group0;
     if constexpr (SHARED) {
@@ -174,29 +178,34 @@ merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict_
         __syncthreads();
         keys = group_ids;
     }
-    if (i >= tokens) return;
     const int own = (i - group0) / run;
     const uint32_t k = (uint32_t)keys[i - group0];
-    int32_t pos[kWays];
+    constexpr int kEach = kWays / kMergeShare;
+    int32_t pos[kEach];
 #pragma unroll
-    for (int j = 0; j < kWays; ++j) pos[j] = 0;
+    for (int j = 0; j < kEach; ++j) pos[j] = 0;
     for (int32_t half = run; half; half >>= 1) {
 #pragma unroll
-        for (int j = 0; j < kWays; ++j) {
-            const int64_t before = (int64_t)j * run;                 // keys of the group ahead of run j
-            if (before >= left) break;                               // no such run (the same for the whole CTA)
+        for (int j = 0; j < kEach; ++j) {
+            const int r = j * kMergeShare + share;
+            const int64_t before = (int64_t)r * run;                 // keys of the group ahead of run r
             const int32_t at = pos[j] + half;
             const bool there = at <= run && before + at <= left;
-            const uint32_t limit = j == own ? 0u : k + (j < own ? 1u : 0u);
+            const uint32_t limit = r == own ? 0u : k + (r < own ? 1u : 0u);
             const uint32_t other = (uint32_t)keys[there ? (int32_t)before + at - 1 : 0];
             pos[j] = there && other < limit ? at : pos[j];
         }
     }
-    int64_t to = (int64_t)group0 + (i - group0 - own * run);
+    int32_t ahead = 0;
 #pragma unroll
-    for (int j = 0; j < kWays; ++j) to += pos[j];
-    ids_out[to] = (int32_t)k;
-    order_out[to] = order_in[i];
+    for (int j = 0; j < kEach; ++j) ahead += pos[j];
+#pragma unroll
+    for (int d = 1; d < kMergeShare; d *= 2) ahead += __shfl_xor_sync(0xFFFFFFFFu, ahead, d);
+    if (share == 0 && place < tokens) {
+        const int32_t to = group0 + (i - group0 - own * run) + ahead;
+        ids_out[to] = (int32_t)k;
+        order_out[to] = from;
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ sums
@@ -577,7 +586,7 @@ int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, 
         return rc;
     int cur = 0;
     for (int64_t run = kRun; run < tokens; run *= kWays, cur ^= 1) {
-        const dim3 grid((unsigned)((tokens + kMergeThreads - 1) / kMergeThreads));
+        const dim3 grid((unsigned)((tokens + kMergeKeys - 1) / kMergeKeys));
         if (run == kRun) {
             constexpr size_t smem = sizeof(int32_t) * kRun * kWays;
             CAST_CUDA_TRY(cudaFuncSetAttribute(merge_runs_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
