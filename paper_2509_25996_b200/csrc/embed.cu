@@ -150,7 +150,7 @@ rank_runs_kernel(const int32_t* __restrict__ ids, const SortStart start, int64_t
 }
 
 constexpr int kMergeKeys = 128;                   // per CTA ...
-constexpr int kMergeShare = 4;                    // ... searched for by this many threads each
+constexpr int kMergeShare = 8;                    // ... searched for by this many threads each
 constexpr int kMergeThreads = kMergeKeys * kMergeShare;
 
 // Merges groups of kWays runs of `run` keys.  A thread's searches advance together and without branches: independent loads in
