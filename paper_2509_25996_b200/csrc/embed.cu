@@ -19,9 +19,9 @@
 //     table of 32000 rows: 12.4 us, sorted 14.3).
 //   * rows without a token become zeros in further CTAs of the kernel that sums: each looks up which of its kZeroRows rows
 //     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.  (Zeros beside the
-//     ranking or the merge, whose latency they would hide, took 113 and 105 us where this takes 97: writes alone are slower.)
-// Bounded by HBM behind two short sorting kernels: 16384 tokens x 4096 into 32000 rows 97 us for 399 MB (4.1 TB/s; ranking and
-// merging 16 us of it), 1000 tokens x 768 into 50257 rows 21 us for 79 MB.
+//     ranking or the merge, whose latency they would hide, took 113 and 105 us where this took 97: writes alone are slower.)
+// Bounded by HBM behind two short sorting kernels: 16384 tokens x 4096 into 32000 rows 91.5 us for 399 MB (4.3 TB/s; ranking and
+// merging 13 us of it), 1000 tokens x 768 into 50257 rows 21 us for 79 MB.
 #include <cmath>
 #include <type_traits>
 
