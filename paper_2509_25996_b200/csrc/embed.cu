@@ -477,6 +477,7 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
     ids[threadIdx.x] = (int)threadIdx.x < a.tokens ? (uint32_t)__ldg(a.ids + threadIdx.x) : 0xFFFFFFFFu;
     __syncthreads();
     if (blockIdx.x >= a.own) {           // a block of rows: zeros where no token is (only in a call of its own)
+        chain_wait();
         const int64_t row0 = (int64_t)(blockIdx.x - a.own) * kZeroRows;
         const int64_t id = (int64_t)ids[threadIdx.x] - row0;
         if (ids[threadIdx.x] < vocab && id >= 0 && id < kZeroRows) atomicOr(&held, 1u << (int)id);
@@ -487,7 +488,12 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
     const int32_t t = (int32_t)(blockIdx.x / a.columns) * (kScatterThreads / a.lanes) + (int)threadIdx.x / a.lanes;      // one token per warp
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const uint32_t id = t < a.tokens ? ids[t] : 0xFFFFFFFFu;
-    if (id >= vocab) return;
+    // Every thread waits for the predecessor, those without a row to add too: what follows the call waits for this grid alone, and a
+    // grid of which no thread had waited (no token has an id) could end before its predecessor.
+    if (id >= vocab) {
+        chain_wait();
+        return;
+    }
     int count = 0;
 #pragma unroll
     for (int k = 0; k < kFew / 32; ++k) {
@@ -499,8 +505,8 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
     __syncwarp();
     const bool first = same[warp][0] == t;
     const int32_t col = column_of<VEC>(a);
-    if (!first || col >= a.dim) return;
     chain_wait();
+    if (!first || col >= a.dim) return;
     uint16_t* to = a.dest + (int64_t)id * a.dim + col;
     typename Cols<VEC>::Raw old = {};
     if (a.accumulate) old = Cols<VEC>::load_own(to);

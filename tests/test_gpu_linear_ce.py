@@ -303,3 +303,35 @@ def test_a_counted_failure_stops_further_calls():
     finally:
         assert cast.cast_product_failures(2) == (0, 1)
     assert all(torch.equal(a, b) for a, b in zip(want, ops.linear_ce(h, w, y)))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_work_behind_a_call_without_any_label(captured):
+    """A copy of grad_weight on the same stream, directly behind a call none of whose tokens has a label, sees the finished
+    product: zeros everywhere.  (200 tokens into 100000 x 2048: the product stores 410 MB.)"""
+    tokens, vocab, dim = 200, 100000, 2048
+    h, w, y = draw(tokens, vocab, dim, 41)
+    y.fill_(-1)
+    gw = torch.empty_like(w)
+    seen = torch.empty_like(w)
+    loss = torch.empty(tokens, device=DEV)
+    need = cast.cast_linear_ce_workspace(tokens, vocab, dim, 0, False, True)[1]
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+
+    def enqueue():
+        gw.fill_(7.0)
+        cast.check(cast.cast_linear_ce(h, w, y, loss, None, gw, tokens, vocab, dim, 1.0, 0, ws, need, torch.cuda.current_stream()))
+        seen.copy_(gw)
+    if captured:
+        run(h[:2], w[:4], y[:2], 1.0)              # what a first call allocates
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            enqueue()
+    for _ in range(5):
+        seen.fill_(3.0)
+        if captured:
+            graph.replay()
+        else:
+            enqueue()
+        torch.cuda.synchronize()
+        assert not seen.any() and not loss.any()
