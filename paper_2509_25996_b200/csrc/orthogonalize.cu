@@ -462,7 +462,9 @@ struct ResultEpi {
 #pragma unroll 1
         for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
-            __syncwarp();          // the chunk before this one has been read
+            // the chunk before this one has been read; its slot, which ordinary stores have written, is the one that is loaded next
+            if constexpr (LO_IN) fence_async_smem();
+            __syncwarp();
             uint32_t slot = e.slots;
             if constexpr (LO_IN) {
                 ring.load<BM, BN, false>(s, e, &map_lo_in);

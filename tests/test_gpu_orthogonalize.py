@@ -206,3 +206,18 @@ def test_refusals():
         ops.orthogonalize(u, coeffs=(1.0, 2.0))
     with pytest.raises(ValueError, match="not contiguous"):
         ops.orthogonalize([x.t() for x in u])
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 2048, 8192), (1, 8192, 2048), (3, 1500, 4100)])
+def test_one_step_over_several_chunks(n, rows, cols):
+    """A last step that still reads the second word, with more chunks per warp than its ring has slots and several tiles per
+    CTA: every slot is written, read and loaded again."""
+    u = draw(n, rows, cols, 21)
+    out = ops.orthogonalize(u, steps=1)
+    for x, o in zip(u, out):
+        want = exact(x, QUINTIC, 1)
+        assert distance(o, want) <= tolerance(1)
+        # chunk by chunk, so that a wrong one is not averaged away; a chunk of 32 x 64 entries averages signs as well
+        err = (o.double() - want).abs()
+        assert float(err.max()) <= 4 * tolerance(1) * float(want.abs().max())
+    assert all(torch.equal(a, b) for a, b in zip(out, ops.orthogonalize(u, steps=1)))
