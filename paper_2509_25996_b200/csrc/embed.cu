@@ -212,21 +212,39 @@ merge_runs_kernel(const int32_t* __restrict__ ids_in, const int32_t* __restrict_
 
 constexpr int kScatterThreads = 256;
 
+// What becomes of a sum: a bf16 row of the table, written or added to, or an fp32 row of its own (gather_rows).
+enum class Into { kTable, kAdded, kRows };
+
 struct ScatterArgs {
     const uint16_t* src;
-    const float* coef;            // per token, or nullptr
+    const float* coef;            // per token (kRows)
     const int32_t* ids;           // sorted
     const int32_t* order;
     float* partial;               // [pieces][2][dim]: what enters a piece, what leaves it
     uint32_t* arrivals;           // [2 pieces + groups][warp columns], zero
-    uint16_t* dest;
+    uint16_t* dest;               // kTable, kAdded
+    float* rows;                  // kRows
+    int32_t* row_of;
     int64_t dim, vocab;
     int32_t tokens, pieces;
     unsigned own, columns;        // CTAs that sum: own / columns for the tokens x columns; the ones after them write zeros
     float scale;
     int lanes;                    // threads per row: 32 .. 256, a power of two
-    int accumulate;
 };
+
+// A finished sum.  `place`: a sorted position (of few tokens, a token) that is this id's alone, by which its row of kRows goes where
+// there are fewer tokens than ids.
+template <int VEC, Into INTO>
+__device__ __forceinline__ void store_sum(const ScatterArgs& a, const Cols<VEC>& acc, int32_t id, int32_t place, int32_t col, const typename Cols<VEC>::Raw& old)
+{
+    if constexpr (INTO == Into::kRows) {
+        const int32_t row = a.tokens > a.vocab ? id : place;
+        acc.store_partial(a.rows + (int64_t)row * a.dim + col);
+        if (col == 0) a.row_of[id] = row;
+    } else {
+        acc.store(a.dest + (int64_t)id * a.dim + col, a.scale, INTO == Into::kAdded, old);
+    }
+}
 
 // Column of this thread: a.lanes threads per row, the rest of a long row in the CTAs beside it.
 template <int VEC>
@@ -342,7 +360,7 @@ __device__ __forceinline__ void add_partials(Cols<VEC>& acc, const float* p, int
 }
 
 // `crossed`: of the row with this id, bit j for the start of piece kGroup group + j, j <= kGroup.  A whole warp; `in`: this lane has columns.
-template <int VEC>
+template <int VEC, Into INTO>
 __device__ __forceinline__ void join_row(const ScatterArgs& a, int32_t id, uint32_t crossed, int32_t group, int32_t col, int32_t warp_col, int32_t warp_cols, bool in)
 {
     const int lane = (int)threadIdx.x & 31;
@@ -351,6 +369,7 @@ __device__ __forceinline__ void join_row(const ScatterArgs& a, int32_t id, uint3
     const int32_t entered = __popc(crossed & ((1u << kGroup) - 1u));            // pieces of the group that it enters
     const int64_t row0 = begins ? 2 * (int64_t)(piece0 + low - 1) + 1 : 2 * (int64_t)piece0;      // its first partial row in the group
     if (!arrive_last(a.arrivals + row0 * warp_cols + warp_col, entered + (begins ? 1 : 0))) return;
+    int32_t place = (piece0 + low) * kPiece;                                     // where it enters a piece for the first time
     Cols<VEC> acc;
     acc.zero();
     if (in) {
@@ -375,6 +394,7 @@ __device__ __forceinline__ void join_row(const ScatterArgs& a, int32_t id, uint3
         // only one row goes on from a group to the next
         if (!arrive_last(a.arrivals + (2 * (int64_t)a.pieces + head) * warp_cols + warp_col, tail - head + 1)) return;
         const uint32_t starts = __ballot_sync(0xFFFFFFFFu, lane <= kGroup && crossing(a, (int64_t)head * kGroup + lane) == id);
+        place = (head * kGroup + __ffs((int)starts) - 1) * kPiece;
         acc.zero();
         if (in) {
             acc.add_partial(a.partial + (2 * (int64_t)(head * kGroup + __ffs((int)starts) - 2) + 1) * a.dim + col);
@@ -382,22 +402,22 @@ __device__ __forceinline__ void join_row(const ScatterArgs& a, int32_t id, uint3
         }
     }
     if (!in) return;
-    uint16_t* dest = a.dest + (int64_t)id * a.dim + col;
     typename Cols<VEC>::Raw old = {};
-    if (a.accumulate) old = Cols<VEC>::load_own(dest);
-    acc.store(dest, a.scale, a.accumulate, old);
+    if constexpr (INTO == Into::kAdded) old = Cols<VEC>::load_own(a.dest + (int64_t)id * a.dim + col);
+    store_sum<VEC, INTO>(a, acc, id, place, col, old);
 }
 
-// One piece of kPiece sorted tokens per group of a.lanes threads.  ACC: table rows are added to; what is there is asked for
-// together with the token rows, which would otherwise be one dependent load after the other.
-template <int VEC, bool COEF, bool ACC>
-__global__ void __launch_bounds__(kScatterThreads, ACC ? 2 : 3)
+// One piece of kPiece sorted tokens per group of a.lanes threads.  kAdded: what is there is asked for together with the token
+// rows, which would otherwise be one dependent load after the other.
+template <int VEC, Into INTO>
+__global__ void __launch_bounds__(kScatterThreads, INTO == Into::kTable ? 3 : 2)
 piece_sums_kernel(const __grid_constant__ ScatterArgs a)
 {
     constexpr int kBatch = 8;             // token rows asked for at a time
+    constexpr bool COEF = INTO == Into::kRows, ACC = INTO == Into::kAdded;
     chain_next();
     chain_wait();
-    if constexpr (!ACC) {
+    if constexpr (INTO == Into::kTable) {
         if (blockIdx.x >= a.own) {
             zero_block<VEC>(a);
             return;
@@ -446,7 +466,7 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
             const uint32_t own = id[b + i + 1];
             if (id[b + i + 2] != own) {                    // its last token
                 if (entered) acc.store_partial(partial);
-                else acc.store(a.dest + (int64_t)own * a.dim + col, a.scale, ACC, old[ACC ? i : 0]);
+                else store_sum<VEC, INTO>(a, acc, (int32_t)own, p0 + b + i, col, old[ACC ? i : 0]);
                 entered = false;
                 acc.zero();
             } else if (b + i == kPiece - 1) {              // goes on in the next piece
@@ -456,15 +476,15 @@ piece_sums_kernel(const __grid_constant__ ScatterArgs a)
     }
     const bool enters = id[0] == id[1] && id[1] != kNoId, leaves = id[kPiece] == id[kPiece + 1] && id[kPiece] < kNoId;
     const int32_t warp_col = col / (32 * VEC), warp_cols = (int32_t)a.columns * (a.lanes / 32);
-    if (enters) join_row<VEC>(a, (int32_t)id[1], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[1]), group, col, warp_col, warp_cols, in);
+    if (enters) join_row<VEC, INTO>(a, (int32_t)id[1], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[1]), group, col, warp_col, warp_cols, in);
     if (leaves && !(enters && id[kPiece] == id[1]))
-        join_row<VEC>(a, (int32_t)id[kPiece], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[kPiece]), group, col, warp_col, warp_cols, in);
+        join_row<VEC, INTO>(a, (int32_t)id[kPiece], __ballot_sync(0xFFFFFFFFu, crosses == (int32_t)id[kPiece]), group, col, warp_col, warp_cols, in);
 }
 
 // Few tokens need no order: the threads that hold an id's first token list the others by warp votes over all ids.
 constexpr int kFew = 256;
 
-template <int VEC, bool COEF>
+template <int VEC, Into INTO>
 __global__ void __launch_bounds__(kScatterThreads)
 few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      // a.ids: as the caller gave them
 {
@@ -476,7 +496,7 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
     if (threadIdx.x == 0) held = 0;
     ids[threadIdx.x] = (int)threadIdx.x < a.tokens ? (uint32_t)__ldg(a.ids + threadIdx.x) : 0xFFFFFFFFu;
     __syncthreads();
-    if (blockIdx.x >= a.own) {           // a block of rows: zeros where no token is (only in a call of its own)
+    if (blockIdx.x >= a.own) {           // a block of rows: zeros where no token is (kTable)
         chain_wait();
         const int64_t row0 = (int64_t)(blockIdx.x - a.own) * kZeroRows;
         const int64_t id = (int64_t)ids[threadIdx.x] - row0;
@@ -507,9 +527,8 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
     const int32_t col = column_of<VEC>(a);
     chain_wait();
     if (!first || col >= a.dim) return;
-    uint16_t* to = a.dest + (int64_t)id * a.dim + col;
     typename Cols<VEC>::Raw old = {};
-    if (a.accumulate) old = Cols<VEC>::load_own(to);
+    if constexpr (INTO == Into::kAdded) old = Cols<VEC>::load_own(a.dest + (int64_t)id * a.dim + col);
     Cols<VEC> acc;
     acc.zero();
     for (int32_t i0 = 0; i0 < count; i0 += 4) {
@@ -521,27 +540,45 @@ few_tokens_kernel(const __grid_constant__ ScatterArgs a, uint32_t vocab)      //
             if (i0 + i < count) {
                 const int32_t token = same[warp][i0 + i];
                 x[i] = Cols<VEC>::load(a.src + (int64_t)token * a.dim + col);
-                if constexpr (COEF) c[i] = __ldg(a.coef + token);
+                if constexpr (INTO == Into::kRows) c[i] = __ldg(a.coef + token);
             }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (i0 + i < count) acc.add(x[i], c[i]);
     }
-    acc.store(to, a.scale, a.accumulate, old);
+    store_sum<VEC, INTO>(a, acc, (int32_t)id, t, col, old);
 }
 
-template <int VEC, bool COEF>
+template <int VEC, Into INTO>
 int launch_scatter(ScatterArgs a, const SortedTokens& sorted, cudaStream_t stream)
 {
-    const int64_t units = (a.dim + VEC - 1) / VEC, groups = kScatterThreads / a.lanes, items = sorted.few ? a.tokens : a.pieces;
+    const int64_t units = (a.dim + VEC - 1) / VEC;
+    a.lanes = 32;
+    while (a.lanes < kScatterThreads && a.lanes < units) a.lanes *= 2;
+    const int64_t groups = kScatterThreads / a.lanes, items = sorted.few ? a.tokens : a.pieces;
     a.columns = (unsigned)((units + a.lanes - 1) / a.lanes);
     a.own = (unsigned)((items + groups - 1) / groups) * a.columns;
-    const unsigned zeros = a.accumulate ? 0u : (unsigned)((a.vocab + kZeroRows - 1) / kZeroRows);
+    const unsigned zeros = INTO == Into::kTable ? (unsigned)((a.vocab + kZeroRows - 1) / kZeroRows) : 0u;
     const dim3 grid(a.own + zeros);
-    if (sorted.few) return launch_chained(sorted.first, few_tokens_kernel<VEC, COEF>, grid, kScatterThreads, 0, stream, 1, a, (uint32_t)a.vocab);
-    return a.accumulate ? launch_chained(false, piece_sums_kernel<VEC, COEF, true>, grid, kScatterThreads, 0, stream, 1, a)
-                        : launch_chained(false, piece_sums_kernel<VEC, COEF, false>, grid, kScatterThreads, 0, stream, 1, a);
+    if (sorted.few) return launch_chained(sorted.first, few_tokens_kernel<VEC, INTO>, grid, kScatterThreads, 0, stream, 1, a, (uint32_t)a.vocab);
+    return launch_chained(false, piece_sums_kernel<VEC, INTO>, grid, kScatterThreads, 0, stream, 1, a);
+}
+
+ScatterArgs scatter_args(const SortedTokens& sorted, const uint16_t* src, int64_t vocab, int64_t dim)
+{
+    ScatterArgs a = {};
+    a.src = src;
+    a.ids = sorted.ids;
+    a.order = sorted.order;
+    a.partial = sorted.partial;
+    a.arrivals = sorted.arrivals;
+    a.tokens = (int32_t)sorted.tokens;
+    a.pieces = (int32_t)((sorted.tokens + kPiece - 1) / kPiece);
+    a.dim = dim;
+    a.vocab = vocab;
+    a.scale = 1.0f;
+    return a;
 }
 
 int64_t sort_array_bytes(int64_t tokens) { return (int64_t)align256(4ull * (uint64_t)tokens); }
@@ -611,30 +648,25 @@ int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, 
     return CAST_OK;
 }
 
-int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t vocab, int64_t dim,
-                 bool accumulate, cudaStream_t stream)
+int scatter_rows(const SortedTokens& sorted, const uint16_t* src, float scale, uint16_t* dest, int64_t vocab, int64_t dim, bool accumulate,
+                 cudaStream_t stream)
 {
-    ScatterArgs a;
-    a.src = src;
-    a.coef = coef;
-    a.ids = sorted.ids;
-    a.order = sorted.order;
-    a.partial = sorted.partial;
-    a.arrivals = sorted.arrivals;
+    ScatterArgs a = scatter_args(sorted, src, vocab, dim);
     a.dest = dest;
-    a.tokens = (int32_t)sorted.tokens;
-    a.pieces = (int32_t)pieces_of(sorted.tokens);
-    a.dim = dim;
-    a.vocab = vocab;
-    a.own = a.columns = 0;
     a.scale = scale;
-    a.accumulate = accumulate;
     const bool vec = dim % 8 == 0 && !((uintptr_t)src & 15u) && !((uintptr_t)dest & 15u);
-    const int64_t units = vec ? dim / 8 : dim;
-    a.lanes = 32;
-    while (a.lanes < kScatterThreads && a.lanes < units) a.lanes *= 2;
-    if (vec) return coef ? launch_scatter<8, true>(a, sorted, stream) : launch_scatter<8, false>(a, sorted, stream);
-    return coef ? launch_scatter<1, true>(a, sorted, stream) : launch_scatter<1, false>(a, sorted, stream);
+    if (vec) return accumulate ? launch_scatter<8, Into::kAdded>(a, sorted, stream) : launch_scatter<8, Into::kTable>(a, sorted, stream);
+    return accumulate ? launch_scatter<1, Into::kAdded>(a, sorted, stream) : launch_scatter<1, Into::kTable>(a, sorted, stream);
+}
+
+int gather_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float* rows, int32_t* row_of, int64_t vocab, int64_t dim,
+                cudaStream_t stream)
+{
+    ScatterArgs a = scatter_args(sorted, src, vocab, dim);
+    a.coef = coef;
+    a.rows = rows;
+    a.row_of = row_of;
+    return launch_scatter<8, Into::kRows>(a, sorted, stream);
 }
 
 }  // namespace cast
@@ -705,5 +737,5 @@ extern "C" int cast_embed_grad(const cast_bf16* grad_out, const int32_t* ids, ca
     if ((rc = check_device_memory(ptrs, 4)) != CAST_OK) return rc;
     SortedTokens sorted;
     if ((rc = sort_tokens(false, ids, tokens, vocab, dim, workspace, &sorted, (cudaStream_t)stream)) != CAST_OK) return rc;
-    return scatter_rows(sorted, grad_out, nullptr, scale, grad_table, vocab, dim, accumulate != 0, (cudaStream_t)stream);
+    return scatter_rows(sorted, grad_out, scale, grad_table, vocab, dim, accumulate != 0, (cudaStream_t)stream);
 }

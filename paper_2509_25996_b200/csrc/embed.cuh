@@ -33,10 +33,17 @@ SortStart sort_start(void* scratch, int64_t tokens, int64_t dim);
 int rank_blocks(int64_t tokens);
 int sort_tokens(bool ranked, const int32_t* ids, int64_t tokens, int64_t vocab, int64_t dim, void* scratch, SortedTokens* sorted, cudaStream_t stream);
 
-// dest[v] = scale * sum_{t: id = v} coef[t] src[t] (coef NULL: 1).  accumulate: added to dest, whose rows without a token are left
-// alone; otherwise those become zero.
-int scatter_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float scale, uint16_t* dest, int64_t vocab, int64_t dim,
-                 bool accumulate, cudaStream_t stream);
+// dest[v] = scale * sum_{t: id = v} src[t].  accumulate: added to dest, whose rows without a token are left alone; otherwise those
+// become zero.
+int scatter_rows(const SortedTokens& sorted, const uint16_t* src, float scale, uint16_t* dest, int64_t vocab, int64_t dim, bool accumulate,
+                 cudaStream_t stream);
+
+// The same sums as fp32 rows of their own, for a product's epilogue to add before its rounding: rows[row_of[v]] = sum_{t: id = v}
+// coef[t] src[t].  `row_of` has an entry for every v, negative where no token has the id: the caller fills it before, the entries
+// of ids in use are set here.  `rows` holds compact_rows() rows.  dim % 8 == 0, all aligned to 16 bytes.
+inline int64_t compact_rows(int64_t tokens, int64_t vocab) { return tokens < vocab ? tokens : vocab; }
+int gather_rows(const SortedTokens& sorted, const uint16_t* src, const float* coef, float* rows, int32_t* row_of, int64_t vocab, int64_t dim,
+                cudaStream_t stream);
 
 // Address ranges [a, a + na) and [b, b + nb) share a byte.
 inline bool ranges_overlap(const void* a, uint64_t na, const void* b, uint64_t nb)

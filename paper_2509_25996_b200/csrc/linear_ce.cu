@@ -7,9 +7,9 @@
 //     target logits   r_i, one warp per token
 //     E = exp(H W^T - r)            product, epilogue writes E (bf16) and the row sums of half a tile each
 //     finish          S, loss, a_i = s / (1 + S_i), b_i = s S_i / (1 + S_i), and a H as bf16
+//     B_v = sum_{label = v} b H     fp32 rows by label (the embedding gradient's sums), before the last piece's dW
 //     dH = a (E W) - b W_label      product over the vocabulary; the label's row is added in fp32 by the epilogue
-//     dW = E^T (a H)                product over the tokens
-//     dW_label -= b H               rows of the piece in label order (the embedding gradient's sums), added in fp32
+//     dW = E^T (a H) - B            product over the tokens; B is subtracted in fp32 by the epilogue
 // The two backward products read E as it was written: no pass over it to apply the normaliser.
 //
 // E is the only large intermediate, 2 bytes per logit of a piece.  Several pieces accumulate dW in fp32.
@@ -18,7 +18,9 @@
 // sum; finish then brings the row to one reference.
 //
 // Rounding: the products take bf16 operands, so E and a H are rounded to bf16 (2^-9 relative each); everything that is
-// summed, and all statistics, are fp32.  The label's terms, the largest of a row, are never rounded before the result is.
+// summed, and all statistics, are fp32.  The label's terms, the largest of a row, are never rounded before the result is: the two
+// parts of a frequent label's row of dW nearly cancel where the head is calibrated and the hidden states have a common mean, so
+// that a rounding of one of them would be up to 30 of the result's.
 //
 // Bounded by the tensor cores, for large calls at the clock that the power limit leaves them (1.3-1.4 GHz): 4096 tokens x 32000
 // x 4096 2.48 ms (1300 TFLOP/s), 8192 x 128256 x 4096 19.9 ms (1300), loss alone of 2047 x 32000 x 5120 0.50 ms (1340).
@@ -54,15 +56,21 @@ __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0
 
 // ------------------------------------------------------------------------------------------------ target logits
 
-// refs[t] = h_t . w_label, 0 without a label.  One warp per token; dim % 8 == 0.  The CTAs after the tokens' own begin the order of
-// the labels, which dW's label terms need.
+// refs[t] = h_t . w_label, 0 without a label.  One warp per token; dim % 8 == 0.  For dW's label terms, the CTAs after the tokens' own
+// begin the order of the labels, and those after them (from `fill0` on) write -1 to `row_of`, the row in B of every label.
 __global__ void __launch_bounds__(kRankThreads)
 target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restrict__ weight, const int32_t* __restrict__ labels,
-                    float* __restrict__ refs, int64_t tokens, int vocab, int dim, unsigned own, const SortStart start)
+                    float* __restrict__ refs, int64_t tokens, int vocab, int dim, unsigned own, unsigned fill0, const SortStart start,
+                    int4* __restrict__ row_of)
 {
     chain_next();
+    if (blockIdx.x >= fill0) {
+        const int64_t v = (int64_t)(blockIdx.x - fill0) * kRankThreads + threadIdx.x;
+        if (4 * v < vocab) row_of[v] = make_int4(-1, -1, -1, -1);        // padded to whole vectors
+        return;
+    }
     if (blockIdx.x >= own) {
-        rank_keys(labels, start, tokens, (uint32_t)vocab, blockIdx.x - own, gridDim.x - own);
+        rank_keys(labels, start, tokens, (uint32_t)vocab, blockIdx.x - own, fill0 - own);
         return;
     }
     const int64_t t = (int64_t)blockIdx.x * (kRankThreads / 32) + (threadIdx.x >> 5);
@@ -451,11 +459,13 @@ join_hidden_grad_kernel(const float* __restrict__ partial, const float* __restri
     *reinterpret_cast<uint4*>(out + t * dim + c) = r;
 }
 
-// dW tile: bf16 result after the last piece, fp32 running sums before it.
+// dW tile: bf16 result after the last piece, less the label's rows; fp32 running sums before it.
 struct WeightGradEpi : StoringEpi {
     CUtensorMap map_out;         // bf16 [vocab][dim]
     CUtensorMap map_acc;         // fp32 [vocab][dim]
     const float* acc;
+    const float* rows;           // B, and the row of it that belongs to a label
+    const int32_t* row_of;
     int add, last;
 
     __device__ __forceinline__ void add_running(const Shape& s, int row, int n1, float (&v)[32]) const
@@ -477,14 +487,29 @@ struct WeightGradEpi : StoringEpi {
     {
         const int row = e.row0 + e.lane;
         if (last) {
+            const int own = row < s.m ? __ldg(row_of + row) : -1;
+            const float* b = rows + (int64_t)(own < 0 ? 0 : own) * s.n;
+            // most tiles of a short call have none (without the branch 48 tokens x 32000 x 768 take 2 us longer)
+            const bool labels = __any_sync(0xFFFFFFFFu, own >= 0);
 #pragma unroll 1
             for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
                 const uint32_t slot = slot_acquire(e);
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
+                    const int n1 = e.col0 + c + 32 * h;
                     float v[32];
                     tmem_load32(e.acc + (uint32_t)(c + 32 * h), v);
-                    if (add) add_running(s, row, e.col0 + c + 32 * h, v);
+                    if (add) add_running(s, row, n1, v);
+                    if (labels) {
+                        float4 x[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            x[q] = own >= 0 && n1 + 4 * q < s.n ? __ldg(reinterpret_cast<const float4*>(b + n1) + q) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            v[4 * q] -= x[q].x; v[4 * q + 1] -= x[q].y; v[4 * q + 2] -= x[q].z; v[4 * q + 3] -= x[q].w;
+                        }
+                    }
                     store_bf16_row(slot, e.lane, h, v);
                 }
                 slot_store(e, slot, &map_out, e.col0 + c, e.row0, 0, e.row0 < s.m);
@@ -557,7 +582,7 @@ int hidden_splits(int64_t tokens, int64_t vocab, int64_t dim, int sms)
 struct Layout {
     int64_t piece, pieces, e_ld, n_tiles;
     int splits;
-    uint64_t e, scaled, refs, a, b, sums, tops, partial, acc, scatter, total;
+    uint64_t e, scaled, refs, a, b, sums, tops, partial, acc, scatter, rows, row_of, total;
 };
 
 int layout_of(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece_tokens, bool want_h, bool want_w, int sms, Layout* l)
@@ -588,6 +613,8 @@ int layout_of(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece_tokens, 
     l->partial = take(p1 > p2 ? p1 : p2);
     l->acc = take(want_w && l->pieces > 1 ? 4ull * (uint64_t)vocab * D : 0);
     l->scatter = take(want_w ? scatter_scratch_bytes(tokens, dim) : 0);
+    l->rows = take(want_w ? 4ull * (uint64_t)compact_rows(tokens, vocab) * D : 0);
+    l->row_of = take(want_w ? 4ull * (uint64_t)vocab : 0);
     l->total = at;
     return CAST_OK;
 }
@@ -679,6 +706,8 @@ int weight_product(const Call& c, int64_t n, bool first, bool last)
     if ((rc = operand_map<true>(&ma, c.ws + l.e, c.vocab, n, 1, l.e_ld, 0, 128)) != CAST_OK) return rc;
     if ((rc = operand_map<true>(&mb, c.ws + l.scaled, c.dim, n, 1, c.dim, 0, BN / CG)) != CAST_OK) return rc;
     epi.acc = reinterpret_cast<const float*>(c.ws + l.acc);
+    epi.rows = reinterpret_cast<const float*>(c.ws + l.rows);
+    epi.row_of = reinterpret_cast<const int32_t*>(c.ws + l.row_of);
     epi.add = !first;
     epi.last = last;
     if ((rc = make_map(&epi.map_out, c.grad_weight, 2, c.dim, c.vocab, 1, c.dim, 0, 64, 32, true)) != CAST_OK) return rc;
@@ -742,8 +771,11 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
     float* b = reinterpret_cast<float*>(ws + l.b);
     const unsigned own = (unsigned)((tokens + kRankThreads / 32 - 1) / (kRankThreads / 32));
     const SortStart start = sort_start(ws + l.scatter, tokens, dim);
-    if ((rc = launch_chained(true, target_logit_kernel, dim3(own + (grad_weight ? (unsigned)rank_blocks(tokens) : 0u)), kRankThreads, 0, st, 1, hidden,
-                             weight, labels, refs, tokens, (int)vocab, (int)dim, own, start)) != CAST_OK)
+    const unsigned fill0 = own + (grad_weight ? (unsigned)rank_blocks(tokens) : 0u);
+    const unsigned fills = grad_weight ? (unsigned)((vocab + 4 * kRankThreads - 1) / (4 * kRankThreads)) : 0u;
+    int32_t* row_of = reinterpret_cast<int32_t*>(ws + l.row_of);
+    if ((rc = launch_chained(true, target_logit_kernel, dim3(fill0 + fills), kRankThreads, 0, st, 1, hidden, weight, labels, refs, tokens, (int)vocab,
+                             (int)dim, own, fill0, start, reinterpret_cast<int4*>(row_of))) != CAST_OK)
         return rc;
     SortedTokens sorted;      // the merges now, while the ids are in L2, not after the products have swept it
     if (grad_weight && (rc = sort_tokens(true, labels, tokens, vocab, dim, ws + l.scatter, &sorted, st)) != CAST_OK) return rc;
@@ -775,11 +807,11 @@ extern "C" int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, 
             rc = paired(n) ? hidden_product<2, 256>(c, t0, n) : hidden_product<1, 128>(c, t0, n);
             if (rc != CAST_OK) return rc;
         }
-        if (grad_weight && (rc = weight_product(c, n, i == 0, i + 1 == l.pieces)) != CAST_OK) return rc;
-    }
-    if (grad_weight) {
         // b holds s S / (1 + S): the label's term of dW is -b H
-        if ((rc = scatter_rows(sorted, hidden, b, -1.0f, grad_weight, vocab, dim, true, st)) != CAST_OK) return rc;
+        if (grad_weight && i + 1 == l.pieces &&
+            (rc = gather_rows(sorted, hidden, b, reinterpret_cast<float*>(ws + l.rows), row_of, vocab, dim, st)) != CAST_OK)
+            return rc;
+        if (grad_weight && (rc = weight_product(c, n, i == 0, i + 1 == l.pieces)) != CAST_OK) return rc;
     }
     return CAST_OK;
 }

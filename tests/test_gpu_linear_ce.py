@@ -335,3 +335,29 @@ def test_work_behind_a_call_without_any_label(captured):
             enqueue()
         torch.cuda.synchronize()
         assert not seen.any() and not loss.any()
+
+
+@pytest.mark.parametrize("tokens,vocab,dim,piece", [(4096, 512, 256, 0), (200, 300, 256, 0), (700, 3000, 136, 300), (3000, 40, 64, 0), (900, 70, 72, 400)])
+@pytest.mark.parametrize("mean", [0.5, 1.0])
+def test_rows_whose_terms_cancel(tokens, vocab, dim, piece, mean):
+    """A calibrated head: labels drawn from the model's own probabilities, hidden states with a common mean, one label that is
+    frequent.  The two parts of its row of dW nearly cancel, so neither may be rounded before their difference is.  Per row j, in norm:
+    the result's rounding, 2^-8 |exact|; the operands' (two of at most 2^-8, independent from token to token, six deviations:
+    6 sqrt(2/3) < 5), 5 2^-8 sqrt(sum p_ij^2 |h_i|^2); and the relative error eps_i of the probabilities."""
+    g = torch.Generator(device=DEV).manual_seed(tokens + dim)
+    mu = torch.randn(dim, generator=g, device=DEV) * mean
+    w = torch.randn((vocab, dim), generator=g, device=DEV) * 0.02
+    w[7] += 6.0 * mu / mu.square().sum()
+    w = w.to(torch.bfloat16)
+    h = (torch.randn((tokens, dim), generator=g, device=DEV) + mu).to(torch.bfloat16)
+    p = torch.softmax(h.double() @ w.double().T, 1)
+    u = torch.rand((tokens, 1), generator=g, device=DEV).double()
+    y = (p.cumsum(1) < u).sum(1).clamp(max=vocab - 1).int()
+    _, _, gw = check(h, w, y, 1.0, "calibrated head", piece=piece)
+    (_, eps), _, (want, _) = exact(h, w, y, 1.0)
+    size = h.double().norm(dim=1)
+    hot = torch.nn.functional.one_hot(y.long(), vocab).double()
+    q = p * (1 - hot)
+    bound = 2.0 ** -8 * want.norm(dim=1) + 5 * 2.0 ** -8 * (q.square().T @ size.square()).sqrt() + (q + (1 - p) * hot).T @ ((eps + 2.0 ** -22) * size)
+    err = (gw.double() - want).norm(dim=1)
+    assert bool((err <= bound).all()), f"worst {float((err / bound).max()):.3g} x the bound, row {int((err / bound).argmax())}"
