@@ -40,9 +40,6 @@ using namespace product;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMostSum = 2.35e17f;        // e^40
 constexpr int kHalves = 2;                  // a tile's columns are summed by two warps
-// The tensor cores truncate where they add a k-step to an accumulator, which shrinks a logit by 1.0e-9 of itself per k on the mean
-// (measured at k = 768, 5120 and 16384: 6.8e-7, 5.0e-6, 1.6e-5); the factor on the accumulators takes the mean out again.
-constexpr double kShrinkPerK = 1.0e-9;
 
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
@@ -106,12 +103,14 @@ target_logit_kernel(const uint16_t* __restrict__ hidden, const uint16_t* __restr
 
 struct ExpEpi : StoringEpi {
     static constexpr bool kInputsOnly = true;
+    // 1024 k: a logit of typical operands loses 1e-6 of itself whatever k is.  Loss of 2047 tokens x 32000 x 5120 against 64 bits:
+    // 3.0e-7 (in one run 1.7e-6), 509 us (507); with 16384 columns 7.4e-7 (1.4e-5).
+    static constexpr int kRunStages = 16;
     CUtensorMap map_e;
     const float* refs;           // target logits of the piece
     const int32_t* labels;
     float* sums;                 // [2 per tile: its halves][tokens]; negative: relative to `tops`
     float* tops;                 // likewise, base 2
-    float to_base2;              // log2(e), and the factor above
     int write_e;
 
     // One pass over the accumulator row relative to ref2: returns the sum; writes E.
@@ -132,7 +131,7 @@ struct ExpEpi : StoringEpi {
                 const int n1 = n + 32 * h;
                 const bool special = !active || (unsigned)(label - n1) < 32u || n1 + 32 > s.n;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = ex2(fmaf(v[i], to_base2, -ref2));
+                for (int i = 0; i < 32; ++i) v[i] = ex2(fmaf(v[i], kLog2e, -ref2));
                 if (__any_sync(0xFFFFFFFFu, special)) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
@@ -180,7 +179,7 @@ struct ExpEpi : StoringEpi {
                 for (int i = 0; i < 32; ++i)
                     if (e.col0 + c + i != label && e.col0 + c + i < s.n) top = fmaxf(top, v[i]);
             }
-            const float top2 = top * to_base2;
+            const float top2 = top * kLog2e;
             if (e.lane == 0) store_wait_all();          // the first pass has been written before the second overwrites it
             __syncwarp();
             const float again = pass<BN>(s, e, over ? top2 : ref2, label, active);
@@ -656,7 +655,6 @@ int exp_product(const Call& c, int64_t t0, int64_t n)
     epi.labels = c.labels + t0;
     epi.sums = reinterpret_cast<float*>(c.ws + l.sums);
     epi.tops = reinterpret_cast<float*>(c.ws + l.tops);
-    epi.to_base2 = (float)(1.4426950408889634 * (1.0 + kShrinkPerK * (double)c.dim));
     epi.write_e = grads;
     epi.map_e = ma;
     if (grads && (rc = make_map(&epi.map_e, c.ws + l.e, 2, c.vocab, n, 1, l.e_ld, 0, 64, 32, true)) != CAST_OK) return rc;

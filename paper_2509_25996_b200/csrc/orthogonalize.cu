@@ -168,6 +168,7 @@ template <bool POLY>
 struct SymEpi {
     static constexpr bool kSym = true;
     static constexpr bool kInputsOnly = false;
+    static constexpr int kRunStages = 0;
     // eight with a ring would leave the products four stages instead of five: twelve 3072 x 768 500 -> 495 us, but 4096 x 11008
     // 2700 -> 2720 and 768 x 768 92.6 -> 93.2; with StepEpi's likewise 2750
     static constexpr int kWarps = POLY ? 4 : 8;
@@ -267,6 +268,7 @@ struct SymEpi {
 struct PartEpi {
     static constexpr bool kSym = true;
     static constexpr bool kInputsOnly = false;
+    static constexpr int kRunStages = 0;
     static constexpr int kWarps = 8;
     static constexpr int kStaging = kSlotBytes;
     struct State {};
@@ -339,6 +341,7 @@ template <bool LO_IN, bool LO_OUT>
 struct StepEpi {
     static constexpr bool kSym = false;
     static constexpr bool kInputsOnly = false;
+    static constexpr int kRunStages = 0;
     static constexpr int kWarps = LO_IN ? 4 : 8;
     // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise a slot for each
     static constexpr int kStaging = (LO_IN ? kRing + 1 : LO_OUT ? 2 : 1) * kSlotBytes;
@@ -434,6 +437,7 @@ template <bool LO_IN>
 struct ResultEpi {
     static constexpr bool kSym = false;
     static constexpr bool kInputsOnly = false;
+    static constexpr int kRunStages = 0;
     static constexpr int kWarps = LO_IN ? 4 : 8;
     static constexpr int kStaging = (LO_IN ? kRing : 1) * kSlotBytes;
     using State = AuxRing;

@@ -20,6 +20,11 @@
 // cycle); smaller tiles are bound by that path and only pay where they fill SMs that large ones leave idle.  On long products
 // (4096 x 32000 x 4096) it runs at 1300 TFLOP/s under the power limit, where a library product of these sizes takes 1370 alone.
 //
+// Long sums: the tensor cores truncate where they add 16 further k to an accumulator, always towards zero, which shrinks a sum of
+// typical operands by 1.0e-9 of itself per k (measured at k = 768, 5120 and 16384; exact sums lose nothing).  Where that matters
+// (Epi::kRunStages) a tile's k is cut into runs of that many stages, each accumulated from zero, and the epilogue warps add the runs in
+// fp32 registers, rounded to nearest, and put the sum back before the epilogue proper: the two accumulators take turns run by run.
+//
 // Every wait is bounded (kWaitCycles, kStageCycles); a role that gives up raises the CTA's stop flag, which ends the other roles, and
 // counts the failure in a word of host memory that the next call of the library reads.
 #pragma once
@@ -244,6 +249,29 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32])
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// 16 columns, whose values may be used at once, and the reverse, complete when it returns.
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16])
+{
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr) : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const float (&v)[16])
+{
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};\n\t"
+                 "tcgen05.wait::st.sync.aligned;"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
+}
+
 // Shared-memory matrix descriptor, 128-byte swizzle (bits 61-63 = 2, version 1 at bit 46): start address, leading and
 // stride byte offsets in units of 16 bytes.
 constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
@@ -329,11 +357,13 @@ __device__ __forceinline__ void slot_store(const EpiTile& e, uint32_t slot_addr,
 }
 
 // An epilogue provides: kSym (only tiles of the lower triangle), kInputsOnly (both operands are the caller's, whole before the
-// call's first kernel began), kWarps, kStaging (bytes per warp), State (kept from tile to tile),
+// call's first kernel began), kRunStages (of k per accumulation, see above; 0: a tile's whole k), kWarps, kStaging (bytes per warp),
+// State (kept from tile to tile),
 // prefetch() (its tensor maps), start() (before the first tile), tile() (false: give up).
 struct StoringEpi {
     static constexpr bool kSym = false;
     static constexpr bool kInputsOnly = false;
+    static constexpr int kRunStages = 0;
     static constexpr int kWarps = 8;
     static constexpr int kStaging = kSlotBytes;
     struct State {};
@@ -512,15 +542,17 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint32_t a0 = desc_lo<A_MN>(ring), b0 = desc_lo<B_MN>(ring + C::blocks * kStageBytesA);
             uint32_t at = 0;          // of the stage, in units of 16 bytes
             if constexpr (!Epi::kInputsOnly) chain_wait();      // the limits below are not for waiting for a predecessor
-            for (int t = first; ok && t < shape.total; t += step, ++n_done) {
-                const Tile tile = tile_of<Epi::kSym>(shape, t);
+            Tile tile = tile_of<Epi::kSym>(shape, first);
+            int run0 = tile.kb0;      // the run of stages that is accumulated next
+            for (int t = first; ok && t < shape.total; ++n_done) {
+                const int run1 = Epi::kRunStages ? min(tile.kb1, run0 + Epi::kRunStages) : tile.kb1;
                 const int buf = n_done & 1;
                 if (!(ok = mbar_wait_warp(acce0 + 8 * buf, (uint32_t)((n_done >> 1) & 1) ^ 1u, stop))) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
                 const uint32_t b_at = kSquare && tile.tm == tile.tn ? a0 : b0;
                 uint32_t accumulate = 0;
-                for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
+                for (int kb = run0; kb < run1; ++kb) {
                     if (!(ok = mbar_wait_warp(full0 + 8 * s, phase, stop))) break;
                     tc_fence_after();
                     if (elect_one()) {
@@ -532,12 +564,20 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                                        kDescHi, shape.idesc, i ? 1u : accumulate);
                         }
                         tc_commit<CG>(empty0 + 8 * s);
-                        if (kb + 1 == tile.kb1) tc_commit<CG>(accf0 + 8 * buf);
+                        if (kb + 1 == run1) tc_commit<CG>(accf0 + 8 * buf);
                     }
                     __syncwarp();
                     accumulate = 1;
                     at += C::stage_bytes >> 4;
                     if (++s == C::stages) { s = 0; at = 0; phase ^= 1u; }
+                }
+                run0 = run1;
+                if (run0 == tile.kb1) {
+                    t += step;
+                    if (t < shape.total) {
+                        tile = tile_of<Epi::kSym>(shape, t);
+                        run0 = tile.kb0;
+                    }
                 }
             }
         }
@@ -559,13 +599,53 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int t = first; t < shape.total; t += step, ++n_done) {
             e.index = t;
             e.tile = tile_of<Epi::kSym>(shape, t);
+            bool ok;
+            float sum[Epi::kRunStages ? C::cols / 16 : 1][16];       // of the runs before the last
+            int run0 = e.tile.kb0;
+            if constexpr (Epi::kRunStages != 0) {
+#pragma unroll
+                for (int j = 0; j < C::cols / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[j][i] = 0.0f;
+#pragma unroll 1
+                for (; run0 + Epi::kRunStages < e.tile.kb1; run0 += Epi::kRunStages, ++n_done) {
+                    const int buf = n_done & 1;
+                    ok = mbar_wait(accf0 + 8 * buf, (uint32_t)(n_done >> 1) & 1u, stop, Epi::kRunStages * kStageCycles);
+                    if (!__all_sync(0xFFFFFFFFu, ok)) break;
+                    tc_fence_after();
+                    const uint32_t acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)((warp & 3) * 32) << 16);
+#pragma unroll
+                    for (int j = 0; j < C::cols / 16; ++j) {
+                        float v[16];
+                        tmem_load16(acc + (uint32_t)(e.c0 + 16 * j), v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[j][i] += v[i];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(map_to_rank(acce0 + 8 * buf, 0));
+                }
+                if (run0 + Epi::kRunStages < e.tile.kb1) break;      // given up
+            }
             const int buf = n_done & 1;
-            bool ok = mbar_wait(accf0 + 8 * buf, (uint32_t)(n_done >> 1) & 1u, stop, (e.tile.kb1 - e.tile.kb0) * kStageCycles);
+            ok = mbar_wait(accf0 + 8 * buf, (uint32_t)(n_done >> 1) & 1u, stop, (e.tile.kb1 - run0) * kStageCycles);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             tc_fence_after();
             e.row0 = e.tile.tm * C::BM + e.first_row;
             e.col0 = e.tile.tn * BN;
             e.acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)((warp & 3) * 32) << 16);
+            if constexpr (Epi::kRunStages != 0) {
+                if (run0 != e.tile.kb0) {
+#pragma unroll
+                    for (int j = 0; j < C::cols / 16; ++j) {
+                        float v[16];
+                        tmem_load16(e.acc + (uint32_t)(e.c0 + 16 * j), v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] += sum[j][i];
+                        tmem_store16(e.acc + (uint32_t)(e.c0 + 16 * j), v);
+                    }
+                }
+            }
             ok = epi.template tile<C::BM, BN>(shape, e, state);
             tc_fence_before();
             __syncwarp();

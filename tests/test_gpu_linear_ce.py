@@ -361,3 +361,40 @@ def test_rows_whose_terms_cancel(tokens, vocab, dim, piece, mean):
     bound = 2.0 ** -8 * want.norm(dim=1) + 5 * 2.0 ** -8 * (q.square().T @ size.square()).sqrt() + (q + (1 - p) * hot).T @ ((eps + 2.0 ** -22) * size)
     err = (gw.double() - want).norm(dim=1)
     assert bool((err <= bound).all()), f"worst {float((err / bound).max()):.3g} x the bound, row {int((err / bound).argmax())}"
+
+
+@pytest.mark.parametrize("dim", [768, 4096, 16384])
+def test_logits_whose_sums_are_exact(dim):
+    """Sparse small integers: every partial sum of a logit is exact in fp32, on whichever unit, so the first term of eps_i falls
+    away and the loss is within 2^-21 max|l_i| + 1.2e-5."""
+    tokens, vocab = 300, 1000
+    g = torch.Generator(device=DEV).manual_seed(dim)
+    h, w = torch.zeros((tokens, dim), device=DEV), torch.zeros((vocab, dim), device=DEV)
+    cols = torch.randperm(dim, generator=g, device=DEV)[:16]
+    h[:, cols] = torch.randint(0, 3, (tokens, 16), generator=g, device=DEV).float()
+    w[:, cols] = torch.randint(-1, 3, (vocab, 16), generator=g, device=DEV).float()
+    h, w = h.to(torch.bfloat16), w.to(torch.bfloat16)
+    y = torch.randint(0, vocab, (tokens,), generator=g, device=DEV).int()
+    loss, _, _ = run(h, w, y, 1.0, want_h=False, want_w=False)
+    (want, _), _, _ = exact(h, w, y, 1.0)
+    top = (h.double() @ w.double().T).abs().amax(1)
+    assert float(top.max()) > 25.0
+    err = (loss.double() - want).abs() / (2.0 ** -21 * top + 1.2e-5)
+    assert float(err.max()) <= 1.0, f"worst {float(err.max()):.3g} x the bound"
+
+
+@pytest.mark.parametrize("tokens", [60, 500])
+def test_long_sums_do_not_shrink(tokens):
+    """A unit that truncates where it adds 16 products to a sum loses at most 2^-24 of it per addition on the mean.  Sums in runs of
+    1024 take 64 of them, 2^-18 of a logit, whatever the depth (16384 in one run: 2^-14); d loss = -shrink sum_{j != label} p_ij l_ij.
+    The rest of the loss is rounded to nearest: its mean error over the tokens is below 2^-20."""
+    vocab, dim = 2000, 16384
+    h, w, y = draw(tokens, vocab, dim, 51, lift=4.0)
+    h = (h.float() * 3).to(torch.bfloat16)                # other logits of up to ten or so
+    loss, _, _ = run(h, w, y, 1.0, want_h=False, want_w=False)
+    (want, _), _, _ = exact(h, w, y, 1.0)
+    l = h.double() @ w.double().T
+    p = torch.softmax(l, 1)
+    p[torch.arange(tokens, device=DEV), y.long()] = 0.0
+    error, bound = abs(float((loss.double() - want).mean())), 2.0 ** -18 * float((p * l.abs()).sum(1).mean()) + 2.0 ** -20
+    assert error <= bound, (error, bound)
