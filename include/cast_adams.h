@@ -515,7 +515,9 @@ CAST_API int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, co
  *                 keep the singular values of X below about 8 (those do: below 1.3).
  *   steps in [1, 100]; eps >= 0; scale finite.  A zero update gives a zero result.
  * rows*cols < 2^31.  The matrices are worked on together, as many at a time as make 64 M entries.
- * Products take fp16 operands (X scaled by 2^12) and accumulate in fp32; X itself is held in 22 bits.
+ * Products take fp16 operands (X scaled by 2^12, A and P = a I + b A + c A A) and accumulate in fp32.  X is held in 22 bits while
+ * the steps that follow multiply its small singular values by more than 4, in 11 bits after that.  With the default coefficients
+ * the result is within 2.0e-3 of the exact one in norm; its own rounding to bf16 is 1.7e-3 of that.
  */
 CAST_API int cast_orthogonalize_workspace(int n, int64_t rows, int64_t cols, uint64_t* bytes);
 CAST_API int cast_orthogonalize(const void* const* updates, int updates_bf16, cast_bf16* const* out, int n, int64_t rows, int64_t cols,

@@ -10,13 +10,16 @@
 // Operands are never transposed in memory: X is read K-major in one product and MN-major in the other.
 //
 // Numbers: the operands are fp16, not bf16.  Every value is bounded (|X| singular values stay near 1), so the range is
-// enough and the 3 more bits of significand are worth 8 times less rounding noise.  Noise of A and P is harmless: it enters
-// through directions that are large already.  Rounding X itself is not: that noise lies in all directions, and a step
-// multiplies small ones by a = 3.4, five steps by 500, which swamps an update of low rank (measured on 768 x 768 of rank 8 over
-// 2 % noise: 2.8e-2 from the exact result, where rounding the result to bf16 is 1.7e-3).  So while the steps still to come
-// amplify by more than kAmplify, X is held as hi + lo, two fp16 words scaled by 2^12 (22 bits): the products read hi, the
-// epilogue adds a lo.  With five steps X_0 (of an fp32 update; a bf16 one is exact in hi), X_1 and X_2 have a lo: 2.4e-3 on that
-// update.
+// enough and the 3 more bits of significand are worth 8 times less rounding noise.  Noise of A and P enters through directions
+// that are large already; what remains of it is P's diagonal, rounded alike in every step (~1e-3 of the result).  Rounding X itself
+// is worse: that noise lies in all directions, and a step multiplies small ones by a = 3.4, five steps by 500, which swamps an
+// update of low rank (measured on 768 x 768 of rank 8 over 2 % noise: 2.8e-2 from the exact result, where rounding the result to
+// bf16 is 1.7e-3).  So while the steps still to come amplify by more than kAmplify, X is held as hi + lo, two fp16 words scaled by
+// 2^12 (22 bits); with five steps X_0 (of an fp32 update; a bf16 one is exact in hi) to X_3 have a lo.  The products read hi;
+// P lo is replaced by kappa lo, kappa the mean of P's diagonal: rounding noise has no direction, so that is the nearest multiple
+// of lo to P lo.  It is a for an update of low rank, and near 1 where most directions have grown: there a lo would be further
+// from P lo than nothing is.  |out - exact| / |exact| for 768 x 768 without structure / of low rank, kAmplify 12 with a lo:
+// 2.00e-3 / 2.55e-3; 4 with a lo: 2.08e-3 / 1.92e-3; 4 with kappa lo: 1.98e-3 / 1.92e-3.
 //
 // What bounds it: for large matrices the tensor cores at the clock that the power limit leaves them (4096 x 11008: 2.69 ms, 1.16
 // PFLOP/s counting symmetric products by half); for twelve 3072 x 768 matrices (496 us) the path from L2 to the SMs, which
@@ -41,7 +44,10 @@ constexpr float kX = 4096.0f;               // X is stored times this
 constexpr int kGroup = 64;                  // matrices per launch at most
 constexpr int64_t kGroupElems = 64 << 20;   // ... and elements, which bounds the workspace
 constexpr int kNormBlocks = 1024;           // per matrix at most
-constexpr float kAmplify = 12.0f;           // X keeps its lo while later steps multiply small directions by more
+// X keeps its lo while later steps multiply small directions by more.  One word of X_4 amplified by 3.4 is 7e-4 of the result
+// at most, of X_3 2.5e-3, more than the result's own rounding.  Keeping X_3's and kappa take twelve
+// 3072 x 768 from 501 to 520 us, one 768 x 768 from 91.2 to 93.3.
+constexpr float kAmplify = 4.0f;
 
 struct PtrTable { const void* p[kGroup]; };
 struct OutTable { uint16_t* p[kGroup]; };
@@ -162,6 +168,30 @@ first_x_kernel(const __grid_constant__ PtrTable updates, const double* __restric
 
 // ------------------------------------------------------------------------------------------------ epilogues
 
+// Mean of the diagonal of a matrix's P, by a converged warp, in the same order everywhere.
+__device__ __forceinline__ float mean_diagonal(const float* traces, int batch, int n)
+{
+    const int blocks = (n + 31) / 32;
+    float sum = 0.0f;
+    for (int i = (int)threadIdx.x & 31; i < blocks; i += 32) sum += __ldg(traces + (int64_t)batch * blocks + i);
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k);
+    return sum / (float)n;
+}
+
+// The ring of lo, and kappa of the matrix at hand.
+struct LoState {
+    AuxRing ring;
+    int batch;
+    float kappa;
+    __device__ __forceinline__ void find_kappa(const float* traces, int of, int n)
+    {
+        if (of == batch) return;
+        batch = of;
+        kappa = mean_diagonal(traces, of, n);
+    }
+};
+
 // A symmetric result, stored at (row, col) and, off the diagonal, at (col, row): scale acc, or with POLY
 // scale acc + add aux + diag I.
 template <bool POLY>
@@ -179,6 +209,7 @@ struct SymEpi {
     CUtensorMap map_mirror;      // the same array, boxes of 64 rows x 32 columns, not swizzled
     CUtensorMap map_aux;         // fp16, read like map_out
     const float* gain;           // per matrix, its square multiplies the result; nullptr: 1
+    float* traces;               // POLY: [batch][blocks], sums of the diagonal over blocks of 32
     float scale, add, diag;
 
     __device__ __forceinline__ void prefetch() const
@@ -201,6 +232,7 @@ struct SymEpi {
     {
         const bool mirror = e.col0 + BN <= e.tile.tm * BM;
         const float g = gain ? __ldg(gain + e.tile.batch) : 1.0f, scale_all = scale * g * g;
+        [[maybe_unused]] float on_diagonal = 0.0f;
 #pragma unroll 1
         for (int c = e.c0; c < e.c1 && e.col0 + c < s.n; c += 64) {
             const int n = e.col0 + c;
@@ -239,6 +271,11 @@ struct SymEpi {
                 for (int i = 0; i < 16; ++i) p[i] = pack_f16(v[2 * i], v[2 * i + 1]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) slot_write(slot, e.lane, 4 * h + q, p[4 * q], p[4 * q + 1], p[4 * q + 2], p[4 * q + 3]);
+                if constexpr (POLY) {
+                    // a lane's own entry of the diagonal, where these 32 rows and columns are the same ones (no branch, as above)
+                    const float own = f16_lo(slot_read_16(slot, e.lane, 32 * h + e.lane));
+                    on_diagonal = e.row0 == n + 32 * h && e.row0 + e.lane < s.m ? own : on_diagonal;
+                }
                 if (mirror) {
                     // rows of 32 elements (64 bytes): column j of the chunk becomes row j, this lane its element
 #pragma unroll
@@ -259,6 +296,13 @@ struct SymEpi {
                 store_commit();
             }
             if constexpr (POLY) ring.next();
+        }
+        if constexpr (POLY) {
+#pragma unroll
+            for (int k = 16; k > 0; k >>= 1) on_diagonal += __shfl_xor_sync(0xFFFFFFFFu, on_diagonal, k);
+            const int first = e.col0 + e.c0;
+            if (e.lane == 0 && e.row0 >= first && e.row0 < min(s.m, first + e.c1 - e.c0))
+                traces[(int64_t)e.tile.batch * ((s.m + 31) / 32) + e.row0 / 32] = on_diagonal;
         }
         return true;
     }
@@ -336,7 +380,7 @@ add_parts_kernel(const float* __restrict__ parts, uint16_t* __restrict__ out, co
     }
 }
 
-// X' = gain acc (+ a lo): as hi + lo, or hi alone.
+// X' = gain acc (+ kappa lo): as hi + lo, or hi alone.
 template <bool LO_IN, bool LO_OUT>
 struct StepEpi {
     static constexpr bool kSym = false;
@@ -345,11 +389,12 @@ struct StepEpi {
     static constexpr int kWarps = LO_IN ? 4 : 8;
     // LO_IN: the ring of lo, replaced in place by the new one, and a slot for hi; otherwise a slot for each
     static constexpr int kStaging = (LO_IN ? kRing + 1 : LO_OUT ? 2 : 1) * kSlotBytes;
-    using State = AuxRing;
+    using State = LoState;
     CUtensorMap map_hi, map_lo;      // X'
     CUtensorMap map_lo_in;           // X
     const float* gain;               // per matrix; nullptr: 1 (only without LO_IN)
-    float a;
+    const float* traces;             // of P (LO_IN)
+    int sq;
 
     __device__ __forceinline__ void prefetch() const
     {
@@ -358,17 +403,21 @@ struct StepEpi {
         if constexpr (LO_OUT) prefetch_map(&map_lo);
     }
     template <int BM, int BN>
-    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
+    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& state) const
     {
         if constexpr (LO_IN) {
-            ring.start<BN, false>(s, e);
-            for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, false>(s, e, &map_lo_in);
+            state.ring.start<BN, false>(s, e);
+            for (int i = 0; i < kRing - 1; ++i) state.ring.load<BM, BN, false>(s, e, &map_lo_in);
+            state.batch = -1;
+            state.find_kappa(traces, tile_of<false>(s, e.index).batch, sq);
         }
     }
 
     template <int BM, int BN>
-    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& state) const
     {
+        AuxRing& ring = state.ring;
+        if constexpr (LO_IN) state.find_kappa(traces, e.tile.batch, sq);
         float g = 1.0f;
         if constexpr (!LO_IN) g = gain ? __ldg(gain + e.tile.batch) : 1.0f;
 #pragma unroll 1
@@ -403,8 +452,8 @@ struct StepEpi {
                     for (int i = 0; i < 4; ++i) {
                         float g0 = v[8 * q + 2 * i], g1 = v[8 * q + 2 * i + 1];
                         if constexpr (LO_IN) {
-                            g0 = fmaf(a, f16_lo(w[i]), g0);
-                            g1 = fmaf(a, f16_hi(w[i]), g1);
+                            g0 = fmaf(state.kappa, f16_lo(w[i]), g0);
+                            g1 = fmaf(state.kappa, f16_hi(w[i]), g1);
                         } else {
                             g0 *= g;
                             g1 *= g;
@@ -431,7 +480,7 @@ struct StepEpi {
     }
 };
 
-// The result: bf16(scale (acc + a lo)) into the caller's matrices, whose rows may have any length and alignment: through a slot,
+// The result: bf16(scale (acc + kappa lo)) into the caller's matrices, whose rows may have any length and alignment: through a slot,
 // then whole rows of it by ordinary stores.
 template <bool LO_IN>
 struct ResultEpi {
@@ -440,26 +489,31 @@ struct ResultEpi {
     static constexpr int kRunStages = 0;
     static constexpr int kWarps = LO_IN ? 4 : 8;
     static constexpr int kStaging = (LO_IN ? kRing : 1) * kSlotBytes;
-    using State = AuxRing;
+    using State = LoState;
     CUtensorMap map_lo_in;
     OutTable out;
     const float* gain;               // as in StepEpi
-    float a, scale;
-    int vec;
+    const float* traces;
+    float scale;
+    int sq, vec;
 
     __device__ __forceinline__ void prefetch() const { if constexpr (LO_IN) prefetch_map(&map_lo_in); }
     template <int BM, int BN>
-    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& ring) const
+    __device__ __forceinline__ void start(const Shape& s, const EpiTile& e, State& state) const
     {
         if constexpr (LO_IN) {
-            ring.start<BN, false>(s, e);
-            for (int i = 0; i < kRing - 1; ++i) ring.load<BM, BN, false>(s, e, &map_lo_in);
+            state.ring.start<BN, false>(s, e);
+            for (int i = 0; i < kRing - 1; ++i) state.ring.load<BM, BN, false>(s, e, &map_lo_in);
+            state.batch = -1;
+            state.find_kappa(traces, tile_of<false>(s, e.index).batch, sq);
         }
     }
 
     template <int BM, int BN>
-    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& ring) const
+    __device__ __forceinline__ bool tile(const Shape& s, EpiTile& e, State& state) const
     {
+        AuxRing& ring = state.ring;
+        if constexpr (LO_IN) state.find_kappa(traces, e.tile.batch, sq);
         uint16_t* o = out.p[e.tile.batch];
         float by = scale;
         if constexpr (!LO_IN) by *= gain ? __ldg(gain + e.tile.batch) : 1.0f;
@@ -486,8 +540,8 @@ struct ResultEpi {
                         const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            v[8 * q + 2 * i] = fmaf(a, f16_lo(w[i]), v[8 * q + 2 * i]);
-                            v[8 * q + 2 * i + 1] = fmaf(a, f16_hi(w[i]), v[8 * q + 2 * i + 1]);
+                            v[8 * q + 2 * i] = fmaf(state.kappa, f16_lo(w[i]), v[8 * q + 2 * i]);
+                            v[8 * q + 2 * i + 1] = fmaf(state.kappa, f16_hi(w[i]), v[8 * q + 2 * i + 1]);
                         }
                     }
                     slot_write(slot, e.lane, 4 * h + q, pack_b16(by * v[8 * q], by * v[8 * q + 1]),
@@ -555,7 +609,7 @@ Form choose_form(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int m
 
 struct Layout {
     int64_t group, ld, sq, sq_ld;
-    uint64_t norms, gains, hi[2], lo[2], a, p, parts, total;
+    uint64_t norms, gains, traces, hi[2], lo[2], a, p, parts, total;
 };
 
 Layout layout_of(int64_t n, int64_t rows, int64_t cols)
@@ -572,6 +626,7 @@ Layout layout_of(int64_t n, int64_t rows, int64_t cols)
     const uint64_t x = 2ull * (uint64_t)(l.group * rows * l.ld), q = 2ull * (uint64_t)(l.group * l.sq * l.sq_ld);
     l.norms = take(8ull * kNormBlocks * (uint64_t)l.group);
     l.gains = take(4ull * (uint64_t)l.group);
+    l.traces = take(4ull * (uint64_t)(l.group * ((l.sq + 31) / 32)));
     for (int i = 0; i < 2; ++i) { l.hi[i] = take(x); l.lo[i] = take(x); }
     l.a = take(q);
     l.p = take(q);
@@ -630,6 +685,7 @@ int gram_product(const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, f
     epi.map_out = epi.map_aux = m.a_chunk;
     epi.map_mirror = m.a_mirror;
     epi.gain = gain;
+    epi.traces = nullptr;
     epi.scale = down;
     epi.add = epi.diag = 0.0f;
     const bool narrow = BN / CG == 64;
@@ -638,7 +694,7 @@ int gram_product(const Maps& m, int cur, int64_t mn, int64_t k, int64_t batch, f
 }
 
 template <int CG, int BN>
-int poly_product(const Maps& m, int64_t mn, int64_t batch, const float* q, cudaStream_t stream)
+int poly_product(const Maps& m, int64_t mn, int64_t batch, const float* q, float* traces, cudaStream_t stream)
 {
     Shape s;
     SymEpi<true> epi;
@@ -648,6 +704,7 @@ int poly_product(const Maps& m, int64_t mn, int64_t batch, const float* q, cudaS
     epi.map_mirror = m.p_mirror;
     epi.map_aux = m.a_chunk;
     epi.gain = nullptr;
+    epi.traces = traces;
     epi.diag = q[0];
     epi.add = q[1];
     epi.scale = q[2];
@@ -686,19 +743,20 @@ int gram_product(const Form& form, const Maps& m, int cur, int64_t mn, int64_t k
     return gram_product<1, 64, MN>(m, cur, mn, k, batch, down, gain, stream);
 }
 
-int poly_product(TileForm f, const Maps& m, int64_t mn, int64_t batch, const float* q, cudaStream_t stream)
+int poly_product(TileForm f, const Maps& m, int64_t mn, int64_t batch, const float* q, float* traces, cudaStream_t stream)
 {
-    if (f == kPair256) return poly_product<2, 256>(m, mn, batch, q, stream);
-    if (f == kSingle128) return poly_product<1, 128>(m, mn, batch, q, stream);
-    return poly_product<1, 64>(m, mn, batch, q, stream);
+    if (f == kPair256) return poly_product<2, 256>(m, mn, batch, q, traces, stream);
+    if (f == kSingle128) return poly_product<1, 128>(m, mn, batch, q, traces, stream);
+    return poly_product<1, 64>(m, mn, batch, q, traces, stream);
 }
 
 struct StepCall {
     const Maps* maps;
     const OutTable* out;
     const float* gain;
+    const float* traces;
     int64_t rows, cols, batch, sq;
-    float a, scale;
+    float scale;
     int cur;                          // which X
     bool lo_in, lo_out, last, vec;
     cudaStream_t stream;
@@ -726,7 +784,8 @@ int next_product(const StepCall& c)
     epi.map_lo = m.x_lo[c.cur ^ 1];
     epi.map_lo_in = m.x_lo[c.cur];
     epi.gain = c.gain;
-    epi.a = c.a;
+    epi.traces = c.traces;
+    epi.sq = (int)c.sq;
     return step_product<CG, BN, WIDE>(c, epi);
 }
 
@@ -737,7 +796,8 @@ int result_product(const StepCall& c)
     epi.map_lo_in = c.maps->x_lo[c.cur];
     epi.out = *c.out;
     epi.gain = c.gain;
-    epi.a = c.a;
+    epi.traces = c.traces;
+    epi.sq = (int)c.sq;
     epi.scale = c.scale;
     epi.vec = c.vec;
     return step_product<CG, BN, WIDE>(c, epi);
@@ -872,6 +932,7 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
         const Form gram = choose_form(l.sq, l.sq, big, batch, true);
         const TileForm poly = choose_form(l.sq, l.sq, l.sq, batch, true, 1).tile, step = choose_form(rows, cols, l.sq, batch, false, 1).tile;
         float* parts = reinterpret_cast<float*>(ws + l.parts);
+        float* traces = reinterpret_cast<float*>(ws + l.traces);
         Maps maps;
         if ((rc = make_maps(&maps, hi, lo, a, p, rows, cols, batch, l)) != CAST_OK) return rc;
         bool has_lo = !updates_bf16;
@@ -882,12 +943,12 @@ extern "C" int cast_orthogonalize(const void* const* updates, int updates_bf16, 
             rc = wide ? gram_product<false>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, parts, a, l.sq_ld, st)
                       : gram_product<true>(gram, maps, cur, l.sq, big, batch, 1.0f / (kX * kX), gain, parts, a, l.sq_ld, st);
             if (rc != CAST_OK) return rc;
-            if ((rc = poly_product(poly, maps, l.sq, batch, q, st)) != CAST_OK) return rc;
+            if ((rc = poly_product(poly, maps, l.sq, batch, q, traces, st)) != CAST_OK) return rc;
             const bool last = k + 1 == steps;
             float amplify = 1.0f;      // of a small direction of X', by the steps after this one
             for (int j = k + 1; j < steps; ++j) amplify *= std::fabs(coeffs ? coeffs[3 * j] : kQuintic[0]);
             const bool lo_out = !last && amplify > kAmplify;
-            const StepCall c = {&maps, &to, gain, rows, cols, batch, l.sq, q[0], scale / kX, cur, has_lo, lo_out, last, out_vec, st};
+            const StepCall c = {&maps, &to, gain, traces, rows, cols, batch, l.sq, scale / kX, cur, has_lo, lo_out, last, out_vec, st};
             if ((rc = wide ? step_product<true>(step, c) : step_product<false>(step, c)) != CAST_OK) return rc;
             has_lo = lo_out;
         }

@@ -337,6 +337,15 @@ __device__ __forceinline__ uint4 slot_read(uint32_t slot_addr, int row, int chun
     return w;
 }
 
+// One 2-byte entry of it.
+__device__ __forceinline__ uint32_t slot_read_16(uint32_t slot_addr, int row, int col)
+{
+    unsigned short w;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w)
+                 : "r"(slot_addr + (uint32_t)row * 128u + (uint32_t)(((col >> 3) ^ (row & 7)) << 4) + (uint32_t)(col & 7) * 2u) : "memory");
+    return w;
+}
+
 // The slot of an epilogue that only stores, once the store that last used it has read it.  (One is enough: two such warps share a
 // scheduler, and the other one computes meanwhile.)
 __device__ __forceinline__ uint32_t slot_acquire(const EpiTile& e)

@@ -221,3 +221,16 @@ def test_one_step_over_several_chunks(n, rows, cols):
         err = (o.double() - want).abs()
         assert float(err.max()) <= 4 * tolerance(1) * float(want.abs().max())
     assert all(torch.equal(a, b) for a, b in zip(out, ops.orthogonalize(u, steps=1)))
+
+
+@pytest.mark.parametrize("rows,cols,rank", [(512, 512, 8), (768, 768, 8), (768, 3000, 8), (3000, 768, 8), (1500, 2000, 4), (768, 768, 0), (1024, 1536, 0)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_noise_before_the_last_rounding(rows, cols, rank, dtype):
+    """What the result's own rounding to bf16 leaves is known; the rest has to stay below it.  One fp16 word is rounded by
+    2.1e-4 of itself (2^-11 at most, over all significands).  P's diagonal, alike in each of five steps: 1.05e-3; one word of X_4
+    amplified by 3.44: 7.2e-4; A and the rest of P: 2^-11.  Together 1.4e-3, beside the rounding.  (One word of X_3 as well, amplified
+    by 11.9, would be 2.5e-3.)"""
+    for u in draw(2, rows, cols, 31 + rank, dtype, rank=rank):
+        want = exact(u, QUINTIC, 5)
+        rounding = distance(want.to(torch.bfloat16), want)
+        assert distance(ops.orthogonalize([u])[0], want) <= math.hypot(rounding, 1.4e-3)
