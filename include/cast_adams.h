@@ -514,7 +514,8 @@ CAST_API int cast_linear_ce(const cast_bf16* hidden, const cast_bf16* weight, co
  *   coeffs        host, [steps][3]: a, b, c of every step, or NULL for (3.4445, -4.7750, 2.0315) in all of them.  They must
  *                 keep the singular values of X below about 8 (those do: below 1.3).
  *   steps in [1, 100]; eps >= 0; scale finite.  A zero update gives a zero result.
- * rows*cols < 2^31.  The matrices are worked on together, as many at a time as make 64 M entries.
+ * rows*cols < 2^31.  The matrices are worked on together, as many at a time as make 64 M entries (rows padded
+ * to 64, shorter ones to a multiple of 8; one larger matrix by itself): four such sets of 2-byte words make most of the workspace.
  * Products take fp16 operands (X scaled by 2^12, A and P = a I + b A + c A A) and accumulate in fp32.  X is held in 22 bits while
  * the steps that follow multiply its small singular values by more than 4, in 11 bits after that.  With the default coefficients
  * the result is within 2.0e-3 of the exact one in norm; its own rounding to bf16 is 1.7e-3 of that.

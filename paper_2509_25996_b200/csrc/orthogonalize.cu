@@ -42,7 +42,7 @@ using namespace product;
 
 constexpr float kX = 4096.0f;               // X is stored times this
 constexpr int kGroup = 64;                  // matrices per launch at most
-constexpr int64_t kGroupElems = 64 << 20;   // ... and elements, which bounds the workspace
+constexpr int64_t kGroupElems = 64 << 20;   // ... and elements of padded rows, which bounds the workspace
 constexpr int kNormBlocks = 1024;           // per matrix at most
 // X keeps its lo while later steps multiply small directions by more.  One word of X_4 amplified by 3.4 is 7e-4 of the result
 // at most, of X_3 2.5e-3, more than the result's own rounding.  Keeping X_3's and kappa take twelve
@@ -615,10 +615,11 @@ struct Layout {
 Layout layout_of(int64_t n, int64_t rows, int64_t cols)
 {
     Layout l;
-    int64_t fit = kGroupElems / (rows * cols);
+    // whole 128-byte lines per row, or where a row is shorter than one the 16 bytes that a copy needs
+    l.ld = cols < 64 ? (cols + 7) / 8 * 8 : (cols + 63) / 64 * 64;
+    int64_t fit = kGroupElems / (rows * l.ld);
     fit = fit < 1 ? 1 : fit > kGroup ? kGroup : fit;
     l.group = n < fit ? n : fit;
-    l.ld = (cols + 63) / 64 * 64;
     l.sq = rows < cols ? rows : cols;
     l.sq_ld = (l.sq + 63) / 64 * 64;
     uint64_t at = 0;

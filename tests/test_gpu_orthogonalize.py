@@ -234,3 +234,20 @@ def test_noise_before_the_last_rounding(rows, cols, rank, dtype):
         want = exact(u, QUINTIC, 5)
         rounding = distance(want.to(torch.bfloat16), want)
         assert distance(ops.orthogonalize([u])[0], want) <= math.hypot(rounding, 1.4e-3)
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 20000, 1), (3, 3000, 5), (2, 5000, 16), (2, 4000, 40), (5, 1 << 20, 16), (1, 3, 50), (66, 900, 63)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_shorter_than_a_line(n, rows, cols, dtype):
+    u = draw(n, rows, cols, rows + cols, dtype)
+    guards = [U.Guarded(rows * cols, torch.bfloat16, DEV) for _ in u]
+    rc, need = cast.cast_orthogonalize_workspace(n, rows, cols)
+    cast.check(rc)
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device=DEV)
+    cast.check(cast.cast_orthogonalize(u, dtype == torch.bfloat16, [g.view for g in guards], rows, cols, None, 5, 1e-7, 1.0, ws, need,
+                                       torch.cuda.current_stream()))
+    torch.cuda.synchronize()
+    assert all(g.intact() for g in guards) and bool((ws[need:] == 255).all())
+    for i in {0, n // 2, n - 1}:
+        # few singular values do not average the signs of their errors
+        assert distance(guards[i].view.reshape(rows, cols), exact(u[i], QUINTIC, 5)) <= tolerance(5, 0 if cols < 40 else 1 << 30)

@@ -112,3 +112,12 @@ def test_torch_level_calls_refuse_host_tensors():
         with pytest.raises(ValueError, match="CUDA tensor"):
             call()
     assert ops.orthogonalize([]) == []
+
+
+@pytest.mark.parametrize("n,rows,cols", [(64, 1000000, 1), (16, 4000000, 1), (64, 65536, 16), (64, 1, 1000000), (1, 4000000, 1), (64, 300000, 65), (1000, 40, 7)])
+def test_orthogonalize_workspace_of_narrow_matrices(n, rows, cols):
+    """Four sets of 2-byte words over at most 64 M entries of padded rows, or one matrix of more; the squares, the norms and the
+    sums of splits add less than that again."""
+    rc, need = cast.cast_orthogonalize_workspace(n, rows, cols)
+    padded = rows * (-(-cols // 8) * 8 if cols < 64 else -(-cols // 64) * 64)
+    assert rc == B.CAST_OK and need <= 2 * 8 * max(64 << 20, padded)
