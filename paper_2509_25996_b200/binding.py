@@ -412,7 +412,12 @@ def cast_orthogonalize_workspace(n, rows, cols):
 
 
 def cast_orthogonalize(updates, updates_bf16, outs, rows, cols, coeffs, steps, eps, scale, workspace, workspace_bytes, stream=None) -> int:
-    """`updates`, `outs`: sequences of one buffer per matrix; `coeffs`: a flat sequence of 3 * steps numbers, or None."""
+    """`updates`, `outs`: sequences of one buffer per matrix; `coeffs`: a flat sequence of 3 * steps numbers, or None.
+    CAST_ERR_SHAPE for sequences of another length, of which the library would read past the end."""
+    if updates is not None and outs is not None and len(outs) != len(updates):
+        return CAST_ERR_SHAPE
+    if coeffs is not None and len(coeffs) != 3 * int(steps):
+        return CAST_ERR_SHAPE
     pu = None if updates is None else (ctypes.c_void_p * len(updates))(*[_ptr(u) for u in updates])
     po = None if outs is None else (ctypes.c_void_p * len(outs))(*[_ptr(o) for o in outs])
     pc = None if coeffs is None else (ctypes.c_float * len(coeffs))(*coeffs)

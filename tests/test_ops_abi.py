@@ -121,3 +121,12 @@ def test_orthogonalize_workspace_of_narrow_matrices(n, rows, cols):
     rc, need = cast.cast_orthogonalize_workspace(n, rows, cols)
     padded = rows * (-(-cols // 8) * 8 if cols < 64 else -(-cols // 64) * 64)
     assert rc == B.CAST_OK and need <= 2 * 8 * max(64 << 20, padded)
+
+
+@pytest.mark.parametrize("over", [dict(outs=[A3]), dict(outs=[A3, A4, A5]), dict(outs=[]), dict(coeffs=[3.0, -4.0, 2.0]), dict(coeffs=[1.0] * 16), dict(coeffs=[])])
+def test_orthogonalize_sequences_of_another_length(over):
+    a = dict(updates=[A1, A2], updates_bf16=False, outs=[A3, A4], rows=64, cols=96, coeffs=[1.0] * 15, steps=5, eps=1e-7, scale=1.0, workspace=WS,
+             workspace_bytes=1 << 30)
+    assert cast.cast_orthogonalize(**a) in NO_DEVICE
+    a.update(over)
+    assert cast.cast_orthogonalize(**a) == B.CAST_ERR_SHAPE
