@@ -4,7 +4,8 @@ orthogonalised updates.
 Plumbing only, like `runner`: the functions check their tensors, allocate results and workspace with torch (on the
 current stream, so the caching allocator keeps the workspace until the work is done) and make one call of the library.
 They raise ValueError for tensors the library cannot take as they are (nothing is copied or converted behind the
-caller's back) and CastError for a refused call.
+caller's back) and CastError for a refused call.  The results carry no autograd graph: a tensor that requires a gradient is
+refused while torch records one, not dropped from it silently.
 """
 from __future__ import annotations
 
@@ -16,6 +17,8 @@ from . import binding as B
 
 
 def _need(t: torch.Tensor, name: str, dtype, dims: int, device=None) -> None:
+    if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: requires a gradient, but results carry no autograd graph (call under torch.no_grad(), or pass it detached)")
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed")
     if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):

@@ -130,3 +130,15 @@ def test_orthogonalize_sequences_of_another_length(over):
     assert cast.cast_orthogonalize(**a) in NO_DEVICE
     a.update(over)
     assert cast.cast_orthogonalize(**a) == B.CAST_ERR_SHAPE
+
+
+def test_torch_level_calls_do_not_drop_a_graph():
+    """Tensors that require a gradient are refused while torch records a graph (and get as far as the next check when it does not)."""
+    x = torch.zeros((4, 8), dtype=torch.bfloat16, requires_grad=True)
+    plain = torch.zeros((4, 8), dtype=torch.bfloat16)
+    ids = torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: ops.embed(x, ids), lambda: ops.embed_grad(x, ids, 10), lambda: ops.linear_ce(x, plain, ids), lambda: ops.orthogonalize([x])):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="CUDA tensor"):
+            call()
