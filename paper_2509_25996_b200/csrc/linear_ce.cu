@@ -51,6 +51,15 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// A target logit as a power of two, kept finite (NaN stays), so that a target of no probability at all (a masked row of the head)
+// leaves the other probabilities as they are: a difference with it must not be inf - inf.
+constexpr float kFar = 3.0e38f;
+__device__ __forceinline__ float base2(float ref)
+{
+    const float r = __fmul_rn(ref, kLog2e);          // rounded, whatever it is subtracted from
+    return r < -kFar ? -kFar : r > kFar ? kFar : r;
+}
+
 // ------------------------------------------------------------------------------------------------ target logits
 
 // refs[t] = h_t . w_label, 0 without a label.  One warp per token; dim % 8 == 0.  For dW's label terms, the CTAs after the tokens' own
@@ -162,7 +171,7 @@ struct ExpEpi : StoringEpi {
         if (row < s.m) {
             label = __ldg(labels + row);
             if ((unsigned)label >= (unsigned)s.n) label = -1;
-            ref2 = __ldg(refs + row) * kLog2e;
+            ref2 = base2(__ldg(refs + row));
         }
         const int64_t at = (int64_t)(e.tile.tn * kHalves + (e.c0 ? 1 : 0)) * s.m;
         const bool active = label >= 0;
@@ -237,7 +246,7 @@ finish_kernel(const __grid_constant__ FinishArgs p)
     const bool in = t < p.tokens;
     const int label = in ? p.labels[t] : -1;
     const bool active = (unsigned)label < (unsigned)p.vocab;
-    const float ref = in ? p.refs[t] : 0.0f, ref2 = ref * kLog2e;
+    const float ref = in ? p.refs[t] : 0.0f, ref2 = base2(ref);
 
     // largest reference of the row's tiles (the target logit where none was too large)
     float top2 = ref2;
@@ -276,7 +285,8 @@ finish_kernel(const __grid_constant__ FinishArgs p)
         float s = 0.0f;
         for (int i = 0; i < 32; ++i) s += part[i][k];
         // the epilogue subtracted ref log2(e) rounded to fp32, the same for the whole row: put the rest of that product back
-        const float missed = fmaf(ref, kLog2e, -ref2) * kLn2;
+        const float missed = top2 == ref2 && fabsf(ref2) < kFar ? fmaf(ref, kLog2e, -ref2) * kLn2 : 0.0f;
+        if (ref == INFINITY) s = NAN;          // as is a row with any other infinite logit
         float loss = 0.0f, a = 0.0f, b = 0.0f;
         if (active) {
             const float own = ex2(ref2 - top2);          // the target's own term, 1 unless the reference moved
@@ -284,7 +294,7 @@ finish_kernel(const __grid_constant__ FinishArgs p)
                 s -= s * missed;
                 loss = log1pf(s);
             } else {
-                loss = (top2 - ref2) * kLn2 + logf(own + s);
+                loss = (top2 * kLn2 - ref) + logf(own + s);
             }
             a = (p.grad_scale - p.grad_scale * missed) / (own + s);
             b = p.grad_scale * (s / (own + s));
@@ -321,7 +331,7 @@ finish_kernel(const __grid_constant__ FinishArgs p)
     }
     if (p.e && sh_over[warp]) {
         uint16_t* row = p.e + (t0 + warp) * p.e_ld;
-        const float r2 = p.refs[t0 + warp] * kLog2e;
+        const float r2 = base2(p.refs[t0 + warp]);
         for (int j = wl; j < p.vocab; j += 32) {
             const int64_t at = (int64_t)(j / p.tile_cols) * p.tokens + t0 + warp;
             const float from = p.sums[at] >= 0.0f ? r2 : p.tops[at];

@@ -193,3 +193,23 @@ def test_host_memory_is_refused():
     y = torch.zeros((4, 8), dtype=torch.bfloat16, device=DEV)
     ids = torch.zeros(4, dtype=torch.int32)
     assert cast.cast_embed(x, ids, y, 4, 4, 8) == B.CAST_ERR_MEMORY
+
+
+@pytest.mark.parametrize("tokens,dim", [(40, 64), (40, 61), (2000, 64), (2000, 61)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_not_a_number_stays_in_its_row(tokens, dim, value):
+    vocab = 30
+    ids = draw_ids(tokens, vocab, 14, "any").to(DEV)
+    table, grad = draw((vocab, dim), 15).to(DEV), draw((tokens, dim), 16).to(DEV)
+    out, back = ops.embed(table, ids), ops.embed_grad(grad, ids, vocab)
+    at = int(((ids >= 0) & (ids < vocab)).nonzero()[3])
+    row = int(ids[at])
+    table[row, 9] = value
+    grad[at, 9] = value
+    out2, back2 = ops.embed(table, ids), ops.embed_grad(grad, ids, vocab)
+    hit = ids == row
+    assert torch.equal(out2[~hit], out[~hit]) and not out2[hit][:, 9].isfinite().any()
+    rest = torch.arange(vocab, device=DEV) != row
+    assert torch.equal(back2[rest], back[rest]) and not bool(back2[row, 9].isfinite())
+    cols = torch.arange(dim, device=DEV) != 9
+    assert torch.equal(back2[row, cols], back[row, cols])

@@ -398,3 +398,71 @@ def test_long_sums_do_not_shrink(tokens):
     p[torch.arange(tokens, device=DEV), y.long()] = 0.0
     error, bound = abs(float((loss.double() - want).mean())), 2.0 ** -18 * float((p * l.abs()).sum(1).mean()) + 2.0 ** -20
     assert error <= bound, (error, bound)
+
+
+@pytest.mark.parametrize("tokens,piece", [(40, 0), (300, 0), (300, 130)])
+@pytest.mark.parametrize("feature", [1.0, 2.0])
+def test_labels_on_a_masked_row(tokens, piece, feature):
+    """A row of the head that is masked with the type's lowest value: its logits are -3.4e38, or -inf in fp32.  It changes nothing for
+    the other labels, and a token whose label it is has that loss and the gradient of a target without probability."""
+    h, w, y = draw(tokens, 900, 64, 61)
+    masked, low = 123, float(torch.finfo(torch.bfloat16).min)
+    w[masked] = 0.0
+    w[masked, 0] = low
+    h[:, 0] = feature
+    y[y == masked] = 5
+    y[::3] = masked
+    loss, gh, gw = run(h, w, y, 1.0, piece=piece)
+    l = h.double() @ w.double().T
+    at = torch.arange(tokens, device=DEV)
+    want = (torch.logsumexp(l, 1) - l[at, y.long()]).float()
+    on = y == masked
+    assert torch.equal(torch.isinf(loss), torch.isinf(want)) and bool((loss[on] > 3e38).all())
+    keep = torch.ones(900, dtype=torch.bool, device=DEV)
+    keep[masked] = False
+    # the rest: as if that row were not there
+    y2 = y - (y > masked).int()
+    y2[on] = -1
+    close(loss[~on], tuple(t[~on] for t in exact(h, w[keep], y2, 1.0)[0]), "loss of the others")
+    d = torch.softmax(l, 1)
+    d[at, y.long()] -= 1.0
+    for got, ref, size in ((gh, d @ w.double(), d.abs() @ w.double().abs()), (gw, d.T @ h.double(), d.abs().T @ h.double().abs())):
+        assert bool(torch.isfinite(got).all())
+        assert bool(((got.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 4 * 2.0 ** -8 * size).all())
+
+
+@pytest.mark.parametrize("tokens", [40, 300])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_not_a_number_stays_with_its_token(tokens, value):
+    """An entry of a labelled hidden state that is no number: that token's loss and gradient are none either, nor is dW, to which it
+    belongs; the other tokens' losses and gradients are what they were."""
+    h, w, y = draw(tokens, 700, 64, 62)
+    clean = run(h, w, y, 1.0)
+    h[7, 3] = value
+    loss, gh, gw = run(h, w, y, 1.0)
+    rest = torch.arange(tokens, device=DEV) != 7
+    assert torch.equal(loss[rest], clean[0][rest]) and torch.equal(gh[rest], clean[1][rest])
+    assert not math.isfinite(float(loss[7])) and bool(gh[7].isnan().all()) and bool(gw[:, 3].isnan().all())
+    # an entry of the head: every token's
+    h, w, y = draw(tokens, 700, 64, 63)
+    w[650, 5] = value
+    loss, gh, gw = run(h, w, y, 1.0)
+    ref = torch.nn.functional.cross_entropy(h.double() @ w.double().T, y.long(), reduction="none")
+    assert torch.equal(loss.isfinite(), ref.isfinite())
+    assert bool(gh[:, 5].isnan().all())
+
+
+def test_a_masked_row_of_infinities():
+    """-inf as the logit of a row that is nobody's label: the losses are those without it."""
+    h, w, y = draw(200, 500, 64, 64)
+    h[:, 0] = h[:, 0].abs() + 0.125
+    y[y == 77] = 5
+    w[77] = 0.0
+    w[77, 0] = -float("inf")
+    loss, _, gw = run(h, w, y, 1.0, want_h=False)
+    keep = torch.arange(500, device=DEV) != 77
+    y2 = y - (y > 77).int()
+    ref = exact(h, w[keep], y2, 1.0)
+    close(loss, ref[0], "loss")
+    close(gw[keep], ref[2], "dW")
+    assert not gw[77].any()

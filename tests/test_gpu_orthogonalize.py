@@ -251,3 +251,17 @@ def test_rows_shorter_than_a_line(n, rows, cols, dtype):
     for i in {0, n // 2, n - 1}:
         # few singular values do not average the signs of their errors
         assert distance(guards[i].view.reshape(rows, cols), exact(u[i], QUINTIC, 5)) <= tolerance(5, 0 if cols < 40 else 1 << 30)
+
+
+@pytest.mark.parametrize("rows,cols", [(200, 330), (330, 200), (64, 5000), (1, 9)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_not_a_number_stays_in_its_matrix(rows, cols, value, dtype):
+    """The norm of an update with an entry that is no number is none either, so no entry of its result is one; the other matrices of
+    the call keep theirs."""
+    u = draw(3, rows, cols, 41, dtype)
+    clean = ops.orthogonalize(u)
+    u[1][0, cols // 2] = value
+    out = ops.orthogonalize(u)
+    assert bool(out[1].isnan().all())
+    assert torch.equal(out[0], clean[0]) and torch.equal(out[2], clean[2])
