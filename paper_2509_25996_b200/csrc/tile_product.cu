@@ -73,12 +73,12 @@ int fail_word(unsigned long long** word)
 
 int sm_count(int* n)
 {
-    static int known[64] = {};
+    static std::atomic<int> known[64];      // calls may come from several threads
     int dev;
     CAST_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev < 64 && known[dev] > 0) { *n = known[dev]; return CAST_OK; }
+    if (dev < 64 && (*n = known[dev].load(std::memory_order_relaxed)) > 0) return CAST_OK;
     CAST_CUDA_TRY(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
-    if (dev < 64) known[dev] = *n;
+    if (dev < 64) known[dev].store(*n, std::memory_order_relaxed);
     return CAST_OK;
 }
 

@@ -466,3 +466,27 @@ def test_a_masked_row_of_infinities():
     close(loss, ref[0], "loss")
     close(gw[keep], ref[2], "dW")
     assert not gw[77].any()
+
+
+def test_calls_from_several_threads():
+    """Each thread on a stream of its own, with its own workspace: the results are those of calls one after the other."""
+    import threading
+    inputs = [draw(tokens, 700, 96, 70 + tokens) for tokens in (60, 300, 90, 500)]
+    updates = [torch.randn((200, 96 + 8 * i), generator=torch.Generator(device=DEV).manual_seed(i), device=DEV) for i in range(4)]
+    want = [(ops.linear_ce(*x), ops.orthogonalize([u])[0]) for x, u in zip(inputs, updates)]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(10):
+                got = ops.linear_ce(*inputs[i]), ops.orthogonalize([updates[i]])[0]
+                torch.cuda.current_stream().synchronize()
+                if not (all(torch.equal(a, b) for a, b in zip(got[0], want[i][0])) and torch.equal(got[1], want[i][1])):
+                    wrong.append(i)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not wrong and not any(t.is_alive() for t in threads)
