@@ -3,7 +3,7 @@
     x      = embed(table, ids) * sqrt(d)                 cast_embed
     h      = x + relu(x W1^T) W2^T                       W1, W2 pruned 2:4 by the AdamS plan (its masked bf16 forward weights)
     z      = h W3^T                                      W3 unpruned: momentum orthogonalised by cast_orthogonalize
-    loss   = cross entropy of z table^T                  cast_linear_ce: dz and the head's part of dtable, no logits stored
+    loss   = cross entropy of z table^T                  cast_linear_ce: dz and the head's part of dtable
     dtable += gradient of the lookup                     cast_embed_grad onto the head's gradient: table and head are one matrix
 
 The table is trained by the same AdamS kernel with nothing pruned (4:4).  The data are a random walk over the vocabulary whose

@@ -478,7 +478,8 @@ CAST_API int cast_embed_grad(const cast_bf16* grad_out, const int32_t* ids, cast
                     int64_t dim, float scale, int accumulate, void* workspace, uint64_t workspace_bytes, cast_stream_t stream);
 
 /*
- * cast_linear_ce -- softmax cross entropy of a linear head and its gradients, without the logits in memory.  With
+ * cast_linear_ce -- softmax cross entropy of a linear head and its gradients.  The logits are not stored; their exponentials are, for
+ * the gradients, in bf16 and a piece of the tokens at a time (piece_tokens).  With
  * l = hidden weight^T and p the softmax of each row of l:
  *
  *     loss[i]     = logsumexp(l[i]) - l[i][labels[i]]                     (0 for a token without a label)
@@ -490,7 +491,9 @@ CAST_API int cast_embed_grad(const cast_bf16* grad_out, const int32_t* ids, cast
  *                 Without either, only the loss is computed (scoring).
  *   grad_scale    finite; carries the reduction (1/tokens for a mean) and any loss scaling.
  *   piece_tokens  tokens whose exponentials (bf16 [piece][vocab]) are held at a time; 0 = as many as fit 1 GiB.  With more
- *                 than one piece, grad_weight is accumulated in fp32 in the workspace.
+ *                 than one piece, grad_weight is accumulated in fp32 in the workspace.  The workspace also holds fp32 rows of the
+ *                 labels in use.  In all: 0.38 GB for 4096 tokens x 32000 x 4096, 3.5 GB for 8192 x 128256 x 4096 (33 MB without
+ *                 gradients).
  *   dim % 8 == 0; hidden, weight, grad_hidden, grad_weight and workspace 16-byte aligned.
  * The products take bf16 operands and accumulate in fp32; the loss and all statistics are fp32.  The workspace size depends
  * on the device.  The first call of a process allocates one word of page-locked host memory: make it outside any

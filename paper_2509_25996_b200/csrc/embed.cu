@@ -1,8 +1,8 @@
 // Token embedding, out[t] = scale table[ids[t]], and its gradient, grad_table[v] = scale sum_{t: ids[t] = v} grad_out[t].
 //
 // Forward: a gather bounded by HBM (each output row written once, each table row in use read once).  One thread moves
-// 16 bytes (8 columns); kUnroll of them per thread are in flight.  16384 tokens x 4096 columns (269 MB with 32000 table rows, part
-// of which stays in L2): 32.8 us; 8 tokens: 3 us, less than its launch from Python (11 us).
+// 16 bytes (8 columns); kUnroll of them per thread are in flight.  16384 tokens x 4096 columns whose frequencies fall like 1/rank
+// (134 MB written, ~5500 different rows, 45 MB, read): 33 us, 5.4 TB/s; 8 tokens: 3 us, less than its launch from Python (10 us).
 //
 // Gradient: the tokens are put in the order (id, position) first, so that every table row sums its tokens in one fixed
 // order, in fp32 registers, and is rounded and written once, without atomics: results do not change from run to run.
@@ -21,7 +21,9 @@
 //     the sorted ids hold, so nothing is written twice and the zeros share the bandwidth with the sums.  (Zeros beside the
 //     ranking or the merge, whose latency they would hide, took 113 and 105 us where this took 97: writes alone are slower.)
 // Bounded by HBM behind two short sorting kernels: 16384 tokens x 4096 into 32000 rows 91.5 us for 399 MB (4.3 TB/s; ranking and
-// merging 13 us of it), 1000 tokens x 768 into 50257 rows 21 us for 79 MB.
+// merging 13 us of it), 1000 tokens x 768 into 50257 rows 21 us for 79 MB.  More than kRun kWays = 16384 tokens take a second
+// merge, whose searches go to L2: 16385 tokens 9 us longer; 32768 141 us (531 MB), 65536 233 (799 MB).  Adding to the table:
+// 16384 97-99 us, 32768 181.
 #include <cmath>
 #include <type_traits>
 

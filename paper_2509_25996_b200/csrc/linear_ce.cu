@@ -1,4 +1,5 @@
-// Softmax cross entropy of a linear head, l = hidden weight^T, without the logits in memory, and its gradients.
+// Softmax cross entropy of a linear head, l = hidden weight^T, and its gradients.  The logits are not stored; for the gradients their
+// exponentials are, in bf16, a piece of the tokens at a time (below).
 //
 // With r_i = h_i . w_label(i) (the target logit) and S_i = sum_{j != label} e^(l_ij - r_i):
 //     loss_i = log(1 + S_i),   p_ij = e^(l_ij - r_i) / (1 + S_i),   1 - p_i,label = S_i / (1 + S_i)
@@ -12,21 +13,23 @@
 //     dW = E^T (a H) - B            product over the tokens; B is subtracted in fp32 by the epilogue
 // The two backward products read E as it was written: no pass over it to apply the normaliser.
 //
-// E is the only large intermediate, 2 bytes per logit of a piece.  Several pieces accumulate dW in fp32.
+// E takes 2 bytes per logit of a piece, as much as logits in bf16 would: all of them, 262 MB, for 4096 tokens x 32000; pieces of
+// 1 GiB bound it for more.  Several pieces accumulate dW in fp32 (2.1 GB for 128256 x 4096).  The loss alone needs neither.
 // Range: e^(l - r) beyond e^40 (a target that is that improbable) would leave the range of the later sums.  The epilogue
 // sees it in its row sum, forms that row's part of the tile relative to the tile's own maximum instead and says so by a negative
 // sum; finish then brings the row to one reference.
 //
-// Rounding: the products take bf16 operands, so E and a H are rounded to bf16 (2^-9 relative each); everything that is
+// Rounding: the products take bf16 operands, so E and a H are rounded to bf16 (2^-8 relative at most); everything that is
 // summed, and all statistics, are fp32.  The label's terms, the largest of a row, are never rounded before the result is: the two
 // parts of a frequent label's row of dW nearly cancel where the head is calibrated and the hidden states have a common mean, so
-// that a rounding of one of them would be up to 30 of the result's.
+// that a rounding of one of them would be 30 of the result's (measured: 5.3e-2 of such a row instead of 1.7e-3).
 //
 // Bounded by the tensor cores, for large calls at the clock that the power limit leaves them (1.3-1.4 GHz): 4096 tokens x 32000
-// x 4096 2.48 ms (1300 TFLOP/s), 8192 x 128256 x 4096 19.9 ms (1300), loss alone of 2047 x 32000 x 5120 0.50 ms (1340).
-// 1000 x 50257 x 768 takes 234 us (990): its three products (60, 56 and 57 us alone, tensor pipe 77-83 % busy) read 620 MB of
-// operands each through L2.  48 x 32000 x 768 takes 56 us, where reading and writing the head once takes 15: nine launches,
-// each of a few microseconds.
+// x 4096 2.51-2.59 ms (1260 TFLOP/s), 8192 x 128256 x 4096 20.2-20.8 ms (1260), loss alone of 2047 x 32000 x 5120 0.505 ms (1330).
+// 1000 x 50257 x 768 takes 237 us (976): its three products (61, 56 and 58 us alone, tensor pipe 76-83 % busy) read 620 MB of
+// operands each through L2; by a launch list they are 85 % of the call, target logits, finish, the join of dH and the label sums
+// the rest.  48 x 32000 x 768 takes 59 us, where reading and writing the head once takes 15: seven launches in a chain, of which E
+// and dW (49 MB of the head read, as many of its gradient written) are a quarter each, dH and its join a third.
 #include <cmath>
 
 #include "embed.cuh"
@@ -571,8 +574,10 @@ int64_t sum_rows(int64_t vocab, int64_t tokens)
 
 // Splits of the vocabulary for dH: few tokens give few tiles, and each has the whole vocabulary to sum.  The time of
 // `splits` is taken as rounds of tiles x (blocks + 8 for filling and draining the pipeline), in blocks (~0.3 us for a pair),
-// plus writing and reading the partial sums at ~5 TB/s.  A split has to save a twentieth: SMs that idle in a last round leave
-// their power to the others (4096 tokens x 32000 x 4096, which would take two splits: 2.54-2.58 ms with them, 2.55-2.56 without).
+// plus writing and reading the partial sums at ~5 TB/s.  A split has to save a twentieth of that, which the model does not resolve,
+// as its sums take memory.  Loss and dH, us, with that margin / without: 512 x 128256 x 4096 (2 splits / 9) 787 / 793, 57 x 11076 x
+// 192 (29 / 44) 37 / 43, 430 x 59492 x 192 (31 / 36) 112 / 119, 814 x 95519 x 248 (17 / 18) 202 / 211, 2 x 45992 x 1112 (15 / 16) 94 / 96;
+// 572 x 2176 x 1488 (1 / 3) 60 / 57, 55 x 1010 x 1800 (1 / 4) 43 / 42, 4096 x 32000 x 4096 (1 / 2) 1634 / 1621.
 int hidden_splits(int64_t tokens, int64_t vocab, int64_t dim, int sms)
 {
     const bool two = paired(tokens);

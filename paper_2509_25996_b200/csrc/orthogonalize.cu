@@ -21,10 +21,10 @@
 // from P lo than nothing is.  |out - exact| / |exact| for 768 x 768 without structure / of low rank, kAmplify 12 with a lo:
 // 2.00e-3 / 2.55e-3; 4 with a lo: 2.08e-3 / 1.92e-3; 4 with kappa lo: 1.98e-3 / 1.92e-3.
 //
-// What bounds it: for large matrices the tensor cores at the clock that the power limit leaves them (4096 x 11008: 2.69 ms, 1.16
-// PFLOP/s counting symmetric products by half); for twelve 3072 x 768 matrices (496 us) the path from L2 to the SMs, which
+// What bounds it: for large matrices the tensor cores at the clock that the power limit leaves them (4096 x 11008: 2.77 ms, 1.13
+// PFLOP/s counting symmetric products by half); for twelve 3072 x 768 matrices (522 us) the path from L2 to the SMs, which
 // feeds a pair's tile 64 bytes per cycle and SM, just as much as it consumes, and X and its two words, which exceed L2; for one
-// 768 x 768 (91 us) the chain of 17 kernels, of ~5.4 us each: 1 us until the first operands are there, 1.8 us of products, 1 us
+// 768 x 768 (93 us) the chain of 17 kernels, of ~5.4 us each: 1 us until the first operands are there, 1.8 us of products, 1 us
 // of epilogue, 1.5 us until its successor sees the results.
 #include <algorithm>
 #include <cmath>
@@ -585,7 +585,8 @@ struct Form { TileForm tile; int splits; };
 // tensor cores; a single CTA is bound by its L2 port, 64 bytes per cycle: 512 cycles for 32 KB (128 x 128), 384 for 24 KB
 // (128 x 64).  Filling and draining a tile's pipeline: about 3000 cycles and 16 per column of its epilogue.  Splits of k (symmetric
 // products only) cost another kernel, about 8000 cycles, and their sums written and read at ~2.5 KB per cycle.  (Measured from
-// 256 x 256 to 4096 x 4096, alone and in batches: no other tile is more than 3 % faster than the one chosen.)
+// 256 x 256 to 4096 x 4096, alone and in batches: no other tile is more than 3 % faster than the one chosen.  The cycles are those
+// of operands in L2, the same for all forms where they are not: the choice goes by their order, not by their sum.)
 Form choose_form(int64_t m, int64_t n, int64_t k, int64_t batch, bool sym, int most_splits = kMostSplits)
 {
     const int64_t kb = (k + kBK - 1) / kBK;

@@ -18,7 +18,8 @@
 //
 // Tiles: a pair's 256 x 256 loads 32 KB per CTA for 512 cycles of products, all that a CTA's path from L2 gives (64 bytes per
 // cycle); smaller tiles are bound by that path and only pay where they fill SMs that large ones leave idle.  On long products
-// (4096 x 32000 x 4096) it runs at 1300 TFLOP/s under the power limit, where a library product of these sizes takes 1370 alone.
+// (4096 x 32000 x 4096) it runs at 1250-1300 TFLOP/s under the power limit, where library products of these sizes run at 1340-1400
+// alone.
 //
 // Long sums: the tensor cores truncate where they add 16 further k to an accumulator, always towards zero, which shrinks a sum of
 // typical operands by 1.0e-9 of itself per k (measured at k = 768, 5120 and 16384; exact sums lose nothing).  Where that matters
@@ -287,7 +288,7 @@ constexpr uint32_t kDescStep = MN_MAJOR ? (16 * 128) >> 4 : (16 * 2) >> 4;      
 // ------------------------------------------------------------------------------------------------ the kernel
 
 // Of Epi: kWarps epilogue warps (four where a tile is only one chunk wide), each with kStaging bytes of shared memory.  A stage is
-// one 64-deep block (issued in ~250 cycles, computed in 512 by a pair and 256 by a single CTA with 128 columns), and two of
+// one 64-deep block (issued in about 250 cycles, computed in 512 by a pair and 256 by a single CTA with 128 columns), and two of
 // them where they are computed in 128.
 template <int CG, int BN, class Epi>
 struct Config {
@@ -487,7 +488,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     // The two issuing roles run as whole warps on uniform values, with one lane elected for the instructions themselves: in a
     // single lane's branch the compiler has to move every descriptor word from vector to uniform registers, and issuing the
-    // four products of a stage took ~590 cycles instead of ~250, more than the 512 that they take to compute.
+    // four products of a stage took ~590 cycles, more than the 512 that they take to compute; so it is about half of that.
     if (warp == 0) {
         int s = 0;
         uint32_t phase = 0;
