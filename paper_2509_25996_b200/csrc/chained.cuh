@@ -3,6 +3,8 @@
 //
 // Every kernel of a chain calls chain_next() (its successor may be scheduled) and chain_wait() before it touches memory that
 // others write or read: chain_wait returns once the predecessor has finished, which had waited for its own predecessor.
+// In every CTA some thread waits, also in one without work: a grid of which none had could end before its predecessor, and what
+// follows the call on its stream waits for the last grid alone.
 // The first kernel of a call is launched with `first`, an ordinary launch behind whatever the stream holds.
 #pragma once
 
