@@ -538,6 +538,112 @@ CAST_API int cast_orthogonalize(const void* const* updates, int updates_bf16, ca
 CAST_API int cast_product_failures(unsigned long long* count_out, int action);
 
 /*
+ * What stands between the matrices of a layer, and between the backward pass and the optimizer step.  (The paper has no counterpart to
+ * these entry points either; the shared conventions of the ends of a model hold.)
+ *
+ * cast_rms_norm -- root-mean-square norm of rows, behind the addition to the residual stream.  Asynchronous on `stream`.
+ *
+ *     h = bf16(x + residual)   (h = x without a residual),      y = weight h / sqrt(mean(h^2) + eps)
+ *
+ *   x          device, bf16 [tokens][dim].          residual   device, bf16 [tokens][dim], or NULL.
+ *   weight     device, [dim]: bf16, or fp32 where weight_fp32 != 0.
+ *   y          device, bf16 [tokens][dim], out.     h          device, bf16 [tokens][dim], out; NULL exactly where residual is.
+ *              h may be x or residual itself; otherwise no result may overlap an input or another result.
+ *   dim in [1, 32768]; eps >= 0 (a row of zeros needs eps > 0).  dim % 8 == 0 with 16-byte aligned buffers takes the vector
+ *   path, anything else a slower scalar one.
+ * y is normalised from the rounded h: what is stored is what a backward pass reads.  Sums and statistics are fp32, and fp64 for rows whose
+ * squares leave the range of fp32; y is rounded once.  NaN and infinities stay in their row.
+ *
+ * cast_rms_norm_mx -- the same with an 8-bit result for block-scaled products: groups of 32 columns of a row (the last one may be shorter)
+ * share a power of two.
+ *
+ *   q          device, e4m3 [tokens][dim], out: y / scale of its group, rounded to nearest even from fp32.
+ *   q_scales   device, e8m0 [tokens][(dim + 31) / 32], out: exponent + 127 of the least power of two with max|y| <= 448 scale; 0 (2^-127) for
+ *              a group of zeros; 255 (NaN) where an entry is not finite, the whole group's q are then NaN, too.
+ */
+CAST_API int cast_rms_norm(const cast_bf16* x, const cast_bf16* residual, const void* weight, int weight_fp32, cast_bf16* y, cast_bf16* h,
+                  int64_t tokens, int64_t dim, float eps, cast_stream_t stream);
+CAST_API int cast_rms_norm_mx(const cast_bf16* x, const cast_bf16* residual, const void* weight, int weight_fp32, uint8_t* q, uint8_t* q_scales,
+                     cast_bf16* h, int64_t tokens, int64_t dim, float eps, cast_stream_t stream);
+
+/*
+ * cast_rms_norm_grad -- gradient of cast_rms_norm.  With r = 1 / sqrt(mean(h^2) + eps), n = h r, g = weight grad_y:
+ *
+ *     grad_x = r (g - n mean(g n)) + grad_h,      grad_weight = sum over the tokens of grad_y n
+ *
+ *   grad_y        device, bf16 [tokens][dim].       h        device, bf16 [tokens][dim]: what the forward call stored (or x).
+ *   grad_h        device, bf16 [tokens][dim], or NULL: the gradient that reaches the residual stream h from what comes after.
+ *   grad_x        device, bf16 [tokens][dim], out: the gradient of h, and so of x and of residual.  May be grad_h itself.
+ *   grad_weight   device, fp32 [dim], out, or NULL (no workspace is needed then).
+ * The statistics are computed again from h.  grad_weight is summed in fp32 by up to a few CTAs per SM and joined in a fixed order.  The
+ * workspace size depends on the device.
+ */
+CAST_API int cast_rms_norm_grad_workspace(int64_t tokens, int64_t dim, uint64_t* bytes);
+CAST_API int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, const void* weight, int weight_fp32, const cast_bf16* grad_h,
+                       cast_bf16* grad_x, float* grad_weight, int64_t tokens, int64_t dim, float eps, void* workspace, uint64_t workspace_bytes,
+                       cast_stream_t stream);
+
+/*
+ * cast_rotary -- rotary positions with one or several axes (text; time, height and width of images and video).  Asynchronous on `stream`.
+ *
+ *     pair i of every head of token t turns by the angle frequencies[i] * positions[axes[i]][t]:
+ *     (a, b) -> (a cos - b sin, a sin + b cos)
+ *
+ * The pairs are columns (i, i + pairs), or (2i, 2i + 1) where adjacent != 0; columns from 2 * pairs on are copied.  inverse != 0 turns the other
+ * way: the gradient.
+ *
+ *   sets          host array of n_sets (1 to 4) arrays of heads, e.g. queries and keys (cast_heads_t: bf16, strides in entries, the
+ *                 columns of a head contiguous; tokens and heads in either order; an input may be broadcast by a stride of 0).  out may be in itself
+ *                 with the same strides, and sets may lie side by side in the rows of one fused array; otherwise no result may overlap
+ *                 an input or another result.
+ *   positions     device, int32 [n_axes][tokens], any value.
+ *   frequencies   device, fp64 [pairs]: radians per position.
+ *   axes          device, int32 [pairs], or NULL for axis 0; a pair of an axis outside [0, n_axes) does not turn.
+ *   n_axes in [1, 64]; pairs in [1, 512]; 2 * pairs <= head_dim <= 1024; at most 65536 heads in all sets.
+ * Multiples of 8 columns (halves: of 8 pairs) and of 8 in the strides with 16-byte aligned buffers take the vector path.  Angles are formed
+ * and reduced in fp64, cosines, sines and products are fp32; results are rounded once.
+ */
+typedef struct {
+    const cast_bf16* in;
+    cast_bf16* out;
+    int64_t heads;
+    int64_t in_token_stride, in_head_stride;
+    int64_t out_token_stride, out_head_stride;
+} cast_heads_t;
+CAST_API int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* positions, const double* frequencies, const int32_t* axes, int n_axes,
+                int pairs, int adjacent, int inverse, int64_t tokens, int64_t head_dim, cast_stream_t stream);
+
+/*
+ * cast_grads_* -- the global norm of the gradients of a model, and their clipping.
+ *
+ *     norm = |scale| sqrt(sum over all tensors of g^2),       out = g * scale * min(1, max_norm / norm)
+ *
+ * cast_grads_create takes the tensors of a set once (like a plan; they keep their places), the calls are asynchronous on `stream`:
+ *
+ *   grads      host array of n: device pointers, fp32 or bf16 each.  out is where a tensor's clipped gradient goes, in fp32 or bf16 (e.g. from
+ *              gradients accumulated in fp32 to the bf16 ones that a step takes); it may be grad itself in the same type.  NULL in
+ *              all of them: a set for norms alone.  No result may overlap another one or another tensor's gradient.
+ *   scale      finite: what every gradient is multiplied by (1 / accumulated micro-batches); it counts in the norm.
+ *   max_norm   >= 0; infinity only scales.  A norm that is not a number makes every result NaN; an infinite one makes the finite ones 0.
+ *   norm       device, fp32, out: the norm before clipping.
+ * The factor is formed on the device; nothing is synchronised.  A tensor that keeps its place is not written where the factor is 1.
+ * Squares are summed in fp32 over 32 entries at most and in fp64 beyond.  The workspace (cast_grads_workspace) depends on the device; create and all
+ * calls belong to the same current device.
+ */
+typedef struct {
+    const void* grad;
+    void* out;
+    int64_t count;
+    int32_t grad_bf16;
+    int32_t out_bf16;
+} cast_grad_t;
+CAST_API int cast_grads_create(const cast_grad_t* grads, int n, void** set_out);
+CAST_API int cast_grads_workspace(void* set, uint64_t* bytes);
+CAST_API int cast_grads_norm(void* set, float scale, float* norm, void* workspace, uint64_t workspace_bytes, cast_stream_t stream);
+CAST_API int cast_grads_clip(void* set, float max_norm, float scale, float* norm, void* workspace, uint64_t workspace_bytes, cast_stream_t stream);
+CAST_API int cast_grads_destroy(void* set);
+
+/*
  * Measurement aids.  Neither computes anything of the method (the paper has no counterpart); a benchmark puts their
  * times beside a measured step.
  *

@@ -12,6 +12,8 @@ from .binding import (  # noqa: F401
     cast_host_step_static, cast_kd_loss, cast_prune_fold, cast_plan_prune_fold, cast_mask_stats, cast_plan_mask_stats,
     cast_embed, cast_embed_grad, cast_embed_grad_workspace, cast_linear_ce, cast_linear_ce_workspace,
     cast_orthogonalize, cast_orthogonalize_workspace, cast_product_failures,
+    cast_rms_norm, cast_rms_norm_mx, cast_rms_norm_grad, cast_rms_norm_grad_workspace, cast_rotary,
+    cast_grads_create, cast_grads_workspace, cast_grads_norm, cast_grads_clip, cast_grads_destroy,
     cast_probe_launch, cast_probe_stream, cast_bulk_timeout_count,
     cast_strerror, cast_last_cuda_error, cast_kernel_launch_count,
 )

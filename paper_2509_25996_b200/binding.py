@@ -46,6 +46,8 @@ EXPORTS = (
     "cast_host_step_static", "cast_kd_loss", "cast_prune_fold", "cast_plan_prune_fold", "cast_mask_stats", "cast_plan_mask_stats",
     "cast_embed", "cast_embed_grad", "cast_embed_grad_workspace", "cast_linear_ce", "cast_linear_ce_workspace",
     "cast_orthogonalize", "cast_orthogonalize_workspace", "cast_product_failures",
+    "cast_rms_norm", "cast_rms_norm_mx", "cast_rms_norm_grad", "cast_rms_norm_grad_workspace", "cast_rotary",
+    "cast_grads_create", "cast_grads_workspace", "cast_grads_norm", "cast_grads_clip", "cast_grads_destroy",
     "cast_probe_launch", "cast_probe_stream", "cast_bulk_timeout_count",
     "cast_strerror", "cast_last_cuda_error", "cast_kernel_launch_count",
 )
@@ -74,6 +76,21 @@ class cast_hyper_t(ctypes.Structure):
         ("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
         ("eps", ctypes.c_float), ("l1_coeff", ctypes.c_float),
         ("step", ctypes.c_int64), ("total_steps", ctypes.c_int64), ("flags", ctypes.c_uint32),
+    ]
+
+
+class cast_heads_t(ctypes.Structure):
+    _fields_ = [
+        ("input", ctypes.c_void_p), ("out", ctypes.c_void_p), ("heads", ctypes.c_int64),
+        ("in_token_stride", ctypes.c_int64), ("in_head_stride", ctypes.c_int64),
+        ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+    ]
+
+
+class cast_grad_t(ctypes.Structure):
+    _fields_ = [
+        ("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64),
+        ("grad_bf16", ctypes.c_int32), ("out_bf16", ctypes.c_int32),
     ]
 
 
@@ -172,6 +189,20 @@ def load_library() -> ctypes.CDLL:
                                        ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
     lib.cast_product_failures.restype = ctypes.c_int
     lib.cast_product_failures.argtypes = [ctypes.POINTER(ctypes.c_ulonglong), ctypes.c_int]
+    for name in ("cast_rms_norm", "cast_rms_norm_mx", "cast_rms_norm_grad", "cast_rms_norm_grad_workspace", "cast_rotary", "cast_grads_create",
+                 "cast_grads_workspace", "cast_grads_norm", "cast_grads_clip", "cast_grads_destroy"):
+        getattr(lib, name).restype = ctypes.c_int
+    lib.cast_rms_norm.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int] + [ctypes.c_void_p] * 2 + [ctypes.c_int64] * 2 + [ctypes.c_float, ctypes.c_void_p]
+    lib.cast_rms_norm_mx.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int] + [ctypes.c_void_p] * 3 + [ctypes.c_int64] * 2 + [ctypes.c_float, ctypes.c_void_p]
+    lib.cast_rms_norm_grad_workspace.argtypes = [ctypes.c_int64, ctypes.c_int64, size_out]
+    lib.cast_rms_norm_grad.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int] + [ctypes.c_void_p] * 3 + [ctypes.c_int64] * 2 + \
+        [ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
+    lib.cast_rotary.argtypes = [ctypes.POINTER(cast_heads_t), ctypes.c_int] + [ctypes.c_void_p] * 3 + [ctypes.c_int] * 4 + [ctypes.c_int64] * 2 + [ctypes.c_void_p]
+    lib.cast_grads_create.argtypes = [ctypes.POINTER(cast_grad_t), ctypes.c_int, ctypes.POINTER(ctypes.c_void_p)]
+    lib.cast_grads_workspace.argtypes = [ctypes.c_void_p, size_out]
+    lib.cast_grads_norm.argtypes = [ctypes.c_void_p, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
+    lib.cast_grads_clip.argtypes = [ctypes.c_void_p, ctypes.c_float, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
+    lib.cast_grads_destroy.argtypes = [ctypes.c_void_p]
     lib.cast_host_ctx_sync.restype = ctypes.c_int
     lib.cast_host_ctx_sync.argtypes = [ctypes.c_void_p]
     lib.cast_host_ctx_destroy.restype = ctypes.c_int
@@ -423,6 +454,71 @@ def cast_orthogonalize(updates, updates_bf16, outs, rows, cols, coeffs, steps, e
     pc = None if coeffs is None else (ctypes.c_float * len(coeffs))(*coeffs)
     return load_library().cast_orthogonalize(pu, 1 if updates_bf16 else 0, po, 0 if updates is None else len(updates), int(rows), int(cols),
                                              pc, int(steps), eps, scale, _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def cast_rms_norm(x, residual, weight, weight_fp32, y, h, tokens, dim, eps, stream=None) -> int:
+    return load_library().cast_rms_norm(_ptr(x), _ptr(residual), _ptr(weight), 1 if weight_fp32 else 0, _ptr(y), _ptr(h), int(tokens), int(dim), eps,
+                                        _stream(stream))
+
+
+def cast_rms_norm_mx(x, residual, weight, weight_fp32, q, q_scales, h, tokens, dim, eps, stream=None) -> int:
+    return load_library().cast_rms_norm_mx(_ptr(x), _ptr(residual), _ptr(weight), 1 if weight_fp32 else 0, _ptr(q), _ptr(q_scales), _ptr(h), int(tokens),
+                                           int(dim), eps, _stream(stream))
+
+
+def cast_rms_norm_grad_workspace(tokens, dim):
+    """Returns (status, bytes)."""
+    out = ctypes.c_uint64(0)
+    rc = load_library().cast_rms_norm_grad_workspace(int(tokens), int(dim), ctypes.byref(out))
+    return rc, out.value
+
+
+def cast_rms_norm_grad(grad_y, h, weight, weight_fp32, grad_h, grad_x, grad_weight, tokens, dim, eps, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().cast_rms_norm_grad(_ptr(grad_y), _ptr(h), _ptr(weight), 1 if weight_fp32 else 0, _ptr(grad_h), _ptr(grad_x), _ptr(grad_weight),
+                                             int(tokens), int(dim), eps, _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def make_heads(x, out, heads, in_token_stride, in_head_stride, out_token_stride, out_head_stride) -> cast_heads_t:
+    return cast_heads_t(_ptr(x), _ptr(out), int(heads), int(in_token_stride), int(in_head_stride), int(out_token_stride), int(out_head_stride))
+
+
+def cast_rotary(sets: Sequence[cast_heads_t], positions, frequencies, axes, n_axes, pairs, adjacent, inverse, tokens, head_dim, stream=None) -> int:
+    n = len(sets)
+    arr = (cast_heads_t * max(n, 1))(*sets)
+    return load_library().cast_rotary(arr, n, _ptr(positions), _ptr(frequencies), _ptr(axes), int(n_axes), int(pairs), 1 if adjacent else 0,
+                                      1 if inverse else 0, int(tokens), int(head_dim), _stream(stream))
+
+
+def make_grad(grad, out, count, grad_bf16, out_bf16) -> cast_grad_t:
+    return cast_grad_t(_ptr(grad), _ptr(out), int(count), 1 if grad_bf16 else 0, 1 if out_bf16 else 0)
+
+
+def cast_grads_create(grads: Sequence[cast_grad_t]):
+    """Returns (status, handle of the set or None)."""
+    n = len(grads)
+    arr = (cast_grad_t * max(n, 1))(*grads)
+    out = ctypes.c_void_p(None)
+    rc = load_library().cast_grads_create(arr if n else None, n, ctypes.byref(out))
+    return rc, (out.value if rc == CAST_OK else None)
+
+
+def cast_grads_workspace(grads):
+    """Returns (status, bytes)."""
+    out = ctypes.c_uint64(0)
+    rc = load_library().cast_grads_workspace(grads, ctypes.byref(out))
+    return rc, out.value
+
+
+def cast_grads_norm(grads, scale, norm, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().cast_grads_norm(grads, scale, _ptr(norm), _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def cast_grads_clip(grads, max_norm, scale, norm, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().cast_grads_clip(grads, max_norm, scale, _ptr(norm), _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def cast_grads_destroy(grads) -> int:
+    return load_library().cast_grads_destroy(grads)
 
 
 def cast_product_failures(action: int = 0):

@@ -1,5 +1,5 @@
 """Torch-level calls of the operators around the sparse step: token embedding and gradient, linear cross entropy,
-orthogonalised updates.
+orthogonalised updates, root-mean-square norm and gradient, rotary positions, gradient clipping.
 
 Plumbing only, like `runner`: the functions check their tensors, allocate results and workspace with torch (on the
 current stream, so the caching allocator keeps the workspace until the work is done) and make one call of the library.
@@ -9,6 +9,7 @@ refused while torch records one, not dropped from it silently.
 """
 from __future__ import annotations
 
+import math
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -157,3 +158,234 @@ def orthogonalize(updates: Sequence[torch.Tensor], steps: int = 5, coeffs: Optio
     _on(first.device, lambda stream: B.cast_orthogonalize([u.data_ptr() for u in updates], first.dtype == torch.bfloat16, [o.data_ptr() for o in outs],
                                                           rows, cols, coeffs, steps, eps, scale, ws.data_ptr(), ws.numel(), stream))
     return list(outs)
+
+
+def _rows(x: torch.Tensor, weight: torch.Tensor, first: str) -> Tuple[int, int]:
+    """(tokens, dim) of an array of rows and the weight of their columns."""
+    if isinstance(x, torch.Tensor) and x.dim() < 1:
+        raise ValueError(f"{first}: no columns")
+    _need(x, first, torch.bfloat16, x.dim() if isinstance(x, torch.Tensor) else 1)
+    _need(weight, "weight", (torch.float32, torch.bfloat16), 1, x.device)
+    dim = x.shape[-1]
+    if weight.shape[0] != dim:
+        raise ValueError(f"weight: {weight.shape[0]} entries for {dim} columns")
+    return (x.numel() // dim if dim else 0), dim
+
+
+def _like(t: Optional[torch.Tensor], name: str, x: torch.Tensor) -> None:
+    if t is not None:
+        _need(t, name, torch.bfloat16, x.dim(), x.device)
+        if t.shape != x.shape:
+            raise ValueError(f"{name}: shape {tuple(t.shape)} instead of {tuple(x.shape)}")
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, out: Optional[torch.Tensor] = None,
+             sum_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(y, h): h = x + residual (x itself without a residual), y = weight h / sqrt(mean(h^2) + eps) over the last dimension, both
+    bf16.  weight: bf16 or fp32.  sum_out may be residual (or x), which h then replaces."""
+    tokens, dim = _rows(x, weight, "x")
+    _like(residual, "residual", x)
+    _like(out, "out", x)
+    _like(sum_out, "sum_out", x)
+    if residual is None and sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    y = torch.empty_like(x) if out is None else out
+    h = x if residual is None else torch.empty_like(x) if sum_out is None else sum_out
+    if tokens:
+        _on(x.device, lambda stream: B.cast_rms_norm(x.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
+                                                     weight.dtype == torch.float32, y.data_ptr(), None if residual is None else h.data_ptr(), tokens, dim,
+                                                     eps, stream))
+    return y, h
+
+
+def rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                sum_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(q, scales, h): rms_norm with y as float8_e4m3fn values and a power of two (float8_e8m0fnu) for every 32 columns."""
+    tokens, dim = _rows(x, weight, "x")
+    _like(residual, "residual", x)
+    _like(sum_out, "sum_out", x)
+    if residual is None and sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    q = torch.empty_like(x, dtype=torch.float8_e4m3fn)
+    scales = x.new_empty((*x.shape[:-1], (dim + 31) // 32), dtype=torch.float8_e8m0fnu)
+    h = x if residual is None else torch.empty_like(x) if sum_out is None else sum_out
+    if tokens:
+        _on(x.device, lambda stream: B.cast_rms_norm_mx(x.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
+                                                        weight.dtype == torch.float32, q.data_ptr(), scales.data_ptr(),
+                                                        None if residual is None else h.data_ptr(), tokens, dim, eps, stream))
+    return q, scales, h
+
+
+def rms_norm_grad(grad_y: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, grad_h: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  weight_grad: bool = True, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(grad_x bf16, grad_weight fp32 or None) of rms_norm from the h it returned.  grad_h: the gradient that reaches h from what
+    comes after on the residual stream; grad_x is then the gradient of x and of residual.  out may be grad_h."""
+    tokens, dim = _rows(h, weight, "h")
+    _like(grad_y, "grad_y", h)
+    _like(grad_h, "grad_h", h)
+    _like(out, "out", h)
+    gx = torch.empty_like(h) if out is None else out
+    gw = weight.new_empty(dim, dtype=torch.float32) if weight_grad else None
+    if tokens == 0:
+        return gx, gw.zero_() if gw is not None else None
+    def call(stream):
+        ws = _workspace(B.cast_rms_norm_grad_workspace(tokens, dim), h) if weight_grad else None             # depends on the device
+        return B.cast_rms_norm_grad(grad_y.data_ptr(), h.data_ptr(), weight.data_ptr(), weight.dtype == torch.float32,
+                                    None if grad_h is None else grad_h.data_ptr(), gx.data_ptr(), None if gw is None else gw.data_ptr(), tokens, dim, eps,
+                                    None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream)
+    _on(h.device, call)
+    return gx, gw
+
+
+class RotarySpectrum:
+    """Which columns of a head turn together, how fast, and with which axis of the positions.
+
+    frequencies: radians per position of every pair of columns.  axes: the axis of every pair (None: all on axis 0).
+    adjacent: pairs are columns (2i, 2i + 1) instead of (i, i + pairs)."""
+
+    def __init__(self, frequencies: Sequence[float], axes: Optional[Sequence[int]] = None, adjacent: bool = False, device=None):
+        frequencies = [float(f) for f in frequencies]
+        axes = [0] * len(frequencies) if axes is None else [int(a) for a in axes]
+        if not frequencies or len(axes) != len(frequencies):
+            raise ValueError(f"{len(axes)} axes for {len(frequencies)} frequencies")
+        if not all(math.isfinite(f) for f in frequencies):
+            raise ValueError("frequencies: not all finite")
+        if min(axes) < 0:
+            raise ValueError("axes: negative")
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        self.pairs, self.n_axes, self.adjacent = len(frequencies), max(axes) + 1, bool(adjacent)
+        self.frequencies = torch.tensor(frequencies, dtype=torch.float64, device=device)
+        self.axes = torch.tensor(axes, dtype=torch.int32, device=device)
+
+    @classmethod
+    def of(cls, dims: int, base: float = 10000.0, sections: Optional[Sequence[int]] = None, per_axis: bool = False, adjacent: bool = False,
+           device=None) -> "RotarySpectrum":
+        """The usual spectrum of `dims` turning columns: base^(-2i / dims) for pair i.  sections: how many consecutive pairs
+        belong to each axis; per_axis: every axis has the spectrum of its own columns instead of its part of the whole one."""
+        if dims < 2 or dims % 2:
+            raise ValueError(f"{dims} columns do not make pairs")
+        sections = [dims // 2] if sections is None else [int(n) for n in sections]
+        if sum(sections) != dims // 2 or min(sections) < 0:
+            raise ValueError(f"sections {sections} of {dims // 2} pairs")
+        frequencies: List[float] = []
+        axes: List[int] = []
+        for axis, n in enumerate(sections):
+            frequencies += [base ** -(j / n if per_axis else (len(axes) + j) / (dims // 2)) for j in range(n)]
+            axes += [axis] * n
+        return cls(frequencies, axes, adjacent, device)
+
+
+def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, spectrum: RotarySpectrum, inverse: bool = False,
+           out: Optional[Tuple[torch.Tensor, Optional[torch.Tensor]]] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Turns the heads of q and k (bf16 [tokens, heads, head_dim], any strides with contiguous columns; k may be None) by the
+    positions, int32 [axes, tokens] or [tokens].  inverse: the other way, which takes gradients back.  out: where the results go (q and k
+    themselves, or arrays of any strides); new contiguous arrays without."""
+    _need(positions, "positions", torch.int32, positions.dim() if isinstance(positions, torch.Tensor) and positions.dim() in (1, 2) else 2)
+    dev = positions.device
+    n_axes, tokens = (1, positions.shape[0]) if positions.dim() == 1 else positions.shape
+    if n_axes < spectrum.n_axes:
+        raise ValueError(f"positions: {n_axes} axes for a spectrum of {spectrum.n_axes}")
+    if spectrum.frequencies.device != dev:
+        raise ValueError(f"spectrum: on {spectrum.frequencies.device} instead of {dev}")
+    results: List[Optional[torch.Tensor]] = []
+    sets = []
+    head_dim = q.shape[-1] if isinstance(q, torch.Tensor) and q.dim() else 0
+    for i, (x, name) in enumerate(((q, "q"), (k, "k"))):
+        if x is None and i == 1:
+            if out is not None and out[1] is not None:
+                raise ValueError("out[1]: there is no k")
+            results.append(None)
+            continue
+        _need_heads(x, name, dev, (tokens, None, head_dim))
+        if out is None:
+            o = x.new_empty(x.shape)
+        else:
+            o = out[i]
+            _need_heads(o, f"out[{i}]", dev, tuple(x.shape))
+        results.append(o)
+        if x.shape[1]:
+            sets.append(B.cast_heads_t(x.data_ptr(), o.data_ptr(), x.shape[1], x.stride(0), x.stride(1), o.stride(0), o.stride(1)))
+    if 2 * spectrum.pairs > head_dim:
+        raise ValueError(f"spectrum: {2 * spectrum.pairs} columns of heads of {head_dim}")
+    if tokens and sets:
+        _on(dev, lambda stream: B.cast_rotary(sets, positions.data_ptr(), spectrum.frequencies.data_ptr(), spectrum.axes.data_ptr(), n_axes,
+                                              spectrum.pairs, spectrum.adjacent, inverse, tokens, head_dim, stream))
+    return results[0], results[1]
+
+
+def _need_heads(t: torch.Tensor, name: str, device, shape) -> None:
+    if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: requires a gradient, but results carry no autograd graph (call under torch.no_grad(), or pass it detached)")
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor is needed")
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{name}: {t.dtype} is not {torch.bfloat16}")
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device} instead of {device}")
+    if t.dim() != 3 or t.shape[0] != shape[0] or t.shape[2] != shape[2] or shape[1] not in (None, t.shape[1]):
+        raise ValueError(f"{name}: shape {tuple(t.shape)} instead of {tuple('heads' if s is None else s for s in shape)}")
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name}: the columns of a head are not contiguous")
+
+
+class GradientSet:
+    """The gradients of a model as one set, for their global norm and clipping.
+
+    grads: contiguous fp32 or bf16 tensors of one device.  outs: where the clipped gradients go, fp32 or bf16, one of the same number
+    of entries for each, e.g. the bf16 gradients that a step takes behind ones accumulated in fp32.  Without outs clip() works in place.
+    The tensors are kept alive and keep their places."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
+        self._handle = None
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if len(grads) == 0 or len(outs) != len(grads):
+            raise ValueError(f"{len(outs)} outs for {len(grads)} grads")
+        kinds = (torch.float32, torch.bfloat16)
+        _need(grads[0], "grads[0]", kinds, grads[0].dim() if isinstance(grads[0], torch.Tensor) else 1)
+        self.device = grads[0].device
+        rows = []
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            _need(g, f"grads[{i}]", kinds, g.dim() if isinstance(g, torch.Tensor) else 1, self.device)
+            _need(o, f"outs[{i}]", kinds, o.dim() if isinstance(o, torch.Tensor) else 1, self.device)
+            if o.numel() != g.numel():
+                raise ValueError(f"outs[{i}]: {o.numel()} entries instead of {g.numel()}")
+            if g.numel():
+                rows.append(B.cast_grad_t(g.data_ptr(), o.data_ptr(), g.numel(), g.dtype == torch.bfloat16, o.dtype == torch.bfloat16))
+        self.grads, self.outs = grads, outs
+        self._empty = not rows
+        if rows:
+            with torch.cuda.device(self.device):
+                rc, self._handle = B.cast_grads_create(rows)
+                B.check(rc)
+                rc, self._bytes = B.cast_grads_workspace(self._handle)
+                B.check(rc)
+
+    def _call(self, call) -> torch.Tensor:
+        if self._handle is None:
+            if not self._empty:
+                raise ValueError("the set is closed")
+            return torch.zeros((), dtype=torch.float32, device=self.device)
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        ws = torch.empty(self._bytes, dtype=torch.uint8, device=self.device)
+        _on(self.device, lambda stream: call(norm.data_ptr(), ws.data_ptr(), stream))
+        return norm
+
+    def norm(self, scale: float = 1.0) -> torch.Tensor:
+        """The norm of scale times all gradients, fp32 on the device."""
+        return self._call(lambda norm, ws, stream: B.cast_grads_norm(self._handle, scale, norm, ws, self._bytes, stream))
+
+    def clip(self, max_norm: float, scale: float = 1.0) -> torch.Tensor:
+        """outs = grads * scale * min(1, max_norm / norm); returns the norm (of scale times all gradients, before clipping)."""
+        return self._call(lambda norm, ws, stream: B.cast_grads_clip(self._handle, max_norm, scale, norm, ws, self._bytes, stream))
+
+    def close(self) -> None:
+        if self._handle is not None:
+            handle, self._handle = self._handle, None
+            B.check(B.cast_grads_destroy(handle))
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
