@@ -197,7 +197,7 @@ def load_library() -> ctypes.CDLL:
     lib.cast_rms_norm_grad_workspace.argtypes = [ctypes.c_int64, ctypes.c_int64, size_out]
     lib.cast_rms_norm_grad.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int] + [ctypes.c_void_p] * 3 + [ctypes.c_int64] * 2 + \
         [ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
-    lib.cast_rotary.argtypes = [ctypes.POINTER(cast_heads_t), ctypes.c_int] + [ctypes.c_void_p] * 3 + [ctypes.c_int] * 4 + [ctypes.c_int64] * 2 + [ctypes.c_void_p]
+    lib.cast_rotary.argtypes = [ctypes.c_void_p, ctypes.c_int] + [ctypes.c_void_p] * 3 + [ctypes.c_int] * 4 + [ctypes.c_int64] * 2 + [ctypes.c_void_p]
     lib.cast_grads_create.argtypes = [ctypes.POINTER(cast_grad_t), ctypes.c_int, ctypes.POINTER(ctypes.c_void_p)]
     lib.cast_grads_workspace.argtypes = [ctypes.c_void_p, size_out]
     lib.cast_grads_norm.argtypes = [ctypes.c_void_p, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]
@@ -482,10 +482,14 @@ def make_heads(x, out, heads, in_token_stride, in_head_stride, out_token_stride,
     return cast_heads_t(_ptr(x), _ptr(out), int(heads), int(in_token_stride), int(in_head_stride), int(out_token_stride), int(out_head_stride))
 
 
-def cast_rotary(sets: Sequence[cast_heads_t], positions, frequencies, axes, n_axes, pairs, adjacent, inverse, tokens, head_dim, stream=None) -> int:
-    n = len(sets)
-    arr = (cast_heads_t * max(n, 1))(*sets)
-    return load_library().cast_rotary(arr, n, _ptr(positions), _ptr(frequencies), _ptr(axes), int(n_axes), int(pairs), 1 if adjacent else 0,
+def cast_rotary(sets, positions, frequencies, axes, n_axes, pairs, adjacent, inverse, tokens, head_dim, stream=None) -> int:
+    """`sets`: a sequence of cast_heads_t, or the bytes of such an array."""
+    if isinstance(sets, bytes):
+        n = len(sets) // ctypes.sizeof(cast_heads_t)
+    else:
+        n = len(sets)
+        sets = (cast_heads_t * max(n, 1))(*sets)
+    return load_library().cast_rotary(sets, n, _ptr(positions), _ptr(frequencies), _ptr(axes), int(n_axes), int(pairs), 1 if adjacent else 0,
                                       1 if inverse else 0, int(tokens), int(head_dim), _stream(stream))
 
 

@@ -247,14 +247,63 @@ struct NormGradArgs {
     float eps;
 };
 
-template <int W, int N, bool SPLIT, bool RES, class WT>
-__global__ void __launch_bounds__(SPLIT ? (N == 4 || N == 32 ? 1024 : 512) : 256)
+// The rows of a CTA pass through a ring of kStages rows' worth of its threads' own accesses: with 16-byte accesses the copies go to shared
+// memory without waiting (cp.async: a thread reads only what it copied itself, so no barrier is needed), one access of one
+// column goes through registers, when its row's turn comes.
+__device__ __forceinline__ void copy_async(uint4* shared, const void* global, bool in)
+{
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(shared);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(global), "r"(in ? 16 : 0) : "memory");      // zeros where not `in`
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
+
+// Entries of one access of the row that is being worked on.
+template <int W, int N, int STAGES, bool RES>
+struct GradRow {
+    using A = Access<W>;
+    using Raw = typename A::Raw;
+    static constexpr int kArrays = RES ? 3 : 2;
+    Raw held[W == 8 ? 1 : kArrays * N];             // W == 1: the row's accesses
+    uint4* ring;                                     // W == 8: [STAGES][kArrays][N][threads]
+
+    static __device__ __forceinline__ const uint16_t* source(const NormGradArgs& a, int k) { return k == 0 ? a.h : k == 1 ? a.dy : a.dh; }
+    __device__ __forceinline__ void fetch(const NormGradArgs& a, int64_t row, int lane, int stage)
+    {
+        if constexpr (W == 8) {
+#pragma unroll
+            for (int k = 0; k < kArrays; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int c = i * a.lanes + lane;
+                    const bool in = row < a.tokens && c < a.units;
+                    copy_async(ring + ((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x, source(a, k) + (in ? row * a.dim + c * 8 : 0), in);
+                }
+            copies_commit();
+        } else {
+#pragma unroll
+            for (int k = 0; k < kArrays; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int c = i * a.lanes + lane;
+                    held[k * N + i] = A::zero();
+                    if (row < a.tokens && c < a.units) held[k * N + i] = source(a, k)[row * a.dim + c];
+                }
+        }
+    }
+    __device__ __forceinline__ void get(int k, int i, int stage, float (&v)[W]) const
+    {
+        if constexpr (W == 8) A::unpack(ring[((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x], v);
+        else A::unpack(held[k * N + i], v);
+    }
+};
+
+template <int W, int N, int STAGES, bool SPLIT, bool RES, class WT>
+__global__ void __launch_bounds__(SPLIT ? (W * N <= 16 ? 512 : 1024) : 256, SPLIT && W * N > 8 ? 1 : 2)
 rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
 {
     using A = Access<W>;
-    using Raw = typename A::Raw;
-    constexpr bool AHEAD = W * N <= 16;              // the next row in registers beside the current one
-    extern __shared__ float sums[];                  // !SPLIT: [rows of the CTA][dim]
+    extern __shared__ uint4 dynamic[];               // the ring; !SPLIT, afterwards: [rows of the CTA][dim] sums
     __shared__ float2 part[2][kMostWarps];
     __shared__ double part64[2][kMostWarps];
     const int lane = SPLIT ? (int)threadIdx.x : (int)threadIdx.x & (a.lanes - 1);
@@ -264,41 +313,42 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < W; ++j) dw[i][j] = 0.0f;
-    Raw dy[N], h[N], dh[N];
-    auto fetch = [&](int64_t row, Raw (&dy)[N], Raw (&h)[N], Raw (&dh)[N]) {
+    auto weight = [&](int i, float (&w)[W]) {
+        const int c = i * a.lanes + lane;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = i * a.lanes + lane;
-            dy[i] = h[i] = dh[i] = A::zero();
-            if (row < a.tokens && c < a.units) {
-                const int64_t at = row * a.dim + (int64_t)c * W;
-                dy[i] = *reinterpret_cast<const Raw*>(a.dy + at);
-                h[i] = *reinterpret_cast<const Raw*>(a.h + at);
-                if constexpr (RES) dh[i] = *reinterpret_cast<const Raw*>(a.dh + at);
-            }
-        }
+        for (int j = 0; j < W; ++j) w[j] = 0.0f;
+        if (c < a.units) A::weights(static_cast<const WT*>(a.weight) + c * W, w);
     };
+    constexpr bool KEPT = W * N <= 16;                // the weights of a thread's columns in registers
+    float kept[KEPT ? N : 1][W];
+    if constexpr (KEPT) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) weight(i, kept[i]);
+    }
     const int64_t step = (int64_t)gridDim.x * rows;
     int64_t row0 = (int64_t)blockIdx.x * rows;
-    fetch(row0 + sub, dy, h, dh);
-    for (int turn = 0; row0 < a.tokens; row0 += step, turn ^= 1) {
+    GradRow<W, N, STAGES, RES> x;
+    x.ring = dynamic;
+    if constexpr (W == 8) {
+#pragma unroll
+        for (int k = 0; k < STAGES - 1; ++k) x.fetch(a, row0 + sub + k * step, lane, k);
+    }
+    int stage = 0;
+    for (int turn = 0; row0 < a.tokens; row0 += step, turn ^= 1, stage = stage + 1 == STAGES ? 0 : stage + 1) {
         const int64_t row = row0 + sub;
-        Raw dy2[N], h2[N], dh2[N];
-        if constexpr (AHEAD) fetch(row + step, dy2, h2, dh2);
+        x.fetch(a, row + (W == 8 ? (STAGES - 1) * step : 0), lane, W == 8 ? (stage + STAGES - 1) % STAGES : 0);
+        if constexpr (W == 8) copies_wait<STAGES - 1>();
         float2 s = make_float2(0.0f, 0.0f);          // sums of h^2 and of g h
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = i * a.lanes + lane;
             float u[W], v[W], w[W];
-            A::unpack(h[i], u);
-            A::unpack(dy[i], v);
-#pragma unroll
-            for (int j = 0; j < W; ++j) w[j] = 0.0f;
-            if (c < a.units) A::weights(static_cast<const WT*>(a.weight) + c * W, w);
+            x.get(0, i, stage, u);
+            x.get(1, i, stage, v);
+            if constexpr (!KEPT) weight(i, w);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 s.x = fmaf(u[j], u[j], s.x);
-                s.y = fmaf(v[j] * w[j], u[j], s.y);
+                s.y = fmaf(v[j] * (KEPT ? kept[KEPT ? i : 0][j] : w[j]), u[j], s.y);
             }
         }
         for (int d = (SPLIT ? 32 : a.lanes) >> 1; d > 0; d >>= 1) {
@@ -323,13 +373,10 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             double s64 = 0.0, m64 = 0.0;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int c = i * a.lanes + lane;
                 float u[W], v[W], w[W];
-                A::unpack(h[i], u);
-                A::unpack(dy[i], v);
-#pragma unroll
-                for (int j = 0; j < W; ++j) w[j] = 0.0f;
-                if (c < a.units) A::weights(static_cast<const WT*>(a.weight) + c * W, w);
+                x.get(0, i, stage, u);
+                x.get(1, i, stage, v);
+                weight(i, w);
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
                     s64 = fma((double)u[j], (double)u[j], s64);
@@ -352,27 +399,22 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             const int c = i * a.lanes + lane;
             if (row >= a.tokens || c >= a.units) continue;
             float u[W], v[W], w[W], o[W];
-            A::unpack(h[i], u);
-            A::unpack(dy[i], v);
-            A::weights(static_cast<const WT*>(a.weight) + c * W, w);
-            if constexpr (RES) A::unpack(dh[i], o);
+            x.get(0, i, stage, u);
+            x.get(1, i, stage, v);
+            if constexpr (!KEPT) weight(i, w);
+            if constexpr (RES) x.get(2, i, stage, o);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 const float n = u[j] * pre * scaled;
                 dw[i][j] = fmaf(v[j], n, dw[i][j]);
-                const float d = fmaf(v[j], w[j], -n * m);
+                const float d = fmaf(v[j], KEPT ? kept[KEPT ? i : 0][j] : w[j], -n * m);
                 o[j] = RES ? fmaf(r, d, o[j]) : r * d;
             }
-            *reinterpret_cast<Raw*>(a.dx + row * a.dim + (int64_t)c * W) = A::pack(o);
-        }
-        if constexpr (AHEAD) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) { dy[i] = dy2[i]; h[i] = h2[i]; dh[i] = dh2[i]; }
-        } else if (row0 + step < a.tokens) {
-            fetch(row + step, dy, h, dh);
+            *reinterpret_cast<typename A::Raw*>(a.dx + row * a.dim + (int64_t)c * W) = A::pack(o);
         }
     }
     chain_next();
+    if constexpr (W == 8) copies_wait<0>();
     if (!a.partial) return;
     float* out = a.partial + (int64_t)blockIdx.x * a.dim;
     if constexpr (SPLIT) {
@@ -380,10 +422,17 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
         for (int i = 0; i < N; ++i) {
             const int c = i * a.lanes + lane;
             if (c >= a.units) continue;
-#pragma unroll
-            for (int j = 0; j < W; ++j) out[c * W + j] = dw[i][j];
+            if constexpr (W == 8) {
+                float4* q = reinterpret_cast<float4*>(out + c * 8);
+                q[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
+                q[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
+            } else {
+                out[c] = dw[i][0];
+            }
         }
     } else {
+        float* sums = reinterpret_cast<float*>(dynamic);
+        __syncthreads();                             // the ring has been read
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = i * a.lanes + lane;
@@ -401,44 +450,50 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
 }
 
 // dweight[c] = sum of `rows` partial rows: 32 columns per CTA, its warps share the rows.
-constexpr int kJoinWarps = 16;
+constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
 join_weight_grad_kernel(const float* partial, float* out, int32_t rows, int32_t dim)
 {
-    __shared__ float sums[kJoinWarps][32];
+    __shared__ float sums[kJoinWarps][33];
     chain_next();
     chain_wait();
     const int lane = (int)threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float v = 0.0f;
     if (c < dim) {
-#pragma unroll 4
+#pragma unroll 8
         for (int r = warp; r < rows; r += kJoinWarps) v += __ldcg(partial + (int64_t)r * dim + c);
     }
     sums[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && c < dim) {
-        v = sums[0][lane];
+    v = sums[lane][warp];                            // warp w adds up column w
 #pragma unroll
-        for (int i = 1; i < kJoinWarps; ++i) v += sums[i][lane];
-        out[c] = v;
-    }
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    const int64_t own = (int64_t)blockIdx.x * 32 + warp;
+    if (lane == 0 && own < dim) out[own] = v;
 }
 
-Spread grad_spread_of(int64_t units, int w)
+struct GradSpread {
+    Spread s;
+    int stages;
+};
+
+GradSpread grad_spread_of(int64_t units, int w)
 {
     if (w == 8) {
-        if (units <= 64) {                    // up to 512 columns: in a warp
+        if (units <= 128) {                   // up to 1024 columns: in a warp
             int lanes = 8;
             while (lanes < 32 && lanes < units) lanes *= 2;
-            return {lanes, units <= lanes ? 1 : 2, false};
+            const int n = (int)((units + lanes - 1) / lanes);
+            return {{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4, false}, n <= 2 ? 4 : 2};
         }
+        // stages of 48 bytes for each access: 96 KB a CTA (two of them on an SM), 192 KB for wider rows (one)
         const int n = units <= 512 ? 1 : units <= 1024 ? 2 : 4;
-        return {(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true};
+        return {{(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true}, units <= 1024 ? 4 : units <= 2048 ? 2 : 1};
     }
-    if (units <= 256) return {32, 8, false};
+    if (units <= 256) return {{32, 8, false}, 1};
     const int n = units <= 4096 ? 8 : 32;
-    return {(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true};
+    return {{(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true}, 1};
 }
 
 int sm_count(int* sms)
@@ -452,32 +507,34 @@ int sm_count(int* sms)
 // CTAs of the gradient kernel: what the SMs hold at a time, and no more than there are groups of rows.
 int64_t grad_ctas(const Spread& s, int64_t tokens, int sms)
 {
-    const int threads = s.split ? s.lanes : 256;
-    const int64_t rows = s.split ? 1 : threads / s.lanes, groups = (tokens + rows - 1) / rows;
-    const int64_t held = (int64_t)sms * (threads >= 1024 ? 1 : 1024 / threads);
+    const int64_t rows = s.split ? 1 : 256 / s.lanes, groups = (tokens + rows - 1) / rows;
+    const int64_t held = (int64_t)sms * (s.split && s.n * s.lanes > 512 ? 1 : 2);
     return groups < held ? groups : held;
 }
 
 // Workspace for either width of access: which one a call takes depends on its pointers.
 uint64_t grad_workspace(int64_t tokens, int64_t dim, int sms)
 {
-    const int64_t wide = dim % 8 == 0 ? grad_ctas(grad_spread_of(dim / 8, 8), tokens, sms) : 0, one = grad_ctas(grad_spread_of(dim, 1), tokens, sms);
+    const int64_t wide = dim % 8 == 0 ? grad_ctas(grad_spread_of(dim / 8, 8).s, tokens, sms) : 0, one = grad_ctas(grad_spread_of(dim, 1).s, tokens, sms);
     return sizeof(float) * (uint64_t)(wide > one ? wide : one) * (uint64_t)dim;
 }
 
-template <int W, int N, bool SPLIT, bool RES, class WT>
+template <int W, int N, int STAGES, bool SPLIT, bool RES, class WT>
 int launch_grad(const NormGradArgs& a, unsigned ctas, cudaStream_t stream)
 {
     const unsigned threads = SPLIT ? (unsigned)a.lanes : 256u;
-    const size_t smem = SPLIT || !a.partial ? 0 : sizeof(float) * (threads / a.lanes) * (size_t)a.dim;
-    return launch_chained(true, rms_norm_grad_kernel<W, N, SPLIT, RES, WT>, dim3(ctas), threads, smem, stream, 1, a);
+    const size_t ring = W == 8 ? (size_t)STAGES * (RES ? 3 : 2) * N * threads * 16 : 0, sums = SPLIT ? 0 : sizeof(float) * (threads / a.lanes) * (size_t)a.dim;
+    const size_t smem = ring > sums ? ring : sums;
+    const auto kernel = rms_norm_grad_kernel<W, N, STAGES, SPLIT, RES, WT>;
+    if (smem > 40960) CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    return launch_chained(true, kernel, dim3(ctas), threads, smem, stream, 1, a);
 }
 
-template <int W, int N, bool SPLIT>
+template <int W, int N, int STAGES, bool SPLIT>
 int launch_grad(const NormGradArgs& a, bool weight_fp32, unsigned ctas, cudaStream_t stream)
 {
-    if (a.dh) return weight_fp32 ? launch_grad<W, N, SPLIT, true, float>(a, ctas, stream) : launch_grad<W, N, SPLIT, true, uint16_t>(a, ctas, stream);
-    return weight_fp32 ? launch_grad<W, N, SPLIT, false, float>(a, ctas, stream) : launch_grad<W, N, SPLIT, false, uint16_t>(a, ctas, stream);
+    if (a.dh) return weight_fp32 ? launch_grad<W, N, STAGES, SPLIT, true, float>(a, ctas, stream) : launch_grad<W, N, STAGES, SPLIT, true, uint16_t>(a, ctas, stream);
+    return weight_fp32 ? launch_grad<W, N, STAGES, SPLIT, false, float>(a, ctas, stream) : launch_grad<W, N, STAGES, SPLIT, false, uint16_t>(a, ctas, stream);
 }
 
 int check_norm(const void* weight, int weight_fp32, int64_t tokens, int64_t dim, float eps)
@@ -579,7 +636,8 @@ extern "C" int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, c
     const int w = dim % 8 == 0 && aligned(grad_y, 16) && aligned(h, 16) && aligned(grad_h, 16) && aligned(grad_x, 16) && aligned(weight, 16) ? 8 : 1;
     NormGradArgs a = {grad_y, h, grad_h, weight, grad_x, grad_weight ? static_cast<float*>(workspace) : nullptr, (int32_t)tokens, (int32_t)dim,
                       (int32_t)(dim / w), 0, eps};
-    const Spread s = grad_spread_of(a.units, w);
+    const GradSpread g = grad_spread_of(a.units, w);
+    const Spread& s = g.s;
     a.lanes = s.lanes;
     const unsigned ctas = (unsigned)grad_ctas(s, tokens, sms);
     if (grad_weight && workspace_bytes < grad_workspace(tokens, dim, sms)) return CAST_ERR_PLAN;
@@ -588,10 +646,14 @@ extern "C" int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, c
     const bool f = weight_fp32 != 0;
     const cudaStream_t st = (cudaStream_t)stream;
     if (w == 8) {
-        if (!s.split) rc = s.n == 1 ? launch_grad<8, 1, false>(a, f, ctas, st) : launch_grad<8, 2, false>(a, f, ctas, st);
-        else rc = s.n == 1 ? launch_grad<8, 1, true>(a, f, ctas, st) : s.n == 2 ? launch_grad<8, 2, true>(a, f, ctas, st) : launch_grad<8, 4, true>(a, f, ctas, st);
+        if (!s.split)
+            rc = s.n == 1 ? launch_grad<8, 1, 4, false>(a, f, ctas, st) : s.n == 2 ? launch_grad<8, 2, 4, false>(a, f, ctas, st) : launch_grad<8, 4, 2, false>(a, f, ctas, st);
+        else if (s.n <= 2)
+            rc = s.n == 1 ? launch_grad<8, 1, 4, true>(a, f, ctas, st) : launch_grad<8, 2, 4, true>(a, f, ctas, st);
+        else
+            rc = g.stages == 2 ? launch_grad<8, 4, 2, true>(a, f, ctas, st) : launch_grad<8, 4, 1, true>(a, f, ctas, st);
     } else {
-        rc = !s.split ? launch_grad<1, 8, false>(a, f, ctas, st) : s.n == 8 ? launch_grad<1, 8, true>(a, f, ctas, st) : launch_grad<1, 32, true>(a, f, ctas, st);
+        rc = !s.split ? launch_grad<1, 8, 1, false>(a, f, ctas, st) : s.n == 8 ? launch_grad<1, 8, 1, true>(a, f, ctas, st) : launch_grad<1, 32, 1, true>(a, f, ctas, st);
     }
     if (rc != CAST_OK || !grad_weight) return rc;
     return launch_chained(false, join_weight_grad_kernel, dim3((unsigned)((dim + 31) / 32)), 32 * kJoinWarps, 0, st, 1, (const float*)a.partial, grad_weight,

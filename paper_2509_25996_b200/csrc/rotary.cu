@@ -18,8 +18,17 @@ namespace {
 constexpr int kMostSets = 4;              // arrays of heads turned by one call (queries, keys, ...)
 constexpr int kMostPairs = 512;
 constexpr int kTurnThreads = 256;
-constexpr int kItems = 4;                 // units of a thread
-constexpr int kAngles = 2048;             // cosines and sines of a CTA (16 KB)
+constexpr int kItems = 4;                 // units that a thread has in flight
+constexpr int kBatch = kTurnThreads * kItems;
+constexpr int kAngles = 1024;             // cosines and sines of a CTA (8 KB)
+constexpr int kMostUnits = 16384;         // of a CTA
+
+// i / d for i < 2^16, d < 2^16
+struct Divisor {
+    uint32_t d, magic;
+};
+Divisor divisor(uint32_t d) { return {d, d > 1 ? (uint32_t)(0x100000000ull / d + 1) : 0u}; }
+__device__ __forceinline__ uint32_t divide(uint32_t i, Divisor v) { return v.d > 1 ? __umulhi(i, v.magic) : i; }
 
 struct HeadSet {
     const uint16_t* in;
@@ -36,7 +45,9 @@ struct RotaryArgs {
     int32_t sets, heads;              // heads of all sets together
     int32_t tokens, n_axes, pairs;
     int32_t turned;                   // units of a head that turn; each holds W pairs (halves) or W columns (adjacent)
-    int32_t units;                    // and with those that are copied
+    Divisor units;                    // and with those that are copied
+    Divisor token_units;              // of a token in a CTA (of the last CTA of a token's heads: fewer)
+    Divisor pair_count;
     int32_t tile_tokens, tile_heads;  // of a CTA
     int32_t head_tiles;
     float sign;
@@ -49,38 +60,44 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
     // one column per access cannot hold an adjacent pair: two accesses then, too
     constexpr bool TWO = !ADJACENT || W == 1;
+    constexpr int P = W == 1 ? 1 : ADJACENT ? W / 2 : W;        // pairs of a unit
     using A = Access<W>;
     using Raw = typename A::Raw;
-    __shared__ float2 angle[kAngles];
+    // [token][pair of a unit / 2][unit][2]: neighbouring units, which neighbouring threads hold, lie side by side
+    __shared__ __align__(16) float2 angle[kAngles];
     const int64_t token0 = (int64_t)(blockIdx.x / a.head_tiles) * a.tile_tokens;
     const int head0 = (int)(blockIdx.x % a.head_tiles) * a.tile_heads;
     const int tokens = (int)min((int64_t)a.tile_tokens, a.tokens - token0), heads = min(a.tile_heads, a.heads - head0);
-    const int per_token = heads * a.units, total = tokens * per_token;
+    const uint32_t total = (uint32_t)tokens * (uint32_t)heads * a.units.d;
     Raw x[kItems], y[TWO ? kItems : 1];
     uint16_t* dst[kItems];
-    int place[kItems];                    // of the unit's first angle, -1: a copy, -2: none
+    int place[kItems];                    // of the unit's first angles, -1: a copy, -2: none
+    auto fetch = [&](uint32_t first) {
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        const int i = (int)threadIdx.x + k * kTurnThreads;
-        place[k] = -2;
-        if (i >= total) continue;
-        const int t = i / per_token, rest = i - t * per_token, hd = rest / a.units, u = rest - hd * a.units, head = head0 + hd;
-        int s = 0;
-        while (s + 1 < a.sets && head >= a.set[s + 1].first) ++s;
-        const HeadSet& hs = a.set[s];
-        const int64_t token = token0 + t, own = head - hs.first;
-        const bool turns = u < a.turned;
-        // the unit's first column
-        const int col = turns ? (ADJACENT ? u * (W == 1 ? 2 : W) : u * W) : 2 * a.pairs + (u - a.turned) * W;
-        const uint16_t* src = hs.in + token * hs.in_token + own * hs.in_head + col;
-        dst[k] = hs.out + token * hs.out_token + own * hs.out_head + col;
-        place[k] = turns ? t * a.pairs + (ADJACENT && W > 1 ? u * (W / 2) : u * W) : -1;
-        x[k] = *reinterpret_cast<const Raw*>(src);
-        if constexpr (TWO)
-            if (turns) y[k] = *reinterpret_cast<const Raw*>(src + (ADJACENT ? 1 : a.pairs));
-    }
-    for (int i = (int)threadIdx.x; i < tokens * a.pairs; i += kTurnThreads) {
-        const int t = i / a.pairs, p = i - t * a.pairs;
+        for (int k = 0; k < kItems; ++k) {
+            const uint32_t i = first + threadIdx.x + k * kTurnThreads;
+            place[k] = -2;
+            if (i >= total) continue;
+            // several tokens only with all of their heads: token_units is theirs then
+            const uint32_t t = a.tile_tokens > 1 ? divide(i, a.token_units) : 0u, rest = i - t * a.token_units.d, hd = divide(rest, a.units);
+            const int u = (int)(rest - hd * a.units.d), head = head0 + (int)hd;
+            int s = 0;
+            while (s + 1 < a.sets && head >= a.set[s + 1].first) ++s;
+            const HeadSet& hs = a.set[s];
+            const int64_t token = token0 + t, own = head - hs.first;
+            const bool turns = u < a.turned;
+            const int col = turns ? (ADJACENT ? u * 2 * P : u * W) : 2 * a.pairs + (u - a.turned) * W;      // the unit's first column
+            const uint16_t* src = hs.in + token * hs.in_token + own * hs.in_head + col;
+            dst[k] = hs.out + token * hs.out_token + own * hs.out_head + col;
+            place[k] = turns ? (int)t * a.pairs + u * (P > 1 ? 2 : 1) : -1;
+            x[k] = *reinterpret_cast<const Raw*>(src);
+            if constexpr (TWO)
+                if (turns) y[k] = *reinterpret_cast<const Raw*>(src + (ADJACENT ? 1 : a.pairs));
+        }
+    };
+    fetch(0);
+    for (uint32_t i = threadIdx.x; i < (uint32_t)(tokens * a.pairs); i += kTurnThreads) {
+        const uint32_t t = divide(i, a.pair_count), p = i - t * a.pairs;
         const uint32_t axis = a.axes ? (uint32_t)__ldg(a.axes + p) : 0u;
         float2 cs = make_float2(1.0f, 0.0f);              // a pair of no axis does not turn
         if (axis < (uint32_t)a.n_axes) {
@@ -88,58 +105,71 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
             sincospif(2.0f * (float)(turns - rint(turns)), &cs.y, &cs.x);
             cs.y *= a.sign;
         }
-        angle[i] = cs;
+        angle[t * a.pairs + (P > 1 ? (p % P / 2 * a.turned + p / P) * 2 + p % 2 : p)] = cs;
     }
     __syncthreads();
+    for (uint32_t first = 0;;) {
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        if (place[k] == -2) continue;
-        if (place[k] == -1) {
-            *reinterpret_cast<Raw*>(dst[k]) = x[k];
-            continue;
-        }
-        float u[W], v[W];
-        A::unpack(x[k], u);
-        if constexpr (TWO) {
-            A::unpack(y[k], v);
+        for (int k = 0; k < kItems; ++k) {
+            if (place[k] == -2) continue;
+            if (place[k] == -1) {
+                *reinterpret_cast<Raw*>(dst[k]) = x[k];
+                continue;
+            }
+            float u[W], v[W];
+            A::unpack(x[k], u);
+            if constexpr (TWO) A::unpack(y[k], v);
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float2 cs = angle[place[k] + j];
-                const float p = u[j], q = v[j];
-                u[j] = p * cs.x - q * cs.y;
-                v[j] = p * cs.y + q * cs.x;
+            for (int j = 0; j < P; j += 2) {
+                float4 cs;
+                if constexpr (P > 1) {
+                    cs = *reinterpret_cast<const float4*>(angle + place[k] + j * a.turned);
+                } else {
+                    const float2 one = angle[place[k]];
+                    cs = make_float4(one.x, one.y, 0.0f, 0.0f);
+                }
+#pragma unroll
+                for (int e = 0; e < (P > 1 ? 2 : 1); ++e) {
+                    const float c = e ? cs.z : cs.x, s = e ? cs.w : cs.y;
+                    float& p = TWO ? u[j + e] : u[(2 * (j + e)) % W];
+                    float& q = TWO ? v[j + e] : u[(2 * (j + e) + 1) % W];
+                    const float p0 = p, q0 = q;
+                    p = p0 * c - q0 * s;
+                    q = p0 * s + q0 * c;
+                }
             }
             *reinterpret_cast<Raw*>(dst[k]) = A::pack(u);
-            *reinterpret_cast<Raw*>(dst[k] + (ADJACENT ? 1 : a.pairs)) = A::pack(v);
-        } else {
-#pragma unroll
-            for (int j = 0; j < W / 2; ++j) {
-                const float2 cs = angle[place[k] + j];
-                const float p = u[2 * j], q = u[2 * j + 1];
-                u[2 * j] = p * cs.x - q * cs.y;
-                u[2 * j + 1] = p * cs.y + q * cs.x;
-            }
-            *reinterpret_cast<Raw*>(dst[k]) = A::pack(u);
+            if constexpr (TWO) *reinterpret_cast<Raw*>(dst[k] + (ADJACENT ? 1 : a.pairs)) = A::pack(v);
         }
+        first += kBatch;
+        if (first >= total) break;
+        fetch(first);
     }
 }
 
 template <int W, bool ADJACENT>
-int launch_rotary(RotaryArgs a, int64_t head_dim, cudaStream_t stream)
+int launch_rotary(RotaryArgs a, int64_t head_dim, int sms, cudaStream_t stream)
 {
-    a.turned = ADJACENT ? (W == 1 ? a.pairs : 2 * a.pairs / W) : a.pairs / W;
-    a.units = a.turned + (int)((head_dim - 2 * a.pairs) / W);
-    // As many tokens as fill the CTA's units and leave their angles in shared memory; a token of more units is shared by CTAs.
-    constexpr int room = kTurnThreads * kItems;
-    const int64_t token_units = (int64_t)a.heads * a.units;
-    if (token_units <= room) {
-        a.tile_heads = a.heads;
-        a.tile_tokens = (int)(room / token_units);
-        if (a.tile_tokens > kAngles / a.pairs) a.tile_tokens = kAngles / a.pairs;
+    a.turned = W == 1 ? a.pairs : ADJACENT ? 2 * a.pairs / W : a.pairs / W;
+    const int units = a.turned + (int)((head_dim - 2 * a.pairs) / W);
+    // Several tokens per CTA, so that their angles keep its threads busy, but not so many that SMs stay idle; a token of more units
+    // than a batch is shared by CTAs where there are few tokens, and where its units exceed a CTA's most.
+    const int64_t token_units = (int64_t)a.heads * units, wanted = (int64_t)sms * 8;
+    a.tile_heads = a.heads;
+    a.tile_tokens = 1;
+    if (token_units > kMostUnits || (token_units > kBatch && a.tokens < wanted)) {
+        const int64_t pieces = (token_units + kBatch - 1) / kBatch;
+        a.tile_heads = (int)((a.heads + pieces - 1) / pieces);
     } else {
-        a.tile_tokens = 1;
-        a.tile_heads = room / a.units;        // at least 1: a head has at most 1024 columns
+        int64_t most = kAngles / a.pairs;
+        if (most > kMostUnits / token_units) most = kMostUnits / token_units;
+        if (most > 4096 / token_units + 1) most = 4096 / token_units + 1;
+        if (most > a.tokens / wanted) most = a.tokens / wanted;
+        if (most > 1) a.tile_tokens = (int)most;
     }
+    a.units = divisor((uint32_t)units);
+    a.token_units = divisor((uint32_t)(a.tile_heads * units));
+    a.pair_count = divisor((uint32_t)a.pairs);
     a.head_tiles = (a.heads + a.tile_heads - 1) / a.tile_heads;
     const int64_t grid = (int64_t)((a.tokens + a.tile_tokens - 1) / a.tile_tokens) * a.head_tiles;
     if (grid > 0x7FFFFFFF) return CAST_ERR_SHAPE;
@@ -241,6 +271,9 @@ extern "C" int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* 
     a.pairs = pairs;
     a.sign = inverse ? -1.0f : 1.0f;
     const cudaStream_t st = (cudaStream_t)stream;
-    if (vec) return adjacent ? launch_rotary<8, true>(a, head_dim, st) : launch_rotary<8, false>(a, head_dim, st);
-    return adjacent ? launch_rotary<1, true>(a, head_dim, st) : launch_rotary<1, false>(a, head_dim, st);
+    int device = 0, sms = 0;
+    CAST_CUDA_TRY(cudaGetDevice(&device));
+    CAST_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    if (vec) return adjacent ? launch_rotary<8, true>(a, head_dim, sms, st) : launch_rotary<8, false>(a, head_dim, sms, st);
+    return adjacent ? launch_rotary<1, true>(a, head_dim, sms, st) : launch_rotary<1, false>(a, head_dim, sms, st);
 }

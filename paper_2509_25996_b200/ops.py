@@ -9,7 +9,9 @@ refused while torch records one, not dropped from it silently.
 """
 from __future__ import annotations
 
+import functools
 import math
+import struct
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -167,8 +169,8 @@ def _rows(x: torch.Tensor, weight: torch.Tensor, first: str) -> Tuple[int, int]:
     _need(x, first, torch.bfloat16, x.dim() if isinstance(x, torch.Tensor) else 1)
     _need(weight, "weight", (torch.float32, torch.bfloat16), 1, x.device)
     dim = x.shape[-1]
-    if weight.shape[0] != dim:
-        raise ValueError(f"weight: {weight.shape[0]} entries for {dim} columns")
+    if weight.numel() != dim:
+        raise ValueError(f"weight: {weight.numel()} entries for {dim} columns")
     return (x.numel() // dim if dim else 0), dim
 
 
@@ -177,6 +179,10 @@ def _like(t: Optional[torch.Tensor], name: str, x: torch.Tensor) -> None:
         _need(t, name, torch.bfloat16, x.dim(), x.device)
         if t.shape != x.shape:
             raise ValueError(f"{name}: shape {tuple(t.shape)} instead of {tuple(x.shape)}")
+
+
+def _bytes_on(device: torch.device, n: int) -> torch.Tensor:
+    return torch.empty_strided((n,), (1,), dtype=torch.uint8, device=device)
 
 
 def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, out: Optional[torch.Tensor] = None,
@@ -216,6 +222,14 @@ def rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.
     return q, scales, h
 
 
+@functools.lru_cache(maxsize=1024)
+def _rms_norm_grad_bytes(tokens: int, dim: int, device_index: int) -> int:
+    """Workspace on the current device, whose index the caller names."""
+    rc, n = B.cast_rms_norm_grad_workspace(tokens, dim)
+    B.check(rc)
+    return n
+
+
 def rms_norm_grad(grad_y: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, grad_h: Optional[torch.Tensor] = None, eps: float = 1e-6,
                   weight_grad: bool = True, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(grad_x bf16, grad_weight fp32 or None) of rms_norm from the h it returned.  grad_h: the gradient that reaches h from what
@@ -225,11 +239,11 @@ def rms_norm_grad(grad_y: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, g
     _like(grad_h, "grad_h", h)
     _like(out, "out", h)
     gx = torch.empty_like(h) if out is None else out
-    gw = weight.new_empty(dim, dtype=torch.float32) if weight_grad else None
+    gw = torch.empty_like(weight, dtype=torch.float32) if weight_grad else None
     if tokens == 0:
         return gx, gw.zero_() if gw is not None else None
     def call(stream):
-        ws = _workspace(B.cast_rms_norm_grad_workspace(tokens, dim), h) if weight_grad else None             # depends on the device
+        ws = _bytes_on(h.device, _rms_norm_grad_bytes(tokens, dim, h.device.index)) if weight_grad else None
         return B.cast_rms_norm_grad(grad_y.data_ptr(), h.data_ptr(), weight.data_ptr(), weight.dtype == torch.float32,
                                     None if grad_h is None else grad_h.data_ptr(), gx.data_ptr(), None if gw is None else gw.data_ptr(), tokens, dim, eps,
                                     None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream)
@@ -288,7 +302,7 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, 
     if spectrum.frequencies.device != dev:
         raise ValueError(f"spectrum: on {spectrum.frequencies.device} instead of {dev}")
     results: List[Optional[torch.Tensor]] = []
-    sets = []
+    sets = b""
     head_dim = q.shape[-1] if isinstance(q, torch.Tensor) and q.dim() else 0
     for i, (x, name) in enumerate(((q, "q"), (k, "k"))):
         if x is None and i == 1:
@@ -296,15 +310,16 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, 
                 raise ValueError("out[1]: there is no k")
             results.append(None)
             continue
-        _need_heads(x, name, dev, (tokens, None, head_dim))
+        heads, from_token, from_head = _need_heads(x, name, dev, tokens, None, head_dim)
         if out is None:
-            o = x.new_empty(x.shape)
+            o = torch.empty_like(x, memory_format=torch.contiguous_format)
+            to_token, to_head = heads * head_dim, head_dim
         else:
             o = out[i]
-            _need_heads(o, f"out[{i}]", dev, tuple(x.shape))
+            _, to_token, to_head = _need_heads(o, f"out[{i}]", dev, tokens, heads, head_dim)
         results.append(o)
-        if x.shape[1]:
-            sets.append(B.cast_heads_t(x.data_ptr(), o.data_ptr(), x.shape[1], x.stride(0), x.stride(1), o.stride(0), o.stride(1)))
+        if heads:
+            sets += struct.pack("7q", x.data_ptr(), o.data_ptr(), heads, from_token, from_head, to_token, to_head)      # a cast_heads_t
     if 2 * spectrum.pairs > head_dim:
         raise ValueError(f"spectrum: {2 * spectrum.pairs} columns of heads of {head_dim}")
     if tokens and sets:
@@ -313,19 +328,23 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, 
     return results[0], results[1]
 
 
-def _need_heads(t: torch.Tensor, name: str, device, shape) -> None:
+def _need_heads(t: torch.Tensor, name: str, device, tokens: int, heads: Optional[int], head_dim: int) -> Tuple[int, int, int]:
+    """(heads, token stride, head stride) of an array of heads."""
     if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name}: requires a gradient, but results carry no autograd graph (call under torch.no_grad(), or pass it detached)")
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed")
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16:
         raise ValueError(f"{name}: {t.dtype} is not {torch.bfloat16}")
     if t.device != device:
         raise ValueError(f"{name}: on {t.device} instead of {device}")
-    if t.dim() != 3 or t.shape[0] != shape[0] or t.shape[2] != shape[2] or shape[1] not in (None, t.shape[1]):
-        raise ValueError(f"{name}: shape {tuple(t.shape)} instead of {tuple('heads' if s is None else s for s in shape)}")
-    if t.stride(2) != 1 and t.shape[2] > 1:
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != head_dim or heads not in (None, shape[1]):
+        raise ValueError(f"{name}: shape {tuple(shape)} instead of {(tokens, 'heads' if heads is None else heads, head_dim)}")
+    token_stride, head_stride, column_stride = t.stride()
+    if column_stride != 1 and head_dim > 1:
         raise ValueError(f"{name}: the columns of a head are not contiguous")
+    return shape[1], token_stride, head_stride
 
 
 class GradientSet:
@@ -366,8 +385,8 @@ class GradientSet:
             if not self._empty:
                 raise ValueError("the set is closed")
             return torch.zeros((), dtype=torch.float32, device=self.device)
-        norm = torch.empty((), dtype=torch.float32, device=self.device)
-        ws = torch.empty(self._bytes, dtype=torch.uint8, device=self.device)
+        norm = torch.empty_strided((), (), dtype=torch.float32, device=self.device)
+        ws = _bytes_on(self.device, self._bytes)
         _on(self.device, lambda stream: call(norm.data_ptr(), ws.data_ptr(), stream))
         return norm
 
