@@ -45,4 +45,46 @@ template <> struct Access<1> {
     static __device__ __forceinline__ void weights(const float* p, float (&v)[1]) { v[0] = __ldg(p); }
 };
 
+// Two fp32 operations by one instruction.
+__device__ __forceinline__ uint64_t bits(float2 v) { return (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x); }
+__device__ __forceinline__ float2 float2_of(uint64_t b) { return make_float2(__uint_as_float((uint32_t)b), __uint_as_float((uint32_t)(b >> 32))); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return float2_of(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return float2_of(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return float2_of(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// The columns of a 16-byte access as pairs.
+struct Pairs {
+    static __device__ __forceinline__ void unpack(const uint4& r, float2 (&v)[4])
+    {
+        v[0] = make_float2(bf16_low(r.x), bf16_high(r.x)); v[1] = make_float2(bf16_low(r.y), bf16_high(r.y));
+        v[2] = make_float2(bf16_low(r.z), bf16_high(r.z)); v[3] = make_float2(bf16_low(r.w), bf16_high(r.w));
+    }
+    static __device__ __forceinline__ uint4 pack(const float2 (&v)[4])
+    {
+        return make_uint4(bf16_pair(v[0].x, v[0].y), bf16_pair(v[1].x, v[1].y), bf16_pair(v[2].x, v[2].y), bf16_pair(v[3].x, v[3].y));
+    }
+    static __device__ __forceinline__ void weights(const uint16_t* p, float2 (&v)[4]) { unpack(__ldg(reinterpret_cast<const uint4*>(p)), v); }
+    static __device__ __forceinline__ void weights(const float* p, float2 (&v)[4])
+    {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+        v[0] = make_float2(a.x, a.y); v[1] = make_float2(a.z, a.w); v[2] = make_float2(b.x, b.y); v[3] = make_float2(b.z, b.w);
+    }
+};
+
 }  // namespace cast

@@ -40,6 +40,7 @@ struct NormArgs {
     int32_t units;            // accesses of a row
     int32_t lanes;            // threads of a row
     float eps;
+    float inverse_dim;
 };
 
 // Sum over the `lanes` threads of a row (all of the CTA with SPLIT); every one of them gets it, summed in the same order.
@@ -62,6 +63,24 @@ __device__ __forceinline__ T row_sum(T v, int lanes, T* shared)
 __device__ __forceinline__ bool odd_row(float mean_eps) { return !(mean_eps < 0x1p100f && mean_eps > 0x1p-100f); }
 // A power of two that brings the entries of such a row back into the range: 1/sqrt(mean) = pre * (1/sqrt(mean) / pre).
 __device__ __forceinline__ float odd_factor(double mean_eps) { return mean_eps < 1.0 ? 0x1p64f : 0x1p-64f; }
+
+// A thread's sums of h^2 and of weight dy h (dy may be NULL) over its columns of such a row, in fp64 and from memory again: rare, and
+// outside of what the other rows' code keeps in registers.
+template <int W>
+__device__ __noinline__ double2 odd_sums(const uint16_t* h, const uint16_t* dy, const void* weight, bool weight_fp32, int dim, int lanes, int lane)
+{
+    double hh = 0.0, gh = 0.0;
+    for (int c = lane * W; c < dim; c += lanes * W)
+        for (int j = 0; j < W; ++j) {
+            const double v = (double)bf16_low(h[c + j]);
+            hh = fma(v, v, hh);
+            if (dy) {
+                const double w = (double)(weight_fp32 ? static_cast<const float*>(weight)[c + j] : bf16_low(static_cast<const uint16_t*>(weight)[c + j]));
+                gh = fma((double)bf16_low(dy[c + j]) * w, v, gh);
+            }
+        }
+    return make_double2(hh, gh);
+}
 
 // Two e4m3 values, the first in the low byte; beyond +-448 only by a rounding, NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi)
@@ -132,7 +151,7 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
         for (int j = 0; j < W; ++j) square = fmaf(v[j], v[j], square);
     }
-    const float mean = row_sum<SPLIT>(square, a.lanes, part) / (float)a.dim + a.eps;
+    const float mean = fmaf(row_sum<SPLIT>(square, a.lanes, part), a.inverse_dim, a.eps);
     float r = __frsqrt_rn(mean), pre = 1.0f;
     if (SPLIT ? odd_row(mean) : __any_sync(0xFFFFFFFFu, odd_row(mean))) {
         double s = 0.0;
@@ -198,8 +217,7 @@ Spread spread_of(int64_t units, int w)
         if (units <= 128) {                   // up to 1024 columns: in a warp
             int lanes = 8;
             while (lanes < 32 && lanes < units) lanes *= 2;
-            const int n = (int)((units + lanes - 1) / lanes);
-            return {lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4, false};
+            return {lanes, (int)((units + lanes - 1) / lanes), false};
         }
         const int n = units <= 512 ? 1 : units <= 2048 ? 2 : 4;
         return {(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true};
@@ -244,149 +262,187 @@ struct NormGradArgs {
     int32_t dim;
     int32_t units;
     int32_t lanes;
+    int32_t window;           // W == 1: entries of shared memory for a row of one array
     float eps;
+    float inverse_dim;
 };
 
-// The rows of a CTA pass through a ring of kStages rows' worth of its threads' own accesses: with 16-byte accesses the copies go to shared
-// memory without waiting (cp.async: a thread reads only what it copied itself, so no barrier is needed), one access of one
-// column goes through registers, when its row's turn comes.
-__device__ __forceinline__ void copy_async(uint4* shared, const void* global, bool in)
+__device__ __forceinline__ void copy_async(void* shared, const void* global, int bytes)      // 16 bytes, those beyond `bytes` as zeros
 {
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(shared);
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(global), "r"(in ? 16 : 0) : "memory");      // zeros where not `in`
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(global), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
 
-// Entries of one access of the row that is being worked on.
+// A thread's N parts of a row: with W == 8 the 4 pairs of neighbouring columns of an access, with W == 1 one pair of columns `lanes` apart.
+template <int W>
+struct Part {
+    static constexpr int kPairs = W == 8 ? 4 : 1;
+    static __device__ __forceinline__ int column(int i, int e, int lanes, int lane) { return W == 8 ? (i * lanes + lane) * 8 + e : (2 * i + e) * lanes + lane; }
+};
+
+// STAGES rows of the arrays on their way through shared memory.  W == 8: every thread copies the accesses that it will read itself,
+// [STAGES][arrays][N][threads], so that no barrier is needed.  W == 1: the threads of a row copy the 16-byte blocks that the row
+// touches (rows begin anywhere), and read single columns of one another's blocks behind a barrier.
 template <int W, int N, int STAGES, bool RES>
-struct GradRow {
-    using A = Access<W>;
-    using Raw = typename A::Raw;
+struct Ring {
     static constexpr int kArrays = RES ? 3 : 2;
-    Raw held[W == 8 ? 1 : kArrays * N];             // W == 1: the row's accesses
-    uint4* ring;                                     // W == 8: [STAGES][kArrays][N][threads]
+    uint4* base;
+    int first[W == 8 ? 1 : kArrays];                 // W == 1: where the current row begins
 
     static __device__ __forceinline__ const uint16_t* source(const NormGradArgs& a, int k) { return k == 0 ? a.h : k == 1 ? a.dy : a.dh; }
-    __device__ __forceinline__ void fetch(const NormGradArgs& a, int64_t row, int lane, int stage)
+    __device__ __forceinline__ void fetch(const NormGradArgs& a, int64_t row, int lane, int stage, int sub, int rows)
     {
-        if constexpr (W == 8) {
 #pragma unroll
-            for (int k = 0; k < kArrays; ++k)
+        for (int k = 0; k < kArrays; ++k) {
+            if constexpr (W == 8) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const int c = i * a.lanes + lane;
                     const bool in = row < a.tokens && c < a.units;
-                    copy_async(ring + ((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x, source(a, k) + (in ? row * a.dim + c * 8 : 0), in);
+                    copy_async(base + ((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x, source(a, k) + (in ? row * a.dim + c * 8 : 0), in ? 16 : 0);
                 }
-            copies_commit();
-        } else {
+            } else if (row < a.tokens) {
+                const uint16_t *begin = source(a, k), *end = begin + (int64_t)a.tokens * a.dim, *from = begin + row * a.dim;
+                const int skip = (int)((uintptr_t)from & 15u) / 2, blocks = (skip + a.dim + 7) / 8;
+                uint16_t* to = reinterpret_cast<uint16_t*>(base) + ((stage * kArrays + k) * rows + sub) * a.window;
+                for (int c = lane; c < blocks; c += a.lanes) {
+                    const uint16_t* p = from - skip + 8 * c;
+                    if (p >= begin) {
+                        copy_async(to + 8 * c, p, (int)min((int64_t)16, (int64_t)(end - p) * 2));
+                    } else {
+                        for (int j = (int)(begin - p); j < 8 && p + j < end; ++j) to[8 * c + j] = p[j];      // the array begins inside a block
+                    }
+                }
+            }
+        }
+        copies_commit();
+    }
+    // W == 1: the row at hand
+    __device__ __forceinline__ void turn_to(const NormGradArgs& a, int64_t row, int stage, int sub, int rows)
+    {
+        if constexpr (W == 1) {
 #pragma unroll
             for (int k = 0; k < kArrays; ++k)
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int c = i * a.lanes + lane;
-                    held[k * N + i] = A::zero();
-                    if (row < a.tokens && c < a.units) held[k * N + i] = source(a, k)[row * a.dim + c];
-                }
+                first[k] = ((stage * kArrays + k) * rows + sub) * a.window + (int)((uintptr_t)(source(a, k) + row * a.dim) & 15u) / 2;
         }
     }
-    __device__ __forceinline__ void get(int k, int i, int stage, float (&v)[W]) const
+    __device__ __forceinline__ void get(const NormGradArgs& a, int k, int i, int lane, int stage, float2 (&v)[Part<W>::kPairs]) const
     {
-        if constexpr (W == 8) A::unpack(ring[((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x], v);
-        else A::unpack(held[k * N + i], v);
+        if constexpr (W == 8) {
+            Pairs::unpack(base[((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x], v);
+        } else {
+            const uint16_t* row = reinterpret_cast<const uint16_t*>(base) + first[k];
+            const int c = Part<1>::column(i, 0, a.lanes, lane), d = Part<1>::column(i, 1, a.lanes, lane);
+            v[0] = make_float2(c < a.dim ? bf16_low(row[c]) : 0.0f, d < a.dim ? bf16_low(row[d]) : 0.0f);
+        }
     }
 };
 
+// Threads that a CTA has at most, and CTAs that the registers are to hold.
+template <int W, int N, bool SPLIT> constexpr int grad_threads() { return !SPLIT ? 256 : N * Part<W>::kPairs <= 8 ? 512 : 1024; }
+template <int W, int N, bool SPLIT> constexpr int grad_blocks() { return SPLIT ? 1 : 2; }
+
 template <int W, int N, int STAGES, bool SPLIT, bool RES, class WT>
-__global__ void __launch_bounds__(SPLIT ? (W * N <= 16 ? 512 : 1024) : 256, SPLIT && W * N > 8 ? 1 : 2)
+__global__ void __launch_bounds__(grad_threads<W, N, SPLIT>(), grad_blocks<W, N, SPLIT>())
 rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
 {
-    using A = Access<W>;
+    constexpr int Q = Part<W>::kPairs;
     extern __shared__ uint4 dynamic[];               // the ring; !SPLIT, afterwards: [rows of the CTA][dim] sums
     __shared__ float2 part[2][kMostWarps];
     __shared__ double part64[2][kMostWarps];
     const int lane = SPLIT ? (int)threadIdx.x : (int)threadIdx.x & (a.lanes - 1);
     const int rows = SPLIT ? 1 : (int)blockDim.x / a.lanes, sub = SPLIT ? 0 : (int)threadIdx.x / a.lanes;
-    float dw[N][W];
+    float2 dw[N][Q];
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < W; ++j) dw[i][j] = 0.0f;
-    auto weight = [&](int i, float (&w)[W]) {
-        const int c = i * a.lanes + lane;
+        for (int j = 0; j < Q; ++j) dw[i][j] = both(0.0f);
+    auto weight = [&](int i, float2 (&w)[Q]) {
+        const WT* p = static_cast<const WT*>(a.weight);
+        const int c = Part<W>::column(i, 0, a.lanes, lane);
 #pragma unroll
-        for (int j = 0; j < W; ++j) w[j] = 0.0f;
-        if (c < a.units) A::weights(static_cast<const WT*>(a.weight) + c * W, w);
+        for (int j = 0; j < Q; ++j) w[j] = both(0.0f);
+        if constexpr (W == 8) {
+            if (c < a.dim) Pairs::weights(p + c, w);
+        } else {
+            const int d = Part<W>::column(i, 1, a.lanes, lane);
+            float v[1];
+            if (c < a.dim) { Access<1>::weights(p + c, v); w[0].x = v[0]; }
+            if (d < a.dim) { Access<1>::weights(p + d, v); w[0].y = v[0]; }
+        }
     };
-    constexpr bool KEPT = W * N <= 16;                // the weights of a thread's columns in registers
-    float kept[KEPT ? N : 1][W];
-    if constexpr (KEPT) {
+    constexpr bool KEPT = N * Q <= 8;                // a row stays in registers between its two halves
+    constexpr bool WEIGHTS = N * Q <= 12;            // and the weights of a thread's columns for good
+    float2 kept[WEIGHTS ? N : 1][Q];
+    if constexpr (WEIGHTS) {
 #pragma unroll
         for (int i = 0; i < N; ++i) weight(i, kept[i]);
     }
     const int64_t step = (int64_t)gridDim.x * rows;
     int64_t row0 = (int64_t)blockIdx.x * rows;
-    GradRow<W, N, STAGES, RES> x;
-    x.ring = dynamic;
-    if constexpr (W == 8) {
+    Ring<W, N, STAGES, RES> ring;
+    ring.base = dynamic;
 #pragma unroll
-        for (int k = 0; k < STAGES - 1; ++k) x.fetch(a, row0 + sub + k * step, lane, k);
-    }
+    for (int k = 0; k + 1 < STAGES; ++k) ring.fetch(a, row0 + sub + k * step, lane, k, sub, rows);
     int stage = 0;
     for (int turn = 0; row0 < a.tokens; row0 += step, turn ^= 1, stage = stage + 1 == STAGES ? 0 : stage + 1) {
-        const int64_t row = row0 + sub;
-        x.fetch(a, row + (W == 8 ? (STAGES - 1) * step : 0), lane, W == 8 ? (stage + STAGES - 1) % STAGES : 0);
-        if constexpr (W == 8) copies_wait<STAGES - 1>();
-        float2 s = make_float2(0.0f, 0.0f);          // sums of h^2 and of g h
+        const int64_t row = row0 + sub, ahead = row + (STAGES - 1) * step;
+        const int free = stage == 0 ? STAGES - 1 : stage - 1;         // the row before was there
+        if constexpr (W == 8) {
+            ring.fetch(a, ahead, lane, free, sub, rows);
+            copies_wait<STAGES - 1>();
+        } else if constexpr (STAGES > 1) {
+            copies_wait<STAGES - 2>();
+            if constexpr (SPLIT) __syncthreads(); else __syncwarp();   // everyone's blocks are there, and the row before has been read
+            ring.fetch(a, ahead, lane, free, sub, rows);
+        } else {
+            if constexpr (SPLIT) __syncthreads(); else __syncwarp();
+            ring.fetch(a, ahead, lane, free, sub, rows);
+            copies_wait<0>();
+            if constexpr (SPLIT) __syncthreads(); else __syncwarp();
+        }
+        const bool active = row < a.tokens;
+        ring.turn_to(a, active ? row : 0, stage, sub, rows);
+        float2 u[KEPT ? N : 1][Q], g[KEPT ? N : 1][Q], v[KEPT ? N : 1][Q];
+        float2 hh = both(0.0f), gh = both(0.0f);     // sums of h^2 and of g h
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float u[W], v[W], w[W];
-            x.get(0, i, stage, u);
-            x.get(1, i, stage, v);
-            if constexpr (!KEPT) weight(i, w);
+            const int e = KEPT ? i : 0;
+            ring.get(a, 0, i, lane, stage, u[e]);
+            ring.get(a, 1, i, lane, stage, v[e]);
+            if (W == 1 && !active) u[e][0] = v[e][0] = both(0.0f);
+            float2 w[Q];
+            if constexpr (!WEIGHTS) weight(i, w);
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                s.x = fmaf(u[j], u[j], s.x);
-                s.y = fmaf(v[j] * (KEPT ? kept[KEPT ? i : 0][j] : w[j]), u[j], s.y);
+            for (int j = 0; j < Q; ++j) {
+                g[e][j] = mul2(v[e][j], WEIGHTS ? kept[WEIGHTS ? i : 0][j] : w[j]);
+                hh = fma2(u[e][j], u[e][j], hh);
+                gh = fma2(g[e][j], u[e][j], gh);
             }
         }
-        for (int d = (SPLIT ? 32 : a.lanes) >> 1; d > 0; d >>= 1) {
-            s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, d);
-            s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, d);
-        }
+        float2 s = make_float2(hh.x + hh.y, gh.x + gh.y);
+        for (int d = (SPLIT ? 32 : a.lanes) >> 1; d > 0; d >>= 1)
+            s = add2(s, make_float2(__shfl_xor_sync(0xFFFFFFFFu, s.x, d), __shfl_xor_sync(0xFFFFFFFFu, s.y, d)));
         if constexpr (SPLIT) {
             // two buffers: a warp may be one row ahead of another, not two
             if ((threadIdx.x & 31) == 0) part[turn][threadIdx.x >> 5] = s;
             __syncthreads();
             s = part[turn][0];
-            for (int i = 1; i < (int)(blockDim.x >> 5); ++i) {
-                const float2 o = part[turn][i];
-                s.x += o.x;
-                s.y += o.y;
-            }
+            for (int i = 1; i < (int)(blockDim.x >> 5); ++i) s = add2(s, part[turn][i]);
         }
-        const float mean = s.x / (float)a.dim + a.eps;
-        float r = __frsqrt_rn(mean), pre = 1.0f, scaled = r;             // r = pre * scaled
-        float m = s.y / (float)a.dim * r;                               // mean(g n)
-        if (SPLIT ? odd_row(mean) : __any_sync(0xFFFFFFFFu, odd_row(mean))) {
-            double s64 = 0.0, m64 = 0.0;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float u[W], v[W], w[W];
-                x.get(0, i, stage, u);
-                x.get(1, i, stage, v);
-                weight(i, w);
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    s64 = fma((double)u[j], (double)u[j], s64);
-                    m64 = fma((double)v[j] * (double)w[j], (double)u[j], m64);
-                }
-            }
+        const float mean = fmaf(s.x, a.inverse_dim, a.eps);
+        float r = __frsqrt_rn(mean), scaled = r;                        // n = h * scaled
+        float m = s.y * a.inverse_dim * r;                              // mean(g n)
+        float pre = 1.0f;
+        const bool odd = odd_row(mean);
+        if (SPLIT ? odd : __any_sync(0xFFFFFFFFu, odd)) {
+            const double2 own = odd_sums<W>(a.h + row * a.dim, a.dy + row * a.dim, a.weight, std::is_same<WT, float>::value, active ? a.dim : 0, a.lanes, lane);
             if constexpr (SPLIT) __syncthreads();                        // the row before may have been an odd one, too
-            s64 = row_sum<SPLIT>(s64, a.lanes, part64[0]) / (double)a.dim + (double)a.eps;
-            m64 = row_sum<SPLIT>(m64, a.lanes, part64[1]) / (double)a.dim;
-            if (odd_row(mean)) {
+            const double s64 = row_sum<SPLIT>(own.x, a.lanes, part64[0]) / (double)a.dim + (double)a.eps;
+            const double m64 = row_sum<SPLIT>(own.y, a.lanes, part64[1]) / (double)a.dim;
+            if (odd) {
                 const double r64 = 1.0 / sqrt(s64);
                 pre = odd_factor(s64);
                 scaled = (float)(r64 / (double)pre);
@@ -396,50 +452,59 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = i * a.lanes + lane;
-            if (row >= a.tokens || c >= a.units) continue;
-            float u[W], v[W], w[W], o[W];
-            x.get(0, i, stage, u);
-            x.get(1, i, stage, v);
-            if constexpr (!KEPT) weight(i, w);
-            if constexpr (RES) x.get(2, i, stage, o);
+            const int c = Part<W>::column(i, 0, a.lanes, lane), e = KEPT ? i : 0;
+            if (!active || c >= a.dim) continue;
+            if constexpr (!KEPT) {
+                float2 w[Q];
+                ring.get(a, 0, i, lane, stage, u[0]);
+                ring.get(a, 1, i, lane, stage, v[0]);
+                if constexpr (!WEIGHTS) weight(i, w);
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float n = u[j] * pre * scaled;
-                dw[i][j] = fmaf(v[j], n, dw[i][j]);
-                const float d = fmaf(v[j], KEPT ? kept[KEPT ? i : 0][j] : w[j], -n * m);
-                o[j] = RES ? fmaf(r, d, o[j]) : r * d;
+                for (int j = 0; j < Q; ++j) g[0][j] = mul2(v[0][j], WEIGHTS ? kept[WEIGHTS ? i : 0][j] : w[j]);
             }
-            *reinterpret_cast<typename A::Raw*>(a.dx + row * a.dim + (int64_t)c * W) = A::pack(o);
+            if (odd) {
+#pragma unroll
+                for (int j = 0; j < Q; ++j) u[e][j] = mul2(u[e][j], both(pre));
+            }
+            float2 o[Q];
+            if constexpr (RES) ring.get(a, 2, i, lane, stage, o);
+#pragma unroll
+            for (int j = 0; j < Q; ++j) {
+                const float2 n = mul2(u[e][j], both(scaled));
+                dw[i][j] = fma2(v[e][j], n, dw[i][j]);
+                const float2 d = fma2(n, both(-m), g[e][j]);
+                o[j] = RES ? fma2(both(r), d, o[j]) : mul2(both(r), d);
+            }
+            uint16_t* to = a.dx + row * a.dim + c;
+            if constexpr (W == 8) {
+                *reinterpret_cast<uint4*>(to) = Pairs::pack(o);
+            } else {
+                const uint32_t two = bf16_pair(o[0].x, o[0].y);
+                to[0] = (uint16_t)two;
+                if (c + a.lanes < a.dim) to[a.lanes] = (uint16_t)(two >> 16);
+            }
         }
     }
     chain_next();
-    if constexpr (W == 8) copies_wait<0>();
+    copies_wait<0>();
     if (!a.partial) return;
     float* out = a.partial + (int64_t)blockIdx.x * a.dim;
-    if constexpr (SPLIT) {
+    float* sums = reinterpret_cast<float*>(dynamic);
+    if constexpr (!SPLIT) __syncthreads();           // the ring has been read
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = i * a.lanes + lane;
-            if (c >= a.units) continue;
-            if constexpr (W == 8) {
-                float4* q = reinterpret_cast<float4*>(out + c * 8);
-                q[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
-                q[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
-            } else {
-                out[c] = dw[i][0];
-            }
+    for (int i = 0; i < N; ++i) {
+        const int c = Part<W>::column(i, 0, a.lanes, lane);
+        if (c >= a.dim) continue;
+        float* to = (SPLIT ? out : sums + sub * a.dim) + c;
+        if constexpr (W == 8) {
+            reinterpret_cast<float4*>(to)[0] = make_float4(dw[i][0].x, dw[i][0].y, dw[i][1].x, dw[i][1].y);
+            reinterpret_cast<float4*>(to)[1] = make_float4(dw[i][2].x, dw[i][2].y, dw[i][3].x, dw[i][3].y);
+        } else {
+            to[0] = dw[i][0].x;
+            if (c + a.lanes < a.dim) to[a.lanes] = dw[i][0].y;
         }
-    } else {
-        float* sums = reinterpret_cast<float*>(dynamic);
-        __syncthreads();                             // the ring has been read
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = i * a.lanes + lane;
-            if (c >= a.units) continue;
-#pragma unroll
-            for (int j = 0; j < W; ++j) sums[sub * a.dim + c * W + j] = dw[i][j];
-        }
+    }
+    if constexpr (!SPLIT) {
         __syncthreads();
         for (int c = threadIdx.x; c < a.dim; c += blockDim.x) {
             float v = sums[c];
@@ -473,27 +538,50 @@ join_weight_grad_kernel(const float* partial, float* out, int32_t rows, int32_t 
     if (lane == 0 && own < dim) out[own] = v;
 }
 
+// Entries that a row of `dim` columns takes in shared memory when it begins anywhere.
+int64_t window_of(int64_t dim) { return (dim + 7 + 7) / 8 * 8; }
+
 struct GradSpread {
-    Spread s;
+    int lanes, n;
+    bool split;
     int stages;
+    int64_t bytes;            // of shared memory
+    int held;                 // CTAs that an SM holds
 };
 
-GradSpread grad_spread_of(int64_t units, int w)
+GradSpread grad_spread_of(int64_t dim, int w, bool res)
 {
+    GradSpread g = {};
+    const int64_t units = dim / w, arrays = res ? 3 : 2;
     if (w == 8) {
         if (units <= 128) {                   // up to 1024 columns: in a warp
-            int lanes = 8;
-            while (lanes < 32 && lanes < units) lanes *= 2;
-            const int n = (int)((units + lanes - 1) / lanes);
-            return {{lanes, n <= 1 ? 1 : n <= 2 ? 2 : 4, false}, n <= 2 ? 4 : 2};
+            g.lanes = 8;
+            while (g.lanes < 32 && g.lanes < units) g.lanes *= 2;
+            g.n = (int)((units + g.lanes - 1) / g.lanes);
+            g.stages = g.n <= 2 ? 4 : 2;
+        } else {
+            g.split = true;
+            g.n = units <= 1024 ? 2 : 4;
+            g.lanes = (int)((units + g.n * 32 - 1) / (g.n * 32)) * 32;
+            g.stages = units <= 1024 ? 4 : units <= 2048 ? 2 : 1;
         }
-        // stages of 48 bytes for each access: 96 KB a CTA (two of them on an SM), 192 KB for wider rows (one)
-        const int n = units <= 512 ? 1 : units <= 1024 ? 2 : 4;
-        return {{(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true}, units <= 1024 ? 4 : units <= 2048 ? 2 : 1};
+        g.bytes = g.stages * arrays * g.n * (g.split ? g.lanes : 256) * 16;
+    } else {
+        g.split = dim > 256;
+        g.n = !g.split ? 4 : dim <= 8192 ? 8 : 16;
+        g.lanes = !g.split ? 32 : (int)((dim + g.n * 64 - 1) / (g.n * 64)) * 32;
+        const int64_t row = arrays * window_of(dim) * 2 * (g.split ? 1 : 256 / g.lanes);
+        g.stages = g.n <= 8 ? (4 * row <= 110000 ? 4 : 2) : 2 * row <= 220000 ? 2 : 1;
+        g.bytes = g.stages * row;
     }
-    if (units <= 256) return {{32, 8, false}, 1};
-    const int n = units <= 4096 ? 8 : 32;
-    return {{(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true}, 1};
+    const int64_t sums = g.split ? 0 : 4 * dim * (256 / g.lanes);
+    if (g.bytes < sums) g.bytes = sums;
+    const int threads = g.split ? g.lanes : 256;
+    g.held = (int)(220000 / (g.bytes + 2048));
+    const int by_registers = threads <= 512 ? 512 / threads : 1;
+    if (g.held > by_registers) g.held = by_registers;
+    if (g.held < 1) g.held = 1;
+    return g;
 }
 
 int sm_count(int* sms)
@@ -505,36 +593,37 @@ int sm_count(int* sms)
 }
 
 // CTAs of the gradient kernel: what the SMs hold at a time, and no more than there are groups of rows.
-int64_t grad_ctas(const Spread& s, int64_t tokens, int sms)
+int64_t grad_ctas(const GradSpread& g, int64_t tokens, int sms)
 {
-    const int64_t rows = s.split ? 1 : 256 / s.lanes, groups = (tokens + rows - 1) / rows;
-    const int64_t held = (int64_t)sms * (s.split && s.n * s.lanes > 512 ? 1 : 2);
+    const int64_t rows = g.split ? 1 : 256 / g.lanes, groups = (tokens + rows - 1) / rows, held = (int64_t)sms * g.held;
     return groups < held ? groups : held;
 }
 
-// Workspace for either width of access: which one a call takes depends on its pointers.
+// Workspace for every form of the call: which one it takes depends on its pointers.
 uint64_t grad_workspace(int64_t tokens, int64_t dim, int sms)
 {
-    const int64_t wide = dim % 8 == 0 ? grad_ctas(grad_spread_of(dim / 8, 8).s, tokens, sms) : 0, one = grad_ctas(grad_spread_of(dim, 1).s, tokens, sms);
-    return sizeof(float) * (uint64_t)(wide > one ? wide : one) * (uint64_t)dim;
+    int64_t most = 0;
+    for (int w = 1; w <= 8; w += 7)
+        for (int res = 0; res < 2; ++res) {
+            const int64_t n = dim % w == 0 ? grad_ctas(grad_spread_of(dim, w, res != 0), tokens, sms) : 0;
+            if (n > most) most = n;
+        }
+    return sizeof(float) * (uint64_t)most * (uint64_t)dim;
 }
 
 template <int W, int N, int STAGES, bool SPLIT, bool RES, class WT>
-int launch_grad(const NormGradArgs& a, unsigned ctas, cudaStream_t stream)
+int launch_grad(const NormGradArgs& a, const GradSpread& g, unsigned ctas, cudaStream_t stream)
 {
-    const unsigned threads = SPLIT ? (unsigned)a.lanes : 256u;
-    const size_t ring = W == 8 ? (size_t)STAGES * (RES ? 3 : 2) * N * threads * 16 : 0, sums = SPLIT ? 0 : sizeof(float) * (threads / a.lanes) * (size_t)a.dim;
-    const size_t smem = ring > sums ? ring : sums;
     const auto kernel = rms_norm_grad_kernel<W, N, STAGES, SPLIT, RES, WT>;
-    if (smem > 40960) CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    return launch_chained(true, kernel, dim3(ctas), threads, smem, stream, 1, a);
+    if (g.bytes > 40960) CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)g.bytes));
+    return launch_chained(true, kernel, dim3(ctas), SPLIT ? (unsigned)a.lanes : 256u, (size_t)g.bytes, stream, 1, a);
 }
 
 template <int W, int N, int STAGES, bool SPLIT>
-int launch_grad(const NormGradArgs& a, bool weight_fp32, unsigned ctas, cudaStream_t stream)
+int launch_grad(const NormGradArgs& a, const GradSpread& g, bool weight_fp32, unsigned ctas, cudaStream_t stream)
 {
-    if (a.dh) return weight_fp32 ? launch_grad<W, N, STAGES, SPLIT, true, float>(a, ctas, stream) : launch_grad<W, N, STAGES, SPLIT, true, uint16_t>(a, ctas, stream);
-    return weight_fp32 ? launch_grad<W, N, STAGES, SPLIT, false, float>(a, ctas, stream) : launch_grad<W, N, STAGES, SPLIT, false, uint16_t>(a, ctas, stream);
+    if (a.dh) return weight_fp32 ? launch_grad<W, N, STAGES, SPLIT, true, float>(a, g, ctas, stream) : launch_grad<W, N, STAGES, SPLIT, true, uint16_t>(a, g, ctas, stream);
+    return weight_fp32 ? launch_grad<W, N, STAGES, SPLIT, false, float>(a, g, ctas, stream) : launch_grad<W, N, STAGES, SPLIT, false, uint16_t>(a, g, ctas, stream);
 }
 
 int check_norm(const void* weight, int weight_fp32, int64_t tokens, int64_t dim, float eps)
@@ -571,12 +660,16 @@ int norm_impl(const uint16_t* x, const uint16_t* residual, const void* weight, i
     const void* ptrs[7] = {x, residual, weight, y, q, scales, h};
     if ((rc = check_device_memory(ptrs, 7)) != CAST_OK) return rc;
     const int w = dim % 8 == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(weight, 16) && aligned(y, 16) && aligned(q, 8) && aligned(h, 16) ? 8 : 1;
-    NormArgs a = {x, residual, weight, y, q, scales, h, (int32_t)tokens, (int32_t)dim, (int32_t)(dim / w), 0, eps};
+    NormArgs a = {x, residual, weight, y, q, scales, h, (int32_t)tokens, (int32_t)dim, (int32_t)(dim / w), 0, eps, 1.0f / (float)dim};
     const Spread s = spread_of(a.units, w);
     a.lanes = s.lanes;
     const bool f = weight_fp32 != 0;
     if (w == 8) {
-        if (!s.split) return s.n == 1 ? launch_norm<8, 1, false>(a, f, stream) : s.n == 2 ? launch_norm<8, 2, false>(a, f, stream) : launch_norm<8, 4, false>(a, f, stream);
+        if (!s.split)
+            return s.n == 1   ? launch_norm<8, 1, false>(a, f, stream)
+                   : s.n == 2 ? launch_norm<8, 2, false>(a, f, stream)
+                   : s.n == 3 ? launch_norm<8, 3, false>(a, f, stream)
+                              : launch_norm<8, 4, false>(a, f, stream);
         return s.n == 1 ? launch_norm<8, 1, true>(a, f, stream) : s.n == 2 ? launch_norm<8, 2, true>(a, f, stream) : launch_norm<8, 4, true>(a, f, stream);
     }
     if (!s.split) return launch_norm<1, 8, false>(a, f, stream);
@@ -634,26 +727,31 @@ extern "C" int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, c
     int sms = 0;
     if ((rc = sm_count(&sms)) != CAST_OK) return rc;
     const int w = dim % 8 == 0 && aligned(grad_y, 16) && aligned(h, 16) && aligned(grad_h, 16) && aligned(grad_x, 16) && aligned(weight, 16) ? 8 : 1;
-    NormGradArgs a = {grad_y, h, grad_h, weight, grad_x, grad_weight ? static_cast<float*>(workspace) : nullptr, (int32_t)tokens, (int32_t)dim,
-                      (int32_t)(dim / w), 0, eps};
-    const GradSpread g = grad_spread_of(a.units, w);
-    const Spread& s = g.s;
-    a.lanes = s.lanes;
-    const unsigned ctas = (unsigned)grad_ctas(s, tokens, sms);
+    const GradSpread g = grad_spread_of(dim, w, grad_h != nullptr);
+    const NormGradArgs a = {grad_y, h, grad_h, weight, grad_x, grad_weight ? static_cast<float*>(workspace) : nullptr, (int32_t)tokens, (int32_t)dim,
+                            (int32_t)(dim / w), g.lanes, (int32_t)window_of(dim), eps, 1.0f / (float)dim};
+    const unsigned ctas = (unsigned)grad_ctas(g, tokens, sms);
     if (grad_weight && workspace_bytes < grad_workspace(tokens, dim, sms)) return CAST_ERR_PLAN;
     const void* ptrs[7] = {grad_y, h, grad_h, weight, grad_x, grad_weight, grad_weight ? workspace : nullptr};
     if ((rc = check_device_memory(ptrs, 7)) != CAST_OK) return rc;
     const bool f = weight_fp32 != 0;
     const cudaStream_t st = (cudaStream_t)stream;
     if (w == 8) {
-        if (!s.split)
-            rc = s.n == 1 ? launch_grad<8, 1, 4, false>(a, f, ctas, st) : s.n == 2 ? launch_grad<8, 2, 4, false>(a, f, ctas, st) : launch_grad<8, 4, 2, false>(a, f, ctas, st);
-        else if (s.n <= 2)
-            rc = s.n == 1 ? launch_grad<8, 1, 4, true>(a, f, ctas, st) : launch_grad<8, 2, 4, true>(a, f, ctas, st);
+        if (!g.split)
+            rc = g.n == 1   ? launch_grad<8, 1, 4, false>(a, g, f, ctas, st)
+                 : g.n == 2 ? launch_grad<8, 2, 4, false>(a, g, f, ctas, st)
+                 : g.n == 3 ? launch_grad<8, 3, 2, false>(a, g, f, ctas, st)
+                            : launch_grad<8, 4, 2, false>(a, g, f, ctas, st);
         else
-            rc = g.stages == 2 ? launch_grad<8, 4, 2, true>(a, f, ctas, st) : launch_grad<8, 4, 1, true>(a, f, ctas, st);
+            rc = g.n == 2        ? launch_grad<8, 2, 4, true>(a, g, f, ctas, st)
+                 : g.stages == 2 ? launch_grad<8, 4, 2, true>(a, g, f, ctas, st)
+                                 : launch_grad<8, 4, 1, true>(a, g, f, ctas, st);
+    } else if (!g.split) {
+        rc = launch_grad<1, 4, 4, false>(a, g, f, ctas, st);
+    } else if (g.n == 8) {
+        rc = g.stages == 4 ? launch_grad<1, 8, 4, true>(a, g, f, ctas, st) : launch_grad<1, 8, 2, true>(a, g, f, ctas, st);
     } else {
-        rc = !s.split ? launch_grad<1, 8, 1, false>(a, f, ctas, st) : s.n == 8 ? launch_grad<1, 8, 1, true>(a, f, ctas, st) : launch_grad<1, 32, 1, true>(a, f, ctas, st);
+        rc = g.stages == 2 ? launch_grad<1, 16, 2, true>(a, g, f, ctas, st) : launch_grad<1, 16, 1, true>(a, g, f, ctas, st);
     }
     if (rc != CAST_OK || !grad_weight) return rc;
     return launch_chained(false, join_weight_grad_kernel, dim3((unsigned)((dim + 31) / 32)), 32 * kJoinWarps, 0, st, 1, (const float*)a.partial, grad_weight,

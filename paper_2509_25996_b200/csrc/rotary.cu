@@ -18,10 +18,9 @@ namespace {
 constexpr int kMostSets = 4;              // arrays of heads turned by one call (queries, keys, ...)
 constexpr int kMostPairs = 512;
 constexpr int kTurnThreads = 256;
-constexpr int kItems = 4;                 // units that a thread has in flight
+constexpr int kItems = 4;                 // units of a thread
 constexpr int kBatch = kTurnThreads * kItems;
 constexpr int kAngles = 1024;             // cosines and sines of a CTA (8 KB)
-constexpr int kMostUnits = 16384;         // of a CTA
 
 // i / d for i < 2^16, d < 2^16
 struct Divisor {
@@ -44,59 +43,91 @@ struct RotaryArgs {
     const int32_t* positions;         // [n_axes][tokens]
     int32_t sets, heads;              // heads of all sets together
     int32_t tokens, n_axes, pairs;
-    int32_t turned;                   // units of a head that turn; each holds W pairs (halves) or W columns (adjacent)
+    int32_t turned;                   // units of a head that turn
     Divisor units;                    // and with those that are copied
-    Divisor token_units;              // of a token in a CTA (of the last CTA of a token's heads: fewer)
+    Divisor token_units;              // of a token in a CTA
     Divisor pair_count;
     int32_t tile_tokens, tile_heads;  // of a CTA
     int32_t head_tiles;
     float sign;
 };
 
-// W: columns per access.  Halves: a unit is W columns of the first half and the W of the second that go with them.
+// W bf16 columns of one access, as words of two (W == 1: one in the low half)
+template <int W> struct Words { uint32_t w[W > 1 ? W / 2 : 1]; };
+template <int W>
+__device__ __forceinline__ Words<W> load_words(const uint16_t* p)
+{
+    Words<W> r;
+    if constexpr (W == 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+    } else if constexpr (W == 4) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        r.w[0] = v.x; r.w[1] = v.y;
+    } else if constexpr (W == 2) {
+        r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+        r.w[0] = *p;
+    }
+    return r;
+}
+template <int W>
+__device__ __forceinline__ void store_words(uint16_t* p, const Words<W>& r)
+{
+    if constexpr (W == 8) *reinterpret_cast<uint4*>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    else if constexpr (W == 4) *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
+    else if constexpr (W == 2) *reinterpret_cast<uint32_t*>(p) = r.w[0];
+    else *p = (uint16_t)r.w[0];
+}
+
+// A unit is what a thread turns of a head.  Halves: W columns of the first half and the W of the second that go with them.  Adjacent:
+// W columns (of which the last turning unit may copy some), or with W == 1 two single ones.
 template <int W, bool ADJACENT>
-__global__ void __launch_bounds__(kTurnThreads)
+struct Unit {
+    static constexpr bool kTwo = !ADJACENT || W == 1;                        // two accesses
+    static constexpr int kPairs = ADJACENT ? (W == 1 ? 1 : W / 2) : W;
+    static constexpr int kColumns = ADJACENT ? 2 * kPairs : W;               // from one unit's first column to the next one's
+};
+
+template <int W, bool ADJACENT>
+__global__ void __launch_bounds__(kTurnThreads, ADJACENT ? 5 : 4)
 rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
-    // one column per access cannot hold an adjacent pair: two accesses then, too
-    constexpr bool TWO = !ADJACENT || W == 1;
-    constexpr int P = W == 1 ? 1 : ADJACENT ? W / 2 : W;        // pairs of a unit
-    using A = Access<W>;
-    using Raw = typename A::Raw;
+    using U = Unit<W, ADJACENT>;
+    constexpr int P = U::kPairs;
     // [token][pair of a unit / 2][unit][2]: neighbouring units, which neighbouring threads hold, lie side by side
     __shared__ __align__(16) float2 angle[kAngles];
     const int64_t token0 = (int64_t)(blockIdx.x / a.head_tiles) * a.tile_tokens;
     const int head0 = (int)(blockIdx.x % a.head_tiles) * a.tile_heads;
     const int tokens = (int)min((int64_t)a.tile_tokens, a.tokens - token0), heads = min(a.tile_heads, a.heads - head0);
     const uint32_t total = (uint32_t)tokens * (uint32_t)heads * a.units.d;
-    Raw x[kItems], y[TWO ? kItems : 1];
+    Words<W> x[kItems], y[U::kTwo ? kItems : 1];
     uint16_t* dst[kItems];
     int place[kItems];                    // of the unit's first angles, -1: a copy, -2: none
-    auto fetch = [&](uint32_t first) {
+    int left[ADJACENT && W == 8 ? kItems : 1];        // pairs that turn from the unit's first one on
 #pragma unroll
-        for (int k = 0; k < kItems; ++k) {
-            const uint32_t i = first + threadIdx.x + k * kTurnThreads;
-            place[k] = -2;
-            if (i >= total) continue;
-            // several tokens only with all of their heads: token_units is theirs then
-            const uint32_t t = a.tile_tokens > 1 ? divide(i, a.token_units) : 0u, rest = i - t * a.token_units.d, hd = divide(rest, a.units);
-            const int u = (int)(rest - hd * a.units.d), head = head0 + (int)hd;
-            int s = 0;
-            while (s + 1 < a.sets && head >= a.set[s + 1].first) ++s;
-            const HeadSet& hs = a.set[s];
-            const int64_t token = token0 + t, own = head - hs.first;
-            const bool turns = u < a.turned;
-            const int col = turns ? (ADJACENT ? u * 2 * P : u * W) : 2 * a.pairs + (u - a.turned) * W;      // the unit's first column
-            const uint16_t* src = hs.in + token * hs.in_token + own * hs.in_head + col;
-            dst[k] = hs.out + token * hs.out_token + own * hs.out_head + col;
-            place[k] = turns ? (int)t * a.pairs + u * (P > 1 ? 2 : 1) : -1;
-            x[k] = *reinterpret_cast<const Raw*>(src);
-            if constexpr (TWO)
-                if (turns) y[k] = *reinterpret_cast<const Raw*>(src + (ADJACENT ? 1 : a.pairs));
-        }
-    };
-    fetch(0);
-    for (uint32_t i = threadIdx.x; i < (uint32_t)(tokens * a.pairs); i += kTurnThreads) {
+    for (int k = 0; k < kItems; ++k) {
+        const uint32_t i = threadIdx.x + k * blockDim.x;
+        place[k] = -2;
+        if (i >= total) continue;
+        // several tokens only with all of their heads: token_units is theirs then
+        const uint32_t t = a.tile_tokens > 1 ? divide(i, a.token_units) : 0u, rest = i - t * a.token_units.d, hd = divide(rest, a.units);
+        const int u = (int)(rest - hd * a.units.d), head = head0 + (int)hd;
+        int s = 0;
+        while (s + 1 < a.sets && head >= a.set[s + 1].first) ++s;
+        const HeadSet& hs = a.set[s];
+        const int64_t token = token0 + t, own = head - hs.first;
+        const bool turns = u < a.turned;
+        const int col = turns ? u * U::kColumns : (U::kTwo ? 2 * a.pairs : a.turned * W) + (u - a.turned) * W;      // the unit's first column
+        const uint16_t* src = hs.in + token * hs.in_token + own * hs.in_head + col;
+        dst[k] = hs.out + token * hs.out_token + own * hs.out_head + col;
+        place[k] = turns ? (int)t * a.turned * P + u * (P > 1 ? 2 : 1) : -1;
+        x[k] = load_words<W>(src);
+        if constexpr (U::kTwo)
+            if (turns) y[k] = load_words<W>(src + (ADJACENT ? 1 : a.pairs));
+        if constexpr (ADJACENT && W == 8) left[k] = a.pairs - u * P;
+    }
+    for (uint32_t i = threadIdx.x; i < (uint32_t)(tokens * a.pairs); i += blockDim.x) {
         const uint32_t t = divide(i, a.pair_count), p = i - t * a.pairs;
         const uint32_t axis = a.axes ? (uint32_t)__ldg(a.axes + p) : 0u;
         float2 cs = make_float2(1.0f, 0.0f);              // a pair of no axis does not turn
@@ -105,75 +136,83 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
             sincospif(2.0f * (float)(turns - rint(turns)), &cs.y, &cs.x);
             cs.y *= a.sign;
         }
-        angle[t * a.pairs + (P > 1 ? (p % P / 2 * a.turned + p / P) * 2 + p % 2 : p)] = cs;
+        angle[t * a.turned * P + (P > 1 ? (p % P / 2 * a.turned + p / P) * 2 + p % 2 : p)] = cs;
     }
     __syncthreads();
-    for (uint32_t first = 0;;) {
 #pragma unroll
-        for (int k = 0; k < kItems; ++k) {
-            if (place[k] == -2) continue;
-            if (place[k] == -1) {
-                *reinterpret_cast<Raw*>(dst[k]) = x[k];
-                continue;
-            }
-            float u[W], v[W];
-            A::unpack(x[k], u);
-            if constexpr (TWO) A::unpack(y[k], v);
+    for (int k = 0; k < kItems; ++k) {
+        if (place[k] == -2) continue;
+        if (place[k] >= 0) {
+            if constexpr (W == 1) {
+                const float2 cs = angle[place[k]];
+                const float p = bf16_low(x[k].w[0]), q = bf16_low(y[k].w[0]);
+                x[k].w[0] = bf16_pair(p * cs.x - q * cs.y, 0.0f);
+                y[k].w[0] = bf16_pair(p * cs.y + q * cs.x, 0.0f);
+            } else if constexpr (ADJACENT) {
+                float2 cs[P];
+                if constexpr (W == 8) {
 #pragma unroll
-            for (int j = 0; j < P; j += 2) {
-                float4 cs;
-                if constexpr (P > 1) {
-                    cs = *reinterpret_cast<const float4*>(angle + place[k] + j * a.turned);
+                    for (int j = 0; j < P; j += 2) {
+                        const float4 two = *reinterpret_cast<const float4*>(angle + place[k] + j * a.turned);
+                        cs[j] = make_float2(two.x, two.y);
+                        cs[j + 1] = make_float2(two.z, two.w);
+                    }
                 } else {
-                    const float2 one = angle[place[k]];
-                    cs = make_float4(one.x, one.y, 0.0f, 0.0f);
+                    cs[0] = angle[place[k]];
                 }
 #pragma unroll
-                for (int e = 0; e < (P > 1 ? 2 : 1); ++e) {
-                    const float c = e ? cs.z : cs.x, s = e ? cs.w : cs.y;
-                    float& p = TWO ? u[j + e] : u[(2 * (j + e)) % W];
-                    float& q = TWO ? v[j + e] : u[(2 * (j + e) + 1) % W];
-                    const float p0 = p, q0 = q;
-                    p = p0 * c - q0 * s;
-                    q = p0 * s + q0 * c;
+                for (int j = 0; j < P; ++j) {
+                    const float p = bf16_low(x[k].w[j]), q = bf16_high(x[k].w[j]);
+                    const uint32_t turned = bf16_pair(p * cs[j].x - q * cs[j].y, p * cs[j].y + q * cs[j].x);
+                    if (W < 8 || j < left[W == 8 ? k : 0]) x[k].w[j] = turned;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < W / 2; ++j) {
+                    const float4 cs = *reinterpret_cast<const float4*>(angle + place[k] + 2 * j * a.turned);
+                    const float2 c = make_float2(cs.x, cs.z), s = make_float2(cs.y, cs.w);
+                    const float2 p = make_float2(bf16_low(x[k].w[j]), bf16_high(x[k].w[j])), q = make_float2(bf16_low(y[k].w[j]), bf16_high(y[k].w[j]));
+                    const float2 u = fma2(p, c, mul2(q, make_float2(-s.x, -s.y))), v = fma2(p, s, mul2(q, c));
+                    x[k].w[j] = bf16_pair(u.x, u.y);
+                    y[k].w[j] = bf16_pair(v.x, v.y);
                 }
             }
-            *reinterpret_cast<Raw*>(dst[k]) = A::pack(u);
-            if constexpr (TWO) *reinterpret_cast<Raw*>(dst[k] + (ADJACENT ? 1 : a.pairs)) = A::pack(v);
+            if constexpr (U::kTwo) store_words<W>(dst[k] + (ADJACENT ? 1 : a.pairs), y[k]);
         }
-        first += kBatch;
-        if (first >= total) break;
-        fetch(first);
+        store_words<W>(dst[k], x[k]);
     }
 }
 
 template <int W, bool ADJACENT>
 int launch_rotary(RotaryArgs a, int64_t head_dim, int sms, cudaStream_t stream)
 {
-    a.turned = W == 1 ? a.pairs : ADJACENT ? 2 * a.pairs / W : a.pairs / W;
-    const int units = a.turned + (int)((head_dim - 2 * a.pairs) / W);
-    // Several tokens per CTA, so that their angles keep its threads busy, but not so many that SMs stay idle; a token of more units
-    // than a batch is shared by CTAs where there are few tokens, and where its units exceed a CTA's most.
-    const int64_t token_units = (int64_t)a.heads * units, wanted = (int64_t)sms * 8;
+    using U = Unit<W, ADJACENT>;
+    a.turned = (a.pairs + U::kPairs - 1) / U::kPairs;
+    const int units = a.turned + (int)((head_dim - (U::kTwo ? 2 * a.pairs : a.turned * W)) / W);
+    // No CTA goes round twice: those that did were slower the more rounds they made (16384 tokens of 64 heads of 128 columns: 88 us,
+    // with twice the tokens per CTA 98, with four times 104).  As many whole tokens as fit, or a part of one token's heads.
+    const int64_t token_units = (int64_t)a.heads * units, slots = (int64_t)a.turned * U::kPairs;
     a.tile_heads = a.heads;
     a.tile_tokens = 1;
-    if (token_units > kMostUnits || (token_units > kBatch && a.tokens < wanted)) {
-        const int64_t pieces = (token_units + kBatch - 1) / kBatch;
-        a.tile_heads = (int)((a.heads + pieces - 1) / pieces);
+    if (token_units > kBatch) {
+        a.tile_heads = kBatch / units;           // at least 1: a head has at most 1024 columns
     } else {
-        int64_t most = kAngles / a.pairs;
-        if (most > kMostUnits / token_units) most = kMostUnits / token_units;
-        if (most > 4096 / token_units + 1) most = 4096 / token_units + 1;
-        if (most > a.tokens / wanted) most = a.tokens / wanted;
+        int64_t most = kBatch / token_units;
+        if (most > kAngles / slots) most = kAngles / slots;
+        if (most > a.tokens / sms) most = a.tokens / sms;             // few tokens: a CTA each
         if (most > 1) a.tile_tokens = (int)most;
     }
     a.units = divisor((uint32_t)units);
     a.token_units = divisor((uint32_t)(a.tile_heads * units));
     a.pair_count = divisor((uint32_t)a.pairs);
     a.head_tiles = (a.heads + a.tile_heads - 1) / a.tile_heads;
+    // threads for the units, or for the angles where those are more work (few heads)
+    int64_t threads = ((int64_t)a.tile_tokens * a.tile_heads * units + kItems - 1) / kItems, of_angles = (int64_t)a.tile_tokens * a.pairs / 2;
+    if (threads < of_angles) threads = of_angles;
+    threads = threads > kTurnThreads ? kTurnThreads : (threads + 31) / 32 * 32;
     const int64_t grid = (int64_t)((a.tokens + a.tile_tokens - 1) / a.tile_tokens) * a.head_tiles;
     if (grid > 0x7FFFFFFF) return CAST_ERR_SHAPE;
-    rotary_kernel<W, ADJACENT><<<(unsigned)grid, kTurnThreads, 0, stream>>>(a);
+    rotary_kernel<W, ADJACENT><<<(unsigned)grid, (unsigned)threads, 0, stream>>>(a);
     CAST_CUDA_TRY(cudaGetLastError());
     count_launch();
     return CAST_OK;
@@ -207,7 +246,8 @@ extern "C" int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* 
     if (tokens < 1 || tokens > 0x3FFFFFFF || pairs < 1 || pairs > kMostPairs || head_dim < 2 * (int64_t)pairs || head_dim > 2 * kMostPairs) return CAST_ERR_SHAPE;
     if (((uintptr_t)positions & 3u) || ((uintptr_t)frequencies & 7u) || ((uintptr_t)axes & 3u)) return CAST_ERR_ALIGN;
     RotaryArgs a = {};
-    bool vec = head_dim % 8 == 0 && pairs % (adjacent ? 4 : 8) == 0;
+    // columns that every address, stride and count is a multiple of
+    uint64_t common = 8u | (uint64_t)head_dim | (adjacent ? 0u : (uint64_t)pairs);
     const uint64_t table_bytes[3] = {4ull * (uint64_t)n_axes * (uint64_t)tokens, 8ull * (uint64_t)pairs, 4ull * (uint64_t)pairs};
     const void* const table[3] = {positions, frequencies, axes};
     cast_heads_t own[kMostSets];
@@ -228,8 +268,8 @@ extern "C" int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* 
             if (strides[j] < 0 || strides[j] > ((int64_t)1 << 40) / (j % 2 ? s.heads : tokens)) return CAST_ERR_SHAPE;
         if (!apart(tokens, s.heads, head_dim, s.out_token_stride, s.out_head_stride)) return CAST_ERR_SHAPE;
         if (((uintptr_t)s.in & 1u) || ((uintptr_t)s.out & 1u)) return CAST_ERR_ALIGN;
-        vec = vec && !((uintptr_t)s.in & 15u) && !((uintptr_t)s.out & 15u);
-        for (int j = 0; j < 4; ++j) vec = vec && strides[j] % 8 == 0;
+        common |= (uintptr_t)s.in / 2 | (uintptr_t)s.out / 2;
+        for (int j = 0; j < 4; ++j) common |= (uint64_t)strides[j];
         in_bytes[i] = span_bytes(tokens, s.heads, head_dim, s.in_token_stride, s.in_head_stride);
         out_bytes[i] = span_bytes(tokens, s.heads, head_dim, s.out_token_stride, s.out_head_stride);
         a.set[i] = {s.in, s.out, s.in_token_stride, s.in_head_stride, s.out_token_stride, s.out_head_stride, (int32_t)heads};
@@ -274,6 +314,13 @@ extern "C" int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* 
     int device = 0, sms = 0;
     CAST_CUDA_TRY(cudaGetDevice(&device));
     CAST_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-    if (vec) return adjacent ? launch_rotary<8, true>(a, head_dim, sms, st) : launch_rotary<8, false>(a, head_dim, sms, st);
-    return adjacent ? launch_rotary<1, true>(a, head_dim, sms, st) : launch_rotary<1, false>(a, head_dim, sms, st);
+    const int w = (int)(common & (~common + 1));          // the lowest bit: 1, 2, 4 or 8
+    if (adjacent)
+        return w == 8   ? launch_rotary<8, true>(a, head_dim, sms, st)
+               : w >= 2 ? launch_rotary<2, true>(a, head_dim, sms, st)
+                        : launch_rotary<1, true>(a, head_dim, sms, st);
+    return w == 8   ? launch_rotary<8, false>(a, head_dim, sms, st)
+           : w == 4 ? launch_rotary<4, false>(a, head_dim, sms, st)
+           : w == 2 ? launch_rotary<2, false>(a, head_dim, sms, st)
+                    : launch_rotary<1, false>(a, head_dim, sms, st);
 }
