@@ -58,6 +58,27 @@ def _on(device: torch.device, call) -> None:
             B.check(call(_raw_stream(device.index)))
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _call(index: int, function, *args) -> None:
+    """One call of the library, with device `index` current and its current stream as the last argument."""
+    if index == _current_device():
+        B.check(function(*args, _raw_stream(index)))
+    else:
+        with torch.cuda.device(index):
+            B.check(function(*args, _raw_stream(index)))
+
+
+def _taken(t, dtype, index: int) -> bool:
+    """The usual case of what _need() asks for, decided in a microsecond less; where this is False, _need() says why or lets it pass."""
+    return type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index and t.is_contiguous() and not t.requires_grad
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
 def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale * table[ids] as bf16 [*ids.shape, dim]; zero rows for ids outside the table."""
     _need(table, "table", torch.bfloat16, 2)
@@ -162,23 +183,25 @@ def orthogonalize(updates: Sequence[torch.Tensor], steps: int = 5, coeffs: Optio
     return list(outs)
 
 
-def _rows(x: torch.Tensor, weight: torch.Tensor, first: str) -> Tuple[int, int]:
-    """(tokens, dim) of an array of rows and the weight of their columns."""
-    if isinstance(x, torch.Tensor) and x.dim() < 1:
+def _rows(x: torch.Tensor, weight: torch.Tensor, first: str, *others: Tuple[Optional[torch.Tensor], str]) -> Tuple[int, int, int]:
+    """(tokens, dim, device index) of an array of rows, the weight of their columns and arrays of the same shape (or None)."""
+    if not isinstance(x, torch.Tensor) or not _taken(x, torch.bfloat16, x.get_device()) or not x.is_cuda:
+        _need(x, first, torch.bfloat16, x.dim() if isinstance(x, torch.Tensor) else 1)
+    index, shape = x.get_device(), x.shape
+    if not shape:
         raise ValueError(f"{first}: no columns")
-    _need(x, first, torch.bfloat16, x.dim() if isinstance(x, torch.Tensor) else 1)
-    _need(weight, "weight", (torch.float32, torch.bfloat16), 1, x.device)
-    dim = x.shape[-1]
+    if not (_taken(weight, torch.bfloat16, index) or _taken(weight, torch.float32, index)) or weight.dim() != 1:
+        _need(weight, "weight", (torch.float32, torch.bfloat16), 1, x.device)
+    dim = shape[-1]
     if weight.numel() != dim:
         raise ValueError(f"weight: {weight.numel()} entries for {dim} columns")
-    return (x.numel() // dim if dim else 0), dim
-
-
-def _like(t: Optional[torch.Tensor], name: str, x: torch.Tensor) -> None:
-    if t is not None:
-        _need(t, name, torch.bfloat16, x.dim(), x.device)
-        if t.shape != x.shape:
-            raise ValueError(f"{name}: shape {tuple(t.shape)} instead of {tuple(x.shape)}")
+    for t, name in others:
+        if t is not None:
+            if not _taken(t, torch.bfloat16, index):
+                _need(t, name, torch.bfloat16, len(shape), x.device)
+            if t.shape != shape:
+                raise ValueError(f"{name}: shape {tuple(t.shape)} instead of {tuple(shape)}")
+    return (x.numel() // dim if dim else 0), dim, index
 
 
 def _bytes_on(device: torch.device, n: int) -> torch.Tensor:
@@ -189,43 +212,36 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
              sum_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(y, h): h = x + residual (x itself without a residual), y = weight h / sqrt(mean(h^2) + eps) over the last dimension, both
     bf16.  weight: bf16 or fp32.  sum_out may be residual (or x), which h then replaces."""
-    tokens, dim = _rows(x, weight, "x")
-    _like(residual, "residual", x)
-    _like(out, "out", x)
-    _like(sum_out, "sum_out", x)
+    tokens, dim, index = _rows(x, weight, "x", (residual, "residual"), (out, "out"), (sum_out, "sum_out"))
     if residual is None and sum_out is not None:
         raise ValueError("sum_out needs a residual")
     y = torch.empty_like(x) if out is None else out
     h = x if residual is None else torch.empty_like(x) if sum_out is None else sum_out
     if tokens:
-        _on(x.device, lambda stream: B.cast_rms_norm(x.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
-                                                     weight.dtype == torch.float32, y.data_ptr(), None if residual is None else h.data_ptr(), tokens, dim,
-                                                     eps, stream))
+        _call(index, B.load_library().cast_rms_norm, x.data_ptr(), _ptr(residual), weight.data_ptr(), weight.dtype is torch.float32, y.data_ptr(),
+              None if residual is None else h.data_ptr(), tokens, dim, eps)
     return y, h
 
 
 def rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
                 sum_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(q, scales, h): rms_norm with y as float8_e4m3fn values and a power of two (float8_e8m0fnu) for every 32 columns."""
-    tokens, dim = _rows(x, weight, "x")
-    _like(residual, "residual", x)
-    _like(sum_out, "sum_out", x)
+    tokens, dim, index = _rows(x, weight, "x", (residual, "residual"), (sum_out, "sum_out"))
     if residual is None and sum_out is not None:
         raise ValueError("sum_out needs a residual")
     q = torch.empty_like(x, dtype=torch.float8_e4m3fn)
     scales = x.new_empty((*x.shape[:-1], (dim + 31) // 32), dtype=torch.float8_e8m0fnu)
     h = x if residual is None else torch.empty_like(x) if sum_out is None else sum_out
     if tokens:
-        _on(x.device, lambda stream: B.cast_rms_norm_mx(x.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
-                                                        weight.dtype == torch.float32, q.data_ptr(), scales.data_ptr(),
-                                                        None if residual is None else h.data_ptr(), tokens, dim, eps, stream))
+        _call(index, B.load_library().cast_rms_norm_mx, x.data_ptr(), _ptr(residual), weight.data_ptr(), weight.dtype is torch.float32, q.data_ptr(),
+              scales.data_ptr(), None if residual is None else h.data_ptr(), tokens, dim, eps)
     return q, scales, h
 
 
 @functools.lru_cache(maxsize=1024)
 def _rms_norm_grad_bytes(tokens: int, dim: int, device_index: int) -> int:
-    """Workspace on the current device, whose index the caller names."""
-    rc, n = B.cast_rms_norm_grad_workspace(tokens, dim)
+    with torch.cuda.device(device_index):
+        rc, n = B.cast_rms_norm_grad_workspace(tokens, dim)
     B.check(rc)
     return n
 
@@ -234,20 +250,17 @@ def rms_norm_grad(grad_y: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, g
                   weight_grad: bool = True, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(grad_x bf16, grad_weight fp32 or None) of rms_norm from the h it returned.  grad_h: the gradient that reaches h from what
     comes after on the residual stream; grad_x is then the gradient of x and of residual.  out may be grad_h."""
-    tokens, dim = _rows(h, weight, "h")
-    _like(grad_y, "grad_y", h)
-    _like(grad_h, "grad_h", h)
-    _like(out, "out", h)
+    tokens, dim, index = _rows(h, weight, "h", (grad_y, "grad_y"), (grad_h, "grad_h"), (out, "out"))
+    if grad_y is None:
+        raise ValueError("grad_y: a CUDA tensor is needed")
     gx = torch.empty_like(h) if out is None else out
     gw = torch.empty_like(weight, dtype=torch.float32) if weight_grad else None
     if tokens == 0:
         return gx, gw.zero_() if gw is not None else None
-    def call(stream):
-        ws = _bytes_on(h.device, _rms_norm_grad_bytes(tokens, dim, h.device.index)) if weight_grad else None
-        return B.cast_rms_norm_grad(grad_y.data_ptr(), h.data_ptr(), weight.data_ptr(), weight.dtype == torch.float32,
-                                    None if grad_h is None else grad_h.data_ptr(), gx.data_ptr(), None if gw is None else gw.data_ptr(), tokens, dim, eps,
-                                    None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream)
-    _on(h.device, call)
+    n = _rms_norm_grad_bytes(tokens, dim, index) if weight_grad else 0
+    ws = _bytes_on(h.device, n) if weight_grad else None
+    _call(index, B.load_library().cast_rms_norm_grad, grad_y.data_ptr(), h.data_ptr(), weight.data_ptr(), weight.dtype is torch.float32, _ptr(grad_h),
+          gx.data_ptr(), _ptr(gw), tokens, dim, eps, _ptr(ws), n)
     return gx, gw
 
 
@@ -294,50 +307,50 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, 
     """Turns the heads of q and k (bf16 [tokens, heads, head_dim], any strides with contiguous columns; k may be None) by the
     positions, int32 [axes, tokens] or [tokens].  inverse: the other way, which takes gradients back.  out: where the results go (q and k
     themselves, or arrays of any strides); new contiguous arrays without."""
-    _need(positions, "positions", torch.int32, positions.dim() if isinstance(positions, torch.Tensor) and positions.dim() in (1, 2) else 2)
-    dev = positions.device
+    if not isinstance(positions, torch.Tensor) or positions.dim() not in (1, 2) or not _taken(positions, torch.int32, positions.get_device()) or not positions.is_cuda:
+        _need(positions, "positions", torch.int32, positions.dim() if isinstance(positions, torch.Tensor) and positions.dim() in (1, 2) else 2)
+    dev, index = positions.device, positions.get_device()
     n_axes, tokens = (1, positions.shape[0]) if positions.dim() == 1 else positions.shape
     if n_axes < spectrum.n_axes:
         raise ValueError(f"positions: {n_axes} axes for a spectrum of {spectrum.n_axes}")
-    if spectrum.frequencies.device != dev:
+    if spectrum.frequencies.get_device() != index:
         raise ValueError(f"spectrum: on {spectrum.frequencies.device} instead of {dev}")
-    results: List[Optional[torch.Tensor]] = []
-    sets = b""
+    if k is None and out is not None and out[1] is not None:
+        raise ValueError("out[1]: there is no k")
     head_dim = q.shape[-1] if isinstance(q, torch.Tensor) and q.dim() else 0
-    for i, (x, name) in enumerate(((q, "q"), (k, "k"))):
-        if x is None and i == 1:
-            if out is not None and out[1] is not None:
-                raise ValueError("out[1]: there is no k")
-            results.append(None)
-            continue
-        heads, from_token, from_head = _need_heads(x, name, dev, tokens, None, head_dim)
+    sets, n_sets = b"", 0
+    results: List[Optional[torch.Tensor]] = [None, None]
+    for i in (0, 1) if k is not None else (0,):
+        x = k if i else q
+        heads, from_token, from_head = _need_heads(x, "k" if i else "q", index, tokens, None, head_dim)
         if out is None:
-            o = torch.empty_like(x, memory_format=torch.contiguous_format)
             to_token, to_head = heads * head_dim, head_dim
+            o = torch.empty_strided((tokens, heads, head_dim), (to_token, to_head, 1), dtype=torch.bfloat16, device=dev)
         else:
             o = out[i]
-            _, to_token, to_head = _need_heads(o, f"out[{i}]", dev, tokens, heads, head_dim)
-        results.append(o)
+            _, to_token, to_head = _need_heads(o, f"out[{i}]", index, tokens, heads, head_dim)
+        results[i] = o
         if heads:
             sets += struct.pack("7q", x.data_ptr(), o.data_ptr(), heads, from_token, from_head, to_token, to_head)      # a cast_heads_t
+            n_sets += 1
     if 2 * spectrum.pairs > head_dim:
         raise ValueError(f"spectrum: {2 * spectrum.pairs} columns of heads of {head_dim}")
-    if tokens and sets:
-        _on(dev, lambda stream: B.cast_rotary(sets, positions.data_ptr(), spectrum.frequencies.data_ptr(), spectrum.axes.data_ptr(), n_axes,
-                                              spectrum.pairs, spectrum.adjacent, inverse, tokens, head_dim, stream))
+    if tokens and n_sets:
+        _call(index, B.load_library().cast_rotary, sets, n_sets, positions.data_ptr(), spectrum.frequencies.data_ptr(), spectrum.axes.data_ptr(), n_axes,
+              spectrum.pairs, spectrum.adjacent, inverse, tokens, head_dim)
     return results[0], results[1]
 
 
-def _need_heads(t: torch.Tensor, name: str, device, tokens: int, heads: Optional[int], head_dim: int) -> Tuple[int, int, int]:
+def _need_heads(t: torch.Tensor, name: str, index: int, tokens: int, heads: Optional[int], head_dim: int) -> Tuple[int, int, int]:
     """(heads, token stride, head stride) of an array of heads."""
-    if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name}: requires a gradient, but results carry no autograd graph (call under torch.no_grad(), or pass it detached)")
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: requires a gradient, but results carry no autograd graph (call under torch.no_grad(), or pass it detached)")
     if t.dtype is not torch.bfloat16:
         raise ValueError(f"{name}: {t.dtype} is not {torch.bfloat16}")
-    if t.device != device:
-        raise ValueError(f"{name}: on {t.device} instead of {device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name}: on {t.device} instead of cuda:{index}")
     shape = t.shape
     if len(shape) != 3 or shape[0] != tokens or shape[2] != head_dim or heads not in (None, shape[1]):
         raise ValueError(f"{name}: shape {tuple(shape)} instead of {(tokens, 'heads' if heads is None else heads, head_dim)}")
@@ -380,23 +393,23 @@ class GradientSet:
                 rc, self._bytes = B.cast_grads_workspace(self._handle)
                 B.check(rc)
 
-    def _call(self, call) -> torch.Tensor:
+    def _run(self, function, *args) -> torch.Tensor:
         if self._handle is None:
             if not self._empty:
                 raise ValueError("the set is closed")
             return torch.zeros((), dtype=torch.float32, device=self.device)
         norm = torch.empty_strided((), (), dtype=torch.float32, device=self.device)
         ws = _bytes_on(self.device, self._bytes)
-        _on(self.device, lambda stream: call(norm.data_ptr(), ws.data_ptr(), stream))
+        _call(self.device.index, function, self._handle, *args, norm.data_ptr(), ws.data_ptr(), self._bytes)
         return norm
 
     def norm(self, scale: float = 1.0) -> torch.Tensor:
         """The norm of scale times all gradients, fp32 on the device."""
-        return self._call(lambda norm, ws, stream: B.cast_grads_norm(self._handle, scale, norm, ws, self._bytes, stream))
+        return self._run(B.load_library().cast_grads_norm, scale)
 
     def clip(self, max_norm: float, scale: float = 1.0) -> torch.Tensor:
         """outs = grads * scale * min(1, max_norm / norm); returns the norm (of scale times all gradients, before clipping)."""
-        return self._call(lambda norm, ws, stream: B.cast_grads_clip(self._handle, max_norm, scale, norm, ws, self._bytes, stream))
+        return self._run(B.load_library().cast_grads_clip, max_norm, scale)
 
     def close(self) -> None:
         if self._handle is not None:
