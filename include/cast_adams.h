@@ -592,7 +592,7 @@ CAST_API int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, con
  * The pairs are columns (i, i + pairs), or (2i, 2i + 1) where adjacent != 0; columns from 2 * pairs on are copied.  inverse != 0 turns the other
  * way: the gradient.
  *
- *   sets          host array of n_sets (1 to 4) arrays of heads, e.g. queries and keys (cast_heads_t: bf16, strides in entries, the
+ *   sets          host array of n_sets (1 to 4) arrays of heads, e.g. queries and keys (cast_heads_t: bf16, strides in entries, below 2^31, the
  *                 columns of a head contiguous; tokens and heads in either order; an input may be broadcast by a stride of 0).  out may be in itself
  *                 with the same strides, and sets may lie side by side in the rows of one fused array; otherwise no result may overlap
  *                 an input or another result.

@@ -18,8 +18,6 @@ namespace {
 constexpr int kMostSets = 4;              // arrays of heads turned by one call (queries, keys, ...)
 constexpr int kMostPairs = 512;
 constexpr int kTurnThreads = 256;
-constexpr int kItems = 4;                 // units of a thread
-constexpr int kBatch = kTurnThreads * kItems;
 constexpr int kAngles = 1024;             // cosines and sines of a CTA (8 KB)
 
 // i / d for i < 2^16, d < 2^16
@@ -32,7 +30,7 @@ __device__ __forceinline__ uint32_t divide(uint32_t i, Divisor v) { return v.d >
 struct HeadSet {
     const uint16_t* in;
     uint16_t* out;
-    int64_t in_token, in_head, out_token, out_head;     // strides in entries
+    int32_t in_token, in_head, out_token, out_head;     // strides in entries
     int32_t first;                                       // heads of the sets before it
 };
 
@@ -89,24 +87,25 @@ struct Unit {
     static constexpr int kColumns = ADJACENT ? 2 * kPairs : W;               // from one unit's first column to the next one's
 };
 
-template <int W, bool ADJACENT>
-__global__ void __launch_bounds__(kTurnThreads, ADJACENT ? 5 : 4)
+// ITEMS: units of a thread, all of them in flight.
+template <int W, bool ADJACENT, int ITEMS>
+__global__ void __launch_bounds__(kTurnThreads, ITEMS < 4 ? 6 : 5)
 rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
     using U = Unit<W, ADJACENT>;
     constexpr int P = U::kPairs;
     // [token][pair of a unit / 2][unit][2]: neighbouring units, which neighbouring threads hold, lie side by side
     __shared__ __align__(16) float2 angle[kAngles];
-    const int64_t token0 = (int64_t)(blockIdx.x / a.head_tiles) * a.tile_tokens;
+    const int token0 = (int)(blockIdx.x / a.head_tiles) * a.tile_tokens;
     const int head0 = (int)(blockIdx.x % a.head_tiles) * a.tile_heads;
-    const int tokens = (int)min((int64_t)a.tile_tokens, a.tokens - token0), heads = min(a.tile_heads, a.heads - head0);
+    const int tokens = min(a.tile_tokens, a.tokens - token0), heads = min(a.tile_heads, a.heads - head0);
     const uint32_t total = (uint32_t)tokens * (uint32_t)heads * a.units.d;
-    Words<W> x[kItems], y[U::kTwo ? kItems : 1];
-    uint16_t* dst[kItems];
-    int place[kItems];                    // of the unit's first angles, -1: a copy, -2: none
-    int left[ADJACENT && W == 8 ? kItems : 1];        // pairs that turn from the unit's first one on
+    Words<W> x[ITEMS], y[U::kTwo ? ITEMS : 1];
+    uint16_t* dst[ITEMS];
+    int place[ITEMS];                    // of the unit's first angles, -1: a copy, -2: none
+    int left[ADJACENT && W == 8 ? ITEMS : 1];        // pairs that turn from the unit's first one on
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         const uint32_t i = threadIdx.x + k * blockDim.x;
         place[k] = -2;
         if (i >= total) continue;
@@ -116,7 +115,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
         int s = 0;
         while (s + 1 < a.sets && head >= a.set[s + 1].first) ++s;
         const HeadSet& hs = a.set[s];
-        const int64_t token = token0 + t, own = head - hs.first;
+        const int64_t token = token0 + (int)t, own = head - hs.first;           // 32-bit factors of the strides
         const bool turns = u < a.turned;
         const int col = turns ? u * U::kColumns : (U::kTwo ? 2 * a.pairs : a.turned * W) + (u - a.turned) * W;      // the unit's first column
         const uint16_t* src = hs.in + token * hs.in_token + own * hs.in_head + col;
@@ -140,7 +139,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         if (place[k] == -2) continue;
         if (place[k] >= 0) {
             if constexpr (W == 1) {
@@ -183,19 +182,20 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
     }
 }
 
-template <int W, bool ADJACENT>
-int launch_rotary(RotaryArgs a, int64_t head_dim, int sms, cudaStream_t stream)
+template <int W, bool ADJACENT, int ITEMS>
+int launch_items(RotaryArgs a, int units, int sms, cudaStream_t stream)
 {
     using U = Unit<W, ADJACENT>;
-    a.turned = (a.pairs + U::kPairs - 1) / U::kPairs;
-    const int units = a.turned + (int)((head_dim - (U::kTwo ? 2 * a.pairs : a.turned * W)) / W);
-    // No CTA goes round twice: those that did were slower the more rounds they made (16384 tokens of 64 heads of 128 columns: 88 us,
+    constexpr int kBatch = kTurnThreads * ITEMS;
+    // No CTA goes round twice: those that did were slower the more rounds they made (16384 tokens of 64 heads of 128 columns, halves: 88 us,
     // with twice the tokens per CTA 98, with four times 104).  As many whole tokens as fit, or a part of one token's heads.
     const int64_t token_units = (int64_t)a.heads * units, slots = (int64_t)a.turned * U::kPairs;
     a.tile_heads = a.heads;
     a.tile_tokens = 1;
     if (token_units > kBatch) {
-        a.tile_heads = kBatch / units;           // at least 1: a head has at most 1024 columns
+        // CTAs of about as many heads each; at least one fits, since a head has at most 1024 columns
+        const int fit = kBatch / units, pieces = (a.heads + fit - 1) / fit;
+        a.tile_heads = (a.heads + pieces - 1) / pieces;
     } else {
         int64_t most = kBatch / token_units;
         if (most > kAngles / slots) most = kAngles / slots;
@@ -207,15 +207,36 @@ int launch_rotary(RotaryArgs a, int64_t head_dim, int sms, cudaStream_t stream)
     a.pair_count = divisor((uint32_t)a.pairs);
     a.head_tiles = (a.heads + a.tile_heads - 1) / a.tile_heads;
     // threads for the units, or for the angles where those are more work (few heads)
-    int64_t threads = ((int64_t)a.tile_tokens * a.tile_heads * units + kItems - 1) / kItems, of_angles = (int64_t)a.tile_tokens * a.pairs / 2;
+    int64_t threads = ((int64_t)a.tile_tokens * a.tile_heads * units + ITEMS - 1) / ITEMS, of_angles = (int64_t)a.tile_tokens * a.pairs / 2;
     if (threads < of_angles) threads = of_angles;
     threads = threads > kTurnThreads ? kTurnThreads : (threads + 31) / 32 * 32;
     const int64_t grid = (int64_t)((a.tokens + a.tile_tokens - 1) / a.tile_tokens) * a.head_tiles;
     if (grid > 0x7FFFFFFF) return CAST_ERR_SHAPE;
-    rotary_kernel<W, ADJACENT><<<(unsigned)grid, (unsigned)threads, 0, stream>>>(a);
+    rotary_kernel<W, ADJACENT, ITEMS><<<(unsigned)grid, (unsigned)threads, 0, stream>>>(a);
     CAST_CUDA_TRY(cudaGetLastError());
     count_launch();
     return CAST_OK;
+}
+
+template <int W, bool ADJACENT>
+int launch_rotary(RotaryArgs a, int64_t head_dim, int sms, cudaStream_t stream)
+{
+    using U = Unit<W, ADJACENT>;
+    a.turned = (a.pairs + U::kPairs - 1) / U::kPairs;
+    const int units = a.turned + (int)((head_dim - (U::kTwo ? 2 * a.pairs : a.turned * W)) / W);
+    // Halves: two units, which are four 16-byte accesses, per thread and 6 CTAs per SM are enough (81.4 us for those 16384 tokens; four units
+    // and 4 CTAs 82.6).  Adjacent units have one access: as many as keep a token in one CTA, which works out its angles once, and leave no
+    // thread idle (8190 tokens of 48 heads of 128 columns: two 38.9 us, three 36.5, four 38.8; 16384 of 64: two 99.9, three 93.5, four 90.0).
+    if constexpr (W == 8 && !ADJACENT) {
+        return launch_items<W, ADJACENT, 2>(a, units, sms, stream);
+    } else if constexpr (W == 8) {
+        const int64_t token_units = (int64_t)a.heads * units;
+        return token_units <= 2 * kTurnThreads   ? launch_items<W, ADJACENT, 2>(a, units, sms, stream)
+               : token_units <= 3 * kTurnThreads ? launch_items<W, ADJACENT, 3>(a, units, sms, stream)
+                                                 : launch_items<W, ADJACENT, 4>(a, units, sms, stream);
+    } else {
+        return launch_items<W, ADJACENT, 4>(a, units, sms, stream);
+    }
 }
 
 // Bytes from the first to behind the last entry of `heads` heads of `tokens` tokens.
@@ -262,17 +283,16 @@ extern "C" int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* 
         if (tokens == 1) s.in_token_stride = s.out_token_stride = 0;
         if (s.heads == 1) s.in_head_stride = s.out_head_stride = 0;
         if (s.heads < 1 || s.heads > 65536) return CAST_ERR_SHAPE;
-        // strides up to 2^40 entries: products with the counts fit 64 bits
         const int64_t strides[4] = {s.in_token_stride, s.in_head_stride, s.out_token_stride, s.out_head_stride};
         for (int j = 0; j < 4; ++j)
-            if (strides[j] < 0 || strides[j] > ((int64_t)1 << 40) / (j % 2 ? s.heads : tokens)) return CAST_ERR_SHAPE;
+            if (strides[j] < 0 || strides[j] > 0x7FFFFFFF) return CAST_ERR_SHAPE;
         if (!apart(tokens, s.heads, head_dim, s.out_token_stride, s.out_head_stride)) return CAST_ERR_SHAPE;
         if (((uintptr_t)s.in & 1u) || ((uintptr_t)s.out & 1u)) return CAST_ERR_ALIGN;
         common |= (uintptr_t)s.in / 2 | (uintptr_t)s.out / 2;
         for (int j = 0; j < 4; ++j) common |= (uint64_t)strides[j];
         in_bytes[i] = span_bytes(tokens, s.heads, head_dim, s.in_token_stride, s.in_head_stride);
         out_bytes[i] = span_bytes(tokens, s.heads, head_dim, s.out_token_stride, s.out_head_stride);
-        a.set[i] = {s.in, s.out, s.in_token_stride, s.in_head_stride, s.out_token_stride, s.out_head_stride, (int32_t)heads};
+        a.set[i] = {s.in, s.out, (int32_t)s.in_token_stride, (int32_t)s.in_head_stride, (int32_t)s.out_token_stride, (int32_t)s.out_head_stride, (int32_t)heads};
         heads += s.heads;
         ptrs[3 + 2 * i] = s.in;
         ptrs[4 + 2 * i] = s.out;
