@@ -100,6 +100,14 @@ __device__ __forceinline__ uint32_t group_scale(uint32_t top)
 // 1 / scale, exact
 __device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float(s == 255u ? 0x7FC00000u : (254u - s) << 23); }
 
+// The largest of three magnitudes as bits, NaN where one is.
+__device__ __forceinline__ uint32_t largest(uint32_t top, float a, float b)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(__uint_as_float(top)), "f"(a), "f"(b));
+    return __float_as_uint(r) & 0x7FFFFFFFu;
+}
+
 template <int W, int N, bool SPLIT, bool RES, bool MX, class WT>
 __global__ void __launch_bounds__(SPLIT ? 1024 : 256)
 rms_norm_kernel(const __grid_constant__ NormArgs a)
@@ -153,7 +161,8 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
     }
     const float mean = fmaf(row_sum<SPLIT>(square, a.lanes, part), a.inverse_dim, a.eps);
     float r = __frsqrt_rn(mean), pre = 1.0f;
-    if (SPLIT ? odd_row(mean) : __any_sync(0xFFFFFFFFu, odd_row(mean))) {
+    const bool odd = odd_row(mean);
+    if (SPLIT ? odd : __any_sync(0xFFFFFFFFu, odd)) {
         double s = 0.0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -163,7 +172,7 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
             for (int j = 0; j < W; ++j) s = fma((double)v[j], (double)v[j], s);
         }
         s = row_sum<SPLIT>(s, a.lanes, part64) / (double)a.dim + (double)a.eps;
-        if (odd_row(mean)) {
+        if (odd) {
             pre = odd_factor(s);
             r = (float)(1.0 / sqrt(s) / (double)pre);
         }
@@ -177,9 +186,13 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
         for (int j = 0; j < W; ++j) w[j] = 0.0f;
         if (in) A::weights(static_cast<const WT*>(a.weight) + c * W, w);
+        if (odd) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] *= pre;
+        }
         // two bf16 entries multiply exactly: one rounding less than the other way round
 #pragma unroll
-        for (int j = 0; j < W; ++j) v[j] = v[j] * pre * w[j] * r;
+        for (int j = 0; j < W; ++j) v[j] = v[j] * w[j] * r;
         if constexpr (!MX) {
             if (in) *reinterpret_cast<Raw*>(a.y + base + (int64_t)c * W) = A::pack(v);
         } else {
@@ -187,7 +200,8 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
             // counts as the largest
             uint32_t top = 0;
 #pragma unroll
-            for (int j = 0; j < W; ++j) top = max(top, __float_as_uint(in ? v[j] : 0.0f) & 0x7FFFFFFFu);
+            for (int j = 0; j < W; j += 2) top = W == 1 ? __float_as_uint(v[0]) & 0x7FFFFFFFu : largest(top, v[j], v[(j + 1) % W]);
+            if (!in) top = 0;
 #pragma unroll
             for (int d = kGroup / W / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
             const uint32_t s = group_scale(top);
@@ -211,15 +225,18 @@ struct Spread {
     bool split;
 };
 
-Spread spread_of(int64_t units, int w)
+Spread spread_of(int64_t units, int w, bool res, bool mx)
 {
     if (w == 8) {
         if (units <= 128) {                   // up to 1024 columns: in a warp
-            int lanes = 8;
-            while (lanes < 32 && lanes < units) lanes *= 2;
+            int lanes = 4;                    // two accesses or more each: 65536 x 128 6.65 us, with one each 8.5
+            while (lanes < 32 && 2 * lanes < units) lanes *= 2;
             return {lanes, (int)((units + lanes - 1) / lanes), false};
         }
-        const int n = units <= 512 ? 1 : units <= 2048 ? 2 : 4;
+        // Fewer accesses per thread leave SMs with too few bytes in flight behind the barrier of a row, more of them with too few CTAs (us;
+        // 16384 x 4096 with residual: one 84.7, two 79.8, four 80.6; without, 8192 x 4096: one 34.6, two 27.6, three 25.5, four 22.9; 8190 x 5120 in
+        // 8 bits: two 49.5, three 47.8, four 47.4; 4096 x 12288 with residual: two 80, four 61.7, eight 69).
+        const int n = units <= 256 ? (res && !mx ? 1 : 2) : units <= 512 ? (res ? 2 : 4) : units <= 768 && res ? 3 : 4;
         return {(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true};
     }
     if (units <= 256) return {32, 8, false};
@@ -661,7 +678,7 @@ int norm_impl(const uint16_t* x, const uint16_t* residual, const void* weight, i
     if ((rc = check_device_memory(ptrs, 7)) != CAST_OK) return rc;
     const int w = dim % 8 == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(weight, 16) && aligned(y, 16) && aligned(q, 8) && aligned(h, 16) ? 8 : 1;
     NormArgs a = {x, residual, weight, y, q, scales, h, (int32_t)tokens, (int32_t)dim, (int32_t)(dim / w), 0, eps, 1.0f / (float)dim};
-    const Spread s = spread_of(a.units, w);
+    const Spread s = spread_of(a.units, w, residual != nullptr, q != nullptr);
     a.lanes = s.lanes;
     const bool f = weight_fp32 != 0;
     if (w == 8) {
@@ -670,7 +687,10 @@ int norm_impl(const uint16_t* x, const uint16_t* residual, const void* weight, i
                    : s.n == 2 ? launch_norm<8, 2, false>(a, f, stream)
                    : s.n == 3 ? launch_norm<8, 3, false>(a, f, stream)
                               : launch_norm<8, 4, false>(a, f, stream);
-        return s.n == 1 ? launch_norm<8, 1, true>(a, f, stream) : s.n == 2 ? launch_norm<8, 2, true>(a, f, stream) : launch_norm<8, 4, true>(a, f, stream);
+        return s.n == 1   ? launch_norm<8, 1, true>(a, f, stream)
+               : s.n == 2 ? launch_norm<8, 2, true>(a, f, stream)
+               : s.n == 3 ? launch_norm<8, 3, true>(a, f, stream)
+                          : launch_norm<8, 4, true>(a, f, stream);
     }
     if (!s.split) return launch_norm<1, 8, false>(a, f, stream);
     return s.n == 8 ? launch_norm<1, 8, true>(a, f, stream) : launch_norm<1, 32, true>(a, f, stream);
