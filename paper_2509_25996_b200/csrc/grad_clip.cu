@@ -382,7 +382,7 @@ extern "C" int cast_grads_create(const cast_grad_t* grads, int n, void** set_out
             throw;
         }
         *set_out = s;
-    } catch (const std::bad_alloc&) {
+    } catch (...) {          // nothing but memory for the tables can fail
         return cuda_failed(cudaErrorMemoryAllocation);
     }
     return CAST_OK;
