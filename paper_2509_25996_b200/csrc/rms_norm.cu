@@ -284,11 +284,11 @@ struct NormGradArgs {
     float inverse_dim;
 };
 
-__device__ __forceinline__ void copy_async(void* shared, const void* global, int bytes)      // 16 bytes, those beyond `bytes` as zeros
+__device__ __forceinline__ void copy_async(uint32_t shared, const void* global, int bytes)      // 16 bytes, those beyond `bytes` as zeros
 {
-    const uint32_t to = (uint32_t)__cvta_generic_to_shared(shared);
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(global), "r"(bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(shared), "l"(global), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
 
@@ -305,70 +305,101 @@ struct Part {
 template <int W, int N, int STAGES, bool RES>
 struct Ring {
     static constexpr int kArrays = RES ? 3 : 2;
-    uint4* base;
+    const NormGradArgs& a;
+    int lane, sub, rows;
+    uint32_t slot;                                   // shared address of this thread's first access (W == 8), or of the ring
+    uint32_t apart;                                  // W == 8: bytes between a thread's slots
+    int64_t row, step;                               // the next row to fetch
+    const uint16_t* next[kArrays];                   // W == 8: its entries
     int first[W == 8 ? 1 : kArrays];                 // W == 1: where the current row begins
 
-    static __device__ __forceinline__ const uint16_t* source(const NormGradArgs& a, int k) { return k == 0 ? a.h : k == 1 ? a.dy : a.dh; }
-    __device__ __forceinline__ void fetch(const NormGradArgs& a, int64_t row, int lane, int stage, int sub, int rows)
+    __device__ __forceinline__ const uint16_t* source(int k) const { return k == 0 ? a.h : k == 1 ? a.dy : a.dh; }
+    __device__ __forceinline__ Ring(const NormGradArgs& args, const uint4* shared, int lane_, int sub_, int rows_, int64_t row_, int64_t step_)
+        : a(args), lane(lane_), sub(sub_), rows(rows_), slot(shared_address(shared) + (W == 8 ? threadIdx.x * 16u : 0u)), apart(blockDim.x * 16u), row(row_), step(step_)
     {
 #pragma unroll
-        for (int k = 0; k < kArrays; ++k) {
-            if constexpr (W == 8) {
+        for (int k = 0; k < kArrays; ++k) next[k] = source(k) + row * a.dim;
+    }
+    // The next row, into `stage`.
+    __device__ __forceinline__ void fetch(int stage)
+    {
+        if (row < a.tokens) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int c = i * a.lanes + lane;
-                    const bool in = row < a.tokens && c < a.units;
-                    copy_async(base + ((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x, source(a, k) + (in ? row * a.dim + c * 8 : 0), in ? 16 : 0);
-                }
-            } else if (row < a.tokens) {
-                const uint16_t *begin = source(a, k), *end = begin + (int64_t)a.tokens * a.dim, *from = begin + row * a.dim;
-                const int skip = (int)((uintptr_t)from & 15u) / 2, blocks = (skip + a.dim + 7) / 8;
-                uint16_t* to = reinterpret_cast<uint16_t*>(base) + ((stage * kArrays + k) * rows + sub) * a.window;
-                for (int c = lane; c < blocks; c += a.lanes) {
-                    const uint16_t* p = from - skip + 8 * c;
-                    if (p >= begin) {
-                        copy_async(to + 8 * c, p, (int)min((int64_t)16, (int64_t)(end - p) * 2));
-                    } else {
-                        for (int j = (int)(begin - p); j < 8 && p + j < end; ++j) to[8 * c + j] = p[j];      // the array begins inside a block
+            for (int k = 0; k < kArrays; ++k) {
+                if constexpr (W == 8) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const int c = i * a.lanes + lane;
+                        copy_async(slot + ((stage * kArrays + k) * N + i) * apart, next[k] + (c < a.units ? c * 8 : 0), c < a.units ? 16 : 0);
+                    }
+                } else {
+                    const uint16_t *begin = source(k), *end = begin + (int64_t)a.tokens * a.dim, *from = next[k];
+                    const int skip = (int)((uintptr_t)from & 15u) / 2, blocks = (skip + a.dim + 7) / 8;
+                    const uint32_t to = slot + ((stage * kArrays + k) * rows + sub) * a.window * 2;
+                    for (int c = lane; c < blocks; c += a.lanes) {
+                        const uint16_t* p = from - skip + 8 * c;
+                        if (p >= begin) {
+                            copy_async(to + 16 * c, p, (int)min((int64_t)16, (int64_t)(end - p) * 2));
+                        } else {
+                            // the array begins inside a block
+                            for (int j = (int)(begin - p); j < 8 && p + j < end; ++j) asm volatile("st.shared.u16 [%0], %1;" :: "r"(to + 16 * c + 2 * j), "h"(p[j]) : "memory");
+                        }
                     }
                 }
             }
         }
         copies_commit();
+        row += step;
+#pragma unroll
+        for (int k = 0; k < kArrays; ++k) next[k] += step * a.dim;
     }
     // W == 1: the row at hand
-    __device__ __forceinline__ void turn_to(const NormGradArgs& a, int64_t row, int stage, int sub, int rows)
+    __device__ __forceinline__ void turn_to(int64_t at, int stage)
     {
         if constexpr (W == 1) {
 #pragma unroll
             for (int k = 0; k < kArrays; ++k)
-                first[k] = ((stage * kArrays + k) * rows + sub) * a.window + (int)((uintptr_t)(source(a, k) + row * a.dim) & 15u) / 2;
+                first[k] = ((stage * kArrays + k) * rows + sub) * a.window + (int)((uintptr_t)(source(k) + at * a.dim) & 15u) / 2;
         }
     }
-    __device__ __forceinline__ void get(const NormGradArgs& a, int k, int i, int lane, int stage, float2 (&v)[Part<W>::kPairs]) const
+    __device__ __forceinline__ uint16_t entry(int at) const
+    {
+        uint16_t v;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(slot + at * 2) : "memory");
+        return v;
+    }
+    __device__ __forceinline__ void get(int k, int i, int stage, float2 (&v)[Part<W>::kPairs]) const
     {
         if constexpr (W == 8) {
-            Pairs::unpack(base[((stage * kArrays + k) * N + i) * (int)blockDim.x + (int)threadIdx.x], v);
+            uint4 r;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(slot + ((stage * kArrays + k) * N + i) * apart) : "memory");
+            Pairs::unpack(r, v);
         } else {
-            const uint16_t* row = reinterpret_cast<const uint16_t*>(base) + first[k];
             const int c = Part<1>::column(i, 0, a.lanes, lane), d = Part<1>::column(i, 1, a.lanes, lane);
-            v[0] = make_float2(c < a.dim ? bf16_low(row[c]) : 0.0f, d < a.dim ? bf16_low(row[d]) : 0.0f);
+            v[0] = make_float2(c < a.dim ? bf16_low(entry(first[k] + c)) : 0.0f, d < a.dim ? bf16_low(entry(first[k] + d)) : 0.0f);
         }
     }
 };
 
+// Rows of 1032 to 4096 columns: three on their way and three CTAs of at most 256 threads per SM.  (16384 x 4096 in us, in short runs and under
+// the power limit: 81.8 / 93.7; four rows and two CTAs with twice the registers 91.2 / 96.5; two rows and four CTAs with 64 registers 87.0 / 96.1.)
+template <int W, int N, int STAGES, bool SPLIT> constexpr bool middle_row() { return SPLIT && W == 8 && N == 2 && STAGES == 3; }
 // Threads that a CTA has at most, and CTAs that the registers are to hold.
-template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_threads() { return !SPLIT ? 256 : N * Part<W>::kPairs <= 8 || (W == 8 && STAGES == 2) ? 512 : 1024; }
-template <int W, int N, bool SPLIT> constexpr int grad_blocks() { return !SPLIT || (W == 8 && N == 2) ? 2 : 1; }
+template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_threads()
+{
+    return !SPLIT || middle_row<W, N, STAGES, SPLIT>() ? 256 : N * Part<W>::kPairs <= 8 || (W == 8 && STAGES == 2) ? 512 : 1024;
+}
+template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_blocks() { return middle_row<W, N, STAGES, SPLIT>() ? 3 : !SPLIT || (W == 8 && N == 2) ? 2 : 1; }
 
 template <int W, int N, int STAGES, bool SPLIT, bool RES, class WT>
-__global__ void __launch_bounds__(grad_threads<W, N, STAGES, SPLIT>(), grad_blocks<W, N, SPLIT>())
+__global__ void __launch_bounds__(grad_threads<W, N, STAGES, SPLIT>(), grad_blocks<W, N, STAGES, SPLIT>())
 rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
 {
     constexpr int Q = Part<W>::kPairs;
     extern __shared__ uint4 dynamic[];               // the ring; !SPLIT, afterwards: [rows of the CTA][dim] sums
-    __shared__ float2 part[2][kMostWarps];
+    __shared__ __align__(16) float2 part[2][kMostWarps];
     __shared__ double part64[2][kMostWarps];
+    if (SPLIT && threadIdx.x < 2) part[threadIdx.x][(blockDim.x >> 5) & 31] = both(0.0f);       // behind an odd number of warps; set before the first barrier
     const int lane = SPLIT ? (int)threadIdx.x : (int)threadIdx.x & (a.lanes - 1);
     const int rows = SPLIT ? 1 : (int)blockDim.x / a.lanes, sub = SPLIT ? 0 : (int)threadIdx.x / a.lanes;
     float2 dw[N][Q];
@@ -390,8 +421,7 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             if (d < a.dim) { Access<1>::weights(p + d, v); w[0].y = v[0]; }
         }
     };
-    // A row stays in registers between its two halves where that leaves room for as many warps; with 4 CTAs of 256 threads per SM instead of
-    // 2, which read it from shared memory twice, 16384 x 4096 take 87.3 instead of 91.2 us.
+    // A row stays in registers between its two halves where that leaves as many warps; the others read it from shared memory twice.
     constexpr bool KEPT = N * Q <= 8 && !(SPLIT && W == 8);
     constexpr bool WEIGHTS = N * Q <= 12;            // and the weights of a thread's columns for good
     float2 kept[WEIGHTS ? N : 1][Q];
@@ -401,36 +431,35 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
     }
     const int64_t step = (int64_t)gridDim.x * rows;
     int64_t row0 = (int64_t)blockIdx.x * rows;
-    Ring<W, N, STAGES, RES> ring;
-    ring.base = dynamic;
+    Ring<W, N, STAGES, RES> ring(a, dynamic, lane, sub, rows, row0 + sub, step);
 #pragma unroll
-    for (int k = 0; k + 1 < STAGES; ++k) ring.fetch(a, row0 + sub + k * step, lane, k, sub, rows);
+    for (int k = 0; k + 1 < STAGES; ++k) ring.fetch(k);
     int stage = 0;
     for (int turn = 0; row0 < a.tokens; row0 += step, turn ^= 1, stage = stage + 1 == STAGES ? 0 : stage + 1) {
-        const int64_t row = row0 + sub, ahead = row + (STAGES - 1) * step;
+        const int64_t row = row0 + sub;
         const int free = stage == 0 ? STAGES - 1 : stage - 1;         // the row before was there
         if constexpr (W == 8) {
-            ring.fetch(a, ahead, lane, free, sub, rows);
+            ring.fetch(free);
             copies_wait<STAGES - 1>();
         } else if constexpr (STAGES > 1) {
             copies_wait<STAGES - 2>();
             if constexpr (SPLIT) __syncthreads(); else __syncwarp();   // everyone's blocks are there, and the row before has been read
-            ring.fetch(a, ahead, lane, free, sub, rows);
+            ring.fetch(free);
         } else {
             if constexpr (SPLIT) __syncthreads(); else __syncwarp();
-            ring.fetch(a, ahead, lane, free, sub, rows);
+            ring.fetch(free);
             copies_wait<0>();
             if constexpr (SPLIT) __syncthreads(); else __syncwarp();
         }
         const bool active = row < a.tokens;
-        ring.turn_to(a, active ? row : 0, stage, sub, rows);
+        ring.turn_to(active ? row : 0, stage);
         float2 u[KEPT ? N : 1][Q], g[KEPT ? N : 1][Q], v[KEPT ? N : 1][Q];
         float2 hh = both(0.0f), gh = both(0.0f);     // sums of h^2 and of g h
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int e = KEPT ? i : 0;
-            ring.get(a, 0, i, lane, stage, u[e]);
-            ring.get(a, 1, i, lane, stage, v[e]);
+            ring.get(0, i, stage, u[e]);
+            ring.get(1, i, stage, v[e]);
             if (W == 1 && !active) u[e][0] = v[e][0] = both(0.0f);
             float2 w[Q];
             if constexpr (!WEIGHTS) weight(i, w);
@@ -448,8 +477,12 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             // two buffers: a warp may be one row ahead of another, not two
             if ((threadIdx.x & 31) == 0) part[turn][threadIdx.x >> 5] = s;
             __syncthreads();
-            s = part[turn][0];
-            for (int i = 1; i < (int)(blockDim.x >> 5); ++i) s = add2(s, part[turn][i]);
+            // two warps' sums by one load; where their number is odd the last one is 0
+            s = both(0.0f);
+            for (int i = 0; i < (int)(blockDim.x >> 5); i += 2) {
+                const float4 two = *reinterpret_cast<const float4*>(&part[turn][i]);
+                s = add2(s, add2(make_float2(two.x, two.y), make_float2(two.z, two.w)));
+            }
         }
         const float mean = fmaf(s.x, a.inverse_dim, a.eps);
         float r = __frsqrt_rn(mean), scaled = r;                        // n = h * scaled
@@ -475,8 +508,8 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             if (!active || c >= a.dim) continue;
             if constexpr (!KEPT) {
                 float2 w[Q];
-                ring.get(a, 0, i, lane, stage, u[0]);
-                ring.get(a, 1, i, lane, stage, v[0]);
+                ring.get(0, i, stage, u[0]);
+                ring.get(1, i, stage, v[0]);
                 if constexpr (!WEIGHTS) weight(i, w);
 #pragma unroll
                 for (int j = 0; j < Q; ++j) g[0][j] = mul2(v[0][j], WEIGHTS ? kept[WEIGHTS ? i : 0][j] : w[j]);
@@ -486,7 +519,7 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
                 for (int j = 0; j < Q; ++j) u[e][j] = mul2(u[e][j], both(pre));
             }
             float2 o[Q];
-            if constexpr (RES) ring.get(a, 2, i, lane, stage, o);
+            if constexpr (RES) ring.get(2, i, stage, o);
 #pragma unroll
             for (int j = 0; j < Q; ++j) {
                 const float2 n = mul2(u[e][j], both(scaled));
@@ -582,7 +615,7 @@ GradSpread grad_spread_of(int64_t dim, int w, bool res)
             g.split = true;
             g.n = units <= 1024 ? 2 : 4;
             g.lanes = (int)((units + g.n * 32 - 1) / (g.n * 32)) * 32;
-            g.stages = units <= 2048 ? 2 : 1;
+            g.stages = units <= 512 ? 3 : units <= 2048 ? 2 : 1;
         }
         g.bytes = g.stages * arrays * g.n * (g.split ? g.lanes : 256) * 16;
     } else {
@@ -597,7 +630,7 @@ GradSpread grad_spread_of(int64_t dim, int w, bool res)
     if (g.bytes < sums) g.bytes = sums;
     const int threads = g.split ? g.lanes : 256;
     g.held = (int)(220000 / (g.bytes + 2048));
-    const int by_registers = g.split && w == 8 && g.n == 2 ? 1024 / (threads < 256 ? 256 : threads) : threads <= 512 ? 512 / threads : 1;
+    const int by_registers = g.split && w == 8 && g.n == 2 ? (units <= 512 ? (threads < 256 ? 4 : 3) : 2) : threads <= 512 ? 512 / threads : 1;
     if (g.held > by_registers) g.held = by_registers;
     if (g.held < 1) g.held = 1;
     return g;
@@ -765,9 +798,9 @@ extern "C" int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, c
                  : g.n == 3 ? launch_grad<8, 3, 2, false>(a, g, f, ctas, st)
                             : launch_grad<8, 4, 2, false>(a, g, f, ctas, st);
         else
-            rc = g.n == 2        ? launch_grad<8, 2, 2, true>(a, g, f, ctas, st)
-                 : g.stages == 2 ? launch_grad<8, 4, 2, true>(a, g, f, ctas, st)
-                                 : launch_grad<8, 4, 1, true>(a, g, f, ctas, st);
+            rc = g.n == 4 ? (g.stages == 2 ? launch_grad<8, 4, 2, true>(a, g, f, ctas, st) : launch_grad<8, 4, 1, true>(a, g, f, ctas, st))
+                 : g.stages == 3 ? launch_grad<8, 2, 3, true>(a, g, f, ctas, st)
+                                 : launch_grad<8, 2, 2, true>(a, g, f, ctas, st);
     } else if (!g.split) {
         rc = launch_grad<1, 4, 4, false>(a, g, f, ctas, st);
     } else if (g.n == 8) {
