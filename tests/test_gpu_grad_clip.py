@@ -194,3 +194,17 @@ def test_shapes_streams_capture_and_refusals():
     s.close()
     with pytest.raises(ValueError, match="closed"):
         s.norm()
+
+
+def test_gradients_of_a_plan_are_clipped_in_place_ahead_of_its_step():
+    from paper_2509_25996_b200 import runner
+    state = runner.DeviceModelState([(96, 64), (32, 128)], seed=1, device=DEV)
+    before = [m.g.clone() for m in state.mats]
+    norm = exact_norm(before, 0.5)
+    check(state.clip_gradients(norm / 4, scale=0.5), [m.g for m in state.mats], before, float(torch.tensor(norm / 4, dtype=torch.float32)), 0.5)
+    again = [m.g.clone() for m in state.mats]
+    assert float(state.clip_gradients(norm)) < norm / 3 and all(torch.equal(m.g, g) for m, g in zip(state.mats, again))
+    state.step(runner.Hyper(), B.CAST_F_RESELECT)
+    state.set_nm(1, 4)
+    assert float(state.clip_gradients(norm)) < norm / 3
+    state.close()
