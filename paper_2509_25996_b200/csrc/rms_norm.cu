@@ -387,11 +387,11 @@ struct Ring {
 // Rows of 1032 to 4096 columns: three on their way, two CTAs of up to 256 threads per SM with 128 registers, so that a row stays in
 // registers between its two halves.  (16384 x 4096 in us, in short runs and under the power limit, where instructions count: 83.0 / 86.0 to 88;
 // read from shared memory twice, 80 registers: 81.6 / 94.6; two rows and four CTAs with 64 registers: 87.0 / 96.1; four rows, two CTAs: 91.2 / 96.5.)
-template <int W, int N, int STAGES, bool SPLIT> constexpr bool middle_row() { return SPLIT && W == 8 && N == 2 && STAGES == 3; }
+template <int W, int N, int STAGES, bool SPLIT> constexpr bool kMiddleRow = SPLIT && W == 8 && N == 2 && STAGES == 3;
 // Threads that a CTA has at most, and CTAs that the registers are to hold.
 template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_threads()
 {
-    return !SPLIT || middle_row<W, N, STAGES, SPLIT>() ? 256 : N * Part<W>::kPairs <= 8 || (W == 8 && STAGES == 2) ? 512 : 1024;
+    return !SPLIT || kMiddleRow<W, N, STAGES, SPLIT> ? 256 : N * Part<W>::kPairs <= 8 || (W == 8 && STAGES == 2) ? 512 : 1024;
 }
 template <int W, int N, int STAGES, bool SPLIT> constexpr int grad_blocks() { return !SPLIT || (W == 8 && N == 2) ? 2 : 1; }
 
@@ -426,7 +426,7 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
         }
     };
     // a row stays in registers between its two halves, or is read from shared memory twice
-    constexpr bool KEPT = N * Q <= 8 && (!SPLIT || W == 1 || middle_row<W, N, STAGES, SPLIT>());
+    constexpr bool KEPT = N * Q <= 8 && (!SPLIT || W == 1 || kMiddleRow<W, N, STAGES, SPLIT>);
     constexpr bool WEIGHTS = N * Q <= 12;            // and the weights of a thread's columns for good
     float2 kept[WEIGHTS ? N : 1][Q];
     if constexpr (WEIGHTS) {
