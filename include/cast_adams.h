@@ -549,8 +549,8 @@ CAST_API int cast_product_failures(unsigned long long* count_out, int action);
  *   weight     device, [dim]: bf16, or fp32 where weight_fp32 != 0.
  *   y          device, bf16 [tokens][dim], out.     h          device, bf16 [tokens][dim], out; NULL exactly where residual is.
  *              h may be x or residual itself; otherwise no result may overlap an input or another result.
- *   dim in [1, 32768]; eps >= 0 (a row of zeros needs eps > 0).  dim % 8 == 0 with 16-byte aligned buffers takes the vector
- *   path, anything else a slower scalar one.
+ *   dim in [1, 32768]; eps >= 0 (a row of zeros needs eps > 0).  dim % 8 == 0 with 16-byte aligned buffers takes the fastest path,
+ *   other widths or places slower ones.
  * y is normalised from the rounded h: what is stored is what a backward pass reads.  Sums and statistics are fp32, and fp64 for rows whose
  * squares leave the range of fp32; y is rounded once.  NaN and infinities stay in their row.
  *
