@@ -5,8 +5,8 @@
 //
 // Forward: one pass; a row stays in registers between its sum of squares and its result.  `lanes` threads share a row, each with up to
 // N accesses of W columns: 4 to 32 lanes of a warp (several rows per warp or CTA, no barrier), or a whole CTA.  Bounded by HBM: 16384 x 4096 with
-// residual 79.5 us (537 MB, 6.75 TB/s), 4096 x 12288 61.6 us (6.54 TB/s); the 8-bit form of 8190 x 5120 47.6 us (295 MB, 6.2 TB/s) and 53 under
-// the power limit: its instructions (two passes over a row in registers, groups' maxima, conversions) keep two thirds of the issue slots busy.
+// residual 79.5 us (537 MB, 6.75 TB/s), 4096 x 12288 61.6 us (6.54 TB/s); the 8-bit form of 8190 x 5120 52.2 us (295 MB, 5.7 TB/s) and 57 under
+// the power limit: its instructions (two passes over a row in registers, groups' maxima, conversions) keep the issue slots busy.
 //
 // Gradient: the statistics of a row come from h again instead of being kept (one more multiply-add per column, 4 bytes per row less, nothing to
 // pass on).  CTAs walk over rows with a stride; a thread owns the same columns of all of its rows and sums their part of
@@ -103,6 +103,65 @@ __device__ __forceinline__ uint32_t group_scale(uint32_t top)
 // 1 / scale, exact
 __device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float(s == 255u ? 0x7FC00000u : (254u - s) << 23); }
 
+// Values in fp32 that lie this near to a border of the 8-bit form (units in the last place; two e4m3 values' middle, or a group's maximum at 448 times a
+// power of two) are worked out again in fp64, so that values and scales are those of the exact norm.  The roundings before it are some tens of half units
+// at most, of the sum (whose error counts half), the root and two products: half a unit in the mean square.  (Looking for such values takes 4 of the 52 us of 8190 x 5120, and one row in twenty is worked out again.)
+constexpr uint32_t kNear = 4;
+// the last 20 bits as the upper ones, from kNear below their middle on: one multiply-add; the smaller, the nearer
+__device__ __forceinline__ uint32_t distance_key(float scaled) { return __float_as_uint(scaled) * 4096u + ((kNear - 0x80000u) << 12); }
+constexpr uint32_t kNearKey = (2 * kNear + 1) << 12;
+// of a group's maximum to 1.75 times a power of two
+__device__ __forceinline__ uint32_t scale_distance(uint32_t top) { return (top & 0x7FFFFFu) + (kNear - 0x600000u); }
+
+// 1 / sqrt(mean(h^2) + eps) of a row from memory in fp64, by `width` lanes of a warp; the row has been stored and the lanes synchronised.
+template <int W>
+__device__ __forceinline__ double exact_factor(const uint16_t* h, int dim, float eps, int width)
+{
+    double s = 0.0;
+    for (int c = ((int)threadIdx.x & (width - 1)) * W; c < dim; c += width * W) {
+        float v[W];
+        Access<W>::unpack(*reinterpret_cast<const typename Access<W>::Raw*>(h + c), v);
+#pragma unroll
+        for (int j = 0; j < W; ++j) s = fma((double)v[j], (double)v[j], s);
+    }
+    for (int d = width >> 1; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    return 1.0 / sqrt(s / (double)dim + (double)eps);
+}
+
+// fp64 to fp32 such that a later rounding to fewer bits is that of the fp64 value: cut, with the last bit set where something was cut off.
+__device__ __forceinline__ float to_odd(double v)
+{
+    const float f = __double2float_rz(v);
+    return (double)f == v ? f : __uint_as_float(__float_as_uint(f) | 1u);
+}
+
+// The 8-bit values (x, y) and the scale (z) of one access in fp64.  A whole warp; everything by value, so that its other paths keep their registers.
+template <int W, class WT>
+__device__ __forceinline__ uint4 exact_group(typename Access<W>::Raw raw, const WT* weight, double r, bool in)
+{
+    float h[W], w[W];
+    Access<W>::unpack(raw, h);
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j] = 0.0f;
+    if (in) Access<W>::weights(weight, w);
+    double y[W], top = 0.0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        y[j] = (double)h[j] * (double)w[j] * r;
+        top = fmax(top, fabs(y[j]));
+    }
+#pragma unroll
+    for (int d = kGroup / W / 2; d > 0; d >>= 1) top = fmax(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    const uint32_t scale = group_scale(__float_as_uint(__double2float_ru(top)));
+    const double inv = (double)inverse_scale(scale);
+    if constexpr (W == 8) {
+        return make_uint4(e4m3_pair(to_odd(y[0] * inv), to_odd(y[1] * inv)) | e4m3_pair(to_odd(y[2] * inv), to_odd(y[3] * inv)) << 16,
+                          e4m3_pair(to_odd(y[4] * inv), to_odd(y[5] * inv)) | e4m3_pair(to_odd(y[6] * inv), to_odd(y[7] * inv)) << 16, scale, 0u);
+    } else {
+        return make_uint4(e4m3_pair(to_odd(y[0] * inv), 0.0f), 0u, scale, 0u);
+    }
+}
+
 // The largest of three magnitudes as bits, NaN where one is.
 __device__ __forceinline__ uint32_t largest(uint32_t top, float a, float b)
 {
@@ -180,6 +239,12 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
             r = (float)(1.0 / sqrt(s) / (double)pre);
         }
     }
+    auto store_8_bits = [&](int c, const uint2& q, uint32_t scale) {
+        if constexpr (W == 8) *reinterpret_cast<uint2*>(a.q + base + (int64_t)c * W) = q;
+        else a.q[base + c] = (uint8_t)q.x;
+        if (c % (kGroup / W) == 0) a.scales[row * ((a.dim + kGroup - 1) / kGroup) + c / (kGroup / W)] = (uint8_t)scale;
+    };
+    uint32_t nearest = 0xFFFFFFFFu, nearest_scale = 0xFFFFFFFFu, not_finite = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int c = i * a.lanes + lane;
@@ -199,8 +264,8 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
         if constexpr (!MX) {
             if (in) *reinterpret_cast<Raw*>(a.y + base + (int64_t)c * W) = A::pack(v);
         } else {
-            // a group is 4 neighbouring lanes of 8 columns, or a warp of one column each; magnitudes are compared as integers, so that NaN
-            // counts as the largest
+            // a group is 4 neighbouring lanes of 8 columns, or a warp of one column each; magnitudes are compared as bits, so that NaN counts
+            // as the largest
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < W; j += 2) top = W == 1 ? __float_as_uint(v[0]) & 0x7FFFFFFFu : largest(top, v[j], v[(j + 1) % W]);
@@ -209,15 +274,32 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
             for (int d = kGroup / W / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
             const uint32_t s = group_scale(top);
             const float inv = inverse_scale(s);
-            if (!in) continue;
-            if constexpr (W == 8) {
-                *reinterpret_cast<uint2*>(a.q + base + (int64_t)c * W) =
-                    make_uint2(e4m3_pair(v[0] * inv, v[1] * inv) | e4m3_pair(v[2] * inv, v[3] * inv) << 16,
-                               e4m3_pair(v[4] * inv, v[5] * inv) | e4m3_pair(v[6] * inv, v[7] * inv) << 16);
-            } else {
-                a.q[base + c] = (uint8_t)e4m3_pair(v[0] * inv, 0.0f);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                v[j] *= inv;
+                nearest = min(nearest, distance_key(v[j]));
             }
-            if (c % (kGroup / W) == 0) a.scales[row * ((a.dim + kGroup - 1) / kGroup) + c / (kGroup / W)] = (uint8_t)s;
+            nearest_scale = min(nearest_scale, scale_distance(top));
+            not_finite |= (s == 255u ? 1u : 0u) << i;
+            if (!in) continue;
+            if constexpr (W == 8) store_8_bits(c, make_uint2(e4m3_pair(v[0], v[1]) | e4m3_pair(v[2], v[3]) << 16, e4m3_pair(v[4], v[5]) | e4m3_pair(v[6], v[7]) << 16), s);
+            else store_8_bits(c, make_uint2(e4m3_pair(v[0], 0.0f), 0u), s);
+        }
+    }
+    if constexpr (MX) {
+        if (__any_sync(0xFFFFFFFFu, nearest < kNearKey || nearest_scale <= 2 * kNear)) {
+            __syncwarp();                            // the row's entries that other lanes stored; other warps' lie before the sum's barrier
+            const uint16_t* stored = (RES ? a.h : a.x) + base;
+            const double factor = exact_factor<W>(stored, active ? a.dim : 0, a.eps, SPLIT ? 32 : a.lanes);
+#pragma unroll 1
+            for (int i = 0; i < N; ++i) {
+                const int c = i * a.lanes + lane;
+                const bool in = active && c < a.units;
+                Raw raw = A::zero();
+                if (in) raw = *reinterpret_cast<const Raw*>(stored + c * W);
+                const uint4 exact = exact_group<W, WT>(raw, static_cast<const WT*>(a.weight) + c * W, factor, in);
+                if (in && !(not_finite >> i & 1u)) store_8_bits(c, make_uint2(exact.x, exact.y), exact.z);
+            }
         }
     }
 }

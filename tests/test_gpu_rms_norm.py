@@ -291,3 +291,22 @@ def test_captured_and_replayed():
     torch.cuda.synchronize()
     for a, b in zip(got, step()):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("tokens,dim,fp32", [(400, 4096, False), (2000, 128, True), (300, 5120, True), (200, 1001, False), (500, 96, False), (3000, 61, True)])
+def test_8_bit_values_are_those_of_the_exact_norm(tokens, dim, fp32):
+    """Values and scales within 4 units in the last place of a border are decided in fp64.  The fp32 evaluation's errors are sums of some tens of
+    independent roundings of half a unit at most (the sum's count half), half a unit in the mean square: 4 are eight times that.  Below e4m3's normal numbers (2^-6 of the scale) a
+    value may be one step off."""
+    eps = 1e-5
+    x, r, w = draw((tokens, dim), 71), draw((tokens, dim), 72, 2.0), weights(dim, fp32)
+    q, s, h = ops.rms_norm_mx(x, w, r, eps)
+    want = R.norm(h.double(), w.double(), float(torch.tensor(eps, dtype=torch.float32)))
+    groups = (dim + 31) // 32
+    top = torch.nn.functional.pad(want.abs(), (0, 32 * groups - dim)).view(tokens, groups, 32).amax(-1)
+    fraction, exponent = torch.frexp(top / 448)
+    least = torch.ldexp(torch.ones_like(top), exponent - (fraction == 0.5).int())
+    assert torch.equal(s.double(), least)
+    v = want / least.repeat_interleave(32, 1)[:, :dim]
+    off = q.double() - R.to_e4m3(v)
+    assert not bool(off[v.abs() >= 2.0 ** -6].any()) and float(off.abs().max()) <= 2.0 ** -9
