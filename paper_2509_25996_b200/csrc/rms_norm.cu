@@ -105,7 +105,8 @@ __device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_fl
 
 // Values in fp32 that lie this near to a border of the 8-bit form (units in the last place; two e4m3 values' middle, or a group's maximum at 448 times a
 // power of two) are worked out again in fp64, so that values and scales are those of the exact norm.  The roundings before it are some tens of half units
-// at most, of the sum (whose error counts half), the root and two products: half a unit in the mean square.  (Looking for such values takes 4 of the 52 us of 8190 x 5120, and one row in twenty is worked out again.)
+// at most, of the sum (whose error counts half), the root and two products: half a unit in the mean square.
+// (Looking for such values takes 4 of the 52 us of 8190 x 5120; one row in twenty is worked out again.)
 constexpr uint32_t kNear = 4;
 // the last 20 bits as the upper ones, from kNear below their middle on: one multiply-add; the smaller, the nearer
 __device__ __forceinline__ uint32_t distance_key(float scaled) { return __float_as_uint(scaled) * 4096u + ((kNear - 0x80000u) << 12); }
