@@ -310,3 +310,48 @@ def test_8_bit_values_are_those_of_the_exact_norm(tokens, dim, fp32):
     v = want / least.repeat_interleave(32, 1)[:, :dim]
     off = q.double() - R.to_e4m3(v)
     assert not bool(off[v.abs() >= 2.0 ** -6].any()) and float(off.abs().max()) <= 2.0 ** -9
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_sizes_and_places_drawn_at_random(seed):
+    import random
+    rng = random.Random(seed)
+    dim = int(2.0 ** rng.uniform(0, 13.2))
+    tokens = rng.randint(1, max(1, min(3000, 400000 // dim)))
+    fp32, residual = rng.random() < 0.5, rng.random() < 0.5
+    x, w = draw((tokens, dim), seed), weights(dim, fp32, seed)
+    r = draw((tokens, dim), seed + 1, 2.0) if residual else None
+    dh = draw((tokens, dim), seed + 2) if residual else None
+    dy = draw((tokens, dim), seed + 3)
+    bands = {}
+    for name, t in (("x", x), ("w", w), ("r", r), ("dh", dh), ("dy", dy)):
+        bands[name] = None if t is None else Banded(t.shape, t.dtype, rng.choice((0, 0, 1, 4, 8, rng.randint(0, 9))), t)
+    at = lambda name: None if bands[name] is None else bands[name].t  # noqa: E731
+    by, bh, bdx = (Banded(x.shape, x.dtype, rng.choice((0, 0, 1, 8, rng.randint(0, 9)))) for _ in range(3))
+    eps, h = 1e-5, stored_sum(x, r)
+    ops.rms_norm(at("x"), at("w"), at("r"), eps, out=by.t, sum_out=bh.t if residual else None)
+    check_y(by.t, h, w, eps)
+    assert not residual or torch.equal(bh.t, h)
+    q, s, _ = ops.rms_norm_mx(at("x"), at("w"), at("r"), eps)
+    check_mx(q, s, h, w, eps)
+    bdh = Banded(x.shape, x.dtype, rng.randint(0, 9), h)
+    dx, dw = ops.rms_norm_grad(at("dy"), bdh.t, at("w"), at("dh"), eps, out=bdx.t)
+    check_grad(dx, dw, dy, h, w, dh, eps)
+    assert all(b is None or b.intact() for b in list(bands.values()) + [by, bh, bdx, bdh])
+    assert torch.equal(at("x"), x) and torch.equal(bdh.t, h)
+
+
+def test_calls_on_two_streams_at_once():
+    """Every call has a workspace and results of its own: what runs beside it does not show."""
+    sets = [(draw((700, 1536), k), draw((700, 1536), k + 50), weights(1536, True, k)) for k in range(4)]
+    alone = [ops.rms_norm_grad(dy, h, w) for dy, h, w in sets]
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    torch.cuda.synchronize()
+    got = [[] for _ in sets]
+    for _ in range(20):
+        for k, (stream, (dy, h, w)) in enumerate(zip(streams, sets)):
+            with torch.cuda.stream(stream):
+                got[k].append(ops.rms_norm_grad(dy, h, w))
+    torch.cuda.synchronize()
+    for k, (dx, dw) in enumerate(alone):
+        assert all(torch.equal(a, dx) and torch.equal(b, dw) for a, b in got[k])

@@ -202,3 +202,38 @@ def test_streams_capture_and_refusals_of_the_torch_calls():
         ops.rotary(q, None, positions, spectrum, out=(q.flip(0)[:, :1].expand(10, 4, 64), None))
     assert cast.cast_rotary([B.make_heads(q.cpu(), q, 4, 256, 64, 256, 64)], positions, spectrum.frequencies, spectrum.axes, 2, 32, False, False, 10,
                             64) == B.CAST_ERR_MEMORY
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_arrangements_drawn_at_random(seed):
+    """Queries and keys of any order, gaps and places, each to a place of its own, against the 64-bit evaluation; nothing else is written."""
+    import random
+    rng = random.Random(seed)
+    tokens, head_dim = rng.choice((1, 2, 3, 17, 150, 600)), rng.choice((8, 24, 34, 64, 80, 128, 130))
+    pairs, n_axes, adjacent = rng.randint(1, head_dim // 2), rng.randint(1, 3), rng.random() < 0.5
+    f, axes = spectrum_lists(pairs, n_axes, seed)
+    spectrum = ops.RotarySpectrum(f, axes, adjacent)
+    gen = torch.Generator().manual_seed(seed)
+    positions = torch.randint(-9, 3000, (max(n_axes, 1), tokens), generator=gen, dtype=torch.int32).to(DEV)
+
+    def place(heads, fill):
+        grain = rng.choice((1, 2, 4, 8))
+        head_stride = head_dim + grain * rng.randint(0, 3)
+        offset = grain * rng.randint(0, 5)
+        if rng.random() < 0.5:
+            token_stride = heads * head_stride + grain * rng.randint(0, 4)
+        else:
+            token_stride = head_dim + grain * rng.randint(0, 2)
+            head_stride = tokens * token_stride + grain * rng.randint(0, 3)
+        n = offset + (tokens - 1) * token_stride + (heads - 1) * head_stride + head_dim
+        flat = fill(n)
+        return flat, flat[offset:].as_strided((tokens, heads, head_dim), (token_stride, head_stride, 1), flat.storage_offset() + offset)
+    heads = [rng.randint(1, 40), rng.randint(1, 9)]
+    ins = [place(h, lambda n: draw((n,), seed))[1] for h in heads]
+    outs = [place(h, lambda n: torch.full((n,), 7.0, dtype=torch.bfloat16, device=DEV)) for h in heads]
+    inverse = rng.random() < 0.5
+    got = ops.rotary(ins[0], ins[1], positions, spectrum, inverse, out=(outs[0][1], outs[1][1]))
+    for x, y, (flat, view) in zip(ins, got, outs):
+        check(y, x, positions, f, axes, adjacent, inverse)
+        view.fill_(7.0)
+        assert bool((flat == 7.0).all())
