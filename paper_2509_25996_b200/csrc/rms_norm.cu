@@ -607,7 +607,7 @@ struct Ring {
     }
 };
 
-// Rows of 1032 to 4096 columns: three on their way, two CTAs of up to 256 threads per SM with 128 registers, so that a row stays in
+// Rows of 776 to 4096 columns: three on their way, two CTAs of up to 256 threads per SM with 128 registers, so that a row stays in
 // registers between its two halves.  (16384 x 4096 in us, in short runs and under the power limit, where instructions count: 83.0 / 86.0 to 88;
 // read from shared memory twice, 80 registers: 81.6 / 94.6; two rows and four CTAs with 64 registers: 87.0 / 96.1; four rows, two CTAs: 91.2 / 96.5.)
 template <int W, int N, int STAGES, bool SPLIT> constexpr bool kMiddleRow = SPLIT && W == 8 && N == 2 && STAGES == 3;
@@ -833,7 +833,7 @@ GradSpread grad_spread_of(int64_t dim, int w, bool res)
     GradSpread g = {};
     const int64_t units = dim / w, arrays = res ? 3 : 2;
     if (w == 8) {
-        if (units <= 128) {                   // up to 1024 columns: in a warp
+        if (units <= 96) {                    // up to 768 columns: in a warp (65536 x 1024: in a warp 98 us, in two 92; x 640: 20.5, 24.6 for 16384)
             g.lanes = 8;
             while (g.lanes < 32 && g.lanes < units) g.lanes *= 2;
             g.n = (int)((units + g.lanes - 1) / g.lanes);
@@ -871,11 +871,13 @@ int sm_count(int* sms)
     return CAST_OK;
 }
 
-// CTAs of the gradient kernel: what the SMs hold at a time, and no more than there are groups of rows.
+// CTAs of the gradient kernel: what the SMs hold at a time; fewer tokens than four rows for each of those, but more than fill two per SM, take
+// fewer, since every one of them leaves a row of sums (1000 x 1024: 7.9 us with a CTA each, 6.0 with two per SM).
 int64_t grad_ctas(const GradSpread& g, int64_t tokens, int sms)
 {
     const int64_t rows = g.split ? 1 : 256 / g.lanes, groups = (tokens + rows - 1) / rows, held = (int64_t)sms * g.held;
-    return groups < held ? groups : held;
+    const int64_t quarter = groups / 4 > 2 * sms ? groups / 4 : 2 * sms, most = quarter < held ? quarter : held;
+    return groups < most ? groups : most;
 }
 
 // Workspace for every form of the call: which one it takes depends on its pointers.
@@ -1037,8 +1039,7 @@ extern "C" int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, c
         if (!g.split)
             rc = g.n == 1   ? launch_grad<8, 1, 4, false>(a, g, f, ctas, st)
                  : g.n == 2 ? launch_grad<8, 2, 4, false>(a, g, f, ctas, st)
-                 : g.n == 3 ? launch_grad<8, 3, 2, false>(a, g, f, ctas, st)
-                            : launch_grad<8, 4, 2, false>(a, g, f, ctas, st);
+                            : launch_grad<8, 3, 2, false>(a, g, f, ctas, st);
         else
             rc = g.n == 4 ? (g.stages == 2 ? launch_grad<8, 4, 2, true>(a, g, f, ctas, st) : launch_grad<8, 4, 1, true>(a, g, f, ctas, st))
                  : g.stages == 3 ? launch_grad<8, 2, 3, true>(a, g, f, ctas, st)
