@@ -42,7 +42,7 @@ struct RotaryArgs {
     const int32_t* axes;              // or NULL: all on axis 0
     const int32_t* positions;         // [n_axes][tokens]
     int32_t sets, heads;              // heads of all sets together
-    int32_t tokens, n_axes, pairs;
+    int32_t tokens, n_axes, pairs, head_dim;
     int32_t turned;                   // units of a head that turn
     Divisor units;                    // and with those that are copied
     Divisor token_units;              // of a token in a CTA
@@ -104,7 +104,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
     const uint32_t total = (uint32_t)tokens * (uint32_t)heads * a.units.d;
     Words<W> x[ITEMS], y[U::kTwo ? ITEMS : 1];
     uint16_t* dst[ITEMS];
-    int place[ITEMS];                    // of the unit's first angles, -1: a copy, -2: none
+    int place[ITEMS];                    // of the unit's first angles, -1: a copy, -3: a copy of one access, -2: none
     int left[ADJACENT && W == 8 ? ITEMS : 1];        // pairs that turn from the unit's first one on
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
@@ -119,13 +119,14 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
         const HeadSet& hs = a.set[s];
         const int64_t token = token0 + (int)t, own = head - hs.first;           // 32-bit factors of the strides
         const bool turns = u < a.turned;
-        const int col = turns ? u * U::kColumns : (U::kTwo ? 2 * a.pairs : a.turned * W) + (u - a.turned) * W;      // the unit's first column
+        // the unit's first column; a copying unit takes as many accesses as a turning one
+        const int col = turns ? u * U::kColumns : U::kTwo ? 2 * a.pairs + (u - a.turned) * 2 * W : u * W;
         const uint16_t* src = hs.in + token * hs.in_token + own * hs.in_head + col;
         dst[k] = hs.out + token * hs.out_token + own * hs.out_head + col;
-        place[k] = turns ? (int)t * a.turned * P + u * (P > 1 ? 2 : 1) : -1;
+        place[k] = turns ? (int)t * a.turned * P + u * (P > 1 ? 2 : 1) : U::kTwo && col + W < a.head_dim ? -1 : -3;
         x[k] = load_words<W>(src);
         if constexpr (U::kTwo)
-            if (turns) y[k] = load_words<W>(src + (ADJACENT ? 1 : a.pairs));
+            if (place[k] != -3) y[k] = load_words<W>(src + (!turns ? W : ADJACENT ? 1 : a.pairs));
         if constexpr (ADJACENT && W == 8) left[k] = a.pairs - u * P;
     }
     for (uint32_t i = threadIdx.x; i < (uint32_t)(tokens * a.pairs); i += blockDim.x) {
@@ -179,6 +180,8 @@ rotary_kernel(const __grid_constant__ RotaryArgs a)
                 }
             }
             if constexpr (U::kTwo) store_words<W>(dst[k] + (ADJACENT ? 1 : a.pairs), y[k]);
+        } else if constexpr (U::kTwo) {
+            if (place[k] == -1) store_words<W>(dst[k] + W, y[k]);
         }
         store_words<W>(dst[k], x[k]);
     }
@@ -225,7 +228,8 @@ int launch_rotary(RotaryArgs a, int64_t head_dim, int sms, cudaStream_t stream)
 {
     using U = Unit<W, ADJACENT>;
     a.turned = (a.pairs + U::kPairs - 1) / U::kPairs;
-    const int units = a.turned + (int)((head_dim - (U::kTwo ? 2 * a.pairs : a.turned * W)) / W);
+    constexpr int copied = U::kTwo ? 2 * W : W;          // columns of a unit
+    const int units = a.turned + (int)((head_dim - (U::kTwo ? 2 * a.pairs : a.turned * W) + copied - 1) / copied);
     // Halves: two units, which are four 16-byte accesses, per thread and 6 CTAs per SM are enough (81.4 us for those 16384 tokens; four units
     // and 4 CTAs 82.6).  Adjacent units have one access: as many as keep a token in one CTA, which works out its angles once, and leave no
     // thread idle (8190 tokens of 48 heads of 128 columns: two 38.9 us, three 36.5, four 38.8; 16384 of 64: two 99.9, three 93.5, four 90.0).
@@ -331,6 +335,7 @@ extern "C" int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* 
     a.tokens = (int32_t)tokens;
     a.n_axes = n_axes;
     a.pairs = pairs;
+    a.head_dim = (int32_t)head_dim;
     a.sign = inverse ? -1.0f : 1.0f;
     const cudaStream_t st = (cudaStream_t)stream;
     int device = 0, sms = 0;
