@@ -281,8 +281,18 @@ class RotarySpectrum:
             raise ValueError("axes: negative")
         device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         self.pairs, self.n_axes, self.adjacent = len(frequencies), max(axes) + 1, bool(adjacent)
-        self.frequencies = torch.tensor(frequencies, dtype=torch.float64, device=device)
-        self.axes = torch.tensor(axes, dtype=torch.int32, device=device)
+        self._frequencies = torch.tensor(frequencies, dtype=torch.float64, device=device)
+        self._axes = torch.tensor(axes, dtype=torch.int32, device=device)
+
+    @property
+    def frequencies(self) -> torch.Tensor:
+        """fp64 [pairs] on the device; its entries may be changed, the tensor stays."""
+        return self._frequencies
+
+    @property
+    def axes(self) -> torch.Tensor:
+        """int32 [pairs] on the device, as frequencies; a pair of an axis that the positions do not have does not turn."""
+        return self._axes
 
     @classmethod
     def of(cls, dims: int, base: float = 10000.0, sections: Optional[Sequence[int]] = None, per_axis: bool = False, adjacent: bool = False,

@@ -178,6 +178,8 @@ def test_spectrum():
     assert all(math.isclose(f, 100.0 ** (-i / 8)) for i, f in enumerate(s.frequencies.tolist()))
     s = ops.RotarySpectrum.of(12, base=100.0, sections=[2, 4], per_axis=True, adjacent=True, device="cpu")
     assert s.adjacent and all(math.isclose(f, 100.0 ** -p) for f, p in zip(s.frequencies.tolist(), (0, 0.5, 0, 0.25, 0.5, 0.75)))
+    with pytest.raises(AttributeError):
+        s.frequencies = torch.ones(2)
     for bad in (lambda: ops.RotarySpectrum.of(7, device="cpu"), lambda: ops.RotarySpectrum.of(8, sections=[3], device="cpu"),
                 lambda: ops.RotarySpectrum.of(8, sections=[5, -1], device="cpu"), lambda: ops.RotarySpectrum([], device="cpu"),
                 lambda: ops.RotarySpectrum([1.0], axes=[0, 1], device="cpu"), lambda: ops.RotarySpectrum([1.0], axes=[-1], device="cpu"),
