@@ -447,9 +447,10 @@ Spread spread_of(int64_t units, int w, bool res, bool mx)
             return {lanes, (int)((units + lanes - 1) / lanes), false};
         }
         // Fewer accesses per thread leave SMs with too few bytes in flight behind the barrier of a row, more of them with too few CTAs (us;
-        // 16384 x 4096 with residual: one 84.7, two 79.8, four 80.6; without, 8192 x 4096: one 34.6, two 27.6, three 25.5, four 22.9; 8190 x 5120 in
-        // 8 bits: two 49.5, three 47.8, four 47.4; 4096 x 12288 with residual: two 80, four 61.7, eight 69).
-        const int n = units <= 256 ? (res && !mx ? 1 : 2) : units <= 512 ? (res ? 2 : 4) : units <= 768 && res ? 3 : 4;
+        // 16384 x 4096 with residual: one 84.7, two 79.8, four 80.6; to 8 bits: two 87.6, four 83.4; without residual, 8192 x 4096: one 34.6, two 27.6,
+        // three 25.5, four 22.9; 4096 x 12288 with residual: two 80, four 61.7, eight 69).
+        const bool plain = res && !mx;
+        const int n = units <= 256 ? (plain ? 1 : 2) : !plain ? 4 : units <= 512 ? 2 : units <= 768 ? 3 : 4;
         return {(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true};
     }
     if (units <= 256) return {32, 8, false};
