@@ -469,6 +469,13 @@ int launch_norm(const NormArgs& a, cudaStream_t stream)
     return CAST_OK;
 }
 
+// One and three accesses per thread of a CTA are taken with a residual and a bf16 result only.
+template <int N>
+int launch_plain_norm(const NormArgs& a, bool weight_fp32, cudaStream_t stream)
+{
+    return weight_fp32 ? launch_norm<8, N, true, true, false, float>(a, stream) : launch_norm<8, N, true, true, false, uint16_t>(a, stream);
+}
+
 template <int W, int N, bool SPLIT>
 int launch_norm(const NormArgs& a, bool weight_fp32, cudaStream_t stream)
 {
@@ -952,9 +959,9 @@ int norm_impl(const uint16_t* x, const uint16_t* residual, const void* weight, i
                    : s.n == 2 ? launch_norm<8, 2, false>(a, f, stream)
                    : s.n == 3 ? launch_norm<8, 3, false>(a, f, stream)
                               : launch_norm<8, 4, false>(a, f, stream);
-        return s.n == 1   ? launch_norm<8, 1, true>(a, f, stream)
+        return s.n == 1   ? launch_plain_norm<1>(a, f, stream)
                : s.n == 2 ? launch_norm<8, 2, true>(a, f, stream)
-               : s.n == 3 ? launch_norm<8, 3, true>(a, f, stream)
+               : s.n == 3 ? launch_plain_norm<3>(a, f, stream)
                           : launch_norm<8, 4, true>(a, f, stream);
     }
     const uintptr_t place = (uintptr_t)x;
