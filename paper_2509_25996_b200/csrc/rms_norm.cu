@@ -5,7 +5,7 @@
 //
 // Forward: one pass; a row stays in registers between its sum of squares and its result.  `lanes` threads share a row, each with up to
 // N accesses of W columns: 4 to 32 lanes of a warp (several rows per warp or CTA, no barrier), or a whole CTA.  Bounded by HBM: 16384 x 4096 with
-// residual 79.5 us (537 MB, 6.75 TB/s), 4096 x 12288 61.6 us (6.54 TB/s); the 8-bit form of 8190 x 5120 52.2 us (295 MB, 5.7 TB/s) and 57 under
+// residual 79.5 us (537 MB, 6.75 TB/s), 4096 x 12288 61.6 us (6.54 TB/s); the 8-bit form of 8190 x 5120 51.9 us (295 MB, 5.7 TB/s) and 56 under
 // the power limit: its instructions (two passes over a row in registers, groups' maxima, conversions) keep the issue slots busy.
 //
 // Gradient: the statistics of a row come from h again instead of being kept (one more multiply-add per column, 4 bytes per row less, nothing to
