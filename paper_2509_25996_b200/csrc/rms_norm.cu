@@ -67,7 +67,7 @@ __device__ __forceinline__ bool odd_row(float mean_eps) { return !(mean_eps < 0x
 // A power of two that brings the entries of such a row back into the range: 1/sqrt(mean) = pre * (1/sqrt(mean) / pre).
 __device__ __forceinline__ float odd_factor(double mean_eps) { return mean_eps < 1.0 ? 0x1p64f : 0x1p-64f; }
 
-// A thread's sums of h^2 and of weight dy h (dy may be NULL) over its columns of such a row, in fp64 and from memory again: rare, and
+// A thread's sums of h^2 and of weight dy h over its columns of such a row, in fp64 and from memory again: rare, and
 // outside of what the other rows' code keeps in registers.
 template <int W>
 __device__ __noinline__ double2 odd_sums(const uint16_t* h, const uint16_t* dy, const void* weight, bool weight_fp32, int dim, int lanes, int lane)
@@ -77,10 +77,8 @@ __device__ __noinline__ double2 odd_sums(const uint16_t* h, const uint16_t* dy, 
         for (int j = 0; j < W; ++j) {
             const double v = (double)bf16_low(h[c + j]);
             hh = fma(v, v, hh);
-            if (dy) {
-                const double w = (double)(weight_fp32 ? static_cast<const float*>(weight)[c + j] : bf16_low(static_cast<const uint16_t*>(weight)[c + j]));
-                gh = fma((double)bf16_low(dy[c + j]) * w, v, gh);
-            }
+            const double w = (double)(weight_fp32 ? static_cast<const float*>(weight)[c + j] : bf16_low(static_cast<const uint16_t*>(weight)[c + j]));
+            gh = fma((double)bf16_low(dy[c + j]) * w, v, gh);
         }
     return make_double2(hh, gh);
 }
