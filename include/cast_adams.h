@@ -557,8 +557,9 @@ CAST_API int cast_product_failures(unsigned long long* count_out, int action);
  * cast_rms_norm_mx -- the same with an 8-bit result for block-scaled products: groups of 32 columns of a row (the last one may be shorter)
  * share a power of two.
  *
- *   q          device, e4m3 [tokens][dim], out: y / scale of its group, rounded to nearest even.  Values and scales within 4 fp32 units of a
- *              border are decided in fp64: they are those of the exact norm of h (a value below 2^-6 of its scale may be one step off).
+ *   q          device, e4m3 [tokens][dim], out: y / scale of its group, rounded to nearest even.  Values and scales that fp32 puts nearer to a
+ *              border than its roundings can be off are decided in fp64: they are those of the exact norm of h wherever weight h stays in the
+ *              normal range of fp32 (a value below 2^-6 of its scale may be one step off).
  *   q_scales   device, e8m0 [tokens][(dim + 31) / 32], out: exponent + 127 of the least power of two with max|y| <= 448 scale; 0 (2^-127) for
  *              a group of zeros; 255 (NaN) where an entry is not finite, the whole group's q are then NaN, too.
  */

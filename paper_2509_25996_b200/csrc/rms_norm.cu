@@ -5,7 +5,7 @@
 //
 // Forward: one pass; a row stays in registers between its sum of squares and its result.  `lanes` threads share a row, each with up to
 // N accesses of W columns: 4 to 32 lanes of a warp (several rows per warp or CTA, no barrier), or a whole CTA.  Bounded by HBM: 16384 x 4096 with
-// residual 79.5 us (537 MB, 6.75 TB/s), 4096 x 12288 61.6 us (6.54 TB/s); the 8-bit form of 8190 x 5120 51.9 us (295 MB, 5.7 TB/s) and 56 under
+// residual 79.5 us (537 MB, 6.75 TB/s), 4096 x 12288 61.6 us (6.54 TB/s); the 8-bit form of 8190 x 5120 52.6 us (295 MB, 5.6 TB/s) and 57 under
 // the power limit: its instructions (two passes over a row in registers, groups' maxima, conversions) keep the issue slots busy.
 //
 // Gradient: the statistics of a row come from h again instead of being kept (one more multiply-add per column, 4 bytes per row less, nothing to
@@ -44,6 +44,7 @@ struct NormArgs {
     int32_t lanes;            // threads of a row
     float eps;
     float inverse_dim;
+    double inverse_dim64;     // 8-bit form
 };
 
 // Sum over the `lanes` threads of a row (all of the CTA with SPLIT); every one of them gets it, summed in the same order.
@@ -83,6 +84,33 @@ __device__ __noinline__ double2 odd_sums(const uint16_t* h, const uint16_t* dy, 
     return make_double2(hh, gh);
 }
 
+// A thread's sum of h^2 as a tree: an addition's operands have been through the same number of roundings, 2 + log2(N W / 4) of them at the end
+// (squares of bf16 entries are exact in fp32).
+template <int W, int N>
+__device__ __forceinline__ float tree_of_squares(const typename Access<W>::Raw (&h)[N])
+{
+    constexpr int EIGHTS = (N * W + 7) / 8;
+    float s[EIGHTS];
+#pragma unroll
+    for (int b = 0; b < EIGHTS; ++b) {
+        float v[8], p[4];
+        if constexpr (W == 8) {
+            Access<8>::unpack(h[b], v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = bf16_low(h[b * 8 + j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[j] = fmaf(v[2 * j], v[2 * j], v[2 * j + 1] * v[2 * j + 1]);
+        s[b] = (p[0] + p[1]) + (p[2] + p[3]);
+    }
+    static_assert(EIGHTS <= 4, "two more additions at most");
+    if constexpr (EIGHTS == 4) return (s[0] + s[1]) + (s[2] + s[3]);
+    else if constexpr (EIGHTS == 3) return (s[0] + s[1]) + s[2];
+    else if constexpr (EIGHTS == 2) return s[0] + s[1];
+    else return s[0];
+}
+
 // Two e4m3 values, the first in the low byte; beyond +-448 only by a rounding, NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi)
 {
@@ -102,15 +130,17 @@ __device__ __forceinline__ uint32_t group_scale(uint32_t top)
 __device__ __forceinline__ float inverse_scale(uint32_t s) { return __uint_as_float(s == 255u ? 0x7FC00000u : (254u - s) << 23); }
 
 // Values in fp32 that lie this near to a border of the 8-bit form (units in the last place; two e4m3 values' middle, or a group's maximum at 448 times a
-// power of two) are worked out again in fp64, so that values and scales are those of the exact norm.  The roundings before it are some tens of half units
-// at most, of the sum (whose error counts half), the root and two products: half a unit in the mean square.
-// (Looking for such values takes 4 of the 52 us of 8190 x 5120; one row in twenty is worked out again.)
-constexpr uint32_t kNear = 4;
+// power of two) are worked out again in fp64, so that values and scales are those of the exact norm.  With u = 2^-24, the most of a rounding, the mean square
+// is off by 6 u where a row has a CTA (5 of a thread's sum, fp64 beyond, its own rounding) and by 12 u where it stays in a warp (5 more of the shuffles, one of
+// 1/dim).  Its root's reciprocal has half of that and u, two products add 2 u: 6 or 9 u of a value, which are 6 m / 2 or 9 m / 2 units at a mantissa m.
+// The borders' mantissas are 31/16 and 7/4 at most: less than 6 or 9 units, and borders are whole units away.
+// (8190 x 5120: 52.6 us; a warp's sums in fp64, too, and 5 units there: 65536 x 256 19.9 instead of 18.8; fp32 throughout and 11 units: 53.6 and 18.8.
+// Exact sums and the look for such values take 5 of the 52.6; one row in twenty is worked out again.)
+template <bool SPLIT> constexpr uint32_t kNear = SPLIT ? 5 : 8;
 // the last 20 bits as the upper ones, from kNear below their middle on: one multiply-add; the smaller, the nearer
-__device__ __forceinline__ uint32_t distance_key(float scaled) { return __float_as_uint(scaled) * 4096u + ((kNear - 0x80000u) << 12); }
-constexpr uint32_t kNearKey = (2 * kNear + 1) << 12;
+__device__ __forceinline__ uint32_t distance_key(float scaled, uint32_t near) { return __float_as_uint(scaled) * 4096u + ((near - 0x80000u) << 12); }
 // of a group's maximum to 1.75 times a power of two
-__device__ __forceinline__ uint32_t scale_distance(uint32_t top) { return (top & 0x7FFFFFu) + (kNear - 0x600000u); }
+__device__ __forceinline__ uint32_t scale_distance(uint32_t top, uint32_t near) { return (top & 0x7FFFFFu) + (near - 0x600000u); }
 
 // 1 / sqrt(mean(h^2) + eps) of a row from memory in fp64, by `width` lanes of a warp; the row has been stored and the lanes synchronised.
 template <int W>
@@ -176,7 +206,7 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
     using A = Access<W>;
     using Raw = typename A::Raw;
     __shared__ float part[kMostWarps];
-    __shared__ double part64[kMostWarps];
+    __shared__ double part64[MX ? 2 : 1][kMostWarps];
     const int lane = SPLIT ? (int)threadIdx.x : (int)threadIdx.x & (a.lanes - 1);
     const int64_t row = SPLIT ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / a.lanes) + threadIdx.x / a.lanes;
     const bool active = SPLIT || row < a.tokens;
@@ -212,15 +242,22 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
             if (active && c < a.units) h[i] = *reinterpret_cast<const Raw*>(a.x + base + (int64_t)c * W);
         }
     }
-    float square = 0.0f;
+    float mean;
+    if constexpr (MX) {
+        const float square = tree_of_squares<W, N>(h);
+        if constexpr (SPLIT) mean = (float)fma(row_sum<SPLIT>((double)square, a.lanes, part64[1]), a.inverse_dim64, (double)a.eps);
+        else mean = fmaf(row_sum<SPLIT>(square, a.lanes, part), a.inverse_dim, a.eps);
+    } else {
+        float square = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float v[W];
-        A::unpack(h[i], v);
+        for (int i = 0; i < N; ++i) {
+            float v[W];
+            A::unpack(h[i], v);
 #pragma unroll
-        for (int j = 0; j < W; ++j) square = fmaf(v[j], v[j], square);
+            for (int j = 0; j < W; ++j) square = fmaf(v[j], v[j], square);
+        }
+        mean = fmaf(row_sum<SPLIT>(square, a.lanes, part), a.inverse_dim, a.eps);
     }
-    const float mean = fmaf(row_sum<SPLIT>(square, a.lanes, part), a.inverse_dim, a.eps);
     float r = __frsqrt_rn(mean), pre = 1.0f;
     const bool odd = odd_row(mean);
     if (SPLIT ? odd : __any_sync(0xFFFFFFFFu, odd)) {
@@ -232,7 +269,7 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
             for (int j = 0; j < W; ++j) s = fma((double)v[j], (double)v[j], s);
         }
-        s = row_sum<SPLIT>(s, a.lanes, part64) / (double)a.dim + (double)a.eps;
+        s = row_sum<SPLIT>(s, a.lanes, part64[0]) / (double)a.dim + (double)a.eps;
         if (odd) {
             pre = odd_factor(s);
             r = (float)(1.0 / sqrt(s) / (double)pre);
@@ -276,9 +313,9 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 v[j] *= inv;
-                nearest = min(nearest, distance_key(v[j]));
+                nearest = min(nearest, distance_key(v[j], kNear<SPLIT>));
             }
-            nearest_scale = min(nearest_scale, scale_distance(top));
+            nearest_scale = min(nearest_scale, scale_distance(top, kNear<SPLIT>));
             not_finite |= (s == 255u ? 1u : 0u) << i;
             if (!in) continue;
             if constexpr (W == 8) store_8_bits(c, make_uint2(e4m3_pair(v[0], v[1]) | e4m3_pair(v[2], v[3]) << 16, e4m3_pair(v[4], v[5]) | e4m3_pair(v[6], v[7]) << 16), s);
@@ -286,7 +323,7 @@ rms_norm_kernel(const __grid_constant__ NormArgs a)
         }
     }
     if constexpr (MX) {
-        if (__any_sync(0xFFFFFFFFu, nearest < kNearKey || nearest_scale <= 2 * kNear)) {
+        if (__any_sync(0xFFFFFFFFu, nearest < (2 * kNear<SPLIT> + 1) << 12 || nearest_scale <= 2 * kNear<SPLIT>)) {
             __syncwarp();                            // the row's entries that other lanes stored; other warps' lie before the sum's barrier
             const uint16_t* stored = (RES ? a.h : a.x) + base;
             const double factor = exact_factor<W>(stored, active ? a.dim : 0, a.eps, SPLIT ? 32 : a.lanes);
@@ -947,7 +984,7 @@ int norm_impl(const uint16_t* x, const uint16_t* residual, const void* weight, i
     const void* ptrs[7] = {x, residual, weight, y, q, scales, h};
     if ((rc = check_device_memory(ptrs, 7)) != CAST_OK) return rc;
     const int w = dim % 8 == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(weight, 16) && aligned(y, 16) && aligned(q, 8) && aligned(h, 16) ? 8 : 1;
-    NormArgs a = {x, residual, weight, y, q, scales, h, (int32_t)tokens, (int32_t)dim, (int32_t)(dim / w), 0, eps, 1.0f / (float)dim};
+    NormArgs a = {x, residual, weight, y, q, scales, h, (int32_t)tokens, (int32_t)dim, (int32_t)(dim / w), 0, eps, 1.0f / (float)dim, 1.0 / (double)dim};
     const Spread s = spread_of(a.units, w, residual != nullptr, q != nullptr);
     a.lanes = s.lanes;
     const bool f = weight_fp32 != 0;

@@ -355,3 +355,41 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for k, (dx, dw) in enumerate(alone):
         assert all(torch.equal(a, dx) and torch.equal(b, dw) for a, b in got[k])
+
+
+def check_mx_exact(q, s, h, w, eps):
+    """Scales are the least powers of two, and values from 2^-6 of the scale on the rounding, of the exact norm; below, one step off at most."""
+    tokens, dim = h.shape
+    want = R.norm(h.double(), w.double(), float(torch.tensor(eps, dtype=torch.float32)))
+    groups = (dim + 31) // 32
+    top = torch.nn.functional.pad(want.abs(), (0, 32 * groups - dim)).view(tokens, groups, 32).amax(-1)
+    fraction, exponent = torch.frexp(top / 448)
+    least = torch.ldexp(torch.ones_like(top), exponent - (fraction == 0.5).int())
+    assert torch.equal(s.double(), least)
+    v = want / least.repeat_interleave(32, 1)[:, :dim]
+    off = q.double() - R.to_e4m3(v)
+    wrong = (off != 0) & (v.abs() >= 2.0 ** -6)
+    assert not bool(wrong.any()), f"{int(wrong.sum())} values"
+    assert float(off.abs().max()) <= 2.0 ** -9
+
+
+@pytest.mark.parametrize("dim", [64, 120, 776, 1000, 2048, 4096, 5120, 8192, 61, 1001, 5121])
+def test_8_bit_values_are_exact_where_roundings_of_the_sum_point_one_way(dim):
+    """One column in eight is a multiple of 1.0 and all others so small that every addition of their squares is rounded the same way, or one entry is far larger
+    than what its thread adds behind it.  The fp32 part of the sum has three roundings at most, whatever the entries."""
+    eps = 1e-5
+    odd = torch.full((dim,), 2.0 ** -12 * (1 + 2.0 ** -7))
+    odd[:max(dim // 4, 1):8] = 1.0
+    gen = torch.Generator().manual_seed(dim)
+    rows = [odd, odd.flip(0)]
+    for k in range(14):
+        signs = torch.where(torch.rand(dim, generator=gen) < 0.5, -1.0, 1.0)
+        if k % 2:
+            signs = signs * torch.randn(dim, generator=gen)
+        signs[(k // 2) * 8 % dim] = 4096.0
+        rows.append(signs)
+    h = torch.stack(rows).to(torch.bfloat16).to(DEV)
+    for seed in range(max(4, 60000 // dim)):
+        w = weights(dim, True, 100 + seed)
+        q, s, _ = ops.rms_norm_mx(h, w, None, eps)
+        check_mx_exact(q, s, h, w, eps)
