@@ -16,6 +16,7 @@
 //
 // Roundings: sums and statistics are fp32 (fp64 for rows whose squares leave the range of fp32), y and dx are rounded once; h is rounded to
 // bf16 first, because that is the stream that is stored and normalised again by the backward pass.
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -863,6 +864,8 @@ join_weight_grad_kernel(const float* partial, float* out, int32_t rows, int32_t 
 // Entries that a row of `dim` columns takes in shared memory when it begins anywhere.
 int64_t window_of(int64_t dim) { return (dim + 7 + 7) / 8 * 8; }
 
+constexpr int kMostRingBytes = 220000;       // of an SM's 227 KB: the kernel's static shared memory and what the system takes of every CTA beside it
+
 struct GradSpread {
     int lanes, n;
     bool split;
@@ -893,13 +896,13 @@ GradSpread grad_spread_of(int64_t dim, int w, bool res)
         g.n = !g.split ? 4 : dim <= 8192 ? 8 : 16;
         g.lanes = !g.split ? 32 : (int)((dim + g.n * 64 - 1) / (g.n * 64)) * 32;
         const int64_t row = arrays * window_of(dim) * 2 * (g.split ? 1 : 256 / g.lanes);
-        g.stages = g.n <= 8 ? (4 * row <= 110000 ? 4 : 2) : 2 * row <= 220000 ? 2 : 1;
+        g.stages = g.n <= 8 ? (4 * row <= kMostRingBytes / 2 ? 4 : 2) : 2 * row <= kMostRingBytes ? 2 : 1;
         g.bytes = g.stages * row;
     }
     const int64_t sums = g.split ? 0 : 4 * dim * (256 / g.lanes);
     if (g.bytes < sums) g.bytes = sums;
     const int threads = g.split ? g.lanes : 256;
-    g.held = (int)(220000 / (g.bytes + 2048));
+    g.held = (int)(kMostRingBytes / (g.bytes + 2048));
     const int by_registers = g.split && w == 8 && units > 512 && units <= 1024 ? 2 : threads <= 512 ? 512 / threads : 1;
     if (g.held > by_registers) g.held = by_registers;
     if (g.held < 1) g.held = 1;
@@ -939,7 +942,15 @@ template <int W, int N, int STAGES, bool SPLIT, bool RES, class WT>
 int launch_grad(const NormGradArgs& a, const GradSpread& g, unsigned ctas, cudaStream_t stream)
 {
     const auto kernel = rms_norm_grad_kernel<W, N, STAGES, SPLIT, RES, WT>;
-    if (g.bytes > 40960) CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)g.bytes));
+    // Once per kernel and device, and for every width at a time: the limit belongs to the kernel, so that a smaller one set by another thread would
+    // refuse this one's launch.
+    static std::atomic<uint64_t> allowed{0};
+    int device = 0;
+    CAST_CUDA_TRY(cudaGetDevice(&device));
+    if (device >= 64 || !(allowed.load(std::memory_order_relaxed) >> device & 1u)) {
+        CAST_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostRingBytes));
+        if (device < 64) allowed.fetch_or(1ull << device, std::memory_order_relaxed);
+    }
     return launch_chained(true, kernel, dim3(ctas), SPLIT ? (unsigned)a.lanes : 256u, (size_t)g.bytes, stream, 1, a);
 }
 

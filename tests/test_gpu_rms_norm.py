@@ -393,3 +393,37 @@ def test_8_bit_values_are_exact_where_roundings_of_the_sum_point_one_way(dim):
         w = weights(dim, True, 100 + seed)
         q, s, _ = ops.rms_norm_mx(h, w, None, eps)
         check_mx_exact(q, s, h, w, eps)
+
+
+def test_calls_from_two_threads_at_once():
+    """Widths that take one kernel with different amounts of shared memory, each from a thread of its own: no call is refused."""
+    import threading
+    tokens, calls = 8, 3000
+    jobs = []
+    for dim in (2560, 4096):
+        dy, h, dh, w = draw((tokens, dim), dim), draw((tokens, dim), dim + 1), draw((tokens, dim), dim + 2), weights(dim, True)
+        want = ops.rms_norm_grad(dy, h, w, dh)
+        rc, need = cast.cast_rms_norm_grad_workspace(tokens, dim)
+        cast.check(rc)
+        got = torch.empty_like(h), torch.empty(dim, device=DEV), torch.empty(need, dtype=torch.uint8, device=DEV)
+        jobs.append((dim, (dy, h, w, dh), want, got, need, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    refused = []
+
+    def run(job):
+        dim, (dy, h, w, dh), _, (dx, dw, ws), need, stream = job
+        call = B.load_library().cast_rms_norm_grad
+        args = (dy.data_ptr(), h.data_ptr(), w.data_ptr(), 1, dh.data_ptr(), dx.data_ptr(), dw.data_ptr(), tokens, dim, 1e-6, ws.data_ptr(), need, stream.cuda_stream)
+        for _ in range(calls):
+            rc = call(*args)
+            if rc != B.CAST_OK:
+                refused.append((dim, rc))
+    threads = [threading.Thread(target=run, args=(job,)) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not refused, (len(refused), refused[0])
+    for _, _, want, got, _, _ in jobs:
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
