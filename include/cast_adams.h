@@ -627,7 +627,8 @@ CAST_API int cast_rotary(const cast_heads_t* sets, int n_sets, const int32_t* po
  *              all of them: a set for norms alone.  No result may overlap another one or another tensor's gradient.
  *   scale      finite: what every gradient is multiplied by (1 / accumulated micro-batches); it counts in the norm.
  *   max_norm   >= 0; infinity only scales.  A norm that is not a number makes every result NaN; an infinite one makes the finite ones 0.
- *   norm       device, fp32, out: the norm before clipping.
+ *   norm       device, fp32, out: the norm before clipping.  Neither norm nor workspace may lie in a gradient of the set, nor in a result of a
+ *              call that writes those.
  * The factor is formed on the device; nothing is synchronised.  A tensor that keeps its place is not written where the factor is 1.
  * Squares are summed in fp32 over 32 entries at most and in fp64 beyond.  The workspace (cast_grads_workspace) depends on the device; create and all
  * calls belong to the same current device.

@@ -41,10 +41,13 @@ struct TensorTable {
     uint32_t n;
 };
 
+struct Span { uintptr_t lo, hi; };
+
 struct GradSet {
     uint64_t magic;
     int device;
     bool outs;                                             // every tensor has a place for its result
+    std::vector<Span> grads_at, outs_at;                   // where they lie, in the order of addresses and apart
     bool small;                                            // one table of few tensors
     TensorTable<kFewTensors> few;
     std::vector<TensorTable<kMostTensors>> tables;
@@ -271,7 +274,26 @@ int set_device(const GradSet& s, int* sms, int* n_sums)
     return CAST_OK;
 }
 
-int check_call(GradSet* s, float scale, const float* norm, const void* workspace, uint64_t workspace_bytes, int* sms, int* n_sums)
+// Ranges in the order of their addresses, those that meet as one.
+void join_spans(std::vector<Span>* spans)
+{
+    std::sort(spans->begin(), spans->end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
+    size_t n = 0;
+    for (const Span& x : *spans) {
+        if (n && x.lo <= (*spans)[n - 1].hi) (*spans)[n - 1].hi = std::max((*spans)[n - 1].hi, x.hi);
+        else (*spans)[n++] = x;
+    }
+    spans->resize(n);
+}
+
+bool lies_in(const std::vector<Span>& spans, const void* p, uint64_t bytes)
+{
+    const uintptr_t lo = (uintptr_t)p, hi = lo + bytes;
+    const auto behind = std::lower_bound(spans.begin(), spans.end(), hi, [](const Span& a, uintptr_t at) { return a.lo < at; });
+    return behind != spans.begin() && (behind - 1)->hi > lo;
+}
+
+int check_call(GradSet* s, bool clip, float scale, const float* norm, const void* workspace, uint64_t workspace_bytes, int* sms, int* n_sums)
 {
     if (!s) return CAST_ERR_PLAN;
     if (!norm || !workspace) return CAST_ERR_NULL;
@@ -281,7 +303,8 @@ int check_call(GradSet* s, float scale, const float* norm, const void* workspace
     if ((rc = set_device(*s, sms, n_sums)) != CAST_OK) return rc;
     const uint64_t need = sizeof(double) * (uint64_t)*n_sums;
     if (workspace_bytes < need) return CAST_ERR_PLAN;
-    if (ranges_overlap(norm, 4, workspace, need)) return CAST_ERR_ALIAS;
+    if (ranges_overlap(norm, 4, workspace, need) || lies_in(s->grads_at, norm, 4) || lies_in(s->grads_at, workspace, need)) return CAST_ERR_ALIAS;
+    if (clip && (lies_in(s->outs_at, norm, 4) || lies_in(s->outs_at, workspace, need))) return CAST_ERR_ALIAS;
     const void* ptrs[2] = {norm, workspace};
     return check_device_memory(ptrs, 2);
 }
@@ -371,6 +394,9 @@ extern "C" int cast_grads_create(const cast_grad_t* grads, int n, void** set_out
         s->small = n <= kFewTensors;
         try {
             for (int i = 0; i < n; ++i) {
+                const cast_grad_t& g = grads[i];
+                s->grads_at.push_back({(uintptr_t)g.grad, (uintptr_t)g.grad + (uint64_t)g.count * (g.grad_bf16 ? 2u : 4u)});
+                if (outs) s->outs_at.push_back({(uintptr_t)g.out, (uintptr_t)g.out + (uint64_t)g.count * (g.out_bf16 ? 2u : 4u)});
                 if (s->small) {
                     add_tensor(&s->few, grads[i]);
                 } else {
@@ -378,6 +404,8 @@ extern "C" int cast_grads_create(const cast_grad_t* grads, int n, void** set_out
                     add_tensor(&s->tables.back(), grads[i]);
                 }
             }
+            join_spans(&s->grads_at);
+            join_spans(&s->outs_at);
         } catch (...) {
             delete s;
             throw;
@@ -405,7 +433,7 @@ extern "C" int cast_grads_norm(void* set, float scale, float* norm, void* worksp
 {
     GradSet* s = set_of(set);
     int sms = 0, n = 0, rc;
-    if ((rc = check_call(s, scale, norm, workspace, workspace_bytes, &sms, &n)) != CAST_OK) return rc;
+    if ((rc = check_call(s, false, scale, norm, workspace, workspace_bytes, &sms, &n)) != CAST_OK) return rc;
     double* sums = static_cast<double*>(workspace);
     if ((rc = launch_squares(*s, sums, sms, (cudaStream_t)stream)) != CAST_OK) return rc;
     return launch_chained(false, norm_kernel, dim3(1), kClipThreads, 0, (cudaStream_t)stream, 1, (const double*)sums, n, (double)scale, norm);
@@ -417,7 +445,7 @@ extern "C" int cast_grads_clip(void* set, float max_norm, float scale, float* no
     int sms = 0, n = 0, rc;
     if (s && !s->outs) return CAST_ERR_NULL;
     if (!(max_norm >= 0.0f)) return CAST_ERR_HYPER;
-    if ((rc = check_call(s, scale, norm, workspace, workspace_bytes, &sms, &n)) != CAST_OK) return rc;
+    if ((rc = check_call(s, true, scale, norm, workspace, workspace_bytes, &sms, &n)) != CAST_OK) return rc;
     double* sums = static_cast<double*>(workspace);
     const cudaStream_t st = (cudaStream_t)stream;
     if ((rc = launch_squares(*s, sums, sms, st)) != CAST_OK) return rc;

@@ -208,3 +208,44 @@ def test_gradients_of_a_plan_are_clipped_in_place_ahead_of_its_step():
     state.set_nm(1, 4)
     assert float(state.clip_gradients(norm)) < norm / 3
     state.close()
+
+
+@pytest.mark.parametrize("n", [3, 50])
+def test_norm_and_workspace_inside_the_tensors_are_refused(n):
+    """The norm and the sums would be written over entries that other threads still read."""
+    flat = torch.ones((2 * n, 4096), device=DEV)
+    before = flat.clone()
+    grads, outs = flat[:n], flat[n:]
+    norm, apart = torch.zeros(64, device=DEV), torch.zeros(1 << 16, dtype=torch.uint8, device=DEV)
+    rc, handle = cast.cast_grads_create([B.make_grad(g[16:-16], o[16:-16], 4064, False, False) for g, o in zip(grads, outs)])
+    cast.check(rc)
+    rc, need = cast.cast_grads_workspace(handle)
+    cast.check(rc)
+    stream = torch.cuda.current_stream()
+
+    def norm_call(place, ws):
+        return cast.cast_grads_norm(handle, 1.0, place, ws, need, stream)
+
+    def clip_call(place, ws):
+        return cast.cast_grads_clip(handle, 1.0, 1.0, place, ws, need, stream)
+    launched = cast.cast_kernel_launch_count()
+    for call in (norm_call, clip_call):
+        for t in (grads[0], grads[n // 2], grads[n - 1]):
+            for at in (16, 2000, 4079):
+                assert call(t[at:], apart) == B.CAST_ERR_ALIAS
+            for at in (12, 1024, 4076):              # its end in the tensor, all of it (or its beginning), its beginning
+                assert call(norm, t.data_ptr() + 4 * at) == B.CAST_ERR_ALIAS
+    for t in (outs[0], outs[n - 1]):
+        assert clip_call(t[16:], apart) == B.CAST_ERR_ALIAS and clip_call(t[4079:], apart) == B.CAST_ERR_ALIAS
+        assert clip_call(norm, t[1024:]) == B.CAST_ERR_ALIAS
+    assert cast.cast_kernel_launch_count() == launched and torch.equal(flat, before)
+    # between the tensors, and a result's place for the norm alone
+    want = math.sqrt(n * 4064)
+    for place in (grads[0][15:], grads[1], grads[n - 1][4080:], outs[0][16:]):
+        cast.check(norm_call(place, apart))
+        assert abs(float(place[0]) - want) <= NORM * want
+        place[0] = 1.0
+    for place in (outs[0][15:], outs[n - 1][4080:]):
+        cast.check(clip_call(place, apart))
+        assert abs(float(place[0]) - want) <= NORM * want
+    cast.check(cast.cast_grads_destroy(handle))
