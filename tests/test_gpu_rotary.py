@@ -237,3 +237,30 @@ def test_arrangements_drawn_at_random(seed):
         check(y, x, positions, f, axes, adjacent, inverse)
         view.fill_(7.0)
         assert bool((flat == 7.0).all())
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_inverse_takes_every_pair_back(adjacent):
+    """<turned x, g> = <x, g turned back> pair by pair, each up to the roundings of the two results: half a step of an entry, times what
+    multiplies it, is 2^-8 |pair of x| |pair of g| at most on either side (the sum of two entries' products is within the product of the pairs' lengths).  Turned
+    the wrong way, or not at all, a pair is off by the sine of its angle times those lengths: the oracle turned the wrong way fails."""
+    tokens, heads, dim = 50, 6, 96
+    sections = [10, 18, 20]
+    spectrum = ops.RotarySpectrum.of(dim, sections=sections, per_axis=True, adjacent=adjacent)
+    gen = torch.Generator().manual_seed(8)
+    positions = torch.randint(1, 300, (3, tokens), generator=gen, dtype=torch.int32).to(DEV)
+    x, g = draw((tokens, heads, dim), 9), draw((tokens, heads, dim), 10)
+    p = dim // 2
+
+    def pairs(t):
+        return t.double().view(tokens, heads, p, 2) if adjacent else t.double().view(tokens, heads, 2, p).transpose(2, 3)
+
+    def disagree(y, back):
+        off = ((pairs(y) * pairs(g)).sum(-1) - (pairs(x) * pairs(back)).sum(-1)).abs()
+        return off > (2 * 2.0 ** -8 + 2.0 ** -18) * pairs(x).norm(dim=-1) * pairs(g).norm(dim=-1) + 1e-30
+    y, _ = ops.rotary(x, None, positions, spectrum)
+    back, _ = ops.rotary(g, None, positions, spectrum, inverse=True)
+    assert not bool(disagree(y, back).any())
+    args = (positions, spectrum.frequencies.tolist(), spectrum.axes.tolist(), adjacent)
+    assert not bool(disagree(R.rotary(x.double(), *args, inverse=False), R.rotary(g.double(), *args, inverse=True)).any())
+    assert float(disagree(y, R.rotary(g.double(), *args, inverse=False)).double().mean()) > 0.4 and float(disagree(y, g).double().mean()) > 0.4
