@@ -577,7 +577,7 @@ CAST_API int cast_rms_norm_mx(const cast_bf16* x, const cast_bf16* residual, con
  *   grad_h        device, bf16 [tokens][dim], or NULL: the gradient that reaches the residual stream h from what comes after.
  *   grad_x        device, bf16 [tokens][dim], out: the gradient of h, and so of x and of residual.  May be grad_h itself.
  *   grad_weight   device, fp32 [dim], out, or NULL (no workspace is needed then).
- * The statistics are computed again from h.  grad_weight is summed in fp32 by up to a few CTAs per SM and joined in a fixed order.  The
+ * The statistics are computed again from h, in fp64 for rows as above and for rows whose sum of g h reaches 2^100.  grad_weight is summed in fp32 by up to a few CTAs per SM and joined in a fixed order.  The
  * workspace size depends on the device.
  */
 CAST_API int cast_rms_norm_grad_workspace(int64_t tokens, int64_t dim, uint64_t* bytes);

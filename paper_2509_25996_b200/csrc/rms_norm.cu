@@ -694,6 +694,9 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
     };
     // a row stays in registers between its two halves, or is read from shared memory twice
     constexpr bool KEPT = N * Q <= 8 && (!SPLIT || W == 1 || kMiddleRow<W, N, STAGES, SPLIT>);
+    // where an odd row's factor enters, by what the others' code pays for it: with g and m, or with what becomes of them (8192 x 5120: 77 and 55.5 us;
+    // 4096 x 2560: 16.4 and 16.6)
+    constexpr bool EARLY = KEPT && W == 8;
     constexpr bool WEIGHTS = N * Q <= 12;            // and the weights of a thread's columns for good
     float2 kept[WEIGHTS ? N : 1][Q];
     if constexpr (WEIGHTS) {
@@ -759,7 +762,7 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
         float r = __frsqrt_rn(mean), scaled = r;                        // n = h * scaled
         float m = s.y * a.inverse_dim * r;                              // mean(g n)
         float pre = 1.0f;
-        const bool odd = odd_row(mean);
+        const bool odd = odd_row(mean) || !(fabsf(s.y) < 0x1p100f);     // or a sum of products that may have left the range
         if (SPLIT ? odd : __any_sync(0xFFFFFFFFu, odd)) {
             const double2 own = odd_sums<W>(a.h + row * a.dim, a.dy + row * a.dim, a.weight, std::is_same<WT, float>::value, active ? a.dim : 0, a.lanes, lane);
             if constexpr (SPLIT) __syncthreads();                        // the row before may have been an odd one, too
@@ -767,10 +770,10 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             const double m64 = row_sum<SPLIT>(own.y, a.lanes, part64[1]) / (double)a.dim;
             if (odd) {
                 const double r64 = 1.0 / sqrt(s64);
-                pre = odd_factor(s64);
+                if (odd_row(mean)) pre = odd_factor(s64);
                 scaled = (float)(r64 / (double)pre);
-                r = (float)r64;
-                m = (float)(m64 * r64);
+                r = pre;                                                // 1/sqrt(mean) itself may have left the range: d times scaled, then pre
+                m = (float)(EARLY ? m64 * r64 * (double)scaled : m64 * r64);
             }
         }
 #pragma unroll
@@ -787,7 +790,10 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             }
             if (odd) {
 #pragma unroll
-                for (int j = 0; j < Q; ++j) u[e][j] = mul2(u[e][j], both(pre));
+                for (int j = 0; j < Q; ++j) {
+                    u[e][j] = mul2(u[e][j], both(pre));
+                    if (EARLY) g[e][j] = mul2(g[e][j], both(scaled));
+                }
             }
             float2 o[Q];
             if constexpr (RES) ring.get(2, i, stage, o);
@@ -795,7 +801,8 @@ rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
             for (int j = 0; j < Q; ++j) {
                 const float2 n = mul2(u[e][j], both(scaled));
                 dw[i][j] = fma2(v[e][j], n, dw[i][j]);
-                const float2 d = fma2(n, both(-m), g[e][j]);
+                float2 d = fma2(n, both(-m), g[e][j]);
+                if (!EARLY && odd) d = mul2(d, both(scaled));
                 o[j] = RES ? fma2(both(r), d, o[j]) : mul2(both(r), d);
             }
             uint16_t* to = a.dx + row * a.dim + c;

@@ -427,3 +427,28 @@ def test_calls_from_two_threads_at_once():
     assert not refused, (len(refused), refused[0])
     for _, _, want, got, _, _ in jobs:
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dim", [64, 61, 768, 2048, 4096, 4097, 8200])
+@pytest.mark.parametrize("residual", [False, True])
+def test_gradients_of_rows_and_results_near_the_ends_of_the_range(dim, residual):
+    """Results in the range of bf16 from factors near its ends: rows below its normal numbers, whose factor 1 / rms is beyond fp32; rows near its
+    largest, whose factor is below fp32's normal numbers; gradients whose products with the row are beyond fp32 although the row's squares are not."""
+    gen = torch.Generator().manual_seed(dim)
+    tokens, rows, grads = 12, [], []
+    for size, grad in ((2.0 ** -127, 2.0 ** -40), (2.0 ** 124, 2.0 ** 100), (2.0 ** 40, 2.0 ** 95), (2.0 ** 49, 2.0 ** 110), (1.0, 1.0), (2.0 ** -60, 2.0 ** -60)):
+        for _ in range(2):
+            rows.append(torch.randn(dim, generator=gen, dtype=torch.float64).clamp(-3.9, 3.9) * size)
+            grads.append(torch.randn(dim, generator=gen, dtype=torch.float64).clamp(-3.9, 3.9) * grad)
+    h, dy = torch.stack(rows).to(torch.bfloat16).to(DEV), torch.stack(grads).to(torch.bfloat16).to(DEV)
+    assert h.shape[0] == tokens and bool(h.isfinite().all()) and bool(dy.isfinite().all())
+    w = weights(dim, True)
+    for t in range(tokens):
+        one, grad = h[t:t + 1].contiguous(), dy[t:t + 1].contiguous()
+        want, want_w = R.norm_grad(grad.double(), one.double(), w.double(), None, 0.0)
+        dh = (want * 0.5).to(torch.bfloat16) if residual else None
+        assert bool((want.abs() < 2.0 ** 126).all())
+        dx, dw = ops.rms_norm_grad(grad, one, w, dh, 0.0)
+        check_grad(dx, dw, grad, one, w, dh, 0.0)
+    dx, dw = ops.rms_norm_grad(dy, h, w, None, 0.0)
+    check_grad(dx, dw, dy, h, w, None, 0.0)
