@@ -5,7 +5,7 @@ Plumbing only, like `runner`: the functions check their tensors, allocate result
 current stream, so the caching allocator keeps the workspace until the work is done) and make one call of the library.
 They raise ValueError for tensors the library cannot take as they are (nothing is copied or converted behind the
 caller's back) and CastError for a refused call.  The results carry no autograd graph: a tensor that requires a gradient is
-refused while torch records one, not dropped from it silently.
+refused while torch records one, and a dual tensor of forward-mode differentiation, not dropped from it silently.
 """
 from __future__ import annotations
 
@@ -15,13 +15,22 @@ import struct
 from typing import List, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
 
-def _need(t: torch.Tensor, name: str, dtype, dims: int, device=None) -> None:
-    if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+def _refuse_derivatives(t: torch.Tensor, name: str) -> None:
+    """A tensor through which torch follows derivatives, which the results would drop."""
+    if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name}: requires a gradient, but results carry no autograd graph (call under torch.no_grad(), or pass it detached)")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name}: has a forward-mode tangent, but results carry none (pass forward_ad.unpack_dual(...).primal)")
+
+
+def _need(t: torch.Tensor, name: str, dtype, dims: int, device=None) -> None:
+    if isinstance(t, torch.Tensor):
+        _refuse_derivatives(t, name)
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed")
     if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
@@ -72,7 +81,8 @@ def _call(index: int, function, *args) -> None:
 
 def _taken(t, dtype, index: int) -> bool:
     """The usual case of what _need() asks for, decided in a microsecond less; where this is False, _need() says why or lets it pass."""
-    return type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index and t.is_contiguous() and not t.requires_grad
+    return type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index and t.is_contiguous() and not t.requires_grad and \
+        forward_ad._current_level < 0
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -355,8 +365,7 @@ def _need_heads(t: torch.Tensor, name: str, index: int, tokens: int, heads: Opti
     """(heads, token stride, head stride) of an array of heads."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name}: requires a gradient, but results carry no autograd graph (call under torch.no_grad(), or pass it detached)")
+    _refuse_derivatives(t, name)
     if t.dtype is not torch.bfloat16:
         raise ValueError(f"{name}: {t.dtype} is not {torch.bfloat16}")
     if t.get_device() != index:

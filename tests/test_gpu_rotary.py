@@ -264,3 +264,18 @@ def test_inverse_takes_every_pair_back(adjacent):
     args = (positions, spectrum.frequencies.tolist(), spectrum.axes.tolist(), adjacent)
     assert not bool(disagree(R.rotary(x.double(), *args, inverse=False), R.rotary(g.double(), *args, inverse=True)).any())
     assert float(disagree(y, R.rotary(g.double(), *args, inverse=False)).double().mean()) > 0.4 and float(disagree(y, g).double().mean()) > 0.4
+
+
+def test_a_dual_tensor_is_refused():
+    from torch.autograd import forward_ad
+    spectrum = ops.RotarySpectrum.of(64)
+    q, positions = draw((10, 4, 64), 21), torch.arange(10, dtype=torch.int32, device=DEV)
+    want, _ = ops.rotary(q, q, positions, spectrum)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(q, torch.ones_like(q))
+        for bad in ((dual, None), (q, dual)):
+            with pytest.raises(ValueError, match="forward-mode tangent"):
+                ops.rotary(*bad, positions, spectrum)
+        with pytest.raises(ValueError, match="forward-mode tangent"):
+            ops.rms_norm(q, torch.ones(64, device=DEV), residual=dual)
+        assert torch.equal(ops.rotary(q, q, positions, spectrum)[1], want)

@@ -237,3 +237,17 @@ def test_reference_of_8_bit_values():
     mid = (grid[1:] + grid[:-1]) / 2
     assert torch.equal(R.to_e4m3(mid), torch.where(bits[:-1] % 2 == 0, grid[:-1], grid[1:]))
     assert torch.equal(R.to_e4m3(mid * (1 + 1e-9)), grid[1:]) and torch.equal(R.to_e4m3(mid * (1 - 1e-9)), grid[:-1])
+
+
+def test_torch_level_calls_do_not_drop_a_tangent():
+    from torch.autograd import forward_ad
+    w, ids = torch.ones(8), torch.zeros(4, dtype=torch.int32)
+    with forward_ad.dual_level():
+        x = forward_ad.make_dual(torch.zeros((4, 8), dtype=torch.bfloat16), torch.ones((4, 8), dtype=torch.bfloat16))
+        for call in calls(x, w, ids) + (lambda: ops.embed(x, ids), lambda: ops.linear_ce(x, x, ids), lambda: ops.orthogonalize([x])):
+            with pytest.raises(ValueError, match="forward-mode tangent"):
+                call()
+        plain = forward_ad.unpack_dual(x).primal
+        for call in calls(plain, w, ids):
+            with pytest.raises(ValueError, match="CUDA tensor"):
+                call()
