@@ -134,13 +134,16 @@ class DeviceModelState:
         else:
             B.check(B.cast_plan_step(self.plan, h, flips, s))
 
-    def clip_gradients(self, max_norm: float, scale: float = 1.0) -> torch.Tensor:
+    def clip_gradients(self, max_norm: float, scale: float = 1.0, stream=None) -> torch.Tensor:
         """Multiplies the gradients of every matrix in place by scale, and by max_norm / norm where their common norm is larger than
-        max_norm; returns the norm (fp32 on the device, before clipping).  On the current stream, ahead of the step.  Gradients that are clipped together
-        with those of other states or tensors take an ops.GradientSet of all of them."""
+        max_norm; returns the norm (fp32 on the device, before clipping).  Asynchronous on `stream` or the current stream, ahead of the step there; the norm
+        belongs to that stream.  Gradients that are clipped together with those of other states or tensors take an ops.GradientSet of all of them."""
         if self._gradients is None:
             self._gradients = ops.GradientSet([m.g for m in self.mats])
-        return self._gradients.clip(max_norm, scale)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.device)
+        with torch.cuda.stream(stream):
+            return self._gradients.clip(max_norm, scale)
 
     def read_stats(self) -> "B.cast_mask_stats_t":
         """Host copy of the statistics accumulator (synchronises)."""

@@ -249,3 +249,26 @@ def test_norm_and_workspace_inside_the_tensors_are_refused(n):
         cast.check(clip_call(place, apart))
         assert abs(float(place[0]) - want) <= NORM * want
     cast.check(cast.cast_grads_destroy(handle))
+
+
+def test_gradients_of_a_plan_are_clipped_on_the_stream_of_its_step():
+    """The clipping waits behind what its stream holds, like the step behind it; nothing of it is on the current stream."""
+    from paper_2509_25996_b200 import runner
+    state = runner.DeviceModelState([(96, 64), (32, 128)], seed=1, device=DEV)
+    before = [m.g.clone() for m in state.mats]
+    norm = exact_norm(before, 1.0)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        for m, g in zip(state.mats, before):
+            m.g.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)          # some 10 ms
+            for m, g in zip(state.mats, before):
+                m.g.copy_(g)
+        got = state.clip_gradients(norm / 4, stream=stream)
+        state.step(runner.Hyper(), B.CAST_F_RESELECT, stream=stream)
+        side.synchronize()
+        check(got, [m.g for m in state.mats], before, float(torch.tensor(norm / 4, dtype=torch.float32)), 1.0)
+    state.close()
