@@ -559,9 +559,10 @@ CAST_API int cast_product_failures(unsigned long long* count_out, int action);
  *
  *   q          device, e4m3 [tokens][dim], out: y / scale of its group, rounded to nearest even.  Values and scales that fp32 puts nearer to a
  *              border than its roundings can be off are decided in fp64: they are those of the exact norm of h wherever weight h stays in the
- *              normal range of fp32 (a value below 2^-6 of its scale may be one step off).
+ *              normal range of fp32 (a value below 2^-6 times its scale may be one step off).
  *   q_scales   device, e8m0 [tokens][(dim + 31) / 32], out: exponent + 127 of the least power of two with max|y| <= 448 scale; 0 (2^-127) for
- *              a group of zeros; 255 (NaN) where an entry is not finite, the whole group's q are then NaN, too.
+ *              a group of zeros; 255 (NaN) where an entry is not finite, the whole group's q are then NaN, too.  Row-major, not in the
+ *              interleaved blocks that a tensor-core operand has.
  */
 CAST_API int cast_rms_norm(const cast_bf16* x, const cast_bf16* residual, const void* weight, int weight_fp32, cast_bf16* y, cast_bf16* h,
                   int64_t tokens, int64_t dim, float eps, cast_stream_t stream);
@@ -577,8 +578,8 @@ CAST_API int cast_rms_norm_mx(const cast_bf16* x, const cast_bf16* residual, con
  *   grad_h        device, bf16 [tokens][dim], or NULL: the gradient that reaches the residual stream h from what comes after.
  *   grad_x        device, bf16 [tokens][dim], out: the gradient of h, and so of x and of residual.  May be grad_h itself.
  *   grad_weight   device, fp32 [dim], out, or NULL (no workspace is needed then).
- * The statistics are computed again from h, in fp64 for rows as above and for rows whose sum of g h reaches 2^100.  grad_weight is summed in fp32 by up to a few CTAs per SM and joined in a fixed order.  The
- * workspace size depends on the device.
+ * The statistics are computed again from h, in fp64 for rows as above and for rows whose sum of g h reaches 2^100.  grad_weight is summed in
+ * fp32 by up to a few CTAs per SM and joined in a fixed order.  The workspace size depends on the device.
  */
 CAST_API int cast_rms_norm_grad_workspace(int64_t tokens, int64_t dim, uint64_t* bytes);
 CAST_API int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, const void* weight, int weight_fp32, const cast_bf16* grad_h,
@@ -595,12 +596,12 @@ CAST_API int cast_rms_norm_grad(const cast_bf16* grad_y, const cast_bf16* h, con
  * way: the gradient.
  *
  *   sets          host array of n_sets (1 to 4) arrays of heads, e.g. queries and keys (cast_heads_t: bf16, strides in entries, below 2^31, the
- *                 columns of a head contiguous; tokens and heads in either order; an input may be broadcast by a stride of 0).  out may be in itself
- *                 with the same strides, and sets may lie side by side in the rows of one fused array; otherwise no result may overlap
- *                 an input or another result.
+ *                 columns of a head contiguous; tokens and heads in either order; an input may be broadcast by a stride of 0; sequences whose
+ *                 tokens do not all lie one stride apart take a call each).  out may be in itself with the same strides, and sets may lie side by side
+ *                 in the rows of one fused array; otherwise no result may overlap an input or another result.
  *   positions     device, int32 [n_axes][tokens], any value.
  *   frequencies   device, fp64 [pairs]: radians per position.
- *   axes          device, int32 [pairs], or NULL for axis 0; a pair of an axis outside [0, n_axes) does not turn.
+ *   axes          device, int32 [pairs], or NULL for axis 0 (n_axes 1 only); a pair of an axis outside [0, n_axes) does not turn.
  *   n_axes in [1, 64]; pairs in [1, 512]; 2 * pairs <= head_dim <= 1024; at most 65536 heads in all sets.
  * Multiples of 8 columns (halves: of 8 pairs) and of 8 in the strides with 16-byte aligned buffers take the vector path.  Angles are formed
  * and reduced in fp64, cosines, sines and products are fp32; results are rounded once.

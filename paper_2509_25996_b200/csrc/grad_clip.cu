@@ -3,9 +3,9 @@
 //
 // A set of tensors is worked on as one list of tiles of kTile entries; its table travels in kernel parameter space.  One kernel walks over
 // the tiles and leaves one fp64 sum per CTA; a second adds those sums, in every CTA and in the same order, and scales the tiles, the last
-// ones first: what the first kernel read last is still in L2.  Bounded by HBM: in + out, and in once more beyond L2, because the factor needs
-// every gradient first.  A set that keeps its place (out = in, no conversion, factor 1) is not written.  fp32 to bf16: 124 M gradients 170 us
-// (1.24 GB moved, 7.3 TB/s with what L2 keeps), 1.62 G 2.45 ms (16.2 GB, 6.6 TB/s); bf16 to bf16: 3.37 G 3.20 ms (20.2 GB, 6.3 TB/s).
+// ones first: part of what the first kernel read last is still in L2 (30 M fp32 gradients to bf16 45.9 us, the other way round 49.5).  Bounded by HBM: in + out, and in once more beyond L2, because the factor needs
+// every gradient first.  A set that keeps its place (out = in, no conversion, factor 1) is not written.  fp32 to bf16: 109 M gradients 170 us
+// (1.09 GB moved, 6.4 TB/s), 1.62 G 2.45 ms (16.2 GB, 6.6 TB/s); bf16 to bf16: 3.37 G 3.20 ms (20.2 GB, 6.3 TB/s).
 //
 // Squares are summed in fp32 over the 32 entries that a thread takes of a tile, and in fp64 beyond; entries whose squares leave the range of fp32
 // are squared in fp64.  The factor is formed in fp64; an entry is multiplied by it in fp32 and rounded once.  The sums' order depends
@@ -24,7 +24,7 @@ namespace {
 
 constexpr int kTile = 8192;
 constexpr int kClipThreads = 256;
-constexpr int kPerSm = 4;                 // CTAs
+constexpr int kPerSm = 4;                 // CTAs; their 64 registers leave clip_kernel 416 bytes of spilled stores, which its wait for HBM covers
 constexpr int kMostTensors = 1024;        // of a launch
 constexpr int kFewTensors = 32;
 constexpr uint64_t kSetMagic = 0x4752414453455431ull;

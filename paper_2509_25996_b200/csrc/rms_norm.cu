@@ -489,6 +489,7 @@ Spread spread_of(int64_t units, int w, bool res, bool mx)
         const int n = units <= 256 ? (plain ? 1 : 2) : !plain ? 4 : units <= 512 ? 2 : units <= 768 ? 3 : 4;
         return {(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true};
     }
+    // single columns: 32 of them spill up to 576 bytes at the 64 registers of 1024 threads; rows beyond 8192 columns take them only off the 16-byte grid
     if (units <= 256) return {32, 8, false};
     const int n = units <= 8192 ? 8 : 32;
     return {(int)((units + n * 32 - 1) / (n * 32)) * 32, n, true};

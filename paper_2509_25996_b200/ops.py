@@ -235,7 +235,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
 
 def rms_norm_mx(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
                 sum_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
-    """(q, scales, h): rms_norm with y as float8_e4m3fn values and a power of two (float8_e8m0fnu) for every 32 columns."""
+    """(q, scales, h): rms_norm with y as float8_e4m3fn values and a power of two (float8_e8m0fnu) for every 32 columns, row-major."""
     tokens, dim, index = _rows(x, weight, "x", (residual, "residual"), (sum_out, "sum_out"))
     if residual is None and sum_out is not None:
         raise ValueError("sum_out needs a residual")
